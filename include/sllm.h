@@ -3,7 +3,9 @@
  *
  * The library converts a tensor checkpoint into a loading-optimized format
  * and streams it from pinned host DRAM into one preallocated HBM buffer
- * (ServerlessLLM, Sec. 4, fast multi-tier checkpoint loading).
+ * (ServerlessLLM, Sec. 4, fast multi-tier checkpoint loading).  Operators on
+ * the loaded weights (4-bit matrices and products with them, embeddings) stand
+ * at the end.
  *
  * Format (Sec. 4.1).  A checkpoint directory holds two files:
  *   sllm.part0  the partition for one GPU: the tensors' bytes only, in the
@@ -474,6 +476,120 @@ int32_t sllm_estimator_bandwidth(const sllm_estimator* e, uint32_t tier, double*
  * reads may be reused as soon as it returns.  NULL is a no-op.
  * Errors: BUSY (a load is running on the handle). */
 int32_t sllm_close(sllm_ckpt* h);
+
+/* =========================================================================
+ * Operators on loaded weights: matrices held in microscaled 4-bit floating
+ * point (MX FP4), products with them, and token embeddings
+ *
+ * Every operator is enqueued on `stream` and returns without waiting; it
+ * allocates nothing (a workspace, where one is needed, is the caller's) and may
+ * be captured into a HIP graph.  Two calls may overlap if neither writes what
+ * the other uses, workspaces included.  The same inputs give the same bytes.
+ *
+ * Buffers are memory of HIP device `device`, each inside one allocation.  An
+ * output overlaps no other buffer of its call.  A buffer of no bytes may be
+ * NULL.  Sums are held in 32-bit floats and rounded once, to nearest even, to
+ * the output's type.
+ *
+ * Errors of all of them: INVAL (NULL or inconsistent argument, a dtype other
+ * than F32, F16 and BF16, sizes that do not fit together, a pointer that is
+ * not aligned, not device memory or overlaps), RANGE (a buffer that runs past
+ * the end of its allocation, a workspace too small, rows or columns of more
+ * than SLLM_MAX_EXTENT), HIP.
+ * ========================================================================= */
+
+#define SLLM_MAX_EXTENT 0x7fff0000ull
+
+/* A matrix in device memory, aligned to its element type: row r starts at
+ * data + r * stride elements and its elements are adjacent. */
+typedef struct sllm_matrix {
+    void*    data;
+    uint64_t rows;
+    uint64_t cols;
+    uint64_t stride;    /* elements, >= cols (any value for one row or none) */
+    uint32_t dtype;     /* SLLM_DTYPE_F32, _F16 or _BF16 */
+    uint32_t reserved;  /* must be 0 */
+} sllm_matrix;
+
+/* A matrix in MX FP4 (the OCP Microscaling formats' MXFP4): each row is cut
+ * into blocks of 32 columns, the last one padded with zeros, and a block is one
+ * E8M0 scale s (2^(s - 127); 255 makes the whole block NaN) and 32 E2M1 codes
+ * (sign bit and 0, 0.5, 1, 1.5, 2, 3, 4, 6).  With blocks = ceil(cols / 32):
+ *   codes   rows * blocks * 16 bytes; a block's column 2 i is the low half of
+ *           its byte i and column 2 i + 1 the high half
+ *   scales  rows * align_up(blocks, 16) bytes, the bytes past a row's blocks
+ *           zero
+ * Both are 16-byte aligned.  Rows are adjacent, so a run of rows is such a
+ * matrix too. */
+typedef struct sllm_mx {
+    void*    codes;
+    void*    scales;
+    uint64_t rows;
+    uint64_t cols;
+} sllm_mx;
+
+/* Token ids in device memory.  An id outside [0, table rows) names no row. */
+typedef struct sllm_ids {
+    const void* data;
+    uint64_t    n;
+    uint32_t    bits;      /* 32 or 64: signed, aligned to their size */
+    uint32_t    reserved;  /* must be 0 */
+} sllm_ids;
+
+/* Bytes of the two buffers of a rows x cols matrix in MX FP4.  Host-only.
+ * Errors: INVAL, RANGE. */
+int32_t sllm_mx_sizes(uint64_t rows, uint64_t cols, uint64_t* codes_bytes, uint64_t* scales_bytes);
+
+/* dst = src in MX FP4.  A block's scale is 2^(floor(log2 a) - 2), a its largest
+ * magnitude, at least 2^-127 (and 2^-127 where a = 0); its elements divided by
+ * the scale go to the nearest E2M1 value, ties to the even code, magnitudes
+ * above 6 to 6.  A block with an infinity or a NaN gets scale 255 and codes 0. */
+int32_t sllm_mx_quantize(const sllm_matrix* src, const sllm_mx* dst, int32_t device, void* stream);
+
+/* dst = the values src stands for, rounded to dst's type. */
+int32_t sllm_mx_dequantize(const sllm_mx* src, const sllm_matrix* dst, int32_t device, void* stream);
+
+/* out = x * transpose(w): x has m rows of k elements, w is n x k, out m x n.
+ * The products of x's elements, in their own type, with the values w stands
+ * for are not rounded before they are summed. */
+int32_t sllm_mx_linear(const sllm_matrix* x, const sllm_mx* w, const sllm_matrix* out, void* workspace,
+                       uint64_t workspace_bytes, int32_t device, void* stream);
+
+/* The same with x in MX FP4 too. */
+int32_t sllm_mx_linear_mx(const sllm_mx* x, const sllm_mx* w, const sllm_matrix* out, void* workspace,
+                          uint64_t workspace_bytes, int32_t device, void* stream);
+
+/* dx = dy * w, the gradient of sllm_mx_linear by x: dy has m rows of n
+ * elements, w is n x k, dx m x k. */
+int32_t sllm_mx_linear_grad(const sllm_matrix* dy, const sllm_mx* w, const sllm_matrix* dx, void* workspace,
+                            uint64_t workspace_bytes, int32_t device, void* stream);
+
+/* Workspace each of the three needs for these operands (their data pointers'
+ * alignment counts, the memory is not read); 0 means none, and workspace may
+ * then be NULL.  A workspace is 16-byte aligned; its contents do not matter and
+ * are overwritten.  Host-only. */
+int32_t sllm_mx_linear_workspace(const sllm_matrix* x, const sllm_mx* w, uint64_t* bytes);
+int32_t sllm_mx_linear_mx_workspace(const sllm_mx* x, const sllm_mx* w, uint64_t* bytes);
+int32_t sllm_mx_linear_grad_workspace(const sllm_matrix* dy, const sllm_mx* w, uint64_t* bytes);
+
+/* out's row i = scale * row ids[i] of table, zeros where ids[i] names no row. */
+int32_t sllm_embedding(const sllm_matrix* table, const sllm_ids* ids, float scale, const sllm_matrix* out,
+                       int32_t device, void* stream);
+
+/* The same from a table in MX FP4. */
+int32_t sllm_embedding_mx(const sllm_mx* table, const sllm_ids* ids, float scale, const sllm_matrix* out,
+                          int32_t device, void* stream);
+
+#define SLLM_GRAD_ACCUMULATE 1u  /* add to grad instead of replacing it */
+
+/* The gradient of a lookup by its table: grad's row v = scale * the sum, in the
+ * order of positions, of dy's rows i with ids[i] = v; zeros where there are
+ * none.  With SLLM_GRAD_ACCUMULATE that is added to what grad holds, in 32 bits,
+ * and rows no id names are not touched.  At most 2^24 ids (RANGE). */
+int32_t sllm_embedding_grad(const sllm_matrix* dy, const sllm_ids* ids, float scale, uint32_t flags,
+                            const sllm_matrix* grad, void* workspace, uint64_t workspace_bytes, int32_t device,
+                            void* stream);
+int32_t sllm_embedding_grad_workspace(uint64_t n_ids, const sllm_matrix* grad, uint64_t* bytes);
 
 /* Message of the last failed call on this thread ("" if none). */
 const char* sllm_last_error(void);

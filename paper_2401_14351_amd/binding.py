@@ -89,6 +89,22 @@ class IpcDesc(C.Structure):
                 ("bytes", C.c_uint64), ("device", C.c_int32), ("flags", C.c_uint32)]
 
 
+class Matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64), ("stride", C.c_uint64),
+                ("dtype", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class Mx(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64)]
+
+
+class Ids(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("n", C.c_uint64), ("bits", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+_MATRIX, _MX, _IDS, _U64 = C.POINTER(Matrix), C.POINTER(Mx), C.POINTER(Ids), C.POINTER(C.c_uint64)
+_WORK = [C.c_void_p, C.c_uint64, C.c_int32, C.c_void_p]  # workspace, its bytes, device, stream
+
 # name -> (restype, argtypes); every symbol the header declares
 SIGNATURES = {
     "sllm_convert": (C.c_int32, [C.POINTER(SrcTensor), C.c_uint64, C.c_char_p, C.POINTER(ConvertOpts)]),
@@ -126,6 +142,19 @@ SIGNATURES = {
     "sllm_estimator_complete": (C.c_int32, [C.c_void_p, C.c_uint64, C.c_double]),
     "sllm_estimator_complete_load": (C.c_int32, [C.c_void_p, C.c_uint64, C.c_void_p]),
     "sllm_estimator_bandwidth": (C.c_int32, [C.c_void_p, C.c_uint32, C.POINTER(C.c_double)]),
+    "sllm_mx_sizes": (C.c_int32, [C.c_uint64, C.c_uint64, _U64, _U64]),
+    "sllm_mx_quantize": (C.c_int32, [_MATRIX, _MX, C.c_int32, C.c_void_p]),
+    "sllm_mx_dequantize": (C.c_int32, [_MX, _MATRIX, C.c_int32, C.c_void_p]),
+    "sllm_mx_linear": (C.c_int32, [_MATRIX, _MX, _MATRIX, *_WORK]),
+    "sllm_mx_linear_mx": (C.c_int32, [_MX, _MX, _MATRIX, *_WORK]),
+    "sllm_mx_linear_grad": (C.c_int32, [_MATRIX, _MX, _MATRIX, *_WORK]),
+    "sllm_mx_linear_workspace": (C.c_int32, [_MATRIX, _MX, _U64]),
+    "sllm_mx_linear_mx_workspace": (C.c_int32, [_MX, _MX, _U64]),
+    "sllm_mx_linear_grad_workspace": (C.c_int32, [_MATRIX, _MX, _U64]),
+    "sllm_embedding": (C.c_int32, [_MATRIX, _IDS, C.c_float, _MATRIX, C.c_int32, C.c_void_p]),
+    "sllm_embedding_mx": (C.c_int32, [_MX, _IDS, C.c_float, _MATRIX, C.c_int32, C.c_void_p]),
+    "sllm_embedding_grad": (C.c_int32, [_MATRIX, _IDS, C.c_float, C.c_uint32, _MATRIX, *_WORK]),
+    "sllm_embedding_grad_workspace": (C.c_int32, [C.c_uint64, _MATRIX, _U64]),
     "sllm_last_error": (C.c_char_p, []),
     "sllm_strerror": (C.c_char_p, [C.c_int32]),
 }

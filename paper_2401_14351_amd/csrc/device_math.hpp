@@ -1,0 +1,55 @@
+// Device helpers of the operators: element types and MX FP4 values.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "operators.hpp"
+
+namespace sllm {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// An element as a 32-bit float (exact) and a float rounded to an element, to
+// nearest even, overflow to infinity.
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(_Float16 v) { return (float)v; }
+__device__ __forceinline__ float to_f32(__bf16 v) { return (float)v; }
+template <typename T>
+__device__ __forceinline__ T from_f32(float v) {
+    return (T)v;
+}
+
+// Run F<T> for the element type of a dtype code.
+#define SLLM_BY_DTYPE(dtype, T, ...)          \
+    do {                                      \
+        if ((dtype) == SLLM_DTYPE_F32) {      \
+            using T = float;                  \
+            __VA_ARGS__;                      \
+        } else if ((dtype) == SLLM_DTYPE_F16) { \
+            using T = _Float16;               \
+            __VA_ARGS__;                      \
+        } else {                              \
+            using T = __bf16;                 \
+            __VA_ARGS__;                      \
+        }                                     \
+    } while (0)
+
+// The scale operand of the conversion instructions: they take a float's
+// exponent field alone, so a scale byte goes there as it is.  0 then means
+// 2^-127 and 255 makes the results NaN, as the format has it.
+__device__ __forceinline__ float mx_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Code c of a byte (0 the low half) under a scale byte, as a 32-bit float.
+__device__ __forceinline__ float mx_value(uint32_t byte, uint32_t half, uint32_t scale) {
+    const f32x2 v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(byte, mx_scale(scale), 0);
+    return half ? v[1] : v[0];
+}
+
+}  // namespace sllm
