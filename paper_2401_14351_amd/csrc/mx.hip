@@ -5,6 +5,7 @@
 #include "device_math.hpp"
 #include "hip_util.hpp"
 #include "operators.hpp"
+#include "products.hpp"
 
 namespace sllm {
 
@@ -136,9 +137,139 @@ int32_t launch_quantize(const sllm_matrix& src, const sllm_mx& dst, hipStream_t 
     return SLLM_OK;
 }
 
-uint64_t linear_workspace(const LinearLaunch& a) { return 0; }
+namespace {
+
+// How a product is carried out, from its operands alone.
+struct Plan {
+    uint32_t parts = 1;        // bfloat16 matrices that x is the sum of
+    bool staged = false;       // x is written out as those first
+    uint64_t depth = 0, cols = 0;
+    uint64_t part_stride = 0;  // elements, of a staged x
+    uint32_t steps = 0, splits = 1;
+    uint32_t tiles_m = 0, tiles_j = 0;
+    uint64_t x_bytes = 0, split_stride = 0, bytes = 0;
+};
+
+Plan plan_linear(const LinearLaunch& a) {
+    Plan p;
+    p.depth = a.grad ? a.n : a.k;
+    p.cols = a.grad ? a.k : a.n;
+    if (a.x.codes || !p.depth || !a.m || !p.cols) return p;
+    p.parts = a.x.dtype == SLLM_DTYPE_BF16 ? 1 : a.x.dtype == SLLM_DTYPE_F16 ? 2 : 3;
+    // The kernel reads x in aligned vectors of eight.
+    p.staged = p.parts > 1 || p.depth % 8 || (a.m > 1 && a.x.stride % 8) || reinterpret_cast<uintptr_t>(a.x.data) % 16;
+    p.part_stride = (p.depth + 7) / 8 * 8;
+    p.steps = (uint32_t)ceil_div(p.depth, kWideStep);
+    p.tiles_m = (uint32_t)ceil_div(a.m, kWideTile);
+    p.tiles_j = (uint32_t)ceil_div(p.cols, kWideTile);
+    const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_j;
+    if (tiles <= 128) p.splits = (uint32_t)std::min<uint64_t>(256 / tiles, std::max<uint64_t>(1, p.steps * p.parts / 8));
+    if (p.staged) p.x_bytes = (a.m * p.parts * p.part_stride * 2 + 255) / 256 * 256;
+    p.split_stride = a.m * ((p.cols + 3) / 4 * 4);
+    p.bytes = p.x_bytes + (p.splits > 1 ? p.splits * p.split_stride * 4 : 0);
+    return p;
+}
+
+// x as the sum of `Parts` bfloat16 matrices: its leading eight bits, the eight
+// after those, the rest.  An infinity or a NaN stays whole in the first.
+template <typename T, int Parts>
+__global__ __launch_bounds__(256) void split_x(const T* x, uint64_t stride, uint64_t rows, uint64_t cols, uint64_t pitch,
+                                               __bf16* out) {
+    const uint64_t vectors = pitch / 8, i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint64_t row = i / vectors, c = i % vectors * 8;
+    if (row >= rows) return;
+    uint16_t v[Parts][8];
+    for (uint32_t e = 0; e < 8; ++e) {
+        float f = c + e < cols ? to_f32(x[row * stride + c + e]) : 0.0f;
+        for (int p = 0; p < Parts; ++p) {
+            const uint32_t bits = __float_as_uint(f);
+            const bool finite = (bits & 0x7f800000) != 0x7f800000;
+            // a NaN whose payload is all in the lower half must not become an infinity
+            v[p][e] = finite || !(bits & 0x7fffff) ? bits >> 16 : 0x7fc0;
+            f = finite ? f - __uint_as_float(bits & 0xffff0000) : 0.0f;
+        }
+    }
+    for (int p = 0; p < Parts; ++p) {
+        u32x4 o;
+        for (int j = 0; j < 4; ++j) o[j] = v[p][2 * j] | (uint32_t)v[p][2 * j + 1] << 16;
+        *reinterpret_cast<u32x4*>(out + (row * Parts + p) * pitch + c) = o;
+    }
+}
+
+// The sum of the splits' matrices, first to last.
+template <typename T>
+__global__ __launch_bounds__(256) void join_splits(const float* in, uint32_t splits, uint64_t split_stride, uint64_t rows,
+                                                   uint64_t cols, T* out, uint64_t stride) {
+    const uint64_t vectors = (cols + 3) / 4, i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint64_t row = i / vectors, c = i % vectors * 4;
+    if (row >= rows) return;
+    f32x4 sum = {0, 0, 0, 0};
+    for (uint32_t s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(in + s * split_stride + i * 4);
+    for (uint32_t e = 0; e < 4 && c + e < cols; ++e) out[row * stride + c + e] = from_f32<T>(sum[e]);
+}
+
+int32_t grid_of(uint64_t threads, uint32_t* blocks) {
+    const uint64_t n = ceil_div(threads, 256);
+    if (n > UINT32_MAX / 256) return fail(SLLM_E_RANGE, "matrix too large");
+    *blocks = (uint32_t)n;
+    return SLLM_OK;
+}
+
+int32_t launch_wide_product(const LinearLaunch& a, const Plan& p, void* workspace, hipStream_t stream) {
+    WideArgs w;
+    w.x = static_cast<const __bf16*>(a.x.data);
+    w.m = a.m, w.depth = p.depth;
+    w.x_stride = a.x.stride, w.part_stride = 0;
+    uint32_t blocks;
+    if (p.staged) {
+        w.x = static_cast<const __bf16*>(workspace);
+        w.x_stride = p.parts * p.part_stride;
+        w.part_stride = p.part_stride;
+        __bf16* x = static_cast<__bf16*>(workspace);
+        SLLM_TRY(grid_of(a.m * p.part_stride / 8, &blocks));
+        if (p.parts == 1)
+            split_x<__bf16, 1><<<blocks, 256, 0, stream>>>(static_cast<const __bf16*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
+        else if (p.parts == 2)
+            split_x<_Float16, 2><<<blocks, 256, 0, stream>>>(static_cast<const _Float16*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
+        else
+            split_x<float, 3><<<blocks, 256, 0, stream>>>(static_cast<const float*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
+        SLLM_HIP(hipGetLastError());
+    }
+    w.parts = p.parts, w.steps = p.steps;
+    w.w_codes = reinterpret_cast<const u32x4*>(a.w_codes);
+    w.w_scales = a.w_scales;
+    w.w_rows = a.n, w.w_blocks = mx_blocks(a.k), w.w_scale_pitch = mx_scale_pitch(a.k);
+    w.tiles_m = p.tiles_m, w.tiles_j = p.tiles_j;
+    w.out_args = OutArgs{a.m, p.cols, a.out_stride, 0, 0};
+    void* out = a.out;
+    uint32_t dtype = a.out_dtype;
+    if (p.splits > 1) {
+        out = static_cast<uint8_t*>(workspace) + p.x_bytes;
+        dtype = SLLM_DTYPE_F32;
+        w.out_args.stride = (p.cols + 3) / 4 * 4;
+        w.out_args.split_stride = p.split_stride;
+    }
+    w.out_args.vector = w.out_args.stride % 4 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
+    if (a.grad)
+        SLLM_TRY(launch_wide<true>(w, p.splits, out, dtype, stream));
+    else
+        SLLM_TRY(launch_wide<false>(w, p.splits, out, dtype, stream));
+    if (p.splits > 1) {
+        SLLM_TRY(grid_of(a.m * w.out_args.stride / 4, &blocks));
+        SLLM_BY_DTYPE(a.out_dtype, T, (join_splits<T><<<blocks, 256, 0, stream>>>(static_cast<const float*>(out), p.splits, p.split_stride,
+                                                                                a.m, p.cols, static_cast<T*>(a.out), a.out_stride)));
+        SLLM_HIP(hipGetLastError());
+    }
+    return SLLM_OK;
+}
+
+}  // namespace
+
+uint64_t linear_workspace(const LinearLaunch& a) { return plan_linear(a).bytes; }
 
 int32_t launch_linear(const LinearLaunch& a, void* workspace, hipStream_t stream) {
+    const Plan plan = plan_linear(a);
+    if (!a.x.codes && plan.depth) return launch_wide_product(a, plan, workspace, stream);
     const Product p{a.x, a.w_codes, a.w_scales, a.m, a.n, a.k, a.grad ? a.n : a.k, a.out, a.out_stride, a.out_dtype};
     const uint64_t gx = ceil_div(a.grad ? a.k : a.n, 32), gy = ceil_div(a.m, 32);
     if (gx > UINT32_MAX / 256 || gy > 65535) return fail(SLLM_E_RANGE, "product too large");

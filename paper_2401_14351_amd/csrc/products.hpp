@@ -1,0 +1,61 @@
+// What the kernels of products with an MX FP4 weight share.
+#pragma once
+
+#include "device_math.hpp"
+
+namespace sllm {
+
+// Where a product's sums go: m x cols, or, where the depth is split over
+// workgroups (blockIdx.y), a 32-bit matrix per split, one after another.
+struct OutArgs {
+    uint64_t m, cols, stride;
+    uint64_t split_stride;  // elements from one split's matrix to the next
+    uint32_t vector;        // rows start on 4 elements
+};
+
+// x (m x depth, parts of it one after another along a row) in bfloat16
+struct WideArgs {
+    const __bf16* x;
+    uint64_t m, depth;       // of a part
+    uint64_t x_stride, part_stride;
+    uint32_t parts, steps;   // steps of a part
+    const u32x4* w_codes;
+    const uint8_t* w_scales;
+    uint64_t w_rows, w_blocks, w_scale_pitch;
+    uint32_t tiles_m, tiles_j;
+    OutArgs out_args;
+};
+
+// A wave's accumulators: fragment [n][m] holds, in lane (r, g), columns
+// n * 16 + 4 g .. + 3 of row m * 16 + r.
+template <int FM, int FN, typename T>
+__device__ __forceinline__ void store_tile(const f32x4 (&acc)[FN][FM], const OutArgs& o, uint64_t m0, uint64_t j0, T* out) {
+    const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    out += blockIdx.y * o.split_stride;
+#pragma unroll
+    for (int m = 0; m < FM; ++m) {
+        const uint64_t row = m0 + m * 16 + r;
+        if (row >= o.m) continue;
+        T* p = out + row * o.stride;
+#pragma unroll
+        for (int n = 0; n < FN; ++n) {
+            const uint64_t j = j0 + n * 16 + g * 4;
+            if (o.vector && j + 4 <= o.cols) {
+                typedef T T4 __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<T4*>(p + j) = T4{from_f32<T>(acc[n][m][0]), from_f32<T>(acc[n][m][1]),
+                                                   from_f32<T>(acc[n][m][2]), from_f32<T>(acc[n][m][3])};
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (j + i < o.cols) p[j + i] = from_f32<T>(acc[n][m][i]);
+            }
+        }
+    }
+}
+
+template <bool Grad>
+int32_t launch_wide(const WideArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
+constexpr uint32_t kWideTile = 256;  // rows of x and columns of the output a workgroup holds
+constexpr uint32_t kWideStep = 64;   // depth of a stage
+
+}  // namespace sllm

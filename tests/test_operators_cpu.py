@@ -217,3 +217,14 @@ def test_python_refuses():
         op.embedding_grad(torch.zeros(3, 4), torch.zeros(3, dtype=torch.int64), 8, accumulate=True)
     with pytest.raises(ValueError):
         op.embedding(torch.zeros(4, 4), torch.zeros(3))
+
+
+@pytest.mark.parametrize("m,n,k", [(0, 0, 0), (0, 8, 64), (4, 0, 64), (4, 8, 0), (1, 1, 1), (4096, 28672, 8192)])
+def test_workspaces_of_any_shape(L, m, n, k):
+    """Host-only, so empty operands are answered here too."""
+    size = C.c_uint64()
+    for dtype in (0, 1, 2):
+        assert L.sllm_mx_linear_workspace(matrix(m, k, dtype=dtype), mx(n, k), size) == 0
+        assert L.sllm_mx_linear_grad_workspace(matrix(m, n, dtype=dtype), mx(n, k), size) == 0
+        assert L.sllm_embedding_grad_workspace(m, matrix(n, k, dtype=dtype), size) == 0
+    assert L.sllm_mx_linear_mx_workspace(mx(m, k), mx(n, k), size) == 0
