@@ -12,16 +12,6 @@ namespace {
 
 constexpr uint32_t kStep = kWideStep;
 
-__device__ const u32x4 kZeros = {0, 0, 0, 0};
-
-__device__ __forceinline__ void load_to_lds(const void* from, void* to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-}
-
-// Every load of this wave has landed, those to LDS included.
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
-
 // A block of 32 codes as bfloat16: four vectors of eight.
 __device__ __forceinline__ void expand(u32x4 codes, uint32_t scale, u32x4 out[4]) {
     const float s = mx_scale(scale);
@@ -54,6 +44,7 @@ __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) 
     __shared__ __align__(16) uint8_t lds_b0[G::kBBytes], lds_b1[G::kBBytes];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t r = lane & 15, g = lane >> 4;
+    const void* const zeros = zero_vector();
     const uint64_t m0 = (uint64_t)blockIdx.x % a.tiles_m * BM, j0 = (uint64_t)blockIdx.x / a.tiles_m * BN;
     const uint32_t steps = a.steps * a.parts;
     const uint32_t t0 = (uint64_t)steps * blockIdx.y / gridDim.y, t1 = (uint64_t)steps * (blockIdx.y + 1) / gridDim.y;
@@ -73,7 +64,7 @@ __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) 
             const uint32_t at = q * G::kWaves + wave;
             const uint64_t row = min(m0 + at / 2 * 16 + r, a.m - 1), c = d + (at % 2 * 4 + g) * 8;
             const void* p = a.x + row * a.x_stride + part * a.part_stride + c;
-            load_to_lds(c < a.depth ? p : &kZeros, to + at * 1024);
+            load_to_lds(c < a.depth ? p : zeros, to + at * 1024);
         }
     };
     u32x4 codes[G::kBlocks];

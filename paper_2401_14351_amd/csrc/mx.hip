@@ -154,16 +154,18 @@ Plan plan_linear(const LinearLaunch& a) {
     Plan p;
     p.depth = a.grad ? a.n : a.k;
     p.cols = a.grad ? a.k : a.n;
-    if (a.x.codes || !p.depth || !a.m || !p.cols) return p;
-    p.parts = a.x.dtype == SLLM_DTYPE_BF16 ? 1 : a.x.dtype == SLLM_DTYPE_F16 ? 2 : 3;
+    if (!p.depth || !a.m || !p.cols) return p;
+    if (!a.x.codes) p.parts = a.x.dtype == SLLM_DTYPE_BF16 ? 1 : a.x.dtype == SLLM_DTYPE_F16 ? 2 : 3;
     // The kernel reads x in aligned vectors of eight.
-    p.staged = p.parts > 1 || p.depth % 8 || (a.m > 1 && a.x.stride % 8) || reinterpret_cast<uintptr_t>(a.x.data) % 16;
+    p.staged = !a.x.codes && (p.parts > 1 || p.depth % 8 || (a.m > 1 && a.x.stride % 8) ||
+                              reinterpret_cast<uintptr_t>(a.x.data) % 16);
     p.part_stride = (p.depth + 7) / 8 * 8;
-    p.steps = (uint32_t)ceil_div(p.depth, kWideStep);
+    const uint32_t step = a.x.codes ? kNarrowStep : kWideStep;
+    p.steps = (uint32_t)ceil_div(p.depth, step);
     p.tiles_m = (uint32_t)ceil_div(a.m, kWideTile);
     p.tiles_j = (uint32_t)ceil_div(p.cols, kWideTile);
     const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_j;
-    if (tiles <= 128) p.splits = (uint32_t)std::min<uint64_t>(256 / tiles, std::max<uint64_t>(1, p.steps * p.parts / 8));
+    if (tiles <= 128) p.splits = (uint32_t)std::min<uint64_t>(256 / tiles, std::max<uint64_t>(1, (uint64_t)p.steps * p.parts * step / 512));
     if (p.staged) p.x_bytes = (a.m * p.parts * p.part_stride * 2 + 255) / 256 * 256;
     p.split_stride = a.m * ((p.cols + 3) / 4 * 4);
     p.bytes = p.x_bytes + (p.splits > 1 ? p.splits * p.split_stride * 4 : 0);
@@ -215,47 +217,57 @@ int32_t grid_of(uint64_t threads, uint32_t* blocks) {
     return SLLM_OK;
 }
 
-int32_t launch_wide_product(const LinearLaunch& a, const Plan& p, void* workspace, hipStream_t stream) {
-    WideArgs w;
-    w.x = static_cast<const __bf16*>(a.x.data);
-    w.m = a.m, w.depth = p.depth;
-    w.x_stride = a.x.stride, w.part_stride = 0;
+// x as the wide kernel reads it, written out in the workspace where it is not so already.
+int32_t stage_x(const LinearLaunch& a, const Plan& p, void* workspace, WideArgs* w, hipStream_t stream) {
+    w->x = static_cast<const __bf16*>(a.x.data);
+    w->x_stride = a.x.stride, w->part_stride = 0;
+    if (!p.staged) return SLLM_OK;
+    __bf16* x = static_cast<__bf16*>(workspace);
+    w->x = x;
+    w->x_stride = p.parts * p.part_stride;
+    w->part_stride = p.part_stride;
     uint32_t blocks;
-    if (p.staged) {
-        w.x = static_cast<const __bf16*>(workspace);
-        w.x_stride = p.parts * p.part_stride;
-        w.part_stride = p.part_stride;
-        __bf16* x = static_cast<__bf16*>(workspace);
-        SLLM_TRY(grid_of(a.m * p.part_stride / 8, &blocks));
-        if (p.parts == 1)
-            split_x<__bf16, 1><<<blocks, 256, 0, stream>>>(static_cast<const __bf16*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
-        else if (p.parts == 2)
-            split_x<_Float16, 2><<<blocks, 256, 0, stream>>>(static_cast<const _Float16*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
-        else
-            split_x<float, 3><<<blocks, 256, 0, stream>>>(static_cast<const float*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
-        SLLM_HIP(hipGetLastError());
-    }
-    w.parts = p.parts, w.steps = p.steps;
-    w.w_codes = reinterpret_cast<const u32x4*>(a.w_codes);
-    w.w_scales = a.w_scales;
-    w.w_rows = a.n, w.w_blocks = mx_blocks(a.k), w.w_scale_pitch = mx_scale_pitch(a.k);
-    w.tiles_m = p.tiles_m, w.tiles_j = p.tiles_j;
-    w.out_args = OutArgs{a.m, p.cols, a.out_stride, 0, 0};
+    SLLM_TRY(grid_of(a.m * p.part_stride / 8, &blocks));
+    if (p.parts == 1)
+        split_x<__bf16, 1><<<blocks, 256, 0, stream>>>(static_cast<const __bf16*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
+    else if (p.parts == 2)
+        split_x<_Float16, 2><<<blocks, 256, 0, stream>>>(static_cast<const _Float16*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
+    else
+        split_x<float, 3><<<blocks, 256, 0, stream>>>(static_cast<const float*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
+    SLLM_HIP(hipGetLastError());
+    return SLLM_OK;
+}
+
+int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipStream_t stream) {
+    OutArgs o{a.m, p.cols, a.out_stride, 0, 0};
     void* out = a.out;
     uint32_t dtype = a.out_dtype;
     if (p.splits > 1) {
         out = static_cast<uint8_t*>(workspace) + p.x_bytes;
         dtype = SLLM_DTYPE_F32;
-        w.out_args.stride = (p.cols + 3) / 4 * 4;
-        w.out_args.split_stride = p.split_stride;
+        o.stride = (p.cols + 3) / 4 * 4;
+        o.split_stride = p.split_stride;
     }
-    w.out_args.vector = w.out_args.stride % 4 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
-    if (a.grad)
-        SLLM_TRY(launch_wide<true>(w, p.splits, out, dtype, stream));
-    else
-        SLLM_TRY(launch_wide<false>(w, p.splits, out, dtype, stream));
+    o.vector = o.stride % 4 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
+    if (a.x.codes) {
+        const NarrowArgs n{reinterpret_cast<const u32x4*>(a.x.codes), a.x.scales, reinterpret_cast<const u32x4*>(a.w_codes),
+                           a.w_scales, a.m, a.n, mx_blocks(a.k), mx_scale_pitch(a.k), p.steps, p.tiles_m, p.tiles_j, o};
+        SLLM_TRY(launch_narrow(n, p.splits, out, dtype, stream));
+    } else {
+        WideArgs w;
+        SLLM_TRY(stage_x(a, p, workspace, &w, stream));
+        w.m = a.m, w.depth = p.depth;
+        w.parts = p.parts, w.steps = p.steps;
+        w.w_codes = reinterpret_cast<const u32x4*>(a.w_codes);
+        w.w_scales = a.w_scales;
+        w.w_rows = a.n, w.w_blocks = mx_blocks(a.k), w.w_scale_pitch = mx_scale_pitch(a.k);
+        w.tiles_m = p.tiles_m, w.tiles_j = p.tiles_j;
+        w.out_args = o;
+        SLLM_TRY(a.grad ? launch_wide<true>(w, p.splits, out, dtype, stream) : launch_wide<false>(w, p.splits, out, dtype, stream));
+    }
     if (p.splits > 1) {
-        SLLM_TRY(grid_of(a.m * w.out_args.stride / 4, &blocks));
+        uint32_t blocks;
+        SLLM_TRY(grid_of(a.m * o.stride / 4, &blocks));
         SLLM_BY_DTYPE(a.out_dtype, T, (join_splits<T><<<blocks, 256, 0, stream>>>(static_cast<const float*>(out), p.splits, p.split_stride,
                                                                                 a.m, p.cols, static_cast<T*>(a.out), a.out_stride)));
         SLLM_HIP(hipGetLastError());
@@ -269,7 +281,7 @@ uint64_t linear_workspace(const LinearLaunch& a) { return plan_linear(a).bytes; 
 
 int32_t launch_linear(const LinearLaunch& a, void* workspace, hipStream_t stream) {
     const Plan plan = plan_linear(a);
-    if (!a.x.codes && plan.depth) return launch_wide_product(a, plan, workspace, stream);
+    if (plan.depth) return launch_tiled(a, plan, workspace, stream);
     const Product p{a.x, a.w_codes, a.w_scales, a.m, a.n, a.k, a.grad ? a.n : a.k, a.out, a.out_stride, a.out_dtype};
     const uint64_t gx = ceil_div(a.grad ? a.k : a.n, 32), gy = ceil_div(a.m, 32);
     if (gx > UINT32_MAX / 256 || gy > 65535) return fail(SLLM_E_RANGE, "product too large");

@@ -26,6 +26,27 @@ struct WideArgs {
     OutArgs out_args;
 };
 
+// What lanes past the end of the depth load.
+static __device__ const u32x4 kZeroVector = {0, 0, 0, 0};
+
+// Its address, as a value the compiler cannot tell: a lane's choice between it
+// and its own address then is a select, not a branch with a load on either side.
+__device__ __forceinline__ const void* zero_vector() {
+    uintptr_t p = reinterpret_cast<uintptr_t>(&kZeroVector);
+    asm("" : "+v"(p));
+    return reinterpret_cast<const void*>(p);
+}
+
+// 16 bytes a lane straight to LDS: `to` is the same in all lanes of the wave, and
+// lane l's go to to + 16 l.
+__device__ __forceinline__ void load_to_lds(const void* from, void* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// Every load of this wave has landed, those to LDS included.
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
 // A wave's accumulators: fragment [n][m] holds, in lane (r, g), columns
 // n * 16 + 4 g .. + 3 of row m * 16 + r.
 template <int FM, int FN, typename T>
@@ -52,6 +73,20 @@ __device__ __forceinline__ void store_tile(const f32x4 (&acc)[FN][FM], const Out
         }
     }
 }
+
+// Both sides in MX FP4.
+struct NarrowArgs {
+    const u32x4* x_codes;
+    const uint8_t* x_scales;
+    const u32x4* w_codes;
+    const uint8_t* w_scales;
+    uint64_t m, n, blocks, scale_pitch;
+    uint32_t steps;
+    uint32_t tiles_m, tiles_j;
+    OutArgs out_args;
+};
+int32_t launch_narrow(const NarrowArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
+constexpr uint32_t kNarrowStep = 256;  // depth of a stage
 
 template <bool Grad>
 int32_t launch_wide(const WideArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
