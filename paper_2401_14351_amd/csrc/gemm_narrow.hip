@@ -12,10 +12,6 @@ namespace {
 
 constexpr uint32_t kStepBlocks = kNarrowStep / kMxBlock;
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ i32x8 fragment(u32x4 v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
-
 template <int BM, int BN, int WM, int WN, typename T>
 __global__ __launch_bounds__(WM* WN * 64) void narrow_product(NarrowArgs a, T* out) {
     constexpr int kWaves = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;

@@ -12,18 +12,6 @@ namespace {
 
 constexpr uint32_t kStep = kWideStep;
 
-// A block of 32 codes as bfloat16: four vectors of eight.
-__device__ __forceinline__ void expand(u32x4 codes, uint32_t scale, u32x4 out[4]) {
-    const float s = mx_scale(scale);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        out[i][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 0));
-        out[i][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 1));
-        out[i][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 2));
-        out[i][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 3));
-    }
-}
-
 template <bool Grad, int BM, int BN, int WM, int WN>
 struct Wide {
     static constexpr int kThreads = WM * WN * 64, kWaves = WM * WN;

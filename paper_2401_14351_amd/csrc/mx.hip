@@ -141,6 +141,7 @@ namespace {
 
 // How a product is carried out, from its operands alone.
 struct Plan {
+    bool skinny = false;       // one launch, nothing staged
     uint32_t parts = 1;        // bfloat16 matrices that x is the sum of
     bool staged = false;       // x is written out as those first
     uint64_t depth = 0, cols = 0;
@@ -154,7 +155,8 @@ Plan plan_linear(const LinearLaunch& a) {
     Plan p;
     p.depth = a.grad ? a.n : a.k;
     p.cols = a.grad ? a.k : a.n;
-    if (!p.depth || !a.m || !p.cols) return p;
+    p.skinny = !a.grad && a.m <= kSkinnyRows;
+    if (!p.depth || !a.m || !p.cols || p.skinny) return p;
     if (!a.x.codes) p.parts = a.x.dtype == SLLM_DTYPE_BF16 ? 1 : a.x.dtype == SLLM_DTYPE_F16 ? 2 : 3;
     // The kernel reads x in aligned vectors of eight.
     p.staged = !a.x.codes && (p.parts > 1 || p.depth % 8 || (a.m > 1 && a.x.stride % 8) ||
@@ -173,7 +175,7 @@ Plan plan_linear(const LinearLaunch& a) {
 }
 
 // x as the sum of `Parts` bfloat16 matrices: its leading eight bits, the eight
-// after those, the rest.  An infinity or a NaN stays whole in the first.
+// after those, the rest.
 template <typename T, int Parts>
 __global__ __launch_bounds__(256) void split_x(const T* x, uint64_t stride, uint64_t rows, uint64_t cols, uint64_t pitch,
                                                __bf16* out) {
@@ -183,13 +185,7 @@ __global__ __launch_bounds__(256) void split_x(const T* x, uint64_t stride, uint
     uint16_t v[Parts][8];
     for (uint32_t e = 0; e < 8; ++e) {
         float f = c + e < cols ? to_f32(x[row * stride + c + e]) : 0.0f;
-        for (int p = 0; p < Parts; ++p) {
-            const uint32_t bits = __float_as_uint(f);
-            const bool finite = (bits & 0x7f800000) != 0x7f800000;
-            // a NaN whose payload is all in the lower half must not become an infinity
-            v[p][e] = finite || !(bits & 0x7fffff) ? bits >> 16 : 0x7fc0;
-            f = finite ? f - __uint_as_float(bits & 0xffff0000) : 0.0f;
-        }
+        for (int p = 0; p < Parts; ++p) v[p][e] = leading_bf16(f);
     }
     for (int p = 0; p < Parts; ++p) {
         u32x4 o;
@@ -281,6 +277,13 @@ uint64_t linear_workspace(const LinearLaunch& a) { return plan_linear(a).bytes; 
 
 int32_t launch_linear(const LinearLaunch& a, void* workspace, hipStream_t stream) {
     const Plan plan = plan_linear(a);
+    if (plan.skinny && plan.depth) {
+        const uint64_t row_bytes = a.x.stride * (a.x.dtype == SLLM_DTYPE_F32 ? 4 : 2);
+        const bool vector = reinterpret_cast<uintptr_t>(a.x.data) % 16 == 0 && (a.m == 1 || row_bytes % 16 == 0);
+        return launch_skinny(SkinnyArgs{a.x.codes ? a.x.codes : a.x.data, a.x.scales, a.m, a.n, a.k, a.x.stride, a.x.dtype, vector,
+                                        reinterpret_cast<const u32x4*>(a.w_codes), a.w_scales, mx_blocks(a.k), mx_scale_pitch(a.k),
+                                        (uint32_t)ceil_div(a.k, 128), a.out, a.out_stride, a.out_dtype}, stream);
+    }
     if (plan.depth) return launch_tiled(a, plan, workspace, stream);
     const Product p{a.x, a.w_codes, a.w_scales, a.m, a.n, a.k, a.grad ? a.n : a.k, a.out, a.out_stride, a.out_dtype};
     const uint64_t gx = ceil_div(a.grad ? a.k : a.n, 32), gy = ceil_div(a.m, 32);

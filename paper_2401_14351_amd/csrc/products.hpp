@@ -47,6 +47,35 @@ __device__ __forceinline__ void load_to_lds(const void* from, void* to) {
 // Every load of this wave has landed, those to LDS included.
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// A block of codes as an operand of the scaled matrix instruction, whose other
+// four registers 4-bit elements do not use.
+__device__ __forceinline__ i32x8 fragment(u32x4 v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
+
+// A block of 32 codes as bfloat16: four vectors of eight.
+__device__ __forceinline__ void expand(u32x4 codes, uint32_t scale, u32x4 out[4]) {
+    const float s = mx_scale(scale);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        out[i][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 0));
+        out[i][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 1));
+        out[i][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 2));
+        out[i][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 3));
+    }
+}
+
+// The leading eight bits of f as a bfloat16, and f less those: two or three of
+// these in turn are all of a float16 or a float.  An infinity or a NaN is whole
+// in the first and leaves zero.
+__device__ __forceinline__ uint32_t leading_bf16(float& f) {
+    const uint32_t bits = __float_as_uint(f);
+    const bool finite = (bits & 0x7f800000) != 0x7f800000;
+    f = finite ? f - __uint_as_float(bits & 0xffff0000) : 0.0f;
+    // a NaN whose payload is all in the lower half must not become an infinity
+    return finite || !(bits & 0x7fffff) ? bits >> 16 : 0x7fc0;
+}
+
 // A wave's accumulators: fragment [n][m] holds, in lane (r, g), columns
 // n * 16 + 4 g .. + 3 of row m * 16 + r.
 template <int FM, int FN, typename T>
@@ -87,6 +116,24 @@ struct NarrowArgs {
 };
 int32_t launch_narrow(const NarrowArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
 constexpr uint32_t kNarrowStep = 256;  // depth of a stage
+
+// At most kSkinnyRows rows of x, of any type (x_scales set: in MX FP4).
+struct SkinnyArgs {
+    const void* x;
+    const uint8_t* x_scales;
+    uint64_t m, n, depth, x_stride;
+    uint32_t x_dtype;
+    uint32_t vector;  // rows of x start on 16 bytes
+    const u32x4* w_codes;
+    const uint8_t* w_scales;
+    uint64_t blocks, scale_pitch;
+    uint32_t steps;   // of 128 of the depth
+    void* out;
+    uint64_t out_stride;
+    uint32_t out_dtype;
+};
+int32_t launch_skinny(const SkinnyArgs& a, hipStream_t stream);
+constexpr uint64_t kSkinnyRows = 32;
 
 template <bool Grad>
 int32_t launch_wide(const WideArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
