@@ -2,6 +2,7 @@
 // dequantisation of a whole matrix, a lookup of every row in turn) and its
 // gradient.
 #include <algorithm>
+#include <utility>
 
 #include "common.hpp"
 #include "device_math.hpp"
@@ -53,33 +54,213 @@ __global__ __launch_bounds__(256) void lookup(Lookup a, T* out) {
     }
 }
 
+// ---------------------------------------------------------------------------
+// Gradient: positions sorted by token, then sums over runs of equal tokens
+// ---------------------------------------------------------------------------
+
+// A key is a token and its position; ids that name no row sort last, as token
+// `vocab`.  Keys differ, so their order is one and the same however it is found.
+constexpr uint32_t kSortTile = 1024;  // keys a workgroup sorts
+constexpr uint32_t kMergeRuns = 16;   // sorted runs merged at once, a lane each
+constexpr uint32_t kWindow = 16;      // sorted positions a workgroup sums together
+constexpr uint32_t kZeroRows = 16;    // table rows a workgroup looks up and clears
+
+__device__ __forceinline__ uint32_t token_of(uint64_t key) { return (uint32_t)(key >> 32); }
+
+// Bitonic sort of a tile, a key a lane: partners up to 32 lanes away by lane
+// exchanges, the others through LDS.
+__global__ __launch_bounds__(1024) void sort_tiles(Ids ids, uint32_t n, uint32_t vocab, uint64_t* out) {
+    __shared__ uint64_t keys[kSortTile];
+    const uint32_t t = threadIdx.x, i = blockIdx.x * kSortTile + t;
+    uint64_t key = ~0ull;
+    if (i < n) {
+        const int32_t id = id_at(ids, i, vocab);
+        key = (uint64_t)(id < 0 ? vocab : (uint32_t)id) << 32 | i;
+    }
+    for (uint32_t k = 2; k <= kSortTile; k *= 2)
+        for (uint32_t j = k / 2; j > 0; j /= 2) {
+            uint64_t other;
+            if (j >= 64) {
+                __syncthreads();
+                keys[t] = key;
+                __syncthreads();
+                other = keys[t ^ j];
+            } else {
+                other = __shfl_xor(key, j);
+            }
+            const bool low = (t & j) == 0, up = (t & k) == 0;
+            key = (low == up) == (key < other) ? key : other;
+        }
+    if (i < n) out[i] = key;
+}
+
+// Merge groups of kMergeRuns sorted runs: a key's place is the number of
+// smaller keys in its group, found by one bisection per run.
+__global__ __launch_bounds__(256) void merge_runs(const uint64_t* in, uint32_t n, uint32_t run, uint64_t* out) {
+    const uint64_t i = ((uint64_t)blockIdx.x * 256 + threadIdx.x) / kMergeRuns;
+    const uint32_t q = threadIdx.x % kMergeRuns;
+    if (i >= n) return;
+    const uint64_t key = in[i];
+    const uint64_t group = i / run / kMergeRuns * kMergeRuns * run;
+    const uint64_t first = group + (uint64_t)q * run;
+    uint32_t count = 0;
+    if (first < n) {
+        uint64_t lo = first, hi = min(first + run, (uint64_t)n);
+        while (lo < hi) {
+            const uint64_t mid = (lo + hi) / 2;
+            if (in[mid] < key)
+                lo = mid + 1;
+            else
+                hi = mid;
+        }
+        count = (uint32_t)(lo - first);
+    }
+    for (uint32_t d = kMergeRuns / 2; d > 0; d /= 2) count += __shfl_xor(count, d);
+    if (q == 0) out[group + count] = key;
+}
+
 struct GradArgs {
-    uint64_t dy_stride;
-    Ids ids;
-    uint64_t n;
+    const uint64_t* keys;  // sorted
+    uint32_t n, vocab, dim;
     float scale;
-    uint32_t vocab, dim;
-    uint64_t grad_stride;
+    uint64_t dy_stride, grad_stride;
     bool accumulate;
+    float* partial;        // a window's first and last run: [windows][2][pitch]
+    uint32_t pitch, windows;
+    uint32_t lanes;        // of a row: 32, 64, 128 or 256
+    uint32_t chunks;       // of a row, lanes * 8 columns each
+    uint32_t sum_blocks;   // workgroups that sum; the rest clear rows
 };
 
-// A workgroup per table row goes through all ids.
-template <typename S, typename T>
-__global__ __launch_bounds__(256) void gather_grad(GradArgs a, const S* dy, T* grad) {
-    for (uint32_t row = blockIdx.x; row < a.vocab; row += gridDim.x)
-        for (uint32_t c = threadIdx.x; c < a.dim; c += 256) {
-            float sum = 0;
-            bool any = false;
-            for (uint64_t i = 0; i < a.n; ++i)
-                if (id_at(a.ids, i, a.vocab) == (int32_t)row) {
-                    sum += to_f32(dy[i * a.dy_stride + c]);
-                    any = true;
-                }
-            const uint64_t at = (uint64_t)row * a.grad_stride + c;
-            sum *= a.scale;
-            if (a.accumulate && any) grad[at] = from_f32<T>(to_f32(grad[at]) + sum);
-            if (!a.accumulate) grad[at] = from_f32<T>(sum);
+// Columns c .. c + 7 of a row, those past the end zero.  Vec: rows start on 16
+// bytes and end on a multiple of eight columns.
+template <bool Vec, typename S>
+__device__ __forceinline__ void load8(const S* row, uint32_t c, uint32_t dim, float (&v)[8]) {
+    S e[8];
+    if constexpr (Vec) {
+        u32x4 raw[sizeof(S) / 2];
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(S) / 2; ++i) raw[i] = reinterpret_cast<const u32x4*>(row + c)[i];
+        __builtin_memcpy(e, raw, sizeof e);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) e[i] = c + i < dim ? row[c + i] : (S)0.0f;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) v[i] = to_f32(e[i]);
+}
+
+template <bool Vec, typename T>
+__device__ __forceinline__ void store8(T* row, uint32_t c, uint32_t dim, const float (&v)[8]) {
+    T e[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) e[i] = from_f32<T>(v[i]);
+    if constexpr (Vec) {
+        u32x4 raw[sizeof(T) / 2];
+        __builtin_memcpy(raw, e, sizeof e);
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(T) / 2; ++i) reinterpret_cast<u32x4*>(row + c)[i] = raw[i];
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (c + i < dim) row[c + i] = e[i];
+    }
+}
+
+// A table row's gradient from its whole sum.
+template <bool Vec, typename T>
+__device__ __forceinline__ void write_row(const GradArgs& a, T* grad, uint32_t token, uint32_t c, float (&sum)[8]) {
+    T* row = grad + (uint64_t)token * a.grad_stride;
+    float old[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (a.accumulate) load8<Vec>(row, c, a.dim, old);
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) sum[i] = old[i] + sum[i] * a.scale;
+    store8<Vec>(row, c, a.dim, sum);
+}
+
+// The first workgroups take windows of sorted positions.  A run of equal tokens
+// inside one window becomes its row at once; one that goes on into the next
+// window, or came from the one before, leaves its sum for join_runs.  The other
+// workgroups clear the rows that no key names.
+template <bool Vec, typename S, typename T>
+__global__ __launch_bounds__(256) void sum_runs(GradArgs a, const S* dy, T* grad) {
+    if (blockIdx.x >= a.sum_blocks) {
+        __shared__ uint32_t named[kZeroRows];
+        const uint32_t row0 = (blockIdx.x - a.sum_blocks) * kZeroRows;
+        if (threadIdx.x < kZeroRows) {
+            const uint64_t key = (uint64_t)(row0 + threadIdx.x) << 32;
+            uint32_t lo = 0, hi = a.n;
+            while (lo < hi) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (a.keys[mid] < key)
+                    lo = mid + 1;
+                else
+                    hi = mid;
+            }
+            named[threadIdx.x] = lo < a.n && token_of(a.keys[lo]) == row0 + threadIdx.x;
         }
+        __syncthreads();
+        const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (uint32_t r = threadIdx.x / a.lanes; r < kZeroRows && row0 + r < a.vocab; r += 256 / a.lanes)
+            if (!named[r])
+                for (uint32_t c = threadIdx.x % a.lanes * 8; c < a.dim; c += a.lanes * 8)
+                    store8<Vec>(grad + (uint64_t)(row0 + r) * a.grad_stride, c, a.dim, zero);
+        return;
+    }
+    const uint32_t per = 256 / a.lanes;  // windows of a workgroup
+    const uint32_t w = blockIdx.x / a.chunks * per + threadIdx.x / a.lanes;
+    const uint32_t c = (blockIdx.x % a.chunks * a.lanes + threadIdx.x % a.lanes) * 8;
+    if (w >= a.windows || c >= a.dim) return;
+    const uint32_t first = w * kWindow, end = min(first + kWindow, a.n);
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    uint32_t token = token_of(a.keys[first]);
+    bool whole = first == 0 || token_of(a.keys[first - 1]) != token;  // the run starts here
+    for (uint32_t i = first; i < end; ++i) {
+        const uint64_t key = a.keys[i];
+        if (token_of(key) != token) {
+            if (whole)
+                write_row<Vec>(a, grad, token, c, sum);
+            else
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) a.partial[(uint64_t)w * 2 * a.pitch + c + e] = sum[e];
+            token = token_of(key);
+            whole = true;
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e) sum[e] = 0;
+        }
+        if (token >= a.vocab) return;
+        float v[8];
+        load8<Vec>(dy + (uint64_t)(uint32_t)key * a.dy_stride, c, a.dim, v);
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) sum[e] += v[e];
+    }
+    const bool goes_on = end < a.n && token_of(a.keys[end]) == token;
+    if (whole && !goes_on)
+        write_row<Vec>(a, grad, token, c, sum);
+    else
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) a.partial[((uint64_t)w * 2 + whole) * a.pitch + c + e] = sum[e];
+}
+
+// The rows of runs that cross windows: the last run of the window where it
+// starts, then the first of each window it goes on into.
+template <bool Vec, typename T>
+__global__ __launch_bounds__(256) void join_runs(GradArgs a, T* grad) {
+    const uint32_t per = 256 / a.lanes;
+    const uint32_t w = blockIdx.x / a.chunks * per + threadIdx.x / a.lanes;
+    const uint32_t c = (blockIdx.x % a.chunks * a.lanes + threadIdx.x % a.lanes) * 8;
+    if (w + 1 >= a.windows || c >= a.dim) return;
+    const uint32_t first = w * kWindow, end = first + kWindow;
+    const uint32_t token = token_of(a.keys[end - 1]);
+    if (token >= a.vocab || token_of(a.keys[end]) != token) return;            // ends here
+    if (token_of(a.keys[first]) == token && first && token_of(a.keys[first - 1]) == token) return;  // starts before
+    float sum[8];
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) sum[e] = a.partial[((uint64_t)w * 2 + 1) * a.pitch + c + e];
+    for (uint32_t next = w + 1; next < a.windows && token_of(a.keys[next * kWindow]) == token; ++next)
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) sum[e] += a.partial[(uint64_t)next * 2 * a.pitch + c + e];
+    write_row<Vec>(a, grad, token, c, sum);
 }
 
 }  // namespace
@@ -98,16 +279,73 @@ int32_t launch_embedding(const EmbeddingLaunch& a, hipStream_t stream) {
     return SLLM_OK;
 }
 
-uint64_t embedding_grad_workspace(uint64_t n_ids, uint64_t vocab, uint64_t dim) { return 0; }
+namespace {
+
+uint64_t align256(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+struct GradPlan {
+    uint64_t windows, pitch, keys_bytes, bytes;
+};
+
+GradPlan plan_grad(uint64_t n, uint64_t dim) {
+    GradPlan p;
+    p.windows = ceil_div(n, kWindow);
+    p.pitch = (dim + 7) / 8 * 8;
+    p.keys_bytes = align256(n * 8);
+    // two copies of the keys where they are merged, sums where runs can cross windows
+    p.bytes = (n > kSortTile ? 2 : 1) * p.keys_bytes + (p.windows > 1 ? p.windows * 2 * p.pitch * 4 : 0);
+    return p;
+}
+
+template <bool Vec, typename S, typename T>
+int32_t launch_sums(const GradArgs& g, const EmbeddingGradLaunch& a, uint64_t grid, hipStream_t stream) {
+    T* grad = static_cast<T*>(a.grad);
+    sum_runs<Vec, S, T><<<(uint32_t)grid, 256, 0, stream>>>(g, static_cast<const S*>(a.dy), grad);
+    SLLM_HIP(hipGetLastError());
+    if (g.windows > 1) {
+        join_runs<Vec, T><<<g.sum_blocks, 256, 0, stream>>>(g, grad);
+        SLLM_HIP(hipGetLastError());
+    }
+    return SLLM_OK;
+}
+
+}  // namespace
+
+uint64_t embedding_grad_workspace(uint64_t n_ids, uint64_t vocab, uint64_t dim) { return plan_grad(n_ids, dim).bytes; }
 
 int32_t launch_embedding_grad(const EmbeddingGradLaunch& a, void* workspace, hipStream_t stream) {
-    const GradArgs g{a.dy_stride, {a.ids, a.ids64}, a.n, a.scale, (uint32_t)a.vocab, (uint32_t)a.dim, a.grad_stride,
-                     a.accumulate};
-    const uint32_t grid = (uint32_t)std::min<uint64_t>(a.vocab, 1u << 20);
-    SLLM_BY_DTYPE(a.dy_dtype, S, SLLM_BY_DTYPE(a.grad_dtype, T, (gather_grad<S, T><<<grid, 256, 0, stream>>>(
-                                                                    g, static_cast<const S*>(a.dy),
-                                                                    static_cast<T*>(a.grad)))));
-    SLLM_HIP(hipGetLastError());
+    const GradPlan p = plan_grad(a.n, a.dim);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    uint64_t* keys = reinterpret_cast<uint64_t*>(ws);
+    if (a.n) {
+        sort_tiles<<<(uint32_t)ceil_div(a.n, kSortTile), kSortTile, 0, stream>>>({a.ids, a.ids64}, (uint32_t)a.n, (uint32_t)a.vocab, keys);
+        SLLM_HIP(hipGetLastError());
+        uint64_t* other = reinterpret_cast<uint64_t*>(ws + p.keys_bytes);
+        for (uint64_t run = kSortTile; run < a.n; run *= kMergeRuns) {
+            merge_runs<<<(uint32_t)ceil_div(a.n * kMergeRuns, 256), 256, 0, stream>>>(keys, (uint32_t)a.n, (uint32_t)run, other);
+            SLLM_HIP(hipGetLastError());
+            std::swap(keys, other);
+        }
+    }
+    GradArgs g;
+    g.keys = keys;
+    g.n = (uint32_t)a.n, g.vocab = (uint32_t)a.vocab, g.dim = (uint32_t)a.dim;
+    g.scale = a.scale;
+    g.dy_stride = a.dy_stride, g.grad_stride = a.grad_stride;
+    g.accumulate = a.accumulate;
+    g.partial = reinterpret_cast<float*>(ws + (a.n > kSortTile ? 2 : 1) * p.keys_bytes);
+    g.pitch = (uint32_t)p.pitch, g.windows = (uint32_t)p.windows;
+    g.lanes = a.dim > 1024 ? 256 : a.dim > 512 ? 128 : a.dim > 256 ? 64 : 32;
+    g.chunks = (uint32_t)ceil_div(a.dim, g.lanes * 8);
+    const uint64_t sums = ceil_div(p.windows, 256 / g.lanes) * g.chunks;
+    const uint64_t grid = sums + (a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows));
+    if (grid > UINT32_MAX / 256) return fail(SLLM_E_RANGE, "gradient too large");
+    g.sum_blocks = (uint32_t)sums;
+    const uint64_t dy_size = a.dy_dtype == SLLM_DTYPE_F32 ? 4 : 2, grad_size = a.grad_dtype == SLLM_DTYPE_F32 ? 4 : 2;
+    const bool vec = a.dim % 8 == 0 && (reinterpret_cast<uintptr_t>(a.dy) | reinterpret_cast<uintptr_t>(a.grad)) % 16 == 0 &&
+                     (a.n <= 1 || a.dy_stride * dy_size % 16 == 0) && (a.vocab <= 1 || a.grad_stride * grad_size % 16 == 0);
+    SLLM_BY_DTYPE(a.dy_dtype, S, SLLM_BY_DTYPE(a.grad_dtype, T, return vec ? (launch_sums<true, S, T>(g, a, grid, stream))
+                                                                          : (launch_sums<false, S, T>(g, a, grid, stream))));
     return SLLM_OK;
 }
 
