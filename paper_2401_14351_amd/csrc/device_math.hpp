@@ -46,10 +46,4 @@ __device__ __forceinline__ T from_f32(float v) {
 // 2^-127 and 255 makes the results NaN, as the format has it.
 __device__ __forceinline__ float mx_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// Code c of a byte (0 the low half) under a scale byte, as a 32-bit float.
-__device__ __forceinline__ float mx_value(uint32_t byte, uint32_t half, uint32_t scale) {
-    const f32x2 v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(byte, mx_scale(scale), 0);
-    return half ? v[1] : v[0];
-}
-
 }  // namespace sllm

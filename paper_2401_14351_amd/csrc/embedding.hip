@@ -31,26 +31,71 @@ struct Lookup {
     uint64_t n;
     float scale;
     uint64_t out_stride;
+    uint32_t lanes;  // of a row: 32, 64, 128 or 256
 };
 
-// A workgroup per row.  S: the table's elements, void for MX FP4.
-template <typename S, typename T>
+// Columns c .. c + 7 of a row, those past the end zero.  Vec: rows start on 16
+// bytes and end on a multiple of eight columns.
+template <bool Vec, typename S>
+__device__ __forceinline__ void load8(const S* row, uint32_t c, uint32_t dim, float (&v)[8]) {
+    S e[8];
+    if constexpr (Vec) {
+        u32x4 raw[sizeof(S) / 2];
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(S) / 2; ++i) raw[i] = reinterpret_cast<const u32x4*>(row + c)[i];
+        __builtin_memcpy(e, raw, sizeof e);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) e[i] = c + i < dim ? row[c + i] : (S)0.0f;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) v[i] = to_f32(e[i]);
+}
+
+template <bool Vec, typename T>
+__device__ __forceinline__ void store8(T* row, uint32_t c, uint32_t dim, const float (&v)[8]) {
+    T e[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) e[i] = from_f32<T>(v[i]);
+    if constexpr (Vec) {
+        u32x4 raw[sizeof(T) / 2];
+        __builtin_memcpy(raw, e, sizeof e);
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(T) / 2; ++i) reinterpret_cast<u32x4*>(row + c)[i] = raw[i];
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (c + i < dim) row[c + i] = e[i];
+    }
+}
+
+// Eight columns a lane, `lanes` of them a row at a time.  S: the table's
+// elements, void for MX FP4.
+template <bool Vec, typename S, typename T>
 __global__ __launch_bounds__(256) void lookup(Lookup a, T* out) {
-    for (uint64_t i = blockIdx.x; i < a.n; i += gridDim.x) {
-        const int64_t row = a.ids.p ? id_at(a.ids, i, a.vocab) : (int64_t)i;
-        for (uint32_t c = threadIdx.x; c < a.dim; c += 256) {
-            float v = 0;
-            if (row >= 0) {
-                if constexpr (__is_same(S, void)) {
-                    const uint32_t blocks = (a.dim + 31) / 32, pitch = (blocks + 15) / 16 * 16;
-                    v = mx_value(a.table.codes[(uint64_t)row * blocks * 16 + c / 2], c & 1,
-                                 a.table.scales[(uint64_t)row * pitch + c / 32]);
-                } else {
-                    v = to_f32(static_cast<const S*>(a.table.data)[row * a.table.stride + c]);
-                }
+    const uint64_t i = (uint64_t)blockIdx.x * (256 / a.lanes) + threadIdx.x / a.lanes;
+    if (i >= a.n) return;
+    const int64_t row = a.ids.p ? id_at(a.ids, i, a.vocab) : (int64_t)i;
+    const uint32_t blocks = (a.dim + 31) / 32, pitch = (blocks + 15) / 16 * 16;
+    for (uint32_t c = threadIdx.x % a.lanes * 8; c < a.dim; c += a.lanes * 8) {
+        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (row >= 0) {
+            if constexpr (__is_same(S, void)) {
+                const uint32_t codes = *reinterpret_cast<const uint32_t*>(a.table.codes + (uint64_t)row * blocks * 16 + c / 2);
+                const float scale = mx_scale(a.table.scales[(uint64_t)row * pitch + c / 32]);
+                const f32x2 two[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0),
+                                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1),
+                                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2),
+                                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3)};
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) v[e] = two[e / 2][e % 2];
+            } else {
+                load8<Vec>(static_cast<const S*>(a.table.data) + (uint64_t)row * a.table.stride, c, a.dim, v);
             }
-            out[i * a.out_stride + c] = from_f32<T>(v * a.scale);
         }
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) v[e] *= a.scale;
+        store8<Vec>(out + i * a.out_stride, c, a.dim, v);
     }
 }
 
@@ -131,41 +176,6 @@ struct GradArgs {
     uint32_t chunks;       // of a row, lanes * 8 columns each
     uint32_t sum_blocks;   // workgroups that sum; the rest clear rows
 };
-
-// Columns c .. c + 7 of a row, those past the end zero.  Vec: rows start on 16
-// bytes and end on a multiple of eight columns.
-template <bool Vec, typename S>
-__device__ __forceinline__ void load8(const S* row, uint32_t c, uint32_t dim, float (&v)[8]) {
-    S e[8];
-    if constexpr (Vec) {
-        u32x4 raw[sizeof(S) / 2];
-#pragma unroll
-        for (uint32_t i = 0; i < sizeof(S) / 2; ++i) raw[i] = reinterpret_cast<const u32x4*>(row + c)[i];
-        __builtin_memcpy(e, raw, sizeof e);
-    } else {
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) e[i] = c + i < dim ? row[c + i] : (S)0.0f;
-    }
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) v[i] = to_f32(e[i]);
-}
-
-template <bool Vec, typename T>
-__device__ __forceinline__ void store8(T* row, uint32_t c, uint32_t dim, const float (&v)[8]) {
-    T e[8];
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) e[i] = from_f32<T>(v[i]);
-    if constexpr (Vec) {
-        u32x4 raw[sizeof(T) / 2];
-        __builtin_memcpy(raw, e, sizeof e);
-#pragma unroll
-        for (uint32_t i = 0; i < sizeof(T) / 2; ++i) reinterpret_cast<u32x4*>(row + c)[i] = raw[i];
-    } else {
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
-            if (c + i < dim) row[c + i] = e[i];
-    }
-}
 
 // A table row's gradient from its whole sum.
 template <bool Vec, typename T>
@@ -249,31 +259,69 @@ __global__ __launch_bounds__(256) void join_runs(GradArgs a, T* grad) {
     const uint32_t per = 256 / a.lanes;
     const uint32_t w = blockIdx.x / a.chunks * per + threadIdx.x / a.lanes;
     const uint32_t c = (blockIdx.x % a.chunks * a.lanes + threadIdx.x % a.lanes) * 8;
-    if (w + 1 >= a.windows || c >= a.dim) return;
+    if (w + 1 >= a.windows) return;
     const uint32_t first = w * kWindow, end = first + kWindow;
     const uint32_t token = token_of(a.keys[end - 1]);
     if (token >= a.vocab || token_of(a.keys[end]) != token) return;            // ends here
     if (token_of(a.keys[first]) == token && first && token_of(a.keys[first - 1]) == token) return;  // starts before
-    float sum[8];
-#pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) sum[e] = a.partial[((uint64_t)w * 2 + 1) * a.pitch + c + e];
-    for (uint32_t next = w + 1; next < a.windows && token_of(a.keys[next * kWindow]) == token; ++next)
-#pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) sum[e] += a.partial[(uint64_t)next * 2 * a.pitch + c + e];
+    // how many windows it goes on into, 32 looked at together (a row has that many lanes or more)
+    const uint32_t lane = threadIdx.x % 64, half = lane & 32;
+    uint32_t last = w;
+    for (uint32_t found = 32; found == 32; last += found) {
+        const uint64_t next = last + 1 + (uint64_t)(lane & 31);
+        const uint64_t same = __ballot(next < a.windows && token_of(a.keys[next * kWindow]) == token);
+        const uint32_t mine = (uint32_t)(same >> half);
+        found = ~mine ? __builtin_ctz(~mine) : 32;
+    }
+    if (c >= a.dim) return;
+    const float* p = a.partial + ((uint64_t)w * 2 + 1) * a.pitch + c;
+    f32x4 lo = reinterpret_cast<const f32x4*>(p)[0], hi = reinterpret_cast<const f32x4*>(p)[1];
+    p += a.pitch;
+#pragma unroll 8
+    for (uint32_t next = w + 1; next <= last; ++next, p += 2 * (uint64_t)a.pitch) {
+        lo += reinterpret_cast<const f32x4*>(p)[0];
+        hi += reinterpret_cast<const f32x4*>(p)[1];
+    }
+    float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     write_row<Vec>(a, grad, token, c, sum);
 }
 
 }  // namespace
 
+namespace {
+
+uint64_t element_bytes(uint32_t dtype) { return dtype == SLLM_DTYPE_F32 ? 4 : 2; }
+
+// Rows at this address, apart by this stride, start on 16 bytes.
+bool on_vectors(const void* data, uint64_t rows, uint64_t stride, uint32_t dtype) {
+    return reinterpret_cast<uintptr_t>(data) % 16 == 0 && (rows <= 1 || stride * element_bytes(dtype) % 16 == 0);
+}
+
+// Lanes that take a row together, eight columns each.
+uint32_t row_lanes(uint64_t dim) { return dim > 1024 ? 256 : dim > 512 ? 128 : dim > 256 ? 64 : 32; }
+
+template <bool Vec, typename T>
+void launch_lookup(const Lookup& l, uint32_t grid, T* out, hipStream_t stream) {
+    if (l.table.codes)
+        lookup<Vec, void, T><<<grid, 256, 0, stream>>>(l, out);
+    else
+        SLLM_BY_DTYPE(l.table.dtype, S, (lookup<Vec, S, T><<<grid, 256, 0, stream>>>(l, out)));
+}
+
+}  // namespace
+
 int32_t launch_embedding(const EmbeddingLaunch& a, hipStream_t stream) {
-    const Lookup l{a.table, (uint32_t)a.vocab, (uint32_t)a.dim, {a.ids, a.ids64}, a.n, a.scale, a.out_stride};
-    const uint32_t grid = (uint32_t)std::min<uint64_t>(a.n, 1u << 20);
+    const uint32_t lanes = row_lanes(a.dim);
+    const Lookup l{a.table, (uint32_t)a.vocab, (uint32_t)a.dim, {a.ids, a.ids64}, a.n, a.scale, a.out_stride, lanes};
+    const uint64_t grid = ceil_div(a.n, 256 / lanes);
+    if (grid > UINT32_MAX / 256) return fail(SLLM_E_RANGE, "%llu rows are more than a launch takes", (unsigned long long)a.n);
+    const bool vec = a.dim % 8 == 0 && on_vectors(a.out, a.n, a.out_stride, a.out_dtype) &&
+                     (a.table.codes || on_vectors(a.table.data, a.vocab, a.table.stride, a.table.dtype));
     SLLM_BY_DTYPE(a.out_dtype, T, {
-        T* out = static_cast<T*>(a.out);
-        if (a.table.codes)
-            lookup<void, T><<<grid, 256, 0, stream>>>(l, out);
+        if (vec)
+            launch_lookup<true>(l, (uint32_t)grid, static_cast<T*>(a.out), stream);
         else
-            SLLM_BY_DTYPE(a.table.dtype, S, (lookup<S, T><<<grid, 256, 0, stream>>>(l, out)));
+            launch_lookup<false>(l, (uint32_t)grid, static_cast<T*>(a.out), stream);
     });
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
@@ -335,15 +383,14 @@ int32_t launch_embedding_grad(const EmbeddingGradLaunch& a, void* workspace, hip
     g.accumulate = a.accumulate;
     g.partial = reinterpret_cast<float*>(ws + (a.n > kSortTile ? 2 : 1) * p.keys_bytes);
     g.pitch = (uint32_t)p.pitch, g.windows = (uint32_t)p.windows;
-    g.lanes = a.dim > 1024 ? 256 : a.dim > 512 ? 128 : a.dim > 256 ? 64 : 32;
+    g.lanes = row_lanes(a.dim);
     g.chunks = (uint32_t)ceil_div(a.dim, g.lanes * 8);
     const uint64_t sums = ceil_div(p.windows, 256 / g.lanes) * g.chunks;
     const uint64_t grid = sums + (a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows));
     if (grid > UINT32_MAX / 256) return fail(SLLM_E_RANGE, "gradient too large");
     g.sum_blocks = (uint32_t)sums;
-    const uint64_t dy_size = a.dy_dtype == SLLM_DTYPE_F32 ? 4 : 2, grad_size = a.grad_dtype == SLLM_DTYPE_F32 ? 4 : 2;
-    const bool vec = a.dim % 8 == 0 && (reinterpret_cast<uintptr_t>(a.dy) | reinterpret_cast<uintptr_t>(a.grad)) % 16 == 0 &&
-                     (a.n <= 1 || a.dy_stride * dy_size % 16 == 0) && (a.vocab <= 1 || a.grad_stride * grad_size % 16 == 0);
+    const bool vec = a.dim % 8 == 0 && on_vectors(a.dy, a.n, a.dy_stride, a.dy_dtype) &&
+                     on_vectors(a.grad, a.vocab, a.grad_stride, a.grad_dtype);
     SLLM_BY_DTYPE(a.dy_dtype, S, SLLM_BY_DTYPE(a.grad_dtype, T, return vec ? (launch_sums<true, S, T>(g, a, grid, stream))
                                                                           : (launch_sums<false, S, T>(g, a, grid, stream))));
     return SLLM_OK;

@@ -1,4 +1,5 @@
-// gfx950 kernels of MX FP4 matrices: quantisation and products.
+// gfx950 kernels of MX FP4 matrices: quantisation, and the way a product is
+// carried out (the products' own kernels are in gemm_*.hip).
 #include <algorithm>
 
 #include "common.hpp"
@@ -24,115 +25,80 @@ __device__ __forceinline__ uint32_t block_scale(float top) {
     return e == 255 ? 255 : e < 2 ? 0 : e - 2;
 }
 
-// One lane per block.
-template <typename T>
-__global__ __launch_bounds__(256) void mx_quantize(const T* src, uint64_t stride, uint64_t rows, uint32_t cols,
-                                                   uint32_t scale_pitch, uint8_t* codes, uint8_t* scales) {
-    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    const uint64_t row = i / scale_pitch;
-    const uint32_t b = i % scale_pitch, blocks = (cols + 31) / 32;
+// x of the lane a DPP control names, among the four lanes of a block
+template <int Ctrl>
+__device__ __forceinline__ float quad(float x) {
+    return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), Ctrl, 0xF, 0xF, true));
+}
+
+// Four lanes a block, eight columns each, `lanes` of them a row at a time.
+// Vec: rows start on 16 bytes and end on a multiple of eight columns.
+template <bool Vec, typename T>
+__global__ __launch_bounds__(256) void mx_quantize(const T* src, uint64_t stride, uint64_t rows, uint32_t cols, uint32_t lanes,
+                                                   uint8_t* codes, uint8_t* scales) {
+    const uint64_t row = (uint64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes;
     if (row >= rows) return;
-    if (b >= blocks) {
-        scales[row * scale_pitch + b] = 0;
-        return;
-    }
-    float v[32], top = 0;
-    bool finite = true;
-    for (uint32_t c = 0; c < 32; ++c) {
-        v[c] = b * 32 + c < cols ? to_f32(src[row * stride + b * 32 + c]) : 0.0f;
-        finite &= (__float_as_uint(v[c]) & 0x7f800000) != 0x7f800000;
-        top = fmaxf(top, fabsf(v[c]));
-    }
-    const uint32_t s = finite ? block_scale(top) : 255;
-    u32x4 out = {0, 0, 0, 0};
-    if (finite)
-        for (uint32_t c = 0; c < 32; c += 2) {
-            const uint32_t two = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[c], v[c + 1], mx_scale(s), 0) & 0xff;
-            out[c / 8] |= two << (c % 8 * 4);
+    const uint32_t blocks = (cols + 31) / 32, pitch = (blocks + 15) / 16 * 16;
+    const T* x = src + row * stride;
+    uint32_t* out = reinterpret_cast<uint32_t*>(codes + row * blocks * 16);
+    uint8_t* scale_row = scales + row * pitch;
+    for (uint32_t i = threadIdx.x % lanes; i < pitch * 4; i += lanes) {
+        const uint32_t b = i / 4, c = i * 8;
+        if (b >= blocks) {
+            if (i % 4 == 0) scale_row[b] = 0;
+            continue;
         }
-    reinterpret_cast<u32x4*>(codes)[row * blocks + b] = out;
-    scales[row * scale_pitch + b] = s;
-}
-
-// ---------------------------------------------------------------------------
-// Products
-// ---------------------------------------------------------------------------
-
-struct Product {
-    Operand x;
-    const uint8_t* w_codes;
-    const uint8_t* w_scales;
-    uint64_t m, n, k;
-    uint64_t x_cols;
-    void* out;
-    uint64_t out_stride;
-    uint32_t out_dtype;
-};
-
-__device__ float mx_at(const uint8_t* codes, const uint8_t* scales, uint64_t cols, uint64_t r, uint64_t c) {
-    const uint64_t blocks = (cols + 31) / 32, pitch = (blocks + 15) / 16 * 16;
-    return mx_value(codes[r * blocks * 16 + c / 2], c & 1, scales[r * pitch + c / 32]);
-}
-
-// A tile of 32 x 32 outputs a workgroup, 32 steps of the sum at a time through LDS.
-template <bool Grad>
-__global__ __launch_bounds__(256) void mx_product(Product p) {
-    __shared__ float xs[32][33], ws[32][33];
-    const uint64_t cols = Grad ? p.k : p.n, depth = Grad ? p.n : p.k;
-    const uint64_t m0 = (uint64_t)blockIdx.y * 32, j0 = (uint64_t)blockIdx.x * 32;
-    const uint32_t tx = threadIdx.x % 32, ty = threadIdx.x / 32;
-    float acc[4] = {0, 0, 0, 0};
-    for (uint64_t d0 = 0; d0 < depth; d0 += 32) {
-        for (uint32_t r = ty; r < 32; r += 8) {
-            const uint64_t m = m0 + r, d = d0 + tx;
-            float v = 0;
-            if (m < p.m && d < depth) {
-                if (p.x.codes)
-                    v = mx_at(p.x.codes, p.x.scales, p.x_cols, m, d);
-                else if (p.x.dtype == SLLM_DTYPE_F32)
-                    v = static_cast<const float*>(p.x.data)[m * p.x.stride + d];
-                else if (p.x.dtype == SLLM_DTYPE_F16)
-                    v = to_f32(static_cast<const _Float16*>(p.x.data)[m * p.x.stride + d]);
-                else
-                    v = to_f32(static_cast<const __bf16*>(p.x.data)[m * p.x.stride + d]);
-            }
-            xs[r][tx] = v;
-            // ws[d][j]
-            const uint64_t n = Grad ? d0 + r : j0 + r, k = Grad ? j0 + tx : d0 + tx;
-            const float w = n < p.n && k < p.k ? mx_at(p.w_codes, p.w_scales, p.k, n, k) : 0.0f;
-            if (Grad)
-                ws[r][tx] = w;
-            else
-                ws[tx][r] = w;
+        T e[8];
+        if (Vec && c < cols) {
+            u32x4 raw[sizeof(T) / 2];
+#pragma unroll
+            for (uint32_t j = 0; j < sizeof(T) / 2; ++j) raw[j] = reinterpret_cast<const u32x4*>(x + c)[j];
+            __builtin_memcpy(e, raw, sizeof e);
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) e[j] = c + j < cols ? x[c + j] : (T)0.0f;
         }
-        __syncthreads();
-        for (uint32_t d = 0; d < 32; ++d)
-            for (uint32_t i = 0; i < 4; ++i) acc[i] += xs[ty + 8 * i][d] * ws[d][tx];
-        __syncthreads();
-    }
-    for (uint32_t i = 0; i < 4; ++i) {
-        const uint64_t m = m0 + ty + 8 * i, j = j0 + tx;
-        if (m >= p.m || j >= cols) continue;
-        const uint64_t at = m * p.out_stride + j;
-        if (p.out_dtype == SLLM_DTYPE_F32)
-            static_cast<float*>(p.out)[at] = acc[i];
-        else if (p.out_dtype == SLLM_DTYPE_F16)
-            static_cast<_Float16*>(p.out)[at] = from_f32<_Float16>(acc[i]);
-        else
-            static_cast<__bf16*>(p.out)[at] = from_f32<__bf16>(acc[i]);
+        // magnitudes as integers order as the numbers do, infinities and NaN above all others
+        uint32_t top = 0;
+        float v[8];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+            v[j] = to_f32(e[j]);
+            top = max(top, __float_as_uint(v[j]) & 0x7fffffff);
+        }
+        top = max(top, __float_as_uint(quad<0xB1>(__uint_as_float(top))));  // lanes 1 0 3 2
+        top = max(top, __float_as_uint(quad<0x4E>(__uint_as_float(top))));  // lanes 2 3 0 1
+        const uint32_t s = block_scale(__uint_as_float(top));
+        const float f = mx_scale(s);
+        uint32_t packed = 0;
+        if (s != 255) {
+            packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(packed, v[0], v[1], f, 0);
+            packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(packed, v[2], v[3], f, 1);
+            packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(packed, v[4], v[5], f, 2);
+            packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(packed, v[6], v[7], f, 3);
+        }
+        out[i] = packed;
+        if (i % 4 == 0) scale_row[b] = s;
     }
 }
 
 }  // namespace
 
 int32_t launch_quantize(const sllm_matrix& src, const sllm_mx& dst, hipStream_t stream) {
-    const uint32_t pitch = (uint32_t)mx_scale_pitch(src.cols);
-    const uint64_t grid = ceil_div(src.rows * pitch, 256);
-    if (grid > UINT32_MAX / 256) return fail(SLLM_E_RANGE, "matrix too large");
-    SLLM_BY_DTYPE(src.dtype, T,
-                  mx_quantize<T><<<(uint32_t)grid, 256, 0, stream>>>(
-                      static_cast<const T*>(src.data), src.stride, src.rows, (uint32_t)src.cols, pitch,
-                      static_cast<uint8_t*>(dst.codes), static_cast<uint8_t*>(dst.scales)));
+    const uint64_t vectors = mx_scale_pitch(src.cols) * 4;
+    const uint32_t lanes = vectors >= 256 ? 256 : vectors >= 128 ? 128 : 64;
+    const uint64_t grid = ceil_div(src.rows, 256 / lanes);
+    if (grid > UINT32_MAX / 256) return fail(SLLM_E_RANGE, "%llu rows are more than a launch takes", (unsigned long long)src.rows);
+    const uint64_t row_bytes = src.stride * (src.dtype == SLLM_DTYPE_F32 ? 4 : 2);
+    const bool vec = src.cols % 8 == 0 && reinterpret_cast<uintptr_t>(src.data) % 16 == 0 && (src.rows == 1 || row_bytes % 16 == 0);
+    uint8_t *codes = static_cast<uint8_t*>(dst.codes), *scales = static_cast<uint8_t*>(dst.scales);
+    SLLM_BY_DTYPE(src.dtype, T, {
+        const T* x = static_cast<const T*>(src.data);
+        if (vec)
+            mx_quantize<true, T><<<(uint32_t)grid, 256, 0, stream>>>(x, src.stride, src.rows, (uint32_t)src.cols, lanes, codes, scales);
+        else
+            mx_quantize<false, T><<<(uint32_t)grid, 256, 0, stream>>>(x, src.stride, src.rows, (uint32_t)src.cols, lanes, codes, scales);
+    });
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
 }
@@ -213,6 +179,15 @@ int32_t grid_of(uint64_t threads, uint32_t* blocks) {
     return SLLM_OK;
 }
 
+int32_t join(const Plan& p, const float* sums, uint32_t splits, const LinearLaunch& a, hipStream_t stream) {
+    uint32_t blocks;
+    SLLM_TRY(grid_of(a.m * ceil_div(p.cols, 4), &blocks));
+    SLLM_BY_DTYPE(a.out_dtype, T, (join_splits<T><<<blocks, 256, 0, stream>>>(sums, splits, p.split_stride, a.m, p.cols,
+                                                                             static_cast<T*>(a.out), a.out_stride)));
+    SLLM_HIP(hipGetLastError());
+    return SLLM_OK;
+}
+
 // x as the wide kernel reads it, written out in the workspace where it is not so already.
 int32_t stage_x(const LinearLaunch& a, const Plan& p, void* workspace, WideArgs* w, hipStream_t stream) {
     w->x = static_cast<const __bf16*>(a.x.data);
@@ -261,14 +236,7 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
         w.out_args = o;
         SLLM_TRY(a.grad ? launch_wide<true>(w, p.splits, out, dtype, stream) : launch_wide<false>(w, p.splits, out, dtype, stream));
     }
-    if (p.splits > 1) {
-        uint32_t blocks;
-        SLLM_TRY(grid_of(a.m * o.stride / 4, &blocks));
-        SLLM_BY_DTYPE(a.out_dtype, T, (join_splits<T><<<blocks, 256, 0, stream>>>(static_cast<const float*>(out), p.splits, p.split_stride,
-                                                                                a.m, p.cols, static_cast<T*>(a.out), a.out_stride)));
-        SLLM_HIP(hipGetLastError());
-    }
-    return SLLM_OK;
+    return p.splits > 1 ? join(p, static_cast<const float*>(out), p.splits, a, stream) : SLLM_OK;
 }
 
 }  // namespace
@@ -285,16 +253,8 @@ int32_t launch_linear(const LinearLaunch& a, void* workspace, hipStream_t stream
                                         (uint32_t)ceil_div(a.k, 128), a.out, a.out_stride, a.out_dtype}, stream);
     }
     if (plan.depth) return launch_tiled(a, plan, workspace, stream);
-    const Product p{a.x, a.w_codes, a.w_scales, a.m, a.n, a.k, a.grad ? a.n : a.k, a.out, a.out_stride, a.out_dtype};
-    const uint64_t gx = ceil_div(a.grad ? a.k : a.n, 32), gy = ceil_div(a.m, 32);
-    if (gx > UINT32_MAX / 256 || gy > 65535) return fail(SLLM_E_RANGE, "product too large");
-    const dim3 grid((uint32_t)gx, (uint32_t)gy);
-    if (a.grad)
-        mx_product<true><<<grid, 256, 0, stream>>>(p);
-    else
-        mx_product<false><<<grid, 256, 0, stream>>>(p);
-    SLLM_HIP(hipGetLastError());
-    return SLLM_OK;
+    // a depth of zero: sums of nothing
+    return join(plan, nullptr, 0, a, stream);
 }
 
 }  // namespace sllm
