@@ -20,7 +20,7 @@ struct Wide {
     static constexpr int kABytes = BM * kStep * 2;
     static constexpr int kBBytes = Grad ? kStep * kPitch : BN * kStep * 2;
     static constexpr int kBlocks = BN * kStep / 32 / kThreads;     // blocks of W a lane expands a stage
-    static constexpr int kLoads = BM / 16 * 2 / kWaves;            // loads of x a wave issues a stage
+    static constexpr int kLoads = BM / 8 / kWaves;                 // loads of x a wave issues a stage
 };
 
 template <bool Grad, int BM, int BN, int WM, int WN, typename T>
@@ -33,7 +33,8 @@ __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) 
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t r = lane & 15, g = lane >> 4;
     const void* const zeros = zero_vector();
-    const uint64_t m0 = (uint64_t)blockIdx.x % a.tiles_m * BM, j0 = (uint64_t)blockIdx.x / a.tiles_m * BN;
+    const Tile tile = tile_of(blockIdx.x, a.tiles_m, a.tiles_j);
+    const uint64_t m0 = (uint64_t)tile.m * BM, j0 = (uint64_t)tile.j * BN;
     const uint32_t steps = a.steps * a.parts;
     const uint32_t t0 = (uint64_t)steps * blockIdx.y / gridDim.y, t1 = (uint64_t)steps * (blockIdx.y + 1) / gridDim.y;
 
@@ -43,41 +44,48 @@ __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) 
 #pragma unroll
         for (int m = 0; m < G::FM; ++m) acc[n][m] = f32x4{0, 0, 0, 0};
 
-    // x by loads straight to LDS: one load holds 16 rows x 32 of the depth
+    // x by loads straight to LDS: one load holds 8 rows x 64 of the depth, and
+    // a lane takes the same columns of each of its rows
+    static_assert(G::kWaves % 2 == 0, "");
+    const uint32_t x_col = (lane % 8 ^ (wave % 2 * 4 + lane / 16)) * 8;
+    const __bf16* x_at[G::kLoads];
+#pragma unroll
+    for (int q = 0; q < G::kLoads; ++q)
+        x_at[q] = a.x + min(m0 + (q * G::kWaves + wave) * 8 + lane / 8, a.m - 1) * a.x_stride + x_col;
     auto load_x = [&](uint32_t t, uint8_t* to) {
         const uint32_t part = t / a.steps;
-        const uint64_t d = (uint64_t)(t - part * a.steps) * kStep;
+        const uint64_t d = (uint64_t)(t - part * a.steps) * kStep, at = part * a.part_stride + d;
+        const bool inside = d + x_col < a.depth;
 #pragma unroll
         for (int q = 0; q < G::kLoads; ++q) {
-            const uint32_t at = q * G::kWaves + wave;
-            const uint64_t row = min(m0 + at / 2 * 16 + r, a.m - 1), c = d + (at % 2 * 4 + g) * 8;
-            const void* p = a.x + row * a.x_stride + part * a.part_stride + c;
-            load_to_lds(c < a.depth ? p : zeros, to + at * 1024);
+            const void* p = x_at[q] + at;
+            load_to_lds(inside ? p : zeros, to + (q * G::kWaves + wave) * 1024);
         }
     };
-    u32x4 codes[G::kBlocks];
-    uint32_t scales[G::kBlocks];
-    auto load_w = [&](uint32_t t) {
-        const uint64_t d = (uint64_t)(t % a.steps) * kStep;
+    // The blocks a lane expands, of two stages: a row's are neighbours then.
+    // Past the end of the depth x is zero, so any codes do under a finite scale.
+    u32x4 codes[2][G::kBlocks];
+    uint32_t scales[2][G::kBlocks];
+    const uint32_t w_in = Grad ? tid / (BN / 32) : tid % 2;  // this lane's place in a stage's depth: row or block
+    auto load_w = [&](uint32_t t, int to) {
+        const uint64_t s = t % a.steps;
 #pragma unroll
         for (int q = 0; q < G::kBlocks; ++q) {
-            const uint32_t i = q * G::kThreads + tid;
-            const uint64_t row = Grad ? d + i / (BN / 32) : j0 + i / 2;
-            const uint64_t b = Grad ? j0 / 32 + i % (BN / 32) : d / 32 + i % 2;
-            codes[q] = u32x4{0, 0, 0, 0};
-            scales[q] = 0;
-            if (row < a.w_rows && b < a.w_blocks) {
-                codes[q] = a.w_codes[row * a.w_blocks + b];
-                scales[q] = a.w_scales[row * a.w_scale_pitch + b];
-            }
+            const uint64_t row = Grad ? s * kStep + w_in + q * (G::kThreads / (BN / 32)) : j0 + (q * G::kThreads + tid) / 2;
+            const uint64_t b = Grad ? j0 / 32 + tid % (BN / 32) : s * 2 + w_in;
+            const uint64_t row_at = min(row, a.w_rows - 1), b_at = min(b, a.w_blocks - 1);
+            codes[to][q] = a.w_codes[row_at * a.w_blocks + b_at];
+            scales[to][q] = a.w_scales[row_at * a.w_scale_pitch + b_at];
         }
     };
-    auto store_w = [&](uint8_t* to) {
+    auto store_w = [&](uint32_t t, int from, uint8_t* to) {
+        const uint64_t s = t % a.steps;
 #pragma unroll
         for (int q = 0; q < G::kBlocks; ++q) {
-            const uint32_t i = q * G::kThreads + tid;
+            const bool inside = Grad ? s * kStep + w_in + q * (G::kThreads / (BN / 32)) < a.w_rows : s * 2 + w_in < a.w_blocks;
             u32x4 v[4];
-            expand(codes[q], scales[q], v);
+            expand(codes[from][q], inside ? scales[from][q] : 0, v);
+            const uint32_t i = q * G::kThreads + tid;
             if constexpr (Grad) {
                 const uint32_t row = i / (BN / 32), b = i % (BN / 32);
                 uint8_t* p = to + row * G::kPitch + b * 64;
@@ -93,24 +101,13 @@ __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) 
     };
 
     const uint32_t wm = wave % WM, wn = wave / WM;
-    if (t0 < t1) {
-        load_x(t0, lds_a0);
-        load_w(t0);
-        store_w(lds_b0);
-    }
-    auto stage = [&](uint32_t t, const uint8_t* a_now, uint8_t* a_next, const uint8_t* b_now, uint8_t* b_next) {
-        wait_loads();
-        __syncthreads();
-        if (t + 1 < t1) {
-            load_w(t + 1);
-            load_x(t + 1, a_next);
-        }
-        const uint32_t a_at = wm * G::FM * 2048 + (g >> 1) * 1024 + (g & 1) * 512 + r * 16;
+    const uint32_t c0 = chunk_at(r, 2 * g), c1 = chunk_at(r, 2 * g + 1);
+    auto stage = [&](const uint8_t* a_now, const uint8_t* b_now) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             bf16x8 x[G::FM], w[G::FN];
 #pragma unroll
-            for (int m = 0; m < G::FM; ++m) x[m] = *reinterpret_cast<const bf16x8*>(a_now + (a_at + m * 2048 + j * 256));
+            for (int m = 0; m < G::FM; ++m) x[m] = *reinterpret_cast<const bf16x8*>(a_now + ((wm * G::FM + m) * 2048 + (j ? c1 : c0)));
 #pragma unroll
             for (int n = 0; n < G::FN; ++n) {
                 if constexpr (Grad) {
@@ -133,11 +130,30 @@ __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) 
                 for (int m = 0; m < G::FM; ++m)
                     acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[n], x[m], acc[n][m], 0, 0, 0);
         }
-        if (t + 1 < t1) store_w(b_next);
     };
+    if (t0 < t1) {
+        load_x(t0, lds_a0);
+        load_w(t0, 0);
+        load_w(t0 + 1, 1);
+        store_w(t0, 0, lds_b0);
+    }
     for (uint32_t t = t0; t < t1; t += 2) {
-        stage(t, lds_a0, lds_a1, lds_b0, lds_b1);
-        if (t + 1 < t1) stage(t + 1, lds_a1, lds_a0, lds_b1, lds_b0);
+        wait_loads();
+        __syncthreads();
+        if (t + 1 < t1) load_x(t + 1, lds_a1);
+        stage(lds_a0, lds_b0);
+        if (t + 1 < t1) {
+            store_w(t + 1, 1, lds_b1);
+            wait_loads();
+            __syncthreads();
+            if (t + 2 < t1) {
+                load_x(t + 2, lds_a0);
+                load_w(t + 2, 0);
+                load_w(t + 3, 1);
+            }
+            stage(lds_a1, lds_b1);
+            if (t + 2 < t1) store_w(t + 2, 0, lds_b0);
+        }
     }
 
     store_tile<G::FM, G::FN>(acc, a.out_args, m0 + wm * G::FM * 16, j0 + wn * G::FN * 16, out);

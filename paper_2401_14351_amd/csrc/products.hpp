@@ -5,6 +5,8 @@
 
 namespace sllm {
 
+constexpr uint32_t kTileRows = 4;  // of tiles that neighbouring workgroups share
+
 // Where a product's sums go: m x cols, or, where the depth is split over
 // workgroups (blockIdx.y), a 32-bit matrix per split, one after another.
 struct OutArgs {
@@ -46,6 +48,27 @@ __device__ __forceinline__ void load_to_lds(const void* from, void* to) {
 
 // Every load of this wave has landed, those to LDS included.
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
+// The tile of a workgroup.  Workgroups go to the eight XCDs in turn; each XCD
+// takes a run of tiles of its own, four rows of tiles at a time, so that its
+// 32 CUs work on a patch of the output and find each other's operands in its L2.
+struct Tile {
+    uint32_t m, j;
+};
+__device__ __forceinline__ Tile tile_of(uint32_t block, uint32_t tiles_m, uint32_t tiles_j) {
+    const uint32_t tiles = tiles_m * tiles_j, xcd = block % 8, q = tiles / 8, rest = tiles % 8;
+    const uint32_t i = xcd * q + min(xcd, rest) + block / 8;
+    const uint32_t group = i / (kTileRows * tiles_j), in = i % (kTileRows * tiles_j);
+    const uint32_t rows = min(kTileRows, tiles_m - group * kTileRows);
+    return {group * kTileRows + in % rows, in / rows};
+}
+
+// Where chunk c (of eight, 16 bytes each) of row r of a tile lies in LDS.  Rows
+// are 128 bytes: eight lanes load one, whole, and a load straight to LDS puts
+// lane l's bytes at 16 l, so the order of a row's chunks is chosen by what each
+// lane loads.  It changes every other row, so that the 16 rows a fragment reads
+// in one column of chunks are in all banks once.
+__device__ __forceinline__ uint32_t chunk_at(uint32_t r, uint32_t c) { return r * 128 + (c ^ (r >> 1 & 7)) * 16; }
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
