@@ -14,7 +14,7 @@ constexpr uint32_t kStepBlocks = kNarrowStep / kMxBlock;
 
 template <int BM, int BN, int WM, int WN, typename T>
 __global__ __launch_bounds__(WM* WN * 64) void narrow_product(NarrowArgs a, T* out) {
-    constexpr int kWaves = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
+    constexpr int kWaves = WM * WN, FM = BM / WM / 32, FN = BN / WN / 32;
     constexpr int kRowBytes = kNarrowStep / 2;
     // The two stages are variables of their own: the compiler then sees that
     // loads into one do not touch what is read from the other.
@@ -23,7 +23,7 @@ __global__ __launch_bounds__(WM* WN * 64) void narrow_product(NarrowArgs a, T* o
     // scales of two stages: 16 bytes a row, x's rows then w's
     __shared__ __align__(16) uint8_t lds_s0[(BM + BN) * 16], lds_s1[(BM + BN) * 16];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t r = lane & 15, g = lane >> 4;
+    const uint32_t r = lane & 31, h = lane >> 5;
     const void* const zeros = zero_vector();
     const Tile tile = tile_of(blockIdx.x, a.tiles_m, a.tiles_j);
     const uint64_t m0 = (uint64_t)tile.m * BM, j0 = (uint64_t)tile.j * BN;
@@ -33,93 +33,127 @@ __global__ __launch_bounds__(WM* WN * 64) void narrow_product(NarrowArgs a, T* o
     const uint32_t t0 = (uint64_t)pairs * blockIdx.y / gridDim.y * 2;
     const uint32_t t1 = min((uint32_t)((uint64_t)pairs * (blockIdx.y + 1) / gridDim.y * 2), a.steps);
 
-    f32x4 acc[FN][FM];
+    f32x16 acc[FN][FM];
 #pragma unroll
     for (int n = 0; n < FN; ++n)
 #pragma unroll
-        for (int m = 0; m < FM; ++m) acc[n][m] = f32x4{0, 0, 0, 0};
+        for (int m = 0; m < FM; ++m) acc[n][m] = f32x16{};
 
-    // one load holds 8 rows x 8 blocks
+    // One load holds 8 rows x 8 blocks, and a lane takes the same blocks of each
+    // of its rows.
+    static_assert(kWaves % 2 == 0, "");
+    const uint32_t block = lane % 8 ^ (wave % 2 * 4 + lane / 16);
+    const u32x4 *x_at[BM / 8 / kWaves], *w_at[BN / 8 / kWaves];
+#pragma unroll
+    for (int q = 0; q < BM / 8 / kWaves; ++q)
+        x_at[q] = a.x_codes + min(m0 + (q * kWaves + wave) * 8 + lane / 8, a.m - 1) * a.blocks;
+#pragma unroll
+    for (int q = 0; q < BN / 8 / kWaves; ++q)
+        w_at[q] = a.w_codes + min(j0 + (q * kWaves + wave) * 8 + lane / 8, a.n - 1) * a.blocks;
+    // 16 scale bytes a row: two stages' worth, a lane each
+    static_assert((BM + BN) / 64 == kWaves, "");
+    const uint8_t* scales_at = wave < BM / 64 ? a.x_scales + min(m0 + tid, a.m - 1) * a.scale_pitch
+                                              : a.w_scales + min(j0 + tid - BM, a.n - 1) * a.scale_pitch;
     auto load = [&](uint32_t t, uint8_t* to_x, uint8_t* to_w) {
-        const uint64_t b0 = (uint64_t)t * kStepBlocks;
+        const uint64_t b = (uint64_t)t * kStepBlocks + block, at = min(b, a.blocks - 1);
 #pragma unroll
         for (int q = 0; q < BM / 8 / kWaves; ++q) {
-            const uint32_t at = q * kWaves + wave, row8 = at * 8 + lane / 8;
-            const uint64_t row = min(m0 + row8, a.m - 1), b = b0 + (lane % 8 ^ (row8 >> 1 & 7));
-            load_to_lds(b < a.blocks ? (const void*)(a.x_codes + row * a.blocks + b) : zeros, to_x + at * 1024);
+            const void* p = x_at[q] + at;
+            load_to_lds(b < a.blocks ? p : zeros, to_x + (q * kWaves + wave) * 1024);
         }
+        // past the end of the depth x is zero, so any finite values do
 #pragma unroll
-        for (int q = 0; q < BN / 8 / kWaves; ++q) {
-            // past the end of the depth x is zero, so any finite values do
-            const uint32_t at = q * kWaves + wave, row8 = at * 8 + lane / 8;
-            const uint64_t row = min(j0 + row8, a.n - 1), b = min(b0 + (lane % 8 ^ (row8 >> 1 & 7)), a.blocks - 1);
-            load_to_lds(a.w_codes + row * a.blocks + b, to_w + at * 1024);
-        }
+        for (int q = 0; q < BN / 8 / kWaves; ++q) load_to_lds(w_at[q] + at, to_w + (q * kWaves + wave) * 1024);
     };
-    // 16 scale bytes a row: two stages' worth, a lane each
-    auto load_scales = [&](uint32_t t, uint8_t* to) {
-        const uint64_t b0 = (uint64_t)t * kStepBlocks;
-#pragma unroll
-        for (int q = 0; q < (BM + BN) / 64 / kWaves; ++q) {
-            const uint32_t at = q * kWaves + wave, i = at * 64 + lane;
-            const uint8_t* p = at < BM / 64 ? a.x_scales + min(m0 + i, a.m - 1) * a.scale_pitch
-                                            : a.w_scales + min(j0 + i - BM, a.n - 1) * a.scale_pitch;
-            load_to_lds(p + b0, to + at * 1024);
-        }
+    auto load_scales = [&](uint32_t t, uint8_t* to) { load_to_lds(scales_at + (uint64_t)t * kStepBlocks, to + wave * 1024); };
+
+    // Of a stage, lane (r, h) multiplies blocks 4 h .. 4 h + 3 of its rows, one a
+    // step; a row's four scale bytes are one register.
+    struct Scales {
+        uint32_t x[FM], w[FN];
     };
-    // Lane (r, g) multiplies blocks 2 g and 2 g + 1 of its rows.
-    const uint32_t c0 = chunk_at(r, 2 * g), c1 = chunk_at(r, 2 * g + 1);
-    const uint32_t x_row = wm * FM * 16, w_row = wn * FN * 16;
-    auto stage = [&](uint32_t t, const uint8_t* x_now, const uint8_t* w_now, const uint8_t* s_now, uint32_t half) {
+    auto read_scales = [&](uint32_t t, const uint8_t* from) {
         // scale bytes past the row's end may hold anything
-        const uint64_t b = (uint64_t)t * kStepBlocks + 2 * g;
-        const uint32_t mask = b + 1 < a.blocks ? 0xffff : b < a.blocks ? 0xff : 0;
-        uint32_t xs[FM], ws[FN];
+        const uint64_t b = (uint64_t)t * kStepBlocks + 4 * h;
+        const uint32_t left = b < a.blocks ? (uint32_t)min(a.blocks - b, (uint64_t)4) : 0;
+        const uint32_t mask = left == 4 ? ~0u : (1u << left * 8) - 1;
+        Scales s;
 #pragma unroll
         for (int m = 0; m < FM; ++m)
-            xs[m] = *reinterpret_cast<const uint16_t*>(s_now + ((x_row + m * 16 + r) * 16 + half * 8 + g * 2)) & mask;
+            s.x[m] = *reinterpret_cast<const uint32_t*>(from + ((wm * FM + m) * 512 + r * 16 + t % 2 * 8 + h * 4)) & mask;
 #pragma unroll
         for (int n = 0; n < FN; ++n)
-            ws[n] = *reinterpret_cast<const uint16_t*>(s_now + ((BM + w_row + n * 16 + r) * 16 + half * 8 + g * 2)) & mask;
-        auto step = [&](auto which) {
-            constexpr int j = decltype(which)::value;
-            u32x4 x[FM];
-#pragma unroll
-            for (int m = 0; m < FM; ++m) x[m] = *reinterpret_cast<const u32x4*>(x_now + ((x_row + m * 16) * 128 + (j ? c1 : c0)));
-#pragma unroll
-            for (int n = 0; n < FN; ++n) {
-                const u32x4 w = *reinterpret_cast<const u32x4*>(w_now + ((w_row + n * 16) * 128 + (j ? c1 : c0)));
-#pragma unroll
-                for (int m = 0; m < FM; ++m)
-                    acc[n][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(w), fragment(x[m]), acc[n][m], 4, 4,
-                                                                                 j, ws[n], j, xs[m]);
-            }
-        };
-        step(std::integral_constant<int, 0>());
-        step(std::integral_constant<int, 1>());
+            s.w[n] = *reinterpret_cast<const uint32_t*>(from + (BM * 16 + (wn * FN + n) * 512 + r * 16 + t % 2 * 8 + h * 4)) & mask;
+        return s;
     };
-    // stages t and t + 1 with their scales; those of the next pair into `s_next`
-    auto pair = [&](uint32_t t, const uint8_t* s_now, uint8_t* s_next) {
+    struct Fragments {
+        u32x4 x[FM], w[FN];
+    };
+    const uint32_t chunk = chunk_at(r, 4 * h);
+    auto read = [&](const uint8_t* x_now, const uint8_t* w_now, uint32_t s) {
+        Fragments f;
+        const uint32_t c = chunk ^ s * 16;
+#pragma unroll
+        for (int n = 0; n < FN; ++n) f.w[n] = *reinterpret_cast<const u32x4*>(w_now + ((wn * FN + n) * 4096 + c));
+#pragma unroll
+        for (int m = 0; m < FM; ++m) f.x[m] = *reinterpret_cast<const u32x4*>(x_now + ((wm * FM + m) * 4096 + c));
+        return f;
+    };
+    auto multiply = [&](const Fragments& f, const Scales& s, auto which) {
+        constexpr int j = decltype(which)::value;
+        pin(acc);
+#pragma unroll
+        for (int m = 0; m < FM; ++m)
+#pragma unroll
+            for (int n = 0; n < FN; ++n)
+                acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fragment(f.w[n]), fragment(f.x[m]), acc[n][m], 4, 4, j,
+                                                                            s.w[n], j, s.x[m]);
+        pin(acc);
+    };
+    // While one step is multiplied the next is read; the next stage's first step
+    // past the barrier, where its loads have landed and this stage's buffers are
+    // free for the loads of the one after.
+    Fragments f0, f1;
+    Scales now, next;
+    auto stage = [&](uint32_t t, uint8_t* x_now, uint8_t* w_now, const uint8_t* x_next, const uint8_t* w_next, const uint8_t* scales,
+                     uint8_t* scales_to) {
+        f1 = read(x_now, w_now, 1);
+        multiply(f0, now, std::integral_constant<int, 0>());
+        f0 = read(x_now, w_now, 2);
+        multiply(f1, now, std::integral_constant<int, 1>());
+        f1 = read(x_now, w_now, 3);
+        multiply(f0, now, std::integral_constant<int, 2>());
         wait_loads();
         __syncthreads();
-        if (t + 1 < t1) load(t + 1, lds_x1, lds_w1);
-        if (t + 2 < t1) load_scales(t + 2, s_next);
-        stage(t, lds_x0, lds_w0, s_now, 0);
-        if (t + 1 >= t1) return;
-        wait_loads();
-        __syncthreads();
-        if (t + 2 < t1) load(t + 2, lds_x0, lds_w0);
-        stage(t + 1, lds_x1, lds_w1, s_now, 1);
+        if (t + 2 < t1) {
+            load(t + 2, x_now, w_now);
+            if (scales_to) load_scales(t + 2, scales_to);
+        }
+        f0 = read(x_next, w_next, 0);
+        next = read_scales(t + 1, scales);
+        multiply(f1, now, std::integral_constant<int, 3>());
+        now = next;
     };
     if (t0 < t1) {
         load(t0, lds_x0, lds_w0);
         load_scales(t0, lds_s0);
+        wait_loads();
+        __syncthreads();
+        if (t0 + 1 < t1) load(t0 + 1, lds_x1, lds_w1);
+        f0 = read(lds_x0, lds_w0, 0);
+        now = read_scales(t0, lds_s0);
     }
     for (uint32_t t = t0; t < t1; t += 4) {
-        pair(t, lds_s0, lds_s1);
-        if (t + 2 < t1) pair(t + 2, lds_s1, lds_s0);
+        stage(t, lds_x0, lds_w0, lds_x1, lds_w1, lds_s0, lds_s1);
+        if (t + 1 < t1) {
+            stage(t + 1, lds_x1, lds_w1, lds_x0, lds_w0, lds_s1, nullptr);
+            if (t + 2 < t1) {
+                stage(t + 2, lds_x0, lds_w0, lds_x1, lds_w1, lds_s1, lds_s0);
+                if (t + 3 < t1) stage(t + 3, lds_x1, lds_w1, lds_x0, lds_w0, lds_s0, nullptr);
+            }
+        }
     }
-    store_tile<FM, FN>(acc, a.out_args, m0 + wm * FM * 16, j0 + wn * FN * 16, out);
+    store_tile<FM, FN>(acc, a.out_args, m0 + wm * FM * 32, j0 + wn * FN * 32, out);
 }
 
 }  // namespace

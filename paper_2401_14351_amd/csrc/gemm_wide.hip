@@ -12,151 +12,162 @@ namespace {
 
 constexpr uint32_t kStep = kWideStep;
 
-template <bool Grad, int BM, int BN, int WM, int WN>
-struct Wide {
-    static constexpr int kThreads = WM * WN * 64, kWaves = WM * WN;
-    static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;     // fragments of a wave
-    static constexpr int kPitch = BN * 2 + 32;                     // bytes of a row of W's tile in LDS (Grad)
-    static constexpr int kABytes = BM * kStep * 2;
-    static constexpr int kBBytes = Grad ? kStep * kPitch : BN * kStep * 2;
-    static constexpr int kBlocks = BN * kStep / 32 / kThreads;     // blocks of W a lane expands a stage
-    static constexpr int kLoads = BM / 8 / kWaves;                 // loads of x a wave issues a stage
-};
-
 template <bool Grad, int BM, int BN, int WM, int WN, typename T>
 __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) {
-    using G = Wide<Grad, BM, BN, WM, WN>;
+    constexpr int kThreads = WM * WN * 64, kWaves = WM * WN, FM = BM / WM / 32, FN = BN / WN / 32;
+    constexpr int kLoads = BM / 8 / kWaves;               // loads of x a wave issues a stage
+    constexpr int kBlocks = BN * kStep / 32 / kThreads;   // blocks of W a lane expands a stage
+    constexpr int kPitch = BN * 2 + 32;                   // bytes of a row of W's tile in LDS (Grad)
+    constexpr int kXBytes = BM * kStep * 2, kWBytes = Grad ? kStep * kPitch : BN * kStep * 2;
     // The two stages are variables of their own: the compiler then sees that
     // loads into one do not touch what is read from the other.
-    __shared__ __align__(16) uint8_t lds_a0[G::kABytes], lds_a1[G::kABytes];
-    __shared__ __align__(16) uint8_t lds_b0[G::kBBytes], lds_b1[G::kBBytes];
+    __shared__ __align__(16) uint8_t lds_x0[kXBytes], lds_x1[kXBytes];
+    __shared__ __align__(16) uint8_t lds_w0[kWBytes], lds_w1[kWBytes];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t r = lane & 15, g = lane >> 4;
+    const uint32_t r = lane & 31, h = lane >> 5;
     const void* const zeros = zero_vector();
     const Tile tile = tile_of(blockIdx.x, a.tiles_m, a.tiles_j);
     const uint64_t m0 = (uint64_t)tile.m * BM, j0 = (uint64_t)tile.j * BN;
     const uint32_t steps = a.steps * a.parts;
     const uint32_t t0 = (uint64_t)steps * blockIdx.y / gridDim.y, t1 = (uint64_t)steps * (blockIdx.y + 1) / gridDim.y;
+    const uint32_t wm = wave % WM, wn = wave / WM;
 
-    f32x4 acc[G::FN][G::FM];
+    f32x16 acc[FN][FM];
 #pragma unroll
-    for (int n = 0; n < G::FN; ++n)
+    for (int n = 0; n < FN; ++n)
 #pragma unroll
-        for (int m = 0; m < G::FM; ++m) acc[n][m] = f32x4{0, 0, 0, 0};
+        for (int m = 0; m < FM; ++m) acc[n][m] = f32x16{};
 
     // x by loads straight to LDS: one load holds 8 rows x 64 of the depth, and
     // a lane takes the same columns of each of its rows
-    static_assert(G::kWaves % 2 == 0, "");
+    static_assert(kWaves % 2 == 0, "");
     const uint32_t x_col = (lane % 8 ^ (wave % 2 * 4 + lane / 16)) * 8;
-    const __bf16* x_at[G::kLoads];
+    const __bf16* x_at[kLoads];
 #pragma unroll
-    for (int q = 0; q < G::kLoads; ++q)
-        x_at[q] = a.x + min(m0 + (q * G::kWaves + wave) * 8 + lane / 8, a.m - 1) * a.x_stride + x_col;
+    for (int q = 0; q < kLoads; ++q) x_at[q] = a.x + min(m0 + (q * kWaves + wave) * 8 + lane / 8, a.m - 1) * a.x_stride + x_col;
     auto load_x = [&](uint32_t t, uint8_t* to) {
         const uint32_t part = t / a.steps;
         const uint64_t d = (uint64_t)(t - part * a.steps) * kStep, at = part * a.part_stride + d;
         const bool inside = d + x_col < a.depth;
 #pragma unroll
-        for (int q = 0; q < G::kLoads; ++q) {
+        for (int q = 0; q < kLoads; ++q) {
             const void* p = x_at[q] + at;
-            load_to_lds(inside ? p : zeros, to + (q * G::kWaves + wave) * 1024);
+            load_to_lds(inside ? p : zeros, to + (q * kWaves + wave) * 1024);
         }
     };
     // The blocks a lane expands, of two stages: a row's are neighbours then.
     // Past the end of the depth x is zero, so any codes do under a finite scale.
-    u32x4 codes[2][G::kBlocks];
-    uint32_t scales[2][G::kBlocks];
+    u32x4 codes[2][kBlocks];
+    uint32_t scales[2][kBlocks];
     const uint32_t w_in = Grad ? tid / (BN / 32) : tid % 2;  // this lane's place in a stage's depth: row or block
     auto load_w = [&](uint32_t t, int to) {
         const uint64_t s = t % a.steps;
 #pragma unroll
-        for (int q = 0; q < G::kBlocks; ++q) {
-            const uint64_t row = Grad ? s * kStep + w_in + q * (G::kThreads / (BN / 32)) : j0 + (q * G::kThreads + tid) / 2;
+        for (int q = 0; q < kBlocks; ++q) {
+            const uint64_t row = Grad ? s * kStep + w_in + q * (kThreads / (BN / 32)) : j0 + (q * kThreads + tid) / 2;
             const uint64_t b = Grad ? j0 / 32 + tid % (BN / 32) : s * 2 + w_in;
             const uint64_t row_at = min(row, a.w_rows - 1), b_at = min(b, a.w_blocks - 1);
             codes[to][q] = a.w_codes[row_at * a.w_blocks + b_at];
             scales[to][q] = a.w_scales[row_at * a.w_scale_pitch + b_at];
         }
     };
+    // W's tile in LDS: like x's, rows of the weight by the depth, or (Grad) rows
+    // of the depth by the tile's columns, whose order changes from block to block
+    // so that a wave's stores reach all banks.
     auto store_w = [&](uint32_t t, int from, uint8_t* to) {
         const uint64_t s = t % a.steps;
 #pragma unroll
-        for (int q = 0; q < G::kBlocks; ++q) {
-            const bool inside = Grad ? s * kStep + w_in + q * (G::kThreads / (BN / 32)) < a.w_rows : s * 2 + w_in < a.w_blocks;
+        for (int q = 0; q < kBlocks; ++q) {
+            const bool inside = Grad ? s * kStep + w_in + q * (kThreads / (BN / 32)) < a.w_rows : s * 2 + w_in < a.w_blocks;
             u32x4 v[4];
             expand(codes[from][q], inside ? scales[from][q] : 0, v);
-            const uint32_t i = q * G::kThreads + tid;
-            if constexpr (Grad) {
-                const uint32_t row = i / (BN / 32), b = i % (BN / 32);
-                uint8_t* p = to + row * G::kPitch + b * 64;
+            const uint32_t i = q * kThreads + tid;
 #pragma unroll
-                for (uint32_t w = 0; w < 4; ++w) *reinterpret_cast<u32x4*>(p + (w ^ (b & 3)) * 16) = v[w];
-            } else {
-                const uint32_t row = i / 2, b = i % 2;
-                uint8_t* p = to + row / 16 * 2048 + b * 512 + row % 16 * 16;
-#pragma unroll
-                for (uint32_t w = 0; w < 4; ++w) *reinterpret_cast<u32x4*>(p + w % 2 * 1024 + w / 2 * 256) = v[w];
+            for (uint32_t w = 0; w < 4; ++w) {
+                const uint32_t at = Grad ? i / (BN / 32) * kPitch + i % (BN / 32) * 64 + (w ^ (i & 3)) * 16
+                                         : chunk_at(i / 2, i % 2 * 4) ^ w * 16;
+                *reinterpret_cast<u32x4*>(to + at) = v[w];
             }
         }
     };
 
-    const uint32_t wm = wave % WM, wn = wave / WM;
-    const uint32_t c0 = chunk_at(r, 2 * g), c1 = chunk_at(r, 2 * g + 1);
-    auto stage = [&](const uint8_t* a_now, const uint8_t* b_now) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            bf16x8 x[G::FM], w[G::FN];
-#pragma unroll
-            for (int m = 0; m < G::FM; ++m) x[m] = *reinterpret_cast<const bf16x8*>(a_now + ((wm * G::FM + m) * 2048 + (j ? c1 : c0)));
-#pragma unroll
-            for (int n = 0; n < G::FN; ++n) {
-                if constexpr (Grad) {
-                    // four rows of the tile and 16 columns a read, transposed: lane r gets column r
-                    const uint32_t f = wn * G::FN + n, b = f >> 1;
-                    const uint32_t piece = (2 * (f & 1) + (r >> 1 & 1)) ^ (b & 3);
-                    const uint8_t* p = b_now + (16 * g + 8 * j + (r >> 2)) * G::kPitch + b * 64 + piece * 16 + (r & 1) * 8;
-                    typedef short s16x4 __attribute__((ext_vector_type(4)));
-                    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * G::kPitch));
-                    w[n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                } else {
-                    w[n] = *reinterpret_cast<const bf16x8*>(b_now + (wn * G::FN * 2048 + lane * 16 + n * 2048 + j * 1024));
-                }
-            }
-#pragma unroll
-            for (int n = 0; n < G::FN; ++n)
-#pragma unroll
-                for (int m = 0; m < G::FM; ++m)
-                    acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[n], x[m], acc[n][m], 0, 0, 0);
-        }
+    struct Fragments {
+        bf16x8 x[FM], w[FN];
     };
-    if (t0 < t1) {
-        load_x(t0, lds_a0);
-        load_w(t0, 0);
-        load_w(t0 + 1, 1);
-        store_w(t0, 0, lds_b0);
-    }
-    for (uint32_t t = t0; t < t1; t += 2) {
+    // Step s of a stage is, in lane (r, h), eight of the depth from 32 h + 8 s.
+    const uint32_t chunk = chunk_at(r, 4 * h);
+    auto read = [&](const uint8_t* x_now, const uint8_t* w_now, uint32_t s) {
+        Fragments f;
+        const uint32_t c = chunk ^ s * 16;
+#pragma unroll
+        for (int n = 0; n < FN; ++n) {
+            if constexpr (Grad) {
+                // Four rows of the tile and 16 columns a read and 16 lanes,
+                // transposed: a lane gets a column.
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+                const uint32_t b = wn * FN + n, l = lane & 15;
+                const uint32_t piece = ((lane >> 4 & 1) * 2 + (l >> 1 & 1)) ^ (b & 3);
+                const uint32_t at = (32 * h + 8 * s + (l >> 2)) * kPitch + b * 64 + piece * 16 + (l & 1) * 8;
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(w_now + at));
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(w_now + (at + 4 * kPitch)));
+                f.w[n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            } else {
+                f.w[n] = *reinterpret_cast<const bf16x8*>(w_now + ((wn * FN + n) * 4096 + c));
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < FM; ++m) f.x[m] = *reinterpret_cast<const bf16x8*>(x_now + ((wm * FM + m) * 4096 + c));
+        return f;
+    };
+    auto multiply = [&](const Fragments& f) {
+        pin(acc);
+#pragma unroll
+        for (int m = 0; m < FM; ++m)
+#pragma unroll
+            for (int n = 0; n < FN; ++n) acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.w[n], f.x[m], acc[n][m], 0, 0, 0);
+        pin(acc);
+    };
+    // While one step is multiplied the next is read; the next stage's first step
+    // past the barrier, where its loads have landed and this stage's buffers are
+    // free for the loads of the one after.
+    Fragments f0, f1;
+    auto stage = [&](uint32_t t, int parity, uint8_t* x_now, const uint8_t* w_now, const uint8_t* x_next, uint8_t* w_next) {
+        f1 = read(x_now, w_now, 1);
+        multiply(f0);
+        f0 = read(x_now, w_now, 2);
+        multiply(f1);
+        f1 = read(x_now, w_now, 3);
+        if (t + 1 < t1) store_w(t + 1, parity ^ 1, w_next);
+        multiply(f0);
         wait_loads();
         __syncthreads();
-        if (t + 1 < t1) load_x(t + 1, lds_a1);
-        stage(lds_a0, lds_b0);
-        if (t + 1 < t1) {
-            store_w(t + 1, 1, lds_b1);
-            wait_loads();
-            __syncthreads();
-            if (t + 2 < t1) {
-                load_x(t + 2, lds_a0);
+        if (t + 2 < t1) {
+            load_x(t + 2, x_now);
+            if (parity == 0) {
                 load_w(t + 2, 0);
                 load_w(t + 3, 1);
             }
-            stage(lds_a1, lds_b1);
-            if (t + 2 < t1) store_w(t + 2, 0, lds_b0);
         }
+        f0 = read(x_next, w_next, 0);
+        multiply(f1);
+    };
+    if (t0 < t1) {
+        load_x(t0, lds_x0);
+        load_w(t0, 0);
+        load_w(t0 + 1, 1);
+        store_w(t0, 0, lds_w0);
+        wait_loads();
+        __syncthreads();
+        if (t0 + 1 < t1) load_x(t0 + 1, lds_x1);
+        f0 = read(lds_x0, lds_w0, 0);
+    }
+    for (uint32_t t = t0; t < t1; t += 2) {
+        stage(t, 0, lds_x0, lds_w0, lds_x1, lds_w1);
+        if (t + 1 < t1) stage(t + 1, 1, lds_x1, lds_w1, lds_x0, lds_w0);
     }
 
-    store_tile<G::FM, G::FN>(acc, a.out_args, m0 + wm * G::FM * 16, j0 + wn * G::FN * 16, out);
+    store_tile<FM, FN>(acc, a.out_args, m0 + wm * FM * 32, j0 + wn * FN * 32, out);
 }
 
 }  // namespace

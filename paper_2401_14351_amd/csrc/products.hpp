@@ -66,8 +66,8 @@ __device__ __forceinline__ Tile tile_of(uint32_t block, uint32_t tiles_m, uint32
 // Where chunk c (of eight, 16 bytes each) of row r of a tile lies in LDS.  Rows
 // are 128 bytes: eight lanes load one, whole, and a load straight to LDS puts
 // lane l's bytes at 16 l, so the order of a row's chunks is chosen by what each
-// lane loads.  It changes every other row, so that the 16 rows a fragment reads
-// in one column of chunks are in all banks once.
+// lane loads.  It changes every other row, so that 16 rows read in one column of
+// chunks are in all banks once.  chunk_at(r, c ^ s) is chunk_at(r, c) ^ 16 s.
 __device__ __forceinline__ uint32_t chunk_at(uint32_t r, uint32_t c) { return r * 128 + (c ^ (r >> 1 & 7)) * 16; }
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -99,30 +99,47 @@ __device__ __forceinline__ uint32_t leading_bf16(float& f) {
     return finite || !(bits & 0x7fffff) ? bits >> 16 : 0x7fc0;
 }
 
-// A wave's accumulators: fragment [n][m] holds, in lane (r, g), columns
-// n * 16 + 4 g .. + 3 of row m * 16 + r.
+// Keeps products between the reads before and after them.  Matrix instructions
+// have no order of their own against loads and barriers: the compiler puts a
+// stage's products off past its barrier, and holds all of its fragments till
+// then in more registers than there are, or makes them before the reads that
+// they are meant to hide.
+template <int FM, int FN>
+__device__ __forceinline__ void pin(f32x16 (&acc)[FN][FM]) {
+#pragma unroll
+    for (int n = 0; n < FN; ++n)
+#pragma unroll
+        for (int m = 0; m < FM; ++m) asm volatile("" : "+v"(acc[n][m]));
+}
+
+// A wave's accumulators: element 4 q + i of fragment [n][m] is, in lane (r, h) of
+// two halves of 32, column n * 32 + 8 q + 4 h + i of row m * 32 + r.
 template <int FM, int FN, typename T>
-__device__ __forceinline__ void store_tile(const f32x4 (&acc)[FN][FM], const OutArgs& o, uint64_t m0, uint64_t j0, T* out) {
-    const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+__device__ __forceinline__ void store_tile(const f32x16 (&acc)[FN][FM], const OutArgs& o, uint64_t m0, uint64_t j0, T* out) {
+    const uint32_t lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
     out += blockIdx.y * o.split_stride;
 #pragma unroll
     for (int m = 0; m < FM; ++m) {
-        const uint64_t row = m0 + m * 16 + r;
+        const uint64_t row = m0 + m * 32 + r;
         if (row >= o.m) continue;
         T* p = out + row * o.stride;
 #pragma unroll
-        for (int n = 0; n < FN; ++n) {
-            const uint64_t j = j0 + n * 16 + g * 4;
-            if (o.vector && j + 4 <= o.cols) {
-                typedef T T4 __attribute__((ext_vector_type(4)));
-                *reinterpret_cast<T4*>(p + j) = T4{from_f32<T>(acc[n][m][0]), from_f32<T>(acc[n][m][1]),
-                                                   from_f32<T>(acc[n][m][2]), from_f32<T>(acc[n][m][3])};
-            } else {
+        for (int n = 0; n < FN; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (j + i < o.cols) p[j + i] = from_f32<T>(acc[n][m][i]);
+            for (int q = 0; q < 4; ++q) {
+                const uint64_t j = j0 + n * 32 + q * 8 + h * 4;
+                T v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(acc[n][m][4 * q + i]);
+                if (o.vector && j + 4 <= o.cols) {
+                    typedef T T4 __attribute__((ext_vector_type(4)));
+                    *reinterpret_cast<T4*>(p + j) = T4{v[0], v[1], v[2], v[3]};
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (j + i < o.cols) p[j + i] = v[i];
+                }
             }
-        }
     }
 }
 
