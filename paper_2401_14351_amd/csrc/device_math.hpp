@@ -27,6 +27,10 @@ __device__ __forceinline__ T from_f32(float v) {
     return (T)v;
 }
 
+// On a lambda of a kernel: one that is not inlined takes what it captures, the
+// accumulators among it, through memory.
+#define SLLM_INLINE __attribute__((always_inline))
+
 // Run F<T> for the element type of a dtype code.
 #define SLLM_BY_DTYPE(dtype, T, ...)          \
     do {                                      \

@@ -11,27 +11,24 @@ namespace sllm {
 namespace {
 
 constexpr uint32_t kStepBlocks = kNarrowStep / kMxBlock;
+constexpr uint32_t kStageBlocks = 4;  // of a stage: 64 bytes a row
 
 template <int BM, int BN, int WM, int WN, typename T>
 __global__ __launch_bounds__(WM* WN * 64) void narrow_product(NarrowArgs a, T* out) {
     constexpr int kWaves = WM * WN, FM = BM / WM / 32, FN = BN / WN / 32;
-    constexpr int kRowBytes = kNarrowStep / 2;
-    // The two stages are variables of their own: the compiler then sees that
-    // loads into one do not touch what is read from the other.
-    __shared__ __align__(16) uint8_t lds_x0[BM * kRowBytes], lds_x1[BM * kRowBytes];
-    __shared__ __align__(16) uint8_t lds_w0[BN * kRowBytes], lds_w1[BN * kRowBytes];
-    // scales of two stages: 16 bytes a row, x's rows then w's
-    __shared__ __align__(16) uint8_t lds_s0[(BM + BN) * 16], lds_s1[(BM + BN) * 16];
+    // The stages in flight are variables of their own: the compiler then sees
+    // that loads into one do not touch what is read from another.
+    constexpr int kStageBytes = (BM + BN) * 64;
+    __shared__ __align__(16) uint8_t b0[kStageBytes], b1[kStageBytes], b2[kStageBytes], b3[kStageBytes];
+    // scales of four stages: 16 bytes a row, x's rows then w's
+    __shared__ __align__(16) uint8_t s0[(BM + BN) * 16], s1[(BM + BN) * 16];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t r = lane & 31, h = lane >> 5;
     const void* const zeros = zero_vector();
     const Tile tile = tile_of(blockIdx.x, a.tiles_m, a.tiles_j);
     const uint64_t m0 = (uint64_t)tile.m * BM, j0 = (uint64_t)tile.j * BN;
     const uint32_t wm = wave % WM, wn = wave / WM;
-    // splits begin at pairs of stages, which share their scales
-    const uint32_t pairs = (a.steps + 1) / 2;
-    const uint32_t t0 = (uint64_t)pairs * blockIdx.y / gridDim.y * 2;
-    const uint32_t t1 = min((uint32_t)((uint64_t)pairs * (blockIdx.y + 1) / gridDim.y * 2), a.steps);
+    const uint32_t t0 = (uint64_t)a.steps * blockIdx.y / gridDim.y, t1 = (uint64_t)a.steps * (blockIdx.y + 1) / gridDim.y;
 
     f32x16 acc[FN][FM];
 #pragma unroll
@@ -39,67 +36,76 @@ __global__ __launch_bounds__(WM* WN * 64) void narrow_product(NarrowArgs a, T* o
 #pragma unroll
         for (int m = 0; m < FM; ++m) acc[n][m] = f32x16{};
 
-    // One load holds 8 rows x 8 blocks, and a lane takes the same blocks of each
+    // One load holds 16 rows x 4 blocks, and a lane takes the same block of each
     // of its rows.
-    static_assert(kWaves % 2 == 0, "");
-    const uint32_t block = lane % 8 ^ (wave % 2 * 4 + lane / 16);
-    const u32x4 *x_at[BM / 8 / kWaves], *w_at[BN / 8 / kWaves];
+    constexpr int kXLoads = BM / 16 / kWaves, kWLoads = BN / 16 / kWaves;
+    const uint32_t block = lane % 4 ^ lane / 16;
+    const u32x4 *x_at[kXLoads], *w_at[kWLoads];
 #pragma unroll
-    for (int q = 0; q < BM / 8 / kWaves; ++q)
-        x_at[q] = a.x_codes + min(m0 + (q * kWaves + wave) * 8 + lane / 8, a.m - 1) * a.blocks;
+    for (int q = 0; q < kXLoads; ++q) x_at[q] = a.x_codes + min(m0 + (q * kWaves + wave) * 16 + lane / 4, a.m - 1) * a.blocks;
 #pragma unroll
-    for (int q = 0; q < BN / 8 / kWaves; ++q)
-        w_at[q] = a.w_codes + min(j0 + (q * kWaves + wave) * 8 + lane / 8, a.n - 1) * a.blocks;
-    // 16 scale bytes a row: two stages' worth, a lane each
-    static_assert((BM + BN) / 64 == kWaves, "");
-    const uint8_t* scales_at = wave < BM / 64 ? a.x_scales + min(m0 + tid, a.m - 1) * a.scale_pitch
-                                              : a.w_scales + min(j0 + tid - BM, a.n - 1) * a.scale_pitch;
-    auto load = [&](uint32_t t, uint8_t* to_x, uint8_t* to_w) {
-        const uint64_t b = (uint64_t)t * kStepBlocks + block, at = min(b, a.blocks - 1);
+    for (int q = 0; q < kWLoads; ++q) w_at[q] = a.w_codes + min(j0 + (q * kWaves + wave) * 16 + lane / 4, a.n - 1) * a.blocks;
+    // 16 scale bytes a row: four stages' worth, a lane each
+    constexpr int kScaleLoads = (BM + BN) / 64 / kWaves;
+    const uint8_t* scales_at[kScaleLoads];
 #pragma unroll
-        for (int q = 0; q < BM / 8 / kWaves; ++q) {
-            const void* p = x_at[q] + at;
-            load_to_lds(b < a.blocks ? p : zeros, to_x + (q * kWaves + wave) * 1024);
+    for (int q = 0; q < kScaleLoads; ++q) {
+        const uint32_t at = q * kWaves + wave, i = at * 64 + lane;
+        scales_at[q] = at < BM / 64 ? a.x_scales + min(m0 + i, a.m - 1) * a.scale_pitch
+                                    : a.w_scales + min(j0 + i - BM, a.n - 1) * a.scale_pitch;
+    }
+    // Stages are counted in blocks of the depth.  Every stage loads, those past
+    // the end too, so that the loads to wait for can be told by their number.
+    constexpr int kLoads = kXLoads + kWLoads;
+    auto load = [&](uint64_t at, uint8_t* to) SLLM_INLINE {
+        const uint64_t b = at + block, inside = min(b, a.blocks - 1);
+#pragma unroll
+        for (int q = 0; q < kXLoads; ++q) {
+            const void* p = x_at[q] + inside;
+            load_to_lds(b < a.blocks ? p : zeros, to + (q * kWaves + wave) * 1024);
         }
         // past the end of the depth x is zero, so any finite values do
 #pragma unroll
-        for (int q = 0; q < BN / 8 / kWaves; ++q) load_to_lds(w_at[q] + at, to_w + (q * kWaves + wave) * 1024);
+        for (int q = 0; q < kWLoads; ++q) load_to_lds(w_at[q] + inside, to + (BM * 64 + (q * kWaves + wave) * 1024));
     };
-    auto load_scales = [&](uint32_t t, uint8_t* to) { load_to_lds(scales_at + (uint64_t)t * kStepBlocks, to + wave * 1024); };
+    auto load_scales = [&](uint32_t t, uint8_t* to) SLLM_INLINE {
+        const uint64_t b = min((uint64_t)t * kStepBlocks, a.scale_pitch - kStepBlocks);
+#pragma unroll
+        for (int q = 0; q < kScaleLoads; ++q) load_to_lds(scales_at[q] + b, to + (q * kWaves + wave) * 1024);
+    };
 
-    // Of a stage, lane (r, h) multiplies blocks 4 h .. 4 h + 3 of its rows, one a
-    // step; a row's four scale bytes are one register.
+    // Of a stage, lane (r, h) multiplies blocks 2 h and 2 h + 1 of its rows, one a
+    // step; a row's two scale bytes are one register.
     struct Scales {
         uint32_t x[FM], w[FN];
     };
-    auto read_scales = [&](uint32_t t, const uint8_t* from) {
+    auto read_scales = [&](uint64_t at, const uint8_t* from, uint32_t stage) SLLM_INLINE {
         // scale bytes past the row's end may hold anything
-        const uint64_t b = (uint64_t)t * kStepBlocks + 4 * h;
-        const uint32_t left = b < a.blocks ? (uint32_t)min(a.blocks - b, (uint64_t)4) : 0;
-        const uint32_t mask = left == 4 ? ~0u : (1u << left * 8) - 1;
+        const uint64_t b = at + 2 * h;
+        const uint32_t mask = b + 1 < a.blocks ? 0xffff : b < a.blocks ? 0xff : 0;
         Scales s;
 #pragma unroll
         for (int m = 0; m < FM; ++m)
-            s.x[m] = *reinterpret_cast<const uint32_t*>(from + ((wm * FM + m) * 512 + r * 16 + t % 2 * 8 + h * 4)) & mask;
+            s.x[m] = *reinterpret_cast<const uint16_t*>(from + ((wm * FM + m) * 512 + r * 16 + h * 2 + stage * 4)) & mask;
 #pragma unroll
         for (int n = 0; n < FN; ++n)
-            s.w[n] = *reinterpret_cast<const uint32_t*>(from + (BM * 16 + (wn * FN + n) * 512 + r * 16 + t % 2 * 8 + h * 4)) & mask;
+            s.w[n] = *reinterpret_cast<const uint16_t*>(from + (BM * 16 + (wn * FN + n) * 512 + r * 16 + h * 2 + stage * 4)) & mask;
         return s;
     };
     struct Fragments {
         u32x4 x[FM], w[FN];
     };
-    const uint32_t chunk = chunk_at(r, 4 * h);
-    auto read = [&](const uint8_t* x_now, const uint8_t* w_now, uint32_t s) {
+    const uint32_t chunk = short_chunk_at(r, 2 * h);
+    auto read = [&](const uint8_t* from, uint32_t s) SLLM_INLINE {
         Fragments f;
         const uint32_t c = chunk ^ s * 16;
 #pragma unroll
-        for (int n = 0; n < FN; ++n) f.w[n] = *reinterpret_cast<const u32x4*>(w_now + ((wn * FN + n) * 4096 + c));
+        for (int n = 0; n < FN; ++n) f.w[n] = *reinterpret_cast<const u32x4*>(from + (BM * 64 + (wn * FN + n) * 2048 + c));
 #pragma unroll
-        for (int m = 0; m < FM; ++m) f.x[m] = *reinterpret_cast<const u32x4*>(x_now + ((wm * FM + m) * 4096 + c));
+        for (int m = 0; m < FM; ++m) f.x[m] = *reinterpret_cast<const u32x4*>(from + ((wm * FM + m) * 2048 + c));
         return f;
     };
-    auto multiply = [&](const Fragments& f, const Scales& s, auto which) {
+    auto multiply = [&](const Fragments& f, const Scales& s, auto which) SLLM_INLINE {
         constexpr int j = decltype(which)::value;
         pin(acc);
 #pragma unroll
@@ -110,50 +116,54 @@ __global__ __launch_bounds__(WM* WN * 64) void narrow_product(NarrowArgs a, T* o
                                                                             s.w[n], j, s.x[m]);
         pin(acc);
     };
-    // While one step is multiplied the next is read; the next stage's first step
-    // past the barrier, where its loads have landed and this stage's buffers are
-    // free for the loads of the one after.
+    // A ring of four stages, three of them in flight.  While one step is
+    // multiplied the next is read; the next stage's first step past the barrier,
+    // where its loads have landed.  The buffer of the stage before is free from
+    // its barrier on and takes the loads of the third stage ahead.
     Fragments f0, f1;
-    Scales now, next;
-    auto stage = [&](uint32_t t, uint8_t* x_now, uint8_t* w_now, const uint8_t* x_next, const uint8_t* w_next, const uint8_t* scales,
-                     uint8_t* scales_to) {
-        f1 = read(x_now, w_now, 1);
+    Scales now;
+    auto stage = [&](uint64_t at, const uint8_t* here, const uint8_t* next_one, uint8_t* last, const uint8_t* scales,
+                     uint32_t next_stage, auto more) SLLM_INLINE {
+        f1 = read(here, 1);
+        load(at + 3 * kStageBlocks, last);
+        more();
         multiply(f0, now, std::integral_constant<int, 0>());
-        f0 = read(x_now, w_now, 2);
+        wait_but_loads<2 * kLoads>();  // younger than the next stage's: those of the two after it
+        barrier();
+        f0 = read(next_one, 0);
+        const Scales next = read_scales(at + kStageBlocks, scales, next_stage);
         multiply(f1, now, std::integral_constant<int, 1>());
-        f1 = read(x_now, w_now, 3);
-        multiply(f0, now, std::integral_constant<int, 2>());
-        wait_loads();
-        __syncthreads();
-        if (t + 2 < t1) {
-            load(t + 2, x_now, w_now);
-            if (scales_to) load_scales(t + 2, scales_to);
-        }
-        f0 = read(x_next, w_next, 0);
-        next = read_scales(t + 1, scales);
-        multiply(f1, now, std::integral_constant<int, 3>());
         now = next;
     };
+    auto four_stages = [&](uint32_t t, uint8_t* s_now, uint8_t* s_next) SLLM_INLINE {
+        const uint64_t at = (uint64_t)t * kStepBlocks;
+        const auto none = []() SLLM_INLINE {};
+        stage(at, b0, b1, b3, s_now, 1, [&]() SLLM_INLINE { load_scales(t + 1, s_next); });
+        stage(at + 4, b1, b2, b0, s_now, 2, none);
+        stage(at + 8, b2, b3, b1, s_now, 3, none);
+        stage(at + 12, b3, b0, b2, s_next, 0, none);
+    };
     if (t0 < t1) {
-        load(t0, lds_x0, lds_w0);
-        load_scales(t0, lds_s0);
-        wait_loads();
-        __syncthreads();
-        if (t0 + 1 < t1) load(t0 + 1, lds_x1, lds_w1);
-        f0 = read(lds_x0, lds_w0, 0);
-        now = read_scales(t0, lds_s0);
-    }
-    for (uint32_t t = t0; t < t1; t += 4) {
-        stage(t, lds_x0, lds_w0, lds_x1, lds_w1, lds_s0, lds_s1);
-        if (t + 1 < t1) {
-            stage(t + 1, lds_x1, lds_w1, lds_x0, lds_w0, lds_s1, nullptr);
-            if (t + 2 < t1) {
-                stage(t + 2, lds_x0, lds_w0, lds_x1, lds_w1, lds_s1, lds_s0);
-                if (t + 3 < t1) stage(t + 3, lds_x1, lds_w1, lds_x0, lds_w0, lds_s0, nullptr);
-            }
+        const uint64_t at = (uint64_t)t0 * kStepBlocks;
+        load_scales(t0, s0);
+        load(at, b0);
+        load(at + 4, b1);
+        load(at + 8, b2);
+        wait_but_loads<2 * kLoads>();
+        barrier();
+        f0 = read(b0, 0);
+        now = read_scales(at, s0, 0);
+        for (uint32_t t = t0; t < t1; t += 2) {
+            four_stages(t, s0, s1);
+            if (t + 1 < t1) four_stages(t + 1, s1, s0);
         }
+        wait_but_loads<0>();
+        barrier();
     }
-    store_tile<FM, FN>(acc, a.out_args, m0 + wm * FM * 32, j0 + wn * FN * 32, out);
+    // the output goes through a stage's buffer
+    static_assert(kStageBytes >= kWaves * kTurnBytes, "");
+    uint8_t* const turn = b0 + wave * kTurnBytes;
+    store_tile<FM, FN>(acc, a.out_args, m0 + wm * FM * 32, j0 + wn * FN * 32, out, turn);
 }
 
 }  // namespace

@@ -12,24 +12,25 @@ namespace {
 
 constexpr uint32_t kStep = kWideStep;
 
-template <bool Grad, int BM, int BN, int WM, int WN, typename T>
+template <int BM, int BN, int WM, int WN, typename T>
 __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) {
-    constexpr int kThreads = WM * WN * 64, kWaves = WM * WN, FM = BM / WM / 32, FN = BN / WN / 32;
-    constexpr int kLoads = BM / 8 / kWaves;               // loads of x a wave issues a stage
-    constexpr int kBlocks = BN * kStep / 32 / kThreads;   // blocks of W a lane expands a stage
-    constexpr int kPitch = BN * 2 + 32;                   // bytes of a row of W's tile in LDS (Grad)
-    constexpr int kXBytes = BM * kStep * 2, kWBytes = Grad ? kStep * kPitch : BN * kStep * 2;
-    // The two stages are variables of their own: the compiler then sees that
-    // loads into one do not touch what is read from the other.
+    constexpr int kWaves = WM * WN, FM = BM / WM / 32, FN = BN / WN / 32;
+    constexpr int kXLoads = BM / 8 / kWaves, kWLoads = BN / 16 / kWaves, kScaleWaves = BN / 64;
+    constexpr int kXBytes = BM * kStep * 2, kWBytes = BN * 64, kScaleBytes = BN * 4;
+    static_assert(kScaleWaves <= kWaves, "");
+    // The stages are variables of their own: the compiler then sees that loads
+    // into one do not touch what is read from another.
     __shared__ __align__(16) uint8_t lds_x0[kXBytes], lds_x1[kXBytes];
-    __shared__ __align__(16) uint8_t lds_w0[kWBytes], lds_w1[kWBytes];
+    // W and its scales, of two stages
+    __shared__ __align__(16) uint8_t lds_w0[kWBytes + kScaleBytes], lds_w1[kWBytes + kScaleBytes];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t r = lane & 31, h = lane >> 5;
     const void* const zeros = zero_vector();
     const Tile tile = tile_of(blockIdx.x, a.tiles_m, a.tiles_j);
     const uint64_t m0 = (uint64_t)tile.m * BM, j0 = (uint64_t)tile.j * BN;
-    const uint32_t steps = a.steps * a.parts;
-    const uint32_t t0 = (uint64_t)steps * blockIdx.y / gridDim.y, t1 = (uint64_t)steps * (blockIdx.y + 1) / gridDim.y;
+    // a part's steps are even: stages go in pairs that share a piece of W
+    const uint32_t pairs = a.steps / 2 * a.parts;
+    const uint32_t t0 = (uint64_t)pairs * blockIdx.y / gridDim.y * 2, t1 = (uint64_t)pairs * (blockIdx.y + 1) / gridDim.y * 2;
     const uint32_t wm = wave % WM, wn = wave / WM;
 
     f32x16 acc[FN][FM];
@@ -42,53 +43,50 @@ __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) 
     // a lane takes the same columns of each of its rows
     static_assert(kWaves % 2 == 0, "");
     const uint32_t x_col = (lane % 8 ^ (wave % 2 * 4 + lane / 16)) * 8;
-    const __bf16* x_at[kLoads];
+    const __bf16* x_at[kXLoads];
 #pragma unroll
-    for (int q = 0; q < kLoads; ++q) x_at[q] = a.x + min(m0 + (q * kWaves + wave) * 8 + lane / 8, a.m - 1) * a.x_stride + x_col;
-    auto load_x = [&](uint32_t t, uint8_t* to) {
+    for (int q = 0; q < kXLoads; ++q) x_at[q] = a.x + min(m0 + (q * kWaves + wave) * 8 + lane / 8, a.m - 1) * a.x_stride + x_col;
+    auto load_x = [&](uint32_t t, uint8_t* to) SLLM_INLINE {
         const uint32_t part = t / a.steps;
         const uint64_t d = (uint64_t)(t - part * a.steps) * kStep, at = part * a.part_stride + d;
         const bool inside = d + x_col < a.depth;
 #pragma unroll
-        for (int q = 0; q < kLoads; ++q) {
+        for (int q = 0; q < kXLoads; ++q) {
             const void* p = x_at[q] + at;
             load_to_lds(inside ? p : zeros, to + (q * kWaves + wave) * 1024);
         }
     };
-    // The blocks a lane expands, of two stages: a row's are neighbours then.
-    // Past the end of the depth x is zero, so any codes do under a finite scale.
-    u32x4 codes[2][kBlocks];
-    uint32_t scales[2][kBlocks];
-    const uint32_t w_in = Grad ? tid / (BN / 32) : tid % 2;  // this lane's place in a stage's depth: row or block
-    auto load_w = [&](uint32_t t, int to) {
-        const uint64_t s = t % a.steps;
+    // W's codes likewise, one load 16 rows x 128 of the depth, and four scale
+    // bytes a row.  Past the end of the depth x is zero, so any codes do.
+    const uint32_t w_block = lane % 4 ^ lane / 16;
+    const u32x4* w_at[kWLoads];
 #pragma unroll
-        for (int q = 0; q < kBlocks; ++q) {
-            const uint64_t row = Grad ? s * kStep + w_in + q * (kThreads / (BN / 32)) : j0 + (q * kThreads + tid) / 2;
-            const uint64_t b = Grad ? j0 / 32 + tid % (BN / 32) : s * 2 + w_in;
-            const uint64_t row_at = min(row, a.w_rows - 1), b_at = min(b, a.w_blocks - 1);
-            codes[to][q] = a.w_codes[row_at * a.w_blocks + b_at];
-            scales[to][q] = a.w_scales[row_at * a.w_scale_pitch + b_at];
-        }
+    for (int q = 0; q < kWLoads; ++q) w_at[q] = a.w_codes + min(j0 + (q * kWaves + wave) * 16 + lane / 4, a.w_rows - 1) * a.w_blocks;
+    const uint8_t* scales_at = a.w_scales + min(j0 + (wave % kScaleWaves) * 64 + lane, a.w_rows - 1) * a.w_scale_pitch;
+    auto load_w = [&](uint32_t t, uint8_t* to) SLLM_INLINE {
+        const uint64_t b0 = (uint64_t)(t % a.steps) * 2, b = min(b0 + w_block, a.w_blocks - 1);
+#pragma unroll
+        for (int q = 0; q < kWLoads; ++q) load_to_lds(w_at[q] + b, to + (q * kWaves + wave) * 1024);
+        if (wave < kScaleWaves) load_word_to_lds(scales_at + b0, to + (kWBytes + wave * 256));
     };
-    // W's tile in LDS: like x's, rows of the weight by the depth, or (Grad) rows
-    // of the depth by the tile's columns, whose order changes from block to block
-    // so that a wave's stores reach all banks.
-    auto store_w = [&](uint32_t t, int from, uint8_t* to) {
-        const uint64_t s = t % a.steps;
+
+    // Of a stage, lane (r, h) has 32 of the depth of its rows: the block of W
+    // that it expands as it goes, eight codes a step.
+    struct Weight {
+        u32x4 codes[FN];
+        float scale[FN];
+    };
+    const uint32_t w_chunk = short_chunk_at(r, h);
+    auto read_w = [&](uint32_t t, const uint8_t* from, uint32_t odd) SLLM_INLINE {
+        const bool inside = (uint64_t)(t % a.steps) * 2 + h < a.w_blocks;  // scale bytes past the row's end may hold anything
+        Weight w;
 #pragma unroll
-        for (int q = 0; q < kBlocks; ++q) {
-            const bool inside = Grad ? s * kStep + w_in + q * (kThreads / (BN / 32)) < a.w_rows : s * 2 + w_in < a.w_blocks;
-            u32x4 v[4];
-            expand(codes[from][q], inside ? scales[from][q] : 0, v);
-            const uint32_t i = q * kThreads + tid;
-#pragma unroll
-            for (uint32_t w = 0; w < 4; ++w) {
-                const uint32_t at = Grad ? i / (BN / 32) * kPitch + i % (BN / 32) * 64 + (w ^ (i & 3)) * 16
-                                         : chunk_at(i / 2, i % 2 * 4) ^ w * 16;
-                *reinterpret_cast<u32x4*>(to + at) = v[w];
-            }
+        for (int n = 0; n < FN; ++n) {
+            w.codes[n] = *reinterpret_cast<const u32x4*>(from + ((wn * FN + n) * 2048 + (w_chunk ^ odd * 32)));
+            const uint8_t s = from[kWBytes + ((wn * FN + n) * 128 + r * 4 + h + odd * 2)];
+            w.scale[n] = mx_scale(inside ? s : 0);
         }
+        return w;
     };
 
     struct Fragments {
@@ -96,31 +94,17 @@ __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) 
     };
     // Step s of a stage is, in lane (r, h), eight of the depth from 32 h + 8 s.
     const uint32_t chunk = chunk_at(r, 4 * h);
-    auto read = [&](const uint8_t* x_now, const uint8_t* w_now, uint32_t s) {
+    auto read = [&](const uint8_t* from, const Weight& w, auto which) SLLM_INLINE {
+        constexpr int s = decltype(which)::value;
         Fragments f;
         const uint32_t c = chunk ^ s * 16;
 #pragma unroll
-        for (int n = 0; n < FN; ++n) {
-            if constexpr (Grad) {
-                // Four rows of the tile and 16 columns a read and 16 lanes,
-                // transposed: a lane gets a column.
-                typedef short s16x4 __attribute__((ext_vector_type(4)));
-                typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                const uint32_t b = wn * FN + n, l = lane & 15;
-                const uint32_t piece = ((lane >> 4 & 1) * 2 + (l >> 1 & 1)) ^ (b & 3);
-                const uint32_t at = (32 * h + 8 * s + (l >> 2)) * kPitch + b * 64 + piece * 16 + (l & 1) * 8;
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(w_now + at));
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(w_now + (at + 4 * kPitch)));
-                f.w[n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-            } else {
-                f.w[n] = *reinterpret_cast<const bf16x8*>(w_now + ((wn * FN + n) * 4096 + c));
-            }
-        }
+        for (int m = 0; m < FM; ++m) f.x[m] = *reinterpret_cast<const bf16x8*>(from + ((wm * FM + m) * 4096 + c));
 #pragma unroll
-        for (int m = 0; m < FM; ++m) f.x[m] = *reinterpret_cast<const bf16x8*>(x_now + ((wm * FM + m) * 4096 + c));
+        for (int n = 0; n < FN; ++n) f.w[n] = __builtin_bit_cast(bf16x8, expand8(w.codes[n][s], w.scale[n]));
         return f;
     };
-    auto multiply = [&](const Fragments& f) {
+    auto multiply = [&](const Fragments& f) SLLM_INLINE {
         pin(acc);
 #pragma unroll
         for (int m = 0; m < FM; ++m)
@@ -131,55 +115,63 @@ __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) 
     // While one step is multiplied the next is read; the next stage's first step
     // past the barrier, where its loads have landed and this stage's buffers are
     // free for the loads of the one after.
+    typedef std::integral_constant<int, 0> S0;
+    typedef std::integral_constant<int, 1> S1;
+    typedef std::integral_constant<int, 2> S2;
+    typedef std::integral_constant<int, 3> S3;
     Fragments f0, f1;
-    auto stage = [&](uint32_t t, int parity, uint8_t* x_now, const uint8_t* w_now, const uint8_t* x_next, uint8_t* w_next) {
-        f1 = read(x_now, w_now, 1);
+    Weight now;
+    auto stage = [&](uint32_t t, uint8_t* x_now, const uint8_t* x_next, const uint8_t* w_next, uint32_t odd_next, auto load_more) SLLM_INLINE {
+        f1 = read(x_now, now, S1());
         multiply(f0);
-        f0 = read(x_now, w_now, 2);
+        f0 = read(x_now, now, S2());
         multiply(f1);
-        f1 = read(x_now, w_now, 3);
-        if (t + 1 < t1) store_w(t + 1, parity ^ 1, w_next);
+        f1 = read(x_now, now, S3());
         multiply(f0);
-        wait_loads();
-        __syncthreads();
-        if (t + 2 < t1) {
-            load_x(t + 2, x_now);
-            if (parity == 0) {
-                load_w(t + 2, 0);
-                load_w(t + 3, 1);
-            }
-        }
-        f0 = read(x_next, w_next, 0);
+        wait_but_loads<0>();
+        barrier();
+        now = read_w(t + 1, w_next, odd_next);
+        if (t + 2 < t1) load_x(t + 2, x_now);
+        load_more();
+        f0 = read(x_next, now, S0());
         multiply(f1);
+    };
+    // a pair of stages whose W is in w_now; the pair after the next goes there
+    auto pair = [&](uint32_t t, uint8_t* w_now, const uint8_t* w_next) SLLM_INLINE {
+        stage(t, lds_x0, lds_x1, w_now, 1, []() SLLM_INLINE {});
+        stage(t + 1, lds_x1, lds_x0, w_next, 0, [&]() SLLM_INLINE {
+            if (t + 4 < t1) load_w(t + 4, w_now);
+        });
     };
     if (t0 < t1) {
         load_x(t0, lds_x0);
-        load_w(t0, 0);
-        load_w(t0 + 1, 1);
-        store_w(t0, 0, lds_w0);
-        wait_loads();
-        __syncthreads();
-        if (t0 + 1 < t1) load_x(t0 + 1, lds_x1);
-        f0 = read(lds_x0, lds_w0, 0);
-    }
-    for (uint32_t t = t0; t < t1; t += 2) {
-        stage(t, 0, lds_x0, lds_w0, lds_x1, lds_w1);
-        if (t + 1 < t1) stage(t + 1, 1, lds_x1, lds_w1, lds_x0, lds_w0);
+        load_w(t0, lds_w0);
+        wait_but_loads<0>();
+        barrier();
+        load_x(t0 + 1, lds_x1);
+        if (t0 + 2 < t1) load_w(t0 + 2, lds_w1);
+        now = read_w(t0, lds_w0, 0);
+        f0 = read(lds_x0, now, S0());
+        for (uint32_t t = t0; t < t1; t += 4) {
+            pair(t, lds_w0, lds_w1);
+            if (t + 2 < t1) pair(t + 2, lds_w1, lds_w0);
+        }
     }
 
-    store_tile<FM, FN>(acc, a.out_args, m0 + wm * FM * 32, j0 + wn * FN * 32, out);
+    __syncthreads();  // the last stage's reads are done
+    // the output goes through a buffer of x
+    static_assert(kXBytes >= kWaves * kTurnBytes, "");
+    uint8_t* const turn = lds_x0 + wave * kTurnBytes;
+    store_tile<FM, FN>(acc, a.out_args, m0 + wm * FM * 32, j0 + wn * FN * 32, out, turn);
 }
 
 }  // namespace
 
-template <bool Grad>
 int32_t launch_wide(const WideArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream) {
     const dim3 grid(a.tiles_m * a.tiles_j, splits);
-    SLLM_BY_DTYPE(out_dtype, T, (wide_product<Grad, 256, 256, 2, 4, T><<<grid, 512, 0, stream>>>(a, static_cast<T*>(out))));
+    SLLM_BY_DTYPE(out_dtype, T, (wide_product<256, 256, 2, 4, T><<<grid, 512, 0, stream>>>(a, static_cast<T*>(out))));
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
 }
-template int32_t launch_wide<false>(const WideArgs&, uint32_t, void*, uint32_t, hipStream_t);
-template int32_t launch_wide<true>(const WideArgs&, uint32_t, void*, uint32_t, hipStream_t);
 
 }  // namespace sllm

@@ -130,6 +130,7 @@ Plan plan_linear(const LinearLaunch& a) {
     p.part_stride = (p.depth + 7) / 8 * 8;
     const uint32_t step = a.x.codes ? kNarrowStep : kWideStep;
     p.steps = (uint32_t)ceil_div(p.depth, step);
+    if (!a.x.codes) p.steps += p.steps % 2;
     p.tiles_m = (uint32_t)ceil_div(a.m, kWideTile);
     p.tiles_j = (uint32_t)ceil_div(p.cols, kWideTile);
     const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_j;
@@ -219,7 +220,7 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
         o.stride = (p.cols + 3) / 4 * 4;
         o.split_stride = p.split_stride;
     }
-    o.vector = o.stride % 4 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
+    o.vector = reinterpret_cast<uintptr_t>(out) % 16 == 0 && (a.m == 1 || o.stride * (dtype == SLLM_DTYPE_F32 ? 4 : 2) % 16 == 0);
     if (a.x.codes) {
         const NarrowArgs n{reinterpret_cast<const u32x4*>(a.x.codes), a.x.scales, reinterpret_cast<const u32x4*>(a.w_codes),
                            a.w_scales, a.m, a.n, mx_blocks(a.k), mx_scale_pitch(a.k), p.steps, p.tiles_m, p.tiles_j, o};
@@ -234,7 +235,7 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
         w.w_rows = a.n, w.w_blocks = mx_blocks(a.k), w.w_scale_pitch = mx_scale_pitch(a.k);
         w.tiles_m = p.tiles_m, w.tiles_j = p.tiles_j;
         w.out_args = o;
-        SLLM_TRY(a.grad ? launch_wide<true>(w, p.splits, out, dtype, stream) : launch_wide<false>(w, p.splits, out, dtype, stream));
+        SLLM_TRY(a.grad ? launch_grad(w, p.splits, out, dtype, stream) : launch_wide(w, p.splits, out, dtype, stream));
     }
     return p.splits > 1 ? join(p, static_cast<const float*>(out), p.splits, a, stream) : SLLM_OK;
 }

@@ -12,7 +12,7 @@ constexpr uint32_t kTileRows = 4;  // of tiles that neighbouring workgroups shar
 struct OutArgs {
     uint64_t m, cols, stride;
     uint64_t split_stride;  // elements from one split's matrix to the next
-    uint32_t vector;        // rows start on 4 elements
+    uint32_t vector;        // rows start on 16 bytes
 };
 
 // x (m x depth, parts of it one after another along a row) in bfloat16
@@ -20,7 +20,7 @@ struct WideArgs {
     const __bf16* x;
     uint64_t m, depth;       // of a part
     uint64_t x_stride, part_stride;
-    uint32_t parts, steps;   // steps of a part
+    uint32_t parts, steps;   // steps of a part, an even number
     const u32x4* w_codes;
     const uint8_t* w_scales;
     uint64_t w_rows, w_blocks, w_scale_pitch;
@@ -46,8 +46,34 @@ __device__ __forceinline__ void load_to_lds(const void* from, void* to) {
                                      (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-// Every load of this wave has landed, those to LDS included.
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+// Four bytes a lane, lane l's to to + 4 l.
+__device__ __forceinline__ void load_word_to_lds(const void* from, void* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                     (__attribute__((address_space(3))) void*)to, 4, 0, 0);
+}
+
+// Lanes of a wave see what each other wrote to LDS.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// All but the last N loads of this wave have landed, those to LDS included, and
+// its reads and writes of LDS are done.  The counts are in the operand's fields:
+// vmcnt in bits 3:0 and 15:14, expcnt (not waited for) in 6:4, lgkmcnt in 11:8.
+template <int N>
+__device__ __forceinline__ void wait_but_loads() {
+    static_assert(N < 64, "");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);
+}
+
+// A barrier that waits for nothing else: __syncthreads would wait for all loads.
+__device__ __forceinline__ void barrier() {
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
 
 // The tile of a workgroup.  Workgroups go to the eight XCDs in turn; each XCD
 // takes a run of tiles of its own, four rows of tiles at a time, so that its
@@ -70,22 +96,29 @@ __device__ __forceinline__ Tile tile_of(uint32_t block, uint32_t tiles_m, uint32
 // chunks are in all banks once.  chunk_at(r, c ^ s) is chunk_at(r, c) ^ 16 s.
 __device__ __forceinline__ uint32_t chunk_at(uint32_t r, uint32_t c) { return r * 128 + (c ^ (r >> 1 & 7)) * 16; }
 
+// The same for rows of 64 bytes, four chunks: four rows are in all banks once.
+__device__ __forceinline__ uint32_t short_chunk_at(uint32_t r, uint32_t c) { return r * 64 + (c ^ (r >> 2 & 3)) * 16; }
+
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // A block of codes as an operand of the scaled matrix instruction, whose other
 // four registers 4-bit elements do not use.
 __device__ __forceinline__ i32x8 fragment(u32x4 v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
 
-// A block of 32 codes as bfloat16: four vectors of eight.
-__device__ __forceinline__ void expand(u32x4 codes, uint32_t scale, u32x4 out[4]) {
-    const float s = mx_scale(scale);
+// Eight codes as bfloat16.
+__device__ __forceinline__ u32x4 expand8(uint32_t codes, float scale) {
+    u32x4 v;
+    v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+    v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+    v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+    v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+    return v;
+}
+
+// A block of 32 codes: four vectors of eight.
+__device__ __forceinline__ void expand(u32x4 codes, uint32_t scale, u32x4 (&out)[4]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        out[i][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 0));
-        out[i][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 1));
-        out[i][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 2));
-        out[i][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], s, 3));
-    }
+    for (int i = 0; i < 4; ++i) out[i] = expand8(codes[i], mx_scale(scale));
 }
 
 // The leading eight bits of f as a bfloat16, and f less those: two or three of
@@ -112,35 +145,63 @@ __device__ __forceinline__ void pin(f32x16 (&acc)[FN][FM]) {
         for (int m = 0; m < FM; ++m) asm volatile("" : "+v"(acc[n][m]));
 }
 
-// A wave's accumulators: element 4 q + i of fragment [n][m] is, in lane (r, h) of
-// two halves of 32, column n * 32 + 8 q + 4 h + i of row m * 32 + r.
+// A wave's accumulators to memory: element 4 q + i of fragment [n][m] is, in lane
+// (r, h) of two halves of 32, column n * 32 + 8 q + 4 h + i of row m * 32 + r.
+// Stored from there a lane would write 8 bytes of a row of its own, so 32 rows
+// by as many columns as are 128 bytes go through `turn` (this wave's alone) at a
+// time, and eight lanes write a row's 128 bytes.
+constexpr uint32_t kTurnBytes = 32 * 128;
 template <int FM, int FN, typename T>
-__device__ __forceinline__ void store_tile(const f32x16 (&acc)[FN][FM], const OutArgs& o, uint64_t m0, uint64_t j0, T* out) {
+__device__ __forceinline__ void store_tile(const f32x16 (&acc)[FN][FM], const OutArgs& o, uint64_t m0, uint64_t j0, T* out,
+                                           uint8_t* turn) {
+    constexpr int kCols = 128 / sizeof(T), kFragments = kCols / 32, kChunk = 16 / sizeof(T);
+    static_assert(FN % kFragments == 0, "");
     const uint32_t lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
     out += blockIdx.y * o.split_stride;
 #pragma unroll
-    for (int m = 0; m < FM; ++m) {
-        const uint64_t row = m0 + m * 32 + r;
-        if (row >= o.m) continue;
-        T* p = out + row * o.stride;
+    for (int m = 0; m < FM; ++m)
 #pragma unroll
-        for (int n = 0; n < FN; ++n)
+        for (int n0 = 0; n0 < FN; n0 += kFragments) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint64_t j = j0 + n * 32 + q * 8 + h * 4;
-                T v[4];
+            for (int n = 0; n < kFragments; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(acc[n][m][4 * q + i]);
-                if (o.vector && j + 4 <= o.cols) {
-                    typedef T T4 __attribute__((ext_vector_type(4)));
-                    *reinterpret_cast<T4*>(p + j) = T4{v[0], v[1], v[2], v[3]};
-                } else {
+                for (int q = 0; q < 4; ++q) {
+                    T v[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (j + i < o.cols) p[j + i] = v[i];
+                    for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(acc[n0 + n][m][4 * q + i]);
+                    const uint32_t col = n * 32 + q * 8 + h * 4;
+                    __builtin_memcpy(turn + chunk_at(r, col / kChunk) + col % kChunk * sizeof(T), v, sizeof v);
+                }
+            wave_sync();
+            const uint64_t row0 = m0 + m * 32, col0 = j0 + n0 * 32;
+            if (o.vector) {
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    const uint32_t row = i * 8 + lane / 8;
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(turn + chunk_at(row, lane % 8));
+                    const uint64_t col = col0 + lane % 8 * kChunk;
+                    if (row0 + row >= o.m) continue;
+                    T* p = out + (row0 + row) * o.stride + col;
+                    if (col + kChunk <= o.cols) {
+                        *reinterpret_cast<u32x4*>(p) = v;
+                    } else {
+                        T e[kChunk];
+                        __builtin_memcpy(e, &v, sizeof e);
+#pragma unroll
+                        for (int k = 0; k < kChunk; ++k)
+                            if (col + k < o.cols) p[k] = e[k];
+                    }
+                }
+            } else {
+                for (uint32_t i = lane; i < 32 * kCols; i += 64) {
+                    const uint32_t row = i / kCols, c = i % kCols;
+                    T v;
+                    __builtin_memcpy(&v, turn + chunk_at(row, c / kChunk) + c % kChunk * sizeof(T), sizeof v);
+                    if (row0 + row < o.m && col0 + c < o.cols) out[(row0 + row) * o.stride + col0 + c] = v;
                 }
             }
-    }
+            wave_sync();
+        }
 }
 
 // Both sides in MX FP4.
@@ -155,7 +216,7 @@ struct NarrowArgs {
     OutArgs out_args;
 };
 int32_t launch_narrow(const NarrowArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
-constexpr uint32_t kNarrowStep = 256;  // depth of a stage
+constexpr uint32_t kNarrowStep = 512;  // depth whose scales are loaded together
 
 // At most kSkinnyRows rows of x, of any type (x_scales set: in MX FP4).
 struct SkinnyArgs {
@@ -175,8 +236,8 @@ struct SkinnyArgs {
 int32_t launch_skinny(const SkinnyArgs& a, hipStream_t stream);
 constexpr uint64_t kSkinnyRows = 32;
 
-template <bool Grad>
 int32_t launch_wide(const WideArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
+int32_t launch_grad(const WideArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
 constexpr uint32_t kWideTile = 256;  // rows of x and columns of the output a workgroup holds
 constexpr uint32_t kWideStep = 64;   // depth of a stage
 
