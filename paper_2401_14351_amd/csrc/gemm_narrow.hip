@@ -14,7 +14,7 @@ constexpr uint32_t kStepBlocks = kNarrowStep / kMxBlock;
 constexpr uint32_t kStageBlocks = 4;  // of a stage: 64 bytes a row
 
 template <int BM, int BN, int WM, int WN, typename T>
-__global__ __launch_bounds__(WM* WN * 64) void narrow_product(NarrowArgs a, T* out) {
+__global__ __launch_bounds__(WM* WN * 64, 2) void narrow_product(NarrowArgs a, T* out) {
     constexpr int kWaves = WM * WN, FM = BM / WM / 32, FN = BN / WN / 32;
     // The stages in flight are variables of their own: the compiler then sees
     // that loads into one do not touch what is read from another.
@@ -62,48 +62,47 @@ __global__ __launch_bounds__(WM* WN * 64) void narrow_product(NarrowArgs a, T* o
 #pragma unroll
         for (int q = 0; q < kXLoads; ++q) {
             const void* p = x_at[q] + inside;
-            load_to_lds(b < a.blocks ? p : zeros, to + (q * kWaves + wave) * 1024);
+            load_to_lds(b < a.blocks ? p : zeros, to, (q * kWaves + wave) * 1024);
         }
         // past the end of the depth x is zero, so any finite values do
 #pragma unroll
-        for (int q = 0; q < kWLoads; ++q) load_to_lds(w_at[q] + inside, to + (BM * 64 + (q * kWaves + wave) * 1024));
+        for (int q = 0; q < kWLoads; ++q) load_to_lds(w_at[q] + inside, to, BM * 64 + (q * kWaves + wave) * 1024);
     };
     auto load_scales = [&](uint32_t t, uint8_t* to) SLLM_INLINE {
         const uint64_t b = min((uint64_t)t * kStepBlocks, a.scale_pitch - kStepBlocks);
 #pragma unroll
-        for (int q = 0; q < kScaleLoads; ++q) load_to_lds(scales_at[q] + b, to + (q * kWaves + wave) * 1024);
+        for (int q = 0; q < kScaleLoads; ++q) load_to_lds(scales_at[q] + b, to, (q * kWaves + wave) * 1024);
     };
 
     // Of a stage, lane (r, h) multiplies blocks 2 h and 2 h + 1 of its rows, one a
     // step; a row's two scale bytes are one register.
+    // (Filled through a reference: a returned structure makes its reads' alias
+    // information useless, and they wait for every load under way.)
     struct Scales {
         uint32_t x[FM], w[FN];
     };
-    auto read_scales = [&](uint64_t at, const uint8_t* from, uint32_t stage) SLLM_INLINE {
+    const uint32_t xs_from = opaque(wm * FM * 512 + r * 16 + h * 2), ws_from = opaque((BM + wn * FN * 32 + r) * 16 + h * 2);
+    auto read_scales = [&](Scales& s, uint64_t at, const uint8_t* from, uint32_t stage) SLLM_INLINE {
         // scale bytes past the row's end may hold anything
         const uint64_t b = at + 2 * h;
         const uint32_t mask = b + 1 < a.blocks ? 0xffff : b < a.blocks ? 0xff : 0;
-        Scales s;
 #pragma unroll
         for (int m = 0; m < FM; ++m)
-            s.x[m] = *reinterpret_cast<const uint16_t*>(from + ((wm * FM + m) * 512 + r * 16 + h * 2 + stage * 4)) & mask;
+            s.x[m] = lds_read<uint16_t>(from, xs_from + m * 512 + stage * 4) & mask;
 #pragma unroll
         for (int n = 0; n < FN; ++n)
-            s.w[n] = *reinterpret_cast<const uint16_t*>(from + (BM * 16 + (wn * FN + n) * 512 + r * 16 + h * 2 + stage * 4)) & mask;
-        return s;
+            s.w[n] = lds_read<uint16_t>(from, ws_from + n * 512 + stage * 4) & mask;
     };
     struct Fragments {
         u32x4 x[FM], w[FN];
     };
-    const uint32_t chunk = short_chunk_at(r, 2 * h);
-    auto read = [&](const uint8_t* from, uint32_t s) SLLM_INLINE {
-        Fragments f;
-        const uint32_t c = chunk ^ s * 16;
+    const uint32_t x_from = opaque(wm * FM * 2048 + short_chunk_at(r, 2 * h));
+    const uint32_t w_from = opaque(BM * 64 + wn * FN * 2048 + short_chunk_at(r, 2 * h));
+    auto read = [&](Fragments& f, const uint8_t* from, uint32_t s) SLLM_INLINE {
 #pragma unroll
-        for (int n = 0; n < FN; ++n) f.w[n] = *reinterpret_cast<const u32x4*>(from + (BM * 64 + (wn * FN + n) * 2048 + c));
+        for (int n = 0; n < FN; ++n) f.w[n] = lds_read<u32x4>(from, (w_from ^ s * 16) + n * 2048);
 #pragma unroll
-        for (int m = 0; m < FM; ++m) f.x[m] = *reinterpret_cast<const u32x4*>(from + ((wm * FM + m) * 2048 + c));
-        return f;
+        for (int m = 0; m < FM; ++m) f.x[m] = lds_read<u32x4>(from, (x_from ^ s * 16) + m * 2048);
     };
     auto multiply = [&](const Fragments& f, const Scales& s, auto which) SLLM_INLINE {
         constexpr int j = decltype(which)::value;
@@ -124,14 +123,15 @@ __global__ __launch_bounds__(WM* WN * 64) void narrow_product(NarrowArgs a, T* o
     Scales now;
     auto stage = [&](uint64_t at, const uint8_t* here, const uint8_t* next_one, uint8_t* last, const uint8_t* scales,
                      uint32_t next_stage, auto more) SLLM_INLINE {
-        f1 = read(here, 1);
+        read(f1, here, 1);
         load(at + 3 * kStageBlocks, last);
         more();
         multiply(f0, now, std::integral_constant<int, 0>());
         wait_but_loads<2 * kLoads>();  // younger than the next stage's: those of the two after it
         barrier();
-        f0 = read(next_one, 0);
-        const Scales next = read_scales(at + kStageBlocks, scales, next_stage);
+        read(f0, next_one, 0);
+        Scales next;
+        read_scales(next, at + kStageBlocks, scales, next_stage);
         multiply(f1, now, std::integral_constant<int, 1>());
         now = next;
     };
@@ -151,8 +151,8 @@ __global__ __launch_bounds__(WM* WN * 64) void narrow_product(NarrowArgs a, T* o
         load(at + 8, b2);
         wait_but_loads<2 * kLoads>();
         barrier();
-        f0 = read(b0, 0);
-        now = read_scales(at, s0, 0);
+        read(f0, b0, 0);
+        read_scales(now, at, s0, 0);
         for (uint32_t t = t0; t < t1; t += 2) {
             four_stages(t, s0, s1);
             if (t + 1 < t1) four_stages(t + 1, s1, s0);
@@ -168,9 +168,16 @@ __global__ __launch_bounds__(WM* WN * 64) void narrow_product(NarrowArgs a, T* o
 
 }  // namespace
 
-int32_t launch_narrow(const NarrowArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream) {
+int32_t launch_narrow(const NarrowArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype,
+                    hipStream_t stream) {
     const dim3 grid(a.tiles_m * a.tiles_j, splits);
-    SLLM_BY_DTYPE(out_dtype, T, (narrow_product<256, 256, 2, 4, T><<<grid, 512, 0, stream>>>(a, static_cast<T*>(out))));
+    SLLM_BY_DTYPE(out_dtype, T, {
+        T* to = static_cast<T*>(out);
+        if (tile == kLargeTile)
+            narrow_product<kLargeTile, kLargeTile, 2, 4, T><<<grid, 512, 0, stream>>>(a, to);
+        else
+            narrow_product<kSmallTile, kSmallTile, 2, 2, T><<<grid, 256, 0, stream>>>(a, to);
+    });
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
 }

@@ -155,7 +155,7 @@ __global__ __launch_bounds__(1024) void skinny_product(SkinnyArgs a) {
         auto step = [&](const u32x4 (&codes)[NT], const uint32_t (&scale)[NT], uint64_t b, auto load) {
             u32x4 w[NT][4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) expand(codes[n], b < end ? scale[n] : 0, w[n]);
+            for (int n = 0; n < NT; ++n) expand(codes[n], b < a.blocks ? scale[n] : 0, w[n]);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -172,16 +172,18 @@ __global__ __launch_bounds__(1024) void skinny_product(SkinnyArgs a) {
         for (uint32_t s = s0; s < s1; s += kAhead) {
             const Weight w = ahead;
             if (s + kAhead < s1) ahead = load_w(s + kAhead);
-            const uint64_t depth = min((uint64_t)a.depth, (uint64_t)s1 * 128);
-            if (a.vector && (uint64_t)(s + kAhead) * 128 <= depth) {
+            if (a.vector && (uint64_t)(s + kAhead) * 128 <= a.depth) {
 #pragma unroll
                 for (uint32_t u = 0; u < kAhead; ++u)
-                    step(w.codes[u], w.scale[u], 4 * ((uint64_t)s + u) + g, [](const X* row, uint64_t c) { return load_x_vector(row + c); });
+                    if (s + u < s1)
+                        step(w.codes[u], w.scale[u], 4 * ((uint64_t)s + u) + g, [](const X* row, uint64_t c) { return load_x_vector(row + c); });
             } else {
 #pragma unroll
                 for (uint32_t u = 0; u < kAhead; ++u)
                     if (s + u < s1)
-                        step(w.codes[u], w.scale[u], 4 * ((uint64_t)s + u) + g, [&](const X* row, uint64_t c) { return load_x(row, c, depth); });
+                        step(w.codes[u], w.scale[u], 4 * ((uint64_t)s + u) + g, [&](const X* row, uint64_t c) {
+                            return a.vector && c + 8 <= a.depth ? load_x_vector(row + c) : load_x(row, c, a.depth);
+                        });
             }
         }
     }

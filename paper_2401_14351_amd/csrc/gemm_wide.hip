@@ -13,16 +13,19 @@ namespace {
 constexpr uint32_t kStep = kWideStep;
 
 template <int BM, int BN, int WM, int WN, typename T>
-__global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) {
+__global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* out) {
     constexpr int kWaves = WM * WN, FM = BM / WM / 32, FN = BN / WN / 32;
-    constexpr int kXLoads = BM / 8 / kWaves, kWLoads = BN / 16 / kWaves, kScaleWaves = BN / 64;
+    constexpr int kXLoads = BM / 8 / kWaves, kWLoads = BN / 16 / kWaves;
     constexpr int kXBytes = BM * kStep * 2, kWBytes = BN * 64, kScaleBytes = BN * 4;
-    static_assert(kScaleWaves <= kWaves, "");
+    constexpr int kScaleRows = BN / kWaves;  // whose scales a wave loads
+    static_assert(kScaleRows <= 64, "");
     // The stages are variables of their own: the compiler then sees that loads
-    // into one do not touch what is read from another.
-    __shared__ __align__(16) uint8_t lds_x0[kXBytes], lds_x1[kXBytes];
-    // W and its scales, of two stages
-    __shared__ __align__(16) uint8_t lds_w0[kWBytes + kScaleBytes], lds_w1[kWBytes + kScaleBytes];
+    // into one do not touch what is read from another.  W and its scales are of
+    // two stages each.
+    __shared__ __align__(16) uint8_t x0[kXBytes], x1[kXBytes];
+    __shared__ __align__(16) uint8_t w0[kWBytes + kScaleBytes], w1[kWBytes + kScaleBytes];
+    uint8_t* const x_ring[2] = {x0, x1};
+    uint8_t* const w_ring[2] = {w0, w1};
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t r = lane & 31, h = lane >> 5;
     const void* const zeros = zero_vector();
@@ -53,7 +56,7 @@ __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) 
 #pragma unroll
         for (int q = 0; q < kXLoads; ++q) {
             const void* p = x_at[q] + at;
-            load_to_lds(inside ? p : zeros, to + (q * kWaves + wave) * 1024);
+            load_to_lds(inside ? p : zeros, to, (q * kWaves + wave) * 1024);
         }
     };
     // W's codes likewise, one load 16 rows x 128 of the depth, and four scale
@@ -62,47 +65,44 @@ __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) 
     const u32x4* w_at[kWLoads];
 #pragma unroll
     for (int q = 0; q < kWLoads; ++q) w_at[q] = a.w_codes + min(j0 + (q * kWaves + wave) * 16 + lane / 4, a.w_rows - 1) * a.w_blocks;
-    const uint8_t* scales_at = a.w_scales + min(j0 + (wave % kScaleWaves) * 64 + lane, a.w_rows - 1) * a.w_scale_pitch;
+    const uint8_t* const scales_at = a.w_scales + min(j0 + wave * kScaleRows + lane % kScaleRows, a.w_rows - 1) * a.w_scale_pitch;
     auto load_w = [&](uint32_t t, uint8_t* to) SLLM_INLINE {
         const uint64_t b0 = (uint64_t)(t % a.steps) * 2, b = min(b0 + w_block, a.w_blocks - 1);
 #pragma unroll
-        for (int q = 0; q < kWLoads; ++q) load_to_lds(w_at[q] + b, to + (q * kWaves + wave) * 1024);
-        if (wave < kScaleWaves) load_word_to_lds(scales_at + b0, to + (kWBytes + wave * 256));
+        for (int q = 0; q < kWLoads; ++q) load_to_lds(w_at[q] + b, to, (q * kWaves + wave) * 1024);
+        if (lane < kScaleRows) load_word_to_lds(scales_at + b0, to, kWBytes + wave * kScaleRows * 4);
     };
 
     // Of a stage, lane (r, h) has 32 of the depth of its rows: the block of W
     // that it expands as it goes, eight codes a step.
+    // (Filled through a reference: a returned structure makes its reads' alias
+    // information useless, and they wait for every load under way.)
     struct Weight {
         u32x4 codes[FN];
         float scale[FN];
     };
-    const uint32_t w_chunk = short_chunk_at(r, h);
-    auto read_w = [&](uint32_t t, const uint8_t* from, uint32_t odd) SLLM_INLINE {
+    const uint32_t w_from = opaque(wn * FN * 2048 + short_chunk_at(r, h)), scale_from = opaque(kWBytes + wn * FN * 128 + r * 4 + h);
+    auto read_w = [&](Weight& w, uint32_t t, const uint8_t* from, uint32_t odd) SLLM_INLINE {
         const bool inside = (uint64_t)(t % a.steps) * 2 + h < a.w_blocks;  // scale bytes past the row's end may hold anything
-        Weight w;
 #pragma unroll
         for (int n = 0; n < FN; ++n) {
-            w.codes[n] = *reinterpret_cast<const u32x4*>(from + ((wn * FN + n) * 2048 + (w_chunk ^ odd * 32)));
-            const uint8_t s = from[kWBytes + ((wn * FN + n) * 128 + r * 4 + h + odd * 2)];
+            w.codes[n] = lds_read<u32x4>(from, (w_from ^ odd * 32) + n * 2048);
+            const uint8_t s = lds_read<uint8_t>(from, scale_from + n * 128 + odd * 2);
             w.scale[n] = mx_scale(inside ? s : 0);
         }
-        return w;
     };
 
     struct Fragments {
         bf16x8 x[FM], w[FN];
     };
     // Step s of a stage is, in lane (r, h), eight of the depth from 32 h + 8 s.
-    const uint32_t chunk = chunk_at(r, 4 * h);
-    auto read = [&](const uint8_t* from, const Weight& w, auto which) SLLM_INLINE {
+    const uint32_t x_from = opaque(wm * FM * 4096 + chunk_at(r, 4 * h));
+    auto read = [&](Fragments& f, const uint8_t* from, const Weight& w, auto which) SLLM_INLINE {
         constexpr int s = decltype(which)::value;
-        Fragments f;
-        const uint32_t c = chunk ^ s * 16;
 #pragma unroll
-        for (int m = 0; m < FM; ++m) f.x[m] = *reinterpret_cast<const bf16x8*>(from + ((wm * FM + m) * 4096 + c));
+        for (int m = 0; m < FM; ++m) f.x[m] = lds_read<bf16x8>(from, (x_from ^ s * 16) + m * 4096);
 #pragma unroll
         for (int n = 0; n < FN; ++n) f.w[n] = __builtin_bit_cast(bf16x8, expand8(w.codes[n][s], w.scale[n]));
-        return f;
     };
     auto multiply = [&](const Fragments& f) SLLM_INLINE {
         pin(acc);
@@ -121,55 +121,61 @@ __global__ __launch_bounds__(WM* WN * 64) void wide_product(WideArgs a, T* out) 
     typedef std::integral_constant<int, 3> S3;
     Fragments f0, f1;
     Weight now;
-    auto stage = [&](uint32_t t, uint8_t* x_now, const uint8_t* x_next, const uint8_t* w_next, uint32_t odd_next, auto load_more) SLLM_INLINE {
-        f1 = read(x_now, now, S1());
+    auto stage = [&](uint32_t t, auto which) SLLM_INLINE {
+        constexpr int i = decltype(which)::value;  // t's place among the four stages that W's two buffers hold
+        uint8_t* const here = x_ring[i % 2];
+        read(f1, here, now, S1());
         multiply(f0);
-        f0 = read(x_now, now, S2());
+        read(f0, here, now, S2());
         multiply(f1);
-        f1 = read(x_now, now, S3());
+        read(f1, here, now, S3());
         multiply(f0);
         wait_but_loads<0>();
         barrier();
-        now = read_w(t + 1, w_next, odd_next);
-        if (t + 2 < t1) load_x(t + 2, x_now);
-        load_more();
-        f0 = read(x_next, now, S0());
+        read_w(now, t + 1, w_ring[(i + 1) / 2 % 2], (i + 1) % 2);
+        if (t + 2 < t1) load_x(t + 2, here);
+        if (i % 2 && t + 3 < t1) load_w(t + 3, w_ring[i / 2]);
+        read(f0, x_ring[(i + 1) % 2], now, S0());
         multiply(f1);
-    };
-    // a pair of stages whose W is in w_now; the pair after the next goes there
-    auto pair = [&](uint32_t t, uint8_t* w_now, const uint8_t* w_next) SLLM_INLINE {
-        stage(t, lds_x0, lds_x1, w_now, 1, []() SLLM_INLINE {});
-        stage(t + 1, lds_x1, lds_x0, w_next, 0, [&]() SLLM_INLINE {
-            if (t + 4 < t1) load_w(t + 4, w_now);
-        });
     };
     if (t0 < t1) {
-        load_x(t0, lds_x0);
-        load_w(t0, lds_w0);
+        load_w(t0, w0);
+        load_x(t0, x0);
         wait_but_loads<0>();
         barrier();
-        load_x(t0 + 1, lds_x1);
-        if (t0 + 2 < t1) load_w(t0 + 2, lds_w1);
-        now = read_w(t0, lds_w0, 0);
-        f0 = read(lds_x0, now, S0());
+        load_x(t0 + 1, x1);
+        if (t0 + 2 < t1) load_w(t0 + 2, w1);
+        read_w(now, t0, w0, 0);
+        read(f0, x0, now, S0());
         for (uint32_t t = t0; t < t1; t += 4) {
-            pair(t, lds_w0, lds_w1);
-            if (t + 2 < t1) pair(t + 2, lds_w1, lds_w0);
+            stage(t, S0());
+            stage(t + 1, S1());
+            if (t + 2 < t1) {
+                stage(t + 2, S2());
+                stage(t + 3, S3());
+            }
         }
     }
 
     __syncthreads();  // the last stage's reads are done
-    // the output goes through a buffer of x
-    static_assert(kXBytes >= kWaves * kTurnBytes, "");
-    uint8_t* const turn = lds_x0 + wave * kTurnBytes;
+    // the output goes through x's first two buffers
+    static_assert(2 * kXBytes >= kWaves * kTurnBytes && kXBytes % kTurnBytes == 0, "");
+    uint8_t* const turn = (wave * kTurnBytes < kXBytes ? x0 : x1) + wave * kTurnBytes % kXBytes;
     store_tile<FM, FN>(acc, a.out_args, m0 + wm * FM * 32, j0 + wn * FN * 32, out, turn);
 }
 
 }  // namespace
 
-int32_t launch_wide(const WideArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream) {
+int32_t launch_wide(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype,
+                    hipStream_t stream) {
     const dim3 grid(a.tiles_m * a.tiles_j, splits);
-    SLLM_BY_DTYPE(out_dtype, T, (wide_product<256, 256, 2, 4, T><<<grid, 512, 0, stream>>>(a, static_cast<T*>(out))));
+    SLLM_BY_DTYPE(out_dtype, T, {
+        T* to = static_cast<T*>(out);
+        if (tile == kLargeTile)
+            wide_product<kLargeTile, kLargeTile, 2, 4, T><<<grid, 512, 0, stream>>>(a, to);
+        else
+            wide_product<kSmallTile, kSmallTile, 2, 2, T><<<grid, 256, 0, stream>>>(a, to);
+    });
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
 }

@@ -112,7 +112,7 @@ struct Plan {
     bool staged = false;       // x is written out as those first
     uint64_t depth = 0, cols = 0;
     uint64_t part_stride = 0;  // elements, of a staged x
-    uint32_t steps = 0, splits = 1;
+    uint32_t tile = 0, steps = 0, splits = 1;
     uint32_t tiles_m = 0, tiles_j = 0;
     uint64_t x_bytes = 0, split_stride = 0, bytes = 0;
 };
@@ -131,10 +131,20 @@ Plan plan_linear(const LinearLaunch& a) {
     const uint32_t step = a.x.codes ? kNarrowStep : kWideStep;
     p.steps = (uint32_t)ceil_div(p.depth, step);
     if (!a.x.codes) p.steps += p.steps % 2;
-    p.tiles_m = (uint32_t)ceil_div(a.m, kWideTile);
-    p.tiles_j = (uint32_t)ceil_div(p.cols, kWideTile);
-    const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_j;
-    if (tiles <= 128) p.splits = (uint32_t)std::min<uint64_t>(256 / tiles, std::max<uint64_t>(1, (uint64_t)p.steps * p.parts * step / 512));
+    const auto tiles = [&](uint32_t tile) { return ceil_div(a.m, tile) * ceil_div(p.cols, tile); };
+    const uint64_t depth = (uint64_t)p.steps * p.parts * step, large = tiles(kLargeTile), small = tiles(kSmallTile);
+    if (large >= 192) {
+        p.tile = kLargeTile;
+    } else if (!a.x.codes && large >= 112 && depth >= 8192) {
+        p.tile = kLargeTile;
+        p.splits = 2;
+    } else {
+        p.tile = kSmallTile;
+        const uint64_t fill = a.x.codes ? 128 : 512, piece = a.x.codes ? 4096 : 512;
+        p.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({fill / small, depth / piece, 16}));
+    }
+    p.tiles_m = (uint32_t)ceil_div(a.m, p.tile);
+    p.tiles_j = (uint32_t)ceil_div(p.cols, p.tile);
     if (p.staged) p.x_bytes = (a.m * p.parts * p.part_stride * 2 + 255) / 256 * 256;
     p.split_stride = a.m * ((p.cols + 3) / 4 * 4);
     p.bytes = p.x_bytes + (p.splits > 1 ? p.splits * p.split_stride * 4 : 0);
@@ -224,7 +234,7 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
     if (a.x.codes) {
         const NarrowArgs n{reinterpret_cast<const u32x4*>(a.x.codes), a.x.scales, reinterpret_cast<const u32x4*>(a.w_codes),
                            a.w_scales, a.m, a.n, mx_blocks(a.k), mx_scale_pitch(a.k), p.steps, p.tiles_m, p.tiles_j, o};
-        SLLM_TRY(launch_narrow(n, p.splits, out, dtype, stream));
+        SLLM_TRY(launch_narrow(n, p.tile, p.splits, out, dtype, stream));
     } else {
         WideArgs w;
         SLLM_TRY(stage_x(a, p, workspace, &w, stream));
@@ -235,7 +245,7 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
         w.w_rows = a.n, w.w_blocks = mx_blocks(a.k), w.w_scale_pitch = mx_scale_pitch(a.k);
         w.tiles_m = p.tiles_m, w.tiles_j = p.tiles_j;
         w.out_args = o;
-        SLLM_TRY(a.grad ? launch_grad(w, p.splits, out, dtype, stream) : launch_wide(w, p.splits, out, dtype, stream));
+        SLLM_TRY(a.grad ? launch_grad(w, p.tile, p.splits, out, dtype, stream) : launch_wide(w, p.tile, p.splits, out, dtype, stream));
     }
     return p.splits > 1 ? join(p, static_cast<const float*>(out), p.splits, a, stream) : SLLM_OK;
 }

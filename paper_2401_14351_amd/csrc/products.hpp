@@ -39,17 +39,37 @@ __device__ __forceinline__ const void* zero_vector() {
     return reinterpret_cast<const void*>(p);
 }
 
-// 16 bytes a lane straight to LDS: `to` is the same in all lanes of the wave, and
-// lane l's go to to + 16 l.
-__device__ __forceinline__ void load_to_lds(const void* from, void* to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+// A workgroup's LDS, by a variable and an offset into it.  The compiler keeps track
+// of which variable an access is to, and then waits for no load into another
+// before it, if the address space is known from the start and the address is a
+// short sum: offsets of a lane go through opaque().
+__device__ __forceinline__ uint32_t opaque(uint32_t v) {
+    asm("" : "+v"(v));
+    return v;
+}
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+
+template <typename V>
+__device__ __forceinline__ V lds_read(const uint8_t* p, uint32_t at) {
+    return *reinterpret_cast<const __attribute__((address_space(3))) V*>((const lds_u8*)p + at);
 }
 
-// Four bytes a lane, lane l's to to + 4 l.
-__device__ __forceinline__ void load_word_to_lds(const void* from, void* to) {
+template <typename V>
+__device__ __forceinline__ void lds_write(uint8_t* p, uint32_t at, V v) {
+    *reinterpret_cast<__attribute__((address_space(3))) V*>((lds_u8*)p + at) = v;
+}
+
+// 16 bytes a lane straight to LDS: p + at is the same in all lanes of the wave,
+// and lane l's go to 16 l bytes past it.
+__device__ __forceinline__ void load_to_lds(const void* from, uint8_t* p, uint32_t at) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                     (__attribute__((address_space(3))) void*)to, 4, 0, 0);
+                                     (__attribute__((address_space(3))) void*)((lds_u8*)p + at), 16, 0, 0);
+}
+
+// Four bytes a lane, lane l's to 4 l past p + at.
+__device__ __forceinline__ void load_word_to_lds(const void* from, uint8_t* p, uint32_t at) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                     (__attribute__((address_space(3))) void*)((lds_u8*)p + at), 4, 0, 0);
 }
 
 // Lanes of a wave see what each other wrote to LDS.
@@ -215,7 +235,7 @@ struct NarrowArgs {
     uint32_t tiles_m, tiles_j;
     OutArgs out_args;
 };
-int32_t launch_narrow(const NarrowArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
+int32_t launch_narrow(const NarrowArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
 constexpr uint32_t kNarrowStep = 512;  // depth whose scales are loaded together
 
 // At most kSkinnyRows rows of x, of any type (x_scales set: in MX FP4).
@@ -236,9 +256,9 @@ struct SkinnyArgs {
 int32_t launch_skinny(const SkinnyArgs& a, hipStream_t stream);
 constexpr uint64_t kSkinnyRows = 32;
 
-int32_t launch_wide(const WideArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
-int32_t launch_grad(const WideArgs& a, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
-constexpr uint32_t kWideTile = 256;  // rows of x and columns of the output a workgroup holds
+int32_t launch_wide(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
+int32_t launch_grad(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
+constexpr uint32_t kLargeTile = 256, kSmallTile = 128;  // rows of x and columns of the output a workgroup holds
 constexpr uint32_t kWideStep = 64;   // depth of a stage
 
 }  // namespace sllm
