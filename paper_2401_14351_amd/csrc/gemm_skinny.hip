@@ -10,28 +10,41 @@ namespace sllm {
 
 namespace {
 
-// Eight elements of x as the bfloat16 vectors whose sum they are.
+// The upper halves of two floats, a's first: their leading bfloat16s.
+__device__ __forceinline__ uint32_t upper_halves(float a, float b) {
+    return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
+}
+
+// Eight elements of x as the bfloat16 vectors whose sum they are: each but the
+// last takes the leading eight bits of what is left.  An infinity or a NaN is
+// whole in the first.
 template <typename X>
 struct Parts {
     static constexpr int n = sizeof(X) == 4 ? 3 : 2;
     bf16x8 v[n];
 
-    __device__ __forceinline__ static Parts of(const X (&x)[8]) {
-        Parts p;
-        float f[8];
+    __device__ __forceinline__ void set(const X (&x)[8]) {
+        u32x4 o[n];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = to_f32(x[e]);
+        for (int e = 0; e < 8; e += 2) {
+            // quiet a NaN: its payload may be all in the lower half
+            float a = __builtin_canonicalizef(to_f32(x[e])), b = __builtin_canonicalizef(to_f32(x[e + 1]));
+            constexpr int kNotFinite = 0x207;  // NaN, -inf and +inf as v_cmp_class has them
+            const bool a_ends = __builtin_amdgcn_classf(a, kNotFinite), b_ends = __builtin_amdgcn_classf(b, kNotFinite);
 #pragma unroll
-        for (int i = 0; i < n; ++i) {
-            u32x4 o;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t h = leading_bf16(f[e]);
-                o[e / 2] = e % 2 ? o[e / 2] | h << 16 : h;
+            for (int i = 0; i < n; ++i) {
+                o[i][e / 2] = upper_halves(a, b);
+                if (i + 1 == n) break;
+                a -= __uint_as_float(__float_as_uint(a) & 0xffff0000);
+                b -= __uint_as_float(__float_as_uint(b) & 0xffff0000);
+                if (i == 0) {
+                    a = a_ends ? 0.0f : a;
+                    b = b_ends ? 0.0f : b;
+                }
             }
-            p.v[i] = __builtin_bit_cast(bf16x8, o);
         }
-        return p;
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = __builtin_bit_cast(bf16x8, o[i]);
     }
 };
 
@@ -40,161 +53,241 @@ struct Parts<__bf16> {
     static constexpr int n = 1;
     bf16x8 v[1];
 
-    __device__ __forceinline__ static Parts of(const __bf16 (&x)[8]) {
-        Parts p;
+    __device__ __forceinline__ void set(const __bf16 (&x)[8]) { __builtin_memcpy(v, x, sizeof v); }
+};
+
+// X, or four bits of it a byte
+template <typename X>
+struct Element {
+    typedef X type;
+};
+template <>
+struct Element<void> {
+    typedef uint8_t type;
+};
+
+// Eight elements of a row from column c, those past the end zero.
+template <typename X>
+struct Eight {
+    X e[8];
+
+    __device__ __forceinline__ void load(const X* row, uint64_t c, uint64_t cols, bool vector) {
+        if (vector && c + 8 <= cols) {
+            u32x4 raw[sizeof(X) / 2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p.v[0][e] = x[e];
-        return p;
+            for (uint32_t i = 0; i < sizeof(X) / 2; ++i) raw[i] = reinterpret_cast<const u32x4*>(row + c)[i];
+            __builtin_memcpy(e, raw, sizeof e);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? row[c + i] : (X)0.0f;
+        }
     }
 };
 
-// Eight elements of a row from column c; those past the end are zero.
-template <typename X>
-__device__ __forceinline__ Parts<X> load_x(const X* row, uint64_t c, uint64_t cols) {
-    X x[8];
+// A workgroup makes 16 columns of the output, its waves each a run of the depth;
+// their sums are joined in LDS, first to last.  Of a step of 128 of the depth,
+// lane (r, g) loads block g of row r: the order in which the matrix instructions
+// take a step's columns does not matter as long as both sides have the same.
+//
+// Four steps, a group, are loaded together, and up to two groups are under way.  A
+// row's 16 scale bytes of a group are one load, four bytes a lane, which the
+// lanes then pass around: a load a step kept the address units as long as that
+// step's codes did.  x comes a step ahead, and only in the lanes that have a row
+// of it.
+constexpr uint32_t kGroupBlocks = 16;
+
+// A row's codes and scales of a group.
+struct Group {
+    u32x4 codes[4];
+    uint32_t scales;
+
+    __device__ __forceinline__ void load(const u32x4* row, const uint8_t* scale_row, uint32_t group, uint32_t g, uint64_t blocks) {
+        const uint64_t b = (uint64_t)group * kGroupBlocks;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = c + e < cols ? row[c + e] : (X)0.0f;
-    return Parts<X>::of(x);
+        for (int u = 0; u < 4; ++u) codes[u] = row[min(b + 4 * u + g, blocks - 1)];
+        scales = *reinterpret_cast<const uint32_t*>(scale_row + b + 4 * g);
+    }
+};
+
+// The scale bytes of step u, of what the four lanes of a row loaded: lane (r, u) has them.
+__device__ __forceinline__ uint32_t step_scales(uint32_t scales, int u, uint32_t r) {
+    return (uint32_t)__builtin_amdgcn_ds_bpermute((u * 16 + r) * 4, scales);
 }
 
-template <typename X>
-__device__ __forceinline__ Parts<X> load_x_vector(const X* p) {
-    X x[8];
-    constexpr int kVectors = sizeof(X) / 2;
-    u32x4 v[kVectors];
-#pragma unroll
-    for (int i = 0; i < kVectors; ++i) v[i] = reinterpret_cast<const u32x4*>(p)[i];
-    __builtin_memcpy(x, v, sizeof x);
-    return Parts<X>::of(x);
+// Word j of lane (r, g) becomes word g of lane (r, j): a 4 x 4 transpose among the
+// four lanes of a row, by swaps of half waves and of neighbouring rows of 16
+// lanes.  Then eight columns from 32 j + 8 g are lane (r, g)'s, and one load of x
+// takes 64 bytes of each row, not 16 bytes out of every 64.
+__device__ __forceinline__ u32x4 transpose4(u32x4 v) {
+    const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false));
+    const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false));
+    const u32x2 c = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false));
+    const u32x2 d = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false));
+    return u32x4{c[0], c[1], d[0], d[1]};
 }
 
-// A workgroup makes 16 NT columns of the output, its waves each a run of the
-// depth; their sums are joined in LDS, first to last.  Of a step of 128 of the
-// depth, lane (r, g) holds block g of row r: the order in which the matrix
-// instructions take a block's columns does not matter as long as both sides
-// have the same.
-template <typename X, int MT, int NT>
+// Rows of x a tile of 16 columns of the second operand holds.  A matrix
+// instruction takes 16 whatever they are, so where x has one row, or up to four,
+// a load fetches 16, or four, pieces of the depth for each, side by side, and all
+// but one piece are masked for each instruction: a 16th, or a quarter, of the
+// loads of x and of its splitting into parts.  The pieces' sums are columns of
+// their own until the end.
+template <typename X, int Rows, int MT>
 __global__ __launch_bounds__(1024) void skinny_product(SkinnyArgs a) {
     extern __shared__ float sums[];
     constexpr bool kMx = __is_same(X, void);
+    constexpr uint32_t kPieces = 16 / Rows;
+    static_assert((Rows == 1 || Rows == 4 || Rows == 16) && (Rows == 16 || MT == 1), "");
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t waves = blockDim.x >> 6, r = lane & 15, g = lane >> 4;
-    const uint64_t j0 = (uint64_t)blockIdx.x * 16 * NT;
-    const uint32_t s0 = (uint64_t)a.steps * wave / waves, s1 = (uint64_t)a.steps * (wave + 1) / waves;
+    const uint64_t j0 = (uint64_t)blockIdx.x * 16;
+    const uint32_t g0 = (uint64_t)a.groups * wave / waves, g1 = (uint64_t)a.groups * (wave + 1) / waves;
 
-    f32x4 acc[MT][NT];
+    f32x4 acc[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0, 0, 0, 0};
+    for (int m = 0; m < MT; ++m) acc[m] = f32x4{0, 0, 0, 0};
 
-    const u32x4* w_codes[NT];
-    const uint8_t* w_scales[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const uint64_t row = min(j0 + n * 16 + r, a.n - 1);
-        w_codes[n] = a.w_codes + row * a.blocks;
-        w_scales[n] = a.w_scales + row * a.scale_pitch;
-    }
+    const uint64_t row = min(j0 + r, a.n - 1);
+    const u32x4* const w_codes = a.w_codes + row * a.blocks;
+    const uint8_t* const w_scales = a.w_scales + row * a.scale_pitch;
+    bool has_x[MT];
     uint64_t x_row[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) x_row[m] = min((uint64_t)m * 16 + r, a.m - 1);
-
-    // Kept steps of the weight are loaded ahead of the ones at work.
-    constexpr uint32_t kAhead = 4;
-    struct Weight {
-        u32x4 codes[kAhead][NT];
-        uint32_t scale[kAhead][NT];
+    for (int m = 0; m < MT; ++m) {
+        x_row[m] = m * 16 + r / kPieces;
+        has_x[m] = x_row[m] < a.m;
+        x_row[m] = min(x_row[m], a.m - 1);
+    }
+    constexpr int kRing = sizeof(typename Element<X>::type) == 4 ? 1 : 2;  // registers hold no more
+    Group w[kRing];
+    auto load_w = [&](uint32_t group, int to) SLLM_INLINE {
+        if (group < g1) w[to].load(w_codes, w_scales, group, g, a.blocks);
     };
-    // Blocks past the row's or the run's end: x is zero there, the scale must be a number.
-    const uint64_t end = min(a.blocks, 4 * (uint64_t)s1);
-    auto load_w = [&](uint32_t s) {
-        Weight w;
+    auto run = [&](const auto& multiply) SLLM_INLINE {
 #pragma unroll
-        for (uint32_t u = 0; u < kAhead; ++u) {
-            const uint64_t b = 4 * ((uint64_t)s + u) + g, at = min(b, a.blocks - 1);
+        for (int i = 0; i < kRing; ++i) load_w(g0 + i, i);
+        for (uint32_t group = g0; group < g1; group += kRing)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                w.codes[u][n] = w_codes[n][at];
-                w.scale[u][n] = w_scales[n][at];
+            for (int i = 0; i < kRing; ++i) {
+                if (group + i >= g1) break;
+                multiply(group + i, w[i], i);
+                load_w(group + i + kRing, i);
             }
-        }
-        return w;
     };
-    Weight ahead = load_w(s0);
     if constexpr (kMx) {
-        for (uint32_t s = s0; s < s1; s += kAhead) {
-            const Weight w = ahead;
-            u32x4 x[kAhead][MT];
-            uint32_t xs[kAhead][MT];
+        u32x4 x[2][MT] = {};
+        uint32_t scales[MT] = {};
+        auto load_x = [&](uint32_t step, int to) SLLM_INLINE {
 #pragma unroll
-            for (uint32_t u = 0; u < kAhead; ++u)
+            for (int m = 0; m < MT; ++m)
+                if (has_x[m]) x[to][m] = static_cast<const u32x4*>(a.x)[x_row[m] * a.blocks + min((uint64_t)step * 4 + g, a.blocks - 1)];
+        };
+        if (g0 < g1) load_x(g0 * 4, 0);
+        run([&](uint32_t group, const Group& held, int) SLLM_INLINE {
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const uint64_t b = 4 * ((uint64_t)s + u) + g, at = min(b, a.blocks - 1);
-                    x[u][m] = static_cast<const u32x4*>(a.x)[x_row[m] * a.blocks + at];
-                    xs[u][m] = a.x_scales[x_row[m] * a.scale_pitch + at];
-                }
-            if (s + kAhead < s1) ahead = load_w(s + kAhead);
+            for (int m = 0; m < MT; ++m)
+                scales[m] = *reinterpret_cast<const uint32_t*>(a.x_scales + x_row[m] * a.scale_pitch + group * kGroupBlocks + 4 * g);
 #pragma unroll
-            for (uint32_t u = 0; u < kAhead; ++u) {
-                const uint32_t mask = 4 * ((uint64_t)s + u) + g < end ? ~0u : 0;
+            for (int u = 0; u < 4; ++u) {
+                load_x(group * 4 + u + 1, (u + 1) % 2);
+                // past the end of the depth x is zero, and the scales must be numbers
+                const uint32_t mask = (uint64_t)group * kGroupBlocks + 4 * u + g < a.blocks ? ~0u : 0;
+                const uint32_t ws = step_scales(held.scales, u, r) >> (8 * g) & mask;
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        acc[m][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                            fragment(w.codes[u][n]), fragment(x[u][m] & mask), acc[m][n], 4, 4, 0, w.scale[u][n] & mask, 0,
-                            xs[u][m] & mask);
+                    acc[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(held.codes[u]), fragment(x[u % 2][m] & mask), acc[m],
+                                                                              4, 4, 0, ws, 0, step_scales(scales[m], u, r) >> (8 * g) & mask);
             }
-        }
+        });
     } else {
         const X* x[MT];
 #pragma unroll
         for (int m = 0; m < MT; ++m) x[m] = static_cast<const X*>(a.x) + x_row[m] * a.x_stride;
-        auto step = [&](const u32x4 (&codes)[NT], const uint32_t (&scale)[NT], uint64_t b, auto load) {
-            u32x4 w[NT][4];
+        // the products of step u, j of a group with the parts of x
+        auto multiply = [&](uint32_t group, int u, int j, uint32_t codes, uint32_t scales, const Parts<X> (&p)[MT]) SLLM_INLINE {
+            const bool inside = (uint64_t)group * kGroupBlocks + 4 * u + j < a.blocks;  // else x is zero, any number does
+            const bf16x8 wide = __builtin_bit_cast(bf16x8, expand8(codes, mx_scale(inside ? scales >> (8 * j) & 0xff : 0)));
 #pragma unroll
-            for (int n = 0; n < NT; ++n) expand(codes[n], b < a.blocks ? scale[n] : 0, w[n]);
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const Parts<X> p = load(x[m], b * 32 + j * 8);
-#pragma unroll
-                    for (int i = 0; i < Parts<X>::n; ++i)
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[n][j]), p.v[i],
-                                                                                acc[m][n], 0, 0, 0);
+                for (int i = 0; i < Parts<X>::n; ++i) {
+                    u32x4 v = __builtin_bit_cast(u32x4, p[m].v[i]);
+                    if (Rows == 1) v = r == uint32_t(u * 4 + j) ? v : u32x4{0, 0, 0, 0};
+                    if (Rows == 4) v = r % 4 == uint32_t(j) ? v : u32x4{0, 0, 0, 0};
+                    acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide, __builtin_bit_cast(bf16x8, v), acc[m], 0, 0, 0);
                 }
         };
-        for (uint32_t s = s0; s < s1; s += kAhead) {
-            const Weight w = ahead;
-            if (s + kAhead < s1) ahead = load_w(s + kAhead);
-            if (a.vector && (uint64_t)(s + kAhead) * 128 <= a.depth) {
+        if constexpr (Rows < 16) {
+            // x of a group at a time, as far ahead as the weight
+            constexpr int kLoads = Rows;
+            Eight<X> raw[kRing][kLoads] = {};
+            auto load_x = [&](uint32_t group, int to) SLLM_INLINE {
+                if (group >= g1 || !has_x[0]) return;
 #pragma unroll
-                for (uint32_t u = 0; u < kAhead; ++u)
-                    if (s + u < s1)
-                        step(w.codes[u], w.scale[u], 4 * ((uint64_t)s + u) + g, [](const X* row, uint64_t c) { return load_x_vector(row + c); });
-            } else {
+                for (int q = 0; q < kLoads; ++q)
+                    raw[to][q].load(x[0], (uint64_t)group * 512 + q * 128 + r % kPieces * 32 + 8 * g, a.depth, a.vector);
+            };
 #pragma unroll
-                for (uint32_t u = 0; u < kAhead; ++u)
-                    if (s + u < s1)
-                        step(w.codes[u], w.scale[u], 4 * ((uint64_t)s + u) + g, [&](const X* row, uint64_t c) {
-                            return a.vector && c + 8 <= a.depth ? load_x_vector(row + c) : load_x(row, c, a.depth);
-                        });
-            }
+            for (int i = 0; i < kRing; ++i) load_x(g0 + i, i);
+            run([&](uint32_t group, const Group& held, int at) SLLM_INLINE {
+                Parts<X> p[kLoads][1];
+#pragma unroll
+                for (int q = 0; q < kLoads; ++q) p[q][0].set(raw[at][q].e);
+                load_x(group + kRing, at);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const u32x4 codes = transpose4(held.codes[u]);
+                    const uint32_t scales = step_scales(held.scales, u, r);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) multiply(group, u, j, codes[j], scales, p[u % kLoads]);
+                }
+            });
+        } else {
+            Eight<X> raw[2][4][MT] = {};
+            auto load_x = [&](uint32_t step, int to) SLLM_INLINE {
+                const uint64_t c = (uint64_t)step * 128 + 8 * g;
+                const bool whole = a.vector && (uint64_t)(step + 1) * 128 <= a.depth;
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+                    if (has_x[m])
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (whole)
+                                raw[to][j][m].load(x[m], c + j * 32, ~0ull, true);
+                            else
+                                raw[to][j][m].load(x[m], c + j * 32, a.depth, a.vector);
+                        }
+            };
+            if (g0 < g1) load_x(g0 * 4, 0);
+            run([&](uint32_t group, const Group& held, int) SLLM_INLINE {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (u < 3 || group + 1 < g1) load_x(group * 4 + u + 1, (u + 1) % 2);
+                    const u32x4 codes = transpose4(held.codes[u]);
+                    const uint32_t scales = step_scales(held.scales, u, r);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        Parts<X> p[MT];
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) p[m].set(raw[u % 2][j][m].e);
+                        multiply(group, u, j, codes[j], scales, p);
+                    }
+                }
+            });
         }
     }
+    if constexpr (Rows < 16) {
+#pragma unroll
+        for (uint32_t d = 1; d < kPieces; d *= 2)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[0][i] += __shfl_xor(acc[0][i], d);
+    }
 
-    // lane (r, g) has columns 4 g .. + 3 of the tile for row r of x
-    constexpr uint32_t kCols = 16 * NT, kSums = 16 * MT * kCols;
+    // lane (r, g) has columns 4 g .. + 3 of the tile for row r / kPieces of x
+    constexpr uint32_t kCols = 16, kSums = Rows * MT * kCols;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-            *reinterpret_cast<f32x4*>(sums + wave * kSums + (m * 16 + r) * kCols + n * 16 + g * 4) = acc[m][n];
+        if (r % kPieces == 0) *reinterpret_cast<f32x4*>(sums + wave * kSums + (m * 16 + r / kPieces) * kCols + g * 4) = acc[m];
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < kSums; i += blockDim.x) {
         const uint64_t m = i / kCols, j = j0 + i % kCols;
@@ -211,31 +304,34 @@ __global__ __launch_bounds__(1024) void skinny_product(SkinnyArgs a) {
     }
 }
 
-template <typename X, int MT, int NT>
+template <typename X, int Rows, int MT>
 void launch(const SkinnyArgs& a, hipStream_t stream) {
-    const uint32_t grid = (uint32_t)((a.n + 16 * NT - 1) / (16 * NT));
-    // enough waves to fill the GPU, but two steps of the depth for each
+    const uint32_t grid = (uint32_t)((a.n + 15) / 16);
+    // enough waves to fill the GPU, two groups of the depth for each where there are as many
     uint32_t waves = 4;
-    while (waves < 16 && grid * waves < 2048 && a.steps >= waves * 4) waves *= 2;
-    while (waves > 1 && a.steps < waves) waves /= 2;
-    skinny_product<X, MT, NT><<<grid, waves * 64, waves * 16 * MT * 16 * NT * 4, stream>>>(a);
-}
-
-template <typename X>
-void launch_rows(const SkinnyArgs& a, hipStream_t stream) {
-    if (a.m <= 16)
-        launch<X, 1, 1>(a, stream);
-    else
-        launch<X, 2, 1>(a, stream);
+    while (waves < 16 && (a.groups > waves * 2 || (grid * waves < 2048 && a.groups > waves))) waves *= 2;
+    while (waves > 1 && a.groups < waves) waves /= 2;
+    skinny_product<X, Rows, MT><<<grid, waves * 64, waves * Rows * MT * 16 * 4, stream>>>(a);
 }
 
 }  // namespace
 
 int32_t launch_skinny(const SkinnyArgs& a, hipStream_t stream) {
-    if (a.x_scales)
-        launch_rows<void>(a, stream);
+    if (a.x_scales && a.m <= 16)
+        launch<void, 16, 1>(a, stream);
+    else if (a.x_scales)
+        launch<void, 16, 2>(a, stream);
+    else if (a.m > 16)
+        launch<__bf16, 16, 2>(a, stream);
     else
-        SLLM_BY_DTYPE(a.x_dtype, X, launch_rows<X>(a, stream));
+        SLLM_BY_DTYPE(a.x_dtype, X, {
+            if (a.m == 1)
+                launch<X, 1, 1>(a, stream);
+            else if (a.m <= 4)
+                launch<X, 4, 1>(a, stream);
+            else
+                launch<X, 16, 1>(a, stream);
+        });
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
 }

@@ -121,7 +121,7 @@ Plan plan_linear(const LinearLaunch& a) {
     Plan p;
     p.depth = a.grad ? a.n : a.k;
     p.cols = a.grad ? a.k : a.n;
-    p.skinny = !a.grad && a.m <= kSkinnyRows;
+    p.skinny = !a.grad && a.m <= (a.x.codes || a.x.dtype == SLLM_DTYPE_BF16 ? 32 : 16);
     if (!p.depth || !a.m || !p.cols || p.skinny) return p;
     if (!a.x.codes) p.parts = a.x.dtype == SLLM_DTYPE_BF16 ? 1 : a.x.dtype == SLLM_DTYPE_F16 ? 2 : 3;
     // The kernel reads x in aligned vectors of eight.
@@ -261,7 +261,7 @@ int32_t launch_linear(const LinearLaunch& a, void* workspace, hipStream_t stream
         const bool vector = reinterpret_cast<uintptr_t>(a.x.data) % 16 == 0 && (a.m == 1 || row_bytes % 16 == 0);
         return launch_skinny(SkinnyArgs{a.x.codes ? a.x.codes : a.x.data, a.x.scales, a.m, a.n, a.k, a.x.stride, a.x.dtype, vector,
                                         reinterpret_cast<const u32x4*>(a.w_codes), a.w_scales, mx_blocks(a.k), mx_scale_pitch(a.k),
-                                        (uint32_t)ceil_div(a.k, 128), a.out, a.out_stride, a.out_dtype}, stream);
+                                        (uint32_t)ceil_div(a.k, 512), a.out, a.out_stride, a.out_dtype}, stream);
     }
     if (plan.depth) return launch_tiled(a, plan, workspace, stream);
     // a depth of zero: sums of nothing

@@ -238,7 +238,7 @@ struct NarrowArgs {
 int32_t launch_narrow(const NarrowArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
 constexpr uint32_t kNarrowStep = 512;  // depth whose scales are loaded together
 
-// At most kSkinnyRows rows of x, of any type (x_scales set: in MX FP4).
+// At most 32 rows of x in bfloat16 or MX FP4 (x_scales set), 16 in float16 or float.
 struct SkinnyArgs {
     const void* x;
     const uint8_t* x_scales;
@@ -248,13 +248,12 @@ struct SkinnyArgs {
     const u32x4* w_codes;
     const uint8_t* w_scales;
     uint64_t blocks, scale_pitch;
-    uint32_t steps;   // of 128 of the depth
+    uint32_t groups;  // of 512 of the depth
     void* out;
     uint64_t out_stride;
     uint32_t out_dtype;
 };
 int32_t launch_skinny(const SkinnyArgs& a, hipStream_t stream);
-constexpr uint64_t kSkinnyRows = 32;
 
 int32_t launch_wide(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
 int32_t launch_grad(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
