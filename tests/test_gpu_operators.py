@@ -578,3 +578,17 @@ def test_offsets_past_32_bits():
     grad = op.embedding_grad(x, torch.tensor([rows - 2, 5], device="cuda"), rows)
     assert torch.equal(grad[rows - 2], x[0]) and torch.equal(grad[5], x[1])
     assert not grad[6:rows - 2].any() and not grad[:5].any() and not grad[-1].any()
+
+
+@pytest.mark.parametrize("n", [1, 1000, 1024, 1025, 5000, 20000])
+def test_embedding_grad_of_a_very_tall_table(n):
+    """Tables of 2^22 rows and more sort by wider keys; just below that, by the narrow ones."""
+    for vocab in ((1 << 22) - 2, (1 << 22) - 1, 1 << 22, (1 << 22) + 7):
+        dy = normal((n, 8), torch.float32, n)
+        g = gen(vocab)
+        ids = torch.randint(vocab - 50, vocab + 2, (n,), generator=g, device="cuda")
+        grad = op.embedding_grad(dy, ids, vocab)
+        want = O.embedding_grad(host(dy), (ids - (vocab - 60)).tolist(), 60, 1.0)
+        size = O.embedding_grad(np.abs(host(dy)), (ids - (vocab - 60)).tolist(), 60, 1.0)
+        assert_close(grad[-60:], want, 2 * (n + 8) * 2.0 ** -24 * size, torch.float32)
+        assert not grad[:-60].any()
