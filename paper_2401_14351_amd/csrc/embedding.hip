@@ -268,24 +268,35 @@ __global__ __launch_bounds__(256) void sum_runs(GradArgs a, const S* dy, T* grad
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     uint32_t token = token_of(a.keys[first]);
     bool whole = first == 0 || token_of(a.keys[first - 1]) != token;  // the run starts here
-    for (uint32_t i = first; i < end; ++i) {
-        const uint64_t key = a.keys[i];
-        if (token_of(key) != token) {
-            if (whole)
-                write_row<Vec>(a, grad, token, c, sum);
-            else
+    // rows are loaded some ahead of the sum, which a change of token holds up
+    constexpr uint32_t kAhead = 4;
+    for (uint32_t i0 = first; i0 < end; i0 += kAhead) {
+        uint64_t keys[kAhead];
+        float v[kAhead][8];
 #pragma unroll
-                for (uint32_t e = 0; e < 8; ++e) a.partial[(uint64_t)w * 2 * a.pitch + c + e] = sum[e];
-            token = token_of(key);
-            whole = true;
-#pragma unroll
-            for (uint32_t e = 0; e < 8; ++e) sum[e] = 0;
+        for (uint32_t u = 0; u < kAhead; ++u) {
+            keys[u] = a.keys[min(i0 + u, end - 1)];
+            const uint64_t position = token_of(keys[u]) < a.vocab ? (uint32_t)keys[u] : 0;
+            load8<Vec>(dy + position * a.dy_stride, c, a.dim, v[u]);
         }
-        if (token >= a.vocab) return;
-        float v[8];
-        load8<Vec>(dy + (uint64_t)(uint32_t)key * a.dy_stride, c, a.dim, v);
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) sum[e] += v[e];
+        for (uint32_t u = 0; u < kAhead; ++u) {
+            if (i0 + u >= end) break;
+            if (token_of(keys[u]) != token) {
+                if (whole)
+                    write_row<Vec>(a, grad, token, c, sum);
+                else
+#pragma unroll
+                    for (uint32_t e = 0; e < 8; ++e) a.partial[(uint64_t)w * 2 * a.pitch + c + e] = sum[e];
+                token = token_of(keys[u]);
+                whole = true;
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) sum[e] = 0;
+            }
+            if (token >= a.vocab) return;
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e) sum[e] += v[u][e];
+        }
     }
     const bool goes_on = end < a.n && token_of(a.keys[end]) == token;
     if (whole && !goes_on)
