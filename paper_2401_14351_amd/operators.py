@@ -44,7 +44,7 @@ class Mx4:
     """A matrix in MX FP4: ``codes`` (rows, blocks * 16) and ``scales`` (rows,
     blocks rounded up to 16), both contiguous uint8, laid out as ``sllm_mx``."""
 
-    __slots__ = ("codes", "scales", "rows", "cols", "_struct")
+    __slots__ = ("codes", "scales", "rows", "cols", "_struct", "_device")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int):
         code_pitch, scale_pitch = _pitches(cols)
@@ -54,16 +54,22 @@ class Mx4:
                                  f"got {t.dtype} with shape {tuple(t.shape)} and strides {t.stride()}")
         if codes.shape[0] != scales.shape[0] or codes.device != scales.device:
             raise ValueError("codes and scales differ in rows or device")
+        self._set(codes, scales, cols)
+
+    def _set(self, codes, scales, cols):
         self.codes, self.scales = codes, scales
         self.rows, self.cols = codes.shape[0], cols
         self._struct = binding.Mx(codes.data_ptr(), scales.data_ptr(), self.rows, cols)
+        self._device = codes.get_device()
 
     @classmethod
     def empty(cls, rows: int, cols: int, device) -> "Mx4":
         """A matrix whose contents are not set."""
         code_pitch, scale_pitch = _pitches(cols)
-        return cls(torch.empty(rows, code_pitch, dtype=torch.uint8, device=device),
-                   torch.empty(rows, scale_pitch, dtype=torch.uint8, device=device), cols)
+        q = cls.__new__(cls)
+        q._set(torch.empty((rows, code_pitch), dtype=torch.uint8, device=device),
+               torch.empty((rows, scale_pitch), dtype=torch.uint8, device=device), cols)
+        return q
 
     @property
     def shape(self):
@@ -94,24 +100,27 @@ def _matrix(t: torch.Tensor, name: str) -> binding.Matrix:
         raise ValueError(f"{name}: {t.dtype} is not float32, float16 or bfloat16")
     if not t.is_cuda:
         raise ValueError(f"{name} is not in device memory")
-    if t.dim() == 0:
+    dim = t.dim()
+    if dim == 0:
         raise ValueError(f"{name} has no dimensions")
-    cols = t.shape[-1]
-    if cols > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name}: the elements of a row are not adjacent (strides {t.stride()})")
-    if t.dim() == 1:
-        return binding.Matrix(t.data_ptr(), 1, cols, cols, code, 0)
-    if t.dim() > 2:
+    if dim > 2:
+        cols = t.shape[-1]
         rows = t.numel() // cols if cols else t.shape[:-1].numel()
-        if rows and cols:
-            try:
-                t = t.view(rows, cols)
-            except RuntimeError:
-                raise ValueError(f"{name}: its rows are not apart by one stride (strides {t.stride()})") from None
-        else:
+        if not (rows and cols):
             return binding.Matrix(t.data_ptr(), rows, cols, cols, code, 0)
+        try:
+            t = t.view(rows, cols)
+        except RuntimeError:
+            raise ValueError(f"{name}: its rows are not apart by one stride (strides {t.stride()})") from None
+    strides = t.stride()
+    cols = t.shape[-1]
+    if cols > 1 and strides[-1] != 1:
+        raise ValueError(f"{name}: the elements of a row are not adjacent (strides {strides})")
+    if dim == 1:
+        return binding.Matrix(t.data_ptr(), 1, cols, cols, code, 0)
+    rows = t.shape[0]
     # a single row's or no row's stride says nothing
-    return binding.Matrix(t.data_ptr(), t.shape[0], cols, t.stride(0) if t.shape[0] > 1 else cols, code, 0)
+    return binding.Matrix(t.data_ptr(), rows, cols, strides[0] if rows > 1 else cols, code, 0)
 
 
 def _ids(t: torch.Tensor) -> binding.Ids:
@@ -125,37 +134,37 @@ def _ids(t: torch.Tensor) -> binding.Ids:
     return binding.Ids(t.data_ptr(), t.numel(), bits, 0)
 
 
-class _On:
-    """The stream of a call: what is allocated inside belongs to it, and its
-    inputs are kept from reuse until it has passed the call."""
+def _index(t) -> int:
+    return t._device if isinstance(t, Mx4) else t.get_device()
 
-    __slots__ = ("device", "ptr", "_stream", "_context")
 
-    def __init__(self, device: torch.device, stream, *inputs):
-        for t in inputs:
-            if t.device != device:
-                raise ValueError(f"inputs on {device} and {t.device}")
-        self.device = device.index
-        self._context = None
-        if stream is None:
-            self.ptr = torch.cuda.current_stream(device).cuda_stream
-            return
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(stream, device=device)
-        self.ptr = stream.cuda_stream
-        self._context = torch.cuda.stream(stream)
-        for t in inputs:
+def _one_device(first, *others) -> int:
+    """The index of the device that all of them are on."""
+    device = _index(first)
+    for t in others:
+        if t is not None and _index(t) != device:
+            raise ValueError(f"inputs on {first.device} and {t.device}")
+    return device
+
+
+# torch.cuda.current_stream(device).cuda_stream without the stream object, which costs 2 us
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _on_stream(stream, operator, *args, keep=(), **kwargs):
+    """Run ``operator`` with ``stream`` current: what it allocates then belongs to
+    that stream, and its inputs are kept from reuse until it has passed the call."""
+    device = keep[0].device
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    with torch.cuda.stream(stream):
+        result = operator(*args, **kwargs)
+    for t in keep:
+        if t is not None:
             for u in ((t.codes, t.scales) if isinstance(t, Mx4) else (t,)):
                 u.record_stream(stream)
-
-    def __enter__(self):
-        if self._context is not None:
-            self._context.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self._context is not None:
-            self._context.__exit__(*exc)
+    return result
 
 
 def _output(out: Optional[torch.Tensor], shape, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
@@ -167,30 +176,9 @@ def _output(out: Optional[torch.Tensor], shape, dtype: torch.dtype, device: torc
 
 
 def _refuse_grad(*tensors):
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        raise ValueError("an operator that writes to a given tensor takes no part in autograd")
-
-
-def mx4_quantize(x: torch.Tensor, out: Optional[Mx4] = None, stream=None) -> Mx4:
-    """The rows of x (its leading dimensions flattened) in MX FP4."""
-    src = _matrix(x, "x")
-    if out is not None and out.shape != (src.rows, src.cols):
-        raise ValueError(f"out: expected {src.rows} x {src.cols}, got {out.rows} x {out.cols}")
-    with _On(x.device, stream, x, *(() if out is None else (out,))) as on:
-        if out is None:
-            out = Mx4.empty(src.rows, src.cols, x.device)
-        binding.check(binding.lib().sllm_mx_quantize(src, out._struct, on.device, on.ptr))
-    return out
-
-
-def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
-                   stream=None) -> torch.Tensor:
-    """The values q stands for, rounded to ``dtype`` (or the type of ``out``)."""
-    _refuse_grad(out)
-    with _On(q.device, stream, q, *(() if out is None else (out,))) as on:
-        out = _output(out, (q.rows, q.cols), dtype, q.device)
-        binding.check(binding.lib().sllm_mx_dequantize(q._struct, _matrix(out, "out"), on.device, on.ptr))
-    return out
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError("an operator that writes to a given tensor takes no part in autograd")
 
 
 def _workspace(query, *args) -> int:
@@ -200,6 +188,43 @@ def _workspace(query, *args) -> int:
     return n.value
 
 
+def _call(fn, query, operands, out, device):
+    """fn over its operands and output, with the workspace that the query asks for."""
+    n = _workspace(query, *operands)
+    if n:
+        ws = torch.empty(n, dtype=torch.uint8, device=torch.device("cuda", device))
+        code = fn(*operands, out, ws.data_ptr(), n, device, _raw_stream(device))
+    else:
+        code = fn(*operands, out, None, 0, device, _raw_stream(device))
+    binding.check(code)
+
+
+def mx4_quantize(x: torch.Tensor, out: Optional[Mx4] = None, stream=None) -> Mx4:
+    """The rows of x (its leading dimensions flattened) in MX FP4."""
+    if stream is not None:
+        return _on_stream(stream, mx4_quantize, x, out, keep=(x, out))
+    src = _matrix(x, "x")
+    device = _one_device(x, out)
+    if out is None:
+        out = Mx4.empty(src.rows, src.cols, x.device)
+    elif out.rows != src.rows or out.cols != src.cols:
+        raise ValueError(f"out: expected {src.rows} x {src.cols}, got {out.rows} x {out.cols}")
+    binding.check(binding.lib().sllm_mx_quantize(src, out._struct, device, _raw_stream(device)))
+    return out
+
+
+def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """The values q stands for, rounded to ``dtype`` (or the type of ``out``)."""
+    if stream is not None:
+        return _on_stream(stream, mx4_dequantize, q, dtype, out, keep=(q, out))
+    _refuse_grad(out)
+    device = _one_device(q)
+    out = _output(out, (q.rows, q.cols), dtype, q.device)
+    binding.check(binding.lib().sllm_mx_dequantize(q._struct, _matrix(out, "out"), device, _raw_stream(device)))
+    return out
+
+
 def mx4_linear(x: Union[torch.Tensor, Mx4], w: Mx4, out: Optional[torch.Tensor] = None,
                out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
     """``x @ w.T``: (..., w.rows) for x (..., w.cols).
@@ -207,37 +232,32 @@ def mx4_linear(x: Union[torch.Tensor, Mx4], w: Mx4, out: Optional[torch.Tensor] 
     x as a tensor keeps its own precision; as an :class:`Mx4` both sides are in
     four bits.  The result has ``out_dtype``, by default x's type (bfloat16 for
     an :class:`Mx4`)."""
+    if stream is not None:
+        return _on_stream(stream, mx4_linear, x, w, out, out_dtype, keep=(x, w, out))
+    _refuse_grad(out)
     if isinstance(x, Mx4):
-        _refuse_grad(out)
-        return _linear_mx(x, w, out, out_dtype, stream)
-    if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
-        _refuse_grad(out)
+        return _linear_mx(x, w, out, out_dtype)
+    if x.requires_grad and torch.is_grad_enabled():
         if out is not None:
             raise ValueError("an operator that writes to a given tensor takes no part in autograd")
-        return _Linear.apply(x, w, out_dtype, stream)
-    return _linear(x, w, out, out_dtype, stream)
+        return _Linear.apply(x, w, out_dtype)
+    return _linear(x, w, out, out_dtype)
 
 
-def _linear(x, w, out, out_dtype, stream):
+def _linear(x, w, out, out_dtype):
     L = binding.lib()
-    xs = _matrix(x, "x")
-    with _On(x.device, stream, x, w, *(() if out is None else (out,))) as on:
-        out = _output(out, x.shape[:-1] + (w.rows,), out_dtype or x.dtype, x.device)
-        n = _workspace(L.sllm_mx_linear_workspace, xs, w._struct)
-        ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
-        binding.check(L.sllm_mx_linear(xs, w._struct, _matrix(out, "out"), ws.data_ptr() if n else None, n, on.device,
-                                       on.ptr))
+    src = _matrix(x, "x")
+    device = _one_device(x, w)
+    out = _output(out, x.shape[:-1] + (w.rows,), out_dtype or x.dtype, x.device)
+    _call(L.sllm_mx_linear, L.sllm_mx_linear_workspace, (src, w._struct), _matrix(out, "out"), device)
     return out
 
 
-def _linear_mx(x, w, out, out_dtype, stream):
+def _linear_mx(x, w, out, out_dtype):
     L = binding.lib()
-    with _On(x.device, stream, x, w, *(() if out is None else (out,))) as on:
-        out = _output(out, (x.rows, w.rows), out_dtype or torch.bfloat16, x.device)
-        n = _workspace(L.sllm_mx_linear_mx_workspace, x._struct, w._struct)
-        ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
-        binding.check(L.sllm_mx_linear_mx(x._struct, w._struct, _matrix(out, "out"), ws.data_ptr() if n else None, n,
-                                          on.device, on.ptr))
+    device = _one_device(x, w)
+    out = _output(out, (x.rows, w.rows), out_dtype or torch.bfloat16, x.device)
+    _call(L.sllm_mx_linear_mx, L.sllm_mx_linear_mx_workspace, (x._struct, w._struct), _matrix(out, "out"), device)
     return out
 
 
@@ -245,29 +265,28 @@ def mx4_linear_grad(dy: torch.Tensor, w: Mx4, out: Optional[torch.Tensor] = None
                     out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
     """``dy @ w``, the gradient of :func:`mx4_linear` by x: (..., w.cols) for dy
     (..., w.rows)."""
+    if stream is not None:
+        return _on_stream(stream, mx4_linear_grad, dy, w, out, out_dtype, keep=(dy, w, out))
     _refuse_grad(dy, out)
     L = binding.lib()
-    ds = _matrix(dy, "dy")
-    with _On(dy.device, stream, dy, w, *(() if out is None else (out,))) as on:
-        out = _output(out, dy.shape[:-1] + (w.cols,), out_dtype or dy.dtype, dy.device)
-        n = _workspace(L.sllm_mx_linear_grad_workspace, ds, w._struct)
-        ws = torch.empty(n, dtype=torch.uint8, device=dy.device) if n else None
-        binding.check(L.sllm_mx_linear_grad(ds, w._struct, _matrix(out, "out"), ws.data_ptr() if n else None, n,
-                                            on.device, on.ptr))
+    src = _matrix(dy, "dy")
+    device = _one_device(dy, w)
+    out = _output(out, dy.shape[:-1] + (w.cols,), out_dtype or dy.dtype, dy.device)
+    _call(L.sllm_mx_linear_grad, L.sllm_mx_linear_grad_workspace, (src, w._struct), _matrix(out, "out"), device)
     return out
 
 
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, out_dtype, stream):
+    def forward(ctx, x, w, out_dtype):
         ctx.w, ctx.dtype = w, x.dtype
-        return _linear(x, w, None, out_dtype, stream)
+        return _linear(x, w, None, out_dtype)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         # gradients of sums and means arrive with strides of 0
-        return mx4_linear_grad(dy.contiguous(), ctx.w, out_dtype=ctx.dtype), None, None, None
+        return mx4_linear_grad(dy.contiguous(), ctx.w, out_dtype=ctx.dtype), None, None
 
 
 def embedding(table: Union[torch.Tensor, Mx4], tokens: torch.Tensor, scale: float = 1.0,
@@ -277,26 +296,28 @@ def embedding(table: Union[torch.Tensor, Mx4], tokens: torch.Tensor, scale: floa
     ``tokens.shape + (columns,)``, in ``out_dtype`` (by default the table's
     type, bfloat16 for an :class:`Mx4`).  A token outside the table is padding:
     a row of zeros."""
-    if not isinstance(table, Mx4) and torch.is_grad_enabled() and table.requires_grad:
-        _refuse_grad(out)
+    if stream is not None:
+        return _on_stream(stream, embedding, table, tokens, scale, out, out_dtype, keep=(table, tokens, out))
+    _refuse_grad(out)
+    if not isinstance(table, Mx4) and table.requires_grad and torch.is_grad_enabled():
         if out is not None:
             raise ValueError("an operator that writes to a given tensor takes no part in autograd")
-        return _Embedding.apply(table, tokens, scale, out_dtype, stream)
-    return _embedding(table, tokens, scale, out, out_dtype, stream)
+        return _Embedding.apply(table, tokens, scale, out_dtype)
+    return _embedding(table, tokens, scale, out, out_dtype)
 
 
-def _embedding(table, tokens, scale, out, out_dtype, stream):
+def _embedding(table, tokens, scale, out, out_dtype):
     L = binding.lib()
     ids = _ids(tokens)
-    mx = isinstance(table, Mx4)
-    if not mx and table.dim() != 2:
+    device = _one_device(table, tokens)
+    if isinstance(table, Mx4):
+        fn, rows, cols, dtype = L.sllm_embedding_mx, table._struct, table.cols, torch.bfloat16
+    elif table.dim() == 2:
+        fn, rows, cols, dtype = L.sllm_embedding, _matrix(table, "table"), table.shape[1], table.dtype
+    else:
         raise ValueError(f"table: expected rows and columns, got shape {tuple(table.shape)}")
-    with _On(table.device, stream, table, tokens, *(() if out is None else (out,))) as on:
-        cols = table.cols if mx else table.shape[1]
-        out = _output(out, tokens.shape + (cols,), out_dtype or (torch.bfloat16 if mx else table.dtype), table.device)
-        fn = L.sllm_embedding_mx if mx else L.sllm_embedding
-        binding.check(fn(table._struct if mx else _matrix(table, "table"), ids, scale, _matrix(out, "out"), on.device,
-                         on.ptr))
+    out = _output(out, tokens.shape + (cols,), out_dtype or dtype, table.device)
+    binding.check(fn(rows, ids, scale, _matrix(out, "out"), device, _raw_stream(device)))
     return out
 
 
@@ -306,32 +327,35 @@ def embedding_grad(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: fl
     """The gradient of :func:`embedding` by a table of ``vocab`` rows: row v is
     ``scale`` times the sum of dy over the positions of token v, in their order.
     ``accumulate`` adds it to ``out`` instead of replacing its contents."""
+    if stream is not None:
+        return _on_stream(stream, embedding_grad, dy, tokens, vocab, scale, out, out_dtype, accumulate,
+                          keep=(dy, tokens, out))
     _refuse_grad(dy, out)
     if accumulate and out is None:
         raise ValueError("accumulate needs a gradient to add to")
     if dy.shape[:-1] != tokens.shape:
         raise ValueError(f"dy of shape {tuple(dy.shape)} for tokens of shape {tuple(tokens.shape)}")
     L = binding.lib()
-    ids, ds = _ids(tokens), _matrix(dy, "dy")
-    with _On(dy.device, stream, dy, tokens, *(() if out is None else (out,))) as on:
-        out = _output(out, (vocab, dy.shape[-1]), out_dtype or dy.dtype, dy.device)
-        grad = _matrix(out, "out")
-        n = _workspace(L.sllm_embedding_grad_workspace, ids.n, grad)
-        ws = torch.empty(n, dtype=torch.uint8, device=dy.device) if n else None
-        binding.check(L.sllm_embedding_grad(ds, ids, scale, 1 if accumulate else 0, grad, ws.data_ptr() if n else None, n,
-                                            on.device, on.ptr))
+    ids, src = _ids(tokens), _matrix(dy, "dy")
+    device = _one_device(dy, tokens)
+    out = _output(out, (vocab, dy.shape[-1]), out_dtype or dy.dtype, dy.device)
+    grad = _matrix(out, "out")
+    n = _workspace(L.sllm_embedding_grad_workspace, ids.n, grad)
+    ws = torch.empty(n, dtype=torch.uint8, device=dy.device) if n else None
+    binding.check(L.sllm_embedding_grad(src, ids, scale, 1 if accumulate else 0, grad, ws.data_ptr() if n else None, n,
+                                        device, _raw_stream(device)))
     return out
 
 
 class _Embedding(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, table, tokens, scale, out_dtype, stream):
+    def forward(ctx, table, tokens, scale, out_dtype):
         ctx.save_for_backward(tokens)
         ctx.vocab, ctx.dtype, ctx.scale = table.shape[0], table.dtype, scale
-        return _embedding(table, tokens, scale, None, out_dtype, stream)
+        return _embedding(table, tokens, scale, None, out_dtype)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         (tokens,) = ctx.saved_tensors
-        return embedding_grad(dy.contiguous(), tokens, ctx.vocab, ctx.scale, out_dtype=ctx.dtype), None, None, None, None
+        return embedding_grad(dy.contiguous(), tokens, ctx.vocab, ctx.scale, out_dtype=ctx.dtype), None, None, None
