@@ -218,7 +218,15 @@ struct GradArgs {
     uint32_t lanes;        // of a row: 32, 64, 128 or 256
     uint32_t chunks;       // of a row, lanes * 8 columns each
     uint32_t sum_blocks;   // workgroups that sum; the rest clear rows
+    // of a row to clear: its bytes, those a lane stores at once (16, 4 or 2), and its lanes (a power of two)
+    uint64_t row_bytes;
+    uint32_t unit, clear_lanes;
 };
+
+template <typename U>
+__device__ __forceinline__ void clear_row(uint8_t* row, uint64_t bytes, uint32_t lane, uint32_t lanes) {
+    for (uint64_t i = lane; i < bytes / sizeof(U); i += lanes) reinterpret_cast<U*>(row)[i] = U{};
+}
 
 // A table row's gradient from its whole sum.
 template <bool Vec, typename T>
@@ -253,11 +261,17 @@ __global__ __launch_bounds__(256) void sum_runs(GradArgs a, const S* dy, T* grad
             named[threadIdx.x] = lo < a.n && token_of(a.keys[lo]) == row0 + threadIdx.x;
         }
         __syncthreads();
-        const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        for (uint32_t r = threadIdx.x / a.lanes; r < kZeroRows && row0 + r < a.vocab; r += 256 / a.lanes)
-            if (!named[r])
-                for (uint32_t c = threadIdx.x % a.lanes * 8; c < a.dim; c += a.lanes * 8)
-                    store8<Vec>(grad + (uint64_t)(row0 + r) * a.grad_stride, c, a.dim, zero);
+        const uint32_t lane = threadIdx.x & (a.clear_lanes - 1), shift = __builtin_ctz(a.clear_lanes);
+        for (uint32_t r = threadIdx.x >> shift; r < kZeroRows && row0 + r < a.vocab; r += 256u >> shift) {
+            if (named[r]) continue;
+            uint8_t* row = reinterpret_cast<uint8_t*>(grad + (uint64_t)(row0 + r) * a.grad_stride);
+            if (a.unit == 16)
+                clear_row<u32x4>(row, a.row_bytes, lane, a.clear_lanes);
+            else if (a.unit == 4)
+                clear_row<uint32_t>(row, a.row_bytes, lane, a.clear_lanes);
+            else
+                clear_row<uint16_t>(row, a.row_bytes, lane, a.clear_lanes);
+        }
         return;
     }
     const uint32_t per = 256 / a.lanes;  // windows of a workgroup
@@ -448,6 +462,11 @@ int32_t launch_embedding_grad(const EmbeddingGradLaunch& a, void* workspace, hip
     const uint64_t grid = sums + (a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows));
     if (grid > UINT32_MAX / 256) return fail(SLLM_E_RANGE, "gradient too large");
     g.sum_blocks = (uint32_t)sums;
+    const uint64_t size = element_bytes(a.grad_dtype), row_bytes = a.dim * size;
+    const uint64_t steps = reinterpret_cast<uintptr_t>(a.grad) | row_bytes | (a.vocab > 1 ? a.grad_stride * size : 0);
+    g.row_bytes = row_bytes;
+    g.unit = steps % 16 == 0 ? 16 : steps % 4 == 0 ? 4 : 2;
+    for (g.clear_lanes = 1; g.clear_lanes < 256 && g.clear_lanes < row_bytes / g.unit;) g.clear_lanes *= 2;
     const bool vec = a.dim % 8 == 0 && on_vectors(a.dy, a.n, a.dy_stride, a.dy_dtype) &&
                      on_vectors(a.grad, a.vocab, a.grad_stride, a.grad_dtype);
     SLLM_BY_DTYPE(a.dy_dtype, S, SLLM_BY_DTYPE(a.grad_dtype, T, return vec ? (launch_sums<true, S, T>(g, a, grid, stream))
