@@ -108,7 +108,7 @@ __global__ __launch_bounds__(256) void lookup(Lookup a, T* out) {
 constexpr uint32_t kSortTile = 1024;  // keys a workgroup sorts
 constexpr uint32_t kMergeRuns = 16;   // sorted runs merged at once, a lane each
 constexpr uint32_t kWindow = 16;      // sorted positions a workgroup sums together
-constexpr uint32_t kZeroRows = 16;    // table rows a workgroup looks up and clears
+constexpr uint32_t kZeroRows = 16;    // table rows a workgroup looks up and clears, 16 lanes each
 
 __device__ __forceinline__ uint32_t token_of(uint64_t key) { return (uint32_t)(key >> 32); }
 
@@ -242,24 +242,25 @@ __device__ __forceinline__ void write_row(const GradArgs& a, T* grad, uint32_t t
 // The first workgroups take windows of sorted positions.  A run of equal tokens
 // inside one window becomes its row at once; one that goes on into the next
 // window, or came from the one before, leaves its sum for join_runs.  The other
-// workgroups clear the rows that no key names.
+// workgroups clear the rows that no key names, each row looked for by 16 lanes:
+// the search is a chain of loads that nothing can be written before the end of.
 template <bool Vec, typename S, typename T>
 __global__ __launch_bounds__(256) void sum_runs(GradArgs a, const S* dy, T* grad) {
     if (blockIdx.x >= a.sum_blocks) {
         __shared__ uint32_t named[kZeroRows];
         const uint32_t row0 = (blockIdx.x - a.sum_blocks) * kZeroRows;
-        if (threadIdx.x < kZeroRows) {
-            const uint64_t key = (uint64_t)(row0 + threadIdx.x) << 32;
-            uint32_t lo = 0, hi = a.n;
-            while (lo < hi) {
-                const uint32_t mid = (lo + hi) / 2;
-                if (a.keys[mid] < key)
-                    lo = mid + 1;
-                else
-                    hi = mid;
-            }
-            named[threadIdx.x] = lo < a.n && token_of(a.keys[lo]) == row0 + threadIdx.x;
+        const uint32_t probe = threadIdx.x % 16, token = row0 + threadIdx.x / 16;
+        const uint64_t key = (uint64_t)token << 32;
+        uint32_t lo = 0, hi = a.n;  // the first key of the token or a later one is in [lo, hi]
+        while (__any(lo < hi)) {
+            const uint32_t step = (hi - lo) / 17 + 1;
+            const uint64_t at = lo + (uint64_t)(probe + 1) * step - 1;
+            const uint64_t less = __ballot(at < hi && a.keys[at] < key);
+            const uint32_t count = __popc((uint32_t)(less >> (threadIdx.x & 48)) & 0xffff);
+            hi = (uint32_t)min((uint64_t)hi, lo + (uint64_t)(count + 1) * step - 1);
+            lo += count * step;
         }
+        if (probe == 0) named[threadIdx.x / 16] = lo < a.n && token_of(a.keys[lo]) == token;
         __syncthreads();
         const uint32_t lane = threadIdx.x & (a.clear_lanes - 1), shift = __builtin_ctz(a.clear_lanes);
         for (uint32_t r = threadIdx.x >> shift; r < kZeroRows && row0 + r < a.vocab; r += 256u >> shift) {
