@@ -12,13 +12,15 @@ namespace {
 
 constexpr uint32_t kStep = kWideStep;
 
-template <int BM, int BN, int WM, int WN, typename T>
+// X: what dy is multiplied in.
+template <int BM, int BN, int WM, int WN, typename X, typename T>
 __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* out) {
     constexpr int kThreads = WM * WN * 64, kWaves = WM * WN, FM = BM / WM / 32, FN = BN / WN / 32;
     constexpr int kLoads = BM / 8 / kWaves;               // loads of x a wave issues a stage
     constexpr int kWords = BN * kStep / 8 / kThreads;     // of W, eight codes each, that a lane expands a stage
     constexpr int kPitch = BN * 2 + 32;                   // bytes of a row of W's tile in LDS
     constexpr int kXBytes = BM * kStep * 2, kWBytes = kStep * kPitch;
+    constexpr bool kHalf = __is_same(X, _Float16);
     // The stages are variables of their own: the compiler then sees that loads
     // into one do not touch what is read from another.
     __shared__ __align__(16) uint8_t x0[kXBytes], x1[kXBytes];
@@ -44,7 +46,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
     // a lane takes the same columns of each of its rows
     static_assert(kWaves % 2 == 0, "");
     const uint32_t x_col = (lane % 8 ^ (wave % 2 * 4 + lane / 16)) * 8;
-    const __bf16* x_at[kLoads];
+    const uint16_t* x_at[kLoads];
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) x_at[q] = a.x + min(m0 + (q * kWaves + wave) * 8 + lane / 8, a.m - 1) * a.x_stride + x_col;
     auto load_x = [&](uint32_t t, uint8_t* to) SLLM_INLINE {
@@ -77,17 +79,24 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
 #pragma unroll
     for (uint32_t w = 0; w < kWords; ++w)
         w_to[w] = opaque(w_row * kPitch + w_block * 64 + ((w_part * kWords + w) ^ (w_block & 3)) * 16);
-    auto store_w = [&](uint32_t t, int from, uint8_t* to) SLLM_INLINE {
+    uint32_t beyond = 0;  // scales that float16 does not hold
+    auto store_w = [&](uint32_t t, int from, uint8_t* to, auto type) SLLM_INLINE {
+        typedef decltype(type) W;
         const bool inside = (uint64_t)(t % a.steps) * kStep + w_row < a.w_rows;
-        const float scale = mx_scale(inside ? scales[from] : 0);
+        float scale = mx_scale(inside ? scales[from] : 0);
+        if constexpr (__is_same(W, _Float16)) {
+            scale *= 1 << kHalfShift;
 #pragma unroll
-        for (uint32_t w = 0; w < kWords; ++w) lds_write(to, w_to[w], expand8(codes[from][w], scale));
+            for (uint32_t w = 0; w < kWords; ++w) beyond |= (uint32_t)inside & beyond_half(scales[from], codes[from][w]);
+        }
+#pragma unroll
+        for (uint32_t w = 0; w < kWords; ++w) lds_write(to, w_to[w], expand8<W>(codes[from][w], scale));
     };
 
     // (Filled through a reference: a returned structure makes its reads' alias
     // information useless, and they wait for every load under way.)
     struct Fragments {
-        bf16x8 x[FM], w[FN];
+        u32x4 x[FM], w[FN];
     };
     // Step s of a stage is, in lane (r, h), eight of the depth from 32 h + 8 s.
     // Of W four rows of the tile and 16 columns are read by 16 lanes, transposed:
@@ -107,17 +116,24 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
             const lds_u8* const p = (const lds_u8*)w_now + w_from[n] + 8 * s * kPitch;
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * kPitch));
-            f.w[n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            f.w[n] = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
 #pragma unroll
-        for (int m = 0; m < FM; ++m) f.x[m] = lds_read<bf16x8>(x_now, (x_from ^ s * 16) + m * 4096);
+        for (int m = 0; m < FM; ++m) f.x[m] = lds_read<u32x4>(x_now, (x_from ^ s * 16) + m * 4096);
     };
+    uint32_t met[FM] = {};  // the bits of x's rows
     auto multiply = [&](const Fragments& f) SLLM_INLINE {
+        if constexpr (kHalf)
+#pragma unroll
+            for (int m = 0; m < FM; ++m) {
+                met[m] |= f.x[m][0] | f.x[m][1] | f.x[m][2] | f.x[m][3];
+                asm volatile("" : "+v"(met[m]));  // now, not when all of the depth has been read
+            }
         pin(acc);
 #pragma unroll
         for (int m = 0; m < FM; ++m)
 #pragma unroll
-            for (int n = 0; n < FN; ++n) acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.w[n], f.x[m], acc[n][m], 0, 0, 0);
+            for (int n = 0; n < FN; ++n) acc[n][m] = product<X>(f.w[n], f.x[m], acc[n][m]);
         pin(acc);
     };
     // While one step is multiplied the next is read; the next stage's first step
@@ -132,7 +148,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
         read(f0, here, w_ring[i], 2);
         multiply(f1);
         read(f1, here, w_ring[i], 3);
-        store_w(t + 1, i ^ 1, w_ring[i ^ 1]);
+        store_w(t + 1, i ^ 1, w_ring[i ^ 1], X());
         multiply(f0);
         wait_but_loads<0>();
         barrier();
@@ -145,7 +161,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
         load_w(t0, 0);
         load_w(t0 + 1, 1);
         load_x(t0, x0);
-        store_w(t0, 0, w0);
+        store_w(t0, 0, w0, X());
         wait_but_loads<0>();
         barrier();
         load_w(t0 + 2, 0);
@@ -158,26 +174,67 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
     }
 
     __syncthreads();  // the last stage's reads are done
+    if constexpr (kHalf) {
+#pragma unroll
+        for (int m = 0; m < FM; ++m) beyond |= all_subnormal(met[m]);
+        if (__syncthreads_or(beyond)) {
+#pragma unroll
+            for (int n = 0; n < FN; ++n)
+#pragma unroll
+                for (int m = 0; m < FM; ++m) acc[n][m] = f32x16{};
+            for (uint32_t t = t0; t < t1; ++t) {
+                load_x(t, x0);
+                load_w(t, 0);
+                store_w(t, 0, w0, __bf16());
+                wait_but_loads<0>();
+                barrier();
+#pragma unroll
+                for (uint32_t s = 0; s < 4; ++s) {
+                    read(f0, x0, w0, s);
+#pragma unroll
+                    for (int m = 0; m < FM; ++m) {
+                        u32x4 hi, lo;
+                        split_half(f0.x[m], hi, lo);
+#pragma unroll
+                        for (int n = 0; n < FN; ++n)
+                            acc[n][m] = product<__bf16>(f0.w[n], lo, product<__bf16>(f0.w[n], hi, acc[n][m]));
+                        pin(acc);
+                    }
+                }
+                __syncthreads();
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < FN; ++n)
+#pragma unroll
+                for (int m = 0; m < FM; ++m) acc[n][m] *= 1.0f / (1 << kHalfShift);
+        }
+    }
     // the output goes through x's first two buffers
     static_assert(2 * kXBytes >= kWaves * kTurnBytes && kXBytes % kTurnBytes == 0, "");
     uint8_t* const turn = (wave * kTurnBytes < kXBytes ? x0 : x1) + wave * kTurnBytes % kXBytes;
     store_tile<FM, FN>(acc, a.out_args, m0 + wm * FM * 32, j0 + wn * FN * 32, out, turn);
 }
 
-}  // namespace
-
-int32_t launch_grad(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype,
-                    hipStream_t stream) {
+template <typename X>
+int32_t launch(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream) {
     const dim3 grid(a.tiles_m * a.tiles_j, splits);
     SLLM_BY_DTYPE(out_dtype, T, {
         T* to = static_cast<T*>(out);
         if (tile == kLargeTile)
-            grad_product<kLargeTile, kLargeTile, 2, 4, T><<<grid, 512, 0, stream>>>(a, to);
+            grad_product<kLargeTile, kLargeTile, 2, 4, X, T><<<grid, 512, 0, stream>>>(a, to);
         else
-            grad_product<kSmallTile, kSmallTile, 2, 2, T><<<grid, 256, 0, stream>>>(a, to);
+            grad_product<kSmallTile, kSmallTile, 2, 2, X, T><<<grid, 256, 0, stream>>>(a, to);
     });
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
+}
+
+}  // namespace
+
+int32_t launch_grad(const WideArgs& a, bool half, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype,
+                    hipStream_t stream) {
+    return (half ? launch<_Float16> : launch<__bf16>)(a, tile, splits, out, out_dtype, stream);
 }
 
 }  // namespace sllm

@@ -12,11 +12,13 @@ namespace {
 
 constexpr uint32_t kStep = kWideStep;
 
-template <int BM, int BN, int WM, int WN, typename T>
+// X: what x is multiplied in.
+template <int BM, int BN, int WM, int WN, typename X, typename T>
 __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* out) {
     constexpr int kWaves = WM * WN, FM = BM / WM / 32, FN = BN / WN / 32;
     constexpr int kXLoads = BM / 8 / kWaves, kWLoads = BN / 16 / kWaves;
     constexpr int kXBytes = BM * kStep * 2, kWBytes = BN * 64, kScaleBytes = BN * 4;
+    constexpr bool kHalf = __is_same(X, _Float16);
     constexpr int kScaleRows = BN / kWaves;  // whose scales a wave loads
     static_assert(kScaleRows <= 64, "");
     // The stages are variables of their own: the compiler then sees that loads
@@ -46,7 +48,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
     // a lane takes the same columns of each of its rows
     static_assert(kWaves % 2 == 0, "");
     const uint32_t x_col = (lane % 8 ^ (wave % 2 * 4 + lane / 16)) * 8;
-    const __bf16* x_at[kXLoads];
+    const uint16_t* x_at[kXLoads];
 #pragma unroll
     for (int q = 0; q < kXLoads; ++q) x_at[q] = a.x + min(m0 + (q * kWaves + wave) * 8 + lane / 8, a.m - 1) * a.x_stride + x_col;
     auto load_x = [&](uint32_t t, uint8_t* to) SLLM_INLINE {
@@ -82,34 +84,47 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
         float scale[FN];
     };
     const uint32_t w_from = opaque(wn * FN * 2048 + short_chunk_at(r, h)), scale_from = opaque(kWBytes + wn * FN * 128 + r * 4 + h);
-    auto read_w = [&](Weight& w, uint32_t t, const uint8_t* from, uint32_t odd) SLLM_INLINE {
+    uint32_t beyond = 0;  // scales that float16 does not hold
+    auto read_w = [&](Weight& w, uint32_t t, const uint8_t* from, uint32_t odd, auto type) SLLM_INLINE {
         const bool inside = (uint64_t)(t % a.steps) * 2 + h < a.w_blocks;  // scale bytes past the row's end may hold anything
 #pragma unroll
         for (int n = 0; n < FN; ++n) {
             w.codes[n] = lds_read<u32x4>(from, (w_from ^ odd * 32) + n * 2048);
             const uint8_t s = lds_read<uint8_t>(from, scale_from + n * 128 + odd * 2);
             w.scale[n] = mx_scale(inside ? s : 0);
+            if constexpr (__is_same(decltype(type), _Float16)) {
+                const u32x4 c = w.codes[n];
+                w.scale[n] *= 1 << kHalfShift;
+                beyond |= (uint32_t)(inside && t < t1) & beyond_half(s, c[0] | c[1] | c[2] | c[3]);
+            }
         }
     };
 
     struct Fragments {
-        bf16x8 x[FM], w[FN];
+        u32x4 x[FM], w[FN];
     };
     // Step s of a stage is, in lane (r, h), eight of the depth from 32 h + 8 s.
     const uint32_t x_from = opaque(wm * FM * 4096 + chunk_at(r, 4 * h));
     auto read = [&](Fragments& f, const uint8_t* from, const Weight& w, auto which) SLLM_INLINE {
         constexpr int s = decltype(which)::value;
 #pragma unroll
-        for (int m = 0; m < FM; ++m) f.x[m] = lds_read<bf16x8>(from, (x_from ^ s * 16) + m * 4096);
+        for (int m = 0; m < FM; ++m) f.x[m] = lds_read<u32x4>(from, (x_from ^ s * 16) + m * 4096);
 #pragma unroll
-        for (int n = 0; n < FN; ++n) f.w[n] = __builtin_bit_cast(bf16x8, expand8(w.codes[n][s], w.scale[n]));
+        for (int n = 0; n < FN; ++n) f.w[n] = expand8<X>(w.codes[n][s], w.scale[n]);
     };
+    uint32_t met[FM] = {};  // the bits of x's rows
     auto multiply = [&](const Fragments& f) SLLM_INLINE {
+        if constexpr (kHalf)
+#pragma unroll
+            for (int m = 0; m < FM; ++m) {
+                met[m] |= f.x[m][0] | f.x[m][1] | f.x[m][2] | f.x[m][3];
+                asm volatile("" : "+v"(met[m]));  // now, not when all of the depth has been read
+            }
         pin(acc);
 #pragma unroll
         for (int m = 0; m < FM; ++m)
 #pragma unroll
-            for (int n = 0; n < FN; ++n) acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.w[n], f.x[m], acc[n][m], 0, 0, 0);
+            for (int n = 0; n < FN; ++n) acc[n][m] = product<X>(f.w[n], f.x[m], acc[n][m]);
         pin(acc);
     };
     // While one step is multiplied the next is read; the next stage's first step
@@ -132,7 +147,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
         multiply(f0);
         wait_but_loads<0>();
         barrier();
-        read_w(now, t + 1, w_ring[(i + 1) / 2 % 2], (i + 1) % 2);
+        read_w(now, t + 1, w_ring[(i + 1) / 2 % 2], (i + 1) % 2, X());
         if (t + 2 < t1) load_x(t + 2, here);
         if (i % 2 && t + 3 < t1) load_w(t + 3, w_ring[i / 2]);
         read(f0, x_ring[(i + 1) % 2], now, S0());
@@ -145,7 +160,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
         barrier();
         load_x(t0 + 1, x1);
         if (t0 + 2 < t1) load_w(t0 + 2, w1);
-        read_w(now, t0, w0, 0);
+        read_w(now, t0, w0, 0, X());
         read(f0, x0, now, S0());
         for (uint32_t t = t0; t < t1; t += 4) {
             stage(t, S0());
@@ -158,26 +173,67 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
     }
 
     __syncthreads();  // the last stage's reads are done
+    if constexpr (kHalf) {
+#pragma unroll
+        for (int m = 0; m < FM; ++m) beyond |= all_subnormal(met[m]);
+        if (__syncthreads_or(beyond)) {
+#pragma unroll
+            for (int n = 0; n < FN; ++n)
+#pragma unroll
+                for (int m = 0; m < FM; ++m) acc[n][m] = f32x16{};
+            for (uint32_t t = t0; t < t1; ++t) {
+                if (t % 2 == 0) load_w(t, w0);
+                load_x(t, x0);
+                wait_but_loads<0>();
+                barrier();
+                read_w(now, t, w0, t % 2, __bf16());
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int m = 0; m < FM; ++m) {
+                        u32x4 hi, lo;
+                        split_half(lds_read<u32x4>(x0, (x_from ^ s * 16) + m * 4096), hi, lo);
+#pragma unroll
+                        for (int n = 0; n < FN; ++n) {
+                            const u32x4 w = expand8(now.codes[n][s], now.scale[n]);
+                            acc[n][m] = product<__bf16>(w, lo, product<__bf16>(w, hi, acc[n][m]));
+                        }
+                        pin(acc);
+                    }
+                __syncthreads();
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < FN; ++n)
+#pragma unroll
+                for (int m = 0; m < FM; ++m) acc[n][m] *= 1.0f / (1 << kHalfShift);
+        }
+    }
     // the output goes through x's first two buffers
     static_assert(2 * kXBytes >= kWaves * kTurnBytes && kXBytes % kTurnBytes == 0, "");
     uint8_t* const turn = (wave * kTurnBytes < kXBytes ? x0 : x1) + wave * kTurnBytes % kXBytes;
     store_tile<FM, FN>(acc, a.out_args, m0 + wm * FM * 32, j0 + wn * FN * 32, out, turn);
 }
 
-}  // namespace
-
-int32_t launch_wide(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype,
-                    hipStream_t stream) {
+template <typename X>
+int32_t launch(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream) {
     const dim3 grid(a.tiles_m * a.tiles_j, splits);
     SLLM_BY_DTYPE(out_dtype, T, {
         T* to = static_cast<T*>(out);
         if (tile == kLargeTile)
-            wide_product<kLargeTile, kLargeTile, 2, 4, T><<<grid, 512, 0, stream>>>(a, to);
+            wide_product<kLargeTile, kLargeTile, 2, 4, X, T><<<grid, 512, 0, stream>>>(a, to);
         else
-            wide_product<kSmallTile, kSmallTile, 2, 2, T><<<grid, 256, 0, stream>>>(a, to);
+            wide_product<kSmallTile, kSmallTile, 2, 2, X, T><<<grid, 256, 0, stream>>>(a, to);
     });
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
+}
+
+}  // namespace
+
+int32_t launch_wide(const WideArgs& a, bool half, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype,
+                    hipStream_t stream) {
+    return (half ? launch<_Float16> : launch<__bf16>)(a, tile, splits, out, out_dtype, stream);
 }
 
 }  // namespace sllm

@@ -123,7 +123,7 @@ Plan plan_linear(const LinearLaunch& a) {
     p.cols = a.grad ? a.k : a.n;
     p.skinny = !a.grad && a.m <= (a.x.codes || a.x.dtype == SLLM_DTYPE_BF16 ? 32 : 16);
     if (!p.depth || !a.m || !p.cols || p.skinny) return p;
-    if (!a.x.codes) p.parts = a.x.dtype == SLLM_DTYPE_BF16 ? 1 : a.x.dtype == SLLM_DTYPE_F16 ? 2 : 3;
+    if (!a.x.codes) p.parts = a.x.dtype == SLLM_DTYPE_F32 ? 3 : 1;
     // The kernel reads x in aligned vectors of eight.
     p.staged = !a.x.codes && (p.parts > 1 || p.depth % 8 || (a.m > 1 && a.x.stride % 8) ||
                               reinterpret_cast<uintptr_t>(a.x.data) % 16);
@@ -152,17 +152,22 @@ Plan plan_linear(const LinearLaunch& a) {
 }
 
 // x as the sum of `Parts` bfloat16 matrices: its leading eight bits, the eight
-// after those, the rest.
+// after those, the rest.  Of one part it is a copy, of any 16 bits.
 template <typename T, int Parts>
 __global__ __launch_bounds__(256) void split_x(const T* x, uint64_t stride, uint64_t rows, uint64_t cols, uint64_t pitch,
-                                               __bf16* out) {
+                                               uint16_t* out) {
     const uint64_t vectors = pitch / 8, i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
     const uint64_t row = i / vectors, c = i % vectors * 8;
     if (row >= rows) return;
     uint16_t v[Parts][8];
     for (uint32_t e = 0; e < 8; ++e) {
-        float f = c + e < cols ? to_f32(x[row * stride + c + e]) : 0.0f;
-        for (int p = 0; p < Parts; ++p) v[p][e] = leading_bf16(f);
+        const T at = c + e < cols ? x[row * stride + c + e] : T(0);
+        if constexpr (Parts == 1) {
+            v[0][e] = at;
+        } else {
+            float f = at;
+            for (int p = 0; p < Parts; ++p) v[p][e] = leading_bf16(f);
+        }
     }
     for (int p = 0; p < Parts; ++p) {
         u32x4 o;
@@ -201,19 +206,17 @@ int32_t join(const Plan& p, const float* sums, uint32_t splits, const LinearLaun
 
 // x as the wide kernel reads it, written out in the workspace where it is not so already.
 int32_t stage_x(const LinearLaunch& a, const Plan& p, void* workspace, WideArgs* w, hipStream_t stream) {
-    w->x = static_cast<const __bf16*>(a.x.data);
+    w->x = static_cast<const uint16_t*>(a.x.data);
     w->x_stride = a.x.stride, w->part_stride = 0;
     if (!p.staged) return SLLM_OK;
-    __bf16* x = static_cast<__bf16*>(workspace);
+    uint16_t* x = static_cast<uint16_t*>(workspace);
     w->x = x;
     w->x_stride = p.parts * p.part_stride;
     w->part_stride = p.part_stride;
     uint32_t blocks;
     SLLM_TRY(grid_of(a.m * p.part_stride / 8, &blocks));
     if (p.parts == 1)
-        split_x<__bf16, 1><<<blocks, 256, 0, stream>>>(static_cast<const __bf16*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
-    else if (p.parts == 2)
-        split_x<_Float16, 2><<<blocks, 256, 0, stream>>>(static_cast<const _Float16*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
+        split_x<uint16_t, 1><<<blocks, 256, 0, stream>>>(static_cast<const uint16_t*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
     else
         split_x<float, 3><<<blocks, 256, 0, stream>>>(static_cast<const float*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
     SLLM_HIP(hipGetLastError());
@@ -245,7 +248,8 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
         w.w_rows = a.n, w.w_blocks = mx_blocks(a.k), w.w_scale_pitch = mx_scale_pitch(a.k);
         w.tiles_m = p.tiles_m, w.tiles_j = p.tiles_j;
         w.out_args = o;
-        SLLM_TRY(a.grad ? launch_grad(w, p.tile, p.splits, out, dtype, stream) : launch_wide(w, p.tile, p.splits, out, dtype, stream));
+        const bool half = a.x.dtype == SLLM_DTYPE_F16;
+        SLLM_TRY((a.grad ? launch_grad : launch_wide)(w, half, p.tile, p.splits, out, dtype, stream));
     }
     return p.splits > 1 ? join(p, static_cast<const float*>(out), p.splits, a, stream) : SLLM_OK;
 }

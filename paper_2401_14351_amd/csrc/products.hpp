@@ -15,9 +15,9 @@ struct OutArgs {
     uint32_t vector;        // rows start on 16 bytes
 };
 
-// x (m x depth, parts of it one after another along a row) in bfloat16
+// x (m x depth) in float16, or (parts of it one after another along a row) in bfloat16
 struct WideArgs {
-    const __bf16* x;
+    const uint16_t* x;
     uint64_t m, depth;       // of a part
     uint64_t x_stride, part_stride;
     uint32_t parts, steps;   // steps of a part, an even number
@@ -125,22 +125,6 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // four registers 4-bit elements do not use.
 __device__ __forceinline__ i32x8 fragment(u32x4 v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
 
-// Eight codes as bfloat16.
-__device__ __forceinline__ u32x4 expand8(uint32_t codes, float scale) {
-    u32x4 v;
-    v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
-    v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
-    v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
-    v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
-    return v;
-}
-
-// A block of 32 codes: four vectors of eight.
-__device__ __forceinline__ void expand(u32x4 codes, uint32_t scale, u32x4 (&out)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = expand8(codes[i], mx_scale(scale));
-}
-
 // The leading eight bits of f as a bfloat16, and f less those: two or three of
 // these in turn are all of a float16 or a float.  An infinity or a NaN is whole
 // in the first and leaves zero.
@@ -150,6 +134,75 @@ __device__ __forceinline__ uint32_t leading_bf16(float& f) {
     f = finite ? f - __uint_as_float(bits & 0xffff0000) : 0.0f;
     // a NaN whose payload is all in the lower half must not become an infinity
     return finite || !(bits & 0x7fffff) ? bits >> 16 : 0x7fc0;
+}
+
+// Eight codes as bfloat16 or float16.
+template <typename X = __bf16>
+__device__ __forceinline__ u32x4 expand8(uint32_t codes, float scale) {
+    u32x4 v;
+    if constexpr (__is_same(X, __bf16)) {
+        v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+        v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+        v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+        v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+    } else {
+        v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0));
+        v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1));
+        v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2));
+        v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3));
+    }
+    return v;
+}
+
+// 16 of the depth by 32 columns and 32 rows.
+template <typename X>
+__device__ __forceinline__ f32x16 product(u32x4 w, u32x4 x, f32x16 acc) {
+    if constexpr (__is_same(X, __bf16))
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), acc, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, w), __builtin_bit_cast(f16x8, x), acc, 0, 0, 0);
+}
+
+// An x in float16 is multiplied as it is, by W in float16 too, times 2^kHalfShift:
+// exact for scales of 2^-31 to 2^5, so for values from 2^-32 to 192.  The matrix
+// instruction adds products of a subnormal (below 2^-14) as if they were of 2^-14:
+// it drops their bits under 2^-24 of that.  A workgroup that has met another scale,
+// other than over zeros, or a row of x with nothing but subnormals starts again
+// with W and two parts of x in bfloat16, which hold all of them.  4096 x 8192 by
+// 8192 takes 519 us, as two parts throughout 935, where every workgroup starts
+// again 2000.
+constexpr int kHalfShift = 8;
+constexpr uint32_t kHalfScale = 127 - 31, kHalfScales = 37;
+
+__device__ __forceinline__ uint32_t beyond_half(uint32_t scale, uint32_t codes) {
+    return (uint32_t)(scale - kHalfScale >= kHalfScales) & ((uint32_t)(scale == 255) | (uint32_t)((codes & 0x77777777) != 0));
+}
+
+// From the bits that any element of a row has, of the halves that lanes l and l + 32 have met.
+__device__ __forceinline__ uint32_t all_subnormal(uint32_t bits) {
+    bits |= __shfl_xor(bits, 32);
+    return (uint32_t)((bits & 0x7c007c00) == 0) & (uint32_t)((bits & 0x03ff03ff) != 0);
+}
+
+// A vector of float16 as the sum of two in bfloat16: the leading eight bits of
+// each element and the rest.  An infinity or a NaN is whole in the first.
+__device__ __forceinline__ void split_half(u32x4 v, u32x4& hi, u32x4& lo) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t first[2], rest[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t half = v[i] >> 16 * e & 0xffff, size = half & 0x7fff;
+            const float f = (float)__builtin_bit_cast(_Float16, (uint16_t)half);
+            const uint32_t bits = __float_as_uint(f);
+            const float left = f - __uint_as_float(bits & 0xffff0000);
+            // a NaN whose payload is all in the lower half must not become an infinity
+            first[e] = bits >> 16 | (size > 0x7c00 ? 0x40u : 0u);
+            rest[e] = size >= 0x7c00 ? 0u : __float_as_uint(left) >> 16;
+        }
+        hi[i] = first[0] | first[1] << 16;
+        lo[i] = rest[0] | rest[1] << 16;
+    }
 }
 
 // Keeps products between the reads before and after them.  Matrix instructions
@@ -255,8 +308,9 @@ struct SkinnyArgs {
 };
 int32_t launch_skinny(const SkinnyArgs& a, hipStream_t stream);
 
-int32_t launch_wide(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
-int32_t launch_grad(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
+// half: x is in float16
+int32_t launch_wide(const WideArgs& a, bool half, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
+int32_t launch_grad(const WideArgs& a, bool half, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
 constexpr uint32_t kLargeTile = 256, kSmallTile = 128;  // rows of x and columns of the output a workgroup holds
 constexpr uint32_t kWideStep = 64;   // depth of a stage
 

@@ -301,6 +301,39 @@ def test_linear_extreme_scales(m):
     assert_close(got, O.linear(a, smallv), sum_bound(a, smallv.T, 128) + 128 * 2.0 ** -149, torch.float32)
 
 
+@pytest.mark.parametrize("m,n,k", [(70, 200, 320), (129, 130, 1100), (3300, 3600, 96), (3300, 96, 3600)])
+@pytest.mark.parametrize("scale", [0, 30, 95, 96, 132, 133, 180])
+def test_linear_half_any_scale(m, n, k, scale):
+    """x in float16 against blocks whose values float16 holds, scaled or not, and one that it may not."""
+    w, wv = random_mx4(n, k, 15, (96, 133))
+    x, dy = normal((m, k), torch.float16, 16), normal((m, n), torch.float16, 17)
+    x[0, :] = 2.0 ** -24  # the smallest
+    x[m - 1, ::2] = 2.0 ** -15
+    dy[0, :] = -2.0 ** -24
+    for row, block in ((n - 1, (k - 1) // 32), (n // 2, 1)):
+        w.scales[row, block] = scale
+        wv = O.dequantize(w.codes.cpu().numpy(), w.scales.cpu().numpy(), k)
+        a, b = host(x), host(dy)
+        assert_close(op.mx4_linear(x, w, out_dtype=torch.float32), O.linear(a, wv), sum_bound(a, wv.T, k), torch.float32)
+        assert_close(op.mx4_linear_grad(dy, w, out_dtype=torch.float32), O.linear_grad(b, wv), sum_bound(b, wv, n), torch.float32)
+    w.scales[n - 1, 0] = 255
+    y = op.mx4_linear(x, w, out_dtype=torch.float32)
+    assert y[:, n - 1].isnan().all() and y[:, :n - 1].isfinite().all()
+    dx = op.mx4_linear_grad(dy, w, out_dtype=torch.float32)
+    assert dx[:, :32].isnan().all() and dx[:, 32:].isfinite().all()
+
+
+def test_linear_half_small_values():
+    """A weight far below float16's range against large x: no value is lost."""
+    m, n, k = 150, 140, 256
+    w, wv = random_mx4(n, k, 18, (1, 60))
+    x = normal((m, k), torch.float16, 19, 1000.0)
+    dy = normal((m, n), torch.float16, 20, 1000.0)
+    a, b = host(x), host(dy)
+    assert_close(op.mx4_linear(x, w, out_dtype=torch.float32), O.linear(a, wv), sum_bound(a, wv.T, k), torch.float32)
+    assert_close(op.mx4_linear_grad(dy, w, out_dtype=torch.float32), O.linear_grad(b, wv), sum_bound(b, wv, n), torch.float32)
+
+
 def test_linear_same_bytes_again():
     for m in (1, 30, 200):
         x = normal((m, 4096), torch.bfloat16, 1)
