@@ -32,6 +32,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
     const void* const zeros = zero_vector();
     const Tile tile = tile_of(blockIdx.x, a.tiles_m, a.tiles_j);
     const uint64_t m0 = (uint64_t)tile.m * BM, j0 = (uint64_t)tile.j * BN;
+    // the parts of x take a piece of W in turn: it comes from memory once, then from L2
     const uint32_t steps = a.steps * a.parts;
     const uint32_t t0 = (uint64_t)steps * blockIdx.y / gridDim.y, t1 = (uint64_t)steps * (blockIdx.y + 1) / gridDim.y;
     const uint32_t wm = wave % WM, wn = wave / WM;
@@ -50,8 +51,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) x_at[q] = a.x + min(m0 + (q * kWaves + wave) * 8 + lane / 8, a.m - 1) * a.x_stride + x_col;
     auto load_x = [&](uint32_t t, uint8_t* to) SLLM_INLINE {
-        const uint32_t part = t / a.steps;
-        const uint64_t d = (uint64_t)(t - part * a.steps) * kStep, at = part * a.part_stride + d;
+        const uint64_t d = (uint64_t)(t / a.parts) * kStep, at = t % a.parts * a.part_stride + d;
         const bool inside = d + x_col < a.depth;
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
     const uint32_t w_row = tid / kRowLanes, w_block = tid % kRowLanes / kParts, w_part = tid % kParts;
     const uint64_t w_at = min(j0 / 32 + w_block, a.w_blocks - 1);
     auto load_w = [&](uint32_t t, int to) SLLM_INLINE {
-        const uint64_t row = min((uint64_t)(min(t, t1 - 1) % a.steps) * kStep + w_row, a.w_rows - 1);
+        const uint64_t row = min((uint64_t)(min(t, t1 - 1) / a.parts) * kStep + w_row, a.w_rows - 1);
         codes[to] = reinterpret_cast<const words*>(a.w_codes + row * a.w_blocks + w_at)[w_part];
         scales[to] = a.w_scales[row * a.w_scale_pitch + w_at];
     };
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
     uint32_t beyond = 0;  // scales that float16 does not hold
     auto store_w = [&](uint32_t t, int from, uint8_t* to, auto type) SLLM_INLINE {
         typedef decltype(type) W;
-        const bool inside = (uint64_t)(t % a.steps) * kStep + w_row < a.w_rows;
+        const bool inside = (uint64_t)(t / a.parts) * kStep + w_row < a.w_rows;
         float scale = mx_scale(inside ? scales[from] : 0);
         if constexpr (__is_same(W, _Float16)) {
             scale *= 1 << kHalfShift;
@@ -210,21 +210,27 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
                 for (int m = 0; m < FM; ++m) acc[n][m] *= 1.0f / (1 << kHalfShift);
         }
     }
-    // the output goes through x's first two buffers
-    static_assert(2 * kXBytes >= kWaves * kTurnBytes && kXBytes % kTurnBytes == 0, "");
-    uint8_t* const turn = (wave * kTurnBytes < kXBytes ? x0 : x1) + wave * kTurnBytes % kXBytes;
+    // the output goes through the stages' buffers, a part of one for each wave
+    constexpr int kTurns = kXBytes / kTurnBytes;
+    static_assert(kXBytes % kTurnBytes == 0 && kWBytes >= kTurnBytes && 2 * kTurns + 2 >= kWaves, "");
+    const int turn_at = (int)wave % kTurns * kTurnBytes, turn_of = (int)wave / kTurns;
+    uint8_t* const turn = (turn_of == 0 ? x0 : turn_of == 1 ? x1 : wave == 2 * kTurns ? w0 : w1) + (turn_of < 2 ? turn_at : 0);
     store_tile<FM, FN>(acc, a.out_args, m0 + wm * FM * 32, j0 + wn * FN * 32, out, turn);
 }
 
 template <typename X>
-int32_t launch(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream) {
+int32_t launch(const WideArgs& a, uint32_t tile_m, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream) {
     const dim3 grid(a.tiles_m * a.tiles_j, splits);
     SLLM_BY_DTYPE(out_dtype, T, {
         T* to = static_cast<T*>(out);
-        if (tile == kLargeTile)
+        if (tile_m == kLargeTile)
             grad_product<kLargeTile, kLargeTile, 2, 4, X, T><<<grid, 512, 0, stream>>>(a, to);
-        else
+        else if (tile_m == kSmallTile)
             grad_product<kSmallTile, kSmallTile, 2, 2, X, T><<<grid, 256, 0, stream>>>(a, to);
+        else if (tile_m == 64)
+            grad_product<64, kSmallTile, 2, 2, X, T><<<grid, 256, 0, stream>>>(a, to);
+        else
+            grad_product<32, kSmallTile, 1, 4, X, T><<<grid, 256, 0, stream>>>(a, to);
     });
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
@@ -232,9 +238,9 @@ int32_t launch(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uin
 
 }  // namespace
 
-int32_t launch_grad(const WideArgs& a, bool half, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype,
+int32_t launch_grad(const WideArgs& a, bool half, uint32_t tile_m, uint32_t splits, void* out, uint32_t out_dtype,
                     hipStream_t stream) {
-    return (half ? launch<_Float16> : launch<__bf16>)(a, tile, splits, out, out_dtype, stream);
+    return (half ? launch<_Float16> : launch<__bf16>)(a, tile_m, splits, out, out_dtype, stream);
 }
 
 }  // namespace sllm

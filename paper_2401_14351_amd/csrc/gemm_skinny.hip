@@ -321,8 +321,6 @@ int32_t launch_skinny(const SkinnyArgs& a, hipStream_t stream) {
         launch<void, 16, 1>(a, stream);
     else if (a.x_scales)
         launch<void, 16, 2>(a, stream);
-    else if (a.m > 16)
-        launch<__bf16, 16, 2>(a, stream);
     else
         SLLM_BY_DTYPE(a.x_dtype, X, {
             if (a.m == 1)

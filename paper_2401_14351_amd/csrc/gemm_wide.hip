@@ -209,21 +209,27 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
                 for (int m = 0; m < FM; ++m) acc[n][m] *= 1.0f / (1 << kHalfShift);
         }
     }
-    // the output goes through x's first two buffers
-    static_assert(2 * kXBytes >= kWaves * kTurnBytes && kXBytes % kTurnBytes == 0, "");
-    uint8_t* const turn = (wave * kTurnBytes < kXBytes ? x0 : x1) + wave * kTurnBytes % kXBytes;
+    // the output goes through the stages' buffers, a part of one for each wave
+    constexpr int kTurns = kXBytes / kTurnBytes;
+    static_assert(kXBytes % kTurnBytes == 0 && kWBytes >= kTurnBytes && 2 * kTurns + 2 >= kWaves, "");
+    const int turn_at = (int)wave % kTurns * kTurnBytes, turn_of = (int)wave / kTurns;
+    uint8_t* const turn = (turn_of == 0 ? x0 : turn_of == 1 ? x1 : wave == 2 * kTurns ? w0 : w1) + (turn_of < 2 ? turn_at : 0);
     store_tile<FM, FN>(acc, a.out_args, m0 + wm * FM * 32, j0 + wn * FN * 32, out, turn);
 }
 
 template <typename X>
-int32_t launch(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream) {
+int32_t launch(const WideArgs& a, uint32_t tile_m, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream) {
     const dim3 grid(a.tiles_m * a.tiles_j, splits);
     SLLM_BY_DTYPE(out_dtype, T, {
         T* to = static_cast<T*>(out);
-        if (tile == kLargeTile)
+        if (tile_m == kLargeTile)
             wide_product<kLargeTile, kLargeTile, 2, 4, X, T><<<grid, 512, 0, stream>>>(a, to);
-        else
+        else if (tile_m == kSmallTile)
             wide_product<kSmallTile, kSmallTile, 2, 2, X, T><<<grid, 256, 0, stream>>>(a, to);
+        else if (tile_m == 64)
+            wide_product<64, kSmallTile, 2, 2, X, T><<<grid, 256, 0, stream>>>(a, to);
+        else
+            wide_product<32, kSmallTile, 1, 4, X, T><<<grid, 256, 0, stream>>>(a, to);
     });
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
@@ -231,9 +237,9 @@ int32_t launch(const WideArgs& a, uint32_t tile, uint32_t splits, void* out, uin
 
 }  // namespace
 
-int32_t launch_wide(const WideArgs& a, bool half, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype,
+int32_t launch_wide(const WideArgs& a, bool half, uint32_t tile_m, uint32_t splits, void* out, uint32_t out_dtype,
                     hipStream_t stream) {
-    return (half ? launch<_Float16> : launch<__bf16>)(a, tile, splits, out, out_dtype, stream);
+    return (half ? launch<_Float16> : launch<__bf16>)(a, tile_m, splits, out, out_dtype, stream);
 }
 
 }  // namespace sllm

@@ -112,16 +112,31 @@ struct Plan {
     bool staged = false;       // x is written out as those first
     uint64_t depth = 0, cols = 0;
     uint64_t part_stride = 0;  // elements, of a staged x
-    uint32_t tile = 0, steps = 0, splits = 1;
+    uint32_t tile_m = 0, tile_n = 0, steps = 0, splits = 1;
     uint32_t tiles_m = 0, tiles_j = 0;
     uint64_t x_bytes = 0, split_stride = 0, bytes = 0;
 };
+
+// Whether a product goes to the kernel of few rows.  It reads all of x for every
+// 16 columns of the output, in registers and without a launch more, so it gains
+// where rows and columns are few; measured in us here and by tiles, W 11008 x 4096
+// unless said: bfloat16 5 rows 12.5 and 15.7, 8 rows 14.1 and 15.9, 16 rows 17.8 and
+// 16.4, 16 rows by 32000 x 4096 42 and 30; float16 16 rows by 4096 x 4096 9.6 and
+// 12.6, 5 rows 19.1 and 16.9; float 16 rows 31 and 34, 16 rows by 32000 x 4096 71 and
+// 67; MX FP4 16 rows 11.3 and 15.2, 32 rows 17.1 and 15.6.
+bool few_rows(const LinearLaunch& a) {
+    if (a.grad) return false;
+    if (a.x.codes) return a.m <= 32 && a.m * a.n <= 1 << 18;
+    if (a.m <= 4) return true;
+    if (a.x.dtype == SLLM_DTYPE_F16) return a.m <= 16 && a.n <= 8192;
+    return a.m <= 16 && a.m * a.n <= (a.x.dtype == SLLM_DTYPE_F32 ? 1 << 18 : 1 << 17);
+}
 
 Plan plan_linear(const LinearLaunch& a) {
     Plan p;
     p.depth = a.grad ? a.n : a.k;
     p.cols = a.grad ? a.k : a.n;
-    p.skinny = !a.grad && a.m <= (a.x.codes || a.x.dtype == SLLM_DTYPE_BF16 ? 32 : 16);
+    p.skinny = few_rows(a);
     if (!p.depth || !a.m || !p.cols || p.skinny) return p;
     if (!a.x.codes) p.parts = a.x.dtype == SLLM_DTYPE_F32 ? 3 : 1;
     // The kernel reads x in aligned vectors of eight.
@@ -131,20 +146,33 @@ Plan plan_linear(const LinearLaunch& a) {
     const uint32_t step = a.x.codes ? kNarrowStep : kWideStep;
     p.steps = (uint32_t)ceil_div(p.depth, step);
     if (!a.x.codes) p.steps += p.steps % 2;
-    const auto tiles = [&](uint32_t tile) { return ceil_div(a.m, tile) * ceil_div(p.cols, tile); };
-    const uint64_t depth = (uint64_t)p.steps * p.parts * step, large = tiles(kLargeTile), small = tiles(kSmallTile);
-    if (large >= 192) {
-        p.tile = kLargeTile;
-    } else if (!a.x.codes && large >= 112 && depth >= 8192) {
-        p.tile = kLargeTile;
+    const auto tiles = [&](uint32_t rows, uint32_t cols) { return ceil_div(a.m, rows) * ceil_div(p.cols, cols); };
+    const uint64_t depth = (uint64_t)p.steps * p.parts * step, large = tiles(kLargeTile, kLargeTile);
+    const bool tall = a.m > kSmallTile;
+    // Large tiles read the least per product, and serve where most CUs get one (in
+    // us, large and small: 432 tiles 251 and 279, 172 tiles 93 and 97, MX FP4 39 and
+    // 45), or half of one that is deep enough to pay for the join (128 tiles of a
+    // depth of 11008: 180 and 208, MX FP4 73 and 81; of 4096 by 86 tiles 65 and 61).
+    // Small ones are as tall as there are rows, to half a tile, since the rows past
+    // the last cost as much (16 rows by 11008 x 4096: 32 tall 16.4, 64 18.7, 128 21.9;
+    // 64 rows: 25.2, 21.0, 24.9), and split the depth until there are two for each
+    // CU, of 512 of it at least: half as many take 64 rows by 4096 x 4096 from 17.6 to
+    // 19.1, 1024 of it 333 rows by 2047 x 1000 from 15.3 to 20.1, 256 of it 64 rows by
+    // 4096 x 4096 to 22.9.  With both sides in MX FP4 a tile is done four times as
+    // fast, and splits pay later.
+    if (tall && large >= 160) {
+        p.tile_m = p.tile_n = kLargeTile;
+    } else if (tall && large >= 112 && depth >= 8192) {
+        p.tile_m = p.tile_n = kLargeTile;
         p.splits = 2;
     } else {
-        p.tile = kSmallTile;
+        p.tile_n = kSmallTile;
+        p.tile_m = a.x.codes || a.m > 64 ? kSmallTile : a.m > 32 ? 64 : 32;
         const uint64_t fill = a.x.codes ? 128 : 512, piece = a.x.codes ? 4096 : 512;
-        p.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({fill / small, depth / piece, 16}));
+        p.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({fill / tiles(p.tile_m, p.tile_n), depth / piece, 16}));
     }
-    p.tiles_m = (uint32_t)ceil_div(a.m, p.tile);
-    p.tiles_j = (uint32_t)ceil_div(p.cols, p.tile);
+    p.tiles_m = (uint32_t)ceil_div(a.m, p.tile_m);
+    p.tiles_j = (uint32_t)ceil_div(p.cols, p.tile_n);
     if (p.staged) p.x_bytes = (a.m * p.parts * p.part_stride * 2 + 255) / 256 * 256;
     p.split_stride = a.m * ((p.cols + 3) / 4 * 4);
     p.bytes = p.x_bytes + (p.splits > 1 ? p.splits * p.split_stride * 4 : 0);
@@ -237,7 +265,7 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
     if (a.x.codes) {
         const NarrowArgs n{reinterpret_cast<const u32x4*>(a.x.codes), a.x.scales, reinterpret_cast<const u32x4*>(a.w_codes),
                            a.w_scales, a.m, a.n, mx_blocks(a.k), mx_scale_pitch(a.k), p.steps, p.tiles_m, p.tiles_j, o};
-        SLLM_TRY(launch_narrow(n, p.tile, p.splits, out, dtype, stream));
+        SLLM_TRY(launch_narrow(n, p.tile_n, p.splits, out, dtype, stream));
     } else {
         WideArgs w;
         SLLM_TRY(stage_x(a, p, workspace, &w, stream));
@@ -249,7 +277,7 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
         w.tiles_m = p.tiles_m, w.tiles_j = p.tiles_j;
         w.out_args = o;
         const bool half = a.x.dtype == SLLM_DTYPE_F16;
-        SLLM_TRY((a.grad ? launch_grad : launch_wide)(w, half, p.tile, p.splits, out, dtype, stream));
+        SLLM_TRY((a.grad ? launch_grad : launch_wide)(w, half, p.tile_m, p.splits, out, dtype, stream));
     }
     return p.splits > 1 ? join(p, static_cast<const float*>(out), p.splits, a, stream) : SLLM_OK;
 }

@@ -221,13 +221,14 @@ __device__ __forceinline__ void pin(f32x16 (&acc)[FN][FM]) {
 // A wave's accumulators to memory: element 4 q + i of fragment [n][m] is, in lane
 // (r, h) of two halves of 32, column n * 32 + 8 q + 4 h + i of row m * 32 + r.
 // Stored from there a lane would write 8 bytes of a row of its own, so 32 rows
-// by as many columns as are 128 bytes go through `turn` (this wave's alone) at a
-// time, and eight lanes write a row's 128 bytes.
+// by as many columns as are 128 bytes (or as the wave has) go through `turn` (this
+// wave's alone) at a time, and eight lanes write a row's 128 bytes.
 constexpr uint32_t kTurnBytes = 32 * 128;
 template <int FM, int FN, typename T>
 __device__ __forceinline__ void store_tile(const f32x16 (&acc)[FN][FM], const OutArgs& o, uint64_t m0, uint64_t j0, T* out,
                                            uint8_t* turn) {
-    constexpr int kCols = 128 / sizeof(T), kFragments = kCols / 32, kChunk = 16 / sizeof(T);
+    constexpr int kFragments = FN == 1 ? 1 : 4 / sizeof(T), kCols = kFragments * 32, kChunk = 16 / sizeof(T);
+    constexpr uint32_t kLanes = kCols / kChunk, kRows = 64 / kLanes;
     static_assert(FN % kFragments == 0, "");
     const uint32_t lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
     out += blockIdx.y * o.split_stride;
@@ -249,10 +250,10 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[FN][FM], const Ou
             const uint64_t row0 = m0 + m * 32, col0 = j0 + n0 * 32;
             if (o.vector) {
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    const uint32_t row = i * 8 + lane / 8;
-                    const u32x4 v = *reinterpret_cast<const u32x4*>(turn + chunk_at(row, lane % 8));
-                    const uint64_t col = col0 + lane % 8 * kChunk;
+                for (uint32_t i = 0; i < 32 / kRows; ++i) {
+                    const uint32_t row = i * kRows + lane / kLanes;
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(turn + chunk_at(row, lane % kLanes));
+                    const uint64_t col = col0 + lane % kLanes * kChunk;
                     if (row0 + row >= o.m) continue;
                     T* p = out + (row0 + row) * o.stride + col;
                     if (col + kChunk <= o.cols) {
@@ -291,7 +292,7 @@ struct NarrowArgs {
 int32_t launch_narrow(const NarrowArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
 constexpr uint32_t kNarrowStep = 512;  // depth whose scales are loaded together
 
-// At most 32 rows of x in bfloat16 or MX FP4 (x_scales set), 16 in float16 or float.
+// At most 32 rows of x in MX FP4 (x_scales set), 16 in other types.
 struct SkinnyArgs {
     const void* x;
     const uint8_t* x_scales;
@@ -309,9 +310,11 @@ struct SkinnyArgs {
 int32_t launch_skinny(const SkinnyArgs& a, hipStream_t stream);
 
 // half: x is in float16
-int32_t launch_wide(const WideArgs& a, bool half, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
-int32_t launch_grad(const WideArgs& a, bool half, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
-constexpr uint32_t kLargeTile = 256, kSmallTile = 128;  // rows of x and columns of the output a workgroup holds
+int32_t launch_wide(const WideArgs& a, bool half, uint32_t tile_m, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
+int32_t launch_grad(const WideArgs& a, bool half, uint32_t tile_m, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
+// Rows of x and columns of the output a workgroup holds; small tiles may be 64 or
+// 32 rows tall (`tile_m`) where x is not in MX FP4.
+constexpr uint32_t kLargeTile = 256, kSmallTile = 128;
 constexpr uint32_t kWideStep = 64;   // depth of a stage
 
 }  // namespace sllm

@@ -323,6 +323,21 @@ def test_linear_half_any_scale(m, n, k, scale):
     assert dx[:, :32].isnan().all() and dx[:, 32:].isfinite().all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n", [(4, 33000), (5, 33000), (16, 8200), (16, 17000), (17, 8200), (32, 8200), (33, 8200), (64, 300),
+                                 (65, 300), (128, 300), (129, 300)])
+def test_linear_around_row_limits(dtype, m, n):
+    """Where the way of carrying out a product changes with its rows and columns."""
+    k = 160
+    w, wv = random_mx4(n, k, m)
+    x = normal((m, k), dtype, 21)
+    a = host(x)
+    assert_close(op.mx4_linear(x, w), O.linear(a, wv), sum_bound(a, wv.T, k), dtype)
+    q = op.mx4_quantize(x)
+    a = host(op.mx4_dequantize(q, torch.float32))
+    assert_close(op.mx4_linear(q, w, out_dtype=dtype), O.linear(a, wv), sum_bound(a, wv.T, k), dtype)
+
+
 def test_linear_half_small_values():
     """A weight far below float16's range against large x: no value is lost."""
     m, n, k = 150, 140, 256
