@@ -346,8 +346,23 @@ __global__ __launch_bounds__(256) void join_runs(GradArgs a, T* grad) {
     const float* p = a.partial + ((uint64_t)w * 2 + 1) * a.pitch + c;
     f32x4 lo = reinterpret_cast<const f32x4*>(p)[0], hi = reinterpret_cast<const f32x4*>(p)[1];
     p += a.pitch;
+    uint32_t next = w + 1;
+    // a frequent token's run is a hundred windows long, and each is a load from far away
+    constexpr uint32_t kTogether = 16;
+    for (; next + kTogether <= last + 1; next += kTogether) {
+        f32x4 far[kTogether][2];
+#pragma unroll
+        for (uint32_t i = 0; i < kTogether; ++i, p += 2 * (uint64_t)a.pitch)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) far[i][e] = reinterpret_cast<const f32x4*>(p)[e];
+#pragma unroll
+        for (uint32_t i = 0; i < kTogether; ++i) {
+            lo += far[i][0];
+            hi += far[i][1];
+        }
+    }
 #pragma unroll 8
-    for (uint32_t next = w + 1; next <= last; ++next, p += 2 * (uint64_t)a.pitch) {
+    for (; next <= last; ++next, p += 2 * (uint64_t)a.pitch) {
         lo += reinterpret_cast<const f32x4*>(p)[0];
         hi += reinterpret_cast<const f32x4*>(p)[1];
     }
@@ -420,7 +435,11 @@ int32_t launch_sums(const GradArgs& g, const EmbeddingGradLaunch& a, uint64_t gr
     sum_runs<Vec, S, T><<<(uint32_t)grid, 256, 0, stream>>>(g, static_cast<const S*>(a.dy), grad);
     SLLM_HIP(hipGetLastError());
     if (g.windows > 1) {
-        join_runs<Vec, T><<<g.sum_blocks, 256, 0, stream>>>(g, grad);
+        // a frequent token's columns go to several CUs, each of which takes in only so much
+        GradArgs j = g;
+        j.lanes = std::min(g.lanes, 64u);
+        j.chunks = (uint32_t)ceil_div(g.dim, j.lanes * 8);
+        join_runs<Vec, T><<<(uint32_t)(ceil_div(g.windows, 256 / j.lanes) * j.chunks), 256, 0, stream>>>(j, grad);
         SLLM_HIP(hipGetLastError());
     }
     return SLLM_OK;
