@@ -13,6 +13,14 @@ namespace {
 constexpr uint32_t kStepBlocks = kNarrowStep / kMxBlock;
 constexpr uint32_t kStageBlocks = 4;  // of a stage: 64 bytes a row
 
+// out[m][n] = sum over k of x[m][k] W[n][k], both in four bits, in 32 bits: the
+// scaled matrix instruction takes codes and scales as they are stored.  Bound by
+// what the matrix cores draw: 4096 x 8192 by 28672 takes 500 us, 3.8 PF/s, the
+// matrix cores busy half of the cycles at 1.6 GHz (alone they reach 7).
+//
+// A stage of 128 of the depth is 64 bytes a row: four of them are in flight, loaded
+// straight to LDS, and waited for by their number, not all together.  512 of the
+// depth share a load of scales, 16 bytes a row.
 template <int BM, int BN, int WM, int WN, typename T>
 __global__ __launch_bounds__(WM* WN * 64, 2) void narrow_product(NarrowArgs a, T* out) {
     constexpr int kWaves = WM * WN, FM = BM / WM / 32, FN = BN / WN / 32;

@@ -84,6 +84,11 @@ struct Eight {
     }
 };
 
+// out[m][j] = sum over k of x[m][k] W[j][k] for few rows of x, in 32 bits.  Bound by
+// reading W from memory, and for small ones by the launch and the way there: one
+// row by 32000 x 4096 (70 MB) 17.5 us, 4.0 TB/s, by 11008 x 4096 9.6, by 4096 x 4096
+// 5.4.  With 16 rows x is read as often as W has columns, and bounds it.
+//
 // A workgroup makes 16 columns of the output, its waves each a run of the depth;
 // their sums are joined in LDS, first to last.  Of a step of 128 of the depth,
 // lane (r, g) loads block g of row r: the order in which the matrix instructions
@@ -131,7 +136,8 @@ __device__ __forceinline__ u32x4 transpose4(u32x4 v) {
 // a load fetches 16, or four, pieces of the depth for each, side by side, and all
 // but one piece are masked for each instruction: a 16th, or a quarter, of the
 // loads of x and of its splitting into parts.  The pieces' sums are columns of
-// their own until the end.
+// their own until the end.  One row by 32000 x 4096: 17.5 us, in quarters 19.3, by 16
+// rows 26.2; four rows by 11008 x 4096: 10.0 and 12.9.
 template <typename X, int Rows, int MT>
 __global__ __launch_bounds__(1024) void skinny_product(SkinnyArgs a) {
     extern __shared__ float sums[];
@@ -307,7 +313,9 @@ __global__ __launch_bounds__(1024) void skinny_product(SkinnyArgs a) {
 template <typename X, int Rows, int MT>
 void launch(const SkinnyArgs& a, hipStream_t stream) {
     const uint32_t grid = (uint32_t)((a.n + 15) / 16);
-    // enough waves to fill the GPU, two groups of the depth for each where there are as many
+    // Enough waves to fill the GPU, two groups of the depth for each where there are
+    // as many: one row by 32000 x 4096 17.5 us with four waves, 20.0 with eight; by
+    // 1024 x 8192 5.9 with 16, 7.3 with four.
     uint32_t waves = 4;
     while (waves < 16 && (a.groups > waves * 2 || (grid * waves < 2048 && a.groups > waves))) waves *= 2;
     while (waves > 1 && a.groups < waves) waves /= 2;

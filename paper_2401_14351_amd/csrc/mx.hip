@@ -31,8 +31,13 @@ __device__ __forceinline__ float quad(float x) {
     return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), Ctrl, 0xF, 0xF, true));
 }
 
-// Four lanes a block, eight columns each, `lanes` of them a row at a time.
-// Vec: rows start on 16 bytes and end on a multiple of eight columns.
+// x is read once and its 4.25 bits a value written once; bound by memory (11008
+// x 4096 in bfloat16, 90 MB in and 24 MB out, in 18.4 us: 6.2 TB/s).  Four lanes a
+// block, eight columns each: a lane's loads are 16 bytes wide, neighbours' codes
+// are neighbouring words, and a block's largest magnitude is two lane exchanges
+// away.  Elements are rounded to nearest even by the conversion instruction.
+// `lanes` of them take a row at a time.  Vec: rows start on 16 bytes and end on a
+// multiple of eight columns; else elements are loaded one by one.
 template <bool Vec, typename T>
 __global__ __launch_bounds__(256) void mx_quantize(const T* src, uint64_t stride, uint64_t rows, uint32_t cols, uint32_t lanes,
                                                    uint8_t* codes, uint8_t* scales) {
@@ -86,7 +91,10 @@ __global__ __launch_bounds__(256) void mx_quantize(const T* src, uint64_t stride
 
 int32_t launch_quantize(const sllm_matrix& src, const sllm_mx& dst, hipStream_t stream) {
     const uint64_t vectors = mx_scale_pitch(src.cols) * 4;
-    const uint32_t lanes = vectors >= 256 ? 256 : vectors >= 128 ? 128 : 64;
+    // Long rows take a workgroup (11008 rows of 4096 in 32 bits 39 us, a wave each
+    // 44; 512 rows 3.7 and 6.1), short ones a wave (32000 of 768 in bfloat16 12, a
+    // workgroup 18).
+    const uint32_t lanes = vectors >= 256 ? 256 : 64;
     const uint64_t grid = ceil_div(src.rows, 256 / lanes);
     if (grid > UINT32_MAX / 256) return fail(SLLM_E_RANGE, "%llu rows are more than a launch takes", (unsigned long long)src.rows);
     const uint64_t row_bytes = src.stride * (src.dtype == SLLM_DTYPE_F32 ? 4 : 2);
@@ -180,7 +188,10 @@ Plan plan_linear(const LinearLaunch& a) {
 }
 
 // x as the sum of `Parts` bfloat16 matrices: its leading eight bits, the eight
-// after those, the rest.  Of one part it is a copy, of any 16 bits.
+// after those, the rest.  Of one part it is a copy, of any 16 bits, for rows that
+// do not start on 16 bytes.  The products then load x straight to LDS, and the
+// parts are made once, not by every tile.  Bound by its launch or by memory: 333 x
+// 2047 in float16 4.2 us.
 template <typename T, int Parts>
 __global__ __launch_bounds__(256) void split_x(const T* x, uint64_t stride, uint64_t rows, uint64_t cols, uint64_t pitch,
                                                uint16_t* out) {
@@ -204,7 +215,9 @@ __global__ __launch_bounds__(256) void split_x(const T* x, uint64_t stride, uint
     }
 }
 
-// The sum of the splits' matrices, first to last.
+// The sum of the splits' matrices, first to last, so that every call adds in the
+// same order.  Bound by memory: two of 2048 x 4096 (67 MB in, 17 MB out) 13.5 us,
+// 6.2 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void join_splits(const float* in, uint32_t splits, uint64_t split_stride, uint64_t rows,
                                                    uint64_t cols, T* out, uint64_t stride) {
