@@ -399,7 +399,7 @@ bool on_vectors(const void* data, uint64_t rows, uint64_t stride, uint32_t dtype
 
 // Lanes that take a row together, eight columns each: a workgroup for long rows
 // (512 rows of 4096 looked up in 3.6 us, by a wave each 4.7), a wave or half of one
-// for others (16384 of 768 9.8, by workgroups 12.4; of 256 5.8, by waves 5.5).
+// for others (16384 of 768 9.8, by workgroups 12.4; of 256 4.6, by waves 5.4).
 uint32_t row_lanes(uint64_t dim) { return dim > 1024 ? 256 : dim > 256 ? 64 : 32; }
 
 template <bool Vec, typename T>
