@@ -161,13 +161,16 @@ Plan plan_linear(const LinearLaunch& a) {
     // us, large and small: 432 tiles 251 and 279, 172 tiles 93 and 97, MX FP4 39 and
     // 45), or half of one that is deep enough to pay for the join (128 tiles of a
     // depth of 11008: 180 and 208, MX FP4 73 and 81; of 4096 by 86 tiles 65 and 61).
-    // Small ones are as tall as there are rows, to half a tile, since the rows past
+    // Small ones are 32 or 64 rows tall where there are no more, since the rows past
     // the last cost as much (16 rows by 11008 x 4096: 32 tall 16.4, 64 18.7, 128 21.9;
-    // 64 rows: 25.2, 21.0, 24.9), and split the depth until there are two for each
-    // CU, of 512 of it at least: half as many take 64 rows by 4096 x 4096 from 17.6 to
-    // 19.1, 1024 of it 333 rows by 2047 x 1000 from 15.3 to 20.1, 256 of it 64 rows by
-    // 4096 x 4096 to 22.9.  With both sides in MX FP4 a tile is done four times as
-    // fast, and splits pay later.
+    // 64 rows: 25.2, 21.0, 24.9), and 32 for problems of few stages of 128 x 128 x 64,
+    // which would leave CUs empty (400 stages, 700 x 700 x 700: 32 tall 12.1, 64 14.2,
+    // 128 18.3; 4096, 1000 x 2000 x 2000: 20.3, 26.0, 25.9; 6144, 300 x 4096 x 4096:
+    // 34.2, 27.5, 29.2; 8192, 512 x 4096 x 4096: 38.5, 34.4, 33.5).  They split the
+    // depth until there are two for each CU, of 512 of it at least: half as many take
+    // 64 rows by 4096 x 4096 from 17.6 to 19.1, 1024 of it 333 rows by 2047 x 1000 from
+    // 15.3 to 20.1, 256 of it 64 rows by 4096 x 4096 to 22.9.  With both sides in MX
+    // FP4 a tile is done four times as fast, and splits pay later.
     if (tall && large >= 160) {
         p.tile_m = p.tile_n = kLargeTile;
     } else if (tall && large >= 112 && depth >= 8192) {
@@ -175,7 +178,8 @@ Plan plan_linear(const LinearLaunch& a) {
         p.splits = 2;
     } else {
         p.tile_n = kSmallTile;
-        p.tile_m = a.x.codes || a.m > 64 ? kSmallTile : a.m > 32 ? 64 : 32;
+        const bool short_tiles = a.m <= 32 || tiles(kSmallTile, kSmallTile) * p.steps * p.parts <= 4096;
+        p.tile_m = a.x.codes ? kSmallTile : short_tiles ? 32 : a.m <= 64 ? 64 : kSmallTile;
         const uint64_t fill = a.x.codes ? 128 : 512, piece = a.x.codes ? 4096 : 512;
         p.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({fill / tiles(p.tile_m, p.tile_n), depth / piece, 16}));
     }

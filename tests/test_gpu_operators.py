@@ -338,6 +338,48 @@ def test_linear_around_row_limits(dtype, m, n):
     assert_close(op.mx4_linear(q, w, out_dtype=dtype), O.linear(a, wv), sum_bound(a, wv.T, k), dtype)
 
 
+@pytest.fixture(scope="module", params=[(130, 2100, 8200), (50, 4300, 8200), (3300, 3600, 96), (3300, 96, 3600)],
+                ids=lambda s: "x".join(map(str, s)))
+def large_weight(request):
+    m, n, k = request.param
+    return (m, n, k) + random_mx4(n, k, 23)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_every_tile(large_weight, dtype):
+    """Problems that go by the tallest tiles of each kind, with rows and columns past the last whole one."""
+    m, n, k, w, wv = large_weight
+    x, dy = normal((m, k), dtype, 24), normal((m, n), dtype, 25)
+    a, b = host(x), host(dy)
+    assert_close(op.mx4_linear(x, w), O.linear(a, wv), sum_bound(a, wv.T, k), dtype)
+    assert_close(op.mx4_linear_grad(dy, w), O.linear_grad(b, wv), sum_bound(b, wv, n), dtype)
+    q = op.mx4_quantize(x)
+    a = host(op.mx4_dequantize(q, torch.float32))
+    assert_close(op.mx4_linear(q, w, out_dtype=dtype), O.linear(a, wv), sum_bound(a, wv.T, k), dtype)
+
+
+def test_linear_in_halves():
+    """Large tiles with the depth in two, where float's three parts make it deep enough."""
+    m, n, k = 1500, 4900, 2800
+    w, wv = random_mx4(n, k, 26)
+    x = normal((m, k), torch.float32, 27)
+    assert_close(op.mx4_linear(x, w), O.linear(host(x), wv), sum_bound(host(x), wv.T, k), torch.float32)
+    v, vv = random_mx4(k, n, 28)
+    assert_close(op.mx4_linear_grad(x, v), O.linear_grad(host(x), vv), sum_bound(host(x), vv, k), torch.float32)
+
+
+def test_linear_mx_in_halves():
+    """The same with both sides in MX FP4, against the small tiles that 100 rows at a time go by: each is off by
+    at most a sum's bound."""
+    m, n, k = 1500, 4900, 8200
+    w, _ = random_mx4(n, k, 29, (120, 124))
+    q = op.mx4_quantize(normal((m, k), torch.float32, 30))
+    whole = op.mx4_linear(q, w, out_dtype=torch.float32)
+    parts = torch.cat([op.mx4_linear(q[r:r + 100], w, out_dtype=torch.float32) for r in range(0, m, 100)])
+    sizes = op.mx4_dequantize(q, torch.float32).abs() @ op.mx4_dequantize(w, torch.float32).abs().T
+    assert ((whole - parts).abs() <= 2 * 2 * (k + 8) * 2.0 ** -24 * sizes).all()
+
+
 def test_linear_half_small_values():
     """A weight far below float16's range against large x: no value is lost."""
     m, n, k = 150, 140, 256
