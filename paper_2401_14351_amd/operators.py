@@ -71,6 +71,14 @@ class Mx4:
                torch.empty((rows, scale_pitch), dtype=torch.uint8, device=device), cols)
         return q
 
+    @classmethod
+    def _beside(cls, t: torch.Tensor, rows: int, cols: int) -> "Mx4":
+        """One whose contents are not set, where t is: half a microsecond less than by naming the device."""
+        code_pitch, scale_pitch = _pitches(cols)
+        q = cls.__new__(cls)
+        q._set(t.new_empty((rows, code_pitch), dtype=torch.uint8), t.new_empty((rows, scale_pitch), dtype=torch.uint8), cols)
+        return q
+
     @property
     def shape(self):
         return torch.Size((self.rows, self.cols))
@@ -167,12 +175,19 @@ def _on_stream(stream, operator, *args, keep=(), **kwargs):
     return result
 
 
-def _output(out: Optional[torch.Tensor], shape, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
+def _output(out: Optional[torch.Tensor], shape, rows: int, cols: int, dtype: torch.dtype, like: torch.Tensor):
+    """A result of ``rows`` x ``cols`` and its rows: ``out``, or a new tensor where ``like`` is."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if out.shape != torch.Size(shape) or out.device != device:
-        raise ValueError(f"out: expected shape {tuple(shape)} on {device}, got {tuple(out.shape)} on {out.device}")
-    return out
+        code = _DTYPE.get(dtype)
+        if code is None:
+            raise ValueError(f"out: {dtype} is not float32, float16 or bfloat16")
+        out = like.new_empty(shape, dtype=dtype)
+        return out, binding.Matrix(out.data_ptr(), rows, cols, cols, code, 0)
+    if out.shape != torch.Size(shape) or out.device != like.device:
+        raise ValueError(f"out: expected shape {tuple(shape)} on {like.device}, got {tuple(out.shape)} on {out.device}")
+    if out.requires_grad:
+        _refuse_grad(out)
+    return out, _matrix(out, "out")
 
 
 def _refuse_grad(*tensors):
@@ -192,7 +207,7 @@ def _call(fn, query, operands, out, device):
     """fn over its operands and output, with the workspace that the query asks for."""
     n = _workspace(query, *operands)
     if n:
-        ws = torch.empty(n, dtype=torch.uint8, device=torch.device("cuda", device))
+        ws = torch.empty(n, dtype=torch.uint8, device=f"cuda:{device}")
         code = fn(*operands, out, ws.data_ptr(), n, device, _raw_stream(device))
     else:
         code = fn(*operands, out, None, 0, device, _raw_stream(device))
@@ -206,7 +221,7 @@ def mx4_quantize(x: torch.Tensor, out: Optional[Mx4] = None, stream=None) -> Mx4
     src = _matrix(x, "x")
     device = _one_device(x, out)
     if out is None:
-        out = Mx4.empty(src.rows, src.cols, x.device)
+        out = Mx4._beside(x, src.rows, src.cols)
     elif out.rows != src.rows or out.cols != src.cols:
         raise ValueError(f"out: expected {src.rows} x {src.cols}, got {out.rows} x {out.cols}")
     binding.check(binding.lib().sllm_mx_quantize(src, out._struct, device, _raw_stream(device)))
@@ -218,10 +233,9 @@ def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, out: Optional[to
     """The values q stands for, rounded to ``dtype`` (or the type of ``out``)."""
     if stream is not None:
         return _on_stream(stream, mx4_dequantize, q, dtype, out, keep=(q, out))
-    _refuse_grad(out)
-    device = _one_device(q)
-    out = _output(out, (q.rows, q.cols), dtype, q.device)
-    binding.check(binding.lib().sllm_mx_dequantize(q._struct, _matrix(out, "out"), device, _raw_stream(device)))
+    device = q._device
+    out, rows = _output(out, (q.rows, q.cols), q.rows, q.cols, dtype, q.codes)
+    binding.check(binding.lib().sllm_mx_dequantize(q._struct, rows, device, _raw_stream(device)))
     return out
 
 
@@ -234,7 +248,6 @@ def mx4_linear(x: Union[torch.Tensor, Mx4], w: Mx4, out: Optional[torch.Tensor] 
     an :class:`Mx4`)."""
     if stream is not None:
         return _on_stream(stream, mx4_linear, x, w, out, out_dtype, keep=(x, w, out))
-    _refuse_grad(out)
     if isinstance(x, Mx4):
         return _linear_mx(x, w, out, out_dtype)
     if x.requires_grad and torch.is_grad_enabled():
@@ -248,16 +261,16 @@ def _linear(x, w, out, out_dtype):
     L = binding.lib()
     src = _matrix(x, "x")
     device = _one_device(x, w)
-    out = _output(out, x.shape[:-1] + (w.rows,), out_dtype or x.dtype, x.device)
-    _call(L.sllm_mx_linear, L.sllm_mx_linear_workspace, (src, w._struct), _matrix(out, "out"), device)
+    out, rows = _output(out, (*x.shape[:-1], w.rows), src.rows, w.rows, out_dtype or x.dtype, x)
+    _call(L.sllm_mx_linear, L.sllm_mx_linear_workspace, (src, w._struct), rows, device)
     return out
 
 
 def _linear_mx(x, w, out, out_dtype):
     L = binding.lib()
     device = _one_device(x, w)
-    out = _output(out, (x.rows, w.rows), out_dtype or torch.bfloat16, x.device)
-    _call(L.sllm_mx_linear_mx, L.sllm_mx_linear_mx_workspace, (x._struct, w._struct), _matrix(out, "out"), device)
+    out, rows = _output(out, (x.rows, w.rows), x.rows, w.rows, out_dtype or torch.bfloat16, x.codes)
+    _call(L.sllm_mx_linear_mx, L.sllm_mx_linear_mx_workspace, (x._struct, w._struct), rows, device)
     return out
 
 
@@ -267,12 +280,12 @@ def mx4_linear_grad(dy: torch.Tensor, w: Mx4, out: Optional[torch.Tensor] = None
     (..., w.rows)."""
     if stream is not None:
         return _on_stream(stream, mx4_linear_grad, dy, w, out, out_dtype, keep=(dy, w, out))
-    _refuse_grad(dy, out)
+    _refuse_grad(dy)
     L = binding.lib()
     src = _matrix(dy, "dy")
     device = _one_device(dy, w)
-    out = _output(out, dy.shape[:-1] + (w.cols,), out_dtype or dy.dtype, dy.device)
-    _call(L.sllm_mx_linear_grad, L.sllm_mx_linear_grad_workspace, (src, w._struct), _matrix(out, "out"), device)
+    out, rows = _output(out, (*dy.shape[:-1], w.cols), src.rows, w.cols, out_dtype or dy.dtype, dy)
+    _call(L.sllm_mx_linear_grad, L.sllm_mx_linear_grad_workspace, (src, w._struct), rows, device)
     return out
 
 
@@ -298,7 +311,6 @@ def embedding(table: Union[torch.Tensor, Mx4], tokens: torch.Tensor, scale: floa
     a row of zeros."""
     if stream is not None:
         return _on_stream(stream, embedding, table, tokens, scale, out, out_dtype, keep=(table, tokens, out))
-    _refuse_grad(out)
     if not isinstance(table, Mx4) and table.requires_grad and torch.is_grad_enabled():
         if out is not None:
             raise ValueError("an operator that writes to a given tensor takes no part in autograd")
@@ -311,13 +323,14 @@ def _embedding(table, tokens, scale, out, out_dtype):
     ids = _ids(tokens)
     device = _one_device(table, tokens)
     if isinstance(table, Mx4):
-        fn, rows, cols, dtype = L.sllm_embedding_mx, table._struct, table.cols, torch.bfloat16
+        fn, src, dtype = L.sllm_embedding_mx, table._struct, torch.bfloat16
     elif table.dim() == 2:
-        fn, rows, cols, dtype = L.sllm_embedding, _matrix(table, "table"), table.shape[1], table.dtype
+        fn, src, dtype = L.sllm_embedding, _matrix(table, "table"), table.dtype
     else:
         raise ValueError(f"table: expected rows and columns, got shape {tuple(table.shape)}")
-    out = _output(out, tokens.shape + (cols,), out_dtype or dtype, table.device)
-    binding.check(fn(rows, ids, scale, _matrix(out, "out"), device, _raw_stream(device)))
+    like = table.codes if isinstance(table, Mx4) else table
+    out, rows = _output(out, (*tokens.shape, src.cols), ids.n, src.cols, out_dtype or dtype, like)
+    binding.check(fn(src, ids, scale, rows, device, _raw_stream(device)))
     return out
 
 
@@ -330,7 +343,7 @@ def embedding_grad(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: fl
     if stream is not None:
         return _on_stream(stream, embedding_grad, dy, tokens, vocab, scale, out, out_dtype, accumulate,
                           keep=(dy, tokens, out))
-    _refuse_grad(dy, out)
+    _refuse_grad(dy)
     if accumulate and out is None:
         raise ValueError("accumulate needs a gradient to add to")
     if dy.shape[:-1] != tokens.shape:
@@ -338,8 +351,7 @@ def embedding_grad(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: fl
     L = binding.lib()
     ids, src = _ids(tokens), _matrix(dy, "dy")
     device = _one_device(dy, tokens)
-    out = _output(out, (vocab, dy.shape[-1]), out_dtype or dy.dtype, dy.device)
-    grad = _matrix(out, "out")
+    out, grad = _output(out, (vocab, src.cols), vocab, src.cols, out_dtype or dy.dtype, dy)
     n = _workspace(L.sllm_embedding_grad_workspace, ids.n, grad)
     ws = torch.empty(n, dtype=torch.uint8, device=dy.device) if n else None
     binding.check(L.sllm_embedding_grad(src, ids, scale, 1 if accumulate else 0, grad, ws.data_ptr() if n else None, n,
