@@ -23,6 +23,8 @@ other tensors are refused, not copied.
 from __future__ import annotations
 
 import ctypes as C
+import functools
+from types import SimpleNamespace
 from typing import Optional, Union
 
 import torch
@@ -44,7 +46,7 @@ class Mx4:
     """A matrix in MX FP4: ``codes`` (rows, blocks * 16) and ``scales`` (rows,
     blocks rounded up to 16), both contiguous uint8, laid out as ``sllm_mx``."""
 
-    __slots__ = ("codes", "scales", "rows", "cols", "_struct", "_device")
+    __slots__ = ("codes", "scales", "rows", "cols", "_struct", "_address", "_device")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int):
         code_pitch, scale_pitch = _pitches(cols)
@@ -60,6 +62,7 @@ class Mx4:
         self.codes, self.scales = codes, scales
         self.rows, self.cols = codes.shape[0], cols
         self._struct = binding.Mx(codes.data_ptr(), scales.data_ptr(), self.rows, cols)
+        self._address = C.addressof(self._struct)
         self._device = codes.get_device()
 
     @classmethod
@@ -214,10 +217,49 @@ def _call(fn, query, operands, out, device):
     binding.check(code)
 
 
+@functools.lru_cache(maxsize=None)
+def _native():
+    """The extension that makes ordinary calls (tensors on one GPU whose rows need no
+    second look, results allocated) and the entry points' addresses, or None
+    where it was not built for this Python and torch.  Its functions return the
+    result, None for a call that is not ordinary, or a failed call's code."""
+    ext = binding._views_ext()
+    if not hasattr(ext, "product"):
+        return None
+    L = binding.lib()
+    names = ("sllm_mx_quantize", "sllm_mx_dequantize", "sllm_mx_linear", "sllm_mx_linear_workspace", "sllm_mx_linear_mx",
+             "sllm_mx_linear_mx_workspace", "sllm_mx_linear_grad", "sllm_mx_linear_grad_workspace", "sllm_embedding",
+             "sllm_embedding_mx", "sllm_embedding_grad", "sllm_embedding_grad_workspace")
+    return SimpleNamespace(ext=ext, **{n[5:]: C.cast(getattr(L, n), C.c_void_p).value for n in names})
+
+
+def _product(call: str, x, w, out_dtype, grad: int):
+    """A product by the extension, or None."""
+    native, device = _native(), x.get_device()
+    code = -1 if out_dtype is None else _DTYPE.get(out_dtype)
+    if native is None or device < 0 or device != w._device or code is None:
+        return None
+    y = native.ext.product(getattr(native, call), getattr(native, call + "_workspace"), x, w._address, code, grad, device,
+                           _raw_stream(device))
+    if y.__class__ is int:
+        binding.check(y)
+    return y
+
+
 def mx4_quantize(x: torch.Tensor, out: Optional[Mx4] = None, stream=None) -> Mx4:
     """The rows of x (its leading dimensions flattened) in MX FP4."""
     if stream is not None:
         return _on_stream(stream, mx4_quantize, x, out, keep=(x, out))
+    device = x.get_device()
+    if out is None and device >= 0 and _native() is not None:
+        native = _native()
+        parts = native.ext.quantize(native.mx_quantize, x, device, _raw_stream(device))
+        if parts.__class__ is int:
+            binding.check(parts)
+        if parts is not None:
+            q = Mx4.__new__(Mx4)
+            q._set(*parts, x.shape[-1])
+            return q
     src = _matrix(x, "x")
     device = _one_device(x, out)
     if out is None:
@@ -234,6 +276,13 @@ def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, out: Optional[to
     if stream is not None:
         return _on_stream(stream, mx4_dequantize, q, dtype, out, keep=(q, out))
     device = q._device
+    if out is None and device >= 0 and dtype in _DTYPE and _native() is not None:
+        native = _native()
+        y = native.ext.dequantize(native.mx_dequantize, q._address, q.codes, _DTYPE[dtype], device, _raw_stream(device))
+        if y.__class__ is int:
+            binding.check(y)
+        if y is not None:
+            return y
     out, rows = _output(out, (q.rows, q.cols), q.rows, q.cols, dtype, q.codes)
     binding.check(binding.lib().sllm_mx_dequantize(q._struct, rows, device, _raw_stream(device)))
     return out
@@ -258,6 +307,10 @@ def mx4_linear(x: Union[torch.Tensor, Mx4], w: Mx4, out: Optional[torch.Tensor] 
 
 
 def _linear(x, w, out, out_dtype):
+    if out is None:
+        y = _product("mx_linear", x, w, out_dtype, 0)
+        if y is not None:
+            return y
     L = binding.lib()
     src = _matrix(x, "x")
     device = _one_device(x, w)
@@ -267,8 +320,17 @@ def _linear(x, w, out, out_dtype):
 
 
 def _linear_mx(x, w, out, out_dtype):
-    L = binding.lib()
     device = _one_device(x, w)
+    code = _DTYPE.get(out_dtype or torch.bfloat16)
+    if out is None and device >= 0 and code is not None and _native() is not None:
+        native = _native()
+        y = native.ext.product_mx(native.mx_linear_mx, native.mx_linear_mx_workspace, x._address, w._address, x.codes, code,
+                                  device, _raw_stream(device))
+        if y.__class__ is int:
+            binding.check(y)
+        if y is not None:
+            return y
+    L = binding.lib()
     out, rows = _output(out, (x.rows, w.rows), x.rows, w.rows, out_dtype or torch.bfloat16, x.codes)
     _call(L.sllm_mx_linear_mx, L.sllm_mx_linear_mx_workspace, (x._struct, w._struct), rows, device)
     return out
@@ -281,6 +343,10 @@ def mx4_linear_grad(dy: torch.Tensor, w: Mx4, out: Optional[torch.Tensor] = None
     if stream is not None:
         return _on_stream(stream, mx4_linear_grad, dy, w, out, out_dtype, keep=(dy, w, out))
     _refuse_grad(dy)
+    if out is None:
+        dx = _product("mx_linear_grad", dy, w, out_dtype, 1)
+        if dx is not None:
+            return dx
     L = binding.lib()
     src = _matrix(dy, "dy")
     device = _one_device(dy, w)
@@ -319,9 +385,18 @@ def embedding(table: Union[torch.Tensor, Mx4], tokens: torch.Tensor, scale: floa
 
 
 def _embedding(table, tokens, scale, out, out_dtype):
+    device, mx = _one_device(table, tokens), isinstance(table, Mx4)
+    code = (2 if mx else -1) if out_dtype is None else _DTYPE.get(out_dtype)
+    if out is None and device >= 0 and code is not None and _native() is not None:
+        native = _native()
+        y = native.ext.lookup(native.embedding_mx if mx else native.embedding, table._address if mx else table,
+                              table.codes if mx else None, tokens, scale, code, device, _raw_stream(device))
+        if y.__class__ is int:
+            binding.check(y)
+        if y is not None:
+            return y
     L = binding.lib()
     ids = _ids(tokens)
-    device = _one_device(table, tokens)
     if isinstance(table, Mx4):
         fn, src, dtype = L.sllm_embedding_mx, table._struct, torch.bfloat16
     elif table.dim() == 2:
@@ -348,9 +423,18 @@ def embedding_grad(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: fl
         raise ValueError("accumulate needs a gradient to add to")
     if dy.shape[:-1] != tokens.shape:
         raise ValueError(f"dy of shape {tuple(dy.shape)} for tokens of shape {tuple(tokens.shape)}")
+    device = _one_device(dy, tokens)
+    code = -1 if out_dtype is None else _DTYPE.get(out_dtype)
+    if out is None and device >= 0 and code is not None and _native() is not None:
+        native = _native()
+        y = native.ext.lookup_grad(native.embedding_grad, native.embedding_grad_workspace, dy, tokens, vocab, scale, code, device,
+                                   _raw_stream(device))
+        if y.__class__ is int:
+            binding.check(y)
+        if y is not None:
+            return y
     L = binding.lib()
     ids, src = _ids(tokens), _matrix(dy, "dy")
-    device = _one_device(dy, tokens)
     out, grad = _output(out, (vocab, src.cols), vocab, src.cols, out_dtype or dy.dtype, dy)
     n = _workspace(L.sllm_embedding_grad_workspace, ids.n, grad)
     ws = torch.empty(n, dtype=torch.uint8, device=dy.device) if n else None

@@ -1,0 +1,272 @@
+// The operators' calls from Python: operands described, the result and its
+// workspace allocated and the C entry point called in one go.
+//
+// A small operator's kernel takes 3 to 9 us, and its call from Python took longer:
+// 8.5 us, of which 4 are the entry point's (its checks and the launch) and the rest
+// the interpreter's.  These functions take the ordinary call, tensors on a GPU whose
+// rows need no second look, and return None for any other: Python then carries it
+// out, or says what is wrong with it.  A failed call's code is returned as a number.
+//
+// Entry points come as addresses, so this extension needs nothing of libsllm.so.
+#pragma once
+
+#include <Python.h>
+
+#include <ATen/Functions.h>
+#include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <cstdint>
+
+#include "sllm.h"
+
+namespace operators {
+
+inline bool dtype_code(at::ScalarType type, uint32_t* code) {
+    *code = type == at::kFloat ? SLLM_DTYPE_F32 : type == at::kHalf ? SLLM_DTYPE_F16 : SLLM_DTYPE_BF16;
+    return type == at::kFloat || type == at::kHalf || type == at::kBFloat16;
+}
+
+constexpr at::ScalarType kTypes[] = {at::kFloat, at::kHalf, at::kBFloat16};  // by SLLM_DTYPE_*
+
+// A tensor argument, or null where it is not a plain tensor on `device`.
+inline const at::Tensor* tensor(PyObject* o, int64_t device) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return t.is_cuda() && t.layout() == at::kStrided && t.get_device() == device ? &t : nullptr;
+}
+
+// The rows of t, its last dimension's runs of elements.
+inline bool rows_of(const at::Tensor& t, sllm_matrix* m) {
+    uint32_t code;
+    const int64_t dim = t.dim();
+    if (!dtype_code(t.scalar_type(), &code) || dim < 1) return false;
+    const int64_t cols = t.size(dim - 1);
+    const int64_t rows = dim == 1 ? 1 : dim == 2 ? t.size(0) : cols ? t.numel() / cols : 0;
+    if (!rows || !cols || (dim > 2 && !t.is_contiguous()) || (cols > 1 && t.stride(dim - 1) != 1)) return false;
+    const int64_t stride = dim == 2 && rows > 1 ? t.stride(0) : cols;
+    if (stride < 0) return false;
+    *m = sllm_matrix{t.data_ptr(), (uint64_t)rows, (uint64_t)cols, (uint64_t)stride, code, 0};
+    return true;
+}
+
+inline bool ids_of(const at::Tensor& t, sllm_ids* ids) {
+    const bool wide = t.scalar_type() == at::kLong;
+    if ((!wide && t.scalar_type() != at::kInt) || !t.is_contiguous() || !t.numel()) return false;
+    *ids = sllm_ids{t.data_ptr(), (uint64_t)t.numel(), wide ? 64u : 32u, 0};
+    return true;
+}
+
+// A new tensor beside `like`, and its rows.
+inline at::Tensor make(const at::Tensor& like, at::IntArrayRef shape, uint64_t rows, uint32_t code, sllm_matrix* m) {
+    at::Tensor t = at::empty(shape, like.options().dtype(kTypes[code]).requires_grad(false));
+    const uint64_t cols = (uint64_t)shape.back();
+    *m = sllm_matrix{t.data_ptr(), rows, cols, cols, code, 0};
+    return t;
+}
+
+inline at::Tensor bytes(const at::Tensor& like, int64_t rows, int64_t n) {
+    return at::empty({rows, n}, like.options().dtype(at::kByte).requires_grad(false));
+}
+
+inline PyObject* result(int32_t code, at::Tensor&& t) {
+    return code == SLLM_OK ? THPVariable_Wrap(std::move(t)) : PyLong_FromLong(code);
+}
+
+template <typename T>
+T address(PyObject* o) {
+    return reinterpret_cast<T>(PyLong_AsVoidPtr(o));
+}
+
+#define SLLM_PY_ARGS(n, what)                    \
+    if (nargs != n) {                            \
+        PyErr_SetString(PyExc_TypeError, what);  \
+        return nullptr;                          \
+    }
+
+// product(call, workspace, x, w, dtype, grad, device, stream): x @ w.T, or with
+// `grad` x @ w.  w and dtype as sllm_mx's address and SLLM_DTYPE_*, or -1 for x's.
+inline PyObject* product(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    SLLM_PY_ARGS(8, "product(call, workspace, x, w, dtype, grad, device, stream)")
+    typedef int32_t (*Call)(const sllm_matrix*, const sllm_mx*, const sllm_matrix*, void*, uint64_t, int32_t, void*);
+    typedef int32_t (*Workspace)(const sllm_matrix*, const sllm_mx*, uint64_t*);
+    const auto call = address<Call>(args[0]);
+    const auto workspace = address<Workspace>(args[1]);
+    const auto* w = address<const sllm_mx*>(args[3]);
+    const long type = PyLong_AsLong(args[4]), grad = PyLong_AsLong(args[5]), device = PyLong_AsLong(args[6]);
+    void* const stream = PyLong_AsVoidPtr(args[7]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor* x = tensor(args[2], device);
+    sllm_matrix rows, out_rows;
+    if (!x || !rows_of(*x, &rows)) Py_RETURN_NONE;
+    const uint64_t cols = grad ? w->cols : w->rows;
+    if (!cols || rows.cols != (grad ? w->rows : w->cols)) Py_RETURN_NONE;
+    c10::SmallVector<int64_t, 4> shape(x->sizes().begin(), x->sizes().end());
+    shape.back() = (int64_t)cols;
+    at::Tensor out = make(*x, shape, rows.rows, type < 0 ? rows.dtype : (uint32_t)type, &out_rows), ws;
+    int32_t code;
+    {
+        pybind11::gil_scoped_release no_gil;
+        uint64_t n = 0;
+        code = workspace(&rows, w, &n);
+        if (code == SLLM_OK) {
+            if (n) ws = bytes(*x, 1, (int64_t)n);
+            code = call(&rows, w, &out_rows, n ? ws.data_ptr() : nullptr, n, (int32_t)device, stream);
+        }
+    }
+    return result(code, std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// product_mx(call, workspace, x, w, codes, dtype, device, stream): the same with x
+// in MX FP4, whose codes tell where the result is allocated.
+inline PyObject* product_mx(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    SLLM_PY_ARGS(8, "product_mx(call, workspace, x, w, codes, dtype, device, stream)")
+    typedef int32_t (*Call)(const sllm_mx*, const sllm_mx*, const sllm_matrix*, void*, uint64_t, int32_t, void*);
+    typedef int32_t (*Workspace)(const sllm_mx*, const sllm_mx*, uint64_t*);
+    const auto call = address<Call>(args[0]);
+    const auto workspace = address<Workspace>(args[1]);
+    const auto *x = address<const sllm_mx*>(args[2]), *w = address<const sllm_mx*>(args[3]);
+    const long type = PyLong_AsLong(args[5]), device = PyLong_AsLong(args[6]);
+    void* const stream = PyLong_AsVoidPtr(args[7]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor* codes = tensor(args[4], device);
+    if (!codes || !x->rows || !w->rows || x->cols != w->cols) Py_RETURN_NONE;
+    sllm_matrix out_rows;
+    at::Tensor out = make(*codes, {(int64_t)x->rows, (int64_t)w->rows}, x->rows, (uint32_t)type, &out_rows), ws;
+    int32_t code;
+    {
+        pybind11::gil_scoped_release no_gil;
+        uint64_t n = 0;
+        code = workspace(x, w, &n);
+        if (code == SLLM_OK) {
+            if (n) ws = bytes(*codes, 1, (int64_t)n);
+            code = call(x, w, &out_rows, n ? ws.data_ptr() : nullptr, n, (int32_t)device, stream);
+        }
+    }
+    return result(code, std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// quantize(call, x, device, stream) -> (codes, scales)
+inline PyObject* quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    SLLM_PY_ARGS(4, "quantize(call, x, device, stream)")
+    typedef int32_t (*Call)(const sllm_matrix*, const sllm_mx*, int32_t, void*);
+    const auto call = address<Call>(args[0]);
+    const long device = PyLong_AsLong(args[2]);
+    void* const stream = PyLong_AsVoidPtr(args[3]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor* x = tensor(args[1], device);
+    sllm_matrix rows;
+    if (!x || !rows_of(*x, &rows)) Py_RETURN_NONE;
+    const int64_t blocks = ((int64_t)rows.cols + 31) / 32;
+    at::Tensor codes = bytes(*x, (int64_t)rows.rows, blocks * 16), scales = bytes(*x, (int64_t)rows.rows, (blocks + 15) / 16 * 16);
+    const sllm_mx q{codes.data_ptr(), scales.data_ptr(), rows.rows, rows.cols};
+    int32_t code;
+    {
+        pybind11::gil_scoped_release no_gil;
+        code = call(&rows, &q, (int32_t)device, stream);
+    }
+    if (code != SLLM_OK) return PyLong_FromLong(code);
+    auto c = pybind11::reinterpret_steal<pybind11::object>(THPVariable_Wrap(std::move(codes)));
+    auto s = pybind11::reinterpret_steal<pybind11::object>(THPVariable_Wrap(std::move(scales)));
+    return c && s ? PyTuple_Pack(2, c.ptr(), s.ptr()) : nullptr;
+    END_HANDLE_TH_ERRORS
+}
+
+// dequantize(call, q, codes, dtype, device, stream)
+inline PyObject* dequantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    SLLM_PY_ARGS(6, "dequantize(call, q, codes, dtype, device, stream)")
+    typedef int32_t (*Call)(const sllm_mx*, const sllm_matrix*, int32_t, void*);
+    const auto call = address<Call>(args[0]);
+    const auto* q = address<const sllm_mx*>(args[1]);
+    const long type = PyLong_AsLong(args[3]), device = PyLong_AsLong(args[4]);
+    void* const stream = PyLong_AsVoidPtr(args[5]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor* codes = tensor(args[2], device);
+    if (!codes || !q->rows || !q->cols) Py_RETURN_NONE;
+    sllm_matrix out_rows;
+    at::Tensor out = make(*codes, {(int64_t)q->rows, (int64_t)q->cols}, q->rows, (uint32_t)type, &out_rows);
+    int32_t code;
+    {
+        pybind11::gil_scoped_release no_gil;
+        code = call(q, &out_rows, (int32_t)device, stream);
+    }
+    return result(code, std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// lookup(call, table, codes, tokens, scale, dtype, device, stream): table a tensor
+// and codes None, or sllm_mx's address and its codes.
+inline PyObject* lookup(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    SLLM_PY_ARGS(8, "lookup(call, table, codes, tokens, scale, dtype, device, stream)")
+    typedef int32_t (*Call)(const void*, const sllm_ids*, float, const sllm_matrix*, int32_t, void*);
+    const bool mx = args[2] != Py_None;
+    const double scale = PyFloat_AsDouble(args[4]);
+    const long type = PyLong_AsLong(args[5]), device = PyLong_AsLong(args[6]);
+    void* const stream = PyLong_AsVoidPtr(args[7]);
+    const void* table = mx ? PyLong_AsVoidPtr(args[1]) : nullptr;
+    const auto call = address<Call>(args[0]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor *like = tensor(mx ? args[2] : args[1], device), *tokens = tensor(args[3], device);
+    sllm_matrix rows, out_rows;
+    sllm_ids ids;
+    if (!like || !tokens || !ids_of(*tokens, &ids)) Py_RETURN_NONE;
+    if (!mx) {
+        if (like->dim() != 2 || !rows_of(*like, &rows)) Py_RETURN_NONE;
+        table = &rows;
+    }
+    const uint64_t cols = mx ? static_cast<const sllm_mx*>(table)->cols : rows.cols;
+    if (!cols) Py_RETURN_NONE;
+    c10::SmallVector<int64_t, 4> shape(tokens->sizes().begin(), tokens->sizes().end());
+    shape.push_back((int64_t)cols);
+    at::Tensor out = make(*like, shape, ids.n, type < 0 ? rows.dtype : (uint32_t)type, &out_rows);
+    int32_t code;
+    {
+        pybind11::gil_scoped_release no_gil;
+        code = call(table, &ids, (float)scale, &out_rows, (int32_t)device, stream);
+    }
+    return result(code, std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// lookup_grad(call, workspace, dy, tokens, vocab, scale, dtype, device, stream)
+inline PyObject* lookup_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    SLLM_PY_ARGS(9, "lookup_grad(call, workspace, dy, tokens, vocab, scale, dtype, device, stream)")
+    typedef int32_t (*Call)(const sllm_matrix*, const sllm_ids*, float, uint32_t, const sllm_matrix*, void*, uint64_t, int32_t, void*);
+    typedef int32_t (*Workspace)(uint64_t, const sllm_matrix*, uint64_t*);
+    const auto call = address<Call>(args[0]);
+    const auto workspace = address<Workspace>(args[1]);
+    const long long vocab = PyLong_AsLongLong(args[4]);
+    const double scale = PyFloat_AsDouble(args[5]);
+    const long type = PyLong_AsLong(args[6]), device = PyLong_AsLong(args[7]);
+    void* const stream = PyLong_AsVoidPtr(args[8]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor *dy = tensor(args[2], device), *tokens = tensor(args[3], device);
+    sllm_matrix rows, out_rows;
+    sllm_ids ids;
+    if (!dy || !tokens || vocab < 1 || !rows_of(*dy, &rows) || !ids_of(*tokens, &ids) || rows.rows != ids.n) Py_RETURN_NONE;
+    at::Tensor out = make(*dy, {(int64_t)vocab, (int64_t)rows.cols}, (uint64_t)vocab, type < 0 ? rows.dtype : (uint32_t)type, &out_rows), ws;
+    int32_t code;
+    {
+        pybind11::gil_scoped_release no_gil;
+        uint64_t n = 0;
+        code = workspace(ids.n, &out_rows, &n);
+        if (code == SLLM_OK) {
+            if (n) ws = bytes(*dy, 1, (int64_t)n);
+            code = call(&rows, &ids, (float)scale, 0, &out_rows, n ? ws.data_ptr() : nullptr, n, (int32_t)device, stream);
+        }
+    }
+    return result(code, std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+#undef SLLM_PY_ARGS
+
+}  // namespace operators

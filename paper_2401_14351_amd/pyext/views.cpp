@@ -22,6 +22,7 @@
 #include <string>
 #include <vector>
 
+#include "operators.hpp"
 #include "sllm.h"
 
 namespace {
@@ -90,10 +91,20 @@ PyObject* build(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef kMethods[] = {{"build", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(build)), METH_FASTCALL,
-                           "build(buf, table, n, names_read) -> {name: view}"},
+typedef PyObject* (*Function)(PyObject*, PyObject* const*, Py_ssize_t);
+PyMethodDef method(const char* name, Function f, const char* what) {
+    return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, what};
+}
+
+PyMethodDef kMethods[] = {method("build", build, "build(buf, table, n, names_read) -> {name: view}"),
+                          method("product", operators::product, "x @ w.T or x @ w, w in MX FP4"),
+                          method("product_mx", operators::product_mx, "x @ w.T, both in MX FP4"),
+                          method("quantize", operators::quantize, "x in MX FP4: (codes, scales)"),
+                          method("dequantize", operators::dequantize, "what an MX FP4 matrix stands for"),
+                          method("lookup", operators::lookup, "rows of a table by token"),
+                          method("lookup_grad", operators::lookup_grad, "the gradient of a lookup by its table"),
                           {nullptr, nullptr, 0, nullptr}};
-PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_views", "Views over a loaded buffer.", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_views", "Views over a loaded buffer, and calls of the operators on it.", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 

@@ -591,6 +591,50 @@ def test_graph_replays(m):
             assert torch.equal(a, b)
 
 
+def test_calls_in_python(monkeypatch):
+    """The calls that the extension does not make, and all of them without it, have the same results and refusals."""
+    w, _ = random_mx4(130, 96, 41)
+    ids = some_ids(300, 50, torch.int64, 42)
+    table = normal((50, 96), torch.float16, 43)
+    x, dy = normal((2, 3, 96), torch.bfloat16, 44), normal((2, 3, 130), torch.float32, 45)
+    wide = normal((6, 200), torch.bfloat16, 46)
+
+    def results():
+        q = op.mx4_quantize(x)
+        yield q.codes
+        yield q.scales
+        yield op.mx4_dequantize(q, torch.float16)
+        yield op.mx4_linear(x, w)
+        yield op.mx4_linear(x, w, out_dtype=torch.float32)
+        yield op.mx4_linear(x[0, 0], w)
+        yield op.mx4_linear(wide[:, 7:103], w)
+        yield op.mx4_linear(q, w)
+        yield op.mx4_linear_grad(dy, w, out_dtype=torch.float16)
+        yield op.embedding(table, ids, scale=0.5)
+        yield op.embedding(table, ids.view(20, 15).int())
+        yield op.embedding(w, ids, out_dtype=torch.float32)
+        yield op.embedding_grad(normal((300, 96), torch.float32, 47), ids, 50, scale=2.0, out_dtype=torch.bfloat16)
+        yield op.mx4_linear(x[:, :0], w)
+
+    def refusals():
+        for call in (lambda: op.mx4_linear(x[..., :64], w), lambda: op.mx4_linear(x.transpose(0, 2), w),
+                     lambda: op.mx4_linear(x, w, out_dtype=torch.float64), lambda: op.mx4_linear(x.double(), w),
+                     lambda: op.mx4_linear(x.cpu(), w), lambda: op.mx4_quantize(x.double()),
+                     lambda: op.mx4_dequantize(w, torch.int8), lambda: op.embedding(table, ids.float()),
+                     lambda: op.embedding(table, ids.cpu()), lambda: op.embedding(x, ids),
+                     lambda: op.embedding_grad(dy, ids, 50), lambda: op.mx4_linear_grad(x, w)):
+            with pytest.raises((ValueError, binding.SllmError)) as e:
+                call()
+            yield str(e.value)
+
+    assert op._native() is not None
+    native, said = list(results()), list(refusals())
+    monkeypatch.setattr(op, "_native", lambda: None)
+    for a, b in zip(native, list(results()), strict=True):
+        assert a.dtype == b.dtype and a.shape == b.shape and torch.equal(a, b)
+    assert said == list(refusals())
+
+
 def test_refusals():
     w, _ = random_mx4(64, 96, 1)
     x = normal((4, 96), torch.bfloat16, 2)
