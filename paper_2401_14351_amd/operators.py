@@ -167,8 +167,12 @@ def _on_stream(stream, operator, *args, keep=(), **kwargs):
     """Run ``operator`` with ``stream`` current: what it allocates then belongs to
     that stream, and its inputs are kept from reuse until it has passed the call."""
     device = keep[0].device
+    if device.type != "cuda":
+        return operator(*args, **kwargs)  # which says so
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(stream, device=device)
+    elif stream.device != device:
+        raise ValueError(f"a stream of {stream.device} for inputs on {device}")
     with torch.cuda.stream(stream):
         result = operator(*args, **kwargs)
     for t in keep:
