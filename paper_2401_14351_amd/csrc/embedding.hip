@@ -71,9 +71,9 @@ __device__ __forceinline__ void store8(T* row, uint32_t c, uint32_t dim, const f
 
 // out[i] = scale table[ids[i]], the product in 32 bits.  Eight columns a lane,
 // `lanes` of them a row at a time: 16 bytes a store, and of a row in MX FP4 a word
-// of codes.  Bound by memory, which the output is most of: 8191 rows of 8192
-// columns from MX FP4 to bfloat16 25 us, 6.7 TB/s; 16 rows are bound by their two
-// loads one after the other, 3.2 us.  S: the table's elements, void for MX FP4.
+// of codes.  Bound by memory: 8191 rows of 8192 columns from bfloat16 54 us, 5.0
+// TB/s, from MX FP4 36 us, 4.7 TB/s (25 where the last-level cache has the table);
+// 16 rows are bound by their two loads one after the other, 2.9 us.  S: the table's elements, void for MX FP4.
 // Vec: rows start on 16 bytes and end on a multiple of eight columns.
 template <bool Vec, typename S, typename T>
 __global__ __launch_bounds__(256) void lookup(Lookup a, T* out) {
@@ -81,25 +81,45 @@ __global__ __launch_bounds__(256) void lookup(Lookup a, T* out) {
     if (i >= a.n) return;
     const int64_t row = a.ids.p ? id_at(a.ids, i, a.vocab) : (int64_t)i;
     const uint32_t blocks = (a.dim + 31) / 32, pitch = (blocks + 15) / 16 * 16;
-    for (uint32_t c = threadIdx.x % a.lanes * 8; c < a.dim; c += a.lanes * 8) {
-        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    // A word of codes a lane does not fill the memory's latency: several are under way
+    // (8191 rows of 8192 36 us, one at a time 43).
+    constexpr uint32_t kTogether = __is_same(S, void) ? 4 : 1;
+    for (uint32_t c0 = threadIdx.x % a.lanes * 8; c0 < a.dim; c0 += kTogether * a.lanes * 8) {
+        float v[kTogether][8] = {};
         if (row >= 0) {
             if constexpr (__is_same(S, void)) {
-                const uint32_t codes = *reinterpret_cast<const uint32_t*>(a.table.codes + (uint64_t)row * blocks * 16 + c / 2);
-                const float scale = mx_scale(a.table.scales[(uint64_t)row * pitch + c / 32]);
-                const f32x2 two[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0),
-                                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1),
-                                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2),
-                                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3)};
+                uint32_t codes[kTogether] = {}, scales[kTogether] = {};
 #pragma unroll
-                for (uint32_t e = 0; e < 8; ++e) v[e] = two[e / 2][e % 2];
+                for (uint32_t u = 0; u < kTogether; ++u) {
+                    if (u * a.lanes * 8 >= a.dim) break;  // short rows have none of these
+                    const uint32_t c = min(c0 + u * a.lanes * 8, a.dim - 1) & ~7u;
+                    codes[u] = *reinterpret_cast<const uint32_t*>(a.table.codes + (uint64_t)row * blocks * 16 + c / 2);
+                    scales[u] = a.table.scales[(uint64_t)row * pitch + c / 32];
+                }
+#pragma unroll
+                for (uint32_t u = 0; u < kTogether; ++u) {
+                    const float scale = mx_scale(scales[u]);
+                    const f32x2 two[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], scale, 0),
+                                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], scale, 1),
+                                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], scale, 2),
+                                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], scale, 3)};
+#pragma unroll
+                    for (uint32_t e = 0; e < 8; ++e) v[u][e] = two[e / 2][e % 2];
+                }
             } else {
-                load8<Vec>(static_cast<const S*>(a.table.data) + (uint64_t)row * a.table.stride, c, a.dim, v);
+#pragma unroll
+                for (uint32_t u = 0; u < kTogether; ++u)
+                    load8<Vec>(static_cast<const S*>(a.table.data) + (uint64_t)row * a.table.stride, c0, a.dim, v[u]);
             }
         }
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) v[e] *= a.scale;
-        store8<Vec>(out + i * a.out_stride, c, a.dim, v);
+        for (uint32_t u = 0; u < kTogether; ++u) {
+            const uint32_t c = c0 + u * a.lanes * 8;
+            if (c >= a.dim) break;
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e) v[u][e] *= a.scale;
+            store8<Vec>(out + i * a.out_stride, c, a.dim, v[u]);
+        }
     }
 }
 

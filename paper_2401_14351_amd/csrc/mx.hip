@@ -32,8 +32,9 @@ __device__ __forceinline__ float quad(float x) {
 }
 
 // x is read once and its 4.25 bits a value written once; bound by memory (11008
-// x 4096 in bfloat16, 90 MB in and 24 MB out, in 18.4 us: 6.2 TB/s).  Four lanes a
-// block, eight columns each: a lane's loads are 16 bytes wide, neighbours' codes
+// x 4096 in bfloat16, 90 MB in and 24 MB out, in 23.6 us, 4.8 TB/s; in 18.4 where
+// the last-level cache still has x; two loads a lane under way take 25.8).  Four
+// lanes a block, eight columns each: a lane's loads are 16 bytes wide, neighbours' codes
 // are neighbouring words, and a block's largest magnitude is two lane exchanges
 // away.  Elements are rounded to nearest even by the conversion instruction.
 // `lanes` of them take a row at a time.  Vec: rows start on 16 bytes and end on a
