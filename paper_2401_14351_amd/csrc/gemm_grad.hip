@@ -92,7 +92,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
         const bool inside = (uint64_t)(t / a.parts) * kStep + w_row < a.w_rows;
         float scale = mx_scale(inside ? scales[from] : 0);
         if constexpr (__is_same(W, _Float16)) {
-            scale *= 1 << kHalfShift;
+            scale = half_scale(inside ? scales[from] : 0);
 #pragma unroll
             for (uint32_t w = 0; w < kWords; ++w) beyond |= (uint32_t)inside & beyond_half(scales[from], codes[from][w]);
         }

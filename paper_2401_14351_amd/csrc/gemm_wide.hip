@@ -103,7 +103,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
             w.scale[n] = mx_scale(inside ? s : 0);
             if constexpr (__is_same(decltype(type), _Float16)) {
                 const u32x4 c = w.codes[n];
-                w.scale[n] *= 1 << kHalfShift;
+                w.scale[n] = half_scale(inside ? s : 0);
                 beyond |= (uint32_t)(inside && t < t1) & beyond_half(s, c[0] | c[1] | c[2] | c[3]);
             }
         }

@@ -174,6 +174,10 @@ __device__ __forceinline__ f32x16 product(u32x4 w, u32x4 x, f32x16 acc) {
 constexpr int kHalfShift = 8;
 constexpr uint32_t kHalfScale = 127 - 31, kHalfScales = 37;
 
+// A block's scale for its values in float16, times 2^kHalfShift.  A block of zeros may
+// have any scale: those that the sum would make infinite stay finite, and zeros zeros.
+__device__ __forceinline__ float half_scale(uint32_t byte) { return mx_scale(min(byte, 254u - kHalfShift) + kHalfShift); }
+
 __device__ __forceinline__ uint32_t beyond_half(uint32_t scale, uint32_t codes) {
     return (uint32_t)(scale - kHalfScale >= kHalfScales) & ((uint32_t)(scale == 255) | (uint32_t)((codes & 0x77777777) != 0));
 }
