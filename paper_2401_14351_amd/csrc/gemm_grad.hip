@@ -32,6 +32,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
     // into one do not touch what is read from another.
     __shared__ __align__(16) uint8_t x0[kXBytes], x1[kXBytes];
     __shared__ __align__(16) uint8_t w0[kWBytes], w1[kWBytes];
+    __shared__ uint32_t marks[kHalf ? kMarkWords : 1];  // stages with blocks of W that are added afterwards
     uint8_t* const x_ring[2] = {x0, x1};
     uint8_t* const w_ring[2] = {w0, w1};
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -86,18 +87,23 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
 #pragma unroll
     for (uint32_t w = 0; w < kWords; ++w)
         w_to[w] = opaque(w_row * kPitch + w_block * 64 + ((w_part * kWords + w) ^ (w_block & 3)) * 16);
-    uint32_t beyond = 0;  // scales that float16 does not hold
-    auto store_w = [&](uint32_t t, int from, uint8_t* to, auto type) SLLM_INLINE {
+    auto store_w = [&](uint32_t t, int from, uint8_t* to, auto type, bool beyond_only) SLLM_INLINE {
         typedef decltype(type) W;
         const bool inside = (uint64_t)(t / a.parts) * kStep + w_row < a.w_rows;
-        float scale = mx_scale(inside ? scales[from] : 0);
-        if constexpr (__is_same(W, _Float16)) {
-            scale = half_scale(inside ? scales[from] : 0);
+        const uint32_t s = inside ? scales[from] : 0;
+        const float scale = __is_same(W, _Float16) ? half_scale(s) : mx_scale(s);
+        bool left_out = false;
 #pragma unroll
-            for (uint32_t w = 0; w < kWords; ++w) beyond |= (uint32_t)inside & beyond_half(scales[from], codes[from][w]);
+        for (uint32_t w = 0; w < kWords; ++w) {
+            uint32_t c = codes[from][w];
+            if constexpr (kHalf) {
+                const bool beyond = inside & beyond_half(s, c);
+                if (__is_same(W, _Float16) ? beyond : beyond_only && !beyond) c = 0;
+                left_out |= beyond;
+            }
+            lds_write(to, w_to[w], expand8<W>(c, scale));
         }
-#pragma unroll
-        for (uint32_t w = 0; w < kWords; ++w) lds_write(to, w_to[w], expand8<W>(codes[from][w], scale));
+        if (__is_same(W, _Float16) && __any(left_out)) mark_stage(marks, t);
     };
 
     // (Filled through a reference: a returned structure makes its reads' alias
@@ -128,19 +134,26 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
 #pragma unroll
         for (int m = 0; m < FM; ++m) f.x[m] = lds_read<u32x4>(x_now, (x_from ^ s * 16) + m * 4096);
     };
-    uint32_t met[FM] = {};  // the bits of x's rows
-    auto multiply = [&](const Fragments& f) SLLM_INLINE {
-        if constexpr (kHalf)
+    bool fits = true;  // this lane's rows of x
+    _Float16 factor[FM];
+    float unit[FM];
+    if constexpr (kHalf)
 #pragma unroll
-            for (int m = 0; m < FM; ++m) {
-                met[m] |= f.x[m][0] | f.x[m][1] | f.x[m][2] | f.x[m][3];
-                asm volatile("" : "+v"(met[m]));  // now, not when all of the depth has been read
-            }
+        for (int m = 0; m < FM; ++m) {
+            const uint32_t range = a.ranges[min(m0 + (wm * FM + m) * 32 + r, a.m - 1)];
+            fits &= row_fits(range);
+            factor[m] = (_Float16)(float)(1 << row_shift(range));
+            unit[m] = 1.0f / (1 << (row_shift(range) + kHalfShift));
+        }
+    auto multiply = [&](const Fragments& f) SLLM_INLINE {
+        u32x4 x[FM];
+#pragma unroll
+        for (int m = 0; m < FM; ++m) x[m] = kHalf ? __builtin_bit_cast(u32x4, __builtin_bit_cast(f16x8, f.x[m]) * factor[m]) : f.x[m];
         pin(acc);
 #pragma unroll
         for (int m = 0; m < FM; ++m)
 #pragma unroll
-            for (int n = 0; n < FN; ++n) acc[n][m] = product<X>(f.w[n], f.x[m], acc[n][m]);
+            for (int n = 0; n < FN; ++n) acc[n][m] = product<X>(f.w[n], x[m], acc[n][m]);
         pin(acc);
     };
     // While one step is multiplied the next is read; the next stage's first step
@@ -155,7 +168,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
         read(f0, here, w_ring[i], 2);
         multiply(f1);
         read(f1, here, w_ring[i], 3);
-        store_w(t + 1, i ^ 1, w_ring[i ^ 1], X());
+        store_w(t + 1, i ^ 1, w_ring[i ^ 1], X(), false);
         multiply(f0);
         wait_but_loads<0>();
         barrier();
@@ -164,11 +177,15 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
         read(f0, x_ring[i ^ 1], w_ring[i ^ 1], 0);
         multiply(f1);
     };
+    if constexpr (kHalf) {
+        if (tid < kMarkWords) marks[tid] = 0;
+        __syncthreads();  // before the first piece of W may mark its stage
+    }
     if (t0 < t1) {
         load_w(t0, 0);
         load_w(t0 + 1, 1);
         load_x(t0, x0);
-        store_w(t0, 0, w0, X());
+        store_w(t0, 0, w0, X(), false);
         wait_but_loads<0>();
         barrier();
         load_w(t0 + 2, 0);
@@ -182,39 +199,34 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void grad_product(WideArgs a, T* ou
 
     __syncthreads();  // the last stage's reads are done
     if constexpr (kHalf) {
+        const bool again = __syncthreads_or(!fits);
 #pragma unroll
-        for (int m = 0; m < FM; ++m) beyond |= all_subnormal(met[m]);
-        if (__syncthreads_or(beyond)) {
+        for (int n = 0; n < FN; ++n)
 #pragma unroll
-            for (int n = 0; n < FN; ++n)
+            for (int m = 0; m < FM; ++m) acc[n][m] = again ? f32x16{} : acc[n][m] * unit[m];
+        // All of W again, or what was left out of it.  With nothing to overlap, a stage
+        // takes four times what it takes above.
+        for (uint32_t t = t0; t < t1; ++t) {
+            if (!again && !marked(marks, t)) continue;
+            load_x(t, x0);
+            load_w(t, 0);
+            store_w(t, 0, w0, __bf16(), !again);
+            wait_but_loads<0>();
+            barrier();
 #pragma unroll
-                for (int m = 0; m < FM; ++m) acc[n][m] = f32x16{};
-            for (uint32_t t = t0; t < t1; ++t) {
-                load_x(t, x0);
-                load_w(t, 0);
-                store_w(t, 0, w0, __bf16());
-                wait_but_loads<0>();
-                barrier();
+            for (uint32_t s = 0; s < 4; ++s) {
+                read(f0, x0, w0, s);
 #pragma unroll
-                for (uint32_t s = 0; s < 4; ++s) {
-                    read(f0, x0, w0, s);
+                for (int m = 0; m < FM; ++m) {
+                    u32x4 hi, lo;
+                    split_half(f0.x[m], hi, lo);
 #pragma unroll
-                    for (int m = 0; m < FM; ++m) {
-                        u32x4 hi, lo;
-                        split_half(f0.x[m], hi, lo);
-#pragma unroll
-                        for (int n = 0; n < FN; ++n)
-                            acc[n][m] = product<__bf16>(f0.w[n], lo, product<__bf16>(f0.w[n], hi, acc[n][m]));
-                        pin(acc);
-                    }
+                    for (int n = 0; n < FN; ++n)
+                        acc[n][m] = product<__bf16>(f0.w[n], lo, product<__bf16>(f0.w[n], hi, acc[n][m]));
+                    pin(acc);
                 }
-                __syncthreads();
             }
-        } else {
-#pragma unroll
-            for (int n = 0; n < FN; ++n)
-#pragma unroll
-                for (int m = 0; m < FM; ++m) acc[n][m] *= 1.0f / (1 << kHalfShift);
+            __syncthreads();
         }
     }
     // the output goes through the stages' buffers, a part of one for each wave

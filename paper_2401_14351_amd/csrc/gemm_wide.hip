@@ -35,6 +35,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
     // two stages each.
     __shared__ __align__(16) uint8_t x0[kXBytes], x1[kXBytes];
     __shared__ __align__(16) uint8_t w0[kWBytes + kScaleBytes], w1[kWBytes + kScaleBytes];
+    __shared__ uint32_t marks[kHalf ? kMarkWords : 1];  // stages with blocks of W that are added afterwards
     uint8_t* const x_ring[2] = {x0, x1};
     uint8_t* const w_ring[2] = {w0, w1};
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -93,20 +94,27 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
         float scale[FN];
     };
     const uint32_t w_from = opaque(wn * FN * 2048 + short_chunk_at(r, h)), scale_from = opaque(kWBytes + wn * FN * 128 + r * 4 + h);
-    uint32_t beyond = 0;  // scales that float16 does not hold
-    auto read_w = [&](Weight& w, uint32_t t, const uint8_t* from, uint32_t odd, auto type) SLLM_INLINE {
+    auto read_w = [&](Weight& w, uint32_t t, const uint8_t* from, uint32_t odd, auto type, bool beyond_only) SLLM_INLINE {
         const bool inside = (uint64_t)(t % a.steps) * 2 + h < a.w_blocks;  // scale bytes past the row's end may hold anything
+        bool left_out = false;
 #pragma unroll
         for (int n = 0; n < FN; ++n) {
             w.codes[n] = lds_read<u32x4>(from, (w_from ^ odd * 32) + n * 2048);
-            const uint8_t s = lds_read<uint8_t>(from, scale_from + n * 128 + odd * 2);
-            w.scale[n] = mx_scale(inside ? s : 0);
-            if constexpr (__is_same(decltype(type), _Float16)) {
+            const uint8_t read = lds_read<uint8_t>(from, scale_from + n * 128 + odd * 2), s = inside ? read : 0;
+            w.scale[n] = mx_scale(s);
+            if constexpr (kHalf) {
                 const u32x4 c = w.codes[n];
-                w.scale[n] = half_scale(inside ? s : 0);
-                beyond |= (uint32_t)(inside && t < t1) & beyond_half(s, c[0] | c[1] | c[2] | c[3]);
+                const bool beyond = inside & beyond_half(s, c[0] | c[1] | c[2] | c[3]);
+                if constexpr (__is_same(decltype(type), _Float16)) {
+                    w.scale[n] = half_scale(s);
+                    left_out |= beyond;
+                    w.codes[n] = beyond ? u32x4{0, 0, 0, 0} : c;
+                } else {
+                    w.codes[n] = beyond_only && !beyond ? u32x4{0, 0, 0, 0} : c;
+                }
             }
         }
+        if (__is_same(decltype(type), _Float16) && __any(left_out)) mark_stage(marks, t);
     };
 
     struct Fragments {
@@ -121,19 +129,26 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
 #pragma unroll
         for (int n = 0; n < FN; ++n) f.w[n] = expand8<X>(w.codes[n][s], w.scale[n]);
     };
-    uint32_t met[FM] = {};  // the bits of x's rows
-    auto multiply = [&](const Fragments& f) SLLM_INLINE {
-        if constexpr (kHalf)
+    bool fits = true;  // this lane's rows of x
+    _Float16 factor[FM];
+    float unit[FM];
+    if constexpr (kHalf)
 #pragma unroll
-            for (int m = 0; m < FM; ++m) {
-                met[m] |= f.x[m][0] | f.x[m][1] | f.x[m][2] | f.x[m][3];
-                asm volatile("" : "+v"(met[m]));  // now, not when all of the depth has been read
-            }
+        for (int m = 0; m < FM; ++m) {
+            const uint32_t range = a.ranges[min(m0 + (wm * FM + m) * 32 + r, a.m - 1)];
+            fits &= row_fits(range);
+            factor[m] = (_Float16)(float)(1 << row_shift(range));
+            unit[m] = 1.0f / (1 << (row_shift(range) + kHalfShift));
+        }
+    auto multiply = [&](const Fragments& f) SLLM_INLINE {
+        u32x4 x[FM];
+#pragma unroll
+        for (int m = 0; m < FM; ++m) x[m] = kHalf ? __builtin_bit_cast(u32x4, __builtin_bit_cast(f16x8, f.x[m]) * factor[m]) : f.x[m];
         pin(acc);
 #pragma unroll
         for (int m = 0; m < FM; ++m)
 #pragma unroll
-            for (int n = 0; n < FN; ++n) acc[n][m] = product<X>(f.w[n], f.x[m], acc[n][m]);
+            for (int n = 0; n < FN; ++n) acc[n][m] = product<X>(f.w[n], x[m], acc[n][m]);
         pin(acc);
     };
     // While one step is multiplied the next is read; the next stage's first step
@@ -156,12 +171,13 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
         multiply(f0);
         wait_but_loads<0>();
         barrier();
-        read_w(now, t + 1, w_ring[(i + 1) / 2 % 2], (i + 1) % 2, X());
+        read_w(now, t + 1, w_ring[(i + 1) / 2 % 2], (i + 1) % 2, X(), false);
         if (t + 2 < t1) load_x(t + 2, here);
         if (i % 2 && t + 3 < t1) load_w(t + 3, w_ring[i / 2]);
         read(f0, x_ring[(i + 1) % 2], now, S0());
         multiply(f1);
     };
+    if (kHalf && tid < kMarkWords) marks[tid] = 0;  // a barrier before the first piece of W is read
     if (t0 < t1) {
         load_w(t0, w0);
         load_x(t0, x0);
@@ -169,7 +185,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
         barrier();
         load_x(t0 + 1, x1);
         if (t0 + 2 < t1) load_w(t0 + 2, w1);
-        read_w(now, t0, w0, 0, X());
+        read_w(now, t0, w0, 0, X(), false);
         read(f0, x0, now, S0());
         for (uint32_t t = t0; t < t1; t += 4) {
             stage(t, S0());
@@ -183,39 +199,34 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
 
     __syncthreads();  // the last stage's reads are done
     if constexpr (kHalf) {
+        const bool again = __syncthreads_or(!fits);
 #pragma unroll
-        for (int m = 0; m < FM; ++m) beyond |= all_subnormal(met[m]);
-        if (__syncthreads_or(beyond)) {
+        for (int n = 0; n < FN; ++n)
 #pragma unroll
-            for (int n = 0; n < FN; ++n)
+            for (int m = 0; m < FM; ++m) acc[n][m] = again ? f32x16{} : acc[n][m] * unit[m];
+        // All of W again, or what was left out of it.  With nothing to overlap, a stage
+        // takes four times what it takes above.
+        for (uint32_t t = t0; t < t1; ++t) {
+            if (!again && !marked(marks, t)) continue;
+            load_w(t & ~1u, w0);
+            load_x(t, x0);
+            wait_but_loads<0>();
+            barrier();
+            read_w(now, t, w0, t % 2, __bf16(), !again);
 #pragma unroll
-                for (int m = 0; m < FM; ++m) acc[n][m] = f32x16{};
-            for (uint32_t t = t0; t < t1; ++t) {
-                if (t % 2 == 0) load_w(t, w0);
-                load_x(t, x0);
-                wait_but_loads<0>();
-                barrier();
-                read_w(now, t, w0, t % 2, __bf16());
+            for (int s = 0; s < 4; ++s)
 #pragma unroll
-                for (int s = 0; s < 4; ++s)
+                for (int m = 0; m < FM; ++m) {
+                    u32x4 hi, lo;
+                    split_half(lds_read<u32x4>(x0, (x_from ^ s * 16) + m * 4096), hi, lo);
 #pragma unroll
-                    for (int m = 0; m < FM; ++m) {
-                        u32x4 hi, lo;
-                        split_half(lds_read<u32x4>(x0, (x_from ^ s * 16) + m * 4096), hi, lo);
-#pragma unroll
-                        for (int n = 0; n < FN; ++n) {
-                            const u32x4 w = expand8(now.codes[n][s], now.scale[n]);
-                            acc[n][m] = product<__bf16>(w, lo, product<__bf16>(w, hi, acc[n][m]));
-                        }
-                        pin(acc);
+                    for (int n = 0; n < FN; ++n) {
+                        const u32x4 w = expand8(now.codes[n][s], now.scale[n]);
+                        acc[n][m] = product<__bf16>(w, lo, product<__bf16>(w, hi, acc[n][m]));
                     }
-                __syncthreads();
-            }
-        } else {
-#pragma unroll
-            for (int n = 0; n < FN; ++n)
-#pragma unroll
-                for (int m = 0; m < FM; ++m) acc[n][m] *= 1.0f / (1 << kHalfShift);
+                    pin(acc);
+                }
+            __syncthreads();
         }
     }
     // the output goes through the stages' buffers, a part of one for each wave

@@ -124,15 +124,17 @@ struct Plan {
     uint32_t tile_m = 0, tile_n = 0, steps = 0, splits = 1;
     uint32_t tiles_m = 0, tiles_j = 0;
     uint64_t x_bytes = 0, split_stride = 0, bytes = 0;
+    bool half = false;         // x is multiplied in float16, by the ranges of its rows,
+    uint64_t ranges_at = 0;    // which are here in the workspace
 };
 
 // Whether a product goes to the kernel of few rows.  It reads all of x for every
 // 16 columns of the output, in registers and without a launch more, so it gains
 // where rows and columns are few; measured in us here and by tiles, W 11008 x 4096
 // unless said: bfloat16 5 rows 12.5 and 15.7, 8 rows 14.1 and 15.9, 16 rows 17.8 and
-// 16.4, 16 rows by 32000 x 4096 42 and 30; float16 16 rows by 4096 x 4096 9.6 and
-// 12.6, 5 rows 19.1 and 16.9; float 16 rows 31 and 34, 16 rows by 32000 x 4096 71 and
-// 67; MX FP4 16 rows 11.3 and 15.2, 32 rows 17.1 and 15.6.
+// 16.4, 16 rows by 32000 x 4096 42 and 30; float16 5 rows 17.2 and 18.1, 16 rows 20.1
+// and 19.0, 16 rows by 16384 x 4096 25.2 and 21.5; float 16 rows 31 and 34, 16 rows by
+// 32000 x 4096 71 and 67; MX FP4 16 rows 11.3 and 15.2, 32 rows 17.1 and 15.6.
 bool few_rows(const LinearLaunch& a) {
     if (a.grad) return false;
     if (a.x.codes) return a.m <= 32 && a.m * a.n <= 1 << 18;
@@ -189,6 +191,9 @@ Plan plan_linear(const LinearLaunch& a) {
     if (p.staged) p.x_bytes = (a.m * p.parts * p.part_stride * 2 + 255) / 256 * 256;
     p.split_stride = a.m * ((p.cols + 3) / 4 * 4);
     p.bytes = p.x_bytes + (p.splits > 1 ? p.splits * p.split_stride * 4 : 0);
+    p.half = !a.x.codes && a.x.dtype == SLLM_DTYPE_F16;
+    p.ranges_at = p.bytes;
+    if (p.half) p.bytes += a.m * 4;
     return p;
 }
 
@@ -218,6 +223,48 @@ __global__ __launch_bounds__(256) void split_x(const T* x, uint64_t stride, uint
         for (int j = 0; j < 4; ++j) o[j] = v[p][2 * j] | (uint32_t)v[p][2 * j + 1] << 16;
         *reinterpret_cast<u32x4*>(out + (row * Parts + p) * pitch + c) = o;
     }
+}
+
+// The range of each row of a float16 x (products.hpp says of what), a wave each, or where
+// rows are long a workgroup.  Vec: rows start on 16 bytes.
+template <bool Vec, int Lanes>
+__global__ __launch_bounds__(256) void find_ranges(const uint16_t* x, uint64_t stride, uint64_t rows, uint64_t cols, uint32_t* ranges) {
+    __shared__ uint32_t waves[2][4];
+    const uint64_t row = (uint64_t)blockIdx.x * (256 / Lanes) + threadIdx.x / Lanes;
+    const uint16_t* at = x + min(row, rows - 1) * stride;
+    uint32_t top = 0, bottom = 0xffff;
+    for (uint64_t c = threadIdx.x % Lanes * 8; c < cols; c += Lanes * 8) {
+        uint16_t e[8];
+        if (Vec && c + 8 <= cols) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(at + c);
+            __builtin_memcpy(e, &v, sizeof e);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? at[c + i] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t size = e[i] & 0x7fff;
+            top = max(top, size);
+            bottom = min(bottom, (size - 1) & 0xffff);
+        }
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) {
+        top = max(top, (uint32_t)__shfl_xor(top, d));
+        bottom = min(bottom, (uint32_t)__shfl_xor(bottom, d));
+    }
+    if constexpr (Lanes > 64) {
+        const uint32_t wave = threadIdx.x / 64;
+        if (threadIdx.x % 64 == 0) waves[0][wave] = top, waves[1][wave] = bottom;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            top = max(top, waves[0][w]);
+            bottom = min(bottom, waves[1][w]);
+        }
+    }
+    if (threadIdx.x % Lanes == 0 && row < rows) ranges[row] = bottom << 16 | top;
 }
 
 // The sum of the splits' matrices, first to last, so that every call adds in the
@@ -269,6 +316,17 @@ int32_t stage_x(const LinearLaunch& a, const Plan& p, void* workspace, WideArgs*
     return SLLM_OK;
 }
 
+int32_t launch_ranges(const LinearLaunch& a, const Plan& p, uint32_t* ranges, hipStream_t stream) {
+    const uint16_t* x = static_cast<const uint16_t*>(a.x.data);
+    const bool vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && (a.m == 1 || a.x.stride % 8 == 0), wide = p.depth > 1024;
+    uint32_t blocks;
+    SLLM_TRY(grid_of(a.m * (wide ? 256 : 64), &blocks));
+    const auto kernel = vec ? (wide ? find_ranges<true, 256> : find_ranges<true, 64>) : (wide ? find_ranges<false, 256> : find_ranges<false, 64>);
+    kernel<<<blocks, 256, 0, stream>>>(x, a.x.stride, a.m, p.depth, ranges);
+    SLLM_HIP(hipGetLastError());
+    return SLLM_OK;
+}
+
 int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipStream_t stream) {
     OutArgs o{a.m, p.cols, a.out_stride, 0, 0};
     void* out = a.out;
@@ -287,6 +345,9 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
     } else {
         WideArgs w;
         SLLM_TRY(stage_x(a, p, workspace, &w, stream));
+        uint32_t* ranges = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + p.ranges_at);
+        if (p.half) SLLM_TRY(launch_ranges(a, p, ranges, stream));
+        w.ranges = ranges;
         w.m = a.m, w.depth = p.depth;
         w.parts = p.parts, w.steps = p.steps;
         w.w_codes = reinterpret_cast<const u32x4*>(a.w_codes);
@@ -294,8 +355,7 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
         w.w_rows = a.n, w.w_blocks = mx_blocks(a.k), w.w_scale_pitch = mx_scale_pitch(a.k);
         w.tiles_m = p.tiles_m, w.tiles_j = p.tiles_j;
         w.out_args = o;
-        const bool half = a.x.dtype == SLLM_DTYPE_F16;
-        SLLM_TRY((a.grad ? launch_grad : launch_wide)(w, half, p.tile_m, p.splits, out, dtype, stream));
+        SLLM_TRY((a.grad ? launch_grad : launch_wide)(w, p.half, p.tile_m, p.splits, out, dtype, stream));
     }
     return p.splits > 1 ? join(p, static_cast<const float*>(out), p.splits, a, stream) : SLLM_OK;
 }

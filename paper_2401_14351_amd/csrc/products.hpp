@@ -21,6 +21,7 @@ struct WideArgs {
     uint64_t m, depth;       // of a part
     uint64_t x_stride, part_stride;
     uint32_t parts, steps;   // steps of a part, an even number
+    const uint32_t* ranges;  // of the rows of a float16 x
     const u32x4* w_codes;
     const uint8_t* w_scales;
     uint64_t w_rows, w_blocks, w_scale_pitch;
@@ -163,29 +164,46 @@ __device__ __forceinline__ f32x16 product(u32x4 w, u32x4 x, f32x16 acc) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, w), __builtin_bit_cast(f16x8, x), acc, 0, 0, 0);
 }
 
-// An x in float16 is multiplied as it is, by W in float16 too, times 2^kHalfShift:
-// exact for scales of 2^-31 to 2^5, so for values from 2^-32 to 192.  The matrix
-// instruction adds products of a subnormal (below 2^-14) as if they were of 2^-14:
-// it drops their bits under 2^-24 of that.  A workgroup that has met another scale,
-// other than over zeros, or a row of x with nothing but subnormals starts again
-// with W and two parts of x in bfloat16, which hold all of them.  4096 x 8192 by
-// 8192 takes 519 us, as two parts throughout 935, where every workgroup starts
-// again 2000.
+// An x in float16 is multiplied in float16, W times 2^kHalfShift and x's rows times a
+// power of two each, so that every operand is zero or a normal number.  The matrix
+// instruction adds products of a subnormal (below 2^-14) as if it were 2^-14 and drops
+// what is 24 bits under that, of the sum so far too: with subnormals let in, sums of small
+// products were off by up to 12 times what 32 bits allow.
+//   * Blocks of W whose scale is not 2^-21 to 2^5 (values of 2^-22 to 192), other than
+//     zeros, are left out, their stages marked, and added afterwards in bfloat16, x in
+//     two parts.
+//   * A row of x is multiplied by up to 2^10, which makes 2^-24, the smallest element, a
+//     normal number, but by no more than its largest element allows (a kernel before
+//     finds both).  Where a row has elements more than 2^29 apart, or an infinity or a
+//     NaN, its workgroups take all stages in bfloat16.
+// 4096 x 8192 by 8192 takes 507 us (a bfloat16 x 410), 518 with a block left out in every
+// tile, 2100 where every tile has such a row or leaves all of W out; 64 rows by 4096 x
+// 4096 18.2 (13.6), of which 4 are the kernel before.
 constexpr int kHalfShift = 8;
-constexpr uint32_t kHalfScale = 127 - 31, kHalfScales = 37;
+constexpr uint32_t kHalfScale = 127 - 21, kHalfScales = 27;
 
 // A block's scale for its values in float16, times 2^kHalfShift.  A block of zeros may
 // have any scale: those that the sum would make infinite stay finite, and zeros zeros.
 __device__ __forceinline__ float half_scale(uint32_t byte) { return mx_scale(min(byte, 254u - kHalfShift) + kHalfShift); }
 
-__device__ __forceinline__ uint32_t beyond_half(uint32_t scale, uint32_t codes) {
-    return (uint32_t)(scale - kHalfScale >= kHalfScales) & ((uint32_t)(scale == 255) | (uint32_t)((codes & 0x77777777) != 0));
+// Whether a block, or some of its codes, is left out.
+__device__ __forceinline__ bool beyond_half(uint32_t scale, uint32_t codes) {
+    return (scale - kHalfScale >= kHalfScales) & ((scale == 255) | ((codes & 0x77777777) != 0));
 }
 
-// From the bits that any element of a row has, of the halves that lanes l and l + 32 have met.
-__device__ __forceinline__ uint32_t all_subnormal(uint32_t bits) {
-    bits |= __shfl_xor(bits, 32);
-    return (uint32_t)((bits & 0x7c007c00) == 0) & (uint32_t)((bits & 0x03ff03ff) != 0);
+// Stages of which a workgroup has left something out, a bit each; those of a greater
+// depth share the bits, and nothing is then added for most of them.
+constexpr uint32_t kMarkWords = 64;
+__device__ __forceinline__ void mark_stage(uint32_t* marks, uint32_t t) {
+    if ((threadIdx.x & 63) == 0) atomicOr(&marks[t / 32 % kMarkWords], 1u << t % 32);
+}
+__device__ __forceinline__ bool marked(const uint32_t* marks, uint32_t t) { return marks[t / 32 % kMarkWords] >> t % 32 & 1; }
+
+// A row's range: the bits of its largest magnitude, and above them those of its smallest
+// but zero, less one (all ones where it is all zeros).
+__device__ __forceinline__ int row_shift(uint32_t range) { return min(10, 30 - min(30, (int)(range >> 10 & 31))); }
+__device__ __forceinline__ bool row_fits(uint32_t range) {
+    return (range & 0xffff) < 0x7c00 && ((range >> 16) + 1) << row_shift(range) >= 0x400;
 }
 
 // A vector of float16 as the sum of two in bfloat16: the leading eight bits of

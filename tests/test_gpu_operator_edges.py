@@ -46,3 +46,60 @@ def test_block_of_zeros_under_any_scale(m, n, k, scale):
         a, b = host(x), host(dy)
         assert_close(op.mx4_linear(x, w, out_dtype=torch.float32), O.linear(a, wv), sum_bound(a, wv.T, k), torch.float32)
         assert_close(op.mx4_linear_grad(dy, w, out_dtype=torch.float32), O.linear_grad(b, wv), sum_bound(b, wv, n), torch.float32)
+
+
+def spread(shape, seed, low, high):
+    """float16 values of random signs whose exponents lie in [low, high), subnormals among them."""
+    rng = np.random.default_rng(seed)
+    v = np.ldexp(rng.uniform(1, 2, shape), rng.integers(low, high, shape)) * rng.choice([-1, 1], shape)
+    return torch.from_numpy(v.astype(np.float16)).cuda()
+
+
+@pytest.mark.parametrize("depth", [32, 64, 200])
+@pytest.mark.parametrize("m,n", [(40, 512), (130, 130), (130, 4200), (2600, 4200)])
+@pytest.mark.parametrize("scales,exponents", [((96, 98), (-10, 0)), ((96, 104), (-10, 0)), ((100, 133), (-24, -10)),
+                                              ((100, 133), (-24, 15)), ((114, 128), (-24, 15)), ((106, 107), (-24, 0))])
+def test_linear_half_exponents_apart(depth, m, n, scales, exponents):
+    """Sums over few and small products lose no more than 32 bits do: W or x of any size that float16 has."""
+    w, wv = random_mx4(n, depth, depth, scales)
+    x = spread((m, depth), m, *exponents)
+    a = host(x)
+    assert_close(op.mx4_linear(x, w, out_dtype=torch.float32), O.linear(a, wv), sum_bound(a, wv.T, depth), torch.float32)
+    g, gv = random_mx4(depth, n, depth, scales)
+    assert_close(op.mx4_linear_grad(x, g, out_dtype=torch.float32), O.linear_grad(a, gv), sum_bound(a, gv, depth), torch.float32)
+
+
+@pytest.mark.parametrize("m,n", [(40, 512), (130, 130), (2600, 4200)])
+def test_linear_half_normal_over_zero(m, n):
+    """One normal element, over weights of zero; the rest subnormal over blocks far apart in size."""
+    depth = 64
+    w, _ = random_mx4(n, depth, 3, (100, 133))
+    w.codes[:, 0] &= 0xf0  # column 0
+    wv = values(w)
+    x = spread((m, depth), 4, -24, -14)
+    x[:, 0] = 1.0
+    a = host(x)
+    assert_close(op.mx4_linear(x, w, out_dtype=torch.float32), O.linear(a, wv), sum_bound(a, wv.T, depth), torch.float32)
+    g, _ = random_mx4(depth, n, 5, (100, 133))
+    g.codes[0] = 0
+    gv = values(g)
+    assert_close(op.mx4_linear_grad(x, g, out_dtype=torch.float32), O.linear_grad(a, gv), sum_bound(a, gv, depth), torch.float32)
+
+
+@pytest.mark.parametrize("m,n,k", ROWS)
+def test_linear_half_outliers(m, n, k):
+    """Elements up to float16's largest beside its smallest, a few of each."""
+    w, wv = random_mx4(n, k, 6, (106, 133))
+    for seed, part in ((1, 0.001), (2, 0.2)):
+        def ragged(shape):
+            rng = np.random.default_rng(seed)
+            v = rng.normal(size=shape)
+            v = np.where(rng.random(shape) < part, np.ldexp(v, rng.integers(5, 14, shape)), v)
+            v = np.where(rng.random(shape) < part, np.ldexp(v, -rng.integers(10, 24, shape)), v)
+            v.flat[0], v.flat[-1] = 65504, -64
+            return torch.from_numpy(v.astype(np.float16)).cuda()
+
+        x, dy = ragged((m, k)), ragged((m, n))
+        a, b = host(x), host(dy)
+        assert_close(op.mx4_linear(x, w, out_dtype=torch.float32), O.linear(a, wv), sum_bound(a, wv.T, k), torch.float32)
+        assert_close(op.mx4_linear_grad(dy, w, out_dtype=torch.float32), O.linear_grad(b, wv), sum_bound(b, wv, n), torch.float32)
