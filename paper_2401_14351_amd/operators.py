@@ -251,9 +251,13 @@ def _product(call: str, x, w, out_dtype, grad: int):
 
 
 def mx4_quantize(x: torch.Tensor, out: Optional[Mx4] = None, stream=None) -> Mx4:
-    """The rows of x (its leading dimensions flattened) in MX FP4."""
+    """The rows of x (its leading dimensions flattened) in MX FP4.  No gradient
+    passes: an x that requires one has to be detached, or quantised under
+    ``torch.no_grad()``."""
     if stream is not None:
         return _on_stream(stream, mx4_quantize, x, out, keep=(x, out))
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError("x requires a gradient, which quantisation does not pass on")
     device = x.get_device()
     if out is None and device >= 0 and _native() is not None:
         native = _native()

@@ -103,3 +103,17 @@ def test_linear_half_outliers(m, n, k):
         a, b = host(x), host(dy)
         assert_close(op.mx4_linear(x, w, out_dtype=torch.float32), O.linear(a, wv), sum_bound(a, wv.T, k), torch.float32)
         assert_close(op.mx4_linear_grad(dy, w, out_dtype=torch.float32), O.linear_grad(b, wv), sum_bound(b, wv, n), torch.float32)
+
+
+# ---- autograd ---------------------------------------------------------------
+
+def test_quantising_what_requires_a_gradient_is_refused():
+    x = normal((9, 64), torch.float32, 1).requires_grad_()
+    q = op.Mx4.empty(9, 64, "cuda")
+    for call in (lambda: op.mx4_quantize(x), lambda: op.mx4_quantize(x, out=q), lambda: op.mx4_quantize(x * 2),
+                 lambda: op.mx4_quantize(x, stream=torch.cuda.current_stream())):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    want = op.mx4_quantize(x.detach())
+    with torch.no_grad():
+        assert torch.equal(op.mx4_quantize(x).codes, want.codes)
