@@ -5,6 +5,8 @@ bits is off by at most `sum_bound`, and an output's rounding adds half a unit in
 its last place.
 """
 
+import math
+
 import numpy as np
 import pytest
 
@@ -103,6 +105,42 @@ def test_linear_half_outliers(m, n, k):
         a, b = host(x), host(dy)
         assert_close(op.mx4_linear(x, w, out_dtype=torch.float32), O.linear(a, wv), sum_bound(a, wv.T, k), torch.float32)
         assert_close(op.mx4_linear_grad(dy, w, out_dtype=torch.float32), O.linear_grad(b, wv), sum_bound(b, wv, n), torch.float32)
+
+
+# ---- what is not finite -----------------------------------------------------
+
+def assert_same_kind(got, want):
+    """NaN and infinities, with their signs, where the definition has them."""
+    g = host(got)
+    assert (np.isnan(g) == np.isnan(want)).all()
+    inf = np.isinf(want)
+    assert (np.isinf(g) == inf).all() and (g[inf] == want[inf]).all()
+
+
+def patterns(dtype):
+    """A NaN whose payload is in its lowest bits alone, and others."""
+    quiet = {torch.bfloat16: (0x7f81, torch.int16), torch.float16: (0x7c01, torch.int16), torch.float32: (0x7f800001, torch.int32)}
+    bits, whole = quiet[dtype]
+    low = torch.tensor([bits], dtype=whole).view(dtype)[0]
+    return [torch.tensor(v, dtype=dtype) for v in (math.inf, -math.inf, math.nan)] + [low]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", ROWS)
+@pytest.mark.parametrize("tiny_block", [False, True])
+def test_not_finite_by_element(dtype, m, n, k, tiny_block):
+    """An infinity of x over a zero weight is NaN, over others an infinity of its sign; a NaN is a NaN."""
+    w, _ = random_mx4(n, k, 11, (118, 128))
+    if tiny_block:  # a block that float16 does not hold
+        w.scales[n // 2, 1] = 60
+    wv = values(w)
+    for i, bad in enumerate(patterns(dtype)):
+        x, dy = normal((m, k), dtype, 12), normal((m, n), dtype, 13)
+        x[m // 2, (i * 37 + 5) % k] = bad.cuda()
+        dy[m - 1, n - 1 - i] = bad.cuda()
+        with np.errstate(invalid="ignore"):
+            assert_same_kind(op.mx4_linear(x, w, out_dtype=torch.float32), O.linear(host(x), wv))
+            assert_same_kind(op.mx4_linear_grad(dy, w, out_dtype=torch.float32), O.linear_grad(host(dy), wv))
 
 
 # ---- autograd ---------------------------------------------------------------
