@@ -116,8 +116,9 @@ __global__ __launch_bounds__(256) void lookup(Lookup a, T* out) {
         for (uint32_t u = 0; u < kTogether; ++u) {
             const uint32_t c = c0 + u * a.lanes * 8;
             if (c >= a.dim) break;
+            if (row >= 0)  // else zeros, whatever the scale
 #pragma unroll
-            for (uint32_t e = 0; e < 8; ++e) v[u][e] *= a.scale;
+                for (uint32_t e = 0; e < 8; ++e) v[u][e] *= a.scale;
             store8<Vec>(out + i * a.out_stride, c, a.dim, v[u]);
         }
     }

@@ -143,6 +143,24 @@ def test_not_finite_by_element(dtype, m, n, k, tiny_block):
             assert_same_kind(op.mx4_linear_grad(dy, w, out_dtype=torch.float32), O.linear_grad(host(dy), wv))
 
 
+# ---- lookups ----------------------------------------------------------------
+
+@pytest.mark.parametrize("scale", [-2.0, 0.0, -0.0, math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [7, 96, 1100])
+def test_padding_is_zeros_under_any_scale(scale, dtype, dim):
+    table = normal((9, dim), dtype, 1)
+    q = op.mx4_quantize(table)
+    ids = torch.tensor([3, -1, 8, 9, 0, 1 << 40], device="cuda")
+    for t in (table, q):
+        y = op.embedding(t, ids, scale, out_dtype=dtype)
+        for row in (1, 3, 5):
+            assert not y[row].any() and not y[row].signbit().any()
+        plain = (table if t is table else op.mx4_dequantize(q, torch.float32)).float()
+        want = (plain[[3, 8, 0]] * scale).to(dtype)
+        assert ((y[[0, 2, 4]] == want) | (y[[0, 2, 4]].isnan() & want.isnan())).all()
+
+
 # ---- autograd ---------------------------------------------------------------
 
 def test_quantising_what_requires_a_gradient_is_refused():
