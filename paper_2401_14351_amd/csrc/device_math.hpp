@@ -50,6 +50,17 @@ __device__ __forceinline__ T from_f32(float v) {
         }                                     \
     } while (0)
 
+// Workgroups (of at most 1024 threads) in two dimensions where there are more than one
+// can count, and which of them this one is.  A few more than asked for are launched.
+inline dim3 grid_of(uint64_t blocks) {
+    constexpr uint64_t kMost = 1 << 21;  // a dimension counts threads in 32 bits
+    const uint64_t y = (blocks + kMost - 1) / kMost;
+    return y <= 1 ? dim3((uint32_t)blocks) : dim3((uint32_t)((blocks + y - 1) / y), (uint32_t)y);
+}
+__device__ __forceinline__ uint32_t block_index() {
+    return blockIdx.y ? blockIdx.y * gridDim.x + blockIdx.x : blockIdx.x;
+}
+
 // The scale operand of the conversion instructions: they take a float's
 // exponent field alone, so a scale byte goes there as it is.  0 then means
 // 2^-127 and 255 makes the results NaN, as the format has it.

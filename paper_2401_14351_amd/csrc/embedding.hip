@@ -31,7 +31,7 @@ struct Lookup {
     uint64_t n;
     float scale;
     uint64_t out_stride;
-    uint32_t lanes;  // of a row: 32, 64, 128 or 256
+    uint32_t lanes;  // of a row: 32, 64 or 256
 };
 
 // Columns c .. c + 7 of a row, those past the end zero.  Vec: rows start on 16
@@ -77,7 +77,7 @@ __device__ __forceinline__ void store8(T* row, uint32_t c, uint32_t dim, const f
 // Vec: rows start on 16 bytes and end on a multiple of eight columns.
 template <bool Vec, typename S, typename T>
 __global__ __launch_bounds__(256) void lookup(Lookup a, T* out) {
-    const uint64_t i = (uint64_t)blockIdx.x * (256 / a.lanes) + threadIdx.x / a.lanes;
+    const uint64_t i = (uint64_t)block_index() * (256 / a.lanes) + threadIdx.x / a.lanes;
     if (i >= a.n) return;
     const int64_t row = a.ids.p ? id_at(a.ids, i, a.vocab) : (int64_t)i;
     const uint32_t blocks = (a.dim + 31) / 32, pitch = (blocks + 15) / 16 * 16;
@@ -282,9 +282,11 @@ __device__ __forceinline__ void write_row(const GradArgs& a, T* grad, uint32_t t
 // the search is a chain of loads that nothing can be written before the end of.
 template <bool Vec, typename S, typename T>
 __global__ __launch_bounds__(256) void sum_runs(GradArgs a, const S* dy, T* grad) {
-    if (blockIdx.x >= a.sum_blocks) {
+    const uint32_t block = block_index();
+    if (block >= a.sum_blocks) {
         __shared__ uint32_t named[kZeroRows];
-        const uint32_t row0 = (blockIdx.x - a.sum_blocks) * kZeroRows;
+        const uint32_t row0 = (block - a.sum_blocks) * kZeroRows;
+        if (a.accumulate || row0 >= a.vocab) return;  // of the workgroups launched beyond those asked for
         const uint32_t probe = threadIdx.x % 16, token = row0 + threadIdx.x / 16;
         const uint64_t key = (uint64_t)token << 32;
         uint32_t lo = 0, hi = a.n;  // the first key of the token or a later one is in [lo, hi]
@@ -312,8 +314,8 @@ __global__ __launch_bounds__(256) void sum_runs(GradArgs a, const S* dy, T* grad
         return;
     }
     const uint32_t per = 256 / a.lanes;  // windows of a workgroup
-    const uint32_t w = blockIdx.x / a.chunks * per + threadIdx.x / a.lanes;
-    const uint32_t c = (blockIdx.x % a.chunks * a.lanes + threadIdx.x % a.lanes) * 8;
+    const uint32_t w = block / a.chunks * per + threadIdx.x / a.lanes;
+    const uint32_t c = (block % a.chunks * a.lanes + threadIdx.x % a.lanes) * 8;
     if (w >= a.windows || c >= a.dim) return;
     const uint32_t first = w * kWindow, end = min(first + kWindow, a.n);
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -424,7 +426,7 @@ bool on_vectors(const void* data, uint64_t rows, uint64_t stride, uint32_t dtype
 uint32_t row_lanes(uint64_t dim) { return dim > 1024 ? 256 : dim > 256 ? 64 : 32; }
 
 template <bool Vec, typename T>
-void launch_lookup(const Lookup& l, uint32_t grid, T* out, hipStream_t stream) {
+void launch_lookup(const Lookup& l, dim3 grid, T* out, hipStream_t stream) {
     if (l.table.codes)
         lookup<Vec, void, T><<<grid, 256, 0, stream>>>(l, out);
     else
@@ -436,15 +438,14 @@ void launch_lookup(const Lookup& l, uint32_t grid, T* out, hipStream_t stream) {
 int32_t launch_embedding(const EmbeddingLaunch& a, hipStream_t stream) {
     const uint32_t lanes = row_lanes(a.dim);
     const Lookup l{a.table, (uint32_t)a.vocab, (uint32_t)a.dim, {a.ids, a.ids64}, a.n, a.scale, a.out_stride, lanes};
-    const uint64_t grid = ceil_div(a.n, 256 / lanes);
-    if (grid > UINT32_MAX / 256) return fail(SLLM_E_RANGE, "%llu rows are more than a launch takes", (unsigned long long)a.n);
+    const dim3 grid = grid_of(ceil_div(a.n, 256 / lanes));
     const bool vec = a.dim % 8 == 0 && on_vectors(a.out, a.n, a.out_stride, a.out_dtype) &&
                      (a.table.codes || on_vectors(a.table.data, a.vocab, a.table.stride, a.table.dtype));
     SLLM_BY_DTYPE(a.out_dtype, T, {
         if (vec)
-            launch_lookup<true>(l, (uint32_t)grid, static_cast<T*>(a.out), stream);
+            launch_lookup<true>(l, grid, static_cast<T*>(a.out), stream);
         else
-            launch_lookup<false>(l, (uint32_t)grid, static_cast<T*>(a.out), stream);
+            launch_lookup<false>(l, grid, static_cast<T*>(a.out), stream);
     });
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
@@ -469,9 +470,9 @@ GradPlan plan_grad(uint64_t n, uint64_t dim) {
 }
 
 template <bool Vec, typename S, typename T>
-int32_t launch_sums(const GradArgs& g, const EmbeddingGradLaunch& a, uint64_t grid, hipStream_t stream) {
+int32_t launch_sums(const GradArgs& g, const EmbeddingGradLaunch& a, dim3 grid, hipStream_t stream) {
     T* grad = static_cast<T*>(a.grad);
-    sum_runs<Vec, S, T><<<(uint32_t)grid, 256, 0, stream>>>(g, static_cast<const S*>(a.dy), grad);
+    sum_runs<Vec, S, T><<<grid, 256, 0, stream>>>(g, static_cast<const S*>(a.dy), grad);
     SLLM_HIP(hipGetLastError());
     if (g.windows > 1) {
         // a frequent token's columns go to several CUs, each of which takes in only so much
@@ -518,8 +519,7 @@ int32_t launch_embedding_grad(const EmbeddingGradLaunch& a, void* workspace, hip
     g.lanes = row_lanes(a.dim);
     g.chunks = (uint32_t)ceil_div(a.dim, g.lanes * 8);
     const uint64_t sums = ceil_div(p.windows, 256 / g.lanes) * g.chunks;
-    const uint64_t grid = sums + (a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows));
-    if (grid > UINT32_MAX / 256) return fail(SLLM_E_RANGE, "gradient too large");
+    const dim3 grid = grid_of(sums + (a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows)));
     g.sum_blocks = (uint32_t)sums;
     const uint64_t size = element_bytes(a.grad_dtype), row_bytes = a.dim * size;
     const uint64_t steps = reinterpret_cast<uintptr_t>(a.grad) | row_bytes | (a.vocab > 1 ? a.grad_stride * size : 0);

@@ -146,7 +146,7 @@ __global__ __launch_bounds__(1024) void skinny_product(SkinnyArgs a) {
     static_assert((Rows == 1 || Rows == 4 || Rows == 16) && (Rows == 16 || MT == 1), "");
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t waves = blockDim.x >> 6, r = lane & 15, g = lane >> 4;
-    const uint64_t j0 = (uint64_t)blockIdx.x * 16;
+    const uint64_t j0 = (uint64_t)block_index() * 16;
     const uint32_t g0 = (uint64_t)a.groups * wave / waves, g1 = (uint64_t)a.groups * (wave + 1) / waves;
 
     f32x4 acc[MT];
@@ -319,7 +319,7 @@ void launch(const SkinnyArgs& a, hipStream_t stream) {
     uint32_t waves = 4;
     while (waves < 16 && (a.groups > waves * 2 || (grid * waves < 2048 && a.groups > waves))) waves *= 2;
     while (waves > 1 && a.groups < waves) waves /= 2;
-    skinny_product<X, Rows, MT><<<grid, waves * 64, waves * Rows * MT * 16 * 4, stream>>>(a);
+    skinny_product<X, Rows, MT><<<grid_of(grid), waves * 64, waves * Rows * MT * 16 * 4, stream>>>(a);
 }
 
 }  // namespace

@@ -42,7 +42,7 @@ __device__ __forceinline__ float quad(float x) {
 template <bool Vec, typename T>
 __global__ __launch_bounds__(256) void mx_quantize(const T* src, uint64_t stride, uint64_t rows, uint32_t cols, uint32_t lanes,
                                                    uint8_t* codes, uint8_t* scales) {
-    const uint64_t row = (uint64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes;
+    const uint64_t row = (uint64_t)block_index() * (256 / lanes) + threadIdx.x / lanes;
     if (row >= rows) return;
     const uint32_t blocks = (cols + 31) / 32, pitch = (blocks + 15) / 16 * 16;
     const T* x = src + row * stride;
@@ -96,17 +96,16 @@ int32_t launch_quantize(const sllm_matrix& src, const sllm_mx& dst, hipStream_t 
     // 44; 512 rows 3.7 and 6.1), short ones a wave (32000 of 768 in bfloat16 12, a
     // workgroup 18).
     const uint32_t lanes = vectors >= 256 ? 256 : 64;
-    const uint64_t grid = ceil_div(src.rows, 256 / lanes);
-    if (grid > UINT32_MAX / 256) return fail(SLLM_E_RANGE, "%llu rows are more than a launch takes", (unsigned long long)src.rows);
+    const dim3 grid = grid_of(ceil_div(src.rows, 256 / lanes));
     const uint64_t row_bytes = src.stride * (src.dtype == SLLM_DTYPE_F32 ? 4 : 2);
     const bool vec = src.cols % 8 == 0 && reinterpret_cast<uintptr_t>(src.data) % 16 == 0 && (src.rows == 1 || row_bytes % 16 == 0);
     uint8_t *codes = static_cast<uint8_t*>(dst.codes), *scales = static_cast<uint8_t*>(dst.scales);
     SLLM_BY_DTYPE(src.dtype, T, {
         const T* x = static_cast<const T*>(src.data);
         if (vec)
-            mx_quantize<true, T><<<(uint32_t)grid, 256, 0, stream>>>(x, src.stride, src.rows, (uint32_t)src.cols, lanes, codes, scales);
+            mx_quantize<true, T><<<grid, 256, 0, stream>>>(x, src.stride, src.rows, (uint32_t)src.cols, lanes, codes, scales);
         else
-            mx_quantize<false, T><<<(uint32_t)grid, 256, 0, stream>>>(x, src.stride, src.rows, (uint32_t)src.cols, lanes, codes, scales);
+            mx_quantize<false, T><<<grid, 256, 0, stream>>>(x, src.stride, src.rows, (uint32_t)src.cols, lanes, codes, scales);
     });
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
@@ -205,7 +204,7 @@ Plan plan_linear(const LinearLaunch& a) {
 template <typename T, int Parts>
 __global__ __launch_bounds__(256) void split_x(const T* x, uint64_t stride, uint64_t rows, uint64_t cols, uint64_t pitch,
                                                uint16_t* out) {
-    const uint64_t vectors = pitch / 8, i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint64_t vectors = pitch / 8, i = (uint64_t)block_index() * 256 + threadIdx.x;
     const uint64_t row = i / vectors, c = i % vectors * 8;
     if (row >= rows) return;
     uint16_t v[Parts][8];
@@ -230,7 +229,7 @@ __global__ __launch_bounds__(256) void split_x(const T* x, uint64_t stride, uint
 template <bool Vec, int Lanes>
 __global__ __launch_bounds__(256) void find_ranges(const uint16_t* x, uint64_t stride, uint64_t rows, uint64_t cols, uint32_t* ranges) {
     __shared__ uint32_t waves[2][4];
-    const uint64_t row = (uint64_t)blockIdx.x * (256 / Lanes) + threadIdx.x / Lanes;
+    const uint64_t row = (uint64_t)block_index() * (256 / Lanes) + threadIdx.x / Lanes;
     const uint16_t* at = x + min(row, rows - 1) * stride;
     uint32_t top = 0, bottom = 0xffff;
     for (uint64_t c = threadIdx.x % Lanes * 8; c < cols; c += Lanes * 8) {
@@ -273,7 +272,7 @@ __global__ __launch_bounds__(256) void find_ranges(const uint16_t* x, uint64_t s
 template <typename T>
 __global__ __launch_bounds__(256) void join_splits(const float* in, uint32_t splits, uint64_t split_stride, uint64_t rows,
                                                    uint64_t cols, T* out, uint64_t stride) {
-    const uint64_t vectors = (cols + 3) / 4, i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint64_t vectors = (cols + 3) / 4, i = (uint64_t)block_index() * 256 + threadIdx.x;
     const uint64_t row = i / vectors, c = i % vectors * 4;
     if (row >= rows) return;
     f32x4 sum = {0, 0, 0, 0};
@@ -281,16 +280,8 @@ __global__ __launch_bounds__(256) void join_splits(const float* in, uint32_t spl
     for (uint32_t e = 0; e < 4 && c + e < cols; ++e) out[row * stride + c + e] = from_f32<T>(sum[e]);
 }
 
-int32_t grid_of(uint64_t threads, uint32_t* blocks) {
-    const uint64_t n = ceil_div(threads, 256);
-    if (n > UINT32_MAX / 256) return fail(SLLM_E_RANGE, "matrix too large");
-    *blocks = (uint32_t)n;
-    return SLLM_OK;
-}
-
 int32_t join(const Plan& p, const float* sums, uint32_t splits, const LinearLaunch& a, hipStream_t stream) {
-    uint32_t blocks;
-    SLLM_TRY(grid_of(a.m * ceil_div(p.cols, 4), &blocks));
+    const dim3 blocks = grid_of(ceil_div(a.m * ceil_div(p.cols, 4), 256));
     SLLM_BY_DTYPE(a.out_dtype, T, (join_splits<T><<<blocks, 256, 0, stream>>>(sums, splits, p.split_stride, a.m, p.cols,
                                                                              static_cast<T*>(a.out), a.out_stride)));
     SLLM_HIP(hipGetLastError());
@@ -306,8 +297,7 @@ int32_t stage_x(const LinearLaunch& a, const Plan& p, void* workspace, WideArgs*
     w->x = x;
     w->x_stride = p.parts * p.part_stride;
     w->part_stride = p.part_stride;
-    uint32_t blocks;
-    SLLM_TRY(grid_of(a.m * p.part_stride / 8, &blocks));
+    const dim3 blocks = grid_of(ceil_div(a.m * p.part_stride / 8, 256));
     if (p.parts == 1)
         split_x<uint16_t, 1><<<blocks, 256, 0, stream>>>(static_cast<const uint16_t*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
     else
@@ -319,8 +309,7 @@ int32_t stage_x(const LinearLaunch& a, const Plan& p, void* workspace, WideArgs*
 int32_t launch_ranges(const LinearLaunch& a, const Plan& p, uint32_t* ranges, hipStream_t stream) {
     const uint16_t* x = static_cast<const uint16_t*>(a.x.data);
     const bool vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && (a.m == 1 || a.x.stride % 8 == 0), wide = p.depth > 1024;
-    uint32_t blocks;
-    SLLM_TRY(grid_of(a.m * (wide ? 256 : 64), &blocks));
+    const dim3 blocks = grid_of(ceil_div(a.m, wide ? 1 : 4));
     const auto kernel = vec ? (wide ? find_ranges<true, 256> : find_ranges<true, 64>) : (wide ? find_ranges<false, 256> : find_ranges<false, 64>);
     kernel<<<blocks, 256, 0, stream>>>(x, a.x.stride, a.m, p.depth, ranges);
     SLLM_HIP(hipGetLastError());

@@ -161,6 +161,50 @@ def test_padding_is_zeros_under_any_scale(scale, dtype, dim):
         assert ((y[[0, 2, 4]] == want) | (y[[0, 2, 4]].isnan() & want.isnan())).all()
 
 
+# ---- sizes ------------------------------------------------------------------
+
+def test_more_rows_than_a_launch_of_one_dimension():
+    """2^24 rows of more than 1024 columns: looked up, quantised and back."""
+    rows, cols = (1 << 24) + 3, 1032
+    table = normal((5, cols), torch.bfloat16, 1)
+    ids = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    ids[-3:] = torch.tensor([4, 7, 2])
+    y = op.embedding(table, ids)
+    assert torch.equal(y[-3], table[4]) and not y[-2].any() and torch.equal(y[-1], table[2])
+    assert torch.equal(y[(1 << 24) - 2:1 << 24], table[:1].expand(2, cols)) and torch.equal(y[0], table[0])
+    q = op.mx4_quantize(y)
+    few = op.mx4_quantize(y[-5:])
+    assert torch.equal(q.codes[-5:], few.codes) and torch.equal(q.scales[-5:], few.scales)
+    op.mx4_dequantize(q, out=y)
+    assert torch.equal(y[-5:], op.mx4_dequantize(few)) and torch.equal(y[0], y[-5])
+
+
+def test_gradient_of_a_table_of_many_rows():
+    """More rows to clear than one dimension of a launch counts, 16 a workgroup."""
+    vocab = (1 << 28) + 40
+    out = torch.full((vocab, 1), 3.0, dtype=torch.float16, device="cuda")
+    ids = torch.tensor([vocab - 1, 5, vocab - 2, 5, vocab], device="cuda")
+    op.embedding_grad(torch.tensor([[1.0], [2.0], [4.0], [8.0], [16.0]], device="cuda"), ids, vocab, out=out)
+    assert out[-1].item() == 1 and out[-2].item() == 4 and out[5].item() == 10
+    out[-2:] = 0
+    out[5] = 0
+    assert not out.any()
+
+
+def test_product_with_a_weight_of_many_rows():
+    """2^30 rows of W and one of x: 2^26 workgroups."""
+    n, k = (1 << 30) + 17, 32
+    w = op.Mx4(torch.zeros(n, 16, dtype=torch.uint8, device="cuda"), torch.zeros(n, 16, dtype=torch.uint8, device="cuda"), k)
+    small, sv = random_mx4(20, k, 1)
+    w.codes[-20:], w.scales[-20:] = small.codes, small.scales
+    x = normal((1, k), torch.bfloat16, 2)
+    y = op.mx4_linear(x, w)
+    a = host(x)
+    assert_close(y[:, -20:], O.linear(a, sv), sum_bound(a, sv.T, k), torch.bfloat16)
+    y[:, -20:] = 0
+    assert not y.any()
+
+
 # ---- autograd ---------------------------------------------------------------
 
 def test_quantising_what_requires_a_gradient_is_refused():
