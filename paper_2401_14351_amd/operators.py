@@ -203,6 +203,13 @@ def _refuse_grad(*tensors):
             raise ValueError("an operator that writes to a given tensor takes no part in autograd")
 
 
+def _written(out: Optional[torch.Tensor], *more: torch.Tensor):
+    """Count a write to given tensors as one of torch's own in place: a backward pass that has saved them then raises."""
+    for t in (out, *more):
+        if t is not None and not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 def _workspace(query, *args) -> int:
     """How many bytes of workspace a call with these operands needs."""
     n = C.c_uint64()
@@ -270,12 +277,13 @@ def mx4_quantize(x: torch.Tensor, out: Optional[Mx4] = None, stream=None) -> Mx4
             return q
     src = _matrix(x, "x")
     device = _one_device(x, out)
-    if out is None:
-        out = Mx4._beside(x, src.rows, src.cols)
-    elif out.rows != src.rows or out.cols != src.cols:
-        raise ValueError(f"out: expected {src.rows} x {src.cols}, got {out.rows} x {out.cols}")
-    binding.check(binding.lib().sllm_mx_quantize(src, out._struct, device, _raw_stream(device)))
-    return out
+    q = Mx4._beside(x, src.rows, src.cols) if out is None else out
+    if q.rows != src.rows or q.cols != src.cols:
+        raise ValueError(f"out: expected {src.rows} x {src.cols}, got {q.rows} x {q.cols}")
+    binding.check(binding.lib().sllm_mx_quantize(src, q._struct, device, _raw_stream(device)))
+    if out is not None:
+        _written(out.codes, out.scales)
+    return q
 
 
 def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
@@ -291,9 +299,10 @@ def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, out: Optional[to
             binding.check(y)
         if y is not None:
             return y
-    out, rows = _output(out, (q.rows, q.cols), q.rows, q.cols, dtype, q.codes)
+    y, rows = _output(out, (q.rows, q.cols), q.rows, q.cols, dtype, q.codes)
     binding.check(binding.lib().sllm_mx_dequantize(q._struct, rows, device, _raw_stream(device)))
-    return out
+    _written(out)
+    return y
 
 
 def mx4_linear(x: Union[torch.Tensor, Mx4], w: Mx4, out: Optional[torch.Tensor] = None,
@@ -322,9 +331,10 @@ def _linear(x, w, out, out_dtype):
     L = binding.lib()
     src = _matrix(x, "x")
     device = _one_device(x, w)
-    out, rows = _output(out, (*x.shape[:-1], w.rows), src.rows, w.rows, out_dtype or x.dtype, x)
+    y, rows = _output(out, (*x.shape[:-1], w.rows), src.rows, w.rows, out_dtype or x.dtype, x)
     _call(L.sllm_mx_linear, L.sllm_mx_linear_workspace, (src, w._struct), rows, device)
-    return out
+    _written(out)
+    return y
 
 
 def _linear_mx(x, w, out, out_dtype):
@@ -339,9 +349,10 @@ def _linear_mx(x, w, out, out_dtype):
         if y is not None:
             return y
     L = binding.lib()
-    out, rows = _output(out, (x.rows, w.rows), x.rows, w.rows, out_dtype or torch.bfloat16, x.codes)
+    y, rows = _output(out, (x.rows, w.rows), x.rows, w.rows, out_dtype or torch.bfloat16, x.codes)
     _call(L.sllm_mx_linear_mx, L.sllm_mx_linear_mx_workspace, (x._struct, w._struct), rows, device)
-    return out
+    _written(out)
+    return y
 
 
 def mx4_linear_grad(dy: torch.Tensor, w: Mx4, out: Optional[torch.Tensor] = None,
@@ -358,22 +369,29 @@ def mx4_linear_grad(dy: torch.Tensor, w: Mx4, out: Optional[torch.Tensor] = None
     L = binding.lib()
     src = _matrix(dy, "dy")
     device = _one_device(dy, w)
-    out, rows = _output(out, (*dy.shape[:-1], w.cols), src.rows, w.cols, out_dtype or dy.dtype, dy)
+    dx, rows = _output(out, (*dy.shape[:-1], w.cols), src.rows, w.cols, out_dtype or dy.dtype, dy)
     _call(L.sllm_mx_linear_grad, L.sllm_mx_linear_grad_workspace, (src, w._struct), rows, device)
-    return out
+    _written(out)
+    return dx
 
 
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, out_dtype):
-        ctx.w, ctx.dtype = w, x.dtype
+        # saved as tensors are, so that a change of the weight before the backward pass
+        # raises, and hooks on what is saved see it; tensors of inference mode cannot be
+        ctx.w = w if w.codes.is_inference() or w.scales.is_inference() else None
+        if ctx.w is None:
+            ctx.save_for_backward(w.codes, w.scales)
+        ctx.cols, ctx.dtype = w.cols, x.dtype
         return _linear(x, w, None, out_dtype)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
+        w = Mx4(*ctx.saved_tensors, ctx.cols) if ctx.w is None else ctx.w
         # gradients of sums and means arrive with strides of 0
-        return mx4_linear_grad(dy.contiguous(), ctx.w, out_dtype=ctx.dtype), None, None
+        return mx4_linear_grad(dy.contiguous(), w, out_dtype=ctx.dtype), None, None
 
 
 def embedding(table: Union[torch.Tensor, Mx4], tokens: torch.Tensor, scale: float = 1.0,
@@ -412,9 +430,10 @@ def _embedding(table, tokens, scale, out, out_dtype):
     else:
         raise ValueError(f"table: expected rows and columns, got shape {tuple(table.shape)}")
     like = table.codes if isinstance(table, Mx4) else table
-    out, rows = _output(out, (*tokens.shape, src.cols), ids.n, src.cols, out_dtype or dtype, like)
+    y, rows = _output(out, (*tokens.shape, src.cols), ids.n, src.cols, out_dtype or dtype, like)
     binding.check(fn(src, ids, scale, rows, device, _raw_stream(device)))
-    return out
+    _written(out)
+    return y
 
 
 def embedding_grad(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: float = 1.0,
@@ -443,12 +462,13 @@ def embedding_grad(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: fl
             return y
     L = binding.lib()
     ids, src = _ids(tokens), _matrix(dy, "dy")
-    out, grad = _output(out, (vocab, src.cols), vocab, src.cols, out_dtype or dy.dtype, dy)
+    g, grad = _output(out, (vocab, src.cols), vocab, src.cols, out_dtype or dy.dtype, dy)
     n = _workspace(L.sllm_embedding_grad_workspace, ids.n, grad)
     ws = torch.empty(n, dtype=torch.uint8, device=dy.device) if n else None
     binding.check(L.sllm_embedding_grad(src, ids, scale, 1 if accumulate else 0, grad, ws.data_ptr() if n else None, n,
                                         device, _raw_stream(device)))
-    return out
+    _written(out)
+    return g
 
 
 class _Embedding(torch.autograd.Function):

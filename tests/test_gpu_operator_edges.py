@@ -207,6 +207,65 @@ def test_product_with_a_weight_of_many_rows():
 
 # ---- autograd ---------------------------------------------------------------
 
+def test_a_changed_weight_raises_in_backward():
+    w, wv = random_mx4(48, 64, 1)
+    x = normal((9, 64), torch.float32, 2).requires_grad_()
+    for change in (lambda: op.mx4_quantize(normal((48, 64), torch.float32, 3), out=w), lambda: w.scales.add_(1),
+                   lambda: w.codes.zero_()):
+        y = op.mx4_linear(x, w)
+        change()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+    w, wv = random_mx4(48, 64, 1)
+    op.mx4_linear(x, w).sum().backward()
+    assert_close(x.grad, O.linear_grad(np.ones((9, 48)), wv), sum_bound(np.ones((9, 48)), wv, 48), torch.float32)
+
+
+@pytest.mark.parametrize("write", ["linear", "linear_mx", "linear_grad", "embedding", "embedding_grad", "accumulate", "dequantize"])
+@pytest.mark.parametrize("stream", [False, True])
+def test_a_written_output_raises_in_backward(write, stream):
+    """A tensor saved for a backward pass and then written through out= is told from one that was not."""
+    w, _ = random_mx4(32, 32, 1)
+    x = normal((32, 32), torch.float32, 2)
+    ids = torch.arange(32, device="cuda")
+    held = torch.zeros(32, 32, device="cuda")
+    keep = {"stream": torch.cuda.current_stream()} if stream else {}
+    scale = torch.ones(32, 32, device="cuda", requires_grad=True)
+    y = scale * held
+    {"linear": lambda: op.mx4_linear(x, w, out=held, **keep),
+     "linear_mx": lambda: op.mx4_linear(op.mx4_quantize(x), w, out=held, **keep),
+     "linear_grad": lambda: op.mx4_linear_grad(x, w, out=held, **keep),
+     "embedding": lambda: op.embedding(x, ids, out=held, **keep),
+     "embedding_grad": lambda: op.embedding_grad(x, ids, 32, out=held, **keep),
+     "accumulate": lambda: op.embedding_grad(x, ids, 32, out=held, accumulate=True, **keep),
+     "dequantize": lambda: op.mx4_dequantize(w, out=held, **keep)}[write]()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+
+
+def test_weights_of_inference_mode_serve_training():
+    """They have no versions and cannot be saved, but their gradients are right."""
+    with torch.inference_mode():
+        w = op.mx4_quantize(normal((48, 64), torch.bfloat16, 1))
+        out = torch.empty(48, 64, device="cuda")
+        assert op.mx4_dequantize(w, out=out) is out
+        op.mx4_quantize(normal((48, 64), torch.bfloat16, 1), out=w)
+    wv = values(w)
+    x = normal((9, 64), torch.float32, 2).requires_grad_()
+    op.mx4_linear(x, w).sum().backward()
+    assert_close(x.grad, O.linear_grad(np.ones((9, 48)), wv), sum_bound(np.ones((9, 48)), wv, 48), torch.float32)
+
+
+def test_saved_weights_pass_the_hooks():
+    w, wv = random_mx4(48, 64, 1)
+    x = normal((9, 64), torch.float32, 2).requires_grad_()
+    with torch.autograd.graph.save_on_cpu():
+        y = op.mx4_linear(x, w)
+    w.codes.zero_()  # what was saved is a copy
+    y.sum().backward()
+    assert_close(x.grad, O.linear_grad(np.ones((9, 48)), wv), sum_bound(np.ones((9, 48)), wv, 48), torch.float32)
+
+
 def test_quantising_what_requires_a_gradient_is_refused():
     x = normal((9, 64), torch.float32, 1).requires_grad_()
     q = op.Mx4.empty(9, 64, "cuda")
