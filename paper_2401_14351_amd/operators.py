@@ -44,43 +44,68 @@ def _pitches(cols: int):
 
 class Mx4:
     """A matrix in MX FP4: ``codes`` (rows, blocks * 16) and ``scales`` (rows,
-    blocks rounded up to 16), both contiguous uint8, laid out as ``sllm_mx``."""
+    blocks rounded up to 16), both contiguous uint8, laid out as ``sllm_mx``.
+    It is those tensors, wherever their storage is when it is used."""
 
-    __slots__ = ("codes", "scales", "rows", "cols", "_struct", "_address", "_device")
+    __slots__ = ("_codes", "_scales", "_cols")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int):
+        self._codes, self._scales, self._cols = codes, scales, cols
+        self._check()
+
+    def _check(self):
+        cols = self._cols
         code_pitch, scale_pitch = _pitches(cols)
-        for name, t, pitch in (("codes", codes, code_pitch), ("scales", scales, scale_pitch)):
+        for name, t, pitch in (("codes", self._codes, code_pitch), ("scales", self._scales, scale_pitch)):
             if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[1] != pitch or not t.is_contiguous():
                 raise ValueError(f"{name}: expected a contiguous uint8 tensor of {pitch} columns for {cols} columns, "
                                  f"got {t.dtype} with shape {tuple(t.shape)} and strides {t.stride()}")
-        if codes.shape[0] != scales.shape[0] or codes.device != scales.device:
+        if self._codes.shape[0] != self._scales.shape[0] or self._codes.device != self._scales.device:
             raise ValueError("codes and scales differ in rows or device")
-        self._set(codes, scales, cols)
 
-    def _set(self, codes, scales, cols):
-        self.codes, self.scales = codes, scales
-        self.rows, self.cols = codes.shape[0], cols
-        self._struct = binding.Mx(codes.data_ptr(), scales.data_ptr(), self.rows, cols)
-        self._address = C.addressof(self._struct)
-        self._device = codes.get_device()
+    @classmethod
+    def _of(cls, codes: torch.Tensor, scales: torch.Tensor, cols: int) -> "Mx4":
+        """The same without a check."""
+        q = cls.__new__(cls)
+        q._codes, q._scales, q._cols = codes, scales, cols
+        return q
 
     @classmethod
     def empty(cls, rows: int, cols: int, device) -> "Mx4":
         """A matrix whose contents are not set."""
         code_pitch, scale_pitch = _pitches(cols)
-        q = cls.__new__(cls)
-        q._set(torch.empty((rows, code_pitch), dtype=torch.uint8, device=device),
-               torch.empty((rows, scale_pitch), dtype=torch.uint8, device=device), cols)
-        return q
+        return cls._of(torch.empty((rows, code_pitch), dtype=torch.uint8, device=device),
+                       torch.empty((rows, scale_pitch), dtype=torch.uint8, device=device), cols)
 
     @classmethod
     def _beside(cls, t: torch.Tensor, rows: int, cols: int) -> "Mx4":
         """One whose contents are not set, where t is: half a microsecond less than by naming the device."""
         code_pitch, scale_pitch = _pitches(cols)
-        q = cls.__new__(cls)
-        q._set(t.new_empty((rows, code_pitch), dtype=torch.uint8), t.new_empty((rows, scale_pitch), dtype=torch.uint8), cols)
-        return q
+        return cls._of(t.new_empty((rows, code_pitch), dtype=torch.uint8), t.new_empty((rows, scale_pitch), dtype=torch.uint8), cols)
+
+    def __reduce__(self):
+        return Mx4, (self._codes, self._scales, self._cols)
+
+    @property
+    def _struct(self) -> binding.Mx:
+        self._check()
+        return binding.Mx(self._codes.data_ptr(), self._scales.data_ptr(), self.rows, self._cols)
+
+    @property
+    def codes(self) -> torch.Tensor:
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        return self._scales
+
+    @property
+    def rows(self) -> int:
+        return self._codes.shape[0]
+
+    @property
+    def cols(self) -> int:
+        return self._cols
 
     @property
     def shape(self):
@@ -146,7 +171,7 @@ def _ids(t: torch.Tensor) -> binding.Ids:
 
 
 def _index(t) -> int:
-    return t._device if isinstance(t, Mx4) else t.get_device()
+    return (t._codes if isinstance(t, Mx4) else t).get_device()
 
 
 def _one_device(first, *others) -> int:
@@ -248,10 +273,10 @@ def _product(call: str, x, w, out_dtype, grad: int):
     """A product by the extension, or None."""
     native, device = _native(), x.get_device()
     code = -1 if out_dtype is None else _DTYPE.get(out_dtype)
-    if native is None or device < 0 or device != w._device or code is None:
+    if native is None or device < 0 or code is None:
         return None
-    y = native.ext.product(getattr(native, call), getattr(native, call + "_workspace"), x, w._address, code, grad, device,
-                           _raw_stream(device))
+    y = native.ext.product(getattr(native, call), getattr(native, call + "_workspace"), x, w._codes, w._scales, w._cols, code, grad,
+                           device, _raw_stream(device))
     if y.__class__ is int:
         binding.check(y)
     return y
@@ -272,9 +297,7 @@ def mx4_quantize(x: torch.Tensor, out: Optional[Mx4] = None, stream=None) -> Mx4
         if parts.__class__ is int:
             binding.check(parts)
         if parts is not None:
-            q = Mx4.__new__(Mx4)
-            q._set(*parts, x.shape[-1])
-            return q
+            return Mx4._of(*parts, x.shape[-1])
     src = _matrix(x, "x")
     device = _one_device(x, out)
     q = Mx4._beside(x, src.rows, src.cols) if out is None else out
@@ -291,10 +314,10 @@ def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, out: Optional[to
     """The values q stands for, rounded to ``dtype`` (or the type of ``out``)."""
     if stream is not None:
         return _on_stream(stream, mx4_dequantize, q, dtype, out, keep=(q, out))
-    device = q._device
+    device = _index(q)
     if out is None and device >= 0 and dtype in _DTYPE and _native() is not None:
         native = _native()
-        y = native.ext.dequantize(native.mx_dequantize, q._address, q.codes, _DTYPE[dtype], device, _raw_stream(device))
+        y = native.ext.dequantize(native.mx_dequantize, q._codes, q._scales, q._cols, _DTYPE[dtype], device, _raw_stream(device))
         if y.__class__ is int:
             binding.check(y)
         if y is not None:
@@ -342,8 +365,8 @@ def _linear_mx(x, w, out, out_dtype):
     code = _DTYPE.get(out_dtype or torch.bfloat16)
     if out is None and device >= 0 and code is not None and _native() is not None:
         native = _native()
-        y = native.ext.product_mx(native.mx_linear_mx, native.mx_linear_mx_workspace, x._address, w._address, x.codes, code,
-                                  device, _raw_stream(device))
+        y = native.ext.product_mx(native.mx_linear_mx, native.mx_linear_mx_workspace, x._codes, x._scales, x._cols, w._codes,
+                                  w._scales, w._cols, code, device, _raw_stream(device))
         if y.__class__ is int:
             binding.check(y)
         if y is not None:
@@ -415,8 +438,9 @@ def _embedding(table, tokens, scale, out, out_dtype):
     code = (2 if mx else -1) if out_dtype is None else _DTYPE.get(out_dtype)
     if out is None and device >= 0 and code is not None and _native() is not None:
         native = _native()
-        y = native.ext.lookup(native.embedding_mx if mx else native.embedding, table._address if mx else table,
-                              table.codes if mx else None, tokens, scale, code, device, _raw_stream(device))
+        y = native.ext.lookup(native.embedding_mx if mx else native.embedding, table._codes if mx else table,
+                              table._scales if mx else None, table._cols if mx else 0, tokens, scale, code, device,
+                              _raw_stream(device))
         if y.__class__ is int:
             binding.check(y)
         if y is not None:

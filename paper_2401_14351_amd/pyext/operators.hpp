@@ -57,6 +57,24 @@ inline bool ids_of(const at::Tensor& t, sllm_ids* ids) {
     return true;
 }
 
+// A matrix in MX FP4 from its tensors; null codes where they are not what it is made of.
+// Gives the codes' tensor, which tells where results are allocated.
+inline const at::Tensor* mx_of(PyObject* codes, PyObject* scales, PyObject* cols, int64_t device, sllm_mx* q) {
+    const long long n = PyLong_AsLongLong(cols);
+    if (n < 0) {
+        PyErr_Clear();
+        return nullptr;
+    }
+    const int64_t blocks = (n + 31) / 32;
+    const at::Tensor *c = tensor(codes, device), *s = tensor(scales, device);
+    const auto fits = [](const at::Tensor* t, int64_t pitch) {
+        return t && t->scalar_type() == at::kByte && t->dim() == 2 && t->size(1) == pitch && t->is_contiguous();
+    };
+    if (!fits(c, blocks * 16) || !fits(s, (blocks + 15) / 16 * 16) || c->size(0) != s->size(0)) return nullptr;
+    *q = sllm_mx{c->data_ptr(), s->data_ptr(), (uint64_t)c->size(0), (uint64_t)n};
+    return c;
+}
+
 // A new tensor beside `like`, and its rows.
 inline at::Tensor make(const at::Tensor& like, at::IntArrayRef shape, uint64_t rows, uint32_t code, sllm_matrix* m) {
     at::Tensor t = at::empty(shape, like.options().dtype(kTypes[code]).requires_grad(false));
@@ -84,24 +102,24 @@ T address(PyObject* o) {
         return nullptr;                          \
     }
 
-// product(call, workspace, x, w, dtype, grad, device, stream): x @ w.T, or with
-// `grad` x @ w.  w and dtype as sllm_mx's address and SLLM_DTYPE_*, or -1 for x's.
+// product(call, workspace, x, codes, scales, cols, dtype, grad, device, stream): x @ w.T,
+// or with `grad` x @ w.  dtype as SLLM_DTYPE_*, or -1 for x's.
 inline PyObject* product(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
-    SLLM_PY_ARGS(8, "product(call, workspace, x, w, dtype, grad, device, stream)")
+    SLLM_PY_ARGS(10, "product(call, workspace, x, codes, scales, cols, dtype, grad, device, stream)")
     typedef int32_t (*Call)(const sllm_matrix*, const sllm_mx*, const sllm_matrix*, void*, uint64_t, int32_t, void*);
     typedef int32_t (*Workspace)(const sllm_matrix*, const sllm_mx*, uint64_t*);
     const auto call = address<Call>(args[0]);
     const auto workspace = address<Workspace>(args[1]);
-    const auto* w = address<const sllm_mx*>(args[3]);
-    const long type = PyLong_AsLong(args[4]), grad = PyLong_AsLong(args[5]), device = PyLong_AsLong(args[6]);
-    void* const stream = PyLong_AsVoidPtr(args[7]);
+    const long type = PyLong_AsLong(args[6]), grad = PyLong_AsLong(args[7]), device = PyLong_AsLong(args[8]);
+    void* const stream = PyLong_AsVoidPtr(args[9]);
     if (PyErr_Occurred()) return nullptr;
     const at::Tensor* x = tensor(args[2], device);
     sllm_matrix rows, out_rows;
-    if (!x || !rows_of(*x, &rows)) Py_RETURN_NONE;
-    const uint64_t cols = grad ? w->cols : w->rows;
-    if (!cols || rows.cols != (grad ? w->rows : w->cols)) Py_RETURN_NONE;
+    sllm_mx w;
+    if (!x || !rows_of(*x, &rows) || !mx_of(args[3], args[4], args[5], device, &w)) Py_RETURN_NONE;
+    const uint64_t cols = grad ? w.cols : w.rows;
+    if (!cols || rows.cols != (grad ? w.rows : w.cols)) Py_RETURN_NONE;
     c10::SmallVector<int64_t, 4> shape(x->sizes().begin(), x->sizes().end());
     shape.back() = (int64_t)cols;
     at::Tensor out = make(*x, shape, rows.rows, type < 0 ? rows.dtype : (uint32_t)type, &out_rows), ws;
@@ -109,41 +127,41 @@ inline PyObject* product(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     {
         pybind11::gil_scoped_release no_gil;
         uint64_t n = 0;
-        code = workspace(&rows, w, &n);
+        code = workspace(&rows, &w, &n);
         if (code == SLLM_OK) {
             if (n) ws = bytes(*x, 1, (int64_t)n);
-            code = call(&rows, w, &out_rows, n ? ws.data_ptr() : nullptr, n, (int32_t)device, stream);
+            code = call(&rows, &w, &out_rows, n ? ws.data_ptr() : nullptr, n, (int32_t)device, stream);
         }
     }
     return result(code, std::move(out));
     END_HANDLE_TH_ERRORS
 }
 
-// product_mx(call, workspace, x, w, codes, dtype, device, stream): the same with x
-// in MX FP4, whose codes tell where the result is allocated.
+// product_mx(call, workspace, x's codes, scales, cols, w's codes, scales, cols, dtype, device,
+// stream): the same with x in MX FP4.
 inline PyObject* product_mx(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
-    SLLM_PY_ARGS(8, "product_mx(call, workspace, x, w, codes, dtype, device, stream)")
+    SLLM_PY_ARGS(11, "product_mx(call, workspace, codes, scales, cols, codes, scales, cols, dtype, device, stream)")
     typedef int32_t (*Call)(const sllm_mx*, const sllm_mx*, const sllm_matrix*, void*, uint64_t, int32_t, void*);
     typedef int32_t (*Workspace)(const sllm_mx*, const sllm_mx*, uint64_t*);
     const auto call = address<Call>(args[0]);
     const auto workspace = address<Workspace>(args[1]);
-    const auto *x = address<const sllm_mx*>(args[2]), *w = address<const sllm_mx*>(args[3]);
-    const long type = PyLong_AsLong(args[5]), device = PyLong_AsLong(args[6]);
-    void* const stream = PyLong_AsVoidPtr(args[7]);
+    const long type = PyLong_AsLong(args[8]), device = PyLong_AsLong(args[9]);
+    void* const stream = PyLong_AsVoidPtr(args[10]);
     if (PyErr_Occurred()) return nullptr;
-    const at::Tensor* codes = tensor(args[4], device);
-    if (!codes || !x->rows || !w->rows || x->cols != w->cols) Py_RETURN_NONE;
+    sllm_mx x, w;
+    const at::Tensor* codes = mx_of(args[2], args[3], args[4], device, &x);
+    if (!codes || !mx_of(args[5], args[6], args[7], device, &w) || !x.rows || !w.rows || x.cols != w.cols) Py_RETURN_NONE;
     sllm_matrix out_rows;
-    at::Tensor out = make(*codes, {(int64_t)x->rows, (int64_t)w->rows}, x->rows, (uint32_t)type, &out_rows), ws;
+    at::Tensor out = make(*codes, {(int64_t)x.rows, (int64_t)w.rows}, x.rows, (uint32_t)type, &out_rows), ws;
     int32_t code;
     {
         pybind11::gil_scoped_release no_gil;
         uint64_t n = 0;
-        code = workspace(x, w, &n);
+        code = workspace(&x, &w, &n);
         if (code == SLLM_OK) {
             if (n) ws = bytes(*codes, 1, (int64_t)n);
-            code = call(x, w, &out_rows, n ? ws.data_ptr() : nullptr, n, (int32_t)device, stream);
+            code = call(&x, &w, &out_rows, n ? ws.data_ptr() : nullptr, n, (int32_t)device, stream);
         }
     }
     return result(code, std::move(out));
@@ -177,51 +195,49 @@ inline PyObject* quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
-// dequantize(call, q, codes, dtype, device, stream)
+// dequantize(call, codes, scales, cols, dtype, device, stream)
 inline PyObject* dequantize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
-    SLLM_PY_ARGS(6, "dequantize(call, q, codes, dtype, device, stream)")
+    SLLM_PY_ARGS(7, "dequantize(call, codes, scales, cols, dtype, device, stream)")
     typedef int32_t (*Call)(const sllm_mx*, const sllm_matrix*, int32_t, void*);
     const auto call = address<Call>(args[0]);
-    const auto* q = address<const sllm_mx*>(args[1]);
-    const long type = PyLong_AsLong(args[3]), device = PyLong_AsLong(args[4]);
-    void* const stream = PyLong_AsVoidPtr(args[5]);
+    const long type = PyLong_AsLong(args[4]), device = PyLong_AsLong(args[5]);
+    void* const stream = PyLong_AsVoidPtr(args[6]);
     if (PyErr_Occurred()) return nullptr;
-    const at::Tensor* codes = tensor(args[2], device);
-    if (!codes || !q->rows || !q->cols) Py_RETURN_NONE;
+    sllm_mx q;
+    const at::Tensor* codes = mx_of(args[1], args[2], args[3], device, &q);
+    if (!codes || !q.rows || !q.cols) Py_RETURN_NONE;
     sllm_matrix out_rows;
-    at::Tensor out = make(*codes, {(int64_t)q->rows, (int64_t)q->cols}, q->rows, (uint32_t)type, &out_rows);
+    at::Tensor out = make(*codes, {(int64_t)q.rows, (int64_t)q.cols}, q.rows, (uint32_t)type, &out_rows);
     int32_t code;
     {
         pybind11::gil_scoped_release no_gil;
-        code = call(q, &out_rows, (int32_t)device, stream);
+        code = call(&q, &out_rows, (int32_t)device, stream);
     }
     return result(code, std::move(out));
     END_HANDLE_TH_ERRORS
 }
 
-// lookup(call, table, codes, tokens, scale, dtype, device, stream): table a tensor
-// and codes None, or sllm_mx's address and its codes.
+// lookup(call, table, scales, cols, tokens, scale, dtype, device, stream): table a tensor
+// and scales None, or the codes of one in MX FP4.
 inline PyObject* lookup(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
-    SLLM_PY_ARGS(8, "lookup(call, table, codes, tokens, scale, dtype, device, stream)")
+    SLLM_PY_ARGS(9, "lookup(call, table, scales, cols, tokens, scale, dtype, device, stream)")
     typedef int32_t (*Call)(const void*, const sllm_ids*, float, const sllm_matrix*, int32_t, void*);
     const bool mx = args[2] != Py_None;
-    const double scale = PyFloat_AsDouble(args[4]);
-    const long type = PyLong_AsLong(args[5]), device = PyLong_AsLong(args[6]);
-    void* const stream = PyLong_AsVoidPtr(args[7]);
-    const void* table = mx ? PyLong_AsVoidPtr(args[1]) : nullptr;
+    const double scale = PyFloat_AsDouble(args[5]);
+    const long type = PyLong_AsLong(args[6]), device = PyLong_AsLong(args[7]);
+    void* const stream = PyLong_AsVoidPtr(args[8]);
     const auto call = address<Call>(args[0]);
     if (PyErr_Occurred()) return nullptr;
-    const at::Tensor *like = tensor(mx ? args[2] : args[1], device), *tokens = tensor(args[3], device);
     sllm_matrix rows, out_rows;
+    sllm_mx q;
     sllm_ids ids;
+    const at::Tensor *like = mx ? mx_of(args[1], args[2], args[3], device, &q) : tensor(args[1], device), *tokens = tensor(args[4], device);
     if (!like || !tokens || !ids_of(*tokens, &ids)) Py_RETURN_NONE;
-    if (!mx) {
-        if (like->dim() != 2 || !rows_of(*like, &rows)) Py_RETURN_NONE;
-        table = &rows;
-    }
-    const uint64_t cols = mx ? static_cast<const sllm_mx*>(table)->cols : rows.cols;
+    if (!mx && (like->dim() != 2 || !rows_of(*like, &rows))) Py_RETURN_NONE;
+    const void* const table = mx ? static_cast<const void*>(&q) : &rows;
+    const uint64_t cols = mx ? q.cols : rows.cols;
     if (!cols) Py_RETURN_NONE;
     c10::SmallVector<int64_t, 4> shape(tokens->sizes().begin(), tokens->sizes().end());
     shape.push_back((int64_t)cols);

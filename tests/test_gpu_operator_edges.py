@@ -276,3 +276,18 @@ def test_quantising_what_requires_a_gradient_is_refused():
     want = op.mx4_quantize(x.detach())
     with torch.no_grad():
         assert torch.equal(op.mx4_quantize(x).codes, want.codes)
+
+
+# ---- weights that move ------------------------------------------------------
+
+def test_storage_that_was_exchanged():
+    """A weight is where its tensors are when it is used."""
+    w, _ = random_mx4(48, 64, 1)
+    v, vv = random_mx4(48, 64, 2)
+    x = normal((20, 64), torch.bfloat16, 3)
+    w.codes.data, w.scales.data = v.codes.clone(), v.scales.clone()
+    a = host(x)
+    assert_close(op.mx4_linear(x, w), O.linear(a, vv), sum_bound(a, vv.T, 64), torch.bfloat16)
+    w.codes.data = v.codes[:40].clone()
+    with pytest.raises(ValueError):
+        op.mx4_linear(x, w)
