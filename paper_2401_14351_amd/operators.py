@@ -14,7 +14,8 @@ Operators run on ``stream`` (by default the device's current stream) and return
 without waiting.  Their outputs and workspaces belong to that stream; inputs
 made on another one must be ready for it (``stream.wait_stream(...)``), and are
 kept from reuse until it has passed the call.  ``mx4_linear`` and ``embedding``
-take part in autograd where their input or table requires a gradient.
+take part in autograd where their input or table requires a gradient.  There is
+no forward mode: a tensor with a tangent is refused.
 
 Rows may be apart by any stride, but the elements of a row must be adjacent:
 other tensors are refused, not copied.
@@ -28,6 +29,7 @@ from types import SimpleNamespace
 from typing import Optional, Union
 
 import torch
+import torch.autograd.forward_ad as forward_ad
 
 from paper_2401_14351_amd import binding
 
@@ -207,6 +209,13 @@ def _on_stream(stream, operator, *args, keep=(), **kwargs):
     return result
 
 
+def _refuse_tangent(t):
+    # (unpack_dual looks for the level itself, in half a microsecond more)
+    if getattr(forward_ad, "_current_level", 0) >= 0 and isinstance(t, torch.Tensor) \
+            and forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError("a tensor has a tangent: the operators have no forward mode")
+
+
 def _output(out: Optional[torch.Tensor], shape, rows: int, cols: int, dtype: torch.dtype, like: torch.Tensor):
     """A result of ``rows`` x ``cols`` and its rows: ``out``, or a new tensor where ``like`` is."""
     if out is None:
@@ -217,6 +226,7 @@ def _output(out: Optional[torch.Tensor], shape, rows: int, cols: int, dtype: tor
         return out, binding.Matrix(out.data_ptr(), rows, cols, cols, code, 0)
     if out.shape != torch.Size(shape) or out.device != like.device:
         raise ValueError(f"out: expected shape {tuple(shape)} on {like.device}, got {tuple(out.shape)} on {out.device}")
+    _refuse_tangent(out)
     if out.requires_grad:
         _refuse_grad(out)
     return out, _matrix(out, "out")
@@ -288,6 +298,7 @@ def mx4_quantize(x: torch.Tensor, out: Optional[Mx4] = None, stream=None) -> Mx4
     ``torch.no_grad()``."""
     if stream is not None:
         return _on_stream(stream, mx4_quantize, x, out, keep=(x, out))
+    _refuse_tangent(x)
     if x.requires_grad and torch.is_grad_enabled():
         raise ValueError("x requires a gradient, which quantisation does not pass on")
     device = x.get_device()
@@ -339,6 +350,7 @@ def mx4_linear(x: Union[torch.Tensor, Mx4], w: Mx4, out: Optional[torch.Tensor] 
         return _on_stream(stream, mx4_linear, x, w, out, out_dtype, keep=(x, w, out))
     if isinstance(x, Mx4):
         return _linear_mx(x, w, out, out_dtype)
+    _refuse_tangent(x)
     if x.requires_grad and torch.is_grad_enabled():
         if out is not None:
             raise ValueError("an operator that writes to a given tensor takes no part in autograd")
@@ -384,6 +396,7 @@ def mx4_linear_grad(dy: torch.Tensor, w: Mx4, out: Optional[torch.Tensor] = None
     (..., w.rows)."""
     if stream is not None:
         return _on_stream(stream, mx4_linear_grad, dy, w, out, out_dtype, keep=(dy, w, out))
+    _refuse_tangent(dy)
     _refuse_grad(dy)
     if out is None:
         dx = _product("mx_linear_grad", dy, w, out_dtype, 1)
@@ -426,6 +439,7 @@ def embedding(table: Union[torch.Tensor, Mx4], tokens: torch.Tensor, scale: floa
     a row of zeros."""
     if stream is not None:
         return _on_stream(stream, embedding, table, tokens, scale, out, out_dtype, keep=(table, tokens, out))
+    _refuse_tangent(table)
     if not isinstance(table, Mx4) and table.requires_grad and torch.is_grad_enabled():
         if out is not None:
             raise ValueError("an operator that writes to a given tensor takes no part in autograd")
@@ -469,6 +483,7 @@ def embedding_grad(dy: torch.Tensor, tokens: torch.Tensor, vocab: int, scale: fl
     if stream is not None:
         return _on_stream(stream, embedding_grad, dy, tokens, vocab, scale, out, out_dtype, accumulate,
                           keep=(dy, tokens, out))
+    _refuse_tangent(dy)
     _refuse_grad(dy)
     if accumulate and out is None:
         raise ValueError("accumulate needs a gradient to add to")

@@ -278,6 +278,32 @@ def test_quantising_what_requires_a_gradient_is_refused():
         assert torch.equal(op.mx4_quantize(x).codes, want.codes)
 
 
+def test_tangents_are_refused():
+    import torch.autograd.forward_ad as forward
+
+    w, _ = random_mx4(48, 64, 1)
+    x, dy = normal((9, 64), torch.float32, 2), normal((9, 48), torch.float32, 3)
+    ids = torch.arange(9, device="cuda")
+    with forward.dual_level():
+        a, b = forward.make_dual(x, torch.ones_like(x)), forward.make_dual(dy, torch.ones_like(dy))
+        for call in (lambda: op.mx4_linear(a, w), lambda: op.mx4_linear_grad(b, w), lambda: op.embedding(a, ids),
+                     lambda: op.embedding_grad(a, ids, 9), lambda: op.mx4_quantize(a),
+                     lambda: op.mx4_linear(x, w, out=b), lambda: op.embedding(x, ids, out=a)):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        plain = op.mx4_linear(x, w)  # others are carried out
+    assert torch.equal(plain, op.mx4_linear(x, w))
+
+
+def test_transformed_tensors_are_refused():
+    """Tensors of torch.func's transforms have no memory of their own."""
+    w, _ = random_mx4(48, 64, 1)
+    x = normal((3, 9, 64), torch.float32, 2)
+    for transform in (torch.vmap, lambda f: torch.func.grad(lambda x: f(x).sum()), lambda f: lambda x: torch.func.jvp(f, (x,), (x,))):
+        with pytest.raises((RuntimeError, ValueError)):
+            transform(lambda x: op.mx4_linear(x, w))(x)
+
+
 # ---- weights that move ------------------------------------------------------
 
 def test_storage_that_was_exchanged():
