@@ -17,8 +17,9 @@ kept from reuse until it has passed the call.  ``mx4_linear`` and ``embedding``
 take part in autograd where their input or table requires a gradient.  There is
 no forward mode: a tensor with a tangent is refused.
 
-Rows may be apart by any stride, but the elements of a row must be adjacent:
-other tensors are refused, not copied.
+Rows may be apart by any stride that keeps them from overlapping, but the
+elements of a row must be adjacent: other tensors, broadcast ones among them, are
+refused, not copied.
 """
 
 from __future__ import annotations
@@ -138,6 +139,8 @@ def _matrix(t: torch.Tensor, name: str) -> binding.Matrix:
         raise ValueError(f"{name}: {t.dtype} is not float32, float16 or bfloat16")
     if not t.is_cuda:
         raise ValueError(f"{name} is not in device memory")
+    if t.is_neg():
+        raise ValueError(f"{name} is a negated view of other elements")
     dim = t.dim()
     if dim == 0:
         raise ValueError(f"{name} has no dimensions")
@@ -169,6 +172,8 @@ def _ids(t: torch.Tensor) -> binding.Ids:
         raise ValueError("tokens are not in device memory")
     if not t.is_contiguous():
         raise ValueError(f"tokens are not contiguous (strides {t.stride()})")
+    if t.is_neg():
+        raise ValueError("tokens are a negated view of others")
     return binding.Ids(t.data_ptr(), t.numel(), bits, 0)
 
 

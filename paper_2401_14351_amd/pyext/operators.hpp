@@ -33,7 +33,7 @@ constexpr at::ScalarType kTypes[] = {at::kFloat, at::kHalf, at::kBFloat16};  // 
 inline const at::Tensor* tensor(PyObject* o, int64_t device) {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor& t = THPVariable_Unpack(o);
-    return t.is_cuda() && t.layout() == at::kStrided && t.get_device() == device ? &t : nullptr;
+    return t.is_cuda() && t.layout() == at::kStrided && t.get_device() == device && !t.is_neg() ? &t : nullptr;
 }
 
 // The rows of t, its last dimension's runs of elements.

@@ -205,6 +205,24 @@ def test_product_with_a_weight_of_many_rows():
     assert not y.any()
 
 
+# ---- tensors whose memory is not what they stand for ------------------------
+
+def test_negated_views_are_refused():
+    x = normal((4, 96), torch.float32, 1)
+    w, _ = random_mx4(8, 96, 2)
+    z = torch.complex(normal((4, 1), torch.float32, 3), normal((4, 1), torch.float32, 4)).conj().imag
+    assert z.is_neg()
+    thin, _ = random_mx4(8, 1, 5)
+    neg = torch._neg_view(x)
+    for call in (lambda: op.mx4_linear(neg, w), lambda: op.mx4_linear(z, thin), lambda: op.mx4_quantize(neg),
+                 lambda: op.embedding(neg, torch.zeros(3, dtype=torch.int64, device="cuda")),
+                 lambda: op.embedding(x, torch._neg_view(torch.zeros(3, dtype=torch.int64, device="cuda"))),
+                 lambda: op.embedding_grad(neg, torch.zeros(4, dtype=torch.int64, device="cuda"), 3),
+                 lambda: op.mx4_dequantize(w, out=torch._neg_view(normal((8, 96), torch.float32, 6)))):
+        with pytest.raises(ValueError, match="negat"):
+            call()
+
+
 # ---- autograd ---------------------------------------------------------------
 
 def test_a_changed_weight_raises_in_backward():
