@@ -551,7 +551,8 @@ int32_t sllm_mx_dequantize(const sllm_mx* src, const sllm_matrix* dst, int32_t d
 
 /* out = x * transpose(w): x has m rows of k elements, w is n x k, out m x n.
  * The products of x's elements, in their own type, with the values w stands
- * for are not rounded before they are summed. */
+ * for are not rounded before they are summed; elements of x below 2^-110 in
+ * magnitude count to within 2^-133. */
 int32_t sllm_mx_linear(const sllm_matrix* x, const sllm_mx* w, const sllm_matrix* out, void* workspace,
                        uint64_t workspace_bytes, int32_t device, void* stream);
 
@@ -559,8 +560,8 @@ int32_t sllm_mx_linear(const sllm_matrix* x, const sllm_mx* w, const sllm_matrix
 int32_t sllm_mx_linear_mx(const sllm_mx* x, const sllm_mx* w, const sllm_matrix* out, void* workspace,
                           uint64_t workspace_bytes, int32_t device, void* stream);
 
-/* dx = dy * w, the gradient of sllm_mx_linear by x: dy has m rows of n
- * elements, w is n x k, dx m x k. */
+/* dx = dy * w, the gradient of sllm_mx_linear by x, with the same sums: dy has
+ * m rows of n elements, w is n x k, dx m x k. */
 int32_t sllm_mx_linear_grad(const sllm_matrix* dy, const sllm_mx* w, const sllm_matrix* dx, void* workspace,
                             uint64_t workspace_bytes, int32_t device, void* stream);
 

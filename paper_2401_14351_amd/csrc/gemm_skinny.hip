@@ -15,9 +15,9 @@ __device__ __forceinline__ uint32_t upper_halves(float a, float b) {
     return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
 }
 
-// Eight elements of x as the bfloat16 vectors whose sum they are: each but the
-// last takes the leading eight bits of what is left.  An infinity or a NaN is
-// whole in the first.
+// Eight elements of x as the bfloat16 vectors whose sum they are, as far down as
+// bfloat16's smallest step: each but the last takes the leading eight bits of what
+// is left.  An infinity or a NaN is whole in the first.
 template <typename X>
 struct Parts {
     static constexpr int n = sizeof(X) == 4 ? 3 : 2;

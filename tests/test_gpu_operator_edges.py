@@ -107,6 +107,25 @@ def test_linear_half_outliers(m, n, k):
         assert_close(op.mx4_linear_grad(dy, w, out_dtype=torch.float32), O.linear_grad(b, wv), sum_bound(b, wv, n), torch.float32)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,n", [(1, 40), (4, 40), (16, 40), (40, 40), (300, 300)])
+def test_linear_of_very_small_elements(dtype, m, n):
+    """Elements below 2^-110 count to within 2^-133, which is bfloat16's smallest step; sums that are
+    subnormal are off by half of float32's smallest step each."""
+    depth = 96
+    w, wv = random_mx4(n, depth, 8, (120, 150))
+    rng = np.random.default_rng(9)
+    v = np.ldexp(rng.uniform(1, 2, (m, depth)), rng.integers(-149, -100, (m, depth))) * rng.choice([-1, 1], (m, depth))
+    x = torch.from_numpy(v.astype(np.float32)).cuda().to(dtype)
+    a = host(x)
+    small = np.full_like(a, 2.0 ** -133)
+    bound = sum_bound(a, wv.T, depth) + small @ np.abs(wv).T + depth * 2.0 ** -149
+    assert_close(op.mx4_linear(x, w, out_dtype=torch.float32), O.linear(a, wv), bound, torch.float32)
+    g, gv = random_mx4(depth, n, 10, (120, 150))
+    bound = sum_bound(a, gv, depth) + small @ np.abs(gv) + depth * 2.0 ** -149
+    assert_close(op.mx4_linear_grad(x, g, out_dtype=torch.float32), O.linear_grad(a, gv), bound, torch.float32)
+
+
 # ---- what is not finite -----------------------------------------------------
 
 def assert_same_kind(got, want):
