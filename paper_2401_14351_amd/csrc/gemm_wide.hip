@@ -35,6 +35,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
     // two stages each.
     __shared__ __align__(16) uint8_t x0[kXBytes], x1[kXBytes];
     __shared__ __align__(16) uint8_t w0[kWBytes + kScaleBytes], w1[kWBytes + kScaleBytes];
+    __shared__ uint32_t ranges[kHalf ? BM : 1];
     __shared__ uint32_t marks[kHalf ? kMarkWords : 1];  // stages with blocks of W that are added afterwards
     uint8_t* const x_ring[2] = {x0, x1};
     uint8_t* const w_ring[2] = {w0, w1};
@@ -132,14 +133,16 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void wide_product(WideArgs a, T* ou
     bool fits = true;  // this lane's rows of x
     _Float16 factor[FM];
     float unit[FM];
-    if constexpr (kHalf)
+    if constexpr (kHalf) {
+        if (!a.ranges) find_tile_ranges<BM, kWaves * 64>(a, m0, t0, t1, ranges);
 #pragma unroll
         for (int m = 0; m < FM; ++m) {
-            const uint32_t range = a.ranges[min(m0 + (wm * FM + m) * 32 + r, a.m - 1)];
+            const uint32_t row = (wm * FM + m) * 32 + r, range = a.ranges ? a.ranges[min(m0 + row, a.m - 1)] : ranges[row];
             fits &= row_fits(range);
             factor[m] = (_Float16)(float)(1 << row_shift(range));
             unit[m] = 1.0f / (1 << (row_shift(range) + kHalfShift));
         }
+    }
     auto multiply = [&](const Fragments& f) SLLM_INLINE {
         u32x4 x[FM];
 #pragma unroll

@@ -123,8 +123,8 @@ struct Plan {
     uint32_t tile_m = 0, tile_n = 0, steps = 0, splits = 1;
     uint32_t tiles_m = 0, tiles_j = 0;
     uint64_t x_bytes = 0, split_stride = 0, bytes = 0;
-    bool half = false;         // x is multiplied in float16, by the ranges of its rows,
-    uint64_t ranges_at = 0;    // which are here in the workspace
+    bool ranges = false;       // those of a float16 x's rows are found first, to be
+    uint64_t ranges_at = 0;    // here in the workspace
 };
 
 // Whether a product goes to the kernel of few rows.  It reads all of x for every
@@ -190,9 +190,15 @@ Plan plan_linear(const LinearLaunch& a) {
     if (p.staged) p.x_bytes = (a.m * p.parts * p.part_stride * 2 + 255) / 256 * 256;
     p.split_stride = a.m * ((p.cols + 3) / 4 * 4);
     p.bytes = p.x_bytes + (p.splits > 1 ? p.splits * p.split_stride * 4 : 0);
-    p.half = !a.x.codes && a.x.dtype == SLLM_DTYPE_F16;
+    // A workgroup finds the ranges of its own piece of a float16 x where that is small;
+    // with a kernel before (in us, 64 rows by 768 x 768, a piece of 48 KB, 10.3 and 11.4;
+    // 1024 x 1024 x 1024, 64 KB, 16.7 and 17.7; 1000 x 2000 x 2000, 128 KB, 28.2 and 26.4;
+    // 1024 x 4096 x 4096, 512 KB, 72 and 59).  Where x is copied first that goes along.
+    constexpr uint64_t kOwnRanges = 64 << 10;
+    p.ranges = !a.x.codes && a.x.dtype == SLLM_DTYPE_F16 &&
+               (p.staged || ceil_div(p.steps, p.splits) * kWideStep * p.tile_m * 2 > kOwnRanges);
     p.ranges_at = p.bytes;
-    if (p.half) p.bytes += a.m * 4;
+    if (p.ranges) p.bytes += a.m * 4;
     return p;
 }
 
@@ -225,45 +231,40 @@ __global__ __launch_bounds__(256) void split_x(const T* x, uint64_t stride, uint
 }
 
 // The range of each row of a float16 x (products.hpp says of what), a wave each, or where
-// rows are long a workgroup.  Vec: rows start on 16 bytes.
-template <bool Vec, int Lanes>
-__global__ __launch_bounds__(256) void find_ranges(const uint16_t* x, uint64_t stride, uint64_t rows, uint64_t cols, uint32_t* ranges) {
-    __shared__ uint32_t waves[2][4];
+// rows are long a workgroup; with Copy each row is written to `out` too, as split_x does.
+// Vec: rows start on 16 bytes.  Bound by memory: 4096 x 8192 from cold memory 25.8 us, 13
+// where the last-level cache has it; 64 x 4096 2.8.
+template <bool Vec, bool Copy, int Lanes>
+__global__ __launch_bounds__(256) void find_ranges(const uint16_t* x, uint64_t stride, uint64_t rows, uint64_t cols, uint64_t pitch,
+                                                   uint16_t* out, uint32_t* ranges) {
+    __shared__ uint32_t waves[4];
     const uint64_t row = (uint64_t)block_index() * (256 / Lanes) + threadIdx.x / Lanes;
     const uint16_t* at = x + min(row, rows - 1) * stride;
-    uint32_t top = 0, bottom = 0xffff;
+    RowRange range;
     for (uint64_t c = threadIdx.x % Lanes * 8; c < cols; c += Lanes * 8) {
-        uint16_t e[8];
+        u32x4 v;
         if (Vec && c + 8 <= cols) {
-            const u32x4 v = *reinterpret_cast<const u32x4*>(at + c);
-            __builtin_memcpy(e, &v, sizeof e);
+            v = *reinterpret_cast<const u32x4*>(at + c);
         } else {
+            uint16_t e[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? at[c + i] : 0;
+            __builtin_memcpy(&v, e, sizeof v);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t size = e[i] & 0x7fff;
-            top = max(top, size);
-            bottom = min(bottom, (size - 1) & 0xffff);
-        }
+        range.add(v);
+        if (Copy && row < rows) *reinterpret_cast<u32x4*>(out + row * pitch + c) = v;
     }
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) {
-        top = max(top, (uint32_t)__shfl_xor(top, d));
-        bottom = min(bottom, (uint32_t)__shfl_xor(bottom, d));
-    }
+    range.join(64);
     if constexpr (Lanes > 64) {
-        const uint32_t wave = threadIdx.x / 64;
-        if (threadIdx.x % 64 == 0) waves[0][wave] = top, waves[1][wave] = bottom;
+        if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = range.word();
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            top = max(top, waves[0][w]);
-            bottom = min(bottom, waves[1][w]);
+            range.top = max(range.top, waves[w] & 0xffff);
+            range.bottom = min(range.bottom, waves[w] >> 16);
         }
     }
-    if (threadIdx.x % Lanes == 0 && row < rows) ranges[row] = bottom << 16 | top;
+    if (threadIdx.x % Lanes == 0 && row < rows) ranges[row] = range.word();
 }
 
 // The sum of the splits' matrices, first to last, so that every call adds in the
@@ -288,30 +289,33 @@ int32_t join(const Plan& p, const float* sums, uint32_t splits, const LinearLaun
     return SLLM_OK;
 }
 
-// x as the wide kernel reads it, written out in the workspace where it is not so already.
+// x as the wide kernel reads it, written out in the workspace where it is not so already,
+// and the ranges of a float16 one.
 int32_t stage_x(const LinearLaunch& a, const Plan& p, void* workspace, WideArgs* w, hipStream_t stream) {
     w->x = static_cast<const uint16_t*>(a.x.data);
     w->x_stride = a.x.stride, w->part_stride = 0;
-    if (!p.staged) return SLLM_OK;
+    w->ranges = nullptr;
     uint16_t* x = static_cast<uint16_t*>(workspace);
-    w->x = x;
-    w->x_stride = p.parts * p.part_stride;
-    w->part_stride = p.part_stride;
+    if (p.staged) {
+        w->x = x;
+        w->x_stride = p.parts * p.part_stride;
+        w->part_stride = p.part_stride;
+    }
     const dim3 blocks = grid_of(ceil_div(a.m * p.part_stride / 8, 256));
-    if (p.parts == 1)
+    if (p.ranges) {
+        uint32_t* ranges = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + p.ranges_at);
+        const uint16_t* from = static_cast<const uint16_t*>(a.x.data);
+        const bool vec = reinterpret_cast<uintptr_t>(from) % 16 == 0 && (a.m == 1 || a.x.stride % 8 == 0), wide = p.depth > 1024;
+        const auto kernel = p.staged ? (vec ? (wide ? find_ranges<true, true, 256> : find_ranges<true, true, 64>)
+                                            : (wide ? find_ranges<false, true, 256> : find_ranges<false, true, 64>))
+                                     : (wide ? find_ranges<true, false, 256> : find_ranges<true, false, 64>);
+        kernel<<<grid_of(ceil_div(a.m, wide ? 1 : 4)), 256, 0, stream>>>(from, a.x.stride, a.m, p.depth, p.part_stride, x, ranges);
+        w->ranges = ranges;
+    } else if (p.staged && p.parts == 1) {
         split_x<uint16_t, 1><<<blocks, 256, 0, stream>>>(static_cast<const uint16_t*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
-    else
+    } else if (p.staged) {
         split_x<float, 3><<<blocks, 256, 0, stream>>>(static_cast<const float*>(a.x.data), a.x.stride, a.m, p.depth, p.part_stride, x);
-    SLLM_HIP(hipGetLastError());
-    return SLLM_OK;
-}
-
-int32_t launch_ranges(const LinearLaunch& a, const Plan& p, uint32_t* ranges, hipStream_t stream) {
-    const uint16_t* x = static_cast<const uint16_t*>(a.x.data);
-    const bool vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && (a.m == 1 || a.x.stride % 8 == 0), wide = p.depth > 1024;
-    const dim3 blocks = grid_of(ceil_div(a.m, wide ? 1 : 4));
-    const auto kernel = vec ? (wide ? find_ranges<true, 256> : find_ranges<true, 64>) : (wide ? find_ranges<false, 256> : find_ranges<false, 64>);
-    kernel<<<blocks, 256, 0, stream>>>(x, a.x.stride, a.m, p.depth, ranges);
+    }
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
 }
@@ -334,9 +338,6 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
     } else {
         WideArgs w;
         SLLM_TRY(stage_x(a, p, workspace, &w, stream));
-        uint32_t* ranges = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + p.ranges_at);
-        if (p.half) SLLM_TRY(launch_ranges(a, p, ranges, stream));
-        w.ranges = ranges;
         w.m = a.m, w.depth = p.depth;
         w.parts = p.parts, w.steps = p.steps;
         w.w_codes = reinterpret_cast<const u32x4*>(a.w_codes);
@@ -344,7 +345,7 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
         w.w_rows = a.n, w.w_blocks = mx_blocks(a.k), w.w_scale_pitch = mx_scale_pitch(a.k);
         w.tiles_m = p.tiles_m, w.tiles_j = p.tiles_j;
         w.out_args = o;
-        SLLM_TRY((a.grad ? launch_grad : launch_wide)(w, p.half, p.tile_m, p.splits, out, dtype, stream));
+        SLLM_TRY((a.grad ? launch_grad : launch_wide)(w, a.x.dtype == SLLM_DTYPE_F16, p.tile_m, p.splits, out, dtype, stream));
     }
     return p.splits > 1 ? join(p, static_cast<const float*>(out), p.splits, a, stream) : SLLM_OK;
 }

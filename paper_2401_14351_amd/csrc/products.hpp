@@ -6,6 +6,7 @@
 namespace sllm {
 
 constexpr uint32_t kTileRows = 4;  // of tiles that neighbouring workgroups share
+constexpr uint32_t kWideStep = 64;   // depth of a stage
 
 // Where a product's sums go: m x cols, or, where the depth is split over
 // workgroups (blockIdx.y), a 32-bit matrix per split, one after another.
@@ -21,7 +22,7 @@ struct WideArgs {
     uint64_t m, depth;       // of a part
     uint64_t x_stride, part_stride;
     uint32_t parts, steps;   // steps of a part, an even number
-    const uint32_t* ranges;  // of the rows of a float16 x
+    const uint32_t* ranges;  // of the rows of a float16 x; null: each workgroup finds those of its piece
     const u32x4* w_codes;
     const uint8_t* w_scales;
     uint64_t w_rows, w_blocks, w_scale_pitch;
@@ -173,12 +174,13 @@ __device__ __forceinline__ f32x16 product(u32x4 w, u32x4 x, f32x16 acc) {
 //     zeros, are left out, their stages marked, and added afterwards in bfloat16, x in
 //     two parts.
 //   * A row of x is multiplied by up to 2^10, which makes 2^-24, the smallest element, a
-//     normal number, but by no more than its largest element allows (a kernel before
-//     finds both).  Where a row has elements more than 2^29 apart, or an infinity or a
-//     NaN, its workgroups take all stages in bfloat16.
+//     normal number, but by no more than its largest element allows; a kernel before, or
+//     where that is quicker the workgroup itself, finds both.  Where a row has elements
+//     more than 2^29 apart, or an infinity or a NaN, its workgroups take all stages in
+//     bfloat16.
 // 4096 x 8192 by 8192 takes 507 us (a bfloat16 x 410), 518 with a block left out in every
 // tile, 2100 where every tile has such a row or leaves all of W out; 64 rows by 4096 x
-// 4096 18.2 (13.6), of which 4 are the kernel before.
+// 4096 17.3 (13.6).
 constexpr int kHalfShift = 8;
 constexpr uint32_t kHalfScale = 127 - 21, kHalfScales = 27;
 
@@ -201,9 +203,45 @@ __device__ __forceinline__ bool marked(const uint32_t* marks, uint32_t t) { retu
 
 // A row's range: the bits of its largest magnitude, and above them those of its smallest
 // but zero, less one (all ones where it is all zeros).
+struct RowRange {
+    uint32_t top = 0, bottom = 0xffff;
+
+    __device__ __forceinline__ void add(u32x4 v) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t size = v[i / 2] >> i % 2 * 16 & 0x7fff;
+            top = max(top, size);
+            bottom = min(bottom, (size - 1) & 0xffff);
+        }
+    }
+    // Of `lanes` neighbours, a power of two.
+    __device__ __forceinline__ void join(int lanes) {
+        for (int d = lanes / 2; d > 0; d /= 2) {
+            top = max(top, (uint32_t)__shfl_xor(top, d));
+            bottom = min(bottom, (uint32_t)__shfl_xor(bottom, d));
+        }
+    }
+    __device__ __forceinline__ uint32_t word() const { return bottom << 16 | top; }
+};
 __device__ __forceinline__ int row_shift(uint32_t range) { return min(10, 30 - min(30, (int)(range >> 10 & 31))); }
 __device__ __forceinline__ bool row_fits(uint32_t range) {
     return (range & 0xffff) < 0x7c00 && ((range >> 16) + 1) << row_shift(range) >= 0x400;
+}
+
+// The ranges of a workgroup's rows from m0 on, of stages t0 .. t1 - 1 alone, into LDS.
+template <int Rows, int Threads>
+__device__ __forceinline__ void find_tile_ranges(const WideArgs& a, uint64_t m0, uint32_t t0, uint32_t t1, uint32_t* ranges) {
+    constexpr uint32_t kLanes = Threads / Rows;
+    const uint32_t row = threadIdx.x / kLanes;
+    const uint16_t* x = a.x + min(m0 + row, a.m - 1) * a.x_stride;
+    const uint64_t end = min((uint64_t)t1 * kWideStep, a.depth);
+    RowRange range;
+#pragma unroll 4
+    for (uint64_t c = (uint64_t)t0 * kWideStep + threadIdx.x % kLanes * 8; c < end; c += kLanes * 8)
+        range.add(*reinterpret_cast<const u32x4*>(x + c));
+    range.join(kLanes);
+    if (threadIdx.x % kLanes == 0) ranges[row] = range.word();
+    __syncthreads();
 }
 
 // A vector of float16 as the sum of two in bfloat16: the leading eight bits of
@@ -337,6 +375,5 @@ int32_t launch_grad(const WideArgs& a, bool half, uint32_t tile_m, uint32_t spli
 // Rows of x and columns of the output a workgroup holds; small tiles may be 64 or
 // 32 rows tall (`tile_m`) where x is not in MX FP4.
 constexpr uint32_t kLargeTile = 256, kSmallTile = 128;
-constexpr uint32_t kWideStep = 64;   // depth of a stage
 
 }  // namespace sllm
