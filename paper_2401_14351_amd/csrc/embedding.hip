@@ -73,8 +73,9 @@ __device__ __forceinline__ void store8(T* row, uint32_t c, uint32_t dim, const f
 // `lanes` of them a row at a time: 16 bytes a store, and of a row in MX FP4 a word
 // of codes.  Bound by memory: 8191 rows of 8192 columns from bfloat16 54 us, 5.0
 // TB/s, from MX FP4 36 us, 4.7 TB/s (25 where the last-level cache has the table);
-// 16 rows are bound by their two loads one after the other, 2.9 us.  S: the table's elements, void for MX FP4.
-// Vec: rows start on 16 bytes and end on a multiple of eight columns.
+// 16 rows are bound by their two loads one after the other, 3 us.  S: the table's
+// elements, void for MX FP4.  Vec: rows start on 16 bytes and end on a multiple of eight
+// columns.
 template <bool Vec, typename S, typename T>
 __global__ __launch_bounds__(256) void lookup(Lookup a, T* out) {
     const uint64_t i = (uint64_t)block_index() * (256 / a.lanes) + threadIdx.x / a.lanes;
@@ -82,7 +83,8 @@ __global__ __launch_bounds__(256) void lookup(Lookup a, T* out) {
     const int64_t row = a.ids.p ? id_at(a.ids, i, a.vocab) : (int64_t)i;
     const uint32_t blocks = (a.dim + 31) / 32, pitch = (blocks + 15) / 16 * 16;
     // A word of codes a lane does not fill the memory's latency: several are under way
-    // (8191 rows of 8192 36 us, one at a time 43).
+    // (8191 rows of 8192 from cold memory 36 us, one at a time 43; rows of 2048, where a
+    // lane has one word, 27.7 and 26.4).
     constexpr uint32_t kTogether = __is_same(S, void) ? 4 : 1;
     for (uint32_t c0 = threadIdx.x % a.lanes * 8; c0 < a.dim; c0 += kTogether * a.lanes * 8) {
         float v[kTogether][8] = {};
@@ -176,7 +178,7 @@ __device__ __forceinline__ void sort_tile(uint32_t t, uint32_t& key, uint32_t* k
 // Bitonic sort of a tile, a key a lane: partners up to 32 lanes away by lane
 // exchanges, the others through LDS.  A tile's key is the token and ten bits of
 // the position in 32 bits, where the table has fewer than 2^22 rows; 2,048 ids
-// then take 4.5 us, 9.4 with keys of 64 bits.
+// then take 5.1 us, 9.4 with keys of 64 bits.
 __global__ __launch_bounds__(1024) void sort_tiles(Ids ids, uint32_t n, uint32_t vocab, uint64_t* out) {
     __shared__ uint32_t keys[kSortTile];
     const uint32_t t = threadIdx.x, first = blockIdx.x * kSortTile, i = first + t;

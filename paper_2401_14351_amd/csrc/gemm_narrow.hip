@@ -14,9 +14,11 @@ constexpr uint32_t kStepBlocks = kNarrowStep / kMxBlock;
 constexpr uint32_t kStageBlocks = 4;  // of a stage: 64 bytes a row
 
 // out[m][n] = sum over k of x[m][k] W[n][k], both in four bits, in 32 bits: the
-// scaled matrix instruction takes codes and scales as they are stored.  Bound by
-// what the matrix cores draw: 4096 x 8192 by 28672 takes 500 us, 3.8 PF/s, the
-// matrix cores busy half of the cycles at 1.6 GHz (alone they reach 7).
+// scaled matrix instruction takes codes and scales as they are stored.  4096 x 8192 by
+// 28672 takes 500 to 540 us, 3.6 to 3.85 PF/s: the matrix cores are busy 48 % of the
+// cycles at 1.85 to 1.9 GHz, alone 6.8 to 7.3 PF/s at 1.63 to 1.94.  LDS is in use 38 % of
+// the cycles, over a third of that conflicts, whose cause, the fragments' reads or those of
+// the scales, has not been separated.
 //
 // A stage of 128 of the depth is 64 bytes a row: four of them are in flight, loaded
 // straight to LDS, and waited for by their number, not all together.  512 of the

@@ -12,9 +12,12 @@ namespace {
 
 constexpr uint32_t kStep = kWideStep;
 
-// out[m][j] = sum over k of x[m][k] W[j][k], in 32 bits.  Bound by what the matrix
-// cores draw: 4096 x 8192 by 8192 takes 420 to 490 us by card, 1.1 to 1.3 PF/s, the
-// matrix cores busy half of the cycles at 1.7 GHz (alone they reach 1.8 PF/s, at 1.9).
+// out[m][j] = sum over k of x[m][k] W[j][k], in 32 bits.  4096 x 8192 by 8192, two
+// rounds of tiles, takes 405 to 475 us by card and load, 1.2 to 1.35 PF/s: the matrix
+// cores are busy 62 % of the cycles, at the 1.95 GHz that power leaves (alone they reach
+// 1.8 PF/s, at 1.9).  1999 x 5120 by 13824, 432 tiles on 256 CUs, takes 241 us and keeps
+// them busy 50 %: a sixth of the two rounds is empty.  LDS is in use 16 to 19 % of the
+// cycles, one access cycle in 50 a conflict.
 //
 // Both operands go to LDS by loads that pass no registers, two stages of 64 of the
 // depth ahead.  W stays in four bits up to a lane's registers and becomes bfloat16

@@ -115,7 +115,7 @@ __device__ __forceinline__ Tile tile_of(uint32_t block, uint32_t tiles_m, uint32
 // are 128 bytes: eight lanes load one, whole, and a load straight to LDS puts
 // lane l's bytes at 16 l, so the order of a row's chunks is chosen by what each
 // lane loads.  It changes every other row, so that 16 rows read in one column of
-// chunks are in all banks once.  chunk_at(r, c ^ s) is chunk_at(r, c) ^ 16 s.
+// chunks, by 16 neighbouring lanes, are in all banks once.  chunk_at(r, c ^ s) is chunk_at(r, c) ^ 16 s.
 __device__ __forceinline__ uint32_t chunk_at(uint32_t r, uint32_t c) { return r * 128 + (c ^ (r >> 1 & 7)) * 16; }
 
 // The same for rows of 64 bytes, four chunks: four rows are in all banks once.
