@@ -88,6 +88,27 @@ def test_linear_half_normal_over_zero(m, n):
     assert_close(op.mx4_linear_grad(x, g, out_dtype=torch.float32), O.linear_grad(a, gv), sum_bound(a, gv, depth), torch.float32)
 
 
+@pytest.mark.parametrize("depth", [203, 1501, 4096])
+@pytest.mark.parametrize("first", [0, 1, 8])
+def test_linear_half_ranges_of_any_rows(depth, first):
+    """Rows copied first, by a wave or a workgroup each, and rows that are not: their ranges are their own."""
+    m, n = 70, 300
+    w, _ = random_mx4(n, depth, 7, (118, 128))
+    w.codes[:, 16:] = 0  # sums of 32 products, so that no bits are lost in larger ones
+    wv = values(w)
+    base = spread((m, depth + 16), 8, -24, -13)  # rows start on 16 bytes for one depth and two firsts
+    base[::3] *= 2.0 ** 13
+    base[1::3, first + 40] = 40000  # the smallest elements and a large one, over a weight of zero
+    x = base[:, first:first + depth]
+    a = host(x)
+    assert_close(op.mx4_linear(x, w, out_dtype=torch.float32), O.linear(a, wv), sum_bound(a[:, :32], wv[:, :32].T, 32), torch.float32)
+    g, _ = random_mx4(depth, n, 9, (118, 128))
+    g.codes[32:] = 0
+    gv = values(g)
+    assert_close(op.mx4_linear_grad(x, g, out_dtype=torch.float32), O.linear_grad(a, gv), sum_bound(a[:, :32], gv[:32], 32),
+                 torch.float32)
+
+
 @pytest.mark.parametrize("m,n,k", ROWS)
 def test_linear_half_outliers(m, n, k):
     """Elements up to float16's largest beside its smallest, a few of each."""
