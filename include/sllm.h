@@ -592,6 +592,65 @@ int32_t sllm_embedding_grad(const sllm_matrix* dy, const sllm_ids* ids, float sc
                             void* stream);
 int32_t sllm_embedding_grad_workspace(uint64_t n_ids, const sllm_matrix* grad, uint64_t* bytes);
 
+/* Rows of tokens and heads in device memory, aligned to their element type: head h of
+ * token t starts at data + t * token_stride + h * head_stride elements and its
+ * `dim` elements are adjacent.  Rows do not overlap: either a token's heads lie within
+ * its stride or a head's tokens do.  At most 2^30 rows, and 128 elements each (RANGE). */
+typedef struct sllm_heads {
+    void*    data;
+    uint64_t tokens, heads, dim;
+    uint64_t token_stride, head_stride;  /* elements; any value for one token or head */
+    uint32_t dtype;                      /* SLLM_DTYPE_F32, _F16 or _BF16 */
+    uint32_t reserved;                   /* must be 0 */
+} sllm_heads;
+
+/* Causal attention with a sliding window and sinks, over packed sequences:
+ *   out = softmax over the keys seen of (scale * q . key) times their values
+ * The query at position i of its sequence sees the key at position j of the same one
+ * where j <= i and (i - j < window or j < sinks); window 0: every j <= i.  q and out are
+ * tokens x heads x dim, k and v tokens x kv_heads x dim, of one dtype; heads is a multiple
+ * of kv_heads, and head h has the keys of head h / (heads / kv_heads).  Sequence s is
+ * tokens offsets[s] to offsets[s + 1] - 1; NULL: all of them.  Offsets that go back, or lie
+ * outside the tokens, are taken as the nearest that do not.  Tokens of no sequence have an
+ * output of zeros.
+ *
+ * Scores, their running maximum and sum, and the output's sums are held in 32 bits;
+ * weights are rounded to the dtype before they are multiplied with values, as the largest
+ * weight of a row so far, or up to 2^8 times that, is one.  What a query does not see does
+ * not count, infinities and NaN included.  scale is a positive number.
+ *
+ * lse, if not NULL: tokens x heads floats, the logarithm of the sum of exp(scale * q . key)
+ * over the keys seen (zero for tokens of no sequence), for the gradient. */
+int32_t sllm_attention(const sllm_heads* q, const sllm_heads* k, const sllm_heads* v, const sllm_ids* offsets,
+                       uint64_t window, uint64_t sinks, float scale, const sllm_heads* out, float* lse,
+                       int32_t device, void* stream);
+
+/* Keys and values of sequences, each (sequences, heads, sinks + window, dim), contiguous:
+ * position p is in slot p where p < sinks, and else in slot sinks + (p - sinks) % window,
+ * which holds the last position that has been there. */
+typedef struct sllm_kv_cache {
+    void*    k;
+    void*    v;
+    uint64_t sequences, heads, dim;
+    uint64_t window, sinks;  /* window at least 1, both at most 2^30 together (RANGE) */
+    uint32_t dtype;
+    uint32_t reserved;       /* must be 0 */
+} sllm_kv_cache;
+
+/* The same attention of new tokens behind those in the cache, with its window and sinks.
+ * lengths[s] is how many tokens sequence s has had before; its new tokens are at the
+ * positions from there on, see what they see in the cache and among themselves, and are
+ * written into the cache.  Sequence s's new tokens are offsets[s] to offsets[s + 1] - 1, as
+ * above, or token s alone where offsets is NULL.  A sequence whose length is negative takes
+ * no part: its output is zeros and its cache is left as it is.  lengths is only read. */
+int32_t sllm_attention_cached(const sllm_heads* q, const sllm_heads* k, const sllm_heads* v,
+                              const sllm_kv_cache* cache, const sllm_ids* lengths, const sllm_ids* offsets,
+                              float scale, const sllm_heads* out, void* workspace, uint64_t workspace_bytes,
+                              int32_t device, void* stream);
+int32_t sllm_attention_cached_workspace(const sllm_heads* q, const sllm_heads* k, const sllm_heads* v,
+                                        const sllm_kv_cache* cache, const sllm_ids* lengths,
+                                        const sllm_ids* offsets, uint64_t* bytes);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char* sllm_last_error(void);
 /* Static name of a status code. */

@@ -102,6 +102,17 @@ class Ids(C.Structure):
     _fields_ = [("data", C.c_void_p), ("n", C.c_uint64), ("bits", C.c_uint32), ("reserved", C.c_uint32)]
 
 
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("tokens", C.c_uint64), ("heads", C.c_uint64), ("dim", C.c_uint64),
+                ("token_stride", C.c_uint64), ("head_stride", C.c_uint64), ("dtype", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class KvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("sequences", C.c_uint64), ("heads", C.c_uint64), ("dim", C.c_uint64),
+                ("window", C.c_uint64), ("sinks", C.c_uint64), ("dtype", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+_HEADS, _CACHE = C.POINTER(Heads), C.POINTER(KvCache)
 _MATRIX, _MX, _IDS, _U64 = C.POINTER(Matrix), C.POINTER(Mx), C.POINTER(Ids), C.POINTER(C.c_uint64)
 _WORK = [C.c_void_p, C.c_uint64, C.c_int32, C.c_void_p]  # workspace, its bytes, device, stream
 
@@ -155,6 +166,10 @@ SIGNATURES = {
     "sllm_embedding_mx": (C.c_int32, [_MX, _IDS, C.c_float, _MATRIX, C.c_int32, C.c_void_p]),
     "sllm_embedding_grad": (C.c_int32, [_MATRIX, _IDS, C.c_float, C.c_uint32, _MATRIX, *_WORK]),
     "sllm_embedding_grad_workspace": (C.c_int32, [C.c_uint64, _MATRIX, _U64]),
+    "sllm_attention": (C.c_int32, [_HEADS, _HEADS, _HEADS, _IDS, C.c_uint64, C.c_uint64, C.c_float, _HEADS, C.c_void_p,
+                                   C.c_int32, C.c_void_p]),
+    "sllm_attention_cached": (C.c_int32, [_HEADS, _HEADS, _HEADS, _CACHE, _IDS, _IDS, C.c_float, _HEADS, *_WORK]),
+    "sllm_attention_cached_workspace": (C.c_int32, [_HEADS, _HEADS, _HEADS, _CACHE, _IDS, _IDS, _U64]),
     "sllm_last_error": (C.c_char_p, []),
     "sllm_strerror": (C.c_char_p, [C.c_int32]),
 }

@@ -1,0 +1,262 @@
+// gfx950 kernel of causal attention with a sliding window and sinks, over packed
+// sequences or behind a cache.
+#include <algorithm>
+
+#include "attention.hpp"
+#include "common.hpp"
+#include "device_math.hpp"
+#include "hip_util.hpp"
+
+namespace sllm {
+
+namespace {
+
+constexpr int kWaves = 4, kWaveRows = 32, kRows = kWaves * kWaveRows;
+
+template <typename T>
+constexpr int key_tile() {
+    return sizeof(T) == 4 ? 32 : 64;
+}
+
+// out = softmax(scale q k^T over the keys seen) v.  One pass over the keys: a running
+// maximum and sum of each row's weights, and the output rescaled where the maximum grows by
+// more than 2^8.
+//
+// A workgroup has 128 rows of one key/value head: rows are tokens times the heads that
+// share it, so that keys are read once for all of them.  A wave has 32 rows and makes the
+// transposes: scores of (keys x rows), then output of (elements x rows), so that a row's
+// statistics are its lane's own and weights go into the second product as they come out of
+// the first.
+template <typename T, int D, bool Vec, bool Cached>
+__global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void attention_rows(AttentionArgs a) {
+    constexpr int kKeys = key_tile<T>(), kSteps = D / 16, kParts = D / 32;
+    constexpr uint32_t kBytes = kKeys * RowTile<T, D>::kPitch;
+    __shared__ __align__(16) uint8_t k0[kBytes], v0[kBytes], k1[kBytes], v1[kBytes];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t c = lane & 31, h = lane >> 5;
+
+    // neighbouring pieces of a head on one XCD
+    const uint32_t blocks = gridDim.x, xcd = blockIdx.x % 8, q8 = blocks / 8, rest = blocks % 8;
+    const uint32_t index = xcd * q8 + min(xcd, rest) + blockIdx.x / 8;
+    const uint32_t head = index / a.pieces;  // of keys and values
+    const Piece piece = find_piece(a.offsets, a.wide_offsets, a.sequences, a.tokens, a.group, kRows, index % a.pieces, a.pieces);
+    T* const out = static_cast<T*>(a.out);
+    int64_t past = 0;
+    if (Cached && piece.n) past = read_id(a.lengths, a.wide_lengths, piece.sequence);
+    if (!piece.n || past < 0) {
+        // rows of no sequence, or of one that takes no part, are zeros
+        uint32_t from = piece.piece, to = a.tokens - (piece.past_end - piece.first), step = piece.spare;
+        if (piece.n) from = piece.piece, to = piece.n, step = (uint32_t)(((uint64_t)piece.n * a.group + kRows - 1) / kRows);
+        for (uint32_t t = from; t < to; t += step) {
+            const uint32_t token = piece.n ? piece.first + t : t < piece.first ? t : t - piece.first + piece.past_end;
+            for (uint32_t i = threadIdx.x; i < a.group * a.dim; i += kWaves * 64)
+                out[token * a.out_token + (head * a.group + i / a.dim) * a.out_head + i % a.dim] = (T)0.0f;
+            if (a.lse)
+                for (uint32_t i = threadIdx.x; i < a.group; i += kWaves * 64) a.lse[(uint64_t)token * a.heads + head * a.group + i] = 0.0f;
+        }
+        return;
+    }
+    const uint32_t rows = piece.n * a.group;  // fewer than 2^32
+    // the last pieces see the most keys: they come first
+    const uint32_t row0 = ((rows - 1) / kRows - piece.piece) * kRows, row1 = min(row0 + kRows, rows) - 1;
+    const uint32_t t0 = row0 / a.group, t1 = row1 / a.group;
+    const KeyList keys(past + t0, past + t1, a.window, a.sinks);
+    const int32_t base = (int32_t)(past + t0 - keys.lo) - (int32_t)t0;  // a token's position from lo on, less the token
+
+    // this wave's rows, the last one again past the end
+    const uint32_t wave_row = row0 + wave * kWaveRows, row = min(wave_row + c, rows - 1);
+    const uint32_t token = row / a.group, q_head = head * a.group + row % a.group;
+    const int32_t at = base + (int32_t)token;
+    const int32_t at0 = base + (int32_t)(min(wave_row, rows - 1) / a.group), at1 = base + (int32_t)(min(wave_row + 31, rows - 1) / a.group);
+    Operand8<T> q[kSteps];
+    {
+        const T* p = static_cast<const T*>(a.q) + (uint64_t)(piece.first + token) * a.q_token + q_head * a.q_head;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) q[s] = load8<T, Vec>(p, 16 * s + 8 * h, a.dim);
+    }
+
+    // where key i's row is
+    const int32_t held = Cached ? (int32_t)(past - keys.lo) : 0;  // keys from lo on in the cache
+    const int32_t past_sinks = Cached ? (int32_t)min(past, (int64_t)1 << 30) : 0;
+    int32_t slot0 = 0;                                             // the slot of lo, among the window's
+    if (Cached) slot0 = keys.lo < a.sinks ? (int32_t)(keys.lo - a.sinks) : (int32_t)((uint64_t)(keys.lo - a.sinks) % (uint32_t)a.window);
+    const uint64_t cache_row = Cached ? ((uint64_t)piece.sequence * a.kv_heads + head) * a.slots : 0;
+    const auto key_row = [&](const void* fresh, uint64_t token_stride, uint64_t head_stride, const void* cache, int32_t i) SLLM_INLINE -> const T* {
+        if (i >= keys.total) return nullptr;
+        const int32_t k = i - keys.sinks;
+        const T* const rows_of = static_cast<const T*>(fresh) + head * head_stride;
+        if constexpr (!Cached) {
+            const uint32_t token = k < 0 ? (uint32_t)i : (uint32_t)((int32_t)keys.lo + k);
+            return rows_of + (uint64_t)(piece.first + token) * token_stride;
+        } else {
+            const int32_t fresh_one = k < 0 ? i - past_sinks : k - held;  // of this call's tokens, or before them
+            if (fresh_one >= 0) return rows_of + (uint64_t)(piece.first + (uint32_t)fresh_one) * token_stride;
+            int32_t slot = k < 0 ? i : slot0 + k;
+            if (k >= 0) slot = a.sinks + (slot >= a.window ? slot - a.window : slot);
+            return static_cast<const T*>(cache) + (cache_row + (uint32_t)slot) * a.dim;
+        }
+    };
+    const auto stage = [&](int32_t i0, uint8_t* k, uint8_t* v) SLLM_INLINE {
+        stage_rows<T, D, kKeys, kWaves, Vec>(k, a.dim, [&](uint32_t r) SLLM_INLINE { return key_row(a.k, a.k_token, a.k_head, a.cache_k, i0 + (int32_t)r); });
+        stage_rows<T, D, kKeys, kWaves, Vec>(v, a.dim, [&](uint32_t r) SLLM_INLINE { return key_row(a.v, a.v_token, a.v_head, a.cache_v, i0 + (int32_t)r); });
+    };
+
+    // Weights are 2^(scale s - m) times 2^kUp: float16 has the least of those as normal numbers.
+    constexpr float kUp = __is_same(T, _Float16) ? 7.0f : 0.0f, kSlack = 8.0f;
+    const float scale = a.scale * kLog2e;
+    float m = -__builtin_inff(), m_scaled = 0, sum = 0;
+    f32x16 acc[kParts];
+#pragma unroll
+    for (int d = 0; d < kParts; ++d) acc[d] = f32x16{};
+    const uint32_t rows_at = rows_from<T, D>(lane), columns_at = columns_from<T, D>(lane);
+
+    const auto tile = [&](int32_t i0, const uint8_t* k, const uint8_t* v, auto masked) SLLM_INLINE {
+        constexpr bool kMasked = decltype(masked)::value;
+        f32x16 s[kKeys / 32];
+        const auto sees = [&](int r) SLLM_INLINE { return i0 + r < keys.total && keys.sees(at, i0 + r); };
+#pragma unroll
+        for (int n = 0; n < kKeys / 32; ++n) {
+            s[n] = f32x16{};
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) s[n] = multiply(read_rows<T, D>(k, rows_at, 32 * n, i), q[i], s[n]);
+            if constexpr (kMasked)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!sees(32 * n + 8 * (i / 4) + 4 * h + i % 4)) s[n][i] = -__builtin_inff();
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int n = 0; n < kKeys / 32; ++n)
+#pragma unroll
+            for (int i = n == 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+        if (__any((top - m) * scale > kSlack)) {
+            const f32x2 tops = both_halves(top);
+            const float next = fmaxf(m, fmaxf(tops[0], tops[1]));
+            const float next_scaled = next == -__builtin_inff() ? -kUp : next * scale - kUp;
+            const float f = __builtin_amdgcn_exp2f(m == -__builtin_inff() ? 0.0f : m_scaled - next_scaled);
+            m = next, m_scaled = next_scaled;
+            sum *= f;
+#pragma unroll
+            for (int d = 0; d < kParts; ++d) acc[d] *= f;
+        }
+        Operand8<T> p[kKeys / 16];
+        float part = 0;
+#pragma unroll
+        for (int n = 0; n < kKeys / 32; ++n) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], scale, -m_scaled));
+                part += s[n][i];
+            }
+            p[2 * n] = as_operand<T>(s[n], 0);
+            p[2 * n + 1] = as_operand<T>(s[n], 1);
+        }
+        sum += part;
+        add_weighted<T, D, kKeys, kMasked>(acc, v, columns_at, p, sees);
+    };
+    const auto step = [&](int32_t i0, const uint8_t* k, const uint8_t* v, uint8_t* next_k, uint8_t* next_v) SLLM_INLINE {
+        wait_but_loads<0>();
+        barrier();  // this tile has landed, and all waves are done with the other one
+        if (i0 + kKeys < keys.total) stage(i0 + kKeys, next_k, next_v);
+        if (keys.all(at0, at1, i0, i0 + kKeys - 1))
+            tile(i0, k, v, std::false_type());
+        else if (!keys.none(at0, at1, i0, i0 + kKeys - 1))
+            tile(i0, k, v, std::true_type());
+    };
+    stage(0, k0, v0);
+    for (int32_t i0 = 0; i0 < keys.total; i0 += 2 * kKeys) {
+        step(i0, k0, v0, k1, v1);
+        if (i0 + kKeys < keys.total) step(i0 + kKeys, k1, v1, k0, v0);
+    }
+
+    const f32x2 sums = both_halves(sum);
+    sum = sums[0] + sums[1];
+    if (wave_row + c >= rows) return;
+    const uint64_t out_row = piece.first + token;
+    if (a.lse && h == 0) a.lse[out_row * a.heads + q_head] = (m_scaled + __builtin_amdgcn_logf(sum)) * kLn2;
+    const float f = 1.0f / sum;
+    T* const p = out + out_row * a.out_token + q_head * a.out_head;
+#pragma unroll
+    for (int d = 0; d < kParts; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const uint32_t e = 32 * d + 8 * g + 4 * h;
+            T v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(acc[d][4 * g + i] * f);
+            if (Vec) {
+                if (e < a.dim) __builtin_memcpy(__builtin_assume_aligned(p + e, 4 * sizeof(T)), v, sizeof v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (e + i < a.dim) p[e + i] = v[i];
+            }
+        }
+}
+
+// The new tokens of each sequence into its cache, after the attention that still reads
+// what they replace: of those that share a slot the last one alone.
+template <typename W>
+__global__ __launch_bounds__(256) void write_cache(AttentionArgs a, uint32_t row_words) {
+    // the tokens of sequence blockIdx.x
+    __shared__ uint32_t bounds[2];
+    if (threadIdx.x < 2) bounds[threadIdx.x] = 0;
+    __syncthreads();
+    const auto clamp = [&](int64_t v) { return (uint32_t)min(max(v, (int64_t)0), (int64_t)a.tokens); };
+    const uint32_t s = blockIdx.x;
+    uint32_t most = 0;
+    for (uint32_t i = threadIdx.x; i <= s; i += 256) most = max(most, clamp(read_id(a.offsets, a.wide_offsets, i)));
+    atomicMax(&bounds[0], most);
+    __syncthreads();
+    const uint32_t first = bounds[0], n = max(first, clamp(read_id(a.offsets, a.wide_offsets, s + 1))) - first;
+    const int64_t past = read_id(a.lengths, a.wide_lengths, s);
+    if (past < 0) return;
+    const uint64_t words = (uint64_t)n * a.kv_heads * row_words, step = (uint64_t)gridDim.y * 256;
+    for (uint64_t i = (uint64_t)blockIdx.y * 256 + threadIdx.x; i < words; i += step) {
+        const uint32_t w = i % row_words, head = i / row_words % a.kv_heads, t = i / row_words / a.kv_heads;
+        const int64_t p = past + t;
+        if (p >= a.sinks && p + a.window < past + n) continue;  // a later one has its slot
+        const uint64_t slot = p < a.sinks ? p : a.sinks + (uint64_t)(p - a.sinks) % (uint32_t)a.window;
+        const uint64_t to = (((uint64_t)s * a.kv_heads + head) * a.slots + slot) * row_words + w;
+        const uint64_t size = sizeof(W) / a.element;  // strides are in elements
+        static_cast<W*>(a.cache_k)[to] = static_cast<const W*>(a.k)[((uint64_t)(first + t) * a.k_token + head * a.k_head) / size + w];
+        static_cast<W*>(a.cache_v)[to] = static_cast<const W*>(a.v)[((uint64_t)(first + t) * a.v_token + head * a.v_head) / size + w];
+    }
+}
+
+template <typename T, int D>
+void launch(const AttentionArgs& a, bool vec, dim3 grid, hipStream_t stream) {
+    const auto kernel = a.cache_k ? (vec ? attention_rows<T, D, true, true> : attention_rows<T, D, false, true>)
+                                  : (vec ? attention_rows<T, D, true, false> : attention_rows<T, D, false, false>);
+    kernel<<<grid, kWaves * 64, 0, stream>>>(a);
+}
+
+}  // namespace
+
+int32_t launch_attention(AttentionArgs a, hipStream_t stream) {
+    a.pieces = (uint32_t)(ceil_div((uint64_t)a.tokens * a.group, kRows) + (a.offsets ? a.sequences : 0));
+    const dim3 grid(a.pieces * a.kv_heads);
+    SLLM_BY_DTYPE(a.dtype, T, {
+        if (a.dim <= 64)
+            launch<T, 64>(a, a.vec, grid, stream);
+        else
+            launch<T, 128>(a, a.vec, grid, stream);
+    });
+    SLLM_HIP(hipGetLastError());
+    if (a.cache_k && a.sequences) {
+        a.element = a.dtype == SLLM_DTYPE_F32 ? 4 : 2;
+        const uint32_t row_bytes = a.dim * a.element;
+        // a workgroup for every 4096 of its words, were one sequence to have all tokens
+        const dim3 blocks(a.sequences, (uint32_t)std::min<uint64_t>(ceil_div((uint64_t)a.tokens * a.kv_heads * row_bytes / 16, 4096) + 1, 64));
+        if (a.vec)
+            write_cache<u32x4><<<blocks, 256, 0, stream>>>(a, row_bytes / 16);
+        else if (a.element == 4)
+            write_cache<uint32_t><<<blocks, 256, 0, stream>>>(a, row_bytes / 4);
+        else
+            write_cache<uint16_t><<<blocks, 256, 0, stream>>>(a, row_bytes / 2);
+        SLLM_HIP(hipGetLastError());
+    }
+    return SLLM_OK;
+}
+
+}  // namespace sllm

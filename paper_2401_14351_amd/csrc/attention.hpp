@@ -1,0 +1,335 @@
+// What the attention kernels share: their arguments, the tiles of keys and values in
+// LDS, the way a matrix of scores becomes an operand of the next product.
+#pragma once
+
+#include "operators.hpp"
+#include "products.hpp"
+
+namespace sllm {
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Rows of a tile in LDS are of `D` elements, the head's and zeros after them.  A row is cut
+// into chunks of 16 bytes whose order depends on the row, so that 16 rows read in one
+// column of chunks, by 16 neighbouring lanes, and four rows read 64 bytes wide are both in
+// all 64 banks once.  The place of chunk c ^ d is that of c, exclusive or 16 d.
+template <typename T, int D>
+struct RowTile {
+    static constexpr uint32_t kElements = 16 / sizeof(T), kChunks = D / kElements, kPitch = D * sizeof(T);
+    static constexpr uint32_t kLoadRows = 64 / kChunks;  // whose chunks a wave loads at once
+    static_assert(kChunks == 8 || kChunks == 16 || kChunks == 32, "");
+
+    static __device__ __forceinline__ uint32_t turn(uint32_t row) {
+        return kChunks == 8 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3);
+    }
+    static __device__ __forceinline__ uint32_t at(uint32_t row, uint32_t chunk) { return row * kPitch + (chunk ^ turn(row)) * 16; }
+};
+
+// `Rows` rows into LDS, by all waves: row r from at(r), zeros where that is null.  Vec:
+// rows start on 16 bytes and are whole chunks; loads then go past the registers.
+template <typename T, int D, int Rows, int Waves, bool Vec, typename At>
+__device__ __forceinline__ void stage_rows(uint8_t* to, uint32_t dim, const At& at) {
+    typedef RowTile<T, D> Tile;
+    constexpr uint32_t kLoads = Rows / Tile::kLoadRows / Waves;
+    static_assert(kLoads * Tile::kLoadRows * Waves == Rows, "");
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const void* const zeros = zero_vector();
+#pragma unroll
+    for (uint32_t q = 0; q < kLoads; ++q) {
+        const uint32_t i = q * Waves + wave, row = i * Tile::kLoadRows + lane / Tile::kChunks;
+        const uint32_t e = ((lane % Tile::kChunks) ^ Tile::turn(row)) * Tile::kElements;
+        const T* p = at(row);
+        if constexpr (Vec) {
+            const void* from = p + e;
+            load_to_lds(p && e < dim ? from : zeros, to, i * 1024);
+        } else {
+            T v[Tile::kElements];
+#pragma unroll
+            for (uint32_t k = 0; k < Tile::kElements; ++k) v[k] = p && e + k < dim ? p[e + k] : (T)0.0f;
+            lds_write(to, i * 1024 + lane * 16, __builtin_bit_cast(u32x4, v));
+        }
+    }
+}
+
+// Eight elements of a lane: an operand of 16 of the depth by 32 rows or columns, of which
+// lane (r, h) has row r and depths 8 h to 8 h + 7.
+template <typename T>
+struct Operand8 {
+    u32x4 v;
+};
+template <>
+struct Operand8<float> {
+    f32x8 v;
+};
+
+template <typename T>
+__device__ __forceinline__ f32x16 multiply(const Operand8<T>& a, const Operand8<T>& b, f32x16 acc) {
+    if constexpr (__is_same(T, float)) {
+        // two depths an instruction, one a half wave: which does not matter if both sides agree
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[i], b.v[i], acc, 0, 0, 0);
+        return acc;
+    } else {
+        return product<T>(a.v, b.v, acc);
+    }
+}
+
+// Of rows row0 to row0 + 31 of a tile, step s of 16 of their elements.
+template <typename T, int D>
+__device__ __forceinline__ Operand8<T> read_rows(const uint8_t* tile, uint32_t from, int row0, int s) {
+    Operand8<T> o;
+    if constexpr (__is_same(T, float)) {
+        const f32x4 a = lds_read<f32x4>(tile, (from ^ s * 64) + row0 * RowTile<T, D>::kPitch);
+        const f32x4 b = lds_read<f32x4>(tile, (from ^ (s * 64 + 16)) + row0 * RowTile<T, D>::kPitch);
+        o.v = f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    } else {
+        o.v = lds_read<u32x4>(tile, (from ^ s * 32) + row0 * RowTile<T, D>::kPitch);
+    }
+    return o;
+}
+// The `from` of a lane.
+template <typename T, int D>
+__device__ __forceinline__ uint32_t rows_from(uint32_t lane) {
+    return opaque(RowTile<T, D>::at(lane & 31, (lane >> 5) * (sizeof(T) / 2)));
+}
+
+// Scores come out of a product in registers: of a matrix of 32 rows, lane (c, h) has
+// column c and rows 8 (i / 4) + 4 h + i % 4.  Eight of them, 16 rows in the two halves,
+// are an operand over those rows as they are, if the other side takes the rows in that
+// order: the rows of a tile, element by element, in lane (element, h).
+template <typename T, int D>
+__device__ __forceinline__ Operand8<T> read_columns(const uint8_t* tile, uint32_t from, int row0, int column0) {
+    Operand8<T> o;
+    if constexpr (__is_same(T, float)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            // rows row0 + 8 (j / 4) + 4 h + j % 4: their turn is (j % 4) << 2 | (2 (j / 4) + h)
+            const uint32_t turn = RowTile<T, D>::kChunks == 8 ? (j >> 1 & 1) << 6 | (j >> 2) << 5 : (j & 3) << 6 | (j >> 2) << 5;
+            o.v[j] = lds_read<float>(tile, (from ^ turn ^ column0 * 4) + (row0 + 8 * (j / 4) + j % 4) * RowTile<T, D>::kPitch);
+        }
+    } else {
+        // 16 lanes read four rows of 16 elements and get a column of four each
+        typedef __attribute__((address_space(3))) i16x4 Lds;
+        u32x2 part[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t at = (from ^ column0 * 2 ^ u * 32) + (row0 + 8 * u) * RowTile<T, D>::kPitch;
+            part[u] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)((lds_u8*)tile + at)));
+        }
+        o.v = u32x4{part[0][0], part[0][1], part[1][0], part[1][1]};
+    }
+    return o;
+}
+template <typename T, int D>
+__device__ __forceinline__ uint32_t columns_from(uint32_t lane) {
+    typedef RowTile<T, D> Tile;
+    if constexpr (__is_same(T, float)) {
+        const uint32_t row = 4 * (lane >> 5), c = lane & 31;
+        return opaque(Tile::at(row, c / 4) + c % 4 * 4);
+    } else {
+        const uint32_t row = 4 * (lane >> 5) + (lane >> 2 & 3), c = (lane >> 4 & 1) * 16 + (lane & 3) * 4;
+        return opaque(Tile::at(row, c / 8) + c % 8 * 2);
+    }
+}
+
+// Registers 8 t to 8 t + 7 as an operand, rounded to nearest even.
+template <typename T>
+__device__ __forceinline__ Operand8<T> as_operand(const f32x16& x, int t) {
+    Operand8<T> o;
+    if constexpr (__is_same(T, float)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o.v[j] = x[8 * t + j];
+    } else {
+        typedef T T2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            o.v[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[8 * t + 2 * j], x[8 * t + 2 * j + 1]}, T2));
+    }
+    return o;
+}
+
+// Eight elements of a row in memory from element e, zeros past its end.
+template <typename T, bool Vec>
+__device__ __forceinline__ Operand8<T> load8(const T* row, uint32_t e, uint32_t dim) {
+    T v[8];
+    if constexpr (Vec) {
+        constexpr uint32_t n = 16 / sizeof(T);
+#pragma unroll
+        for (uint32_t i = 0; i < 8 / n; ++i) {
+            u32x4 raw = {0, 0, 0, 0};
+            if (e + i * n < dim) raw = *reinterpret_cast<const u32x4*>(row + e + i * n);
+            __builtin_memcpy(v + i * n, &raw, 16);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = e + i < dim ? row[e + i] : (T)0.0f;
+    }
+    Operand8<T> o;
+    __builtin_memcpy(&o.v, v, sizeof v);
+    return o;
+}
+
+// A lane's and that of the same column in the other half wave.
+__device__ __forceinline__ f32x2 both_halves(float x) {
+    return __builtin_bit_cast(f32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+}
+
+// Products with rows of which some columns must see nothing: what is not a number there
+// would come through a weight of zero.  Such elements are taken out of the operand, and
+// added, as they are, to the columns that see their row.
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t word) {  // halves that are not, as all ones
+    constexpr uint32_t kExponent = __is_same(T, _Float16) ? 0x7c00 : 0x7f80;
+    return ((word & kExponent) == kExponent ? 0xffffu : 0u) | ((word >> 16 & kExponent) == kExponent ? 0xffff0000u : 0u);
+}
+template <typename T>
+__device__ __forceinline__ bool take_out(Operand8<T>& o) {
+    uint32_t any = 0;
+    if constexpr (__is_same(T, float)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool bad = (__float_as_uint(o.v[i]) & 0x7f800000) == 0x7f800000;
+            any |= bad;
+            o.v[i] = bad ? 0.0f : o.v[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t bad = not_finite<T>(o.v[i]);
+            any |= bad;
+            o.v[i] &= ~bad;
+        }
+    }
+    return any != 0;
+}
+
+// acc and the elements that take_out took of `Rows` rows, in lanes that see(row).
+template <typename T, int D, int Rows, typename See>
+__device__ __forceinline__ f32x16 with_taken_out(f32x16 acc, const uint8_t* tile, uint32_t column0, const See see) {
+    const uint32_t h = threadIdx.x >> 5 & 1;
+#pragma unroll 1
+    for (int row = 0; row < Rows; ++row) {
+        const bool seen = see(row);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t c = column0 + 8 * (i / 4) + 4 * h + i % 4;
+            const T v = lds_read<T>(tile, RowTile<T, D>::at(row, c / RowTile<T, D>::kElements) + c % RowTile<T, D>::kElements * sizeof(T));
+            const float f = to_f32(v);
+            if (seen && !(__builtin_fabsf(f) < __builtin_inff())) acc[i] += f;
+        }
+    }
+    return acc;
+}
+
+// acc[d] += the sum over `Rows` rows of a tile of element 32 d .. of the row times the
+// weight of the lane's column, w(t) being the operand of rows 16 t on.
+template <typename T, int D, int Rows, bool Masked, typename See>
+__device__ __forceinline__ void add_weighted(f32x16 (&acc)[D / 32], const uint8_t* tile, uint32_t from, const Operand8<T> (&w)[Rows / 16],
+                                             const See& see) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) {
+        bool out = false;
+#pragma unroll
+        for (int t = 0; t < Rows / 16; ++t) {
+            Operand8<T> v = read_columns<T, D>(tile, from, 16 * t, 32 * d);
+            if constexpr (Masked) out |= take_out(v);
+            acc[d] = multiply(v, w[t], acc[d]);
+        }
+        if constexpr (Masked)
+            if (__any(out)) acc[d] = with_taken_out<T, D, Rows>(acc[d], tile, 32 * d, see);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Sequences
+// ---------------------------------------------------------------------------
+
+__device__ __forceinline__ int64_t read_id(const void* ids, bool wide, uint64_t i) {
+    return wide ? static_cast<const int64_t*>(ids)[i] : static_cast<const int32_t*>(ids)[i];
+}
+
+// A piece of a sequence: tokens first .. first + n - 1 of the packed rows, and which
+// piece of it.  None: n = 0, then `piece` counts those past the last one, of `spare`, and
+// rows before `first` and from `past_end` on belong to no sequence.
+struct Piece {
+    uint32_t sequence, first, n, piece, spare, past_end;
+};
+
+// Piece `index` of all sequences, each cut into ceil(tokens * rows / size).  Offsets are
+// taken as far as they do not go back and lie within the tokens, so that no two sequences
+// share a row whatever they hold.  A wave reads 64 sequences at a time.
+__device__ __forceinline__ Piece find_piece(const void* offsets, bool wide, uint32_t sequences, uint32_t tokens, uint32_t rows,
+                                            uint32_t size, uint32_t index, uint32_t pieces) {
+    const auto cut = [&](uint32_t n) { return (uint32_t)(((uint64_t)n * rows + size - 1) / size); };
+    if (!offsets) {
+        const uint32_t all = cut(tokens);
+        if (index < all) return {0, 0, tokens, index, 0, tokens};
+        return {0, 0, 0, index - all, pieces - all, tokens};
+    }
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t before = 0, start = 0, first_row = 0;  // pieces so far, where the last sequence ended
+    for (uint32_t s0 = 0; s0 < sequences; s0 += 64) {
+        // the ends of sequences s0 .., at least each one's start and the ends before
+        const uint32_t s = s0 + lane;
+        const auto clamp = [&](int64_t v) { return (uint32_t)min(max(v, (int64_t)0), (int64_t)tokens); };
+        if (s0 == 0) first_row = start = __builtin_amdgcn_readfirstlane(clamp(read_id(offsets, wide, 0)));
+        uint32_t end = s < sequences ? clamp(read_id(offsets, wide, s + 1)) : 0;
+        end = max(end, start);
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t v = __shfl_up(end, d);
+            if (lane >= (uint32_t)d) end = max(end, v);
+        }
+        uint32_t from = __shfl_up(end, 1);
+        if (lane == 0) from = start;
+        const uint32_t mine = s < sequences ? cut(end - from) : 0;
+        uint32_t upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t v = __shfl_up(upto, d);
+            if (lane >= (uint32_t)d) upto += v;
+        }
+        const uint64_t found = __ballot(before + upto > index);
+        if (found) {
+            const int at = __builtin_ctzll(found);
+            const uint32_t f = __builtin_amdgcn_readlane(from, at), e = __builtin_amdgcn_readlane(end, at);
+            return {s0 + at, f, e - f, index - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at)), 0, 0};
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+        start = __builtin_amdgcn_readlane(end, 63);
+    }
+    return {0, first_row, 0, index - before, pieces - before, start};
+}
+
+// The keys that the queries at positions i0 to i1 of a sequence see: the first `sinks`
+// positions, those not in the window among them, then lo to i1.  Key c of that list is at
+// distance c - sinks from lo; positions count from lo, in 32 bits.
+struct KeyList {
+    int32_t sinks, total;       // keys before lo, all keys
+    int32_t early, window;      // positions from lo on below this are sinks too
+    int64_t lo;
+
+    __device__ __forceinline__ KeyList(int64_t i0, int64_t i1, int32_t window, int32_t all_sinks) : window(window) {
+        lo = max((int64_t)0, i0 - window + 1);
+        sinks = (int32_t)min((int64_t)all_sinks, lo);
+        early = (int32_t)max((int64_t)0, all_sinks - lo);
+        total = sinks + (int32_t)(i1 - lo + 1);
+    }
+    // whether the query at lo + q sees key c
+    __device__ __forceinline__ bool sees(int32_t q, int32_t c) const {
+        const int32_t k = c - sinks;
+        return k <= q && (k < early || q - k < window);
+    }
+    // whether all queries lo + q0 .. lo + q1 see keys c0 .. c1, and whether none sees any
+    __device__ __forceinline__ bool all(int32_t q0, int32_t q1, int32_t c0, int32_t c1) const {
+        return c1 < total && c1 - sinks <= q0 && (c1 - sinks < early || q1 - (c0 - sinks) < window);
+    }
+    __device__ __forceinline__ bool none(int32_t q0, int32_t q1, int32_t c0, int32_t c1) const {
+        return c0 - sinks > q1 || (c0 - sinks >= early && q0 - (c1 - sinks) >= window);
+    }
+};
+
+}  // namespace sllm

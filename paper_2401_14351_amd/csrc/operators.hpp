@@ -76,4 +76,31 @@ constexpr uint64_t kMaxGradIds = 1ull << 24;
 uint64_t embedding_grad_workspace(uint64_t n_ids, uint64_t vocab, uint64_t dim);
 int32_t launch_embedding_grad(const EmbeddingGradLaunch& a, void* workspace, hipStream_t stream);
 
+// Causal attention of packed sequences, or behind what a cache holds of them (cache_k set).
+// Strides are in elements; window, sinks and tokens are below 2^30.
+struct AttentionArgs {
+    const void *q = nullptr, *k = nullptr, *v = nullptr;
+    uint64_t q_token = 0, q_head = 0, k_token = 0, k_head = 0, v_token = 0, v_head = 0;
+    void* out = nullptr;
+    uint64_t out_token = 0, out_head = 0;
+    float* lse = nullptr;  // tokens x heads
+    uint32_t tokens = 0, heads = 0, kv_heads = 0, group = 0, dim = 0, dtype = 0;
+    int32_t window = 0, sinks = 0;
+    float scale = 0;
+    const void* offsets = nullptr;  // sequences + 1, or null for one sequence
+    uint32_t sequences = 0;
+    bool wide_offsets = false, wide_lengths = false;
+    bool vec = false;  // rows start on 16 bytes and are whole multiples of them
+    const void* lengths = nullptr;
+    void *cache_k = nullptr, *cache_v = nullptr;  // (sequences, kv_heads, slots, dim)
+    uint64_t slots = 0;
+    uint32_t pieces = 0;   // of each key/value head
+    uint32_t element = 0;  // bytes
+};
+int32_t launch_attention(AttentionArgs a, hipStream_t stream);
+
+// One new token a sequence, tokens and sequences being the same.
+uint64_t attention_step_workspace(const AttentionArgs& a);
+int32_t launch_attention_step(const AttentionArgs& a, void* workspace, hipStream_t stream);
+
 }  // namespace sllm

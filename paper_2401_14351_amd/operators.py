@@ -527,3 +527,185 @@ class _Embedding(torch.autograd.Function):
     def backward(ctx, dy):
         (tokens,) = ctx.saved_tensors
         return embedding_grad(dy.contiguous(), tokens, ctx.vocab, ctx.scale, out_dtype=ctx.dtype), None, None, None
+
+
+# ---------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------
+
+def _heads(t: torch.Tensor, name: str) -> binding.Heads:
+    """(tokens, heads, elements) by their strides."""
+    code = _DTYPE.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: {t.dtype} is not float32, float16 or bfloat16")
+    if not t.is_cuda:
+        raise ValueError(f"{name} is not in device memory")
+    if t.is_neg():
+        raise ValueError(f"{name} is a negated view of other elements")
+    if t.dim() != 3:
+        raise ValueError(f"{name}: expected tokens, heads and elements, got shape {tuple(t.shape)}")
+    tokens, heads, dim = t.shape
+    strides = t.stride()
+    if dim > 1 and strides[2] != 1:
+        raise ValueError(f"{name}: the elements of a head are not adjacent (strides {strides})")
+    # a single token's or head's stride says nothing
+    return binding.Heads(t.data_ptr(), tokens, heads, dim, strides[0] if tokens > 1 else heads * dim,
+                         strides[1] if heads > 1 else dim, code, 0)
+
+
+def _index_tensor(t: Optional[torch.Tensor], name: str) -> Optional[binding.Ids]:
+    if t is None:
+        return None
+    if t.dim() != 1:
+        raise ValueError(f"{name}: expected one dimension, got shape {tuple(t.shape)}")
+    try:
+        return _ids(t)
+    except ValueError as e:
+        raise ValueError(str(e).replace("tokens", name)) from None
+
+
+class KvCache:
+    """Keys and values of sequences, each (sequences, heads, sinks + window, elements) and
+    contiguous: the first ``sinks`` positions of a sequence and the last ``window`` ones.
+    Position p is in slot p, or from the sinks on in slot sinks + (p - sinks) % window.
+    It is those tensors, wherever their storage is when it is used."""
+
+    __slots__ = ("k", "v", "window", "sinks")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, window: int, sinks: int = 0):
+        self.k, self.v, self.window, self.sinks = k, v, window, sinks
+        self._check()
+
+    def _check(self):
+        if self.window < 1 or self.sinks < 0:
+            raise ValueError(f"a window of {self.window} and {self.sinks} sinks")
+        for name, t in (("k", self.k), ("v", self.v)):
+            if t.dtype not in _DTYPE:
+                raise ValueError(f"{name}: {t.dtype} is not float32, float16 or bfloat16")
+            if t.dim() != 4 or t.shape[2] != self.sinks + self.window or not t.is_contiguous() or t.is_neg():
+                raise ValueError(f"{name}: expected a contiguous tensor of sequences, heads, {self.sinks + self.window} slots and "
+                                 f"elements, got shape {tuple(t.shape)} and strides {t.stride()}")
+        if self.k.shape != self.v.shape or self.k.dtype != self.v.dtype or self.k.device != self.v.device:
+            raise ValueError("k and v differ in shape, type or device")
+
+    @classmethod
+    def empty(cls, sequences: int, heads: int, dim: int, window: int, sinks: int = 0, dtype=torch.bfloat16, device=None) -> "KvCache":
+        """A cache whose contents are not set, for sequences that have had no tokens."""
+        shape = (sequences, heads, sinks + window, dim)
+        return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device), window, sinks)
+
+    @property
+    def _struct(self) -> binding.KvCache:
+        self._check()
+        n, heads, _, dim = self.k.shape
+        return binding.KvCache(self.k.data_ptr(), self.v.data_ptr(), n, heads, dim, self.window, self.sinks, _DTYPE[self.k.dtype], 0)
+
+    @property
+    def device(self):
+        return self.k.device
+
+    def __getitem__(self, sequences: slice) -> "KvCache":
+        """A run of sequences, sharing this cache's memory."""
+        if not isinstance(sequences, slice) or sequences.step not in (None, 1):
+            raise ValueError("a KvCache is indexed by a run of sequences")
+        return KvCache(self.k[sequences], self.v[sequences], self.window, self.sinks)
+
+    def __repr__(self):
+        n, heads, _, dim = self.k.shape
+        return f"KvCache({n} x {heads} x ({self.sinks} + {self.window}) x {dim}, {self.k.dtype}, {self.device})"
+
+
+def _out_heads(out: Optional[torch.Tensor], like: torch.Tensor):
+    if out is None:
+        out = like.new_empty(like.shape)
+    elif out.shape != like.shape or out.dtype != like.dtype or out.device != like.device:
+        raise ValueError(f"out: expected {like.dtype} of shape {tuple(like.shape)} on {like.device}, "
+                         f"got {out.dtype} of shape {tuple(out.shape)} on {out.device}")
+    else:
+        _refuse_tangent(out)
+        _refuse_grad(out)
+    return out, _heads(out, "out")
+
+
+def _window(window: Optional[int], sinks: int) -> int:
+    if (window is not None and window < 1) or sinks < 0:
+        raise ValueError(f"a window of {window} and {sinks} sinks")
+    return min(window or 0, 1 << 62)
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: Optional[int] = None, sinks: int = 0,
+              offsets: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+              stream=None) -> torch.Tensor:
+    """Causal attention of packed sequences: (tokens, heads, elements) for q of that shape
+    and k and v of (tokens, key/value heads, elements), heads a multiple of theirs.
+
+    The query at position i of its sequence sees the key at position j of the same one
+    where j <= i and (i - j < window or j < sinks); without a window every j <= i.
+    ``offsets`` (int32 or int64, one more than there are sequences) tells where each
+    starts and the last one ends; without it all tokens are one sequence.  Tokens of no
+    sequence are padding: rows of zeros, whose gradients are zeros.  ``scale`` is
+    elements ** -0.5 if not given."""
+    if stream is not None:
+        return _on_stream(stream, attention, q, k, v, window, sinks, offsets, scale, out, keep=(q, k, v, offsets, out))
+    for t in (q, k, v):
+        _refuse_tangent(t)
+    if scale is None:
+        scale = q.shape[-1] ** -0.5 if q.dim() and q.shape[-1] else 1.0
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
+        if out is not None:
+            raise ValueError("an operator that writes to a given tensor takes no part in autograd")
+        return _Attention.apply(q, k, v, window, sinks, offsets, scale)
+    return _attention(q, k, v, window, sinks, offsets, scale, out, None)
+
+
+def _attention(q, k, v, window, sinks, offsets, scale, out, lse):
+    window, args, ids = _window(window, sinks), (_heads(q, "q"), _heads(k, "k"), _heads(v, "v")), _index_tensor(offsets, "offsets")
+    device = _one_device(q, k, v, offsets)
+    y, rows = _out_heads(out, q)
+    binding.check(binding.lib().sllm_attention(*args, ids, window, min(sinks, 1 << 62), scale, rows,
+                                               None if lse is None else lse.data_ptr(), device, _raw_stream(device)))
+    _written(out)
+    return y
+
+
+def attention_cached(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: KvCache, lengths: torch.Tensor,
+                     offsets: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """:func:`attention` of new tokens behind those that ``cache`` holds, with its window
+    and sinks; their keys and values are written into it.
+
+    ``lengths`` (int32 or int64) is how many tokens each sequence has had before, and where
+    its new ones start; it is only read.  The new tokens of a sequence are those between
+    its ``offsets``, or without them one for each sequence, in their order.  A sequence
+    whose length is negative takes no part: its rows are zeros, its cache stays.  No
+    gradient passes."""
+    if stream is not None:
+        return _on_stream(stream, attention_cached, q, k, v, cache, lengths, offsets, scale, out,
+                          keep=(q, k, v, cache.k, cache.v, lengths, offsets, out))
+    for t in (q, k, v, cache.k, cache.v):
+        _refuse_tangent(t)
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError("a tensor requires a gradient, which attention over a cache does not pass on")
+    if scale is None:
+        scale = q.shape[-1] ** -0.5 if q.dim() and q.shape[-1] else 1.0
+    if lengths is None:
+        raise ValueError("lengths: None")
+    args = (_heads(q, "q"), _heads(k, "k"), _heads(v, "v"), cache._struct, _index_tensor(lengths, "lengths"), _index_tensor(offsets, "offsets"))
+    device = _one_device(q, k, v, cache.k, lengths, offsets)
+    y, rows = _out_heads(out, q)
+    L = binding.lib()
+    n = _workspace(L.sllm_attention_cached_workspace, *args)
+    ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    binding.check(L.sllm_attention_cached(*args, scale, rows, ws.data_ptr() if n else None, n, device, _raw_stream(device)))
+    _written(out, cache.k, cache.v)
+    return y
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, window, sinks, offsets, scale):
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        out = _attention(q, k, v, window, sinks, offsets, scale, None, lse)
+        ctx.save_for_backward(q, k, v, out, lse, offsets)
+        ctx.window, ctx.sinks, ctx.scale = window, sinks, scale
+        return out
