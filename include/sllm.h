@@ -479,7 +479,8 @@ int32_t sllm_close(sllm_ckpt* h);
 
 /* =========================================================================
  * Operators on loaded weights: matrices held in microscaled 4-bit floating
- * point (MX FP4), products with them, and token embeddings
+ * point (MX FP4), products with them, token embeddings, and what a decoder
+ * layer has around them: norms and attention
  *
  * Every operator is enqueued on `stream` and returns without waiting; it
  * allocates nothing (a workspace, where one is needed, is the caller's) and may
@@ -565,12 +566,17 @@ int32_t sllm_mx_linear_mx(const sllm_mx* x, const sllm_mx* w, const sllm_matrix*
 int32_t sllm_mx_linear_grad(const sllm_matrix* dy, const sllm_mx* w, const sllm_matrix* dx, void* workspace,
                             uint64_t workspace_bytes, int32_t device, void* stream);
 
-/* Workspace each of the three needs for these operands (their data pointers'
+/* The same with x in MX FP8 (see sllm_mx_octet_quantize). */
+int32_t sllm_mx_linear_octet(const sllm_mx* x, const sllm_mx* w, const sllm_matrix* out, void* workspace,
+                           uint64_t workspace_bytes, int32_t device, void* stream);
+
+/* Workspace each of these needs for these operands (their data pointers'
  * alignment counts, the memory is not read); 0 means none, and workspace may
  * then be NULL.  A workspace is 16-byte aligned; its contents do not matter and
  * are overwritten.  Host-only. */
 int32_t sllm_mx_linear_workspace(const sllm_matrix* x, const sllm_mx* w, uint64_t* bytes);
 int32_t sllm_mx_linear_mx_workspace(const sllm_mx* x, const sllm_mx* w, uint64_t* bytes);
+int32_t sllm_mx_linear_octet_workspace(const sllm_mx* x, const sllm_mx* w, uint64_t* bytes);
 int32_t sllm_mx_linear_grad_workspace(const sllm_matrix* dy, const sllm_mx* w, uint64_t* bytes);
 
 /* out's row i = scale * row ids[i] of table, zeros where ids[i] names no row. */
@@ -591,6 +597,40 @@ int32_t sllm_embedding_grad(const sllm_matrix* dy, const sllm_ids* ids, float sc
                             const sllm_matrix* grad, void* workspace, uint64_t workspace_bytes, int32_t device,
                             void* stream);
 int32_t sllm_embedding_grad_workspace(uint64_t n_ids, const sllm_matrix* grad, uint64_t* bytes);
+
+/* A matrix in MX FP8 (the formats' MXFP8 with E4M3 elements; "octet" here), for activations: an sllm_mx
+ * whose blocks have 32 code bytes each, a column a byte, and the same scales.  Sizes of the
+ * two buffers; host-only.  Errors: INVAL, RANGE. */
+int32_t sllm_mx_octet_sizes(uint64_t rows, uint64_t cols, uint64_t* codes_bytes, uint64_t* scales_bytes);
+
+/* dst = src in MX FP8.  A block's scale is the smallest power of two from 2^-127 on whose
+ * 448-fold is not below its largest magnitude, so nothing saturates; its elements divided by
+ * the scale go to the nearest E4M3 value, ties to the even code.  A block with an infinity or
+ * a NaN gets scale 255 and codes 0. */
+int32_t sllm_mx_octet_quantize(const sllm_matrix* src, const sllm_mx* dst, int32_t device, void* stream);
+
+/* dst = the values src stands for, rounded to dst's type. */
+int32_t sllm_mx_octet_dequantize(const sllm_mx* src, const sllm_matrix* dst, int32_t device, void* stream);
+
+/* h = x + residual, rounded to their dtype, and y = h / sqrt(mean h^2 + eps) * gain, the mean
+ * over a row's columns.  x, residual, h and y are of one shape and dtype, gain is one row of
+ * any dtype; residual and h are both NULL or both not: h is x where there is none.  eps is
+ * not negative.  inverse, if not NULL: each row's 1 / sqrt(mean h^2 + eps), for the gradient. */
+int32_t sllm_rms_norm(const sllm_matrix* x, const sllm_matrix* residual, const sllm_matrix* gain, float eps,
+                      const sllm_matrix* h, const sllm_matrix* y, float* inverse, int32_t device, void* stream);
+
+/* The same with y, not rounded before, in MX FP8. */
+int32_t sllm_rms_norm_octet(const sllm_matrix* x, const sllm_matrix* residual, const sllm_matrix* gain, float eps,
+                          const sllm_matrix* h, const sllm_mx* y, int32_t device, void* stream);
+
+/* The gradients of sllm_rms_norm from those by y and h (dh NULL: zero), and its h and
+ * inverse: with f the inverse and s = dy * gain,
+ *   dx = dh + f * (s - h * f^2 * mean(s * h)), the residual's gradient too, and
+ *   dgain = the sum over rows of dy * h * f, in a fixed order, in gain's dtype. */
+int32_t sllm_rms_norm_grad(const sllm_matrix* dy, const sllm_matrix* dh, const sllm_matrix* h, const sllm_matrix* gain,
+                           const float* inverse, const sllm_matrix* dx, const sllm_matrix* dgain, void* workspace,
+                           uint64_t workspace_bytes, int32_t device, void* stream);
+int32_t sllm_rms_norm_grad_workspace(uint64_t rows, uint64_t cols, uint64_t* bytes);
 
 /* Rows of tokens and heads in device memory, aligned to their element type: head h of
  * token t starts at data + t * token_stride + h * head_stride elements and its
@@ -624,6 +664,20 @@ typedef struct sllm_heads {
 int32_t sllm_attention(const sllm_heads* q, const sllm_heads* k, const sllm_heads* v, const sllm_ids* offsets,
                        uint64_t window, uint64_t sinks, float scale, const sllm_heads* out, float* lse,
                        int32_t device, void* stream);
+
+/* The gradients of sllm_attention by q, k and v, from dout (as out) and the out and lse of
+ * that call: with p = exp(scale q . k - lse) and ds = p (dout . v - dout . out),
+ *   dq = scale * sum ds k, dk = scale * sum ds q, dv = sum p dout,
+ * the last two over all heads that share the key.  p and ds are rounded to the dtype
+ * (a float16 ds times a power of two that keeps it in float16's range) before they are
+ * multiplied; sums are held in 32 bits.  Tokens of no sequence have gradients of zeros. */
+int32_t sllm_attention_grad(const sllm_heads* dout, const sllm_heads* q, const sllm_heads* k, const sllm_heads* v,
+                            const sllm_heads* out, const float* lse, const sllm_ids* offsets, uint64_t window,
+                            uint64_t sinks, float scale, const sllm_heads* dq, const sllm_heads* dk,
+                            const sllm_heads* dv, void* workspace, uint64_t workspace_bytes, int32_t device,
+                            void* stream);
+int32_t sllm_attention_grad_workspace(const sllm_heads* q, const sllm_heads* k, const sllm_ids* offsets,
+                                      uint64_t* bytes);
 
 /* Keys and values of sequences, each (sequences, heads, sinks + window, dim), contiguous:
  * position p is in slot p where p < sinks, and else in slot sinks + (p - sinks) % window,

@@ -162,12 +162,24 @@ SIGNATURES = {
     "sllm_mx_linear_workspace": (C.c_int32, [_MATRIX, _MX, _U64]),
     "sllm_mx_linear_mx_workspace": (C.c_int32, [_MX, _MX, _U64]),
     "sllm_mx_linear_grad_workspace": (C.c_int32, [_MATRIX, _MX, _U64]),
+    "sllm_mx_linear_octet": (C.c_int32, [_MX, _MX, _MATRIX, *_WORK]),
+    "sllm_mx_linear_octet_workspace": (C.c_int32, [_MX, _MX, _U64]),
+    "sllm_mx_octet_sizes": (C.c_int32, [C.c_uint64, C.c_uint64, _U64, _U64]),
+    "sllm_mx_octet_quantize": (C.c_int32, [_MATRIX, _MX, C.c_int32, C.c_void_p]),
+    "sllm_mx_octet_dequantize": (C.c_int32, [_MX, _MATRIX, C.c_int32, C.c_void_p]),
+    "sllm_rms_norm": (C.c_int32, [_MATRIX, _MATRIX, _MATRIX, C.c_float, _MATRIX, _MATRIX, C.c_void_p, C.c_int32, C.c_void_p]),
+    "sllm_rms_norm_octet": (C.c_int32, [_MATRIX, _MATRIX, _MATRIX, C.c_float, _MATRIX, _MX, C.c_int32, C.c_void_p]),
+    "sllm_rms_norm_grad": (C.c_int32, [_MATRIX, _MATRIX, _MATRIX, _MATRIX, C.c_void_p, _MATRIX, _MATRIX, *_WORK]),
+    "sllm_rms_norm_grad_workspace": (C.c_int32, [C.c_uint64, C.c_uint64, _U64]),
     "sllm_embedding": (C.c_int32, [_MATRIX, _IDS, C.c_float, _MATRIX, C.c_int32, C.c_void_p]),
     "sllm_embedding_mx": (C.c_int32, [_MX, _IDS, C.c_float, _MATRIX, C.c_int32, C.c_void_p]),
     "sllm_embedding_grad": (C.c_int32, [_MATRIX, _IDS, C.c_float, C.c_uint32, _MATRIX, *_WORK]),
     "sllm_embedding_grad_workspace": (C.c_int32, [C.c_uint64, _MATRIX, _U64]),
     "sllm_attention": (C.c_int32, [_HEADS, _HEADS, _HEADS, _IDS, C.c_uint64, C.c_uint64, C.c_float, _HEADS, C.c_void_p,
                                    C.c_int32, C.c_void_p]),
+    "sllm_attention_grad": (C.c_int32, [_HEADS, _HEADS, _HEADS, _HEADS, _HEADS, C.c_void_p, _IDS, C.c_uint64, C.c_uint64,
+                                        C.c_float, _HEADS, _HEADS, _HEADS, *_WORK]),
+    "sllm_attention_grad_workspace": (C.c_int32, [_HEADS, _HEADS, _IDS, _U64]),
     "sllm_attention_cached": (C.c_int32, [_HEADS, _HEADS, _HEADS, _CACHE, _IDS, _IDS, C.c_float, _HEADS, *_WORK]),
     "sllm_attention_cached_workspace": (C.c_int32, [_HEADS, _HEADS, _HEADS, _CACHE, _IDS, _IDS, _U64]),
     "sllm_last_error": (C.c_char_p, []),

@@ -214,3 +214,53 @@ extern "C" int32_t sllm_attention_cached_workspace(const sllm_heads* q, const sl
     return SLLM_OK;
 }
 SLLM_CATCH_ALL
+
+extern "C" int32_t sllm_attention_grad(const sllm_heads* dout, const sllm_heads* q, const sllm_heads* k, const sllm_heads* v,
+                                       const sllm_heads* out, const float* lse, const sllm_ids* offsets, uint64_t window, uint64_t sinks,
+                                       float scale, const sllm_heads* dq, const sllm_heads* dk, const sllm_heads* dv, void* workspace,
+                                       uint64_t workspace_bytes, int32_t device, void* stream) try {
+    clear_error();
+    AttentionGradArgs a;
+    Span s[11];
+    int n = 4;
+    SLLM_TRY(common_args(q, k, v, scale, &a, s, &n));
+    SLLM_TRY(out_args("out", out, *q, &a, &s[n++]));
+    SLLM_TRY(heads_span("dout", dout, &s[n++]));
+    SLLM_TRY(same_shape("dout", *dout, *q, q->heads));
+    SLLM_TRY(heads_span("dq", dq, &s[0]));
+    SLLM_TRY(same_shape("dq", *dq, *q, q->heads));
+    SLLM_TRY(heads_span("dk", dk, &s[1]));
+    SLLM_TRY(same_shape("dk", *dk, *k, k->heads));
+    SLLM_TRY(heads_span("dv", dv, &s[2]));
+    SLLM_TRY(same_shape("dv", *dv, *v, k->heads));
+    if (!lse && a.tokens && a.heads) return fail(SLLM_E_INVAL, "lse: NULL");
+    SLLM_TRY(lse_span("lse", lse, a, &s[n++]));
+    SLLM_TRY(offsets_args(offsets, &a, &s[n++]));
+    window_args(window, sinks, &a);
+    SLLM_TRY(workspace_span(workspace, workspace_bytes, attention_grad_workspace(a), &s[3]));
+    a.lse = const_cast<float*>(lse);
+    a.dout = dout->data, a.dout_token = dout->token_stride, a.dout_head = dout->head_stride;
+    a.dq = dq->data, a.dq_token = dq->token_stride, a.dq_head = dq->head_stride;
+    a.dk = dk->data, a.dk_token = dk->token_stride, a.dk_head = dk->head_stride;
+    a.dv = dv->data, a.dv_token = dv->token_stride, a.dv_head = dv->head_stride;
+    a.vec = a.vec && aligned(*dout) && aligned(*dq) && aligned(*dk) && aligned(*dv);
+    DeviceGuard guard(device);
+    if (!guard.ok()) return fail(SLLM_E_HIP, "cannot make device %d current", device);
+    SLLM_TRY(check_spans(s, n, 4, device));
+    if (!a.tokens || !a.heads || !a.dim) return SLLM_OK;
+    return launch_attention_grad(a, workspace, static_cast<hipStream_t>(stream));
+}
+SLLM_CATCH_ALL
+
+extern "C" int32_t sllm_attention_grad_workspace(const sllm_heads* q, const sllm_heads* k, const sllm_ids* offsets, uint64_t* bytes) try {
+    clear_error();
+    if (!bytes) return fail(SLLM_E_INVAL, "bytes: NULL");
+    AttentionArgs a;
+    Span s[4];
+    int n = 0;
+    SLLM_TRY(common_args(q, k, k, 1.0f, &a, s, &n));
+    SLLM_TRY(offsets_args(offsets, &a, &s[n]));
+    *bytes = attention_grad_workspace(a);
+    return SLLM_OK;
+}
+SLLM_CATCH_ALL

@@ -35,25 +35,21 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t c = lane & 31, h = lane >> 5;
 
-    // neighbouring pieces of a head on one XCD
-    const uint32_t blocks = gridDim.x, xcd = blockIdx.x % 8, q8 = blocks / 8, rest = blocks % 8;
-    const uint32_t index = xcd * q8 + min(xcd, rest) + blockIdx.x / 8;
+    const uint32_t index = xcd_index();
     const uint32_t head = index / a.pieces;  // of keys and values
     const Piece piece = find_piece(a.offsets, a.wide_offsets, a.sequences, a.tokens, a.group, kRows, index % a.pieces, a.pieces);
     T* const out = static_cast<T*>(a.out);
     int64_t past = 0;
     if (Cached && piece.n) past = read_id(a.lengths, a.wide_lengths, piece.sequence);
     if (!piece.n || past < 0) {
-        // rows of no sequence, or of one that takes no part, are zeros
-        uint32_t from = piece.piece, to = a.tokens - (piece.past_end - piece.first), step = piece.spare;
-        if (piece.n) from = piece.piece, to = piece.n, step = (uint32_t)(((uint64_t)piece.n * a.group + kRows - 1) / kRows);
-        for (uint32_t t = from; t < to; t += step) {
-            const uint32_t token = piece.n ? piece.first + t : t < piece.first ? t : t - piece.first + piece.past_end;
-            for (uint32_t i = threadIdx.x; i < a.group * a.dim; i += kWaves * 64)
-                out[token * a.out_token + (head * a.group + i / a.dim) * a.out_head + i % a.dim] = (T)0.0f;
-            if (a.lse)
-                for (uint32_t i = threadIdx.x; i < a.group; i += kWaves * 64) a.lse[(uint64_t)token * a.heads + head * a.group + i] = 0.0f;
-        }
+        // tokens of no sequence, or of one that takes no part
+        Piece none = piece;
+        uint32_t tokens = a.tokens;
+        if (piece.n) none.spare = (uint32_t)(((uint64_t)piece.n * a.group + kRows - 1) / kRows), tokens = none.n;
+        T* const from = out + (piece.n ? piece.first * a.out_token : 0);
+        if (piece.n) none.first = none.past_end = 0;
+        clear_spare(none, tokens, from, a.out_token, a.out_head, head * a.group, a.group, a.dim);
+        if (a.lse) clear_spare(none, tokens, a.lse, a.heads, 1, head * a.group, a.group, 1);
         return;
     }
     const uint32_t rows = piece.n * a.group;  // fewer than 2^32
@@ -152,7 +148,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             p[2 * n + 1] = as_operand<T>(s[n], 1);
         }
         sum += part;
-        add_weighted<T, D, kKeys, kMasked>(acc, v, columns_at, p, sees);
+        add_weighted<T, D, kKeys, kMasked>(acc, v, columns_at, 0, p, sees);
     };
     const auto step = [&](int32_t i0, const uint8_t* k, const uint8_t* v, uint8_t* next_k, uint8_t* next_v) SLLM_INLINE {
         wait_but_loads<0>();
@@ -174,24 +170,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     if (wave_row + c >= rows) return;
     const uint64_t out_row = piece.first + token;
     if (a.lse && h == 0) a.lse[out_row * a.heads + q_head] = (m_scaled + __builtin_amdgcn_logf(sum)) * kLn2;
-    const float f = 1.0f / sum;
-    T* const p = out + out_row * a.out_token + q_head * a.out_head;
-#pragma unroll
-    for (int d = 0; d < kParts; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const uint32_t e = 32 * d + 8 * g + 4 * h;
-            T v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(acc[d][4 * g + i] * f);
-            if (Vec) {
-                if (e < a.dim) __builtin_memcpy(__builtin_assume_aligned(p + e, 4 * sizeof(T)), v, sizeof v);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (e + i < a.dim) p[e + i] = v[i];
-            }
-        }
+    store_column<T, D, Vec>(acc, 1.0f / sum, out + out_row * a.out_token + q_head * a.out_head, a.dim);
 }
 
 // The new tokens of each sequence into its cache, after the attention that still reads

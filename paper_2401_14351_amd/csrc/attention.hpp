@@ -206,12 +206,12 @@ __device__ __forceinline__ bool take_out(Operand8<T>& o) {
     return any != 0;
 }
 
-// acc and the elements that take_out took of `Rows` rows, in lanes that see(row).
+// acc and the elements that take_out took of `Rows` rows from row0 on, in lanes that see(row).
 template <typename T, int D, int Rows, typename See>
-__device__ __forceinline__ f32x16 with_taken_out(f32x16 acc, const uint8_t* tile, uint32_t column0, const See see) {
+__device__ __forceinline__ f32x16 with_taken_out(f32x16 acc, const uint8_t* tile, int row0, uint32_t column0, const See see) {
     const uint32_t h = threadIdx.x >> 5 & 1;
 #pragma unroll 1
-    for (int row = 0; row < Rows; ++row) {
+    for (int row = row0; row < row0 + Rows; ++row) {
         const bool seen = see(row);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -224,22 +224,22 @@ __device__ __forceinline__ f32x16 with_taken_out(f32x16 acc, const uint8_t* tile
     return acc;
 }
 
-// acc[d] += the sum over `Rows` rows of a tile of element 32 d .. of the row times the
-// weight of the lane's column, w(t) being the operand of rows 16 t on.
+// acc[d] += the sum over `Rows` rows of a tile, from row0 on, of elements 32 d .. of the row
+// times the weight of the lane's column, w[t] being the operand of rows 16 t on.
 template <typename T, int D, int Rows, bool Masked, typename See>
-__device__ __forceinline__ void add_weighted(f32x16 (&acc)[D / 32], const uint8_t* tile, uint32_t from, const Operand8<T> (&w)[Rows / 16],
-                                             const See& see) {
+__device__ __forceinline__ void add_weighted(f32x16 (&acc)[D / 32], const uint8_t* tile, uint32_t from, int row0,
+                                             const Operand8<T> (&w)[Rows / 16], const See& see) {
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) {
         bool out = false;
 #pragma unroll
         for (int t = 0; t < Rows / 16; ++t) {
-            Operand8<T> v = read_columns<T, D>(tile, from, 16 * t, 32 * d);
+            Operand8<T> v = read_columns<T, D>(tile, from, row0 + 16 * t, 32 * d);
             if constexpr (Masked) out |= take_out(v);
             acc[d] = multiply(v, w[t], acc[d]);
         }
         if constexpr (Masked)
-            if (__any(out)) acc[d] = with_taken_out<T, D, Rows>(acc[d], tile, 32 * d, see);
+            if (__any(out)) acc[d] = with_taken_out<T, D, Rows>(acc[d], tile, row0, 32 * d, see);
     }
 }
 
@@ -302,6 +302,47 @@ __device__ __forceinline__ Piece find_piece(const void* offsets, bool wide, uint
         start = __builtin_amdgcn_readlane(end, 63);
     }
     return {0, first_row, 0, index - before, pieces - before, start};
+}
+
+// The tile of a workgroup: neighbouring ones of a head on one XCD, whose L2 then holds its keys.
+__device__ __forceinline__ uint32_t xcd_index() {
+    const uint32_t xcd = blockIdx.x % 8, q = gridDim.x / 8, rest = gridDim.x % 8;
+    return xcd * q + min(xcd, rest) + blockIdx.x / 8;
+}
+
+// Zeros into the share of a workgroup without a piece: rows `head0` .. + heads - 1 of
+// tokens that belong to no sequence.
+template <typename T>
+__device__ __forceinline__ void clear_spare(const Piece& p, uint32_t tokens, T* out, uint64_t token_stride, uint64_t head_stride,
+                                            uint32_t head0, uint32_t heads, uint32_t dim) {
+    const uint32_t n = tokens - (p.past_end - p.first);
+    for (uint32_t t = p.piece; t < n; t += p.spare) {
+        const uint64_t token = t < p.first ? t : t - p.first + p.past_end;
+        for (uint32_t i = threadIdx.x; i < heads * dim; i += blockDim.x)
+            out[token * token_stride + (head0 + i / dim) * head_stride + i % dim] = (T)0.0f;
+    }
+}
+
+// A lane's column of (elements x columns) sums times f, to a row in memory.
+template <typename T, int D, bool Vec>
+__device__ __forceinline__ void store_column(const f32x16 (&acc)[D / 32], float f, T* row, uint32_t dim) {
+    const uint32_t h = threadIdx.x >> 5 & 1;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const uint32_t e = 32 * d + 8 * g + 4 * h;
+            T v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(acc[d][4 * g + i] * f);
+            if (Vec) {
+                if (e < dim) __builtin_memcpy(__builtin_assume_aligned(row + e, 4 * sizeof(T)), v, sizeof v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (e + i < dim) row[e + i] = v[i];
+            }
+        }
 }
 
 // The keys that the queries at positions i0 to i1 of a sequence see: the first `sinks`

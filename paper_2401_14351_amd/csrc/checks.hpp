@@ -52,10 +52,10 @@ inline int32_t matrix_span(const char* name, const sllm_matrix* m, Span* out) {
     return check_pointer(*out, size);
 }
 
-inline int32_t mx_spans(const char* codes, const char* scales, const sllm_mx* m, Span* out) {
+inline int32_t mx_spans(const char* codes, const char* scales, const sllm_mx* m, Span* out, bool fp8 = false) {
     if (!m) return fail(SLLM_E_INVAL, "%s: NULL", codes);
     SLLM_TRY(check_extent(codes, m->rows, m->cols));
-    out[0] = Span{codes, static_cast<const uint8_t*>(m->codes), m->rows * mx_code_pitch(m->cols)};
+    out[0] = Span{codes, static_cast<const uint8_t*>(m->codes), m->rows * (fp8 ? mx8_code_pitch(m->cols) : mx_code_pitch(m->cols))};
     out[1] = Span{scales, static_cast<const uint8_t*>(m->scales), m->rows * mx_scale_pitch(m->cols)};
     SLLM_TRY(check_pointer(out[0], 16));
     return check_pointer(out[1], 16);

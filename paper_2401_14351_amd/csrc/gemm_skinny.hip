@@ -56,13 +56,18 @@ struct Parts<__bf16> {
     __device__ __forceinline__ void set(const __bf16 (&x)[8]) { __builtin_memcpy(v, x, sizeof v); }
 };
 
-// X, or four bits of it a byte
+// X, or four or eight bits of it a byte
+struct Fp8 {};
 template <typename X>
 struct Element {
     typedef X type;
 };
 template <>
 struct Element<void> {
+    typedef uint8_t type;
+};
+template <>
+struct Element<Fp8> {
     typedef uint8_t type;
 };
 
@@ -141,7 +146,7 @@ __device__ __forceinline__ u32x4 transpose4(u32x4 v) {
 template <typename X, int Rows, int MT>
 __global__ __launch_bounds__(1024) void skinny_product(SkinnyArgs a) {
     extern __shared__ float sums[];
-    constexpr bool kMx = __is_same(X, void);
+    constexpr bool kFp8 = __is_same(X, Fp8), kMx = __is_same(X, void) || kFp8;
     constexpr uint32_t kPieces = 16 / Rows;
     static_assert((Rows == 1 || Rows == 4 || Rows == 16) && (Rows == 16 || MT == 1), "");
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -181,12 +186,22 @@ __global__ __launch_bounds__(1024) void skinny_product(SkinnyArgs a) {
             }
     };
     if constexpr (kMx) {
-        u32x4 x[2][MT] = {};
+        // of four bits a lane has block g of a step, of eight a half each of two blocks:
+        // of blocks g / 2 and 2 + g / 2 elements 16 (g % 2) to 16 (g % 2) + 15
+        constexpr int kWords = kFp8 ? 2 : 1;
+        u32x4 x[2][MT][kWords] = {};
         uint32_t scales[MT] = {};
         auto load_x = [&](uint32_t step, int to) SLLM_INLINE {
 #pragma unroll
             for (int m = 0; m < MT; ++m)
-                if (has_x[m]) x[to][m] = static_cast<const u32x4*>(a.x)[x_row[m] * a.blocks + min((uint64_t)step * 4 + g, a.blocks - 1)];
+                if (has_x[m])
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) {
+                        const u32x4* row = static_cast<const u32x4*>(a.x) + x_row[m] * a.blocks * kWords;
+                        const uint64_t b = (uint64_t)step * 4 + (kFp8 ? 2 * i + g / 2 : g);
+                        x[to][m][i] = kFp8 ? row[min(b, a.blocks - 1) * 2 + g % 2] : row[min(b, a.blocks - 1)];
+                        if (kFp8 && b >= a.blocks) x[to][m][i] = u32x4{0, 0, 0, 0};
+                    }
         };
         if (g0 < g1) load_x(g0 * 4, 0);
         run([&](uint32_t group, const Group& held, int) SLLM_INLINE {
@@ -200,9 +215,17 @@ __global__ __launch_bounds__(1024) void skinny_product(SkinnyArgs a) {
                 const uint32_t mask = (uint64_t)group * kGroupBlocks + 4 * u + g < a.blocks ? ~0u : 0;
                 const uint32_t ws = step_scales(held.scales, u, r) >> (8 * g) & mask;
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
-                    acc[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(held.codes[u]), fragment(x[u % 2][m] & mask), acc[m],
-                                                                              4, 4, 0, ws, 0, step_scales(scales[m], u, r) >> (8 * g) & mask);
+                for (int m = 0; m < MT; ++m) {
+                    const uint32_t xs = step_scales(scales[m], u, r) >> (8 * g) & mask;
+                    if constexpr (kFp8) {
+                        const u32x4 lo = x[u % 2][m][0], hi = x[u % 2][m][1];
+                        const i32x8 v = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+                        acc[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(held.codes[u]), v, acc[m], 4, 0, 0, ws, 0, xs);
+                    } else {
+                        acc[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(held.codes[u]), fragment(x[u % 2][m][0] & mask), acc[m],
+                                                                                  4, 4, 0, ws, 0, xs);
+                    }
+                }
             }
         });
     } else {
@@ -325,7 +348,9 @@ void launch(const SkinnyArgs& a, hipStream_t stream) {
 }  // namespace
 
 int32_t launch_skinny(const SkinnyArgs& a, hipStream_t stream) {
-    if (a.x_scales && a.m <= 16)
+    if (a.x_fp8)
+        launch<Fp8, 16, 1>(a, stream);
+    else if (a.x_scales && a.m <= 16)
         launch<void, 16, 1>(a, stream);
     else if (a.x_scales)
         launch<void, 16, 2>(a, stream);

@@ -136,7 +136,7 @@ struct Plan {
 // 32000 x 4096 71 and 67; MX FP4 16 rows 11.3 and 15.2, 32 rows 17.1 and 15.6.
 bool few_rows(const LinearLaunch& a) {
     if (a.grad) return false;
-    if (a.x.codes) return a.m <= 32 && a.m * a.n <= 1 << 18;
+    if (a.x.codes) return a.m <= (a.x.fp8 ? 16 : 32) && a.m * a.n <= 1 << 18;
     if (a.m <= 4) return true;
     if (a.x.dtype == SLLM_DTYPE_F16) return a.m <= 16 && a.n <= 8192;
     return a.m <= 16 && a.m * a.n <= (a.x.dtype == SLLM_DTYPE_F32 ? 1 << 18 : 1 << 17);
@@ -334,7 +334,7 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
     if (a.x.codes) {
         const NarrowArgs n{reinterpret_cast<const u32x4*>(a.x.codes), a.x.scales, reinterpret_cast<const u32x4*>(a.w_codes),
                            a.w_scales, a.m, a.n, mx_blocks(a.k), mx_scale_pitch(a.k), p.steps, p.tiles_m, p.tiles_j, o};
-        SLLM_TRY(launch_narrow(n, p.tile_n, p.splits, out, dtype, stream));
+        SLLM_TRY((a.x.fp8 ? launch_mx8 : launch_narrow)(n, p.tile_n, p.splits, out, dtype, stream));
     } else {
         WideArgs w;
         SLLM_TRY(stage_x(a, p, workspace, &w, stream));
@@ -359,7 +359,7 @@ int32_t launch_linear(const LinearLaunch& a, void* workspace, hipStream_t stream
     if (plan.skinny && plan.depth) {
         const uint64_t row_bytes = a.x.stride * (a.x.dtype == SLLM_DTYPE_F32 ? 4 : 2);
         const bool vector = reinterpret_cast<uintptr_t>(a.x.data) % 16 == 0 && (a.m == 1 || row_bytes % 16 == 0);
-        return launch_skinny(SkinnyArgs{a.x.codes ? a.x.codes : a.x.data, a.x.scales, a.m, a.n, a.k, a.x.stride, a.x.dtype, vector,
+        return launch_skinny(SkinnyArgs{a.x.codes ? a.x.codes : a.x.data, a.x.scales, a.x.fp8, a.m, a.n, a.k, a.x.stride, a.x.dtype, vector,
                                         reinterpret_cast<const u32x4*>(a.w_codes), a.w_scales, mx_blocks(a.k), mx_scale_pitch(a.k),
                                         (uint32_t)ceil_div(a.k, 512), a.out, a.out_stride, a.out_dtype}, stream);
     }

@@ -10,13 +10,13 @@ namespace sllm {
 
 namespace {
 
-Operand operand(const sllm_matrix& m) { return Operand{m.data, m.stride, m.dtype, nullptr, nullptr}; }
+Operand operand(const sllm_matrix& m) { return Operand{m.data, m.stride, m.dtype, nullptr, nullptr, false}; }
 
-Operand operand(const sllm_mx& m) {
-    return Operand{nullptr, 0, 0, static_cast<const uint8_t*>(m.codes), static_cast<const uint8_t*>(m.scales)};
+Operand operand(const sllm_mx& m, bool fp8 = false) {
+    return Operand{nullptr, 0, 0, static_cast<const uint8_t*>(m.codes), static_cast<const uint8_t*>(m.scales), fp8};
 }
 
-// What a product is of, from its operands: x is a matrix or in MX FP4.
+// What a product is of, from its operands: x is a matrix, or in MX FP4 or FP8.
 struct LinearArgs {
     LinearLaunch a;
     Span x[2], w[2];
@@ -24,13 +24,13 @@ struct LinearArgs {
     uint64_t out_cols = 0;
 };
 
-int32_t linear_args(const sllm_matrix* x, const sllm_mx* x_mx, const sllm_mx* w, bool grad, LinearArgs* out) {
+int32_t linear_args(const sllm_matrix* x, const sllm_mx* x_mx, const sllm_mx* w, bool grad, LinearArgs* out, bool fp8 = false) {
     uint64_t rows, cols;
     if (x_mx || !x) {
-        SLLM_TRY(mx_spans("x codes", "x scales", x_mx, out->x));
+        SLLM_TRY(mx_spans("x codes", "x scales", x_mx, out->x, fp8));
         out->n_x = 2;
         rows = x_mx->rows, cols = x_mx->cols;
-        out->a.x = operand(*x_mx);
+        out->a.x = operand(*x_mx, fp8);
     } else {
         SLLM_TRY(matrix_span(grad ? "dy" : "x", x, out->x));
         out->n_x = 1;
@@ -50,9 +50,9 @@ int32_t linear_args(const sllm_matrix* x, const sllm_mx* x_mx, const sllm_mx* w,
 }
 
 int32_t linear(const sllm_matrix* x, const sllm_mx* x_mx, const sllm_mx* w, const sllm_matrix* out, bool grad,
-               void* workspace, uint64_t workspace_bytes, int32_t device, void* stream) {
+               void* workspace, uint64_t workspace_bytes, int32_t device, void* stream, bool fp8 = false) {
     LinearArgs l;
-    SLLM_TRY(linear_args(x, x_mx, w, grad, &l));
+    SLLM_TRY(linear_args(x, x_mx, w, grad, &l, fp8));
     Span s[6];
     int n = 0;
     SLLM_TRY(matrix_span(grad ? "dx" : "out", out, &s[n++]));
@@ -74,10 +74,10 @@ int32_t linear(const sllm_matrix* x, const sllm_mx* x_mx, const sllm_mx* w, cons
     return launch_linear(l.a, workspace, static_cast<hipStream_t>(stream));
 }
 
-int32_t linear_bytes(const sllm_matrix* x, const sllm_mx* x_mx, const sllm_mx* w, bool grad, uint64_t* bytes) {
+int32_t linear_bytes(const sllm_matrix* x, const sllm_mx* x_mx, const sllm_mx* w, bool grad, uint64_t* bytes, bool fp8 = false) {
     if (!bytes) return fail(SLLM_E_INVAL, "bytes: NULL");
     LinearArgs l;
-    SLLM_TRY(linear_args(x, x_mx, w, grad, &l));
+    SLLM_TRY(linear_args(x, x_mx, w, grad, &l, fp8));
     *bytes = linear_workspace(l.a);
     return SLLM_OK;
 }
@@ -177,6 +177,13 @@ extern "C" int32_t sllm_mx_linear_mx(const sllm_mx* x, const sllm_mx* w, const s
 }
 SLLM_CATCH_ALL
 
+extern "C" int32_t sllm_mx_linear_octet(const sllm_mx* x, const sllm_mx* w, const sllm_matrix* out, void* workspace,
+                                      uint64_t workspace_bytes, int32_t device, void* stream) try {
+    clear_error();
+    return linear(nullptr, x, w, out, false, workspace, workspace_bytes, device, stream, true);
+}
+SLLM_CATCH_ALL
+
 extern "C" int32_t sllm_mx_linear_grad(const sllm_matrix* dy, const sllm_mx* w, const sllm_matrix* dx, void* workspace,
                                        uint64_t workspace_bytes, int32_t device, void* stream) try {
     clear_error();
@@ -195,6 +202,12 @@ SLLM_CATCH_ALL
 extern "C" int32_t sllm_mx_linear_mx_workspace(const sllm_mx* x, const sllm_mx* w, uint64_t* bytes) try {
     clear_error();
     return linear_bytes(nullptr, x, w, false, bytes);
+}
+SLLM_CATCH_ALL
+
+extern "C" int32_t sllm_mx_linear_octet_workspace(const sllm_mx* x, const sllm_mx* w, uint64_t* bytes) try {
+    clear_error();
+    return linear_bytes(nullptr, x, w, false, bytes, true);
 }
 SLLM_CATCH_ALL
 

@@ -16,15 +16,17 @@ constexpr uint32_t kMxBlockBytes = 16;  // their codes
 
 inline uint64_t mx_blocks(uint64_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
 inline uint64_t mx_code_pitch(uint64_t cols) { return mx_blocks(cols) * kMxBlockBytes; }
+inline uint64_t mx8_code_pitch(uint64_t cols) { return mx_blocks(cols) * kMxBlock; }
 inline uint64_t mx_scale_pitch(uint64_t cols) { return (mx_blocks(cols) + 15) / 16 * 16; }
 
-// One operand of a product: a matrix, or one in MX FP4 (codes set).
+// One operand of a product: a matrix, or one in MX FP4 or FP8 (codes set).
 struct Operand {
     const void* data = nullptr;
     uint64_t stride = 0;
     uint32_t dtype = 0;
     const uint8_t* codes = nullptr;
     const uint8_t* scales = nullptr;
+    bool fp8 = false;
 };
 
 // out (m x n) = x (m x k) * transpose(w), w in MX FP4 n x k; or, with `grad`,
@@ -76,6 +78,34 @@ constexpr uint64_t kMaxGradIds = 1ull << 24;
 uint64_t embedding_grad_workspace(uint64_t n_ids, uint64_t vocab, uint64_t dim);
 int32_t launch_embedding_grad(const EmbeddingGradLaunch& a, void* workspace, hipStream_t stream);
 
+// h = x + residual (h = x where there is none); y = h / sqrt(mean h^2 + eps) * gain, as a
+// matrix or in MX FP8 (codes set).
+struct NormLaunch {
+    const void *x = nullptr, *residual = nullptr, *gain = nullptr;
+    uint64_t x_stride = 0, residual_stride = 0, rows = 0, cols = 0;
+    uint32_t dtype = 0, gain_dtype = 0;
+    float eps = 0;
+    void *h = nullptr, *y = nullptr;
+    uint64_t h_stride = 0, y_stride = 0;
+    float* inverse = nullptr;  // of each row's root mean square, if not null
+    uint8_t *codes = nullptr, *scales = nullptr;
+};
+int32_t launch_rms_norm(const NormLaunch& a, hipStream_t stream);
+
+struct NormGradLaunch {
+    const void *dy = nullptr, *dh = nullptr, *h = nullptr, *gain = nullptr;
+    uint64_t dy_stride = 0, dh_stride = 0, h_stride = 0, rows = 0, cols = 0;
+    uint32_t dtype = 0, gain_dtype = 0;
+    const float* inverse = nullptr;
+    void *dx = nullptr, *dgain = nullptr;
+    uint64_t dx_stride = 0;
+};
+uint64_t rms_norm_grad_workspace(uint64_t rows, uint64_t cols);
+int32_t launch_rms_norm_grad(const NormGradLaunch& a, void* workspace, hipStream_t stream);
+
+int32_t launch_mx8_quantize(const sllm_matrix& src, const sllm_mx& dst, hipStream_t stream);
+int32_t launch_mx8_dequantize(const sllm_mx& src, const sllm_matrix& dst, hipStream_t stream);
+
 // Causal attention of packed sequences, or behind what a cache holds of them (cache_k set).
 // Strides are in elements; window, sinks and tokens are below 2^30.
 struct AttentionArgs {
@@ -98,6 +128,16 @@ struct AttentionArgs {
     uint32_t element = 0;  // bytes
 };
 int32_t launch_attention(AttentionArgs a, hipStream_t stream);
+
+struct AttentionGradArgs : AttentionArgs {  // out is read
+    const void* dout = nullptr;
+    uint64_t dout_token = 0, dout_head = 0;
+    void *dq = nullptr, *dk = nullptr, *dv = nullptr;
+    uint64_t dq_token = 0, dq_head = 0, dk_token = 0, dk_head = 0, dv_token = 0, dv_head = 0;
+    float* rows = nullptr;  // tokens x heads, twice
+};
+uint64_t attention_grad_workspace(const AttentionArgs& a);
+int32_t launch_attention_grad(AttentionGradArgs a, void* workspace, hipStream_t stream);
 
 // One new token a sequence, tokens and sequences being the same.
 uint64_t attention_step_workspace(const AttentionArgs& a);

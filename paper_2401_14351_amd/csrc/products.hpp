@@ -350,12 +350,15 @@ struct NarrowArgs {
     OutArgs out_args;
 };
 int32_t launch_narrow(const NarrowArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
+// The same with x in MX FP8: its codes are 32 bytes a block.
+int32_t launch_mx8(const NarrowArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
 constexpr uint32_t kNarrowStep = 512;  // depth whose scales are loaded together
 
-// At most 32 rows of x in MX FP4 (x_scales set), 16 in other types.
+// At most 32 rows of x in MX FP4 (x_scales set), 16 in MX FP8 (x_fp8 too) and other types.
 struct SkinnyArgs {
     const void* x;
     const uint8_t* x_scales;
+    bool x_fp8;
     uint64_t m, n, depth, x_stride;
     uint32_t x_dtype;
     uint32_t vector;  // rows of x start on 16 bytes

@@ -40,25 +40,24 @@ _DTYPE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _ID_BITS = {torch.int32: 32, torch.int64: 64}
 
 
-def _pitches(cols: int):
-    blocks = -(-cols // BLOCK)
-    return blocks * 16, -(-blocks // 16) * 16
-
-
-class Mx4:
-    """A matrix in MX FP4: ``codes`` (rows, blocks * 16) and ``scales`` (rows,
-    blocks rounded up to 16), both contiguous uint8, laid out as ``sllm_mx``.
-    It is those tensors, wherever their storage is when it is used."""
+class _Mx:
+    """Codes and scales of a matrix in blocks of 32 columns."""
 
     __slots__ = ("_codes", "_scales", "_cols")
+    _BLOCK_BYTES: int  # of codes
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int):
         self._codes, self._scales, self._cols = codes, scales, cols
         self._check()
 
+    @classmethod
+    def _pitches(cls, cols: int):
+        blocks = -(-cols // BLOCK)
+        return blocks * cls._BLOCK_BYTES, -(-blocks // 16) * 16
+
     def _check(self):
         cols = self._cols
-        code_pitch, scale_pitch = _pitches(cols)
+        code_pitch, scale_pitch = self._pitches(cols)
         for name, t, pitch in (("codes", self._codes, code_pitch), ("scales", self._scales, scale_pitch)):
             if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[1] != pitch or not t.is_contiguous():
                 raise ValueError(f"{name}: expected a contiguous uint8 tensor of {pitch} columns for {cols} columns, "
@@ -67,27 +66,27 @@ class Mx4:
             raise ValueError("codes and scales differ in rows or device")
 
     @classmethod
-    def _of(cls, codes: torch.Tensor, scales: torch.Tensor, cols: int) -> "Mx4":
+    def _of(cls, codes: torch.Tensor, scales: torch.Tensor, cols: int):
         """The same without a check."""
         q = cls.__new__(cls)
         q._codes, q._scales, q._cols = codes, scales, cols
         return q
 
     @classmethod
-    def empty(cls, rows: int, cols: int, device) -> "Mx4":
+    def empty(cls, rows: int, cols: int, device):
         """A matrix whose contents are not set."""
-        code_pitch, scale_pitch = _pitches(cols)
+        code_pitch, scale_pitch = cls._pitches(cols)
         return cls._of(torch.empty((rows, code_pitch), dtype=torch.uint8, device=device),
                        torch.empty((rows, scale_pitch), dtype=torch.uint8, device=device), cols)
 
     @classmethod
-    def _beside(cls, t: torch.Tensor, rows: int, cols: int) -> "Mx4":
+    def _beside(cls, t: torch.Tensor, rows: int, cols: int):
         """One whose contents are not set, where t is: half a microsecond less than by naming the device."""
-        code_pitch, scale_pitch = _pitches(cols)
+        code_pitch, scale_pitch = cls._pitches(cols)
         return cls._of(t.new_empty((rows, code_pitch), dtype=torch.uint8), t.new_empty((rows, scale_pitch), dtype=torch.uint8), cols)
 
     def __reduce__(self):
-        return Mx4, (self._codes, self._scales, self._cols)
+        return type(self), (self._codes, self._scales, self._cols)
 
     @property
     def _struct(self) -> binding.Mx:
@@ -122,14 +121,31 @@ class Mx4:
     def nbytes(self) -> int:
         return self.codes.numel() + self.scales.numel()
 
-    def __getitem__(self, rows: slice) -> "Mx4":
+    def __getitem__(self, rows: slice):
         """A run of rows, sharing this matrix's memory."""
         if not isinstance(rows, slice) or rows.step not in (None, 1):
-            raise ValueError("an Mx4 is indexed by a run of rows")
-        return Mx4(self.codes[rows], self.scales[rows], self.cols)
+            raise ValueError(f"an {type(self).__name__} is indexed by a run of rows")
+        return type(self)(self.codes[rows], self.scales[rows], self.cols)
 
     def __repr__(self):
-        return f"Mx4({self.rows} x {self.cols}, {self.device})"
+        return f"{type(self).__name__}({self.rows} x {self.cols}, {self.device})"
+
+
+class Mx4(_Mx):
+    """A matrix in MX FP4: ``codes`` (rows, blocks * 16) and ``scales`` (rows,
+    blocks rounded up to 16), both contiguous uint8, laid out as ``sllm_mx``.
+    It is those tensors, wherever their storage is when it is used."""
+
+    __slots__ = ()
+    _BLOCK_BYTES = 16
+
+
+class Mx8(_Mx):
+    """Activations in MX FP8, 8.25 bits a value: as :class:`Mx4`, with ``codes`` (rows,
+    blocks * 32), an E4M3 value each."""
+
+    __slots__ = ()
+    _BLOCK_BYTES = 32
 
 
 def _matrix(t: torch.Tensor, name: str) -> binding.Matrix:
@@ -178,7 +194,7 @@ def _ids(t: torch.Tensor) -> binding.Ids:
 
 
 def _index(t) -> int:
-    return (t._codes if isinstance(t, Mx4) else t).get_device()
+    return (t._codes if isinstance(t, _Mx) else t).get_device()
 
 
 def _one_device(first, *others) -> int:
@@ -209,7 +225,7 @@ def _on_stream(stream, operator, *args, keep=(), **kwargs):
         result = operator(*args, **kwargs)
     for t in keep:
         if t is not None:
-            for u in ((t.codes, t.scales) if isinstance(t, Mx4) else (t,)):
+            for u in ((t.codes, t.scales) if isinstance(t, _Mx) else (t,)):
                 u.record_stream(stream)
     return result
 
@@ -344,16 +360,16 @@ def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, out: Optional[to
     return y
 
 
-def mx4_linear(x: Union[torch.Tensor, Mx4], w: Mx4, out: Optional[torch.Tensor] = None,
+def mx4_linear(x: Union[torch.Tensor, Mx4, Mx8], w: Mx4, out: Optional[torch.Tensor] = None,
                out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
     """``x @ w.T``: (..., w.rows) for x (..., w.cols).
 
     x as a tensor keeps its own precision; as an :class:`Mx4` both sides are in
-    four bits.  The result has ``out_dtype``, by default x's type (bfloat16 for
-    an :class:`Mx4`)."""
+    four bits, as an :class:`Mx8` x is in eight.  The result has ``out_dtype``, by
+    default x's type (bfloat16 for an :class:`Mx4` or :class:`Mx8`)."""
     if stream is not None:
         return _on_stream(stream, mx4_linear, x, w, out, out_dtype, keep=(x, w, out))
-    if isinstance(x, Mx4):
+    if isinstance(x, _Mx):
         return _linear_mx(x, w, out, out_dtype)
     _refuse_tangent(x)
     if x.requires_grad and torch.is_grad_enabled():
@@ -380,6 +396,12 @@ def _linear(x, w, out, out_dtype):
 def _linear_mx(x, w, out, out_dtype):
     device = _one_device(x, w)
     code = _DTYPE.get(out_dtype or torch.bfloat16)
+    if isinstance(x, Mx8):
+        L = binding.lib()
+        y, rows = _output(out, (x.rows, w.rows), x.rows, w.rows, out_dtype or torch.bfloat16, x.codes)
+        _call(L.sllm_mx_linear_octet, L.sllm_mx_linear_octet_workspace, (x._struct, w._struct), rows, device)
+        _written(out)
+        return y
     if out is None and device >= 0 and code is not None and _native() is not None:
         native = _native()
         y = native.ext.product_mx(native.mx_linear_mx, native.mx_linear_mx_workspace, x._codes, x._scales, x._cols, w._codes,
@@ -391,6 +413,38 @@ def _linear_mx(x, w, out, out_dtype):
     L = binding.lib()
     y, rows = _output(out, (x.rows, w.rows), x.rows, w.rows, out_dtype or torch.bfloat16, x.codes)
     _call(L.sllm_mx_linear_mx, L.sllm_mx_linear_mx_workspace, (x._struct, w._struct), rows, device)
+    _written(out)
+    return y
+
+
+def mx8_quantize(x: torch.Tensor, out: Optional[Mx8] = None, stream=None) -> Mx8:
+    """The rows of x (its leading dimensions flattened) in MX FP8, for :func:`mx4_linear`.
+    No gradient passes, as for :func:`mx4_quantize`."""
+    if stream is not None:
+        return _on_stream(stream, mx8_quantize, x, out, keep=(x, out))
+    _refuse_tangent(x)
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError("x requires a gradient, which quantisation does not pass on")
+    src = _matrix(x, "x")
+    device = _one_device(x, out)
+    q = Mx8._beside(x, src.rows, src.cols) if out is None else out
+    if not isinstance(q, Mx8) or q.rows != src.rows or q.cols != src.cols:
+        raise ValueError(f"out: expected an Mx8 of {src.rows} x {src.cols}, got {q!r}")
+    binding.check(binding.lib().sllm_mx_octet_quantize(src, q._struct, device, _raw_stream(device)))
+    if out is not None:
+        _written(out.codes, out.scales)
+    return q
+
+
+def mx8_dequantize(q: Mx8, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The values q stands for, rounded to ``dtype`` (or the type of ``out``)."""
+    if stream is not None:
+        return _on_stream(stream, mx8_dequantize, q, dtype, out, keep=(q, out))
+    if not isinstance(q, Mx8):
+        raise ValueError(f"expected an Mx8, got {q!r}")
+    device = _index(q)
+    y, rows = _output(out, (q.rows, q.cols), q.rows, q.cols, dtype, q.codes)
+    binding.check(binding.lib().sllm_mx_octet_dequantize(q._struct, rows, device, _raw_stream(device)))
     _written(out)
     return y
 
@@ -527,6 +581,83 @@ class _Embedding(torch.autograd.Function):
     def backward(ctx, dy):
         (tokens,) = ctx.saved_tensors
         return embedding_grad(dy.contiguous(), tokens, ctx.vocab, ctx.scale, out_dtype=ctx.dtype), None, None, None
+
+
+# ---------------------------------------------------------------------------
+# norms
+# ---------------------------------------------------------------------------
+
+def rms_norm(x: torch.Tensor, gain: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-5, mx8: bool = False,
+             stream=None):
+    """h / sqrt(mean h^2 + eps) * gain over the last dimension, in x's type, h being x, or
+    with a residual ``x + residual`` rounded to their type: then the norm and h.
+
+    ``gain`` may be of another type.  With ``mx8`` the norm is an :class:`Mx8`, its rows
+    the leading dimensions flattened, and no gradient passes."""
+    if stream is not None:
+        return _on_stream(stream, rms_norm, x, gain, residual, eps, mx8, keep=(x, gain, residual))
+    for t in (x, gain, residual):
+        _refuse_tangent(t)
+    if torch.is_grad_enabled() and (x.requires_grad or gain.requires_grad or (residual is not None and residual.requires_grad)):
+        if mx8:
+            raise ValueError("a tensor requires a gradient, which a norm in MX FP8 does not pass on")
+        y, h = _RmsNorm.apply(x, gain, residual, eps)
+        return y if residual is None else (y, h)
+    y, h, _ = _rms_norm(x, gain, residual, eps, mx8, False)
+    return y if residual is None else (y, h)
+
+
+def _rms_norm(x, gain, residual, eps, mx8, keep):
+    """The norm, h and, with ``keep``, each row's inverse root mean square."""
+    src, g = _matrix(x, "x"), _matrix(gain, "gain")
+    if gain.dim() != 1:
+        raise ValueError(f"gain: expected one dimension, got shape {tuple(gain.shape)}")
+    device, r, h, rows = _one_device(x, gain, residual), None, x, None
+    if residual is not None:
+        if residual.shape != x.shape or residual.dtype != x.dtype:
+            raise ValueError(f"residual: expected {x.dtype} of shape {tuple(x.shape)}, got {residual.dtype} of shape {tuple(residual.shape)}")
+        r = _matrix(residual, "residual")
+        h, rows = _output(None, x.shape, src.rows, src.cols, x.dtype, x)
+    L, stream = binding.lib(), _raw_stream(device)
+    if mx8:
+        y = Mx8._beside(x, src.rows, src.cols)
+        binding.check(L.sllm_rms_norm_octet(src, r, g, eps, rows, y._struct, device, stream))
+        return y, h, None
+    y, y_rows = _output(None, x.shape, src.rows, src.cols, x.dtype, x)
+    inverse = torch.empty(src.rows, dtype=torch.float32, device=x.device) if keep else None
+    binding.check(L.sllm_rms_norm(src, r, g, eps, rows, y_rows, inverse.data_ptr() if keep else None, device, stream))
+    return y, h, inverse
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gain, residual, eps):
+        ctx.set_materialize_grads(False)
+        y, h, inverse = _rms_norm(x, gain, residual, eps, False, True)
+        ctx.save_for_backward(h, gain, inverse)
+        ctx.residual = residual is not None
+        if residual is None:
+            h = None
+        return y, h
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dh):
+        h, gain, inverse = ctx.saved_tensors
+        if dy is None:  # h alone has been used
+            return dh, None, dh if ctx.residual else None, None
+        # gradients of sums and means arrive with strides of 0
+        dy, dh = dy.contiguous(), None if dh is None else dh.contiguous()
+        rows, device = _matrix(h, "h"), h.get_device()
+        dx, dx_rows = _output(None, h.shape, rows.rows, rows.cols, h.dtype, h)
+        dgain = torch.empty(gain.shape, dtype=gain.dtype, device=gain.device)
+        L = binding.lib()
+        n = _workspace(L.sllm_rms_norm_grad_workspace, rows.rows, rows.cols)
+        ws = torch.empty(n, dtype=torch.uint8, device=h.device) if n else None
+        binding.check(L.sllm_rms_norm_grad(_matrix(dy, "dy"), None if dh is None else _matrix(dh, "dh"), rows, _matrix(gain, "gain"),
+                                           inverse.data_ptr(), dx_rows, _matrix(dgain, "dgain"), ws.data_ptr() if n else None, n, device,
+                                           _raw_stream(device)))
+        return dx, dgain, dx if ctx.residual else None, None
 
 
 # ---------------------------------------------------------------------------
@@ -709,3 +840,18 @@ class _Attention(torch.autograd.Function):
         ctx.save_for_backward(q, k, v, out, lse, offsets)
         ctx.window, ctx.sinks, ctx.scale = window, sinks, scale
         return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        q, k, v, out, lse, offsets = ctx.saved_tensors
+        dout = dout.contiguous()  # gradients of sums and means arrive with strides of 0
+        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        L, device, ids = binding.lib(), q.get_device(), _index_tensor(offsets, "offsets")
+        rows = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
+        n = _workspace(L.sllm_attention_grad_workspace, *rows[:2], ids)
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+        binding.check(L.sllm_attention_grad(
+            _heads(dout, "dout"), *rows, _heads(out, "out"), lse.data_ptr(), ids, _window(ctx.window, ctx.sinks), min(ctx.sinks, 1 << 62),
+            ctx.scale, _heads(dq, "dq"), _heads(dk, "dk"), _heads(dv, "dv"), ws.data_ptr() if n else None, n, device, _raw_stream(device)))
+        return dq, dk, dv, None, None, None, None
