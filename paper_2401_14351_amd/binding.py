@@ -163,7 +163,7 @@ SIGNATURES = {
     "sllm_mx_linear_mx_workspace": (C.c_int32, [_MX, _MX, _U64]),
     "sllm_mx_linear_grad_workspace": (C.c_int32, [_MATRIX, _MX, _U64]),
     "sllm_mx_linear_octet": (C.c_int32, [_MX, _MX, _MATRIX, *_WORK]),
-    "sllm_mx_linear_octet_workspace": (C.c_int32, [_MX, _MX, _U64]),
+    "sllm_mx_linear_octet_workspace": (C.c_int32, [_MX, _MX, C.c_uint32, _U64]),
     "sllm_mx_octet_sizes": (C.c_int32, [C.c_uint64, C.c_uint64, _U64, _U64]),
     "sllm_mx_octet_quantize": (C.c_int32, [_MATRIX, _MX, C.c_int32, C.c_void_p]),
     "sllm_mx_octet_dequantize": (C.c_int32, [_MX, _MATRIX, C.c_int32, C.c_void_p]),

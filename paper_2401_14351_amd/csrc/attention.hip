@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     // this wave's rows, the last one again past the end
     const uint32_t wave_row = row0 + wave * kWaveRows, row = min(wave_row + c, rows - 1);
     const uint32_t token = row / a.group, q_head = head * a.group + row % a.group;
-    const int32_t at = base + (int32_t)token;
+    const KeyList::Sight sight = keys.sight(base + (int32_t)token);
     const int32_t at0 = base + (int32_t)(min(wave_row, rows - 1) / a.group), at1 = base + (int32_t)(min(wave_row + 31, rows - 1) / a.group);
     Operand8<T> q[kSteps];
     {
@@ -78,21 +78,38 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     if (Cached) slot0 = keys.lo < a.sinks ? (int32_t)(keys.lo - a.sinks) : (int32_t)((uint64_t)(keys.lo - a.sinks) % (uint32_t)a.window);
     const uint64_t cache_row = Cached ? ((uint64_t)piece.sequence * a.kv_heads + head) * a.slots : 0;
     const auto key_row = [&](const void* fresh, uint64_t token_stride, uint64_t head_stride, const void* cache, int32_t i) SLLM_INLINE -> const T* {
-        if (i >= keys.total) return nullptr;
+        const bool none = i >= keys.total;
+        i = min(i, keys.total - 1);
         const int32_t k = i - keys.sinks;
         const T* const rows_of = static_cast<const T*>(fresh) + head * head_stride;
         if constexpr (!Cached) {
             const uint32_t token = k < 0 ? (uint32_t)i : (uint32_t)((int32_t)keys.lo + k);
-            return rows_of + (uint64_t)(piece.first + token) * token_stride;
+            const T* p = rows_of + (uint64_t)(piece.first + token) * token_stride;
+            return none ? nullptr : p;
         } else {
             const int32_t fresh_one = k < 0 ? i - past_sinks : k - held;  // of this call's tokens, or before them
-            if (fresh_one >= 0) return rows_of + (uint64_t)(piece.first + (uint32_t)fresh_one) * token_stride;
+            const T* p = rows_of + (uint64_t)(piece.first + (uint32_t)max(fresh_one, 0)) * token_stride;
             int32_t slot = k < 0 ? i : slot0 + k;
             if (k >= 0) slot = a.sinks + (slot >= a.window ? slot - a.window : slot);
-            return static_cast<const T*>(cache) + (cache_row + (uint32_t)slot) * a.dim;
+            p = fresh_one >= 0 ? p : static_cast<const T*>(cache) + (cache_row + (uint32_t)slot) * a.dim;
+            return none ? nullptr : p;
         }
     };
+    // Tiles whose keys lie one behind the other need no look at each.
+    constexpr bool kRepeat = Vec && !Cached;
+    const bool repeats = kRepeat && a.dim == D && max(a.k_token, a.v_token) < (1u << 24);
+    LaneOffsets<T, D, kKeys, kWaves> k_at, v_at;
+    if constexpr (kRepeat) {
+        k_at.set(k_at.kRun * a.k_token, [&](uint32_t r) SLLM_INLINE { return r * (uint32_t)a.k_token; });
+        v_at.set(v_at.kRun * a.v_token, [&](uint32_t r) SLLM_INLINE { return r * (uint32_t)a.v_token; });
+    }
     const auto stage = [&](int32_t i0, uint8_t* k, uint8_t* v) SLLM_INLINE {
+        if (repeats && i0 >= keys.sinks && i0 + kKeys <= keys.total) {
+            const uint64_t token = piece.first + (uint32_t)((int32_t)keys.lo + i0 - keys.sinks);
+            k_at.stage(k, static_cast<const T*>(a.k) + head * a.k_head + token * a.k_token);
+            v_at.stage(v, static_cast<const T*>(a.v) + head * a.v_head + token * a.v_token);
+            return;
+        }
         stage_rows<T, D, kKeys, kWaves, Vec>(k, a.dim, [&](uint32_t r) SLLM_INLINE { return key_row(a.k, a.k_token, a.k_head, a.cache_k, i0 + (int32_t)r); });
         stage_rows<T, D, kKeys, kWaves, Vec>(v, a.dim, [&](uint32_t r) SLLM_INLINE { return key_row(a.v, a.v_token, a.v_head, a.cache_v, i0 + (int32_t)r); });
     };
@@ -106,19 +123,31 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     for (int d = 0; d < kParts; ++d) acc[d] = f32x16{};
     const uint32_t rows_at = rows_from<T, D>(lane), columns_at = columns_from<T, D>(lane);
 
-    const auto tile = [&](int32_t i0, const uint8_t* k, const uint8_t* v, auto masked) SLLM_INLINE {
-        constexpr bool kMasked = decltype(masked)::value;
+    bool out_of_sight = false;  // something was taken out
+    const auto tile = [&](int32_t i0, const uint8_t* k, const uint8_t* v, bool masked) SLLM_INLINE {
         f32x16 s[kKeys / 32];
-        const auto sees = [&](int r) SLLM_INLINE { return i0 + r < keys.total && keys.sees(at, i0 + r); };
+        RowFragments<T, D> kf[kKeys / 32];
+        ColumnFragments<T, D, kKeys> vf;
+        kf[0].read(k, rows_at, 0);
+        phase();
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int n = 0; n < kKeys / 32; ++n) {
-            s[n] = f32x16{};
+            if (n + 1 < kKeys / 32)
+                kf[n + 1].read(k, rows_at, 32 * (n + 1));
+            else
+                vf.read(v, columns_at, 0, 0);
+            s[n] = kf[n].times(q);
+            phase();
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if (masked) {
+            const KeyList::Sight here = sight.here();
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) s[n] = multiply(read_rows<T, D>(k, rows_at, 32 * n, i), q[i], s[n]);
-            if constexpr (kMasked)
+            for (int n = 0; n < kKeys / 32; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (!sees(32 * n + 8 * (i / 4) + 4 * h + i % 4)) s[n][i] = -__builtin_inff();
+                    s[n][i] = here.sees(i0 + 32 * n + 8 * (i / 4) + 4 * (int32_t)h + i % 4) ? s[n][i] : -__builtin_inff();
         }
         float top = s[0][0];
 #pragma unroll
@@ -148,16 +177,16 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             p[2 * n + 1] = as_operand<T>(s[n], 1);
         }
         sum += part;
-        add_weighted<T, D, kKeys, kMasked>(acc, v, columns_at, 0, p, sees);
+        phase();
+        __builtin_amdgcn_s_setprio(1);
+        out_of_sight |= add_weighted<T, D, kKeys>(acc, vf, v, columns_at, 0, p, masked);
+        __builtin_amdgcn_s_setprio(0);
     };
     const auto step = [&](int32_t i0, const uint8_t* k, const uint8_t* v, uint8_t* next_k, uint8_t* next_v) SLLM_INLINE {
         wait_but_loads<0>();
         barrier();  // this tile has landed, and all waves are done with the other one
         if (i0 + kKeys < keys.total) stage(i0 + kKeys, next_k, next_v);
-        if (keys.all(at0, at1, i0, i0 + kKeys - 1))
-            tile(i0, k, v, std::false_type());
-        else if (!keys.none(at0, at1, i0, i0 + kKeys - 1))
-            tile(i0, k, v, std::true_type());
+        if (!keys.none(at0, at1, i0, i0 + kKeys - 1)) tile(i0, k, v, !keys.all(at0, at1, i0, i0 + kKeys - 1));
     };
     stage(0, k0, v0);
     for (int32_t i0 = 0; i0 < keys.total; i0 += 2 * kKeys) {
@@ -165,6 +194,9 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         if (i0 + kKeys < keys.total) step(i0 + kKeys, k1, v1, k0, v0);
     }
 
+    if (__any(out_of_sight))
+        for (int32_t i = 0; i < keys.total; ++i)
+            put_back<T, D>(acc, key_row(a.v, a.v_token, a.v_head, a.cache_v, i), a.dim, sight.sees(i));
     const f32x2 sums = both_halves(sum);
     sum = sums[0] + sums[1];
     if (wave_row + c >= rows) return;

@@ -54,6 +54,35 @@ __device__ __forceinline__ void stage_rows(uint8_t* to, uint32_t dim, const At& 
     }
 }
 
+// The same from rows that are whole and whose places repeat: row r + kRun n of a tile is n
+// times `step` bytes behind row r.  A lane then needs one place of its own, or where its
+// chunk changes from load to load two.
+template <typename T, int D, int Rows, int Waves>
+struct LaneOffsets {
+    typedef RowTile<T, D> Tile;
+    static constexpr uint32_t kLoads = Rows / Tile::kLoadRows / Waves, kRun = Waves * Tile::kLoadRows < 16 ? 16 : Waves * Tile::kLoadRows;
+    static constexpr uint32_t kPlaces = kRun / (Waves * Tile::kLoadRows);
+    uint32_t bytes[kPlaces];
+    uint64_t step;
+
+    template <typename At>  // element offset of row r, below kRun
+    __device__ __forceinline__ void set(uint64_t step_elements, const At& at) {
+        const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        step = step_elements * sizeof(T);
+#pragma unroll
+        for (uint32_t q = 0; q < kPlaces; ++q) {
+            const uint32_t row = (q * Waves + wave) * Tile::kLoadRows + lane / Tile::kChunks;
+            bytes[q] = (uint32_t)(at(row) + ((lane % Tile::kChunks) ^ Tile::turn(row)) * Tile::kElements) * (uint32_t)sizeof(T);
+        }
+    }
+    __device__ __forceinline__ void stage(uint8_t* to, const T* base) const {
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (uint32_t q = 0; q < kLoads; ++q)
+            load_to_lds(reinterpret_cast<const uint8_t*>(base) + q / kPlaces * step + bytes[q % kPlaces], to, (q * Waves + wave) * 1024);
+    }
+};
+
 // Eight elements of a lane: an operand of 16 of the depth by 32 rows or columns, of which
 // lane (r, h) has row r and depths 8 h to 8 h + 7.
 template <typename T>
@@ -178,8 +207,8 @@ __device__ __forceinline__ f32x2 both_halves(float x) {
 }
 
 // Products with rows of which some columns must see nothing: what is not a number there
-// would come through a weight of zero.  Such elements are taken out of the operand, and
-// added, as they are, to the columns that see their row.
+// would come through a weight of zero.  Such elements are taken out of the operand, and at
+// the end added, as they are, to the columns that see their row.
 template <typename T>
 __device__ __forceinline__ uint32_t not_finite(uint32_t word) {  // halves that are not, as all ones
     constexpr uint32_t kExponent = __is_same(T, _Float16) ? 0x7c00 : 0x7f80;
@@ -206,41 +235,83 @@ __device__ __forceinline__ bool take_out(Operand8<T>& o) {
     return any != 0;
 }
 
-// acc and the elements that take_out took of `Rows` rows from row0 on, in lanes that see(row).
-template <typename T, int D, int Rows, typename See>
-__device__ __forceinline__ f32x16 with_taken_out(f32x16 acc, const uint8_t* tile, int row0, uint32_t column0, const See see) {
+// acc with what was taken out: the elements of a row in memory that are not finite, where
+// the lane's column sees it.  To be called for all rows: one that has been added already
+// changes nothing the second time.
+template <typename T, int D>
+__device__ __forceinline__ void put_back(f32x16 (&acc)[D / 32], const T* row, uint32_t dim, bool seen) {
     const uint32_t h = threadIdx.x >> 5 & 1;
-#pragma unroll 1
-    for (int row = row0; row < row0 + Rows; ++row) {
-        const bool seen = see(row);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const uint32_t c = column0 + 8 * (i / 4) + 4 * h + i % 4;
-            const T v = lds_read<T>(tile, RowTile<T, D>::at(row, c / RowTile<T, D>::kElements) + c % RowTile<T, D>::kElements * sizeof(T));
-            const float f = to_f32(v);
-            if (seen && !(__builtin_fabsf(f) < __builtin_inff())) acc[i] += f;
+            const uint32_t e = 32 * d + 8 * (i / 4) + 4 * h + i % 4;
+            if (e >= dim) continue;
+            const float f = to_f32(row[e]);
+            if (seen && !(__builtin_fabsf(f) < __builtin_inff())) acc[d][i] += f;
         }
-    }
-    return acc;
 }
 
-// acc[d] += the sum over `Rows` rows of a tile, from row0 on, of elements 32 d .. of the row
-// times the weight of the lane's column, w[t] being the operand of rows 16 t on.
-template <typename T, int D, int Rows, bool Masked, typename See>
-__device__ __forceinline__ void add_weighted(f32x16 (&acc)[D / 32], const uint8_t* tile, uint32_t from, int row0,
-                                             const Operand8<T> (&w)[Rows / 16], const See& see) {
+// Keeps what is before it before what is after it.  Fragments are read in runs, a run ahead
+// of the products that take them: left alone the compiler reads each just before its own.
+__device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
+
+// Rows row0 to row0 + 31 of a tile, as operands.
+template <typename T, int D>
+struct RowFragments {
+    Operand8<T> f[D / 16];
+
+    __device__ __forceinline__ void read(const uint8_t* tile, uint32_t from, int row0) {
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d) {
+        for (int s = 0; s < D / 16; ++s) f[s] = read_rows<T, D>(tile, from, row0, s);
+    }
+    // their products with the lane's columns
+    __device__ __forceinline__ f32x16 times(const Operand8<T> (&columns)[D / 16]) const {
+        f32x16 acc = {};
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) acc = multiply(f[s], columns[s], acc);
+        return acc;
+    }
+};
+
+// Elements 32 d to 32 d + 31 of `Rows` rows, likewise, for acc += the sum over the rows of
+// those times the weight of the lane's column, w[t] being the operand of rows 16 t on.
+template <typename T, int D, int Rows>
+struct ColumnFragments {
+    Operand8<T> f[Rows / 16];
+
+    __device__ __forceinline__ void read(const uint8_t* tile, uint32_t from, int row0, int d) {
+#pragma unroll
+        for (int t = 0; t < Rows / 16; ++t) f[t] = read_columns<T, D>(tile, from, row0 + 16 * t, 32 * d);
+    }
+    __device__ __forceinline__ void add(f32x16& acc, const Operand8<T> (&w)[Rows / 16]) const {
+#pragma unroll
+        for (int t = 0; t < Rows / 16; ++t) acc = multiply(f[t], w[t], acc);
+    }
+    __device__ __forceinline__ bool take_out() {
         bool out = false;
 #pragma unroll
-        for (int t = 0; t < Rows / 16; ++t) {
-            Operand8<T> v = read_columns<T, D>(tile, from, row0 + 16 * t, 32 * d);
-            if constexpr (Masked) out |= take_out(v);
-            acc[d] = multiply(v, w[t], acc[d]);
-        }
-        if constexpr (Masked)
-            if (__any(out)) acc[d] = with_taken_out<T, D, Rows>(acc[d], tile, row0, 32 * d, see);
+        for (int t = 0; t < Rows / 16; ++t) out |= sllm::take_out(f[t]);
+        return out;
     }
+};
+
+// All of them; the first are read already.  masked: some column must not see some row;
+// whether anything was taken out.
+template <typename T, int D, int Rows>
+__device__ __forceinline__ bool add_weighted(f32x16 (&acc)[D / 32], ColumnFragments<T, D, Rows>& first, const uint8_t* tile, uint32_t from,
+                                             int row0, const Operand8<T> (&w)[Rows / 16], bool masked) {
+    bool out = false;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) {
+        ColumnFragments<T, D, Rows> next;
+        if (d + 1 < D / 32) next.read(tile, from, row0, d + 1);
+        if (masked) out |= first.take_out();
+        first.add(acc[d], w);
+        phase();
+        if (d + 1 < D / 32) first = next;
+    }
+    return out;
 }
 
 // ---------------------------------------------------------------------------
@@ -359,10 +430,23 @@ struct KeyList {
         early = (int32_t)max((int64_t)0, all_sinks - lo);
         total = sinks + (int32_t)(i1 - lo + 1);
     }
-    // whether the query at lo + q sees key c
-    __device__ __forceinline__ bool sees(int32_t q, int32_t c) const {
-        const int32_t k = c - sinks;
-        return k <= q && (k < early || q - k < window);
+    // What the query at lo + q sees: up to its own key, all but those from the last sink to
+    // the window.
+    struct Sight {
+        int32_t last, hidden;
+        uint32_t n_hidden;
+
+        __device__ __forceinline__ bool sees(int32_t c) const { return (c <= last) & ((uint32_t)(c - hidden) >= n_hidden); }
+        // the same, not to be found out before this is reached
+        __device__ __forceinline__ Sight here() const {
+            Sight s = *this;
+            asm volatile("" : "+v"(s.last), "+v"(s.hidden), "+v"(s.n_hidden));
+            return s;
+        }
+    };
+    __device__ __forceinline__ Sight sight(int32_t q) const {
+        const int32_t hidden = sinks + early;
+        return {min(q + sinks, total - 1), hidden, (uint32_t)max(0, q + sinks - window + 1 - hidden)};
     }
     // whether all queries lo + q0 .. lo + q1 see keys c0 .. c1, and whether none sees any
     __device__ __forceinline__ bool all(int32_t q0, int32_t q1, int32_t c0, int32_t c1) const {

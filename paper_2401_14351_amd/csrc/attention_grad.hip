@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     const int32_t lo = (int32_t)keys.lo;
     const uint32_t wave_row = row0 + wave * kWaveRows, row = min(wave_row + c, rows - 1);
     const uint32_t token = row / a.group, q_head = head * a.group + row % a.group;
-    const int32_t at = (int32_t)token - lo;
+    const KeyList::Sight sight = keys.sight((int32_t)token - lo);
     const int32_t at0 = (int32_t)(min(wave_row, rows - 1) / a.group) - lo, at1 = (int32_t)(min(wave_row + 31, rows - 1) / a.group) - lo;
     const uint64_t packed = piece.first + token;
     Operand8<T> q[kSteps], dout[kSteps];
@@ -91,11 +91,23 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         a.rows[(uint64_t)a.tokens * a.heads + packed * a.heads + q_head] = delta;
     }
 
+    const bool repeats = Vec && a.dim == D && max(a.k_token, a.v_token) < (1u << 24);
+    LaneOffsets<T, D, kKeys, kWaves> k_at, v_at;
+    if constexpr (Vec) {
+        k_at.set(k_at.kRun * a.k_token, [&](uint32_t r) SLLM_INLINE { return r * (uint32_t)a.k_token; });
+        v_at.set(v_at.kRun * a.v_token, [&](uint32_t r) SLLM_INLINE { return r * (uint32_t)a.v_token; });
+    }
     const auto stage = [&](int32_t i0, uint8_t* k, uint8_t* v) SLLM_INLINE {
+        if (repeats && i0 >= keys.sinks && i0 + kKeys <= keys.total) {
+            const uint64_t token = piece.first + (uint32_t)(lo + i0 - keys.sinks);
+            k_at.stage(k, static_cast<const T*>(a.k) + head * a.k_head + token * a.k_token);
+            v_at.stage(v, static_cast<const T*>(a.v) + head * a.v_head + token * a.v_token);
+            return;
+        }
         const auto row_of = [&](const void* from, uint64_t token_stride, uint64_t head_stride, uint32_t r) SLLM_INLINE -> const T* {
-            const int32_t i = i0 + (int32_t)r, n = i - keys.sinks;
-            if (i >= keys.total) return nullptr;
-            return static_cast<const T*>(from) + head * head_stride + (uint64_t)(piece.first + (uint32_t)(n < 0 ? i : lo + n)) * token_stride;
+            const int32_t i = min(i0 + (int32_t)r, keys.total - 1), n = i - keys.sinks;
+            const T* p = static_cast<const T*>(from) + head * head_stride + (uint64_t)(piece.first + (uint32_t)(n < 0 ? i : lo + n)) * token_stride;
+            return i0 + (int32_t)r < keys.total ? p : nullptr;
         };
         stage_rows<T, D, kKeys, kWaves, Vec>(k, a.dim, [&](uint32_t r) SLLM_INLINE { return row_of(a.k, a.k_token, a.k_head, r); });
         stage_rows<T, D, kKeys, kWaves, Vec>(v, a.dim, [&](uint32_t r) SLLM_INLINE { return row_of(a.v, a.v_token, a.v_head, r); });
@@ -105,21 +117,30 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     for (int d = 0; d < kParts; ++d) acc[d] = f32x16{};
     Range range;
     const uint32_t rows_at = rows_from<T, D>(lane), columns_at = columns_from<T, D>(lane);
-    const auto tile = [&](int32_t i0, const uint8_t* k, const uint8_t* v, auto masked) SLLM_INLINE {
-        constexpr bool kMasked = decltype(masked)::value;
-        const auto sees = [&](int r) SLLM_INLINE { return i0 + r < keys.total && keys.sees(at, i0 + r); };
+    bool out_of_sight = false;  // something was taken out
+    const auto tile = [&](int32_t i0, const uint8_t* k, const uint8_t* v, bool masked) SLLM_INLINE {
         Operand8<T> ds[kKeys / 16];
+        RowFragments<T, D> kf, vf;
+        ColumnFragments<T, D, kKeys> cf;
+        kf.read(k, rows_at, 0);
 #pragma unroll
         for (int n = 0; n < kKeys / 32; ++n) {
-            f32x16 s = {}, dp = {};
+            phase();
+            vf.read(v, rows_at, 32 * n);
+            f32x16 s = kf.times(q);
+            phase();
+            if (n + 1 < kKeys / 32)
+                kf.read(k, rows_at, 32 * (n + 1));
+            else
+                cf.read(k, columns_at, 0, 0);
+            const f32x16 dp = vf.times(dout);
+            phase();
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) s = multiply(read_rows<T, D>(k, rows_at, 32 * n, i), q[i], s);
+            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -lse)) * (dp[i] - delta);
+            if (masked) {
+                const KeyList::Sight here = sight.here();
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) dp = multiply(read_rows<T, D>(v, rows_at, 32 * n, i), dout[i], dp);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -lse)) * (dp[i] - delta);
-                if (kMasked && !sees(32 * n + 8 * (i / 4) + 4 * h + i % 4)) s[i] = 0;
+                for (int i = 0; i < 16; ++i) s[i] = here.sees(i0 + 32 * n + 8 * (i / 4) + 4 * (int32_t)h + i % 4) ? s[i] : 0.0f;
             }
             if constexpr (kHalf) {
                 const float before = range.up;
@@ -136,22 +157,24 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             ds[2 * n] = as_operand<T>(s, 0);
             ds[2 * n + 1] = as_operand<T>(s, 1);
         }
-        add_weighted<T, D, kKeys, kMasked>(acc, k, columns_at, 0, ds, sees);
+        phase();
+        out_of_sight |= add_weighted<T, D, kKeys>(acc, cf, k, columns_at, 0, ds, masked);
     };
     const auto step = [&](int32_t i0, const uint8_t* k, const uint8_t* v, uint8_t* next_k, uint8_t* next_v) SLLM_INLINE {
         wait_but_loads<0>();
         barrier();
         if (i0 + kKeys < keys.total) stage(i0 + kKeys, next_k, next_v);
-        if (keys.all(at0, at1, i0, i0 + kKeys - 1))
-            tile(i0, k, v, std::false_type());
-        else if (!keys.none(at0, at1, i0, i0 + kKeys - 1))
-            tile(i0, k, v, std::true_type());
+        if (!keys.none(at0, at1, i0, i0 + kKeys - 1)) tile(i0, k, v, !keys.all(at0, at1, i0, i0 + kKeys - 1));
     };
     stage(0, k0, v0);
     for (int32_t i0 = 0; i0 < keys.total; i0 += 2 * kKeys) {
         step(i0, k0, v0, k1, v1);
         if (i0 + kKeys < keys.total) step(i0 + kKeys, k1, v1, k0, v0);
     }
+    if (__any(out_of_sight))
+        for (int32_t i = 0; i < keys.total; ++i)
+            put_back<T, D>(acc, static_cast<const T*>(a.k) + head * a.k_head + (uint64_t)(piece.first + (uint32_t)(i < keys.sinks ? i : lo + i - keys.sinks)) * a.k_token,
+                           a.dim, sight.sees(i));
     if (wave_row + c >= rows) return;
     store_column<T, D, Vec>(acc, kHalf ? a.scale / range.up : a.scale, dq + packed * a.dq_token + q_head * a.dq_head, a.dim);
 }
@@ -159,52 +182,90 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
 // dv = p^T dout and dk = scale ds^T q, over the rows (tokens times heads that share the
 // key) that see a key.  A wave has 32 keys, whose statistics are their lanes' own, and the
 // rows come by; scores are of (rows x keys), their gradients' sums of (elements x keys).
+//
+// Two waves of a SIMD hide each other's waits: for that a wave has its keys and the sums in
+// registers, but takes its values from LDS each time.
 template <typename T, int D, bool Vec>
-__global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 128 ? 1 : 2) void attention_grad_kv(AttentionGradArgs a) {
-    constexpr int kTile = tile_rows<T>(), kSteps = D / 16, kParts = D / 32;
+__global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void attention_grad_kv(AttentionGradArgs a) {
+    constexpr int kTile = 32, kSteps = D / 16, kParts = D / 32;
     constexpr bool kHalf = __is_same(T, _Float16);
     constexpr uint32_t kBytes = kTile * RowTile<T, D>::kPitch;
     __shared__ __align__(16) uint8_t q0[kBytes], o0[kBytes], q1[kBytes], o1[kBytes];
     __shared__ __align__(16) uint8_t l0[256], d0[256], l1[256], d1[256];  // rows' lse and delta
+    __shared__ __align__(16) uint8_t values[kRows * RowTile<T, D>::kPitch];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t c = lane & 31, h = lane >> 5;
-    const uint32_t index = xcd_index(), head = index / a.pieces;
-    const Piece piece = find_piece(a.offsets, a.wide_offsets, a.sequences, a.tokens, 1, kRows, index % a.pieces, a.pieces);
+    const uint32_t index = xcd_index(), split = index % a.splits, head = index / a.splits / a.pieces;
+    const Piece piece = find_piece(a.offsets, a.wide_offsets, a.sequences, a.tokens, 1, kRows, index / a.splits % a.pieces, a.pieces);
     T *const dk = static_cast<T*>(a.dk), *const dv = static_cast<T*>(a.dv);
+    // sums of a part of the rows, to be joined: of this split, keys and then values
+    const uint64_t part_token = (uint64_t)a.kv_heads * a.dim, part_size = a.tokens * part_token;
+    float *const part_k = a.parts + 2 * split * part_size, *const part_v = part_k + part_size;
     if (!piece.n) {
-        clear_spare(piece, a.tokens, dk, a.dk_token, a.dk_head, head, 1, a.dim);
-        clear_spare(piece, a.tokens, dv, a.dv_token, a.dv_head, head, 1, a.dim);
+        if (a.splits > 1) {
+            clear_spare(piece, a.tokens, part_k, part_token, a.dim, head, 1, a.dim);
+            clear_spare(piece, a.tokens, part_v, part_token, a.dim, head, 1, a.dim);
+        } else {
+            clear_spare(piece, a.tokens, dk, a.dk_token, a.dk_head, head, 1, a.dim);
+            clear_spare(piece, a.tokens, dv, a.dv_token, a.dv_head, head, 1, a.dim);
+        }
         return;
     }
     const uint32_t window = a.window, sinks = a.sinks;
     const uint32_t key0 = piece.piece * kRows, key1 = min(key0 + kRows, piece.n) - 1;
     const uint32_t last = key0 < sinks ? piece.n - 1 : min(piece.n - 1, key1 + window - 1);  // the last token that sees one
-    const uint32_t row_first = key0 * a.group, row_end = (last + 1) * a.group;
+    const uint32_t all_first = key0 * a.group, all_end = (last + 1) * a.group;
+    // this split's rows, whole tiles of them, perhaps none
+    const uint32_t share = ((all_end - all_first + kTile - 1) / kTile + a.splits - 1) / a.splits * kTile;
+    const uint32_t row_first = min(all_first + split * share, all_end), row_end = min(row_first + share, all_end);
     const uint32_t wave_key0 = min(key0 + wave * kWaveRows, key1), wave_key1 = min(wave_key0 + kWaveRows - 1, key1);
     const uint32_t key = min(key0 + wave * kWaveRows + c, key1);
-    Operand8<T> k[kSteps], v[kSteps];
+    // the rows that see a key
+    const auto seen_rows = [&](uint32_t key, uint32_t& from, uint32_t& n) SLLM_INLINE {
+        from = key * a.group;
+        n = (key < sinks ? piece.n - key : min(piece.n - key, window)) * a.group;
+    };
+    Operand8<T> k[kSteps];
     {
         const T* p = static_cast<const T*>(a.k) + (uint64_t)(piece.first + key) * a.k_token + head * a.k_head;
-        const T* pv = static_cast<const T*>(a.v) + (uint64_t)(piece.first + key) * a.v_token + head * a.v_head;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            k[s] = load8<T, Vec>(p, 16 * s + 8 * h, a.dim);
-            v[s] = load8<T, Vec>(pv, 16 * s + 8 * h, a.dim);
-        }
+        for (int s = 0; s < kSteps; ++s) k[s] = load8<T, Vec>(p, 16 * s + 8 * h, a.dim);
     }
-    const auto stage = [&](uint32_t r0, uint8_t* q, uint8_t* dout, uint8_t* lse, uint8_t* delta) SLLM_INLINE {
-        const auto row_of = [&](const void* from, uint64_t token_stride, uint64_t head_stride, uint32_t r) SLLM_INLINE -> const T* {
-            const uint32_t row = r0 + r, token = row / a.group;
-            if (row >= row_end) return nullptr;
-            return static_cast<const T*>(from) + (uint64_t)(piece.first + token) * token_stride + (head * a.group + row - token * a.group) * head_stride;
+    stage_rows<T, D, kRows, kWaves, Vec>(values, a.dim, [&](uint32_t r) SLLM_INLINE -> const T* {
+        return static_cast<const T*>(a.v) + (uint64_t)(piece.first + min(key0 + r, key1)) * a.v_token + head * a.v_head;
+    });
+    // Tiles whose rows lie alike, a whole number of tokens each, need no look at each.
+    typedef LaneOffsets<T, D, kTile, kWaves> Offsets;
+    const bool repeats = Vec && a.dim == D && Offsets::kRun % a.group == 0 && max(max(a.q_token, a.dout_token), max(a.q_head, a.dout_head)) < (1u << 24);
+    Offsets q_at, o_at;
+    if constexpr (Vec) {
+        const uint32_t tokens = Offsets::kRun / a.group;
+        const auto place = [&](uint64_t token_stride, uint64_t head_stride, uint32_t r) SLLM_INLINE {
+            return r / a.group * (uint32_t)token_stride + r % a.group * (uint32_t)head_stride;
         };
-        stage_rows<T, D, kTile, kWaves, Vec>(q, a.dim, [&](uint32_t r) SLLM_INLINE { return row_of(a.q, a.q_token, a.q_head, r); });
-        stage_rows<T, D, kTile, kWaves, Vec>(dout, a.dim, [&](uint32_t r) SLLM_INLINE { return row_of(a.dout, a.dout_token, a.dout_head, r); });
+        q_at.set(tokens * a.q_token, [&](uint32_t r) SLLM_INLINE { return place(a.q_token, a.q_head, r); });
+        o_at.set(tokens * a.dout_token, [&](uint32_t r) SLLM_INLINE { return place(a.dout_token, a.dout_head, r); });
+    }
+    const uint32_t heads0 = head * a.group;
+    const auto stage = [&](uint32_t r0, uint8_t* q, uint8_t* dout, uint8_t* lse, uint8_t* delta) SLLM_INLINE {
         if (wave < 2) {
             const uint32_t row = min(r0 + lane % kTile, row_end - 1), token = row / a.group;
             const float* p = a.rows + (wave ? (uint64_t)a.tokens * a.heads : 0);
-            load_word_to_lds(p + (uint64_t)(piece.first + token) * a.heads + head * a.group + row - token * a.group, wave ? delta : lse, 0);
+            load_word_to_lds(p + (uint64_t)(piece.first + token) * a.heads + heads0 + row - token * a.group, wave ? delta : lse, 0);
         }
+        if (repeats && r0 + kTile <= row_end) {
+            const uint64_t token = piece.first + r0 / a.group;
+            q_at.stage(q, static_cast<const T*>(a.q) + token * a.q_token + heads0 * a.q_head);
+            o_at.stage(dout, static_cast<const T*>(a.dout) + token * a.dout_token + heads0 * a.dout_head);
+            return;
+        }
+        const auto row_of = [&](const void* from, uint64_t token_stride, uint64_t head_stride, uint32_t r) SLLM_INLINE -> const T* {
+            const uint32_t row = min(r0 + r, row_end - 1), token = row / a.group;
+            const T* p = static_cast<const T*>(from) + (uint64_t)(piece.first + token) * token_stride + (heads0 + row - token * a.group) * head_stride;
+            return r0 + r < row_end ? p : nullptr;
+        };
+        stage_rows<T, D, kTile, kWaves, Vec>(q, a.dim, [&](uint32_t r) SLLM_INLINE { return row_of(a.q, a.q_token, a.q_head, r); });
+        stage_rows<T, D, kTile, kWaves, Vec>(dout, a.dim, [&](uint32_t r) SLLM_INLINE { return row_of(a.dout, a.dout_token, a.dout_head, r); });
     };
     // p is times 2^kUp, which makes float16's least of them normal numbers, and so is ds
     constexpr float kUp = kHalf ? 15.0f : 0.0f;
@@ -213,40 +274,102 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 128 ? 1 : 2) void atte
 #pragma unroll
     for (int d = 0; d < kParts; ++d) acc_k[d] = acc_v[d] = f32x16{};
     Range range;
-    const uint32_t rows_at = rows_from<T, D>(lane), columns_at = columns_from<T, D>(lane);
-    const auto tile = [&](uint32_t r0, const uint8_t* q, const uint8_t* dout, const uint8_t* lse, const uint8_t* delta, auto masked) SLLM_INLINE {
-        constexpr bool kMasked = decltype(masked)::value;
-        const auto sees = [&](int r) SLLM_INLINE {
-            const uint32_t row = r0 + (uint32_t)r, token = row / a.group;
-            return row < row_end && token >= key && (token - key < window || key < sinks);
+    bool out_of_sight = false;  // something was taken out
+    const auto tile = [&](uint32_t r0, const uint8_t* q, const uint8_t* dout, const uint8_t* lse, const uint8_t* delta, bool masked) SLLM_INLINE {
+        // places of fragments are made anew each time: kept, they would take what sums need
+        uint32_t here = threadIdx.x;
+        asm volatile("" : "+v"(here));
+        const uint32_t rows_at = rows_from<T, D>(here & 63), columns_at = columns_from<T, D>(here & 63), h = here >> 5 & 1;
+        const uint32_t values_at = rows_at + wave * kWaveRows * RowTile<T, D>::kPitch;
+        // four fragments at a time, two times four in registers
+        f32x16 s = {}, dp = {};
+        Operand8<T> first[4], second[4];
+        const auto read_q = [&](Operand8<T> (&f)[4], int i) SLLM_INLINE {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = read_rows<T, D>(q, rows_at, 0, i + j);
         };
-#pragma unroll 1
-        for (int n = 0; n < kTile / 32; ++n) {
-            f32x16 s = {}, dp = {};
+        const auto read_o = [&](Operand8<T> (&f)[4], int i) SLLM_INLINE {
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) s = multiply(read_rows<T, D>(q, rows_at, 32 * n, i), k[i], s);
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) dp = multiply(read_rows<T, D>(dout, rows_at, 32 * n, i), v[i], dp);
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const f32x4 l = lds_read<f32x4>(lse, h * 16 + (32 * n + 8 * g) * 4), de = lds_read<f32x4>(delta, h * 16 + (32 * n + 8 * g) * 4);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * g + i], scale, kUp - l[i]));
-                    float d = p * (dp[4 * g + i] - de[i]);
-                    if (kMasked && !sees(32 * n + 8 * g + 4 * h + i)) p = d = 0;
-                    s[4 * g + i] = p, dp[4 * g + i] = d;
-                }
+            for (int j = 0; j < 2; ++j) {
+                f[j] = read_rows<T, D>(dout, rows_at, 0, i + j);
+                f[2 + j] = read_rows<T, D>(values, values_at, 0, i + j);
             }
-            const Operand8<T> p[2] = {as_operand<T>(s, 0), as_operand<T>(s, 1)};
-            add_weighted<T, D, 32, kMasked>(acc_v, dout, columns_at, 32 * n, p, sees);
-            if constexpr (kHalf) {
-                range.fit(acc_k, dp);
-                dp *= range.up;
-            }
-            const Operand8<T> ds[2] = {as_operand<T>(dp, 0), as_operand<T>(dp, 1)};
-            add_weighted<T, D, 32, kMasked>(acc_k, q, columns_at, 32 * n, ds, sees);
+        };
+        __builtin_amdgcn_s_setprio(1);
+        read_q(first, 0);
+        phase();
+#pragma unroll
+        for (int i = 0; i < kSteps; i += 4) {
+            if (i + 4 < kSteps)
+                read_q(second, i + 4);
+            else
+                read_o(second, 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s = multiply(first[j], k[i + j], s);
+            phase();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) first[j] = second[j];
         }
+        ColumnFragments<T, D, 32> oc, qc;
+#pragma unroll
+        for (int i = 0; i < kSteps; i += 2) {
+            if (i + 2 < kSteps) {
+                read_o(second, i + 2);
+            } else {
+                oc.read(dout, columns_at, 0, 0);
+                qc.read(q, columns_at, 0, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) dp = multiply(first[j], first[2 + j], dp);
+            phase();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) first[j] = second[j];
+        }
+        __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 l = lds_read<f32x4>(lse, h * 16 + 8 * g * 4), de = lds_read<f32x4>(delta, h * 16 + 8 * g * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[4 * g + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * g + i], scale, kUp - l[i]));
+                dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - de[i]);
+            }
+        }
+        if (masked) {
+            uint32_t at = key0 + wave * kWaveRows + (here & 31);
+            asm volatile("" : "+v"(at));  // not to be found out before this is reached
+            uint32_t from, n_seen;
+            seen_rows(min(at, key1), from, n_seen);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const bool seen = r0 + 8 * (i / 4) + 4 * h + i % 4 - from < n_seen;
+                s[i] = seen ? s[i] : 0.0f, dp[i] = seen ? dp[i] : 0.0f;
+            }
+        }
+        if constexpr (kHalf) {
+            range.fit(acc_k, dp);
+            dp *= range.up;
+        }
+        const Operand8<T> p[2] = {as_operand<T>(s, 0), as_operand<T>(s, 1)}, ds[2] = {as_operand<T>(dp, 0), as_operand<T>(dp, 1)};
+        phase();
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int d = 0; d < kParts; ++d) {
+            ColumnFragments<T, D, 32> next_o, next_q;
+            if (d + 1 < kParts) {
+                next_o.read(dout, columns_at, 0, d + 1);
+                next_q.read(q, columns_at, 0, d + 1);
+            }
+            if (masked) {
+                out_of_sight |= oc.take_out();
+                out_of_sight |= qc.take_out();
+            }
+            oc.add(acc_v[d], p);
+            qc.add(acc_k[d], ds);
+            phase();
+            if (d + 1 < kParts) oc = next_o, qc = next_q;
+        }
+        __builtin_amdgcn_s_setprio(0);
     };
     const auto step = [&](uint32_t r0, const uint8_t* q, const uint8_t* o, const uint8_t* l, const uint8_t* d, uint8_t* next_q, uint8_t* next_o,
                           uint8_t* next_l, uint8_t* next_d) SLLM_INLINE {
@@ -254,37 +377,81 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 128 ? 1 : 2) void atte
         barrier();
         if (r0 + kTile < row_end) stage(r0 + kTile, next_q, next_o, next_l, next_d);
         const uint32_t qa = r0 / a.group, qb = min(r0 + kTile, row_end) - 1, ta = qa, tb = qb / a.group;
-        if (ta >= wave_key1 && r0 + kTile <= row_end && (tb - wave_key0 < window || wave_key1 < sinks))
-            tile(r0, q, o, l, d, std::false_type());
-        else if (!(tb < wave_key0 || (wave_key0 >= sinks && ta >= wave_key1 + window)))
-            tile(r0, q, o, l, d, std::true_type());
+        const bool all = ta >= wave_key1 && r0 + kTile <= row_end && (tb - wave_key0 < window || wave_key1 < sinks);
+        if (!(tb < wave_key0 || (wave_key0 >= sinks && ta >= wave_key1 + window))) tile(r0, q, o, l, d, !all);
     };
-    stage(row_first, q0, o0, l0, d0);
+    if (row_first < row_end)
+        stage(row_first, q0, o0, l0, d0);
+    else
+        wait_but_loads<0>();  // those of the values
     for (uint32_t r0 = row_first; r0 < row_end; r0 += 2 * kTile) {
         step(r0, q0, o0, l0, d0, q1, o1, l1, d1);
         if (r0 + kTile < row_end) step(r0 + kTile, q1, o1, l1, d1, q0, o0, l0, d0);
     }
+    if (__any(out_of_sight)) {
+        uint32_t seen_from, n_seen;
+        seen_rows(key, seen_from, n_seen);
+        for (uint32_t row = row_first; row < row_end; ++row) {
+            const uint32_t token = row / a.group, q_head = heads0 + row % a.group;
+            const bool seen = row - seen_from < n_seen;
+            put_back<T, D>(acc_v, static_cast<const T*>(a.dout) + (uint64_t)(piece.first + token) * a.dout_token + q_head * a.dout_head, a.dim, seen);
+            put_back<T, D>(acc_k, static_cast<const T*>(a.q) + (uint64_t)(piece.first + token) * a.q_token + q_head * a.q_head, a.dim, seen);
+        }
+    }
     if (key0 + wave * kWaveRows + c > key1) return;
     const uint64_t packed = piece.first + key;
-    store_column<T, D, Vec>(acc_v, kHalf ? 0x1p-15f : 1.0f, dv + packed * a.dv_token + head * a.dv_head, a.dim);
-    store_column<T, D, Vec>(acc_k, kHalf ? a.scale * 0x1p-15f / range.up : a.scale, dk + packed * a.dk_token + head * a.dk_head, a.dim);
+    const float f_v = kHalf ? 0x1p-15f : 1.0f, f_k = kHalf ? a.scale * 0x1p-15f / range.up : a.scale;
+    if (a.splits > 1) {
+        store_column<float, D, Vec>(acc_v, f_v, part_v + packed * part_token + head * a.dim, a.dim);
+        store_column<float, D, Vec>(acc_k, f_k, part_k + packed * part_token + head * a.dim, a.dim);
+        return;
+    }
+    store_column<T, D, Vec>(acc_v, f_v, dv + packed * a.dv_token + head * a.dv_head, a.dim);
+    store_column<T, D, Vec>(acc_k, f_k, dk + packed * a.dk_token + head * a.dk_head, a.dim);
+}
+
+// The splits' sums, first to last, so that every call adds in the same order.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kv(AttentionGradArgs a) {
+    const uint64_t n = (uint64_t)a.tokens * a.kv_heads * a.dim, i = (uint64_t)block_index() * 256 + threadIdx.x;
+    if (i >= n) return;
+    float k = 0, v = 0;
+    for (uint32_t s = 0; s < a.splits; ++s) k += a.parts[2 * s * n + i], v += a.parts[(2 * s + 1) * n + i];
+    const uint64_t token = i / (a.kv_heads * a.dim);
+    const uint32_t head = i / a.dim % a.kv_heads, e = i % a.dim;
+    static_cast<T*>(a.dk)[token * a.dk_token + head * a.dk_head + e] = from_f32<T>(k);
+    static_cast<T*>(a.dv)[token * a.dv_token + head * a.dv_head + e] = from_f32<T>(v);
+}
+
+uint32_t key_pieces(const AttentionArgs& a) { return (uint32_t)ceil_div(a.tokens, kRows) + (a.offsets ? a.sequences : 0); }
+
+// The rows that see a tile of keys are split where there are too few tiles to fill the GPU.
+uint32_t splits_of(const AttentionArgs& a) {
+    const uint64_t blocks = (uint64_t)key_pieces(a) * a.kv_heads;
+    return blocks ? (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(512 / blocks, 8)) : 1;
 }
 
 template <typename T, int D>
 void launch(AttentionGradArgs a, hipStream_t stream) {
-    const uint32_t more = a.offsets ? a.sequences : 0;
-    a.pieces = (uint32_t)ceil_div((uint64_t)a.tokens * a.group, kRows) + more;
+    a.pieces = (uint32_t)ceil_div((uint64_t)a.tokens * a.group, kRows) + (a.offsets ? a.sequences : 0);
     (a.vec ? attention_grad_q<T, D, true> : attention_grad_q<T, D, false>)<<<dim3(a.pieces * a.kv_heads), kWaves * 64, 0, stream>>>(a);
-    a.pieces = (uint32_t)ceil_div(a.tokens, kRows) + more;
-    (a.vec ? attention_grad_kv<T, D, true> : attention_grad_kv<T, D, false>)<<<dim3(a.pieces * a.kv_heads), kWaves * 64, 0, stream>>>(a);
+    a.pieces = key_pieces(a);
+    (a.vec ? attention_grad_kv<T, D, true> : attention_grad_kv<T, D, false>)<<<dim3(a.pieces * a.kv_heads * a.splits), kWaves * 64, 0, stream>>>(a);
+    if (a.splits > 1) join_kv<T><<<grid_of(ceil_div((uint64_t)a.tokens * a.kv_heads * a.dim, 256)), 256, 0, stream>>>(a);
 }
 
 }  // namespace
 
-uint64_t attention_grad_workspace(const AttentionArgs& a) { return (uint64_t)a.tokens * a.heads * 8; }
+uint64_t attention_grad_workspace(const AttentionArgs& a) {
+    const uint64_t rows = (uint64_t)a.tokens * a.heads * 8, splits = splits_of(a);
+    if (splits == 1) return rows;
+    return (rows + 15) / 16 * 16 + splits * a.tokens * a.kv_heads * a.dim * 8;
+}
 
 int32_t launch_attention_grad(AttentionGradArgs a, void* workspace, hipStream_t stream) {
     a.rows = static_cast<float*>(workspace);
+    a.splits = splits_of(a);
+    a.parts = a.rows + ((uint64_t)a.tokens * a.heads * 2 + 3) / 4 * 4;
     SLLM_BY_DTYPE(a.dtype, T, {
         if (a.dim <= 64)
             launch<T, 64>(a, stream);

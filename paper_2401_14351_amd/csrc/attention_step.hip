@@ -13,6 +13,7 @@ namespace {
 constexpr int kWaves = 4, kStepKeys = 32;
 constexpr uint32_t kHeads = 16;           // of a workgroup
 constexpr uint32_t kLeast = kWaves * 64;  // keys of a workgroup, where there are as many
+constexpr uint32_t kMaxSplits = 1024;
 
 // 32 of the depth by 16 columns and 16 rows: lane (r, g) has row r and depths 8 g to 8 g + 7.
 template <typename T>
@@ -266,35 +267,58 @@ __global__ __launch_bounds__(kWaves * 64) void attention_step(AttentionArgs a, u
     }
 }
 
-// The parts of a head's result, first to last, so that every call adds in the same order.
+// The parts of a head's result: eight runs of them side by side, each in order, then those
+// in order, so that every call adds in the same order.  A lane has one element, and the
+// weights of the parts are made once, by all threads.
+constexpr int kRuns = 8;
 template <typename T>
-__global__ __launch_bounds__(128) void join_parts(AttentionArgs a, uint32_t splits, const float* parts) {
-    const uint32_t sequence = blockIdx.x / a.heads, head = blockIdx.x % a.heads, e = threadIdx.x;
+__global__ __launch_bounds__(128 * kRuns) void join_parts(AttentionArgs a, uint32_t splits, const float* parts) {
+    __shared__ float weights[kMaxSplits], values[kRuns][128], totals[kRuns];
+    const uint32_t sequence = blockIdx.x / a.heads, head = blockIdx.x % a.heads, e = threadIdx.x % 128, run = threadIdx.x / 128;
     const int64_t past = read_id(a.lengths, a.wide_lengths, sequence);
-    if (e >= a.dim) return;
     T* const out = static_cast<T*>(a.out) + sequence * a.out_token + head * a.out_head;
-    float total = 0, value = 0;
-    if (past >= 0) {
-        const int32_t used = split_keys(a, past, splits).used;
-        const float* const from = parts + part_at(a, splits, blockIdx.x, 0);
-        const uint32_t pitch = a.dim + 2;
-        float top = -__builtin_inff();
-        for (int32_t s = 0; s < used; ++s) top = fmaxf(top, from[s * pitch]);
-        for (int32_t s = 0; s < used; ++s) {
-            const float at = from[s * pitch], f = at == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(at - top);
-            total += from[s * pitch + 1] * f;
-            value += from[s * pitch + 2 + e] * f;
-        }
-        value /= total;
+    if (past < 0) {
+        if (threadIdx.x < a.dim) out[threadIdx.x] = (T)0.0f;
+        return;
     }
-    out[e] = from_f32<T>(value);
+    const int32_t used = split_keys(a, past, splits).used;
+    const float* const from = parts + part_at(a, splits, blockIdx.x, 0);
+    const uint32_t pitch = a.dim + 2;
+    float top = -__builtin_inff();
+    for (int32_t s = threadIdx.x; s < used; s += 128 * kRuns) weights[s] = from[s * pitch];
+    __syncthreads();
+    for (int32_t s = threadIdx.x % 64; s < used; s += 64) top = fmaxf(top, weights[s]);
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+    __syncthreads();
+    for (int32_t s = threadIdx.x; s < used; s += 128 * kRuns) {
+        const float at = weights[s];
+        weights[s] = at == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(at - top);
+    }
+    __syncthreads();
+    float total = 0, value = 0;
+    const int32_t end = used * (run + 1) / kRuns;
+    if (e < a.dim) {
+#pragma unroll 4
+        for (int32_t s = used * run / kRuns; s < end; ++s) value += from[s * pitch + 2 + e] * weights[s];
+        if (e == 0)
+            for (int32_t s = used * run / kRuns; s < end; ++s) total += from[s * pitch + 1] * weights[s];
+    }
+    values[run][e] = value;
+    if (e == 0) totals[run] = total;
+    __syncthreads();
+    if (run || e >= a.dim) return;
+    value = total = 0;
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) value += values[i][e], total += totals[i];
+    out[e] = from_f32<T>(value / total);
 }
 
 // Workgroups that the keys of a head are split over: as many as fill the GPU, if every
 // sequence fills its cache.
 uint32_t splits_of(const AttentionArgs& a) {
     const uint64_t alone = (uint64_t)a.sequences * a.kv_heads * ceil_div(a.group, kHeads);
-    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(a.slots, kLeast), 1024 / alone));
+    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(a.slots, kLeast), kMaxSplits / alone));
 }
 
 }  // namespace
@@ -313,7 +337,7 @@ int32_t launch_attention_step(const AttentionArgs& a, void* workspace, hipStream
         const auto kernel = a.dim <= 64 ? (a.vec ? attention_step<T, 64, true> : attention_step<T, 64, false>)
                                         : (a.vec ? attention_step<T, 128, true> : attention_step<T, 128, false>);
         kernel<<<grid, kWaves * 64, 0, stream>>>(a, splits, parts);
-        if (splits > 1) join_parts<T><<<dim3(a.sequences * a.heads), 128, 0, stream>>>(a, splits, parts);
+        if (splits > 1) join_parts<T><<<dim3(a.sequences * a.heads), 128 * kRuns, 0, stream>>>(a, splits, parts);
     });
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;

@@ -74,10 +74,12 @@ int32_t linear(const sllm_matrix* x, const sllm_mx* x_mx, const sllm_mx* w, cons
     return launch_linear(l.a, workspace, static_cast<hipStream_t>(stream));
 }
 
-int32_t linear_bytes(const sllm_matrix* x, const sllm_mx* x_mx, const sllm_mx* w, bool grad, uint64_t* bytes, bool fp8 = false) {
+int32_t linear_bytes(const sllm_matrix* x, const sllm_mx* x_mx, const sllm_mx* w, bool grad, uint64_t* bytes, bool fp8 = false,
+                     uint32_t out_dtype = SLLM_DTYPE_BF16) {
     if (!bytes) return fail(SLLM_E_INVAL, "bytes: NULL");
     LinearArgs l;
     SLLM_TRY(linear_args(x, x_mx, w, grad, &l, fp8));
+    l.a.out_dtype = out_dtype;
     *bytes = linear_workspace(l.a);
     return SLLM_OK;
 }
@@ -205,9 +207,11 @@ extern "C" int32_t sllm_mx_linear_mx_workspace(const sllm_mx* x, const sllm_mx* 
 }
 SLLM_CATCH_ALL
 
-extern "C" int32_t sllm_mx_linear_octet_workspace(const sllm_mx* x, const sllm_mx* w, uint64_t* bytes) try {
+extern "C" int32_t sllm_mx_linear_octet_workspace(const sllm_mx* x, const sllm_mx* w, uint32_t out_dtype, uint64_t* bytes) try {
     clear_error();
-    return linear_bytes(nullptr, x, w, false, bytes, true);
+    if (out_dtype != SLLM_DTYPE_F32 && out_dtype != SLLM_DTYPE_F16 && out_dtype != SLLM_DTYPE_BF16)
+        return fail(SLLM_E_INVAL, "dtype %u is not f32, f16 or bf16", out_dtype);
+    return linear_bytes(nullptr, x, w, false, bytes, true, out_dtype);
 }
 SLLM_CATCH_ALL
 

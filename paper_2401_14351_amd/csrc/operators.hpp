@@ -135,6 +135,8 @@ struct AttentionGradArgs : AttentionArgs {  // out is read
     void *dq = nullptr, *dk = nullptr, *dv = nullptr;
     uint64_t dq_token = 0, dq_head = 0, dk_token = 0, dk_head = 0, dv_token = 0, dv_head = 0;
     float* rows = nullptr;  // tokens x heads, twice
+    uint32_t splits = 1;    // of the rows that see a key
+    float* parts = nullptr;
 };
 uint64_t attention_grad_workspace(const AttentionArgs& a);
 int32_t launch_attention_grad(AttentionGradArgs a, void* workspace, hipStream_t stream);

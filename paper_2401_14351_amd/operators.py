@@ -399,7 +399,10 @@ def _linear_mx(x, w, out, out_dtype):
     if isinstance(x, Mx8):
         L = binding.lib()
         y, rows = _output(out, (x.rows, w.rows), x.rows, w.rows, out_dtype or torch.bfloat16, x.codes)
-        _call(L.sllm_mx_linear_octet, L.sllm_mx_linear_octet_workspace, (x._struct, w._struct), rows, device)
+        operands = x._struct, w._struct
+        n = _workspace(L.sllm_mx_linear_octet_workspace, *operands, rows.dtype)
+        ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+        binding.check(L.sllm_mx_linear_octet(*operands, rows, ws.data_ptr() if n else None, n, device, _raw_stream(device)))
         _written(out)
         return y
     if out is None and device >= 0 and code is not None and _native() is not None:
