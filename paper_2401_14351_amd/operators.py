@@ -291,12 +291,14 @@ def _native():
     where it was not built for this Python and torch.  Its functions return the
     result, None for a call that is not ordinary, or a failed call's code."""
     ext = binding._views_ext()
-    if not hasattr(ext, "product"):
+    if not hasattr(ext, "attention_cached"):
         return None
     L = binding.lib()
     names = ("sllm_mx_quantize", "sllm_mx_dequantize", "sllm_mx_linear", "sllm_mx_linear_workspace", "sllm_mx_linear_mx",
              "sllm_mx_linear_mx_workspace", "sllm_mx_linear_grad", "sllm_mx_linear_grad_workspace", "sllm_embedding",
-             "sllm_embedding_mx", "sllm_embedding_grad", "sllm_embedding_grad_workspace")
+             "sllm_embedding_mx", "sllm_embedding_grad", "sllm_embedding_grad_workspace", "sllm_rms_norm", "sllm_rms_norm_octet",
+             "sllm_mx_linear_octet", "sllm_mx_linear_octet_workspace", "sllm_attention", "sllm_attention_cached",
+             "sllm_attention_cached_workspace")
     return SimpleNamespace(ext=ext, **{n[5:]: C.cast(getattr(L, n), C.c_void_p).value for n in names})
 
 
@@ -397,6 +399,14 @@ def _linear_mx(x, w, out, out_dtype):
     device = _one_device(x, w)
     code = _DTYPE.get(out_dtype or torch.bfloat16)
     if isinstance(x, Mx8):
+        if out is None and device >= 0 and code is not None and _native() is not None:
+            native = _native()
+            y = native.ext.product_octet(native.mx_linear_octet, native.mx_linear_octet_workspace, x._codes, x._scales, x._cols, w._codes,
+                                         w._scales, w._cols, code, device, _raw_stream(device))
+            if y.__class__ is int:
+                binding.check(y)
+            if y is not None:
+                return y
         L = binding.lib()
         y, rows = _output(out, (x.rows, w.rows), x.rows, w.rows, out_dtype or torch.bfloat16, x.codes)
         operands = x._struct, w._struct
@@ -606,6 +616,17 @@ def rms_norm(x: torch.Tensor, gain: torch.Tensor, residual: Optional[torch.Tenso
             raise ValueError("a tensor requires a gradient, which a norm in MX FP8 does not pass on")
         y, h = _RmsNorm.apply(x, gain, residual, eps)
         return y if residual is None else (y, h)
+    device, native = x.get_device(), _native()
+    if device >= 0 and native is not None:
+        parts = native.ext.norm(native.rms_norm_octet if mx8 else native.rms_norm, x, gain, residual, eps, 1 if mx8 else 0, device,
+                                _raw_stream(device))
+        if parts.__class__ is int:
+            binding.check(parts)
+        if parts is not None:
+            if not mx8:
+                return parts
+            y = Mx8._of(parts[0], parts[1], x.shape[-1])
+            return y if residual is None else (y, parts[2])
     y, h, _ = _rms_norm(x, gain, residual, eps, mx8, False)
     return y if residual is None else (y, h)
 
@@ -789,6 +810,13 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: Optiona
         if out is not None:
             raise ValueError("an operator that writes to a given tensor takes no part in autograd")
         return _Attention.apply(q, k, v, window, sinks, offsets, scale)
+    device, native = q.get_device(), _native()
+    if out is None and device >= 0 and native is not None:
+        y = native.ext.attention(native.attention, q, k, v, offsets, _window(window, sinks), min(sinks, 1 << 62), scale, device, _raw_stream(device))
+        if y.__class__ is int:
+            binding.check(y)
+        if y is not None:
+            return y
     return _attention(q, k, v, window, sinks, offsets, scale, out, None)
 
 
@@ -824,6 +852,15 @@ def attention_cached(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: K
         scale = q.shape[-1] ** -0.5 if q.dim() and q.shape[-1] else 1.0
     if lengths is None:
         raise ValueError("lengths: None")
+    device, native = q.get_device(), _native()
+    if out is None and device >= 0 and native is not None:
+        y = native.ext.attention_cached(native.attention_cached, native.attention_cached_workspace, q, k, v, cache.k, cache.v, cache.window,
+                                        cache.sinks, lengths, offsets, scale, device, _raw_stream(device))
+        if y.__class__ is int:
+            binding.check(y)
+        if y is not None:
+            _written(None, cache.k, cache.v)
+            return y
     args = (_heads(q, "q"), _heads(k, "k"), _heads(v, "v"), cache._struct, _index_tensor(lengths, "lengths"), _index_tensor(offsets, "offsets"))
     device = _one_device(q, k, v, cache.k, lengths, offsets)
     y, rows = _out_heads(out, q)

@@ -57,9 +57,9 @@ inline bool ids_of(const at::Tensor& t, sllm_ids* ids) {
     return true;
 }
 
-// A matrix in MX FP4 from its tensors; null codes where they are not what it is made of.
+// A matrix in MX FP4, or with blocks of 32 bytes FP8, from its tensors; null codes where they are not what it is made of.
 // Gives the codes' tensor, which tells where results are allocated.
-inline const at::Tensor* mx_of(PyObject* codes, PyObject* scales, PyObject* cols, int64_t device, sllm_mx* q) {
+inline const at::Tensor* mx_of(PyObject* codes, PyObject* scales, PyObject* cols, int64_t device, sllm_mx* q, int64_t block = 16) {
     const long long n = PyLong_AsLongLong(cols);
     if (n < 0) {
         PyErr_Clear();
@@ -70,7 +70,7 @@ inline const at::Tensor* mx_of(PyObject* codes, PyObject* scales, PyObject* cols
     const auto fits = [](const at::Tensor* t, int64_t pitch) {
         return t && t->scalar_type() == at::kByte && t->dim() == 2 && t->size(1) == pitch && t->is_contiguous();
     };
-    if (!fits(c, blocks * 16) || !fits(s, (blocks + 15) / 16 * 16) || c->size(0) != s->size(0)) return nullptr;
+    if (!fits(c, blocks * block) || !fits(s, (blocks + 15) / 16 * 16) || c->size(0) != s->size(0)) return nullptr;
     *q = sllm_mx{c->data_ptr(), s->data_ptr(), (uint64_t)c->size(0), (uint64_t)n};
     return c;
 }
@@ -282,7 +282,5 @@ inline PyObject* lookup_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs)
     return result(code, std::move(out));
     END_HANDLE_TH_ERRORS
 }
-
-#undef SLLM_PY_ARGS
 
 }  // namespace operators

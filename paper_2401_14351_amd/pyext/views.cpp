@@ -22,6 +22,7 @@
 #include <string>
 #include <vector>
 
+#include "layer.hpp"
 #include "operators.hpp"
 #include "sllm.h"
 
@@ -103,6 +104,10 @@ PyMethodDef kMethods[] = {method("build", build, "build(buf, table, n, names_rea
                           method("dequantize", operators::dequantize, "what an MX FP4 matrix stands for"),
                           method("lookup", operators::lookup, "rows of a table by token"),
                           method("lookup_grad", operators::lookup_grad, "the gradient of a lookup by its table"),
+                          method("norm", operators::norm, "a root-mean-square norm"),
+                          method("product_octet", operators::product_octet, "x @ w.T, x in MX FP8, w in MX FP4"),
+                          method("attention", operators::attention, "causal attention of packed sequences"),
+                          method("attention_cached", operators::attention_cached, "the same of new tokens behind a cache"),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_views", "Views over a loaded buffer, and calls of the operators on it.", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
