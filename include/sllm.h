@@ -567,7 +567,7 @@ int32_t sllm_mx_linear_grad(const sllm_matrix* dy, const sllm_mx* w, const sllm_
                             uint64_t workspace_bytes, int32_t device, void* stream);
 
 /* The same with x in MX FP8 (see sllm_mx_octet_quantize).  Where out is in 16 bits, products
- * of eight neighbouring elements of x are added to within 2^-14 of the largest of them
+ * of eight neighbouring elements of x are added to within 2^-13 of the largest of them
  * each, and those sums in 32 bits; where it is F32, elements of x below 2^-126 count to within 2^-134,
  * and nothing is rounded before the sums in 32 bits. */
 int32_t sllm_mx_linear_octet(const sllm_mx* x, const sllm_mx* w, const sllm_matrix* out, void* workspace,

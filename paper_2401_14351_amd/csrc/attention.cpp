@@ -172,6 +172,7 @@ extern "C" int32_t sllm_attention(const sllm_heads* q, const sllm_heads* k, cons
     a.lse = lse;
     SLLM_TRY(offsets_args(offsets, &a, &s[n++]));
     window_args(window, sinks, &a);
+    SLLM_TRY(check_overlaps(s, n, 2));
     DeviceGuard guard(device);
     if (!guard.ok()) return fail(SLLM_E_HIP, "cannot make device %d current", device);
     SLLM_TRY(check_spans(s, n, 2, device));
@@ -193,6 +194,7 @@ extern "C" int32_t sllm_attention_cached(const sllm_heads* q, const sllm_heads* 
     // written: the output, the workspace and the cache, the last two of the parts
     s[2] = parts[5], s[3] = parts[6];
     for (int i = 0; i < 5; ++i) s[4 + i] = parts[i];
+    SLLM_TRY(check_overlaps(s, 9, 4));
     DeviceGuard guard(device);
     if (!guard.ok()) return fail(SLLM_E_HIP, "cannot make device %d current", device);
     SLLM_TRY(check_spans(s, 9, 4, device));
@@ -244,6 +246,7 @@ extern "C" int32_t sllm_attention_grad(const sllm_heads* dout, const sllm_heads*
     a.dk = dk->data, a.dk_token = dk->token_stride, a.dk_head = dk->head_stride;
     a.dv = dv->data, a.dv_token = dv->token_stride, a.dv_head = dv->head_stride;
     a.vec = a.vec && aligned(*dout) && aligned(*dq) && aligned(*dk) && aligned(*dv);
+    SLLM_TRY(check_overlaps(s, n, 4));
     DeviceGuard guard(device);
     if (!guard.ok()) return fail(SLLM_E_HIP, "cannot make device %d current", device);
     SLLM_TRY(check_spans(s, n, 4, device));

@@ -157,7 +157,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         if (__any((top - m) * scale > kSlack)) {
             const f32x2 tops = both_halves(top);
             const float next = fmaxf(m, fmaxf(tops[0], tops[1]));
-            const float next_scaled = next == -__builtin_inff() ? -kUp : next * scale - kUp;
+            const float next_scaled = next == -__builtin_inff() ? -kUp : __builtin_fmaf(next, scale, -kUp);
             const float f = __builtin_amdgcn_exp2f(m == -__builtin_inff() ? 0.0f : m_scaled - next_scaled);
             m = next, m_scaled = next_scaled;
             sum *= f;
@@ -165,12 +165,14 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             for (int d = 0; d < kParts; ++d) acc[d] *= f;
         }
         Operand8<T> p[kKeys / 16];
+        const float m_finite = m == -__builtin_inff() ? 0.0f : m;
         float part = 0;
 #pragma unroll
         for (int n = 0; n < kKeys / 32; ++n) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                s[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], scale, -m_scaled));
+                // (the difference first is exact near the largest score, which 16 bits do not tell)
+                s[n][i] = __builtin_amdgcn_exp2f(sizeof(T) == 4 ? (s[n][i] - m_finite) * scale : __builtin_fmaf(s[n][i], scale, -m_scaled));
                 part += s[n][i];
             }
             p[2 * n] = as_operand<T>(s[n], 0);

@@ -178,7 +178,7 @@ __global__ __launch_bounds__(kWaves * 64) void attention_step(AttentionArgs a, u
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float next = fmaxf(m, top);
-            const float next_scaled = next == -__builtin_inff() ? -kUp : next * scale - kUp;
+            const float next_scaled = next == -__builtin_inff() ? -kUp : __builtin_fmaf(next, scale, -kUp);
             const float f = __builtin_amdgcn_exp2f(m == -__builtin_inff() ? 0.0f : m_scaled - next_scaled);
             m = next, m_scaled = next_scaled;
             sum *= f;
@@ -186,9 +186,10 @@ __global__ __launch_bounds__(kWaves * 64) void attention_step(AttentionArgs a, u
             for (int d = 0; d < kParts; ++d) acc[d] *= f;
         }
         Operand8<T> p;
+        const float m_finite = m == -__builtin_inff() ? 0.0f : m;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e / 4][e % 4], scale, -m_scaled));
+            const float w = __builtin_amdgcn_exp2f(sizeof(T) == 4 ? (s[e / 4][e % 4] - m_finite) * scale : __builtin_fmaf(s[e / 4][e % 4], scale, -m_scaled));
             sum += w;
             s[e / 4][e % 4] = w;
         }

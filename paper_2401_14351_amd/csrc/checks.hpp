@@ -70,13 +70,18 @@ inline int32_t ids_span(const sllm_ids* ids, Span* out) {
     return check_pointer(*out, ids->bits / 8);
 }
 
-// The spans are device memory, and the first n_out, which are written, overlap
-// no other.
-inline int32_t check_spans(const Span* s, int n, int n_out, int32_t device) {
+// The first n_out spans, which are written, overlap no other.
+inline int32_t check_overlaps(const Span* s, int n, int n_out) {
     for (int i = 0; i < n; ++i)
         for (int j = 0; j < n_out; ++j)
             if (i != j && s[i].bytes && s[j].bytes && s[i].p < s[j].p + s[j].bytes && s[j].p < s[i].p + s[i].bytes)
                 return fail(SLLM_E_INVAL, "%s and %s overlap", s[i].name, s[j].name);
+    return SLLM_OK;
+}
+
+// And all of them are device memory.
+inline int32_t check_spans(const Span* s, int n, int n_out, int32_t device) {
+    SLLM_TRY(check_overlaps(s, n, n_out));
     for (int i = 0; i < n; ++i) SLLM_TRY(check_device_range(s[i].p, s[i].bytes, device, s[i].name));
     return SLLM_OK;
 }

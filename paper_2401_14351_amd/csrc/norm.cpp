@@ -72,6 +72,7 @@ int32_t norm(const sllm_matrix* x, const sllm_matrix* residual, const sllm_matri
     a.rows = x->rows, a.cols = x->cols, a.dtype = x->dtype;
     a.eps = eps;
     a.inverse = inverse;
+    SLLM_TRY(check_overlaps(s, n, n_out));
     DeviceGuard guard(device);
     if (!guard.ok()) return fail(SLLM_E_HIP, "cannot make device %d current", device);
     SLLM_TRY(check_spans(s, n, n_out, device));
@@ -130,6 +131,7 @@ extern "C" int32_t sllm_rms_norm_grad(const sllm_matrix* dy, const sllm_matrix* 
     a.inverse = inverse;
     a.dx = dx->data, a.dx_stride = dx->stride;
     a.dgain = dgain->data;
+    SLLM_TRY(check_overlaps(s, n, 3));
     DeviceGuard guard(device);
     if (!guard.ok()) return fail(SLLM_E_HIP, "cannot make device %d current", device);
     SLLM_TRY(check_spans(s, n, 3, device));
@@ -163,6 +165,7 @@ extern "C" int32_t sllm_mx_octet_quantize(const sllm_matrix* src, const sllm_mx*
     SLLM_TRY(mx_spans("codes", "scales", dst, s, true));
     SLLM_TRY(matrix_span("source", src, &s[2]));
     if (src->rows != dst->rows || src->cols != dst->cols) return fail(SLLM_E_INVAL, "source and destination differ in shape");
+    SLLM_TRY(check_overlaps(s, 3, 2));
     DeviceGuard guard(device);
     if (!guard.ok()) return fail(SLLM_E_HIP, "cannot make device %d current", device);
     SLLM_TRY(check_spans(s, 3, 2, device));
@@ -177,6 +180,7 @@ extern "C" int32_t sllm_mx_octet_dequantize(const sllm_mx* src, const sllm_matri
     SLLM_TRY(matrix_span("destination", dst, &s[0]));
     SLLM_TRY(mx_spans("codes", "scales", src, &s[1], true));
     if (src->rows != dst->rows || src->cols != dst->cols) return fail(SLLM_E_INVAL, "source and destination differ in shape");
+    SLLM_TRY(check_overlaps(s, 3, 1));
     DeviceGuard guard(device);
     if (!guard.ok()) return fail(SLLM_E_HIP, "cannot make device %d current", device);
     SLLM_TRY(check_spans(s, 3, 1, device));

@@ -670,6 +670,9 @@ class _RmsNorm(torch.autograd.Function):
         h, gain, inverse = ctx.saved_tensors
         if dy is None:  # h alone has been used
             return dh, None, dh if ctx.residual else None, None
+        if not h.numel():
+            dx = torch.zeros_like(h)
+            return dx, torch.zeros_like(gain), dx if ctx.residual else None, None
         # gradients of sums and means arrive with strides of 0
         dy, dh = dy.contiguous(), None if dh is None else dh.contiguous()
         rows, device = _matrix(h, "h"), h.get_device()
@@ -700,6 +703,8 @@ def _heads(t: torch.Tensor, name: str) -> binding.Heads:
     if t.dim() != 3:
         raise ValueError(f"{name}: expected tokens, heads and elements, got shape {tuple(t.shape)}")
     tokens, heads, dim = t.shape
+    if not t.numel():
+        return binding.Heads(t.data_ptr(), tokens, heads, dim, heads * dim, dim, code, 0)
     strides = t.stride()
     if dim > 1 and strides[2] != 1:
         raise ValueError(f"{name}: the elements of a head are not adjacent (strides {strides})")
