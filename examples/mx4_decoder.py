@@ -4,13 +4,14 @@ A small decoder with the tensor names of the Llama checkpoints, random weights:
 it is converted and loaded into HBM, its matrices are quantised there, and the
 16-bit image is freed.  Then
 
-* a prompt is answered, one token at a time after the prompt itself
-  (``embedding``, ``mx4_linear``; with ``--mx4-prompt`` the prompt's
-  activations are in four bits too);
+* a prompt is answered, one token at a time after the prompt itself, over a cache
+  that holds the last ``--window`` tokens and the first ``--sinks`` (``embedding``,
+  ``rms_norm``, ``mx4_linear``, ``attention_cached``; with ``--mx4-prompt`` or
+  ``--mx8-prompt`` the prompt's activations are in four or eight bits too);
 * the embedding table is tuned to a text while the matrices stay as they are
-  (the backward passes are ``mx4_linear_grad`` and ``embedding_grad``).
+  (``attention``; the backward passes are the operators').
 
-    python examples/mx4_decoder.py [--layers 4] [--dim 1024] [--answer 32] [--steps 20] [--mx4-prompt]
+    python examples/mx4_decoder.py [--layers 4] [--dim 1024] [--answer 32] [--steps 20] [--mx4-prompt | --mx8-prompt]
 """
 
 from __future__ import annotations
@@ -65,24 +66,29 @@ def stacked(*parts: torch.Tensor) -> operators.Mx4:
     return w
 
 
-def norm(x, gain, eps=1e-5):
-    h = x.float()
-    return (h * torch.rsqrt(h.square().mean(-1, keepdim=True) + eps) * gain).to(x.dtype)
-
-
 def rotate(x, first: int):
-    """Rotary positions from ``first`` on: x is (heads, tokens, HEAD) in 32 bits."""
-    angle = torch.arange(first, first + x.shape[1], device=x.device, dtype=torch.float32)[:, None] \
+    """Rotary positions from ``first`` on: x is (tokens, heads, HEAD)."""
+    angle = torch.arange(first, first + x.shape[0], device=x.device, dtype=torch.float32)[:, None, None] \
         * torch.pow(10000.0, -torch.arange(0, HEAD, 2, device=x.device, dtype=torch.float32) / HEAD)
-    a, b = x[..., :HEAD // 2], x[..., HEAD // 2:]
-    return torch.cat([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], -1)
+    a, b = x[..., :HEAD // 2].float(), x[..., HEAD // 2:].float()
+    return torch.cat([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], -1).to(x.dtype)
+
+
+class Cache:
+    """The keys and values of one sequence, layer by layer, and how many tokens it has had."""
+
+    def __init__(self, model: "Decoder"):
+        window = model.window or 4096
+        self.layers = [operators.KvCache.empty(1, model.kv_heads, HEAD, window, model.sinks, dtype=model.dtype, device=model.table.device)
+                       for _ in model.layers]
+        self.past, self.room = 0, None if model.window else window
 
 
 class Decoder:
     """The matrices in MX FP4, activations and the embedding table in ``dtype``."""
 
-    def __init__(self, views, dtype=torch.bfloat16):
-        self.dtype = dtype
+    def __init__(self, views, dtype=torch.bfloat16, window=None, sinks: int = 0):
+        self.dtype, self.window, self.sinks = dtype, window, sinks
         self.table = views["model.embed_tokens.weight"].to(dtype, copy=True)
         self.dim = self.table.shape[1]
         self.layers = []
@@ -99,44 +105,57 @@ class Decoder:
         self.norm = views["model.norm.weight"].float()
         self.head = stacked(views["lm_head.weight"])
 
-    def product(self, x, w, mx4: bool):
-        if mx4:
-            return operators.mx4_linear(operators.mx4_quantize(x), w, out_dtype=self.dtype)
-        return operators.mx4_linear(x, w)
+    def product(self, x, w, bits=None):
+        if bits and not isinstance(x, operators.Mx8):
+            x = (operators.mx4_quantize if bits == 4 else operators.mx8_quantize)(x)
+        return operators.mx4_linear(x, w, out_dtype=self.dtype)
 
     def attention(self, qkv, cache, layer: int):
-        """Causal attention of the new tokens over the cache's and themselves, in 32 bits."""
-        t, kv = qkv.shape[0], self.kv_heads * HEAD
-        q, k, v = (y.float().view(t, -1, HEAD).transpose(0, 1) for y in qkv.split([self.dim, kv, kv], -1))
-        past = cache[layer][0].shape[1] if cache is not None and layer in cache else 0
+        """Causal attention of the new tokens over the cache's and themselves."""
+        kv = self.kv_heads * HEAD
+        q, k, v = (y.unflatten(-1, (-1, HEAD)) for y in qkv.split([self.dim, kv, kv], -1))
+        past = cache.past if cache else 0
         q, k = rotate(q, past), rotate(k, past)
-        if past:
-            k, v = torch.cat([cache[layer][0], k], 1), torch.cat([cache[layer][1], v], 1)
-        if cache is not None:
-            cache[layer] = (k, v)
-        group = q.shape[0] // self.kv_heads
-        k, v = k.repeat_interleave(group, 0), v.repeat_interleave(group, 0)
-        score = torch.matmul(q, k.transpose(1, 2).contiguous()) * HEAD ** -0.5
-        ahead = torch.ones(t, past + t, dtype=torch.bool, device=q.device).triu(past + 1)
-        p = torch.softmax(score.masked_fill(ahead, float("-inf")), -1)
-        return torch.matmul(p, v.contiguous()).transpose(0, 1).reshape(t, self.dim).to(self.dtype)
+        if cache is None:
+            out = operators.attention(q, k, v, window=self.window, sinks=self.sinks)
+        else:
+            n = len(qkv)
+            offsets = None if n == 1 else torch.tensor([0, n], dtype=torch.int32, device=qkv.device)
+            lengths = torch.tensor([past], dtype=torch.int64, device=qkv.device)
+            out = operators.attention_cached(q, k, v, cache.layers[layer], lengths, offsets=offsets)
+        return out.flatten(1)
 
-    def logits(self, tokens, cache=None, mx4: bool = False, table=None):
-        """(tokens, vocab); ``cache`` is a dict that keeps the keys and values of a sequence."""
+    def logits(self, tokens, cache=None, mx4: bool = False, table=None, bits=None):
+        """(tokens, vocab); ``cache`` is a :class:`Cache`; ``bits`` (4 or 8, or ``mx4``) is what
+        activations have in products."""
+        bits = 4 if mx4 else bits
+        if cache and cache.room is not None and cache.past + len(tokens) > cache.room:
+            raise ValueError(f"without a window a sequence has at most {cache.room} tokens")
         x = operators.embedding(self.table if table is None else table, tokens)
-        for i, l in enumerate(self.layers):
-            a = self.attention(self.product(norm(x, l["norm1"]), l["qkv"], mx4), cache, i)
-            x = x + self.product(a, l["out"], mx4)
-            gate, up = self.product(norm(x, l["norm2"]), l["gate_up"], mx4).chunk(2, -1)
-            x = x + self.product(torch.nn.functional.silu(gate) * up, l["down"], mx4)
-        return self.product(norm(x, self.norm), self.head, mx4)
+        new = None  # what the layer before has added
 
-    def answer(self, prompt, n: int, mx4_prompt: bool = False):
+        def norm(gain):
+            nonlocal x
+            if new is None:
+                return operators.rms_norm(x, gain, mx8=bits == 8)
+            y, x = operators.rms_norm(new, gain, residual=x, mx8=bits == 8)
+            return y
+
+        for i, l in enumerate(self.layers):
+            a = self.attention(self.product(norm(l["norm1"]), l["qkv"], bits), cache, i)
+            new = self.product(a, l["out"], bits)
+            gate, up = self.product(norm(l["norm2"]), l["gate_up"], bits).chunk(2, -1)
+            new = self.product(torch.nn.functional.silu(gate) * up, l["down"], bits)
+        if cache:
+            cache.past += len(tokens)
+        return self.product(norm(self.norm), self.head, bits)
+
+    def answer(self, prompt, n: int, mx4_prompt: bool = False, bits=None):
         """The n most likely tokens after the prompt, one after the other."""
-        cache, out = {}, []
+        cache, out = Cache(self), []
         with torch.no_grad():
             for _ in range(n):
-                logits = self.logits(out[-1], cache) if out else self.logits(prompt, cache, mx4_prompt)
+                logits = self.logits(out[-1], cache) if out else self.logits(prompt, cache, mx4_prompt, bits=bits)
                 out.append(logits[-1].argmax().view(1))
         return torch.cat(out) if out else prompt[:0]
 
@@ -163,23 +182,27 @@ def main():
     ap.add_argument("--prompt", type=int, default=512)
     ap.add_argument("--answer", type=int, default=32)
     ap.add_argument("--steps", type=int, default=20)
-    ap.add_argument("--mx4-prompt", action="store_true")
+    ap.add_argument("--window", type=int, help="tokens that attention looks back, all of them if not given")
+    ap.add_argument("--sinks", type=int, default=0, help="first tokens that stay visible")
+    bits = ap.add_mutually_exclusive_group()
+    bits.add_argument("--mx4-prompt", dest="bits", action="store_const", const=4)
+    bits.add_argument("--mx8-prompt", dest="bits", action="store_const", const=8)
     a = ap.parse_args()
 
     spec = checkpoint(a.layers, a.dim, a.ffn, a.vocab, max(1, a.dim // HEAD // 4))
     with tempfile.TemporaryDirectory() as d:
         views = load(spec, os.path.join(d, "ckpt"))
     image = sum(v.numel() * v.element_size() for v in views.values())
-    model = Decoder(views)
+    model = Decoder(views, window=a.window, sinks=a.sinks)
     held = sum(w.nbytes for l in model.layers for w in l.values() if isinstance(w, operators.Mx4)) + model.head.nbytes
     del views
     print(f"loaded {image / 1e6:.1f} MB; the matrices take {held / 1e6:.1f} MB in four bits")
 
     prompt = torch.randint(a.vocab, (a.prompt,), device="cuda:0", generator=torch.Generator("cuda:0").manual_seed(1))
-    model.answer(prompt, 2, a.mx4_prompt)  # first calls load code
+    model.answer(prompt, 2, bits=a.bits)  # first calls load code
     torch.cuda.synchronize()
     t0 = time.perf_counter()
-    answer = model.answer(prompt, a.answer, a.mx4_prompt).tolist()
+    answer = model.answer(prompt, a.answer, bits=a.bits).tolist()
     print(f"{a.prompt} + {a.answer} tokens in {1e3 * (time.perf_counter() - t0):.1f} ms: {answer}")
 
     losses = model.tune(prompt, a.steps, rate=100.0)

@@ -1,21 +1,29 @@
 """Operators on loaded weights (the last section of ``include/sllm.h``).
 
-Matrices in microscaled 4-bit floating point (MX FP4), products with them and
-token embeddings, on torch tensors in device memory:
+Matrices in microscaled 4-bit floating point (MX FP4), products with them, token
+embeddings, and the norms and attention between them, on torch tensors in device
+memory:
 
 * :func:`mx4_quantize`, :func:`mx4_dequantize`: a loaded matrix into an
   :class:`Mx4` (4.25 bits a value) and back.
 * :func:`mx4_linear`: ``x @ W.T`` for one token or a whole prompt, x a tensor
   or an :class:`Mx4`; :func:`mx4_linear_grad`: ``dy @ W``.
+* :func:`mx8_quantize`, :func:`mx8_dequantize`: activations into an :class:`Mx8`
+  (8.25 bits a value), which :func:`mx4_linear` takes for x, and back.
+* :func:`rms_norm`: root-mean-square norms with a residual's addition, in x's type
+  or in MX FP8.
+* :func:`attention`: causal attention of packed sequences, with a sliding window and
+  sinks; :func:`attention_cached`: the same of new tokens over a :class:`KvCache`.
 * :func:`embedding`: scaled table rows by token, from a tensor or an
   :class:`Mx4`; :func:`embedding_grad`: the table's gradient.
 
 Operators run on ``stream`` (by default the device's current stream) and return
 without waiting.  Their outputs and workspaces belong to that stream; inputs
 made on another one must be ready for it (``stream.wait_stream(...)``), and are
-kept from reuse until it has passed the call.  ``mx4_linear`` and ``embedding``
-take part in autograd where their input or table requires a gradient.  There is
-no forward mode: a tensor with a tangent is refused.
+kept from reuse until it has passed the call.  ``mx4_linear``, ``embedding``,
+``rms_norm`` and ``attention`` take part in autograd where one of their inputs
+requires a gradient.  There is no forward mode: a tensor with a tangent is
+refused.
 
 Rows may be apart by any stride that keeps them from overlapping, but the
 elements of a row must be adjacent: other tensors, broadcast ones among them, are
@@ -600,6 +608,14 @@ class _Embedding(torch.autograd.Function):
 # norms
 # ---------------------------------------------------------------------------
 
+def _refuse_capture():
+    # A captured backward pass that reaches a leaf which an eager graph holds too waits for
+    # that leaf's stream, outside the capture, and ends the process.
+    if torch.cuda.is_current_stream_capturing():
+        raise ValueError("norms and attention pass no gradient under graph capture: capture them under torch.no_grad(), "
+                         "or the entry points of their gradients")
+
+
 def rms_norm(x: torch.Tensor, gain: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-5, mx8: bool = False,
              stream=None):
     """h / sqrt(mean h^2 + eps) * gain over the last dimension, in x's type, h being x, or
@@ -614,6 +630,7 @@ def rms_norm(x: torch.Tensor, gain: torch.Tensor, residual: Optional[torch.Tenso
     if torch.is_grad_enabled() and (x.requires_grad or gain.requires_grad or (residual is not None and residual.requires_grad)):
         if mx8:
             raise ValueError("a tensor requires a gradient, which a norm in MX FP8 does not pass on")
+        _refuse_capture()
         y, h = _RmsNorm.apply(x, gain, residual, eps)
         return y if residual is None else (y, h)
     device, native = x.get_device(), _native()
@@ -814,6 +831,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: Optiona
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
         if out is not None:
             raise ValueError("an operator that writes to a given tensor takes no part in autograd")
+        _refuse_capture()
         return _Attention.apply(q, k, v, window, sinks, offsets, scale)
     device, native = q.get_device(), _native()
     if out is None and device >= 0 and native is not None:

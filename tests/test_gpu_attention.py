@@ -571,3 +571,23 @@ def test_autograd():
         op.attention_cached(q, k, v, cache, ids([0] * 40))
     with pytest.raises(RuntimeError):  # the cache has been written to since
         used.backward()
+
+
+def test_no_gradient_under_capture():
+    """A captured backward pass is refused where it would begin; the capture goes on."""
+    q = normal((20, 2, 64), torch.float32, 1).requires_grad_()
+    gain = torch.ones(64, device="cuda", requires_grad=True)
+    with torch.no_grad():
+        want = op.attention(q, q, q), op.rms_norm(q, gain)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(ValueError):
+            op.attention(q, q, q)
+        with pytest.raises(ValueError):
+            op.rms_norm(q, gain)
+        with torch.no_grad():
+            got = op.attention(q, q, q), op.rms_norm(q, gain)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
