@@ -180,6 +180,20 @@ __device__ __forceinline__ Operand8<T> as_operand(const f32x16& x, int t) {
     return o;
 }
 
+// What rounding to an operand has left of them.
+template <typename T>
+__device__ __forceinline__ f32x16 rounded_off(const f32x16& x, const Operand8<T> (&o)[2]) {
+    f32x16 rest;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        T v[8];
+        __builtin_memcpy(v, &o[t].v, sizeof v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) rest[8 * t + j] = x[8 * t + j] - to_f32(v[j]);
+    }
+    return rest;
+}
+
 // Eight elements of a row in memory from element e, zeros past its end.
 template <typename T, bool Vec>
 __device__ __forceinline__ Operand8<T> load8(const T* row, uint32_t e, uint32_t dim) {

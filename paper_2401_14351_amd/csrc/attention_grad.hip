@@ -45,7 +45,7 @@ struct Range {
 template <typename T, int D, bool Vec>
 __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void attention_grad_q(AttentionGradArgs a) {
     constexpr int kKeys = tile_rows<T>(), kSteps = D / 16, kParts = D / 32;
-    constexpr bool kHalf = __is_same(T, _Float16);
+    constexpr bool kHalf = __is_same(T, _Float16), kTwice = sizeof(T) == 2;
     constexpr uint32_t kBytes = kKeys * RowTile<T, D>::kPitch;
     __shared__ __align__(16) uint8_t k0[kBytes], v0[kBytes], k1[kBytes], v1[kBytes];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -119,9 +119,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     const uint32_t rows_at = rows_from<T, D>(lane), columns_at = columns_from<T, D>(lane);
     bool out_of_sight = false;  // something was taken out
     const auto tile = [&](int32_t i0, const uint8_t* k, const uint8_t* v, bool masked) SLLM_INLINE {
-        Operand8<T> ds[kKeys / 16];
         RowFragments<T, D> kf, vf;
-        ColumnFragments<T, D, kKeys> cf;
+        ColumnFragments<T, D, 32> cf;
         kf.read(k, rows_at, 0);
 #pragma unroll
         for (int n = 0; n < kKeys / 32; ++n) {
@@ -129,10 +128,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             vf.read(v, rows_at, 32 * n);
             f32x16 s = kf.times(q);
             phase();
-            if (n + 1 < kKeys / 32)
-                kf.read(k, rows_at, 32 * (n + 1));
-            else
-                cf.read(k, columns_at, 0, 0);
+            cf.read(k, columns_at, 32 * n, 0);
             const f32x16 dp = vf.times(dout);
             phase();
 #pragma unroll
@@ -143,22 +139,28 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
                 for (int i = 0; i < 16; ++i) s[i] = here.sees(i0 + 32 * n + 8 * (i / 4) + 4 * (int32_t)h + i % 4) ? s[i] : 0.0f;
             }
             if constexpr (kHalf) {
-                const float before = range.up;
                 range.fit(acc, s);
-                if (n && __any(before != range.up)) {
-                    // what this tile has rounded already was times the former power
-                    const _Float16 f = (_Float16)(range.up / before);
-#pragma unroll
-                    for (int t = 0; t < 2 * n; ++t)
-                        ds[t].v = __builtin_bit_cast(u32x4, __builtin_bit_cast(f16x8, ds[t].v) * f);
-                }
                 s *= range.up;
             }
-            ds[2 * n] = as_operand<T>(s, 0);
-            ds[2 * n + 1] = as_operand<T>(s, 1);
+            const Operand8<T> ds[2] = {as_operand<T>(s, 0), as_operand<T>(s, 1)};
+            Operand8<T> rest[2];
+            if constexpr (kTwice) {
+                const f32x16 r = rounded_off<T>(s, ds);
+                rest[0] = as_operand<T>(r, 0), rest[1] = as_operand<T>(r, 1);
+            }
+            phase();
+            if (n + 1 < kKeys / 32) kf.read(k, rows_at, 32 * (n + 1));
+#pragma unroll
+            for (int d = 0; d < kParts; ++d) {
+                ColumnFragments<T, D, 32> next;
+                if (d + 1 < kParts) next.read(k, columns_at, 32 * n, d + 1);
+                if (masked) out_of_sight |= cf.take_out();
+                cf.add(acc[d], ds);
+                if constexpr (kTwice) cf.add(acc[d], rest);
+                phase();
+                if (d + 1 < kParts) cf = next;
+            }
         }
-        phase();
-        out_of_sight |= add_weighted<T, D, kKeys>(acc, cf, k, columns_at, 0, ds, masked);
     };
     const auto step = [&](int32_t i0, const uint8_t* k, const uint8_t* v, uint8_t* next_k, uint8_t* next_v) SLLM_INLINE {
         wait_but_loads<0>();
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
 template <typename T, int D, bool Vec>
 __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void attention_grad_kv(AttentionGradArgs a) {
     constexpr int kTile = 32, kSteps = D / 16, kParts = D / 32;
-    constexpr bool kHalf = __is_same(T, _Float16);
+    constexpr bool kHalf = __is_same(T, _Float16), kTwice = sizeof(T) == 2;
     constexpr uint32_t kBytes = kTile * RowTile<T, D>::kPitch;
     __shared__ __align__(16) uint8_t q0[kBytes], o0[kBytes], q1[kBytes], o1[kBytes];
     __shared__ __align__(16) uint8_t l0[256], d0[256], l1[256], d1[256];  // rows' lse and delta
@@ -310,15 +312,13 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
 #pragma unroll
             for (int j = 0; j < 4; ++j) first[j] = second[j];
         }
-        ColumnFragments<T, D, 32> oc, qc;
+        ColumnFragments<T, D, 32> cf;
 #pragma unroll
         for (int i = 0; i < kSteps; i += 2) {
-            if (i + 2 < kSteps) {
+            if (i + 2 < kSteps)
                 read_o(second, i + 2);
-            } else {
-                oc.read(dout, columns_at, 0, 0);
-                qc.read(q, columns_at, 0, 0);
-            }
+            else
+                cf.read(dout, columns_at, 0, 0);
 #pragma unroll
             for (int j = 0; j < 2; ++j) dp = multiply(first[j], first[2 + j], dp);
             phase();
@@ -350,24 +350,36 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             range.fit(acc_k, dp);
             dp *= range.up;
         }
-        const Operand8<T> p[2] = {as_operand<T>(s, 0), as_operand<T>(s, 1)}, ds[2] = {as_operand<T>(dp, 0), as_operand<T>(dp, 1)};
+        const Operand8<T> p[2] = {as_operand<T>(s, 0), as_operand<T>(s, 1)};
         phase();
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int d = 0; d < kParts; ++d) {
-            ColumnFragments<T, D, 32> next_o, next_q;
-            if (d + 1 < kParts) {
-                next_o.read(dout, columns_at, 0, d + 1);
-                next_q.read(q, columns_at, 0, d + 1);
-            }
-            if (masked) {
-                out_of_sight |= oc.take_out();
-                out_of_sight |= qc.take_out();
-            }
-            oc.add(acc_v[d], p);
-            qc.add(acc_k[d], ds);
+            ColumnFragments<T, D, 32> next;
+            if (d + 1 < kParts)
+                next.read(dout, columns_at, 0, d + 1);
+            else
+                next.read(q, columns_at, 0, 0);
+            if (masked) out_of_sight |= cf.take_out();
+            cf.add(acc_v[d], p);
             phase();
-            if (d + 1 < kParts) oc = next_o, qc = next_q;
+            cf = next;
+        }
+        const Operand8<T> ds[2] = {as_operand<T>(dp, 0), as_operand<T>(dp, 1)};
+        Operand8<T> rest[2];
+        if constexpr (kTwice) {
+            const f32x16 r = rounded_off<T>(dp, ds);
+            rest[0] = as_operand<T>(r, 0), rest[1] = as_operand<T>(r, 1);
+        }
+#pragma unroll
+        for (int d = 0; d < kParts; ++d) {
+            ColumnFragments<T, D, 32> next;
+            if (d + 1 < kParts) next.read(q, columns_at, 0, d + 1);
+            if (masked) out_of_sight |= cf.take_out();
+            cf.add(acc_k[d], ds);
+            if constexpr (kTwice) cf.add(acc_k[d], rest);
+            phase();
+            if (d + 1 < kParts) cf = next;
         }
         __builtin_amdgcn_s_setprio(0);
     };

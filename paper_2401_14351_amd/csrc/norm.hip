@@ -323,20 +323,24 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
     }
 }
 
-// The slots' sums, in their order: 16 runs of slots side by side, then those.
+// The slots' sums, in their order: 32 runs of slots side by side, then those.
 template <typename G>
 __global__ __launch_bounds__(1024) void join_gain(const float* parts, uint32_t slots, uint64_t cols, G* out) {
-    __shared__ float sums[16][64];
-    const uint32_t l = threadIdx.x % 64, run = threadIdx.x / 64;
-    const uint64_t c = (uint64_t)block_index() * 64 + l;
+    constexpr uint32_t kRuns = 32, kCols = 32;
+    __shared__ float sums[kRuns][kCols];
+    const uint32_t l = threadIdx.x % kCols, run = threadIdx.x / kCols;
+    const uint64_t c = (uint64_t)block_index() * kCols + l;
     float sum = 0;
-    if (c < cols)
-        for (uint32_t s = (uint64_t)slots * run / 16; s < (uint64_t)slots * (run + 1) / 16; ++s) sum += parts[s * cols + c];
+    if (c < cols) {
+        const uint32_t end = (uint64_t)slots * (run + 1) / kRuns;
+#pragma unroll 8
+        for (uint32_t s = (uint64_t)slots * run / kRuns; s < end; ++s) sum += parts[s * cols + c];
+    }
     sums[run][l] = sum;
     __syncthreads();
     if (run || c >= cols) return;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) sum += sums[i][l];
+    for (uint32_t i = 1; i < kRuns; ++i) sum += sums[i][l];
     out[c] = from_f32<G>(sum);
 }
 
@@ -454,7 +458,7 @@ int32_t launch_rms_norm_grad(const NormGradLaunch& n, void* workspace, hipStream
         SLLM_HIP(hipGetLastError());
     }
     SLLM_BY_DTYPE(n.gain_dtype, G,
-                  (join_gain<G><<<grid_of(ceil_div(n.cols, 64)), 1024, 0, stream>>>(a.parts, a.slots, n.cols, static_cast<G*>(n.dgain))));
+                  (join_gain<G><<<grid_of(ceil_div(n.cols, 32)), 1024, 0, stream>>>(a.parts, a.slots, n.cols, static_cast<G*>(n.dgain))));
     SLLM_HIP(hipGetLastError());
     return SLLM_OK;
 }

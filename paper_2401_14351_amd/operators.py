@@ -299,13 +299,14 @@ def _native():
     where it was not built for this Python and torch.  Its functions return the
     result, None for a call that is not ordinary, or a failed call's code."""
     ext = binding._views_ext()
-    if not hasattr(ext, "attention_cached"):
+    if not hasattr(ext, "attention_grad"):
         return None
     L = binding.lib()
     names = ("sllm_mx_quantize", "sllm_mx_dequantize", "sllm_mx_linear", "sllm_mx_linear_workspace", "sllm_mx_linear_mx",
              "sllm_mx_linear_mx_workspace", "sllm_mx_linear_grad", "sllm_mx_linear_grad_workspace", "sllm_embedding",
              "sllm_embedding_mx", "sllm_embedding_grad", "sllm_embedding_grad_workspace", "sllm_rms_norm", "sllm_rms_norm_octet",
-             "sllm_mx_linear_octet", "sllm_mx_linear_octet_workspace", "sllm_attention", "sllm_attention_cached",
+             "sllm_rms_norm_grad", "sllm_rms_norm_grad_workspace", "sllm_mx_linear_octet", "sllm_mx_linear_octet_workspace",
+             "sllm_attention", "sllm_attention_grad", "sllm_attention_grad_workspace", "sllm_attention_cached",
              "sllm_attention_cached_workspace")
     return SimpleNamespace(ext=ext, **{n[5:]: C.cast(getattr(L, n), C.c_void_p).value for n in names})
 
@@ -674,7 +675,15 @@ class _RmsNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gain, residual, eps):
         ctx.set_materialize_grads(False)
-        y, h, inverse = _rms_norm(x, gain, residual, eps, False, True)
+        parts, device, native = None, x.get_device(), _native()
+        if device >= 0 and native is not None:
+            parts = native.ext.norm_kept(native.rms_norm, x, gain, residual, eps, device, _raw_stream(device))
+            if parts.__class__ is int:
+                binding.check(parts)
+        if parts is None:
+            y, h, inverse = _rms_norm(x, gain, residual, eps, False, True)
+        else:
+            y, inverse, h = parts if residual is not None else (*parts, x)
         ctx.save_for_backward(h, gain, inverse)
         ctx.residual = residual is not None
         if residual is None:
@@ -691,8 +700,15 @@ class _RmsNorm(torch.autograd.Function):
             dx = torch.zeros_like(h)
             return dx, torch.zeros_like(gain), dx if ctx.residual else None, None
         # gradients of sums and means arrive with strides of 0
-        dy, dh = dy.contiguous(), None if dh is None else dh.contiguous()
-        rows, device = _matrix(h, "h"), h.get_device()
+        dy, dh, device, native = dy.contiguous(), None if dh is None else dh.contiguous(), h.get_device(), _native()
+        if native is not None:
+            parts = native.ext.norm_grad(native.rms_norm_grad, native.rms_norm_grad_workspace, dy, dh, h, gain, inverse, device,
+                                         _raw_stream(device))
+            if parts.__class__ is int:
+                binding.check(parts)
+            if parts is not None:
+                return *parts, parts[0] if ctx.residual else None, None
+        rows = _matrix(h, "h")
         dx, dx_rows = _output(None, h.shape, rows.rows, rows.cols, h.dtype, h)
         dgain = torch.empty(gain.shape, dtype=gain.dtype, device=gain.device)
         L = binding.lib()
@@ -835,7 +851,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: Optiona
         return _Attention.apply(q, k, v, window, sinks, offsets, scale)
     device, native = q.get_device(), _native()
     if out is None and device >= 0 and native is not None:
-        y = native.ext.attention(native.attention, q, k, v, offsets, _window(window, sinks), min(sinks, 1 << 62), scale, device, _raw_stream(device))
+        y = native.ext.attention(native.attention, q, k, v, offsets, _window(window, sinks), min(sinks, 1 << 62), scale, device, _raw_stream(device), 0)
         if y.__class__ is int:
             binding.check(y)
         if y is not None:
@@ -898,8 +914,17 @@ def attention_cached(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: K
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, window, sinks, offsets, scale):
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-        out = _attention(q, k, v, window, sinks, offsets, scale, None, lse)
+        parts, device, native = None, q.get_device(), _native()
+        if device >= 0 and native is not None:
+            parts = native.ext.attention(native.attention, q, k, v, offsets, _window(window, sinks), min(sinks, 1 << 62), scale, device,
+                                         _raw_stream(device), 1)
+            if parts.__class__ is int:
+                binding.check(parts)
+        if parts is None:
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+            out = _attention(q, k, v, window, sinks, offsets, scale, None, lse)
+        else:
+            out, lse = parts
         ctx.save_for_backward(q, k, v, out, lse, offsets)
         ctx.window, ctx.sinks, ctx.scale = window, sinks, scale
         return out
@@ -909,8 +934,16 @@ class _Attention(torch.autograd.Function):
     def backward(ctx, dout):
         q, k, v, out, lse, offsets = ctx.saved_tensors
         dout = dout.contiguous()  # gradients of sums and means arrive with strides of 0
+        device, native = q.get_device(), _native()
+        if native is not None:
+            parts = native.ext.attention_grad(native.attention_grad, native.attention_grad_workspace, dout, q, k, v, out, lse, offsets,
+                                              _window(ctx.window, ctx.sinks), min(ctx.sinks, 1 << 62), ctx.scale, device, _raw_stream(device))
+            if parts.__class__ is int:
+                binding.check(parts)
+            if parts is not None:
+                return *parts, None, None, None, None
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-        L, device, ids = binding.lib(), q.get_device(), _index_tensor(offsets, "offsets")
+        L, ids = binding.lib(), _index_tensor(offsets, "offsets")
         rows = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
         n = _workspace(L.sllm_attention_grad_workspace, *rows[:2], ids)
         ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None

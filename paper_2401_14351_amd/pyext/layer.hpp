@@ -6,10 +6,87 @@
 
 namespace operators {
 
-inline PyObject* wrap_pair(at::Tensor&& a, at::Tensor&& b) {
-    auto first = pybind11::reinterpret_steal<pybind11::object>(THPVariable_Wrap(std::move(a)));
-    auto second = pybind11::reinterpret_steal<pybind11::object>(THPVariable_Wrap(std::move(b)));
-    return first && second ? PyTuple_Pack(2, first.ptr(), second.ptr()) : nullptr;
+inline PyObject* wrap_all(std::initializer_list<at::Tensor*> tensors) {
+    auto out = pybind11::reinterpret_steal<pybind11::object>(PyTuple_New((Py_ssize_t)tensors.size()));
+    if (!out) return nullptr;
+    Py_ssize_t i = 0;
+    for (at::Tensor* t : tensors) {
+        PyObject* o = THPVariable_Wrap(std::move(*t));
+        if (!o) return nullptr;
+        PyTuple_SET_ITEM(out.ptr(), i++, o);
+    }
+    return out.release().ptr();
+}
+
+inline at::Tensor floats(const at::Tensor& like, at::IntArrayRef shape) {
+    return at::empty(shape, like.options().dtype(at::kFloat).requires_grad(false));
+}
+
+// norm_kept(call, x, gain, residual, eps, device, stream): (norm, inverse root mean squares)
+// or (norm, inverses, h), for the gradient.
+inline PyObject* norm_kept(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    SLLM_PY_ARGS(7, "norm_kept(call, x, gain, residual, eps, device, stream)")
+    typedef int32_t (*Call)(const sllm_matrix*, const sllm_matrix*, const sllm_matrix*, float, const sllm_matrix*, const sllm_matrix*, float*,
+                            int32_t, void*);
+    const auto call = address<Call>(args[0]);
+    const double eps = PyFloat_AsDouble(args[4]);
+    const long device = PyLong_AsLong(args[5]);
+    void* const stream = PyLong_AsVoidPtr(args[6]);
+    if (PyErr_Occurred()) return nullptr;
+    const bool has_residual = args[3] != Py_None;
+    const at::Tensor *x = tensor(args[1], device), *gain = tensor(args[2], device), *residual = has_residual ? tensor(args[3], device) : nullptr;
+    sllm_matrix rows, gain_row, residual_rows, h_rows, y_rows;
+    if (!x || !gain || (has_residual && !residual) || !rows_of(*x, &rows) || gain->dim() != 1 || !rows_of(*gain, &gain_row)) Py_RETURN_NONE;
+    if (has_residual && (residual->sizes() != x->sizes() || !rows_of(*residual, &residual_rows))) Py_RETURN_NONE;
+    at::Tensor h, y = make(*x, x->sizes(), rows.rows, rows.dtype, &y_rows), inverse = floats(*x, {(int64_t)rows.rows});
+    if (has_residual) h = make(*x, x->sizes(), rows.rows, rows.dtype, &h_rows);
+    int32_t code;
+    {
+        pybind11::gil_scoped_release no_gil;
+        code = call(&rows, has_residual ? &residual_rows : nullptr, &gain_row, (float)eps, has_residual ? &h_rows : nullptr, &y_rows,
+                    inverse.data_ptr<float>(), (int32_t)device, stream);
+    }
+    if (code != SLLM_OK) return PyLong_FromLong(code);
+    return has_residual ? wrap_all({&y, &inverse, &h}) : wrap_all({&y, &inverse});
+    END_HANDLE_TH_ERRORS
+}
+
+// norm_grad(call, workspace, dy, dh, h, gain, inverse, device, stream): (dx, dgain)
+inline PyObject* norm_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    SLLM_PY_ARGS(9, "norm_grad(call, workspace, dy, dh, h, gain, inverse, device, stream)")
+    typedef int32_t (*Call)(const sllm_matrix*, const sllm_matrix*, const sllm_matrix*, const sllm_matrix*, const float*, const sllm_matrix*,
+                            const sllm_matrix*, void*, uint64_t, int32_t, void*);
+    typedef int32_t (*Workspace)(uint64_t, uint64_t, uint64_t*);
+    const auto call = address<Call>(args[0]);
+    const auto workspace = address<Workspace>(args[1]);
+    const long device = PyLong_AsLong(args[7]);
+    void* const stream = PyLong_AsVoidPtr(args[8]);
+    if (PyErr_Occurred()) return nullptr;
+    const bool has_dh = args[3] != Py_None;
+    const at::Tensor *dy = tensor(args[2], device), *dh = has_dh ? tensor(args[3], device) : nullptr, *h = tensor(args[4], device),
+                     *gain = tensor(args[5], device), *inverse = tensor(args[6], device);
+    sllm_matrix dy_rows, dh_rows, h_rows, gain_row, dx_rows, dgain_row;
+    if (!dy || (has_dh && !dh) || !h || !gain || !inverse || !rows_of(*dy, &dy_rows) || (has_dh && !rows_of(*dh, &dh_rows)) ||
+        !rows_of(*h, &h_rows) || !rows_of(*gain, &gain_row) || inverse->scalar_type() != at::kFloat || inverse->numel() != (int64_t)h_rows.rows ||
+        !inverse->is_contiguous())
+        Py_RETURN_NONE;
+    at::Tensor dx = make(*h, h->sizes(), h_rows.rows, h_rows.dtype, &dx_rows), dgain = make(*gain, gain->sizes(), 1, gain_row.dtype, &dgain_row), ws;
+    int32_t code;
+    {
+        pybind11::gil_scoped_release no_gil;
+        uint64_t n = 0;
+        code = workspace(h_rows.rows, h_rows.cols, &n);
+        if (code == SLLM_OK) {
+            if (n) ws = bytes(*h, 1, (int64_t)n);
+            code = call(&dy_rows, has_dh ? &dh_rows : nullptr, &h_rows, &gain_row, inverse->data_ptr<float>(), &dx_rows, &dgain_row,
+                        n ? ws.data_ptr() : nullptr, n, (int32_t)device, stream);
+        }
+    }
+    if (code != SLLM_OK) return PyLong_FromLong(code);
+    return wrap_all({&dx, &dgain});
+    END_HANDLE_TH_ERRORS
 }
 
 // norm(call, x, gain, residual, eps, mx8, device, stream): the norm, and with a residual
@@ -50,14 +127,8 @@ inline PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                    : reinterpret_cast<Call>(call)(&rows, r, &gain_row, (float)eps, to, &y_rows, nullptr, (int32_t)device, stream);
     }
     if (code != SLLM_OK) return PyLong_FromLong(code);
-    if (mx8 && has_residual) {
-        auto c = pybind11::reinterpret_steal<pybind11::object>(THPVariable_Wrap(std::move(y)));
-        auto s = pybind11::reinterpret_steal<pybind11::object>(THPVariable_Wrap(std::move(scales)));
-        auto o = pybind11::reinterpret_steal<pybind11::object>(THPVariable_Wrap(std::move(h)));
-        return c && s && o ? PyTuple_Pack(3, c.ptr(), s.ptr(), o.ptr()) : nullptr;
-    }
-    if (mx8) return wrap_pair(std::move(y), std::move(scales));
-    if (has_residual) return wrap_pair(std::move(y), std::move(h));
+    if (mx8) return has_residual ? wrap_all({&y, &scales, &h}) : wrap_all({&y, &scales});
+    if (has_residual) return wrap_all({&y, &h});
     return THPVariable_Wrap(std::move(y));
     END_HANDLE_TH_ERRORS
 }
@@ -120,10 +191,11 @@ inline at::Tensor like_heads(const at::Tensor& q, const sllm_heads& from, sllm_h
     return t;
 }
 
-// attention(call, q, k, v, offsets, window, sinks, scale, device, stream)
+// attention(call, q, k, v, offsets, window, sinks, scale, device, stream, keep): the output,
+// or with `keep` (output, lse), for the gradient.
 inline PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
-    SLLM_PY_ARGS(10, "attention(call, q, k, v, offsets, window, sinks, scale, device, stream)")
+    SLLM_PY_ARGS(11, "attention(call, q, k, v, offsets, window, sinks, scale, device, stream, keep)")
     typedef int32_t (*Call)(const sllm_heads*, const sllm_heads*, const sllm_heads*, const sllm_ids*, uint64_t, uint64_t, float,
                             const sllm_heads*, float*, int32_t, void*);
     const auto call = address<Call>(args[0]);
@@ -131,6 +203,7 @@ inline PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     const double scale = PyFloat_AsDouble(args[7]);
     const long device = PyLong_AsLong(args[8]);
     void* const stream = PyLong_AsVoidPtr(args[9]);
+    const long keep = PyLong_AsLong(args[10]);
     if (PyErr_Occurred()) return nullptr;
     const at::Tensor* q = tensor(args[1], device);
     sllm_heads q_rows, k_rows, v_rows, out_rows;
@@ -139,13 +212,57 @@ inline PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!heads_of(q, &q_rows) || !heads_of(tensor(args[2], device), &k_rows) || !heads_of(tensor(args[3], device), &v_rows) ||
         !list_of(args[4], device, &ids, &offsets) || window < 0 || sinks < 0)
         Py_RETURN_NONE;
-    at::Tensor out = like_heads(*q, q_rows, &out_rows);
+    at::Tensor out = like_heads(*q, q_rows, &out_rows), lse;
+    if (keep) lse = floats(*q, {q->size(0), q->size(1)});
     int32_t code;
     {
         pybind11::gil_scoped_release no_gil;
-        code = call(&q_rows, &k_rows, &v_rows, offsets, (uint64_t)window, (uint64_t)sinks, (float)scale, &out_rows, nullptr, (int32_t)device, stream);
+        code = call(&q_rows, &k_rows, &v_rows, offsets, (uint64_t)window, (uint64_t)sinks, (float)scale, &out_rows,
+                    keep ? lse.data_ptr<float>() : nullptr, (int32_t)device, stream);
     }
+    if (code == SLLM_OK && keep) return wrap_all({&out, &lse});
     return result(code, std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// attention_grad(call, workspace, dout, q, k, v, out, lse, offsets, window, sinks, scale,
+// device, stream): (dq, dk, dv)
+inline PyObject* attention_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    SLLM_PY_ARGS(14, "attention_grad(call, workspace, dout, q, k, v, out, lse, offsets, window, sinks, scale, device, stream)")
+    typedef int32_t (*Call)(const sllm_heads*, const sllm_heads*, const sllm_heads*, const sllm_heads*, const sllm_heads*, const float*,
+                            const sllm_ids*, uint64_t, uint64_t, float, const sllm_heads*, const sllm_heads*, const sllm_heads*, void*, uint64_t,
+                            int32_t, void*);
+    typedef int32_t (*Workspace)(const sllm_heads*, const sllm_heads*, const sllm_ids*, uint64_t*);
+    const auto call = address<Call>(args[0]);
+    const auto workspace = address<Workspace>(args[1]);
+    const long long window = PyLong_AsLongLong(args[9]), sinks = PyLong_AsLongLong(args[10]);
+    const double scale = PyFloat_AsDouble(args[11]);
+    const long device = PyLong_AsLong(args[12]);
+    void* const stream = PyLong_AsVoidPtr(args[13]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor *q = tensor(args[3], device), *k = tensor(args[4], device), *v = tensor(args[5], device), *lse = tensor(args[7], device);
+    sllm_heads dout, q_rows, k_rows, v_rows, out, dq_rows, dk_rows, dv_rows;
+    sllm_ids ids;
+    const sllm_ids* offsets;
+    if (!heads_of(tensor(args[2], device), &dout) || !heads_of(q, &q_rows) || !heads_of(k, &k_rows) || !heads_of(v, &v_rows) ||
+        !heads_of(tensor(args[6], device), &out) || !lse || lse->scalar_type() != at::kFloat || !lse->is_contiguous() ||
+        lse->numel() != q->size(0) * q->size(1) || !list_of(args[8], device, &ids, &offsets) || window < 0 || sinks < 0)
+        Py_RETURN_NONE;
+    at::Tensor dq = like_heads(*q, q_rows, &dq_rows), dk = like_heads(*k, k_rows, &dk_rows), dv = like_heads(*v, v_rows, &dv_rows), ws;
+    int32_t code;
+    {
+        pybind11::gil_scoped_release no_gil;
+        uint64_t n = 0;
+        code = workspace(&q_rows, &k_rows, offsets, &n);
+        if (code == SLLM_OK) {
+            if (n) ws = bytes(*q, 1, (int64_t)n);
+            code = call(&dout, &q_rows, &k_rows, &v_rows, &out, lse->data_ptr<float>(), offsets, (uint64_t)window, (uint64_t)sinks, (float)scale,
+                        &dq_rows, &dk_rows, &dv_rows, n ? ws.data_ptr() : nullptr, n, (int32_t)device, stream);
+        }
+    }
+    if (code != SLLM_OK) return PyLong_FromLong(code);
+    return wrap_all({&dq, &dk, &dv});
     END_HANDLE_TH_ERRORS
 }
 

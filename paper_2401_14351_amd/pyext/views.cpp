@@ -105,8 +105,11 @@ PyMethodDef kMethods[] = {method("build", build, "build(buf, table, n, names_rea
                           method("lookup", operators::lookup, "rows of a table by token"),
                           method("lookup_grad", operators::lookup_grad, "the gradient of a lookup by its table"),
                           method("norm", operators::norm, "a root-mean-square norm"),
+                          method("norm_kept", operators::norm_kept, "the same, with what its gradient needs"),
+                          method("norm_grad", operators::norm_grad, "the gradients of a norm"),
                           method("product_octet", operators::product_octet, "x @ w.T, x in MX FP8, w in MX FP4"),
                           method("attention", operators::attention, "causal attention of packed sequences"),
+                          method("attention_grad", operators::attention_grad, "the gradients of attention"),
                           method("attention_cached", operators::attention_cached, "the same of new tokens behind a cache"),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_views", "Views over a loaded buffer, and calls of the operators on it.", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
