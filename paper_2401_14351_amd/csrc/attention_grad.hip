@@ -283,47 +283,40 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         asm volatile("" : "+v"(here));
         const uint32_t rows_at = rows_from<T, D>(here & 63), columns_at = columns_from<T, D>(here & 63), h = here >> 5 & 1;
         const uint32_t values_at = rows_at + wave * kWaveRows * RowTile<T, D>::kPitch;
-        // four fragments at a time, two times four in registers
-        f32x16 s = {}, dp = {};
-        Operand8<T> first[4], second[4];
-        const auto read_q = [&](Operand8<T> (&f)[4], int i) SLLM_INLINE {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = read_rows<T, D>(q, rows_at, 0, i + j);
+        // two steps of both products at a time, their fragments read a run ahead
+        struct Run {
+            Operand8<T> q[2], o[2], v[2];
         };
-        const auto read_o = [&](Operand8<T> (&f)[4], int i) SLLM_INLINE {
+        const auto read = [&](Run& f, int i) SLLM_INLINE {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                f[j] = read_rows<T, D>(dout, rows_at, 0, i + j);
-                f[2 + j] = read_rows<T, D>(values, values_at, 0, i + j);
+                f.q[j] = read_rows<T, D>(q, rows_at, 0, i + j);
+                f.o[j] = read_rows<T, D>(dout, rows_at, 0, i + j);
+                f.v[j] = read_rows<T, D>(values, values_at, 0, i + j);
             }
         };
+        f32x16 s = {}, dp = {};
+        Run run;
+        ColumnFragments<T, D, 32> oc, qc;
+        read(run, 0);
         __builtin_amdgcn_s_setprio(1);
-        read_q(first, 0);
         phase();
 #pragma unroll
-        for (int i = 0; i < kSteps; i += 4) {
-            if (i + 4 < kSteps)
-                read_q(second, i + 4);
-            else
-                read_o(second, 0);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s = multiply(first[j], k[i + j], s);
-            phase();
-#pragma unroll
-            for (int j = 0; j < 4; ++j) first[j] = second[j];
-        }
-        ColumnFragments<T, D, 32> cf;
-#pragma unroll
         for (int i = 0; i < kSteps; i += 2) {
-            if (i + 2 < kSteps)
-                read_o(second, i + 2);
-            else
-                cf.read(dout, columns_at, 0, 0);
+            Run next;
+            if (i + 2 < kSteps) {
+                read(next, i + 2);
+            } else {
+                oc.read(dout, columns_at, 0, 0);
+                qc.read(q, columns_at, 0, 0);
+            }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) dp = multiply(first[j], first[2 + j], dp);
+            for (int j = 0; j < 2; ++j) {
+                s = multiply(run.q[j], k[i + j], s);
+                dp = multiply(run.o[j], run.v[j], dp);
+            }
             phase();
-#pragma unroll
-            for (int j = 0; j < 4; ++j) first[j] = second[j];
+            if (i + 2 < kSteps) run = next;
         }
         __builtin_amdgcn_s_setprio(0);
 #pragma unroll
@@ -350,36 +343,33 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             range.fit(acc_k, dp);
             dp *= range.up;
         }
-        const Operand8<T> p[2] = {as_operand<T>(s, 0), as_operand<T>(s, 1)};
-        phase();
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int d = 0; d < kParts; ++d) {
-            ColumnFragments<T, D, 32> next;
-            if (d + 1 < kParts)
-                next.read(dout, columns_at, 0, d + 1);
-            else
-                next.read(q, columns_at, 0, 0);
-            if (masked) out_of_sight |= cf.take_out();
-            cf.add(acc_v[d], p);
-            phase();
-            cf = next;
-        }
-        const Operand8<T> ds[2] = {as_operand<T>(dp, 0), as_operand<T>(dp, 1)};
+        const Operand8<T> p[2] = {as_operand<T>(s, 0), as_operand<T>(s, 1)}, ds[2] = {as_operand<T>(dp, 0), as_operand<T>(dp, 1)};
         Operand8<T> rest[2];
         if constexpr (kTwice) {
             const f32x16 r = rounded_off<T>(dp, ds);
             rest[0] = as_operand<T>(r, 0), rest[1] = as_operand<T>(r, 1);
         }
+        phase();
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int d = 0; d < kParts; ++d) {
-            ColumnFragments<T, D, 32> next;
-            if (d + 1 < kParts) next.read(q, columns_at, 0, d + 1);
-            if (masked) out_of_sight |= cf.take_out();
-            cf.add(acc_k[d], ds);
-            if constexpr (kTwice) cf.add(acc_k[d], rest);
+            ColumnFragments<T, D, 32> next_o, next_q;
+            if (d + 1 < kParts) {
+                next_o.read(dout, columns_at, 0, d + 1);
+                next_q.read(q, columns_at, 0, d + 1);
+            }
+            if (masked) {
+                out_of_sight |= oc.take_out();
+                out_of_sight |= qc.take_out();
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                acc_v[d] = multiply(oc.f[t], p[t], acc_v[d]);
+                acc_k[d] = multiply(qc.f[t], ds[t], acc_k[d]);
+            }
+            if constexpr (kTwice) qc.add(acc_k[d], rest);
             phase();
-            if (d + 1 < kParts) cf = next;
+            if (d + 1 < kParts) oc = next_o, qc = next_q;
         }
         __builtin_amdgcn_s_setprio(0);
     };
