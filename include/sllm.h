@@ -680,7 +680,7 @@ int32_t sllm_attention_grad(const sllm_heads* dout, const sllm_heads* q, const s
                             const sllm_heads* dv, void* workspace, uint64_t workspace_bytes, int32_t device,
                             void* stream);
 int32_t sllm_attention_grad_workspace(const sllm_heads* q, const sllm_heads* k, const sllm_ids* offsets,
-                                      uint64_t* bytes);
+                                      uint64_t window, uint64_t sinks, uint64_t* bytes);
 
 /* Keys and values of sequences, each (sequences, heads, sinks + window, dim), contiguous:
  * position p is in slot p where p < sinks, and else in slot sinks + (p - sinks) % window,

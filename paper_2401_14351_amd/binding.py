@@ -179,7 +179,7 @@ SIGNATURES = {
                                    C.c_int32, C.c_void_p]),
     "sllm_attention_grad": (C.c_int32, [_HEADS, _HEADS, _HEADS, _HEADS, _HEADS, C.c_void_p, _IDS, C.c_uint64, C.c_uint64,
                                         C.c_float, _HEADS, _HEADS, _HEADS, *_WORK]),
-    "sllm_attention_grad_workspace": (C.c_int32, [_HEADS, _HEADS, _IDS, _U64]),
+    "sllm_attention_grad_workspace": (C.c_int32, [_HEADS, _HEADS, _IDS, C.c_uint64, C.c_uint64, _U64]),
     "sllm_attention_cached": (C.c_int32, [_HEADS, _HEADS, _HEADS, _CACHE, _IDS, _IDS, C.c_float, _HEADS, *_WORK]),
     "sllm_attention_cached_workspace": (C.c_int32, [_HEADS, _HEADS, _HEADS, _CACHE, _IDS, _IDS, _U64]),
     "sllm_last_error": (C.c_char_p, []),

@@ -255,14 +255,16 @@ extern "C" int32_t sllm_attention_grad(const sllm_heads* dout, const sllm_heads*
 }
 SLLM_CATCH_ALL
 
-extern "C" int32_t sllm_attention_grad_workspace(const sllm_heads* q, const sllm_heads* k, const sllm_ids* offsets, uint64_t* bytes) try {
+extern "C" int32_t sllm_attention_grad_workspace(const sllm_heads* q, const sllm_heads* k, const sllm_ids* offsets, uint64_t window,
+                                                 uint64_t sinks, uint64_t* bytes) try {
     clear_error();
     if (!bytes) return fail(SLLM_E_INVAL, "bytes: NULL");
-    AttentionArgs a;
+    AttentionGradArgs a;
     Span s[4];
     int n = 0;
     SLLM_TRY(common_args(q, k, k, 1.0f, &a, s, &n));
     SLLM_TRY(offsets_args(offsets, &a, &s[n]));
+    window_args(window, sinks, &a);
     *bytes = attention_grad_workspace(a);
     return SLLM_OK;
 }

@@ -430,6 +430,19 @@ __device__ __forceinline__ void store_column(const f32x16 (&acc)[D / 32], float 
         }
 }
 
+// Where sequence s starts and how many tokens it has, as find_piece takes the offsets.
+__device__ __forceinline__ void find_sequence(const void* offsets, bool wide, uint32_t s, uint32_t tokens, uint32_t& first, uint32_t& n) {
+    first = 0, n = tokens;
+    if (!offsets) return;
+    const auto clamp = [&](int64_t v) { return (uint32_t)min(max(v, (int64_t)0), (int64_t)tokens); };
+    uint32_t most = 0;
+    for (uint32_t i = threadIdx.x & 63; i <= s; i += 64) most = max(most, clamp(read_id(offsets, wide, i)));
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) most = max(most, (uint32_t)__shfl_xor(most, d));
+    first = __builtin_amdgcn_readfirstlane(most);
+    n = __builtin_amdgcn_readfirstlane(max(first, clamp(read_id(offsets, wide, s + 1)))) - first;
+}
+
 // The keys that the queries at positions i0 to i1 of a sequence see: the first `sinks`
 // positions, those not in the window among them, then lo to i1.  Key c of that list is at
 // distance c - sinks from lo; positions count from lo, in 32 bits.

@@ -181,13 +181,37 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     store_column<T, D, Vec>(acc, kHalf ? a.scale / range.up : a.scale, dq + packed * a.dq_token + q_head * a.dq_head, a.dim);
 }
 
+// Tile `index` of the keys that are sinks; none: n = 0.
+__device__ __forceinline__ Piece find_sinks(const AttentionGradArgs& a, uint32_t index) {
+    Piece p;
+    if (a.sink_tiles) {  // one sequence after the other
+        p = {index / a.sink_tiles, 0, 0, index % a.sink_tiles, 1, 0};
+        find_sequence(a.offsets, a.wide_offsets, p.sequence, a.tokens, p.first, p.n);
+    } else {
+        p = find_piece(a.offsets, a.wide_offsets, a.sequences, a.tokens, 1, kRows, index, a.pieces);
+    }
+    if (p.piece * kRows >= min(p.n, (uint32_t)a.sinks)) p.n = 0;
+    return p;
+}
+
+// Where part s of a sink's sums is, by its place among the tokens or by sequence.
+__device__ __forceinline__ uint64_t far_at(const AttentionGradArgs& a, uint32_t s, const Piece& p, uint32_t key, uint32_t head) {
+    const uint64_t row = a.far_packed ? (uint64_t)p.first + key : (uint64_t)p.sequence * a.sinks + key;
+    return ((2 * s * a.far_rows + row) * a.kv_heads + head) * a.dim;
+}
+
 // dv = p^T dout and dk = scale ds^T q, over the rows (tokens times heads that share the
 // key) that see a key.  A wave has 32 keys, whose statistics are their lanes' own, and the
 // rows come by; scores are of (rows x keys), their gradients' sums of (elements x keys).
 //
 // Two waves of a SIMD hide each other's waits: for that a wave has its keys and the sums in
 // registers, but takes its values from LDS each time.
-template <typename T, int D, bool Vec>
+//
+// Far: what the rows behind the window give to the sinks of a tile, every row of a long text
+// to a few keys.  That is split over many workgroups and joined afterwards.  (Left to the tiles
+// of the sinks, a text of 8192 tokens in 32 heads that share 8 heads of keys, a window of 1024
+// and four sinks took 3.4 ms, without sinks 0.92.)
+template <typename T, int D, bool Vec, bool Far>
 __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void attention_grad_kv(AttentionGradArgs a) {
     constexpr int kTile = 32, kSteps = D / 16, kParts = D / 32;
     constexpr bool kHalf = __is_same(T, _Float16), kTwice = sizeof(T) == 2;
@@ -197,8 +221,11 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     __shared__ __align__(16) uint8_t values[kRows * RowTile<T, D>::kPitch];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t c = lane & 31, h = lane >> 5;
-    const uint32_t index = xcd_index(), split = index % a.splits, head = index / a.splits / a.pieces;
-    const Piece piece = find_piece(a.offsets, a.wide_offsets, a.sequences, a.tokens, 1, kRows, index / a.splits % a.pieces, a.pieces);
+    const uint32_t splits = Far ? a.far : a.splits, index = Far ? blockIdx.x : xcd_index(), split = index % splits;
+    const uint32_t head = index / splits / a.pieces;
+    const Piece piece = Far ? find_sinks(a, index / splits % a.pieces)
+                            : find_piece(a.offsets, a.wide_offsets, a.sequences, a.tokens, 1, kRows, index / splits % a.pieces, a.pieces);
+    if (Far && !piece.n) return;
     T *const dk = static_cast<T*>(a.dk), *const dv = static_cast<T*>(a.dv);
     // sums of a part of the rows, to be joined: of this split, keys and then values
     const uint64_t part_token = (uint64_t)a.kv_heads * a.dim, part_size = a.tokens * part_token;
@@ -215,10 +242,10 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     }
     const uint32_t window = a.window, sinks = a.sinks;
     const uint32_t key0 = piece.piece * kRows, key1 = min(key0 + kRows, piece.n) - 1;
-    const uint32_t last = key0 < sinks ? piece.n - 1 : min(piece.n - 1, key1 + window - 1);  // the last token that sees one
-    const uint32_t all_first = key0 * a.group, all_end = (last + 1) * a.group;
+    const uint32_t near_end = min(piece.n, key1 + window);  // behind the last token whose window holds one
+    const uint32_t all_first = (Far ? near_end : key0) * a.group, all_end = (Far ? piece.n : near_end) * a.group;
     // this split's rows, whole tiles of them, perhaps none
-    const uint32_t share = ((all_end - all_first + kTile - 1) / kTile + a.splits - 1) / a.splits * kTile;
+    const uint32_t share = ((all_end - all_first + kTile - 1) / kTile + splits - 1) / splits * kTile;
     const uint32_t row_first = min(all_first + split * share, all_end), row_end = min(row_first + share, all_end);
     const uint32_t wave_key0 = min(key0 + wave * kWaveRows, key1), wave_key1 = min(wave_key0 + kWaveRows - 1, key1);
     const uint32_t key = min(key0 + wave * kWaveRows + c, key1);
@@ -403,6 +430,14 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     if (key0 + wave * kWaveRows + c > key1) return;
     const uint64_t packed = piece.first + key;
     const float f_v = kHalf ? 0x1p-15f : 1.0f, f_k = kHalf ? a.scale * 0x1p-15f / range.up : a.scale;
+    if (Far || (a.far && a.splits == 1 && key < sinks)) {
+        // a part of a sink's sums: of the far rows' splits one after the other, then of the others
+        if (key >= sinks) return;
+        float* const to = a.far_parts + far_at(a, Far ? split : a.far, piece, key, head);
+        store_column<float, D, Vec>(acc_k, f_k, to, a.dim);
+        store_column<float, D, Vec>(acc_v, f_v, to + a.far_rows * a.kv_heads * a.dim, a.dim);
+        return;
+    }
     if (a.splits > 1) {
         store_column<float, D, Vec>(acc_v, f_v, part_v + packed * part_token + head * a.dim, a.dim);
         store_column<float, D, Vec>(acc_k, f_k, part_k + packed * part_token + head * a.dim, a.dim);
@@ -425,6 +460,30 @@ __global__ __launch_bounds__(256) void join_kv(AttentionGradArgs a) {
     static_cast<T*>(a.dv)[token * a.dv_token + head * a.dv_head + e] = from_f32<T>(v);
 }
 
+// A sink's parts, in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void join_sinks(AttentionGradArgs a) {
+    const uint32_t head = blockIdx.x / a.pieces;
+    const Piece piece = find_sinks(a, blockIdx.x % a.pieces);
+    if (!piece.n) return;
+    const uint32_t key0 = piece.piece * kRows, keys = min((uint32_t)kRows, min(piece.n, (uint32_t)a.sinks) - key0);
+    const uint64_t size = (uint64_t)a.tokens * a.kv_heads * a.dim, values = a.far_rows * a.kv_heads * a.dim;
+    for (uint32_t i = threadIdx.x; i < keys * a.dim; i += 256) {
+        const uint32_t key = key0 + i / a.dim, e = i % a.dim;
+        const uint64_t token = piece.first + key, at = (token * a.kv_heads + head) * a.dim + e;
+        float k = 0, v = 0;
+        if (a.splits > 1)
+            for (uint32_t s = 0; s < a.splits; ++s) k += a.parts[2 * s * size + at], v += a.parts[(2 * s + 1) * size + at];
+#pragma unroll 4
+        for (uint32_t s = 0; s < a.far + (a.splits == 1); ++s) {
+            const float* const from = a.far_parts + far_at(a, s, piece, key, head) + e;
+            k += from[0], v += from[values];
+        }
+        static_cast<T*>(a.dk)[token * a.dk_token + head * a.dk_head + e] = from_f32<T>(k);
+        static_cast<T*>(a.dv)[token * a.dv_token + head * a.dv_head + e] = from_f32<T>(v);
+    }
+}
+
 uint32_t key_pieces(const AttentionArgs& a) { return (uint32_t)ceil_div(a.tokens, kRows) + (a.offsets ? a.sequences : 0); }
 
 // The rows that see a tile of keys are split where there are too few tiles to fill the GPU.
@@ -433,27 +492,67 @@ uint32_t splits_of(const AttentionArgs& a) {
     return blocks ? (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(512 / blocks, 8)) : 1;
 }
 
+// The far rows of sinks: runs of about 1024 in a sequence of twice the average, 64 at the most, as far as 256 MB hold their parts
+// and a grid its workgroups.
+void plan_far(AttentionGradArgs* a) {
+    a->far = 0;
+    if (!a->sinks || !a->sequences || a->tokens <= (uint32_t)a->window) return;
+    const uint64_t listed = (uint64_t)a->sequences * a->sinks;
+    a->far_packed = listed > a->tokens;
+    a->far_rows = std::min<uint64_t>(listed, a->tokens);
+    const uint64_t longest = std::min<uint64_t>(a->tokens, 2ull * a->tokens / a->sequences);
+    const uint64_t rows = longest > (uint64_t)a->window ? (longest - a->window) * a->group : 1, bytes = std::max<uint64_t>(a->far_rows * a->kv_heads * a->dim * 8, 1);
+    const uint64_t tiles = ceil_div(a->sinks, kRows) * a->sequences, pieces = key_pieces(*a);
+    a->sink_tiles = tiles <= pieces ? (uint32_t)ceil_div(a->sinks, kRows) : 0;
+    const uint64_t blocks = std::min(tiles, pieces) * a->kv_heads;
+    a->far = (uint32_t)std::max<uint64_t>(
+        1, std::min<uint64_t>({ceil_div(rows, 1024), 64, (256ull << 20) / bytes, (1ull << 22) / std::max<uint64_t>(blocks, 1)}));
+}
+
+struct Room {
+    uint64_t parts, far, bytes;  // where they start
+};
+Room room_of(const AttentionGradArgs& a) {
+    Room r;
+    r.parts = ((uint64_t)a.tokens * a.heads * 8 + 15) / 16 * 16;
+    r.far = r.parts + (a.splits > 1 ? ((uint64_t)a.splits * a.tokens * a.kv_heads * a.dim * 8 + 15) / 16 * 16 : 0);
+    r.bytes = r.far + (a.far ? a.far + 1ull : 0) * a.far_rows * a.kv_heads * a.dim * 8;
+    return r;
+}
+
 template <typename T, int D>
 void launch(AttentionGradArgs a, hipStream_t stream) {
     a.pieces = (uint32_t)ceil_div((uint64_t)a.tokens * a.group, kRows) + (a.offsets ? a.sequences : 0);
     (a.vec ? attention_grad_q<T, D, true> : attention_grad_q<T, D, false>)<<<dim3(a.pieces * a.kv_heads), kWaves * 64, 0, stream>>>(a);
+    if (a.far) {
+        a.pieces = a.sink_tiles ? a.sink_tiles * a.sequences : key_pieces(a);
+        (a.vec ? attention_grad_kv<T, D, true, true> : attention_grad_kv<T, D, false, true>)<<<dim3(a.pieces * a.kv_heads * a.far), kWaves * 64, 0, stream>>>(a);
+    }
     a.pieces = key_pieces(a);
-    (a.vec ? attention_grad_kv<T, D, true> : attention_grad_kv<T, D, false>)<<<dim3(a.pieces * a.kv_heads * a.splits), kWaves * 64, 0, stream>>>(a);
+    (a.vec ? attention_grad_kv<T, D, true, false> : attention_grad_kv<T, D, false, false>)<<<dim3(a.pieces * a.kv_heads * a.splits), kWaves * 64, 0, stream>>>(a);
     if (a.splits > 1) join_kv<T><<<grid_of(ceil_div((uint64_t)a.tokens * a.kv_heads * a.dim, 256)), 256, 0, stream>>>(a);
+    if (a.far) {
+        a.pieces = a.sink_tiles ? a.sink_tiles * a.sequences : key_pieces(a);
+        join_sinks<T><<<dim3(a.pieces * a.kv_heads), 256, 0, stream>>>(a);
+    }
 }
 
 }  // namespace
 
-uint64_t attention_grad_workspace(const AttentionArgs& a) {
-    const uint64_t rows = (uint64_t)a.tokens * a.heads * 8, splits = splits_of(a);
-    if (splits == 1) return rows;
-    return (rows + 15) / 16 * 16 + splits * a.tokens * a.kv_heads * a.dim * 8;
+uint64_t attention_grad_workspace(AttentionGradArgs a) {
+    a.splits = splits_of(a);
+    plan_far(&a);
+    return room_of(a).bytes;
 }
 
 int32_t launch_attention_grad(AttentionGradArgs a, void* workspace, hipStream_t stream) {
-    a.rows = static_cast<float*>(workspace);
     a.splits = splits_of(a);
-    a.parts = a.rows + ((uint64_t)a.tokens * a.heads * 2 + 3) / 4 * 4;
+    plan_far(&a);
+    const Room room = room_of(a);
+    uint8_t* const ws = static_cast<uint8_t*>(workspace);
+    a.rows = reinterpret_cast<float*>(ws);
+    a.parts = reinterpret_cast<float*>(ws + room.parts);
+    a.far_parts = reinterpret_cast<float*>(ws + room.far);
     SLLM_BY_DTYPE(a.dtype, T, {
         if (a.dim <= 64)
             launch<T, 64>(a, stream);

@@ -137,8 +137,15 @@ struct AttentionGradArgs : AttentionArgs {  // out is read
     float* rows = nullptr;  // tokens x heads, twice
     uint32_t splits = 1;    // of the rows that see a key
     float* parts = nullptr;
+    // what rows behind the window give to sinks: in so many parts, rows of sinks in each, by
+    // their place among the tokens or by sequence, and tiles of sinks of a sequence (0: of any)
+    uint32_t far = 0;
+    uint64_t far_rows = 0;
+    bool far_packed = false;
+    uint32_t sink_tiles = 0;
+    float* far_parts = nullptr;
 };
-uint64_t attention_grad_workspace(const AttentionArgs& a);
+uint64_t attention_grad_workspace(AttentionGradArgs a);
 int32_t launch_attention_grad(AttentionGradArgs a, void* workspace, hipStream_t stream);
 
 // One new token a sequence, tokens and sequences being the same.

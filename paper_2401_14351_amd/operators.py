@@ -945,9 +945,10 @@ class _Attention(torch.autograd.Function):
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
         L, ids = binding.lib(), _index_tensor(offsets, "offsets")
         rows = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
-        n = _workspace(L.sllm_attention_grad_workspace, *rows[:2], ids)
+        window, sinks = _window(ctx.window, ctx.sinks), min(ctx.sinks, 1 << 62)
+        n = _workspace(L.sllm_attention_grad_workspace, *rows[:2], ids, window, sinks)
         ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
         binding.check(L.sllm_attention_grad(
-            _heads(dout, "dout"), *rows, _heads(out, "out"), lse.data_ptr(), ids, _window(ctx.window, ctx.sinks), min(ctx.sinks, 1 << 62),
+            _heads(dout, "dout"), *rows, _heads(out, "out"), lse.data_ptr(), ids, window, sinks,
             ctx.scale, _heads(dq, "dq"), _heads(dk, "dk"), _heads(dv, "dv"), ws.data_ptr() if n else None, n, device, _raw_stream(device)))
         return dq, dk, dv, None, None, None, None

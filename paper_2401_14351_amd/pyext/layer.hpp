@@ -233,7 +233,7 @@ inline PyObject* attention_grad(PyObject*, PyObject* const* args, Py_ssize_t nar
     typedef int32_t (*Call)(const sllm_heads*, const sllm_heads*, const sllm_heads*, const sllm_heads*, const sllm_heads*, const float*,
                             const sllm_ids*, uint64_t, uint64_t, float, const sllm_heads*, const sllm_heads*, const sllm_heads*, void*, uint64_t,
                             int32_t, void*);
-    typedef int32_t (*Workspace)(const sllm_heads*, const sllm_heads*, const sllm_ids*, uint64_t*);
+    typedef int32_t (*Workspace)(const sllm_heads*, const sllm_heads*, const sllm_ids*, uint64_t, uint64_t, uint64_t*);
     const auto call = address<Call>(args[0]);
     const auto workspace = address<Workspace>(args[1]);
     const long long window = PyLong_AsLongLong(args[9]), sinks = PyLong_AsLongLong(args[10]);
@@ -254,7 +254,7 @@ inline PyObject* attention_grad(PyObject*, PyObject* const* args, Py_ssize_t nar
     {
         pybind11::gil_scoped_release no_gil;
         uint64_t n = 0;
-        code = workspace(&q_rows, &k_rows, offsets, &n);
+        code = workspace(&q_rows, &k_rows, offsets, (uint64_t)window, (uint64_t)sinks, &n);
         if (code == SLLM_OK) {
             if (n) ws = bytes(*q, 1, (int64_t)n);
             code = call(&dout, &q_rows, &k_rows, &v_rows, &out, lse->data_ptr<float>(), offsets, (uint64_t)window, (uint64_t)sinks, (float)scale,

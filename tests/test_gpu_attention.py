@@ -156,6 +156,17 @@ def test_attention_and_gradients(case, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths,heads,kv,dim,window,sinks", [([900], 4, 1, 64, 50, 3), ([700, 1, 0, 300], 3, 3, 40, 20, 1),
+                                                               ([400, 500], 2, 1, 128, 10, 200), ([60] * 10, 2, 2, 64, 7, 100),
+                                                               ([5] * 66 + [300], 2, 2, 33, 4, 129), ([1500], 1, 1, 80, 1, 2)])
+def test_sinks_far_behind_the_window(lengths, heads, kv, dim, window, sinks, dtype):
+    """Gradients of sinks, which rows far behind the window see: summed apart."""
+    n = sum(lengths)
+    q, k, v = (normal((n, h, dim), dtype, i) for i, h in enumerate((heads, kv, kv)))
+    check(q, k, v, lengths, window, sinks, dtype, dout=normal((n, heads, dim), dtype, 3, 0.1))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("std,scale", [(8.0, 1.0), (30.0, 0.125), (1e-3, 1.0), (1.0, 1e-30), (1.0, 40.0)])
 def test_scores_of_any_size(dtype, std, scale):
     """Rows that one key dominates, that all share alike, and running maxima that grow a lot."""
@@ -530,7 +541,7 @@ def test_captured_forward_and_gradient_calls():
                                             *(op._heads(g, "g") for g in grads), ws.data_ptr(), ws.numel(), 0, stream))
 
     def room():
-        n = op._workspace(L.sllm_attention_grad_workspace, op._heads(q, "q"), op._heads(k, "k"), None)
+        n = op._workspace(L.sllm_attention_grad_workspace, op._heads(q, "q"), op._heads(k, "k"), None, 100, 2)
         return (torch.empty_like(q), torch.empty(300, 4, device="cuda"), [torch.empty_like(t) for t in (q, k, v)],
                 torch.empty(n, dtype=torch.uint8, device="cuda"))
 

@@ -228,8 +228,8 @@ REFUSED = [
     ("sllm_attention_grad", attention_grad(dv=heads(n=2, data=11 * P)), INVAL),           # dk and dv overlap
     ("sllm_attention_grad", attention_grad(n=8), RANGE),
     ("sllm_attention_grad", attention_grad(ws=13 * P + 4), INVAL),
-    ("sllm_attention_grad_workspace", (Q, K, None, None), INVAL),
-    ("sllm_attention_grad_workspace", (Q, heads(n=3), None, C.c_uint64()), INVAL),
+    ("sllm_attention_grad_workspace", (Q, K, None, 0, 0, None), INVAL),
+    ("sllm_attention_grad_workspace", (Q, heads(n=3), None, 0, 0, C.c_uint64()), INVAL),
     ("sllm_rms_norm", norm(x=None), INVAL),
     ("sllm_rms_norm", norm(y=None), INVAL),
     ("sllm_rms_norm", norm(gain=None), INVAL),
@@ -287,7 +287,9 @@ def test_workspaces_of_any_shape(L, tokens, n, kv, dim):
     size = C.c_uint64()
     for dtype in (0, 1, 2):
         q, k = heads(tokens, n, dim, dtype=dtype), heads(tokens, kv, dim, dtype=dtype)
-        assert L.sllm_attention_grad_workspace(q, k, None, size) == 0
+        for window, sinks in ((0, 0), (1, 1), (100, 1 << 40), (1 << 40, 4)):
+            assert L.sllm_attention_grad_workspace(q, k, None, window, sinks, size) == 0
+            assert L.sllm_attention_grad_workspace(q, k, ids(3), window, sinks, size) == 0
         if tokens <= 4096:
             c = cache(tokens, kv, dim, 4096, 4, dtype=dtype)
             assert L.sllm_attention_cached_workspace(q, k, k, c, ids(tokens), None, size) == 0
