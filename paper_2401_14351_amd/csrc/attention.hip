@@ -125,6 +125,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
 
     bool out_of_sight = false;  // something was taken out
     const auto tile = [&](int32_t i0, const uint8_t* k, const uint8_t* v, bool masked) SLLM_INLINE {
+        bool bad = false;
         f32x16 s[kKeys / 32];
         RowFragments<T, D> kf[kKeys / 32];
         ColumnFragments<T, D, kKeys> vf;
@@ -148,6 +149,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     s[n][i] = here.sees(i0 + 32 * n + 8 * (i / 4) + 4 * (int32_t)h + i % 4) ? s[n][i] : -__builtin_inff();
+            bad = any_not_finite<T, D, kKeys>(v);
+            out_of_sight |= bad;
         }
         float top = s[0][0];
 #pragma unroll
@@ -181,7 +184,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         sum += part;
         phase();
         __builtin_amdgcn_s_setprio(1);
-        out_of_sight |= add_weighted<T, D, kKeys>(acc, vf, v, columns_at, 0, p, masked);
+        add_weighted<T, D, kKeys>(acc, vf, v, columns_at, 0, p, bad);
         __builtin_amdgcn_s_setprio(0);
     };
     const auto step = [&](int32_t i0, const uint8_t* k, const uint8_t* v, uint8_t* next_k, uint8_t* next_v) SLLM_INLINE {
@@ -196,7 +199,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         if (i0 + kKeys < keys.total) step(i0 + kKeys, k1, v1, k0, v0);
     }
 
-    if (__any(out_of_sight))
+    if (out_of_sight)
         for (int32_t i = 0; i < keys.total; ++i)
             put_back<T, D>(acc, key_row(a.v, a.v_token, a.v_head, a.cache_v, i), a.dim, sight.sees(i));
     const f32x2 sums = both_halves(sum);

@@ -229,24 +229,35 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t word) {  // halves that 
     return ((word & kExponent) == kExponent ? 0xffffu : 0u) | ((word >> 16 & kExponent) == kExponent ? 0xffff0000u : 0u);
 }
 template <typename T>
-__device__ __forceinline__ bool take_out(Operand8<T>& o) {
-    uint32_t any = 0;
+__device__ __forceinline__ void take_out(Operand8<T>& o) {
     if constexpr (__is_same(T, float)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const bool bad = (__float_as_uint(o.v[i]) & 0x7f800000) == 0x7f800000;
-            any |= bad;
-            o.v[i] = bad ? 0.0f : o.v[i];
+            o.v[i] = (__float_as_uint(o.v[i]) & 0x7f800000) == 0x7f800000 ? 0.0f : o.v[i];
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t bad = not_finite<T>(o.v[i]);
-            any |= bad;
-            o.v[i] &= ~bad;
+            o.v[i] &= ~not_finite<T>(o.v[i]);
         }
     }
-    return any != 0;
+}
+
+// Whether any of `Rows` rows at the start of a tile has an element that is not finite: a step
+// of the exponent carries into the sign where it is all ones.
+template <typename T, int D, int Rows>
+__device__ __forceinline__ bool any_not_finite(const uint8_t* tile) {
+    constexpr uint32_t kMask = __is_same(T, float) ? 0x7f800000 : __is_same(T, _Float16) ? 0x7c007c00 : 0x7f807f80;
+    constexpr uint32_t kStep = __is_same(T, float) ? 0x00800000 : __is_same(T, _Float16) ? 0x04000400 : 0x00800080;
+    uint32_t from = (threadIdx.x & 63) * 16, any = 0;
+    asm volatile("" : "+v"(from));  // not to be found out before this is reached
+#pragma unroll
+    for (uint32_t i = 0; i < Rows * RowTile<T, D>::kPitch / 1024; ++i) {
+        const u32x4 v = lds_read<u32x4>(tile, i * 1024 + from);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) any |= (v[j] & kMask) + kStep;
+    }
+    return __any((any & (__is_same(T, float) ? 0x80000000 : 0x80008000)) != 0);
 }
 
 // acc with what was taken out: the elements of a row in memory that are not finite, where
@@ -302,30 +313,26 @@ struct ColumnFragments {
 #pragma unroll
         for (int t = 0; t < Rows / 16; ++t) acc = multiply(f[t], w[t], acc);
     }
-    __device__ __forceinline__ bool take_out() {
-        bool out = false;
+    // those that are not finite becoming zeros
+    __device__ __forceinline__ void take_out() {
 #pragma unroll
-        for (int t = 0; t < Rows / 16; ++t) out |= sllm::take_out(f[t]);
-        return out;
+        for (int t = 0; t < Rows / 16; ++t) sllm::take_out(f[t]);
     }
 };
 
-// All of them; the first are read already.  masked: some column must not see some row;
-// whether anything was taken out.
+// All of them; the first are read already.  bad: there is something to take out.
 template <typename T, int D, int Rows>
-__device__ __forceinline__ bool add_weighted(f32x16 (&acc)[D / 32], ColumnFragments<T, D, Rows>& first, const uint8_t* tile, uint32_t from,
-                                             int row0, const Operand8<T> (&w)[Rows / 16], bool masked) {
-    bool out = false;
+__device__ __forceinline__ void add_weighted(f32x16 (&acc)[D / 32], ColumnFragments<T, D, Rows>& first, const uint8_t* tile, uint32_t from,
+                                             int row0, const Operand8<T> (&w)[Rows / 16], bool bad) {
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) {
         ColumnFragments<T, D, Rows> next;
         if (d + 1 < D / 32) next.read(tile, from, row0, d + 1);
-        if (masked) out |= first.take_out();
+        if (bad) first.take_out();
         first.add(acc[d], w);
         phase();
         if (d + 1 < D / 32) first = next;
     }
-    return out;
 }
 
 // ---------------------------------------------------------------------------

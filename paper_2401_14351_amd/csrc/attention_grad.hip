@@ -121,6 +121,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     const auto tile = [&](int32_t i0, const uint8_t* k, const uint8_t* v, bool masked) SLLM_INLINE {
         RowFragments<T, D> kf, vf;
         ColumnFragments<T, D, 32> cf;
+        const bool bad = masked && any_not_finite<T, D, kKeys>(k);
+        out_of_sight |= bad;
         kf.read(k, rows_at, 0);
 #pragma unroll
         for (int n = 0; n < kKeys / 32; ++n) {
@@ -154,7 +156,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             for (int d = 0; d < kParts; ++d) {
                 ColumnFragments<T, D, 32> next;
                 if (d + 1 < kParts) next.read(k, columns_at, 32 * n, d + 1);
-                if (masked) out_of_sight |= cf.take_out();
+                if (bad) cf.take_out();
                 cf.add(acc[d], ds);
                 if constexpr (kTwice) cf.add(acc[d], rest);
                 phase();
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         step(i0, k0, v0, k1, v1);
         if (i0 + kKeys < keys.total) step(i0 + kKeys, k1, v1, k0, v0);
     }
-    if (__any(out_of_sight))
+    if (out_of_sight)
         for (int32_t i = 0; i < keys.total; ++i)
             put_back<T, D>(acc, static_cast<const T*>(a.k) + head * a.k_head + (uint64_t)(piece.first + (uint32_t)(i < keys.sinks ? i : lo + i - keys.sinks)) * a.k_token,
                            a.dim, sight.sees(i));
@@ -322,6 +324,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
                 f.v[j] = read_rows<T, D>(values, values_at, 0, i + j);
             }
         };
+        bool bad = false;
         f32x16 s = {}, dp = {};
         Run run;
         ColumnFragments<T, D, 32> oc, qc;
@@ -365,6 +368,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
                 const bool seen = r0 + 8 * (i / 4) + 4 * h + i % 4 - from < n_seen;
                 s[i] = seen ? s[i] : 0.0f, dp[i] = seen ? dp[i] : 0.0f;
             }
+            bad = any_not_finite<T, D, kTile>(dout) | any_not_finite<T, D, kTile>(q);
+            out_of_sight |= bad;
         }
         if constexpr (kHalf) {
             range.fit(acc_k, dp);
@@ -385,9 +390,9 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
                 next_o.read(dout, columns_at, 0, d + 1);
                 next_q.read(q, columns_at, 0, d + 1);
             }
-            if (masked) {
-                out_of_sight |= oc.take_out();
-                out_of_sight |= qc.take_out();
+            if (bad) {
+                oc.take_out();
+                qc.take_out();
             }
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -405,7 +410,12 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         wait_but_loads<0>();
         barrier();
         if (r0 + kTile < row_end) stage(r0 + kTile, next_q, next_o, next_l, next_d);
-        const uint32_t qa = r0 / a.group, qb = min(r0 + kTile, row_end) - 1, ta = qa, tb = qb / a.group;
+        if constexpr (Far) {
+            // every sink is seen, other keys' sums are not kept, and rows past the end are zeros
+            if (wave_key0 < sinks) tile(r0, q, o, l, d, false);
+            return;
+        }
+        const uint32_t ta = r0 / a.group, tb = (min(r0 + kTile, row_end) - 1) / a.group;
         const bool all = ta >= wave_key1 && r0 + kTile <= row_end && (tb - wave_key0 < window || wave_key1 < sinks);
         if (!(tb < wave_key0 || (wave_key0 >= sinks && ta >= wave_key1 + window))) tile(r0, q, o, l, d, !all);
     };
@@ -417,7 +427,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         step(r0, q0, o0, l0, d0, q1, o1, l1, d1);
         if (r0 + kTile < row_end) step(r0 + kTile, q1, o1, l1, d1, q0, o0, l0, d0);
     }
-    if (__any(out_of_sight)) {
+    if (out_of_sight) {
         uint32_t seen_from, n_seen;
         seen_rows(key, seen_from, n_seen);
         for (uint32_t row = row_first; row < row_end; ++row) {
