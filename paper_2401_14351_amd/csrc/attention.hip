@@ -96,15 +96,24 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         }
     };
     // Tiles whose keys lie one behind the other need no look at each.
-    constexpr bool kRepeat = Vec && !Cached;
-    const bool repeats = kRepeat && a.dim == D && max(a.k_token, a.v_token) < (1u << 24);
+    const bool repeats = Vec && a.dim == D && (Cached || max(a.k_token, a.v_token) < (1u << 24));
     LaneOffsets<T, D, kKeys, kWaves> k_at, v_at;
-    if constexpr (kRepeat) {
-        k_at.set(k_at.kRun * a.k_token, [&](uint32_t r) SLLM_INLINE { return r * (uint32_t)a.k_token; });
-        v_at.set(v_at.kRun * a.v_token, [&](uint32_t r) SLLM_INLINE { return r * (uint32_t)a.v_token; });
+    if constexpr (Vec) {
+        const uint32_t k_token = Cached ? D : (uint32_t)a.k_token, v_token = Cached ? D : (uint32_t)a.v_token;
+        k_at.set(k_at.kRun * (uint64_t)k_token, [&](uint32_t r) SLLM_INLINE { return r * k_token; });
+        v_at.set(v_at.kRun * (uint64_t)v_token, [&](uint32_t r) SLLM_INLINE { return r * v_token; });
     }
     const auto stage = [&](int32_t i0, uint8_t* k, uint8_t* v) SLLM_INLINE {
-        if (repeats && i0 >= keys.sinks && i0 + kKeys <= keys.total) {
+        if constexpr (Cached) {
+            // in the window and in the cache, all before its end or all behind it
+            const int32_t n = i0 - keys.sinks, at = slot0 + n;
+            if (repeats && n >= 0 && n + kKeys <= held && (at >= a.window || at + kKeys <= a.window)) {
+                const uint64_t row = cache_row + (uint32_t)(a.sinks + (at >= a.window ? at - a.window : at));
+                k_at.stage(k, static_cast<const T*>(a.cache_k) + row * D);
+                v_at.stage(v, static_cast<const T*>(a.cache_v) + row * D);
+                return;
+            }
+        } else if (repeats && i0 >= keys.sinks && i0 + kKeys <= keys.total) {
             const uint64_t token = piece.first + (uint32_t)((int32_t)keys.lo + i0 - keys.sinks);
             k_at.stage(k, static_cast<const T*>(a.k) + head * a.k_head + token * a.k_token);
             v_at.stage(v, static_cast<const T*>(a.v) + head * a.v_head + token * a.v_token);
@@ -214,29 +223,35 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
 // what they replace: of those that share a slot the last one alone.
 template <typename W>
 __global__ __launch_bounds__(256) void write_cache(AttentionArgs a, uint32_t row_words) {
-    // the tokens of sequence blockIdx.x
-    __shared__ uint32_t bounds[2];
-    if (threadIdx.x < 2) bounds[threadIdx.x] = 0;
-    __syncthreads();
+    // the tokens of sequence blockIdx.x; what is read is asked for at once
+    __shared__ uint32_t bounds[4];
     const auto clamp = [&](int64_t v) { return (uint32_t)min(max(v, (int64_t)0), (int64_t)a.tokens); };
     const uint32_t s = blockIdx.x;
+    const int64_t past = read_id(a.lengths, a.wide_lengths, s);
+    const uint32_t end = clamp(read_id(a.offsets, a.wide_offsets, s + 1));
     uint32_t most = 0;
     for (uint32_t i = threadIdx.x; i <= s; i += 256) most = max(most, clamp(read_id(a.offsets, a.wide_offsets, i)));
-    atomicMax(&bounds[0], most);
+#pragma unroll
+    for (uint32_t lanes = 32; lanes; lanes /= 2) most = max(most, (uint32_t)__shfl_xor((int)most, lanes));
+    if (threadIdx.x % 64 == 0) bounds[threadIdx.x / 64] = most;
     __syncthreads();
-    const uint32_t first = bounds[0], n = max(first, clamp(read_id(a.offsets, a.wide_offsets, s + 1))) - first;
-    const int64_t past = read_id(a.lengths, a.wide_lengths, s);
+    const uint32_t first = max(max(bounds[0], bounds[1]), max(bounds[2], bounds[3])), n = max(first, end) - first;
     if (past < 0) return;
-    const uint64_t words = (uint64_t)n * a.kv_heads * row_words, step = (uint64_t)gridDim.y * 256;
-    for (uint64_t i = (uint64_t)blockIdx.y * 256 + threadIdx.x; i < words; i += step) {
-        const uint32_t w = i % row_words, head = i / row_words % a.kv_heads, t = i / row_words / a.kv_heads;
+    const uint32_t size = sizeof(W) / a.element;  // strides are in elements
+    for (uint32_t t = blockIdx.y; t < n; t += gridDim.y) {
         const int64_t p = past + t;
         if (p >= a.sinks && p + a.window < past + n) continue;  // a later one has its slot
         const uint64_t slot = p < a.sinks ? p : a.sinks + (uint64_t)(p - a.sinks) % (uint32_t)a.window;
-        const uint64_t to = (((uint64_t)s * a.kv_heads + head) * a.slots + slot) * row_words + w;
-        const uint64_t size = sizeof(W) / a.element;  // strides are in elements
-        static_cast<W*>(a.cache_k)[to] = static_cast<const W*>(a.k)[((uint64_t)(first + t) * a.k_token + head * a.k_head) / size + w];
-        static_cast<W*>(a.cache_v)[to] = static_cast<const W*>(a.v)[((uint64_t)(first + t) * a.v_token + head * a.v_head) / size + w];
+        const uint64_t to = ((uint64_t)s * a.kv_heads * a.slots + slot) * row_words;
+        const W* const k = static_cast<const W*>(a.k) + (uint64_t)(first + t) * a.k_token / size;
+        const W* const v = static_cast<const W*>(a.v) + (uint64_t)(first + t) * a.v_token / size;
+        for (uint32_t i = threadIdx.x; i < a.kv_heads * row_words; i += 256) {
+            const uint32_t head = i / row_words, w = i - head * row_words;
+            const uint64_t at = to + (uint64_t)head * a.slots * row_words + w;
+            const W key = k[head * a.k_head / size + w], value = v[head * a.v_head / size + w];
+            static_cast<W*>(a.cache_k)[at] = key;
+            static_cast<W*>(a.cache_v)[at] = value;
+        }
     }
 }
 
@@ -262,8 +277,8 @@ int32_t launch_attention(AttentionArgs a, hipStream_t stream) {
     if (a.cache_k && a.sequences) {
         a.element = a.dtype == SLLM_DTYPE_F32 ? 4 : 2;
         const uint32_t row_bytes = a.dim * a.element;
-        // a workgroup for every 4096 of its words, were one sequence to have all tokens
-        const dim3 blocks(a.sequences, (uint32_t)std::min<uint64_t>(ceil_div((uint64_t)a.tokens * a.kv_heads * row_bytes / 16, 4096) + 1, 64));
+        // a workgroup for each of its tokens, were one sequence to have a few hundred
+        const dim3 blocks(a.sequences, std::min<uint32_t>(a.tokens, a.sequences > 64 ? 16 : 256));
         if (a.vec)
             write_cache<u32x4><<<blocks, 256, 0, stream>>>(a, row_bytes / 16);
         else if (a.element == 4)
