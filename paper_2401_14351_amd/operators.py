@@ -609,10 +609,10 @@ class _Embedding(torch.autograd.Function):
 # norms
 # ---------------------------------------------------------------------------
 
-def _refuse_capture():
+def _refuse_capture(x: torch.Tensor):
     # A captured backward pass that reaches a leaf which an eager graph holds too waits for
     # that leaf's stream, outside the capture, and ends the process.
-    if torch.cuda.is_current_stream_capturing():
+    if x.is_cuda and torch.cuda.is_current_stream_capturing():
         raise ValueError("norms and attention pass no gradient under graph capture: capture them under torch.no_grad(), "
                          "or the entry points of their gradients")
 
@@ -631,7 +631,7 @@ def rms_norm(x: torch.Tensor, gain: torch.Tensor, residual: Optional[torch.Tenso
     if torch.is_grad_enabled() and (x.requires_grad or gain.requires_grad or (residual is not None and residual.requires_grad)):
         if mx8:
             raise ValueError("a tensor requires a gradient, which a norm in MX FP8 does not pass on")
-        _refuse_capture()
+        _refuse_capture(x)
         y, h = _RmsNorm.apply(x, gain, residual, eps)
         return y if residual is None else (y, h)
     device, native = x.get_device(), _native()
@@ -847,7 +847,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: Optiona
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
         if out is not None:
             raise ValueError("an operator that writes to a given tensor takes no part in autograd")
-        _refuse_capture()
+        _refuse_capture(q)
         return _Attention.apply(q, k, v, window, sinks, offsets, scale)
     device, native = q.get_device(), _native()
     if out is None and device >= 0 and native is not None:

@@ -337,3 +337,15 @@ def test_python_refuses():
         op.mx8_dequantize(op.Mx4(u8[:, :32].contiguous(), torch.zeros(4, 16, dtype=torch.uint8), 40))
     with pytest.raises(ValueError):
         q[1]
+
+
+def test_python_refuses_what_requires_a_gradient():
+    """Without a GPU too, whose streams it does not ask for."""
+    torch = pytest.importorskip("torch")
+    from paper_2401_14351_amd import operators as op
+
+    x = torch.zeros(4, 2, 8, requires_grad=True)
+    with pytest.raises(ValueError):
+        op.attention(x, x, x)
+    with pytest.raises(ValueError):
+        op.rms_norm(x[0], torch.ones(8))
