@@ -638,7 +638,8 @@ int32_t sllm_rms_norm_grad_workspace(uint64_t rows, uint64_t cols, uint64_t* byt
 /* Rows of tokens and heads in device memory, aligned to their element type: head h of
  * token t starts at data + t * token_stride + h * head_stride elements and its
  * `dim` elements are adjacent.  Rows do not overlap: either a token's heads lie within
- * its stride or a head's tokens do.  At most 2^30 rows, and 128 elements each (RANGE). */
+ * its stride or a head's tokens do.  At most 2^30 rows of 128 elements each, and 2^16 heads
+ * (RANGE). */
 typedef struct sllm_heads {
     void*    data;
     uint64_t tokens, heads, dim;
@@ -655,7 +656,7 @@ typedef struct sllm_heads {
  * of kv_heads, and head h has the keys of head h / (heads / kv_heads).  Sequence s is
  * tokens offsets[s] to offsets[s + 1] - 1; NULL: all of them.  Offsets that go back, or lie
  * outside the tokens, are taken as the nearest that do not.  Tokens of no sequence have an
- * output of zeros.
+ * output of zeros.  At most 2^16 sequences, and 2^22 times the heads (RANGE).
  *
  * Scores, their running maximum and sum, and the output's sums are held in 32 bits;
  * weights are rounded to the dtype before they are multiplied with values, as the largest
@@ -671,9 +672,9 @@ int32_t sllm_attention(const sllm_heads* q, const sllm_heads* k, const sllm_head
 /* The gradients of sllm_attention by q, k and v, from dout (as out) and the out and lse of
  * that call: with p = exp(scale q . k - lse) and ds = p (dout . v - dout . out),
  *   dq = scale * sum ds k, dk = scale * sum ds q, dv = sum p dout,
- * the last two over all heads that share the key.  p and ds are rounded to the dtype
- * (a float16 ds times a power of two that keeps it in float16's range) before they are
- * multiplied; sums are held in 32 bits.  Tokens of no sequence have gradients of zeros. */
+ * the last two over all heads that share the key.  p is rounded to the dtype before it is
+ * multiplied; ds goes as that and what the rounding leaves, two products (float16's times a
+ * power of two that keeps it in float16's range); sums are held in 32 bits.  Tokens of no sequence have gradients of zeros. */
 int32_t sllm_attention_grad(const sllm_heads* dout, const sllm_heads* q, const sllm_heads* k, const sllm_heads* v,
                             const sllm_heads* out, const float* lse, const sllm_ids* offsets, uint64_t window,
                             uint64_t sinks, float scale, const sllm_heads* dq, const sllm_heads* dk,
@@ -698,8 +699,9 @@ typedef struct sllm_kv_cache {
  * lengths[s] is how many tokens sequence s has had before; its new tokens are at the
  * positions from there on, see what they see in the cache and among themselves, and are
  * written into the cache.  Sequence s's new tokens are offsets[s] to offsets[s + 1] - 1, as
- * above, or token s alone where offsets is NULL.  A sequence whose length is negative takes
- * no part: its output is zeros and its cache is left as it is.  lengths is only read. */
+ * above, or token s alone where offsets is NULL: then at most 2^22 sequences times heads
+ * (RANGE).  A sequence whose length is negative, or above 2^62, takes no part: its output is
+ * zeros and its cache is left as it is.  lengths is only read. */
 int32_t sllm_attention_cached(const sllm_heads* q, const sllm_heads* k, const sllm_heads* v,
                               const sllm_kv_cache* cache, const sllm_ids* lengths, const sllm_ids* offsets,
                               float scale, const sllm_heads* out, void* workspace, uint64_t workspace_bytes,

@@ -12,7 +12,10 @@ namespace sllm {
 namespace {
 
 constexpr uint64_t kMaxRows = 1ull << 30;  // tokens times heads, and a cache's slots
-constexpr uint64_t kMaxDim = 128;
+constexpr uint64_t kMaxDim = 128, kMaxHeads = 1ull << 16;
+// A workgroup looks through the offsets for its piece; sequences times heads have one at least.
+// With these a grid stays below 2^24 workgroups, its threads in 32 bits.
+constexpr uint64_t kMaxSequences = 1ull << 16, kMaxListed = 1ull << 22;
 
 // The extent of `t`: from its first element to its last.
 int32_t heads_span(const char* name, const sllm_heads* t, Span* out) {
@@ -22,9 +25,9 @@ int32_t heads_span(const char* name, const sllm_heads* t, Span* out) {
     if (t->reserved) return fail(SLLM_E_INVAL, "%s: reserved must be 0", name);
     if (t->dim > kMaxDim) return fail(SLLM_E_RANGE, "%s: heads of %llu elements, at most %llu", name, (unsigned long long)t->dim, (unsigned long long)kMaxDim);
     uint64_t rows;
-    if (!mul_ok(t->tokens, t->heads, &rows) || rows > kMaxRows || t->heads > kMaxRows || t->tokens > kMaxRows)
-        return fail(SLLM_E_RANGE, "%s: %llu tokens of %llu heads, at most %llu together", name, (unsigned long long)t->tokens,
-                    (unsigned long long)t->heads, (unsigned long long)kMaxRows);
+    if (!mul_ok(t->tokens, t->heads, &rows) || rows > kMaxRows || t->heads > kMaxHeads || t->tokens > kMaxRows)
+        return fail(SLLM_E_RANGE, "%s: %llu tokens of %llu heads, at most %llu heads and %llu together", name, (unsigned long long)t->tokens,
+                    (unsigned long long)t->heads, (unsigned long long)kMaxHeads, (unsigned long long)kMaxRows);
     if (!rows || !t->dim) {
         *out = Span{name, static_cast<const uint8_t*>(t->data), 0};
         return SLLM_OK;
@@ -87,9 +90,9 @@ int32_t offsets_args(const sllm_ids* offsets, AttentionArgs* a, Span* s) {
     SLLM_TRY(ids_span(offsets, s));
     s->name = "offsets";
     if (!offsets->n) return fail(SLLM_E_INVAL, "offsets: none");
-    if ((offsets->n - 1) * a->heads > kMaxRows / 64)
-        return fail(SLLM_E_RANGE, "%llu sequences of %u heads, at most %llu together", (unsigned long long)(offsets->n - 1), a->heads,
-                    (unsigned long long)(kMaxRows / 64));
+    if (offsets->n - 1 > kMaxSequences || (offsets->n - 1) * a->heads > kMaxListed)
+        return fail(SLLM_E_RANGE, "%llu sequences of %u heads, at most %llu sequences and %llu together", (unsigned long long)(offsets->n - 1),
+                    a->heads, (unsigned long long)kMaxSequences, (unsigned long long)kMaxListed);
     a->offsets = offsets->data, a->wide_offsets = offsets->bits == 64;
     a->sequences = (uint32_t)(offsets->n - 1);
     return SLLM_OK;
@@ -135,9 +138,9 @@ int32_t cached_args(const sllm_heads* q, const sllm_heads* k, const sllm_heads* 
     if (offsets ? offsets->n - 1 != cache->sequences : q->tokens != cache->sequences)
         return fail(SLLM_E_INVAL, "%llu %s for a cache of %llu sequences", (unsigned long long)(offsets ? offsets->n : q->tokens),
                     offsets ? "offsets" : "tokens, one each,", (unsigned long long)cache->sequences);
-    if (!offsets && q->tokens * q->heads > kMaxRows / 64)
+    if (!offsets && q->tokens * q->heads > kMaxListed)
         return fail(SLLM_E_RANGE, "%llu sequences of %llu heads, at most %llu together", (unsigned long long)q->tokens, (unsigned long long)q->heads,
-                    (unsigned long long)(kMaxRows / 64));
+                    (unsigned long long)kMaxListed);
     a->sequences = (uint32_t)cache->sequences;
     a->slots = cache->window + cache->sinks;
     uint64_t bytes = 0;

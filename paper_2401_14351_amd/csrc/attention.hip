@@ -40,7 +40,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     const Piece piece = find_piece(a.offsets, a.wide_offsets, a.sequences, a.tokens, a.group, kRows, index % a.pieces, a.pieces);
     T* const out = static_cast<T*>(a.out);
     int64_t past = 0;
-    if (Cached && piece.n) past = read_id(a.lengths, a.wide_lengths, piece.sequence);
+    if (Cached && piece.n) past = read_length(a, piece.sequence);
     if (!piece.n || past < 0) {
         // tokens of no sequence, or of one that takes no part
         Piece none = piece;
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(256) void write_cache(AttentionArgs a, uint32_t row
     __shared__ uint32_t bounds[4];
     const auto clamp = [&](int64_t v) { return (uint32_t)min(max(v, (int64_t)0), (int64_t)a.tokens); };
     const uint32_t s = blockIdx.x;
-    const int64_t past = read_id(a.lengths, a.wide_lengths, s);
+    const int64_t past = read_length(a, s);
     const uint32_t end = clamp(read_id(a.offsets, a.wide_offsets, s + 1));
     uint32_t most = 0;
     for (uint32_t i = threadIdx.x; i <= s; i += 256) most = max(most, clamp(read_id(a.offsets, a.wide_offsets, i)));

@@ -343,6 +343,13 @@ __device__ __forceinline__ int64_t read_id(const void* ids, bool wide, uint64_t 
     return wide ? static_cast<const int64_t*>(ids)[i] : static_cast<const int32_t*>(ids)[i];
 }
 
+// How many tokens a sequence has had, -1 where it takes no part.  Past 2^62 positions would
+// leave 64 bits.
+__device__ __forceinline__ int64_t read_length(const AttentionArgs& a, uint32_t s) {
+    const int64_t n = read_id(a.lengths, a.wide_lengths, s);
+    return n > 1ll << 62 ? -1 : n;
+}
+
 // A piece of a sequence: tokens first .. first + n - 1 of the packed rows, and which
 // piece of it.  None: n = 0, then `piece` counts those past the last one, of `spare`, and
 // rows before `first` and from `past_end` on belong to no sequence.

@@ -65,7 +65,7 @@ __global__ __launch_bounds__(kWaves * 64) void attention_step(AttentionArgs a, u
     const uint32_t head = rest % a.kv_heads, sequence = rest / a.kv_heads;
     const uint32_t head0 = head * a.group + block * kHeads, heads = min(kHeads, a.group - block * kHeads);
     T* const out = static_cast<T*>(a.out) + (uint64_t)sequence * a.out_token;
-    const int64_t past = read_id(a.lengths, a.wide_lengths, sequence);
+    const int64_t past = read_length(a, sequence);
     if (past < 0) {  // takes no part
         if (splits == 1)
             for (uint32_t i = threadIdx.x; i < heads * a.dim; i += kWaves * 64) out[(head0 + i / a.dim) * a.out_head + i % a.dim] = (T)0.0f;
@@ -276,7 +276,7 @@ template <typename T>
 __global__ __launch_bounds__(128 * kRuns) void join_parts(AttentionArgs a, uint32_t splits, const float* parts) {
     __shared__ float weights[kMaxSplits], values[kRuns][128], totals[kRuns];
     const uint32_t sequence = blockIdx.x / a.heads, head = blockIdx.x % a.heads, e = threadIdx.x % 128, run = threadIdx.x / 128;
-    const int64_t past = read_id(a.lengths, a.wide_lengths, sequence);
+    const int64_t past = read_length(a, sequence);
     T* const out = static_cast<T*>(a.out) + sequence * a.out_token + head * a.out_head;
     if (past < 0) {
         if (threadIdx.x < a.dim) out[threadIdx.x] = (T)0.0f;

@@ -602,3 +602,30 @@ def test_no_gradient_under_capture():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("length", [-1, -1 << 40, (1 << 62) + 1, (1 << 63) - 2])
+def test_sequences_of_no_length_take_no_part(length):
+    """One between two others, by chunks and by single tokens: zeros, its cache as it was, the others as without it."""
+    q, k, v = (normal((6, h, 64), torch.bfloat16, i) for i, h in enumerate((4, 2, 2)))
+    caches = [op.KvCache(normal((3, 2, 24, 64), torch.bfloat16, 5), normal((3, 2, 24, 64), torch.bfloat16, 6), 20, 4) for _ in range(2)]
+    before = caches[0].k.clone(), caches[0].v.clone()
+    for offsets in (ids([0, 1, 4, 6]), None):
+        tokens = 6 if offsets is not None else 3
+        out = [op.attention_cached(*(t[:tokens] for t in (q, k, v)), c, torch.tensor([30, n, 7], device="cuda"), offsets=offsets)
+               for c, n in zip(caches, (length, 9))]
+        mine = slice(1, 4) if offsets is not None else slice(1, 2)
+        assert not out[0][mine].any() and out[1][mine].any()
+        out[1][mine] = 0
+        assert torch.equal(*out)
+        for a, b, c in zip((caches[0].k, caches[0].v), (caches[1].k, caches[1].v), before):
+            assert torch.equal(a[1], c[1]) and not torch.equal(b[1], c[1])
+            assert torch.equal(a[0], b[0]) and torch.equal(a[2], b[2])
+
+
+def test_summed_inputs_have_gradients_of_their_own():
+    """A norm's input and its residual get equal gradients, not one tensor."""
+    x, r = (normal((5, 64), torch.float32, i).requires_grad_() for i in (1, 2))
+    y, h = op.rms_norm(x, torch.ones(64, device="cuda"), r)
+    (y * y + h).sum().backward()
+    assert torch.equal(x.grad, r.grad) and x.grad.data_ptr() != r.grad.data_ptr()

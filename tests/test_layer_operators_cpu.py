@@ -349,3 +349,19 @@ def test_python_refuses_what_requires_a_gradient():
         op.attention(x, x, x)
     with pytest.raises(ValueError):
         op.rms_norm(x[0], torch.ones(8))
+
+
+def test_grids_stay_within_what_can_be_launched(L):
+    """Sequences, heads and both together, at their limits and one past them."""
+    size = C.c_uint64()
+
+    def grad(n, sequences):
+        return L.sllm_attention_grad_workspace(heads(0, n), heads(0, n), ids(sequences + 1), 0, 0, size)
+
+    def step(n, sequences):
+        q = heads(sequences, n)
+        return L.sllm_attention_cached_workspace(q, q, q, cache(sequences, n, window=1), ids(sequences), None, size)
+
+    assert grad(64, 1 << 16) == 0 and grad(64, (1 << 16) + 1) == RANGE and grad(65, 1 << 16) == RANGE and grad(1, (1 << 16) + 1) == RANGE
+    assert grad(1 << 16, 64) == 0 and grad((1 << 16) + 1, 1) == RANGE
+    assert step(1, 1 << 22) == 0 and step(8, 1 << 19) == 0 and step(8, (1 << 19) + 1) == RANGE
