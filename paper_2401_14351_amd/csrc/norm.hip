@@ -128,12 +128,13 @@ struct NormArgs {
 // up to `Held` times eight of its columns each; longer rows are read again, by the threads
 // that have written them.
 //
-// In MX FP8 the norm is held in 64 bits up to its rounding: an element next to the middle
-// of two of the few values there are then goes to the one that is nearer.
+// The sum of squares is held in 64 bits: those of 32-bit elements may leave 32.  In MX FP8
+// the whole norm is, up to its rounding: an element next to the middle of two of the few
+// values there are then goes to the one that is nearer.
 template <typename T, int Lanes, int Held, bool Vec, bool Mx8>
 __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm(NormArgs a) {
     typedef typename std::conditional<Mx8, double, float>::type S;
-    __shared__ S waves[16];
+    __shared__ double waves[16];
     constexpr uint32_t kThreads = Lanes < 256 ? 256 : Lanes;
     const uint64_t row = (uint64_t)block_index() * (kThreads / Lanes) + threadIdx.x / Lanes;
     if (row >= a.rows) return;  // whole waves, and whole workgroups where they meet
@@ -153,10 +154,10 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm(NormArgs a
             for (int i = 0; i < 8; ++i) v.e[i] = from_f32<T>(to_f32(v.e[i]) + to_f32(r.e[i]));
         }
     };
-    S sum = 0;
+    double sum = 0;
     const auto add = [&](const Eight<Vec, T>& v) SLLM_INLINE {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += (S)to_f32(v.e[i]) * (S)to_f32(v.e[i]);
+        for (int i = 0; i < 8; ++i) sum += (double)to_f32(v.e[i]) * (double)to_f32(v.e[i]);
     };
     S f = 0;
     const auto write = [&](uint64_t c, const Eight<Vec, T>& v, const float (&g)[8]) SLLM_INLINE {
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm(NormArgs a
     };
     const auto finish = [&]() SLLM_INLINE {
         sum = row_sum<Lanes>(sum, waves);
-        f = (S)1 / (Mx8 ? (S)sqrt((double)sum / (double)a.cols + a.eps) : (S)sqrtf((float)sum / (float)a.cols + a.eps));
+        f = (S)(1 / sqrt(sum / (double)a.cols + a.eps));
         if (a.inverse && l == 0) a.inverse[row] = (float)f;
     };
     if constexpr (Held > 0) {
@@ -237,7 +238,8 @@ struct NormGradArgs {
 };
 
 // With f = 1 / sqrt(mean h^2 + eps) and s = dy gain: dx = dh + f (s - h f^2 mean(s h)), and
-// the gain's gradient is the sum over rows of dy h f.  Bound by memory.  `Lanes` threads
+// the gain's gradient is the sum over rows of dy h f.  h only comes with its f, as the norm,
+// whose elements are of ordinary size whatever the row's are.  Bound by memory.  `Lanes` threads
 // take a row at a time, of every `slots`-th row, and keep their columns' sums; where a row
 // is too long for that the sums are kept in memory.
 template <typename T, int Lanes, int Held, bool Vec>
@@ -250,7 +252,7 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
     const auto dx_of = [&](const Eight<Vec, T>& dy, const Eight<Vec, T>& h, const Eight<Vec, T>& dh, const float (&g)[8], float f, float along) SLLM_INLINE {
         Eight<Vec, T> dx;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dx.e[i] = from_f32<T>(to_f32(dh.e[i]) + f * (to_f32(dy.e[i]) * g[i] - to_f32(h.e[i]) * along));
+        for (int i = 0; i < 8; ++i) dx.e[i] = from_f32<T>(to_f32(dh.e[i]) + f * (to_f32(dy.e[i]) * g[i] - to_f32(h.e[i]) * f * along));
         return dx;
     };
     const auto load_dh = [&](uint64_t row, uint64_t c) SLLM_INLINE {
@@ -278,11 +280,11 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
             for (int i = 0; i < Held; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float d = to_f32(dy[i].e[e]) * to_f32(h[i].e[e]);
+                    const float d = to_f32(dy[i].e[e]) * (to_f32(h[i].e[e]) * f);
                     dot += d * g[i][e];
-                    sums[i][e] += d * f;
+                    sums[i][e] += d;
                 }
-            const float along = row_sum<Lanes>(dot, waves) / (float)a.cols * f * f;
+            const float along = row_sum<Lanes>(dot, waves) / (float)a.cols;
 #pragma unroll
             for (int i = 0; i < Held; ++i)
                 dx_of(dy[i], h[i], dh[i], g[i], f, along).store(static_cast<T*>(a.dx) + row * a.dx_stride, (i * Lanes + l) * 8, a.cols);
@@ -305,12 +307,12 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
                 load_gain<Vec>(a.gain, a.gain_dtype, c, a.cols, g);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float d = to_f32(dy.e[e]) * to_f32(h.e[e]);
+                    const float d = to_f32(dy.e[e]) * (to_f32(h.e[e]) * f);
                     dot += d * g[e];
-                    if (c + e < a.cols) part[c + e] = (row == slot ? 0.0f : part[c + e]) + d * f;
+                    if (c + e < a.cols) part[c + e] = (row == slot ? 0.0f : part[c + e]) + d;
                 }
             }
-            const float along = row_sum<Lanes>(dot, waves) / (float)a.cols * f * f;
+            const float along = row_sum<Lanes>(dot, waves) / (float)a.cols;
             for (uint64_t c = l * 8; c < a.cols; c += Lanes * 8) {
                 Eight<Vec, T> dy, h;
                 float g[8];

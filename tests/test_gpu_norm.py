@@ -318,3 +318,29 @@ def test_same_bytes_in_streams_and_graphs():
         torch.cuda.synchronize()
         for a, b in zip(run(), held):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,power", [(torch.float32, 100), (torch.float32, -100), (torch.bfloat16, 110), (torch.bfloat16, -90), (torch.float16, 13),
+                                         (torch.float16, -12)])
+@pytest.mark.parametrize("cols", [5, 1024, 4100, 17000, 33000])
+def test_rows_whose_squares_leave_32_bits(cols, dtype, power):
+    """Large or small all over, eps 0: a power of two times an ordinary row has its norm, and that power's inverse times its gradient."""
+    u = normal((4, cols), dtype, cols).float().clamp(-4, 4)
+    u = torch.where(u.abs() < 2.0 ** -2, 0.25, u)  # nothing of it becomes subnormal
+    x = (u * 2.0 ** power).to(dtype).requires_grad_()
+    gain = (1 + normal((cols,), torch.float32, 3, 0.2)).requires_grad_()
+    dy = normal((4, cols), dtype, 4, 0.1)
+    y = op.rms_norm(x, gain, eps=0.0)
+    y.backward(dy)
+    xv, gv, dyv = host(x), host(gain), host(dy)
+    want = O.norm(xv, gv, 0.0)
+    rel = (cols + 16) * E
+    assert_close(y, want, rel * np.abs(want), dtype)
+    dx, dgain = O.norm_grad(dyv, 0 * xv, xv, gv, 0.0)
+    f = 1 / np.sqrt((xv * xv).mean(1, keepdims=True))
+    size = f * (np.abs(dyv * gv) + np.abs(xv) * f * f * np.abs(dyv * gv * xv).mean(1, keepdims=True))
+    if dtype == torch.float16 and power < 0:  # gradients of its inverse: some past the type's largest
+        dx = np.where(np.abs(dx) < 65000, dx, 0)
+        x.grad[torch.from_numpy(dx == 0).to(x.grad.device)] = 0
+    assert_close(x.grad, dx, 5 * rel * size, dtype)
+    assert_close(gain.grad, dgain, (rel + 24 * E) * np.abs(dyv * xv * f).sum(0), torch.float32)
