@@ -60,7 +60,7 @@ __device__ __forceinline__ void load_gain(const void* gain, uint32_t dtype, uint
 template <int Lanes, typename S>
 __device__ __forceinline__ S row_sum(S x, S* waves) {
 #pragma unroll
-    for (int d = 32; d > 0; d /= 2) x += __shfl_xor(x, d);
+    for (int d = Lanes < 64 ? Lanes / 2 : 32; d > 0; d /= 2) x += __shfl_xor(x, d);
     if constexpr (Lanes > 64) {
         if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = x;
         __syncthreads();
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm(NormArgs a
     __shared__ double waves[16];
     constexpr uint32_t kThreads = Lanes < 256 ? 256 : Lanes;
     const uint64_t row = (uint64_t)block_index() * (kThreads / Lanes) + threadIdx.x / Lanes;
-    if (row >= a.rows) return;  // whole waves, and whole workgroups where they meet
+    if (row >= a.rows) return;  // all threads of a row, which alone meet
     const uint32_t l = threadIdx.x % Lanes;
     const T* const x = static_cast<const T*>(a.x) + row * a.x_stride;
     const T* const residual = static_cast<const T*>(a.residual) + row * a.residual_stride;
@@ -241,12 +241,15 @@ struct NormGradArgs {
 // the gain's gradient is the sum over rows of dy h f.  h only comes with its f, as the norm,
 // whose elements are of ordinary size whatever the row's are.  Bound by memory.  `Lanes` threads
 // take a row at a time, of every `slots`-th row, and keep their columns' sums; where a row
-// is too long for that the sums are kept in memory.
+// is too long for that the sums are kept in memory.  Short rows are taken by a workgroup side
+// by side, which adds up their sums.
 template <typename T, int Lanes, int Held, bool Vec>
 __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormGradArgs a) {
     __shared__ float waves[16];
     constexpr uint32_t kThreads = Lanes < 256 ? 256 : Lanes;
-    const uint32_t slot = blockIdx.x * (kThreads / Lanes) + threadIdx.x / Lanes, l = threadIdx.x % Lanes;
+    constexpr uint32_t kSide = Held == 1 ? kThreads / Lanes : 1, kSlots = kThreads / Lanes / kSide;
+    __shared__ float joined[kSide > 1 ? 3 : 1][kSide > 1 ? Lanes * 8 : 1];
+    const uint32_t slot = blockIdx.x * kSlots + threadIdx.x / (Lanes * kSide), l = threadIdx.x % Lanes, side = threadIdx.x / Lanes % kSide;
     if (slot >= a.slots) return;
     float* const part = a.parts + (uint64_t)slot * a.cols;
     const auto dx_of = [&](const Eight<Vec, T>& dy, const Eight<Vec, T>& h, const Eight<Vec, T>& dh, const float (&g)[8], float f, float along) SLLM_INLINE {
@@ -266,7 +269,7 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
         float g[Held][8], sums[Held][8] = {};
 #pragma unroll
         for (int i = 0; i < Held; ++i) load_gain<Vec>(a.gain, a.gain_dtype, (i * Lanes + l) * 8, a.cols, g[i]);
-        for (uint64_t row = slot; row < a.rows; row += a.slots) {
+        for (uint64_t row = (uint64_t)slot * kSide + side; row < a.rows; row += (uint64_t)a.slots * kSide) {
             const float f = a.inverse[row];
             Eight<Vec, T> dy[Held], h[Held], dh[Held];
 #pragma unroll
@@ -288,6 +291,21 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
 #pragma unroll
             for (int i = 0; i < Held; ++i)
                 dx_of(dy[i], h[i], dh[i], g[i], f, along).store(static_cast<T*>(a.dx) + row * a.dx_stride, (i * Lanes + l) * 8, a.cols);
+        }
+        if constexpr (kSide > 1) {
+            // rows of a wave, then the waves
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+#pragma unroll
+                for (int d = Lanes; d < 64; d *= 2) sums[0][e] += __shfl_xor(sums[0][e], d);
+                if (threadIdx.x >= 64 && threadIdx.x % 64 < Lanes) joined[threadIdx.x / 64 - 1][l * 8 + e] = sums[0][e];
+            }
+            __syncthreads();
+            if (side) return;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int w = 0; w < 3; ++w) sums[0][e] += joined[w][l * 8 + e];
         }
 #pragma unroll
         for (int i = 0; i < Held; ++i)
@@ -352,7 +370,12 @@ bool vector_rows(const void* p, uint64_t stride, uint64_t rows, uint64_t cols, u
 
 template <typename T, bool Vec, bool Mx8>
 void launch_rows(const NormArgs& a, hipStream_t stream) {
-    if (a.cols <= 1024 || (a.cols <= 2048 && a.rows >= 1024))
+    if constexpr (!Mx8) {
+        if (a.cols <= 128) return rms_norm<T, 16, 1, Vec, Mx8><<<grid_of(ceil_div(a.rows, 16)), 256, 0, stream>>>(a);
+    }
+    if (a.cols <= 512)
+        rms_norm<T, 64, 1, Vec, Mx8><<<grid_of(ceil_div(a.rows, 4)), 256, 0, stream>>>(a);
+    else if (a.cols <= 1024 || (a.cols <= 2048 && a.rows >= 1024))
         rms_norm<T, 64, 4, Vec, Mx8><<<grid_of(ceil_div(a.rows, 4)), 256, 0, stream>>>(a);
     else if (a.cols <= 4096)
         rms_norm<T, 256, 2, Vec, Mx8><<<grid_of(a.rows), 256, 0, stream>>>(a);
@@ -366,7 +389,11 @@ void launch_rows(const NormArgs& a, hipStream_t stream) {
 
 template <typename T, bool Vec>
 void launch_grad_rows(const NormGradArgs& a, hipStream_t stream) {
-    if (a.cols <= 2048)
+    if (a.cols <= 128)
+        rms_norm_grad<T, 16, 1, Vec><<<dim3(a.slots), 256, 0, stream>>>(a);
+    else if (a.cols <= 512)
+        rms_norm_grad<T, 64, 1, Vec><<<dim3(a.slots), 256, 0, stream>>>(a);
+    else if (a.cols <= 2048)
         rms_norm_grad<T, 64, 4, Vec><<<dim3((uint32_t)ceil_div(a.slots, 4)), 256, 0, stream>>>(a);
     else if (a.cols <= 4096)
         rms_norm_grad<T, 256, 2, Vec><<<dim3(a.slots), 256, 0, stream>>>(a);
@@ -378,10 +405,11 @@ void launch_grad_rows(const NormGradArgs& a, hipStream_t stream) {
         rms_norm_grad<T, 1024, 0, Vec><<<dim3(a.slots), 1024, 0, stream>>>(a);
 }
 
-// Rows of the workspace, one for the rows that a slot of workgroups takes in turn.
+// Rows of the workspace, one for the rows that a slot of workgroups takes in turn, or side by
+// side.
 uint32_t grad_slots(uint64_t rows, uint64_t cols) {
-    const uint64_t most = cols <= 2048 ? 2048 : cols <= 8192 ? 768 : 256;
-    return (uint32_t)std::min<uint64_t>(rows, most);
+    const uint64_t most = cols <= 2048 ? 2048 : cols <= 8192 ? 768 : 256, side = cols <= 128 ? 16 : cols <= 512 ? 4 : 1;
+    return (uint32_t)std::min<uint64_t>(ceil_div(rows, side), most);
 }
 
 // x in MX FP8: as mx_quantize is for MX FP4.

@@ -344,3 +344,14 @@ def test_rows_whose_squares_leave_32_bits(cols, dtype, power):
         x.grad[torch.from_numpy(dx == 0).to(x.grad.device)] = 0
     assert_close(x.grad, dx, 5 * rel * size, dtype)
     assert_close(gain.grad, dgain, (rel + 24 * E) * np.abs(dyv * xv * f).sum(0), torch.float32)
+
+
+@pytest.mark.parametrize("rows,cols", [(15, 8), (17, 128), (33, 129), (40000, 64), (32769, 33), (5, 512), (9001, 257), (2, 513)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_short_rows(rows, cols, dtype):
+    """Heads as rows: many side by side, the last workgroup's not all there."""
+    for residual in (False, True):
+        test_norm_and_gradients(rows, cols, dtype, residual)
+    q = op.rms_norm(normal((rows, cols), dtype, 1), torch.ones(cols, device="cuda"), mx8=True)
+    codes, scales = O.quantize8(O.norm(host(normal((rows, cols), dtype, 1)), np.ones(cols), float(np.float32(1e-5))))
+    assert (q.codes.cpu().numpy() == codes).all() and (q.scales.cpu().numpy() == scales).all()
