@@ -123,10 +123,10 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         stage_rows<T, D, kKeys, kWaves, Vec>(v, a.dim, [&](uint32_t r) SLLM_INLINE { return key_row(a.v, a.v_token, a.v_head, a.cache_v, i0 + (int32_t)r); });
     };
 
-    // Weights are 2^(scale s - m) times 2^kUp: float16 has the least of those as normal numbers.
-    constexpr float kUp = __is_same(T, _Float16) ? 7.0f : 0.0f, kSlack = 8.0f;
     const float scale = a.scale * kLog2e;
-    float m = -__builtin_inff(), m_scaled = 0, sum = 0;
+    Reference<T> ref;
+    bool far = false;  // a row's scores are too large to be scaled as they are
+    float sum = 0;
     f32x16 acc[kParts];
 #pragma unroll
     for (int d = 0; d < kParts; ++d) acc[d] = f32x16{};
@@ -166,25 +166,25 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         for (int n = 0; n < kKeys / 32; ++n)
 #pragma unroll
             for (int i = n == 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
-        if (__any((top - m) * scale > kSlack)) {
+        if (__any((top - ref.most) * scale > ref.kSlack)) {
             const f32x2 tops = both_halves(top);
-            const float next = fmaxf(m, fmaxf(tops[0], tops[1]));
-            const float next_scaled = next == -__builtin_inff() ? -kUp : __builtin_fmaf(next, scale, -kUp);
-            const float f = __builtin_amdgcn_exp2f(m == -__builtin_inff() ? 0.0f : m_scaled - next_scaled);
-            m = next, m_scaled = next_scaled;
+            const float f = ref.raise(fmaxf(ref.most, fmaxf(tops[0], tops[1])), scale);
+            far = __any(ref.less != 0);
             sum *= f;
 #pragma unroll
             for (int d = 0; d < kParts; ++d) acc[d] *= f;
         }
+        if (far)
+#pragma unroll
+            for (int n = 0; n < kKeys / 32; ++n) s[n] -= ref.less;
         Operand8<T> p[kKeys / 16];
-        const float m_finite = m == -__builtin_inff() ? 0.0f : m;
+        const float finite = ref.finite();
         float part = 0;
 #pragma unroll
         for (int n = 0; n < kKeys / 32; ++n) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                // (the difference first is exact near the largest score, which 16 bits do not tell)
-                s[n][i] = __builtin_amdgcn_exp2f(sizeof(T) == 4 ? (s[n][i] - m_finite) * scale : __builtin_fmaf(s[n][i], scale, -m_scaled));
+                s[n][i] = ref.weight(s[n][i], scale, finite);
                 part += s[n][i];
             }
             p[2 * n] = as_operand<T>(s[n], 0);
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     sum = sums[0] + sums[1];
     if (wave_row + c >= rows) return;
     const uint64_t out_row = piece.first + token;
-    if (a.lse && h == 0) a.lse[out_row * a.heads + q_head] = (m_scaled + __builtin_amdgcn_logf(sum)) * kLn2;
+    if (a.lse && h == 0) a.lse[out_row * a.heads + q_head] = ref.log_sum(sum, scale) * kLn2;
     store_column<T, D, Vec>(acc, 1.0f / sum, out + out_row * a.out_token + q_head * a.out_head, a.dim);
 }
 

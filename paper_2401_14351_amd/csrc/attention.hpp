@@ -336,6 +336,45 @@ __device__ __forceinline__ void add_weighted(f32x16 (&acc)[D / 32], ColumnFragme
 }
 
 // ---------------------------------------------------------------------------
+// Softmax
+// ---------------------------------------------------------------------------
+
+// What a row's weights are taken against: of a score s, 2^(scale (s - less) - scaled), which
+// is 2^kUp for the row's largest so far, or up to 2^kSlack times that.  float16 has the least
+// of such weights as normal numbers.  Scores so large that a rounded `scaled` would be off by
+// more than 2^-8 have their own largest taken away first.
+template <typename T>
+struct Reference {
+    static constexpr float kUp = __is_same(T, _Float16) ? 7.0f : 0.0f, kSlack = 8.0f, kFar = 0x1p16f;
+    float most = -__builtin_inff(), less = 0, scaled = 0;
+
+    // The row's largest is now `next`: what is made of the sums so far.
+    __device__ __forceinline__ float raise(float next, float scale) {
+        const bool none = next == -__builtin_inff();
+        const float next_less = sizeof(T) == 2 && !none && __builtin_fabsf(next * scale) > kFar ? next : 0.0f;
+        const float next_scaled = none ? -kUp : __builtin_fmaf(next - next_less, scale, -kUp);
+        const float down = sizeof(T) == 4 ? (most - next) * scale : __builtin_fmaf(less - next_less, scale, scaled) - next_scaled;
+        const float f = __builtin_amdgcn_exp2f(most == -__builtin_inff() ? 0.0f : down);
+        most = next, less = next_less, scaled = next_scaled;
+        return f;
+    }
+    __device__ __forceinline__ float weight(float s, float scale, float finite) const {
+        // (the difference first is exact near the largest score, which 16 bits do not tell)
+        return __builtin_amdgcn_exp2f(sizeof(T) == 4 ? (s - finite) * scale : __builtin_fmaf(s, scale, -scaled));
+    }
+    __device__ __forceinline__ float finite() const { return most == -__builtin_inff() ? 0.0f : most; }
+    // What makes sums of weights those against scale * most - kUp, without its rounding.
+    __device__ __forceinline__ float exact(float scale) const {
+        return sizeof(T) == 4 || most == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(kUp - __builtin_fmaf(most - less, scale, -scaled));
+    }
+    // log2 of the sum of 2^(scale s), of that of weights
+    __device__ __forceinline__ float log_sum(float sum, float scale) const {
+        const float l = __builtin_amdgcn_logf(sum);
+        return sizeof(T) == 4 ? __builtin_fmaf(most, scale, l) : __builtin_fmaf(less, scale, scaled + l);
+    }
+};
+
+// ---------------------------------------------------------------------------
 // Sequences
 // ---------------------------------------------------------------------------
 

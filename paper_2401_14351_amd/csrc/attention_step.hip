@@ -41,7 +41,7 @@ __device__ __forceinline__ Split split_keys(const AttentionArgs& a, int64_t past
 }
 
 // Where a workgroup's part of the result goes: not divided by the sum of its weights,
-// behind its maximum (times the scale) and that sum.
+// behind the largest score and that sum.
 __device__ __forceinline__ uint64_t part_at(const AttentionArgs& a, uint32_t splits, uint64_t row, uint32_t split) {
     return (row * splits + split) * (a.dim + 2);
 }
@@ -129,9 +129,9 @@ __global__ __launch_bounds__(kWaves * 64) void attention_step(AttentionArgs a, u
         }
     };
 
-    constexpr float kUp = __is_same(T, _Float16) ? 7.0f : 0.0f, kSlack = 8.0f;
     const float scale = a.scale * kLog2e;
-    float m = -__builtin_inff(), m_scaled = 0, sum = 0;
+    Reference<T> ref;
+    float sum = 0;
     f32x4 acc[kParts];
 #pragma unroll
     for (int d = 0; d < kParts; ++d) acc[d] = f32x4{0, 0, 0, 0};
@@ -174,22 +174,19 @@ __global__ __launch_bounds__(kWaves * 64) void attention_step(AttentionArgs a, u
         float top = s[0][0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e / 4][e % 4]);
-        if (__any((top - m) * scale > kSlack)) {
+        if (__any((top - ref.most) * scale > ref.kSlack)) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float next = fmaxf(m, top);
-            const float next_scaled = next == -__builtin_inff() ? -kUp : __builtin_fmaf(next, scale, -kUp);
-            const float f = __builtin_amdgcn_exp2f(m == -__builtin_inff() ? 0.0f : m_scaled - next_scaled);
-            m = next, m_scaled = next_scaled;
+            const float f = ref.raise(fmaxf(ref.most, top), scale);
             sum *= f;
 #pragma unroll
             for (int d = 0; d < kParts; ++d) acc[d] *= f;
         }
         Operand8<T> p;
-        const float m_finite = m == -__builtin_inff() ? 0.0f : m;
+        const float finite = ref.finite();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float w = __builtin_amdgcn_exp2f(sizeof(T) == 4 ? (s[e / 4][e % 4] - m_finite) * scale : __builtin_fmaf(s[e / 4][e % 4], scale, -m_scaled));
+            const float w = ref.weight(s[e / 4][e % 4] - ref.less, scale, finite);
             sum += w;
             s[e / 4][e % 4] = w;
         }
@@ -235,12 +232,13 @@ __global__ __launch_bounds__(kWaves * 64) void attention_step(AttentionArgs a, u
     // The waves' parts, one after the other.
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    if (g == 0) tops[wave][r] = m == -__builtin_inff() ? m : m_scaled, sums[wave][r] = sum;
+    const float exact = ref.exact(scale);
+    if (g == 0) tops[wave][r] = ref.most, sums[wave][r] = sum * exact;
     __syncthreads();
     float most = -__builtin_inff();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) most = fmaxf(most, tops[w][r]);
-    const float f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m_scaled - most);
+    const float f = ref.most == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((ref.most - most) * scale) * exact;
     static_assert(sizeof b0 >= kWaves * kHeads * 4, "");
     constexpr uint32_t kPitch = D + 4;  // floats: neighbouring heads in other banks
     float* const joined = reinterpret_cast<float*>(wave < 2 ? b0 : b1) + (wave & 1) * kHeads * kPitch;
@@ -255,7 +253,7 @@ __global__ __launch_bounds__(kWaves * 64) void attention_step(AttentionArgs a, u
         for (int w = 0; w < kWaves; ++w) top = fmaxf(top, tops[w][q_head]);
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            if (tops[w][q_head] != -__builtin_inff()) total += sums[w][q_head] * __builtin_amdgcn_exp2f(tops[w][q_head] - top);
+            if (tops[w][q_head] != -__builtin_inff()) total += sums[w][q_head] * __builtin_amdgcn_exp2f((tops[w][q_head] - top) * scale);
             value += reinterpret_cast<float*>(w < 2 ? b0 : b1)[((w & 1) * kHeads + q_head) * kPitch + e];
         }
         if (splits == 1) {
@@ -294,7 +292,7 @@ __global__ __launch_bounds__(128 * kRuns) void join_parts(AttentionArgs a, uint3
     __syncthreads();
     for (int32_t s = threadIdx.x; s < used; s += 128 * kRuns) {
         const float at = weights[s];
-        weights[s] = at == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(at - top);
+        weights[s] = at == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((at - top) * (a.scale * kLog2e));
     }
     __syncthreads();
     float total = 0, value = 0;

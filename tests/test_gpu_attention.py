@@ -629,3 +629,35 @@ def test_summed_inputs_have_gradients_of_their_own():
     y, h = op.rms_norm(x, torch.ones(64, device="cuda"), r)
     (y * y + h).sum().backward()
     assert torch.equal(x.grad, r.grad) and x.grad.data_ptr() != r.grad.data_ptr()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("power", [17, 20, 29])
+@pytest.mark.parametrize("order", ["up", "down", "only", "below"])
+def test_scores_far_from_zero(dtype, power, order):
+    """Scores of a large power of two, either sign, and something small, which 32 bits hold exactly.
+
+    Exponents are then exact to 2^-16, and what is off is half a step of each weight and of the output."""
+    n, heads, kv, dim = 300, 4, 2, 64
+    big = 2.0 ** power
+    x = normal((n,), torch.float32, 5, 1.0)
+    step = max(2.0 ** (power - 23), 2.0 ** -4)
+    x = (x / step).round() * step if power < 24 else torch.zeros_like(x)
+    third = torch.arange(n, device="cuda") * 3 // n - 1.0  # -1, 0, 1
+    sign = {"up": third, "down": -third, "only": torch.ones_like(third), "below": -torch.ones_like(third)}[order]
+    q, k, v = (torch.zeros(n, h, dim, device="cuda") for h in (heads, kv, kv))
+    q[..., 0], q[..., 1] = 2.0 ** (power // 2), 1
+    k[..., 0], k[..., 1] = (sign * 2.0 ** (power - power // 2))[:, None], x[:, None]
+    v = normal((n, kv, dim), dtype, 7)
+    q, k = q.to(dtype), k.to(dtype)
+    scores = (q.double() @ k.double().repeat_interleave(heads // kv, 1).permute(1, 2, 0)[0]).permute(1, 0, 2).cpu()  # heads x rows x keys
+    scores = scores.masked_fill(torch.ones(n, n, dtype=torch.bool).triu(1), -math.inf)
+    want = (torch.softmax(scores, -1) @ v.double().cpu().repeat_interleave(heads // kv, 1).transpose(0, 1)).transpose(0, 1)
+    tol = (3 * UNIT[dtype] + 2.0 ** -14) * v.double().abs().max().item()
+    out = op.attention(q, k, v, scale=1.0)
+    assert (out.double().cpu() - want).abs().max() <= tol
+    cache = op.KvCache.empty(1, kv, dim, 2000, 0, dtype=dtype, device="cuda")
+    out = op.attention_cached(q[:-1], k[:-1], v[:-1], cache, ids([0]), offsets=ids([0, n - 1]), scale=1.0)
+    assert (out.double().cpu() - want[:-1]).abs().max() <= tol
+    out = op.attention_cached(q[-1:], k[-1:], v[-1:], cache, ids([n - 1]), scale=1.0)
+    assert (out.double().cpu() - want[-1:]).abs().max() <= tol
