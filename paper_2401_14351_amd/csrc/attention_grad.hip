@@ -86,10 +86,6 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         delta = both[0] + both[1];
     }
     const float lse = a.lse[packed * a.heads + q_head] * kLog2e, scale = a.scale * kLog2e;
-    if (h == 0 && wave_row + c < rows) {
-        a.rows[packed * a.heads + q_head] = lse;
-        a.rows[(uint64_t)a.tokens * a.heads + packed * a.heads + q_head] = delta;
-    }
 
     const bool repeats = Vec && a.dim == D && max(a.k_token, a.v_token) < (1u << 24);
     LaneOffsets<T, D, kKeys, kWaves> k_at, v_at;
@@ -112,11 +108,61 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         stage_rows<T, D, kKeys, kWaves, Vec>(k, a.dim, [&](uint32_t r) SLLM_INLINE { return row_of(a.k, a.k_token, a.k_head, r); });
         stage_rows<T, D, kKeys, kWaves, Vec>(v, a.dim, [&](uint32_t r) SLLM_INLINE { return row_of(a.v, a.v_token, a.v_head, r); });
     };
+    const auto each_tile = [&](const auto& work) SLLM_INLINE {
+        const auto step = [&](int32_t i0, const uint8_t* k, const uint8_t* v, uint8_t* next_k, uint8_t* next_v) SLLM_INLINE {
+            wait_but_loads<0>();
+            barrier();
+            if (i0 + kKeys < keys.total) stage(i0 + kKeys, next_k, next_v);
+            if (!keys.none(at0, at1, i0, i0 + kKeys - 1)) work(i0, k, v, !keys.all(at0, at1, i0, i0 + kKeys - 1));
+        };
+        stage(0, k0, v0);
+        for (int32_t i0 = 0; i0 < keys.total; i0 += 2 * kKeys) {
+            step(i0, k0, v0, k1, v1);
+            if (i0 + kKeys < keys.total) step(i0 + kKeys, k1, v1, k0, v0);
+        }
+    };
+    const uint32_t rows_at = rows_from<T, D>(lane), columns_at = columns_from<T, D>(lane);
+    const auto weigh = [&](f32x16& s, const f32x16& dp, int32_t i0, bool masked) SLLM_INLINE {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -lse)) * (dp[i] - delta);
+        if (masked) {
+            const KeyList::Sight here = sight.here();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = here.sees(i0 + 8 * (i / 4) + 4 * (int32_t)h + i % 4) ? s[i] : 0.0f;
+        }
+    };
+    // A row's ds sum to zero.  What they do sum to, delta is off by: out has been rounded, and
+    // its weights.  Of many keys that is little; where there are few they are gone through once
+    // for it.  (Of two bf16 keys dq is off by 0.0043 of itself without, 0.0017 with; of some ten
+    // by a third more than with.)
+    constexpr int32_t kFew = 3 * 64;
+    if (kTwice && keys.total <= kFew) {
+        float sum = 0;
+        each_tile([&](int32_t i0, const uint8_t* k, const uint8_t* v, bool masked) SLLM_INLINE {
+#pragma unroll
+            for (int n = 0; n < kKeys / 32; ++n) {
+                RowFragments<T, D> f;
+                f.read(k, rows_at, 32 * n);
+                f32x16 s = f.times(q);
+                f.read(v, rows_at, 32 * n);
+                weigh(s, f.times(dout), i0 + 32 * n, masked);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum += s[i];
+            }
+        });
+        const f32x2 sums = both_halves(sum);
+        delta += sums[0] + sums[1];
+        barrier();  // the tiles have been read
+    }
+    if (h == 0 && wave_row + c < rows) {
+        a.rows[packed * a.heads + q_head] = lse;
+        a.rows[(uint64_t)a.tokens * a.heads + packed * a.heads + q_head] = delta;
+    }
+
     f32x16 acc[kParts];
 #pragma unroll
     for (int d = 0; d < kParts; ++d) acc[d] = f32x16{};
     Range range;
-    const uint32_t rows_at = rows_from<T, D>(lane), columns_at = columns_from<T, D>(lane);
     bool out_of_sight = false;  // something was taken out
     const auto tile = [&](int32_t i0, const uint8_t* k, const uint8_t* v, bool masked) SLLM_INLINE {
         RowFragments<T, D> kf, vf;
@@ -133,13 +179,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             cf.read(k, columns_at, 32 * n, 0);
             const f32x16 dp = vf.times(dout);
             phase();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -lse)) * (dp[i] - delta);
-            if (masked) {
-                const KeyList::Sight here = sight.here();
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = here.sees(i0 + 32 * n + 8 * (i / 4) + 4 * (int32_t)h + i % 4) ? s[i] : 0.0f;
-            }
+            weigh(s, dp, i0 + 32 * n, masked);
             if constexpr (kHalf) {
                 range.fit(acc, s);
                 s *= range.up;
@@ -164,17 +204,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             }
         }
     };
-    const auto step = [&](int32_t i0, const uint8_t* k, const uint8_t* v, uint8_t* next_k, uint8_t* next_v) SLLM_INLINE {
-        wait_but_loads<0>();
-        barrier();
-        if (i0 + kKeys < keys.total) stage(i0 + kKeys, next_k, next_v);
-        if (!keys.none(at0, at1, i0, i0 + kKeys - 1)) tile(i0, k, v, !keys.all(at0, at1, i0, i0 + kKeys - 1));
-    };
-    stage(0, k0, v0);
-    for (int32_t i0 = 0; i0 < keys.total; i0 += 2 * kKeys) {
-        step(i0, k0, v0, k1, v1);
-        if (i0 + kKeys < keys.total) step(i0 + kKeys, k1, v1, k0, v0);
-    }
+    each_tile(tile);
     if (out_of_sight)
         for (int32_t i = 0; i < keys.total; ++i)
             put_back<T, D>(acc, static_cast<const T*>(a.k) + head * a.k_head + (uint64_t)(piece.first + (uint32_t)(i < keys.sinks ? i : lo + i - keys.sinks)) * a.k_token,

@@ -661,3 +661,32 @@ def test_scores_far_from_zero(dtype, power, order):
     assert (out.double().cpu() - want[:-1]).abs().max() <= tol
     out = op.attention_cached(q[-1:], k[-1:], v[-1:], cache, ids([n - 1]), scale=1.0)
     assert (out.double().cpu() - want[-1:]).abs().max() <= tol
+
+
+@pytest.mark.parametrize("dtype", TYPES[:2])
+@pytest.mark.parametrize("lengths,heads,kv,dim,window,sinks", [([2] * 40, 8, 8, 128, None, 0), ([3, 5, 2, 9, 17, 1, 30] * 4, 6, 2, 40, None, 0),
+                                                               ([400], 4, 4, 64, 3, 1), ([190, 193], 4, 1, 128, 2, 0), ([900], 8, 1, 80, 5, 2)])
+def test_few_keys_have_exact_gradients(lengths, heads, kv, dim, window, sinks, dtype):
+    """Where rows see few keys their gradients by queries and keys are off by their own rounding alone.
+
+    That is at most half a step of each and spread evenly below it: at the most 1 / sqrt(3) = 0.577 of half a step of all
+    of them in the root mean square, where each is just above a power of two.  Sums in 32 bits, and scores' gradients in
+    two parts (2^-16), add a hundredth."""
+    n = sum(lengths)
+    q, k, v, d = (normal((n, h, dim), dtype, i) for i, h in enumerate((heads, kv, kv, heads)))
+    offsets = ids(np.concatenate([[0], np.cumsum(lengths)]))
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    got = torch.autograd.grad(op.attention(*leaves, window=window, sinks=sinks, offsets=offsets), leaves, d)
+    wide = [t.double().cpu().requires_grad_() for t in (q, k, v)]
+    out, at = [], 0
+    for m in lengths:
+        qs, ks, vs = (t[at:at + m].transpose(0, 1) for t in wide)
+        ks, vs = (t.repeat_interleave(heads // kv, 0) for t in (ks, vs))
+        i, j = torch.arange(m)[:, None], torch.arange(m)
+        seen = (j <= i) & ((i - j < (window or m)) | (j < sinks))
+        s = (qs @ ks.transpose(1, 2) * dim ** -0.5).masked_fill(~seen, -math.inf)
+        out.append((torch.softmax(s, -1) @ vs).transpose(0, 1))
+        at += m
+    want = torch.autograd.grad(torch.cat(out), wide, d.double().cpu())
+    for g, w in zip(got[:2], want[:2]):
+        assert (g.double().cpu() - w).norm() <= 0.587 * UNIT[dtype] * w.norm()
