@@ -526,14 +526,24 @@ __global__ __launch_bounds__(256) void join_sinks(AttentionGradArgs a) {
 
 uint32_t key_pieces(const AttentionArgs& a) { return (uint32_t)ceil_div(a.tokens, kRows) + (a.offsets ? a.sequences : 0); }
 
-// The rows that see a tile of keys are split where there are too few tiles to fill the GPU.
+// The rows that see a tile of keys are split where there are too few tiles to fill the GPU, up
+// to four workgroups for each CU: the first tiles of a text have the most rows, and with two of
+// them for each CU all would wait for those.  (The gradients in us, up to two and up to
+// four: 32 heads that share 8 over 8192 tokens 2977 and 2283, over 2048 264 and 246, 8192 with a
+// window of 2048 1137 and 1154; eight: 1203.)  A split has 256 rows at least (1333 tokens in
+// three sequences, 15 heads that share 5, a window of 300: of 128, 256, 512 rows 85, 79, 93), and
+// there are 16 at most (8 heads that share one over 512 tokens: 8 splits 78, 16 68).
 uint32_t splits_of(const AttentionArgs& a) {
     const uint64_t blocks = (uint64_t)key_pieces(a) * a.kv_heads;
-    return blocks ? (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(512 / blocks, 8)) : 1;
+    if (!blocks || !a.sequences) return 1;
+    const uint64_t rows = std::min<uint64_t>(ceil_div(a.tokens, a.sequences), (uint64_t)a.window + kRows) * a.group;
+    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({1024 / blocks, rows / 256, 16}));
 }
 
-// The far rows of sinks: runs of about 1024 in a sequence of twice the average, 64 at the most, as far as 256 MB hold their parts
-// and a grid its workgroups.
+// The far rows of sinks: runs of about 1024 in a sequence of twice the average, 64 at the most,
+// as far as 256 MB hold their parts and a grid its workgroups.  (32 heads that share 8 over 8192
+// tokens, a window of 1024 and four sinks, in us: runs of 256 737, 512 707, 1024 719, 2048 752, one
+// run 1819.)
 void plan_far(AttentionGradArgs* a) {
     a->far = 0;
     if (!a->sinks || !a->sequences || a->tokens <= (uint32_t)a->window) return;

@@ -356,7 +356,7 @@ int32_t launch_tiled(const LinearLaunch& a, const Plan& p, void* workspace, hipS
 // elements of x at a time, and drops what is 2^-13 below the largest of them: 2^-17 of a
 // sum's magnitudes at the most where they are normally distributed, far less than 16 bits
 // tell, but more than 32 bits do.  x is then written out as bfloat16, which holds it, and
-// multiplied so (4096 x 8192 by 28672 1.55 ms, in eight bits 0.86).
+// multiplied so (4096 x 8192 by 28672 1.42 ms, in eight bits 0.83).
 bool widened(const LinearLaunch& a) { return a.x.fp8 && a.out_dtype == SLLM_DTYPE_F32; }
 
 LinearLaunch widen(const LinearLaunch& a, void* x) {

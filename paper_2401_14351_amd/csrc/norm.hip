@@ -368,6 +368,12 @@ bool vector_rows(const void* p, uint64_t stride, uint64_t rows, uint64_t cols, u
     return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && cols % 8 == 0 && (rows <= 1 || stride * size % 16 == 0));
 }
 
+// As few threads as hold a row: a sum within a wave is done sooner than across waves, and what
+// is held in vain costs registers (in bf16, 2^25 elements, us: rows of 128 by 16 threads 25, by
+// 64 81; 512 by 64 threads and one load each 24, with four 41; 1024 by 64 26, by 256 50; 2048 25
+// and 30; 4096 with two loads 24, with four 28; 8192 with four 25, read twice by 1024 threads 30;
+// 16384 by 1024 23.5, read twice 25.5; 32768 held by 1024 32.5, read twice 29).  One wave a row
+// leaves CUs empty where rows are few, from 1025 columns on.
 template <typename T, bool Vec, bool Mx8>
 void launch_rows(const NormArgs& a, hipStream_t stream) {
     if constexpr (!Mx8) {
@@ -381,8 +387,8 @@ void launch_rows(const NormArgs& a, hipStream_t stream) {
         rms_norm<T, 256, 2, Vec, Mx8><<<grid_of(a.rows), 256, 0, stream>>>(a);
     else if (a.cols <= 8192)
         rms_norm<T, 256, 4, Vec, Mx8><<<grid_of(a.rows), 256, 0, stream>>>(a);
-    else if (a.cols <= 32768)
-        rms_norm<T, 1024, 4, Vec, Mx8><<<grid_of(a.rows), 1024, 0, stream>>>(a);
+    else if (a.cols <= 16384)
+        rms_norm<T, 1024, 2, Vec, Mx8><<<grid_of(a.rows), 1024, 0, stream>>>(a);
     else
         rms_norm<T, 1024, 0, Vec, Mx8><<<grid_of(a.rows), 1024, 0, stream>>>(a);
 }
@@ -406,7 +412,10 @@ void launch_grad_rows(const NormGradArgs& a, hipStream_t stream) {
 }
 
 // Rows of the workspace, one for the rows that a slot of workgroups takes in turn, or side by
-// side.
+// side: as many as the GPU holds at once, since more have to be written and joined.  (In bf16,
+// 2^25 elements, us: 1024 columns with 256, 1024, 2048 and 4096 slots 154, 56, 55 and 56; 4096 with
+// 256, 768, 2048, 4096 56, 55, 56, 75; 8192 with 256, 768, 1024, 2048 56, 58, 60, 83; 16384 with
+// 256, 512, 1024 55, 59, 85.)
 uint32_t grad_slots(uint64_t rows, uint64_t cols) {
     const uint64_t most = cols <= 2048 ? 2048 : cols <= 8192 ? 768 : 256, side = cols <= 128 ? 16 : cols <= 512 ? 4 : 1;
     return (uint32_t)std::min<uint64_t>(ceil_div(rows, side), most);
