@@ -348,8 +348,10 @@ void launch(const SkinnyArgs& a, hipStream_t stream) {
 }  // namespace
 
 int32_t launch_skinny(const SkinnyArgs& a, hipStream_t stream) {
-    if (a.x_fp8)
+    if (a.x_fp8 && a.m <= 16)
         launch<Fp8, 16, 1>(a, stream);
+    else if (a.x_fp8)
+        launch<Fp8, 16, 2>(a, stream);
     else if (a.x_scales && a.m <= 16)
         launch<void, 16, 1>(a, stream);
     else if (a.x_scales)

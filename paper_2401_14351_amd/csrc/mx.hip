@@ -133,10 +133,13 @@ struct Plan {
 // unless said: bfloat16 5 rows 12.5 and 15.7, 8 rows 14.1 and 15.9, 16 rows 17.8 and
 // 16.4, 16 rows by 32000 x 4096 42 and 30; float16 5 rows 17.2 and 18.1, 16 rows 20.1
 // and 19.0, 16 rows by 16384 x 4096 25.2 and 21.5; float 16 rows 31 and 34, 16 rows by
-// 32000 x 4096 71 and 67; MX FP4 16 rows 11.3 and 15.2, 32 rows 17.1 and 15.6.
+// 32000 x 4096 71 and 67; MX FP4 16 rows 11.3 and 15.2, 32 rows 17.1 and 15.6;
+// MX FP8 16 rows 12.4 and 17.9, by 16384 x 8192 31.7 and 33.8, more rows by 1024 x 4096
+// 11 to 12 and 17.6, 32 by 4096 x 4096 13.8 and 17.6, by 4096 x 8192 26.5 and 21.3.
 bool few_rows(const LinearLaunch& a) {
     if (a.grad) return false;
-    if (a.x.codes) return a.m <= (a.x.fp8 ? 16 : 32) && a.m * a.n <= 1 << 18;
+    if (a.x.fp8) return a.m <= 16 ? a.m * a.n <= 1 << 18 : a.m <= 32 && a.m * a.n * a.k <= 1 << 29;
+    if (a.x.codes) return a.m <= 32 && a.m * a.n <= 1 << 18;
     if (a.m <= 4) return true;
     if (a.x.dtype == SLLM_DTYPE_F16) return a.m <= 16 && a.n <= 8192;
     return a.m <= 16 && a.m * a.n <= (a.x.dtype == SLLM_DTYPE_F32 ? 1 << 18 : 1 << 17);

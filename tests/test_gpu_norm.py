@@ -355,3 +355,8 @@ def test_short_rows(rows, cols, dtype):
     q = op.rms_norm(normal((rows, cols), dtype, 1), torch.ones(cols, device="cuda"), mx8=True)
     codes, scales = O.quantize8(O.norm(host(normal((rows, cols), dtype, 1)), np.ones(cols), float(np.float32(1e-5))))
     assert (q.codes.cpu().numpy() == codes).all() and (q.scales.cpu().numpy() == scales).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(18, 1, 1), (32, 17, 33), (31, 513, 1100), (25, 100, 4100), (32, 1025, 545), (33, 64, 64)])
+def test_products_of_two_sixteens_of_rows(m, n, k):
+    test_linear8(m, n, k)
