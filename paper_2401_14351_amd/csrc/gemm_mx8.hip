@@ -21,7 +21,9 @@ __device__ __forceinline__ uint32_t pair_at(uint32_t r, uint32_t c) { return r *
 // scaled matrix instruction takes both, and their scales, as they are stored.
 //
 // A stage of 64 of the depth is 64 bytes a row of x and 32 of W: four of them are in flight,
-// loaded straight to LDS, and waited for by their number.  512 of the depth share a load
+// loaded straight to LDS, and waited for by their number.  Bound by the matrix cores, whose
+// clock falls under it, and their waits: 4096 x 8192 by 28672 829 to 875 us, 2.2 to 2.3 PF/s (the
+// library's product of 8192 cubed, both sides in eight bits, 2.7), busy 55 % of the cycles.  512 of the depth share a load
 // of scales, 16 bytes a row.  Of a stage, a lane (r, h) of the instruction holds, in eight
 // bits, elements 16 h to 16 h + 15 of both blocks, and in four all of block h, and gives
 // the scale of block h.

@@ -124,7 +124,8 @@ struct NormArgs {
 };
 
 // h = x + residual, rounded; y = h / sqrt(mean h^2 + eps) * gain.  Bound by memory: x and
-// the residual are read once, h and y written once.  `Lanes` threads take a row and keep
+// the residual are read once, h and y written once (8191 x 5120 in bf16, 336 MB: 66 us, 5.1
+// TB/s; 4096 x 8192 to MX FP8 57 to 65; a row of 4096 3 us, a launch and two reads in turn).  `Lanes` threads take a row and keep
 // up to `Held` times eight of its columns each; longer rows are read again, by the threads
 // that have written them.
 //
@@ -239,7 +240,8 @@ struct NormGradArgs {
 
 // With f = 1 / sqrt(mean h^2 + eps) and s = dy gain: dx = dh + f (s - h f^2 mean(s h)), and
 // the gain's gradient is the sum over rows of dy h f.  h only comes with its f, as the norm,
-// whose elements are of ordinary size whatever the row's are.  Bound by memory.  `Lanes` threads
+// whose elements are of ordinary size whatever the row's are.  Bound by memory (8191 x 5120 in
+// bf16, 252 MB with no dh: 63 to 69 us; 16384 x 8192 161, 5.0 TB/s).  `Lanes` threads
 // take a row at a time, of every `slots`-th row, and keep their columns' sums; where a row
 // is too long for that the sums are kept in memory.  Short rows are taken by a workgroup side
 // by side, which adds up their sums.
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
     }
 }
 
-// The slots' sums, in their order: 32 runs of slots side by side, then those.
+// The slots' sums, in their order: 32 runs of slots side by side, then those (768 x 5120: 4.3 us).
 template <typename G>
 __global__ __launch_bounds__(1024) void join_gain(const float* parts, uint32_t slots, uint64_t cols, G* out) {
     constexpr uint32_t kRuns = 32, kCols = 32;
@@ -404,7 +406,7 @@ void launch_grad_rows(const NormGradArgs& a, hipStream_t stream) {
     else if (a.cols <= 4096)
         rms_norm_grad<T, 256, 2, Vec><<<dim3(a.slots), 256, 0, stream>>>(a);
     else if (a.cols <= 8192)
-        rms_norm_grad<T, 256, 4, Vec><<<dim3(a.slots), 256, 0, stream>>>(a);
+        rms_norm_grad<T, 512, 2, Vec><<<dim3(a.slots), 512, 0, stream>>>(a);
     else if (a.cols <= 16384)
         rms_norm_grad<T, 1024, 2, Vec><<<dim3(a.slots), 1024, 0, stream>>>(a);
     else
@@ -412,12 +414,12 @@ void launch_grad_rows(const NormGradArgs& a, hipStream_t stream) {
 }
 
 // Rows of the workspace, one for the rows that a slot of workgroups takes in turn, or side by
-// side: as many as the GPU holds at once, since more have to be written and joined.  (In bf16,
-// 2^25 elements, us: 1024 columns with 256, 1024, 2048 and 4096 slots 154, 56, 55 and 56; 4096 with
-// 256, 768, 2048, 4096 56, 55, 56, 75; 8192 with 256, 768, 1024, 2048 56, 58, 60, 83; 16384 with
-// 256, 512, 1024 55, 59, 85.)
+// side: as many as the GPU holds at once, since more have to be written and joined.  (2^27
+// elements in bf16, 805 MB, us: 1024 columns with 256, 1024, 2048 and 4096 slots 733, 215, 156 and
+// 174; 4096 with 256, 512, 768 and 2048 213, 153, 161 and 176; 8192 165, 161, 172 and 193, by 256
+// threads that hold twice as much 184, 165, 180 and 193; 16384 160, 170, 184 and 252.)
 uint32_t grad_slots(uint64_t rows, uint64_t cols) {
-    const uint64_t most = cols <= 2048 ? 2048 : cols <= 8192 ? 768 : 256, side = cols <= 128 ? 16 : cols <= 512 ? 4 : 1;
+    const uint64_t most = cols <= 2048 ? 2048 : cols <= 8192 ? 512 : 256, side = cols <= 128 ? 16 : cols <= 512 ? 4 : 1;
     return (uint32_t)std::min<uint64_t>(ceil_div(rows, side), most);
 }
 
