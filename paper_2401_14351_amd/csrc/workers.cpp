@@ -20,6 +20,7 @@ struct Worker {
     std::condition_variable cv;
     std::function<void()> task;
     bool has_task = false;
+    uint32_t keep = 0;  // idle threads kept when the task ends
 };
 
 // Never destroyed: idle threads wait on their workers until the process
@@ -52,7 +53,9 @@ Registry& registry() {
 }
 
 // Idle threads kept (SLLM_IDLE_WORKERS, at most kMaxIdleWorkers; 0 starts
-// every task on a new thread, for comparison), read as each task ends.
+// every task on a new thread, for comparison), read by the thread that starts a task.
+// A worker must not read it: when its task is done the caller goes on, and may change
+// its environment while the worker still looks through it.
 uint32_t max_idle() {
     const char* s = std::getenv("SLLM_IDLE_WORKERS");
     if (!s || !*s) return kMaxIdleWorkers;
@@ -65,17 +68,18 @@ uint32_t max_idle() {
 void worker_main(Worker* w) {
     for (;;) {
         std::function<void()> task;
+        uint32_t keep = 0;
         {
             std::unique_lock<std::mutex> lk(w->mu);
             w->cv.wait(lk, [&] { return w->has_task; });
             task = std::move(w->task);
+            keep = w->keep;
             w->task = nullptr;
             w->has_task = false;
         }
         task();
         task = nullptr;  // drop what the task holds before going idle
         Registry& r = registry();
-        const uint32_t keep = max_idle();
         {
             std::lock_guard<std::mutex> g(r.mu);
             if (r.idle.size() < keep) {
@@ -93,7 +97,8 @@ void worker_main(Worker* w) {
 bool dispatch(std::function<void()> task) {
     Registry& r = registry();
     Worker* w = nullptr;
-    if (max_idle() > 0) {
+    const uint32_t keep = max_idle();
+    if (keep > 0) {
         std::lock_guard<std::mutex> g(r.mu);
         if (!r.idle.empty()) {
             w = r.idle.back();
@@ -105,6 +110,7 @@ bool dispatch(std::function<void()> task) {
             std::lock_guard<std::mutex> g(w->mu);
             w->task = std::move(task);
             w->has_task = true;
+            w->keep = keep;
         }
         w->cv.notify_one();
         return true;
@@ -113,6 +119,7 @@ bool dispatch(std::function<void()> task) {
     if (!w) return false;
     w->task = std::move(task);
     w->has_task = true;
+    w->keep = keep;
     try {
         std::thread(worker_main, w).detach();
     } catch (...) {
