@@ -10,10 +10,11 @@ namespace sllm {
 
 namespace {
 
-// Eight elements from column c, zeros past the end of the row.  Vec: the row starts on 16
-// bytes and ends on a multiple of eight columns.
-template <bool Vec, typename T>
+// Eight elements from column c, every Step-th, zeros past the end of the row.  Vec: the row
+// starts on 16 bytes and ends on a multiple of eight columns, and they are neighbours.
+template <bool Vec, typename T, int Step = 1>
 struct Eight {
+    static_assert(!Vec || Step == 1, "");
     T e[8];
 
     __device__ __forceinline__ void load(const T* row, uint64_t c, uint64_t cols) {
@@ -25,7 +26,7 @@ struct Eight {
             __builtin_memcpy(e, raw, sizeof e);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? row[c + i] : (T)0.0f;
+            for (int i = 0; i < 8; ++i) e[i] = c + i * Step < cols ? row[c + i * Step] : (T)0.0f;
         }
     }
     __device__ __forceinline__ void store(T* row, uint64_t c, uint64_t cols) const {
@@ -38,22 +39,22 @@ struct Eight {
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (c + i < cols) row[c + i] = e[i];
+                if (c + i * Step < cols) row[c + i * Step] = e[i];
         }
     }
 };
 
 // The gain, of any type.
-template <bool Vec, typename G>
+template <bool Vec, int Step, typename G>
 __device__ __forceinline__ void load_floats(const G* from, uint64_t c, uint64_t cols, float (&g)[8]) {
-    Eight<Vec, G> v;
+    Eight<Vec, G, Step> v;
     v.load(from, c, cols);
 #pragma unroll
     for (int i = 0; i < 8; ++i) g[i] = to_f32(v.e[i]);
 }
-template <bool Vec>
+template <bool Vec, int Step>
 __device__ __forceinline__ void load_gain(const void* gain, uint32_t dtype, uint64_t c, uint64_t cols, float (&g)[8]) {
-    SLLM_BY_DTYPE(dtype, G, load_floats<Vec>(static_cast<const G*>(gain), c, cols, g));
+    SLLM_BY_DTYPE(dtype, G, load_floats<Vec, Step>(static_cast<const G*>(gain), c, cols, g));
 }
 
 // The sum over the `Lanes` threads of a row, in all of them: the same order on every call.
@@ -140,28 +141,30 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm(NormArgs a
     const uint64_t row = (uint64_t)block_index() * (kThreads / Lanes) + threadIdx.x / Lanes;
     if (row >= a.rows) return;  // all threads of a row, which alone meet
     const uint32_t l = threadIdx.x % Lanes;
+    constexpr int kStep = Vec || Mx8 ? 1 : Lanes;
+    const uint32_t l0 = kStep == 1 ? l * 8 : l;  // this thread's first column of 8 Lanes
     const T* const x = static_cast<const T*>(a.x) + row * a.x_stride;
     const T* const residual = static_cast<const T*>(a.residual) + row * a.residual_stride;
     T* const h = static_cast<T*>(a.h) + row * a.h_stride;
     const uint64_t blocks = (a.cols + 31) / 32, pitch = (blocks + 15) / 16 * 16;
     const uint64_t end = Mx8 ? pitch * 32 : a.cols;
 
-    const auto load = [&](uint64_t c, Eight<Vec, T>& v) SLLM_INLINE {
+    const auto load = [&](uint64_t c, Eight<Vec, T, kStep>& v) SLLM_INLINE {
         v.load(x, c, a.cols);
         if (a.residual) {
-            Eight<Vec, T> r;
+            Eight<Vec, T, kStep> r;
             r.load(residual, c, a.cols);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v.e[i] = from_f32<T>(to_f32(v.e[i]) + to_f32(r.e[i]));
         }
     };
     double sum = 0;
-    const auto add = [&](const Eight<Vec, T>& v) SLLM_INLINE {
+    const auto add = [&](const Eight<Vec, T, kStep>& v) SLLM_INLINE {
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += (double)to_f32(v.e[i]) * (double)to_f32(v.e[i]);
     };
     S f = 0;
-    const auto write = [&](uint64_t c, const Eight<Vec, T>& v, const float (&g)[8]) SLLM_INLINE {
+    const auto write = [&](uint64_t c, const Eight<Vec, T, kStep>& v, const float (&g)[8]) SLLM_INLINE {
         float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -183,7 +186,7 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm(NormArgs a
             if (b < blocks) *reinterpret_cast<u32x2*>(a.codes + row * blocks * 32 + c) = codes;
             if (c % 32 == 0 && b < pitch) a.scales[row * pitch + b] = b < blocks ? scale : 0;
         } else {
-            Eight<Vec, T> o;
+            Eight<Vec, T, kStep> o;
 #pragma unroll
             for (int i = 0; i < 8; ++i) o.e[i] = from_f32<T>(y[i]);
             o.store(static_cast<T*>(a.y) + row * a.y_stride, c, a.cols);
@@ -195,33 +198,33 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm(NormArgs a
         if (a.inverse && l == 0) a.inverse[row] = (float)f;
     };
     if constexpr (Held > 0) {
-        Eight<Vec, T> v[Held];
+        Eight<Vec, T, kStep> v[Held];
         float g[Held][8];
 #pragma unroll
-        for (int i = 0; i < Held; ++i) load((i * Lanes + l) * 8, v[i]);
+        for (int i = 0; i < Held; ++i) load(i * Lanes * 8 + l0, v[i]);
 #pragma unroll
         for (int i = 0; i < Held; ++i) {
-            load_gain<Vec>(a.gain, a.gain_dtype, (i * Lanes + l) * 8, a.cols, g[i]);
+            load_gain<Vec, kStep>(a.gain, a.gain_dtype, i * Lanes * 8 + l0, a.cols, g[i]);
             add(v[i]);
-            if (a.residual) v[i].store(h, (i * Lanes + l) * 8, a.cols);
+            if (a.residual) v[i].store(h, i * Lanes * 8 + l0, a.cols);
         }
         finish();
 #pragma unroll
         for (int i = 0; i < Held; ++i)
-            if ((i * Lanes + l) * 8 < end) write((i * Lanes + l) * 8, v[i], g[i]);
+            if (i * Lanes * 8 + l0 < end) write(i * Lanes * 8 + l0, v[i], g[i]);
     } else {
-        for (uint64_t c = l * 8; c < a.cols; c += Lanes * 8) {
-            Eight<Vec, T> v;
+        for (uint64_t c = l0; c < a.cols; c += Lanes * 8) {
+            Eight<Vec, T, kStep> v;
             load(c, v);
             add(v);
             if (a.residual) v.store(h, c, a.cols);
         }
         finish();
-        for (uint64_t c = l * 8; c < end; c += Lanes * 8) {
-            Eight<Vec, T> v;
+        for (uint64_t c = l0; c < end; c += Lanes * 8) {
+            Eight<Vec, T, kStep> v;
             float g[8];
             v.load(a.residual ? h : x, c, a.cols);
-            load_gain<Vec>(a.gain, a.gain_dtype, c, a.cols, g);
+            load_gain<Vec, kStep>(a.gain, a.gain_dtype, c, a.cols, g);
             write(c, v, g);
         }
     }
@@ -253,15 +256,17 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
     __shared__ float joined[kSide > 1 ? 3 : 1][kSide > 1 ? Lanes * 8 : 1];
     const uint32_t slot = blockIdx.x * kSlots + threadIdx.x / (Lanes * kSide), l = threadIdx.x % Lanes, side = threadIdx.x / Lanes % kSide;
     if (slot >= a.slots) return;
+    constexpr int kStep = Vec ? 1 : Lanes;
+    const uint32_t l0 = kStep == 1 ? l * 8 : l;  // this thread's first column of 8 Lanes
     float* const part = a.parts + (uint64_t)slot * a.cols;
-    const auto dx_of = [&](const Eight<Vec, T>& dy, const Eight<Vec, T>& h, const Eight<Vec, T>& dh, const float (&g)[8], float f, float along) SLLM_INLINE {
-        Eight<Vec, T> dx;
+    const auto dx_of = [&](const Eight<Vec, T, kStep>& dy, const Eight<Vec, T, kStep>& h, const Eight<Vec, T, kStep>& dh, const float (&g)[8], float f, float along) SLLM_INLINE {
+        Eight<Vec, T, kStep> dx;
 #pragma unroll
         for (int i = 0; i < 8; ++i) dx.e[i] = from_f32<T>(to_f32(dh.e[i]) + f * (to_f32(dy.e[i]) * g[i] - to_f32(h.e[i]) * f * along));
         return dx;
     };
     const auto load_dh = [&](uint64_t row, uint64_t c) SLLM_INLINE {
-        Eight<Vec, T> dh;
+        Eight<Vec, T, kStep> dh;
 #pragma unroll
         for (int i = 0; i < 8; ++i) dh.e[i] = (T)0.0f;
         if (a.dh) dh.load(static_cast<const T*>(a.dh) + row * a.dh_stride, c, a.cols);
@@ -270,15 +275,15 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
     if constexpr (Held > 0) {
         float g[Held][8], sums[Held][8] = {};
 #pragma unroll
-        for (int i = 0; i < Held; ++i) load_gain<Vec>(a.gain, a.gain_dtype, (i * Lanes + l) * 8, a.cols, g[i]);
+        for (int i = 0; i < Held; ++i) load_gain<Vec, kStep>(a.gain, a.gain_dtype, i * Lanes * 8 + l0, a.cols, g[i]);
         for (uint64_t row = (uint64_t)slot * kSide + side; row < a.rows; row += (uint64_t)a.slots * kSide) {
             const float f = a.inverse[row];
-            Eight<Vec, T> dy[Held], h[Held], dh[Held];
+            Eight<Vec, T, kStep> dy[Held], h[Held], dh[Held];
 #pragma unroll
             for (int i = 0; i < Held; ++i) {
-                dy[i].load(static_cast<const T*>(a.dy) + row * a.dy_stride, (i * Lanes + l) * 8, a.cols);
-                h[i].load(static_cast<const T*>(a.h) + row * a.h_stride, (i * Lanes + l) * 8, a.cols);
-                dh[i] = load_dh(row, (i * Lanes + l) * 8);
+                dy[i].load(static_cast<const T*>(a.dy) + row * a.dy_stride, i * Lanes * 8 + l0, a.cols);
+                h[i].load(static_cast<const T*>(a.h) + row * a.h_stride, i * Lanes * 8 + l0, a.cols);
+                dh[i] = load_dh(row, i * Lanes * 8 + l0);
             }
             float dot = 0;
 #pragma unroll
@@ -292,7 +297,7 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
             const float along = row_sum<Lanes>(dot, waves) / (float)a.cols;
 #pragma unroll
             for (int i = 0; i < Held; ++i)
-                dx_of(dy[i], h[i], dh[i], g[i], f, along).store(static_cast<T*>(a.dx) + row * a.dx_stride, (i * Lanes + l) * 8, a.cols);
+                dx_of(dy[i], h[i], dh[i], g[i], f, along).store(static_cast<T*>(a.dx) + row * a.dx_stride, i * Lanes * 8 + l0, a.cols);
         }
         if constexpr (kSide > 1) {
             // rows of a wave, then the waves
@@ -313,32 +318,32 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
         for (int i = 0; i < Held; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if ((i * Lanes + l) * 8 + e < a.cols) part[(i * Lanes + l) * 8 + e] = sums[i][e];
+                if (i * Lanes * 8 + l0 + e * kStep < a.cols) part[i * Lanes * 8 + l0 + e * kStep] = sums[i][e];
     } else {
         for (uint64_t row = slot; row < a.rows; row += a.slots) {
             const float f = a.inverse[row];
             const T *dy_row = static_cast<const T*>(a.dy) + row * a.dy_stride, *h_row = static_cast<const T*>(a.h) + row * a.h_stride;
             float dot = 0;
-            for (uint64_t c = l * 8; c < a.cols; c += Lanes * 8) {
-                Eight<Vec, T> dy, h;
+            for (uint64_t c = l0; c < a.cols; c += Lanes * 8) {
+                Eight<Vec, T, kStep> dy, h;
                 float g[8];
                 dy.load(dy_row, c, a.cols);
                 h.load(h_row, c, a.cols);
-                load_gain<Vec>(a.gain, a.gain_dtype, c, a.cols, g);
+                load_gain<Vec, kStep>(a.gain, a.gain_dtype, c, a.cols, g);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float d = to_f32(dy.e[e]) * (to_f32(h.e[e]) * f);
                     dot += d * g[e];
-                    if (c + e < a.cols) part[c + e] = (row == slot ? 0.0f : part[c + e]) + d;
+                    if (c + e * kStep < a.cols) part[c + e * kStep] = (row == slot ? 0.0f : part[c + e * kStep]) + d;
                 }
             }
             const float along = row_sum<Lanes>(dot, waves) / (float)a.cols;
-            for (uint64_t c = l * 8; c < a.cols; c += Lanes * 8) {
-                Eight<Vec, T> dy, h;
+            for (uint64_t c = l0; c < a.cols; c += Lanes * 8) {
+                Eight<Vec, T, kStep> dy, h;
                 float g[8];
                 dy.load(dy_row, c, a.cols);
                 h.load(h_row, c, a.cols);
-                load_gain<Vec>(a.gain, a.gain_dtype, c, a.cols, g);
+                load_gain<Vec, kStep>(a.gain, a.gain_dtype, c, a.cols, g);
                 dx_of(dy, h, load_dh(row, c), g, f, along).store(static_cast<T*>(a.dx) + row * a.dx_stride, c, a.cols);
             }
         }
