@@ -29,6 +29,17 @@ struct Eight {
             for (int i = 0; i < 8; ++i) e[i] = c + i * Step < cols ? row[c + i * Step] : (T)0.0f;
         }
     }
+    // The same without a condition on a load, where the compiler waits for those one by one: in
+    // the gradients, of 16 bits (8191 x 5121 in bf16: 334 us, 112 so; float 136, 147 so; the norm
+    // itself 90 and 163, since what is past the end is then read too).
+    __device__ __forceinline__ void load_all(const T* row, uint64_t c, uint64_t cols) {
+        if (Vec || sizeof(T) == 4) return load(row, c, cols);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const T v = row[min(c + i * Step, cols - 1)];
+            e[i] = c + i * Step < cols ? v : (T)0.0f;
+        }
+    }
     __device__ __forceinline__ void store(T* row, uint64_t c, uint64_t cols) const {
         if (Vec) {
             u32x4 raw[sizeof(T) / 2];
@@ -269,7 +280,7 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
         Eight<Vec, T, kStep> dh;
 #pragma unroll
         for (int i = 0; i < 8; ++i) dh.e[i] = (T)0.0f;
-        if (a.dh) dh.load(static_cast<const T*>(a.dh) + row * a.dh_stride, c, a.cols);
+        if (a.dh) dh.load_all(static_cast<const T*>(a.dh) + row * a.dh_stride, c, a.cols);
         return dh;
     };
     if constexpr (Held > 0) {
@@ -281,8 +292,8 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
             Eight<Vec, T, kStep> dy[Held], h[Held], dh[Held];
 #pragma unroll
             for (int i = 0; i < Held; ++i) {
-                dy[i].load(static_cast<const T*>(a.dy) + row * a.dy_stride, i * Lanes * 8 + l0, a.cols);
-                h[i].load(static_cast<const T*>(a.h) + row * a.h_stride, i * Lanes * 8 + l0, a.cols);
+                dy[i].load_all(static_cast<const T*>(a.dy) + row * a.dy_stride, i * Lanes * 8 + l0, a.cols);
+                h[i].load_all(static_cast<const T*>(a.h) + row * a.h_stride, i * Lanes * 8 + l0, a.cols);
                 dh[i] = load_dh(row, i * Lanes * 8 + l0);
             }
             float dot = 0;
@@ -327,8 +338,8 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
             for (uint64_t c = l0; c < a.cols; c += Lanes * 8) {
                 Eight<Vec, T, kStep> dy, h;
                 float g[8];
-                dy.load(dy_row, c, a.cols);
-                h.load(h_row, c, a.cols);
+                dy.load_all(dy_row, c, a.cols);
+                h.load_all(h_row, c, a.cols);
                 load_gain<Vec, kStep>(a.gain, a.gain_dtype, c, a.cols, g);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -341,8 +352,8 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
             for (uint64_t c = l0; c < a.cols; c += Lanes * 8) {
                 Eight<Vec, T, kStep> dy, h;
                 float g[8];
-                dy.load(dy_row, c, a.cols);
-                h.load(h_row, c, a.cols);
+                dy.load_all(dy_row, c, a.cols);
+                h.load_all(h_row, c, a.cols);
                 load_gain<Vec, kStep>(a.gain, a.gain_dtype, c, a.cols, g);
                 dx_of(dy, h, load_dh(row, c), g, f, along).store(static_cast<T*>(a.dx) + row * a.dx_stride, c, a.cols);
             }
