@@ -400,13 +400,16 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             asm volatile("" : "+v"(at));  // not to be found out before this is reached
             uint32_t from, n_seen;
             seen_rows(min(at, key1), from, n_seen);
+            n_seen = min(n_seen, max(row_end, from) - from);  // rows past the end have another's statistics
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const bool seen = r0 + 8 * (i / 4) + 4 * h + i % 4 - from < n_seen;
                 s[i] = seen ? s[i] : 0.0f, dp[i] = seen ? dp[i] : 0.0f;
             }
-            bad = any_not_finite<T, D, kTile>(dout) | any_not_finite<T, D, kTile>(q);
-            out_of_sight |= bad;
+            if constexpr (!Far) {  // (far rows are seen, or zeros)
+                bad = any_not_finite<T, D, kTile>(dout) | any_not_finite<T, D, kTile>(q);
+                out_of_sight |= bad;
+            }
         }
         if constexpr (kHalf) {
             range.fit(acc_k, dp);
@@ -448,8 +451,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         barrier();
         if (r0 + kTile < row_end) stage(r0 + kTile, next_q, next_o, next_l, next_d);
         if constexpr (Far) {
-            // every sink is seen, other keys' sums are not kept, and rows past the end are zeros
-            if (wave_key0 < sinks) tile(r0, q, o, l, d, false);
+            // every sink is seen, and other keys' sums are not kept
+            if (wave_key0 < sinks) tile(r0, q, o, l, d, r0 + kTile > row_end);
             return;
         }
         const uint32_t ta = r0 / a.group, tb = (min(r0 + kTile, row_end) - 1) / a.group;
