@@ -17,6 +17,13 @@ constexpr int tile_rows() {
     return sizeof(T) == 4 ? 32 : 64;
 }
 
+// A logarithm of a row's sum past this, to the base of two, is not enough to tell the row's weights:
+// in 32 bits, rounded four times on its way, it is off by up to 2^-22 of itself, and so are
+// they.  Such rows' largest score and the sum against it are found again, one product more (32 heads
+// of 128 elements, 8192 tokens in four sequences, a window of 1024, bf16, every row so: 700 us and 797;
+// rows that are not pay 1 % for the choice).
+constexpr float kFar = 0x1p9f;
+
 // Gradients of scores, in float16, times a power of two that a column keeps to itself and
 // lowers where a larger one comes: they may be of any size, and float16 has few.
 struct Range {
@@ -40,7 +47,7 @@ struct Range {
     }
 };
 
-// With p = exp(scale s - lse) and dp = dout v^T: ds = p (dp - delta), delta = dout . out of
+// With p = exp(scale s - lse), rows far from zero apart, and dp = dout v^T: ds = p (dp - delta), delta = dout . out of
 // a row, and dq = scale ds k.  As the forward pass: a row's statistics are its lane's.
 //
 // Three products of a tile, one of them twice, since ds is rounded: 32 heads of 128 elements,
@@ -71,6 +78,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     const int32_t at0 = (int32_t)(min(wave_row, rows - 1) / a.group) - lo, at1 = (int32_t)(min(wave_row + 31, rows - 1) / a.group) - lo;
     const uint64_t packed = piece.first + token;
     Operand8<T> q[kSteps], dout[kSteps];
+    const float scale = a.scale * kLog2e;
+    float lse = a.lse[packed * a.heads + q_head] * kLog2e, less = 0;  // p = 2^(scale (s - less) - lse)
     // delta by the instructions that make dp, in their order: where a row sees one key, and
     // out is its value, ds is zero
     float delta = 0;
@@ -90,7 +99,13 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         const f32x2 both = both_halves(delta);  // zero in the half that has none
         delta = both[0] + both[1];
     }
-    const float lse = a.lse[packed * a.heads + q_head] * kLog2e, scale = a.scale * kLog2e;
+    const bool far = __builtin_fabsf(lse) > kFar && __builtin_fabsf(lse) < __builtin_inff();
+    __shared__ bool wave_far[kWaves];
+    const bool some_far = __any(far);
+    if (lane == 0) wave_far[wave] = some_far;
+    __syncthreads();
+    const bool any_far = wave_far[0] | wave_far[1] | wave_far[2] | wave_far[3];
+    static_assert(kWaves == 4, "");
 
     const bool repeats = Vec && a.dim == D && max(a.k_token, a.v_token) < (1u << 24);
     LaneOffsets<T, D, kKeys, kWaves> k_at, v_at;
@@ -127,9 +142,40 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         }
     };
     const uint32_t rows_at = rows_from<T, D>(lane), columns_at = columns_from<T, D>(lane);
-    const auto weigh = [&](f32x16& s, const f32x16& dp, int32_t i0, bool masked) SLLM_INLINE {
+    if (any_far) {
+        Reference<float> ref;
+        float sum = 0;
+        each_tile([&](int32_t i0, const uint8_t* k, const uint8_t*, bool masked) SLLM_INLINE {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -lse)) * (dp[i] - delta);
+            for (int n = 0; n < kKeys / 32; ++n) {
+                RowFragments<T, D> f;
+                f.read(k, rows_at, 32 * n);
+                f32x16 s = f.times(q);
+                if (masked) {
+                    const KeyList::Sight here = sight.here();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = here.sees(i0 + 32 * n + 8 * (i / 4) + 4 * (int32_t)h + i % 4) ? s[i] : -__builtin_inff();
+                }
+                float top = s[0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+                const f32x2 tops = both_halves(top);
+                sum *= ref.raise(fmaxf(ref.most, fmaxf(tops[0], tops[1])), scale);
+                const float finite = ref.finite();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum += ref.weight(s[i], scale, finite);
+            }
+        });
+        const f32x2 sums = both_halves(sum);
+        if (far) less = ref.most, lse = __builtin_amdgcn_logf(sums[0] + sums[1]);
+        barrier();  // the tiles have been read
+    }
+    const auto weigh = [&](f32x16& s, const f32x16& dp, int32_t i0, bool masked, auto any_less) SLLM_INLINE {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float near = decltype(any_less)::value ? s[i] - less : s[i];
+            s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(near, scale, -lse)) * (dp[i] - delta);
+        }
         if (masked) {
             const KeyList::Sight here = sight.here();
 #pragma unroll
@@ -150,7 +196,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
                 f.read(k, rows_at, 32 * n);
                 f32x16 s = f.times(q);
                 f.read(v, rows_at, 32 * n);
-                weigh(s, f.times(dout), i0 + 32 * n, masked);
+                weigh(s, f.times(dout), i0 + 32 * n, masked, std::true_type());
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sum += s[i];
             }
@@ -162,6 +208,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     if (h == 0 && wave_row + c < rows) {
         a.rows[packed * a.heads + q_head] = lse;
         a.rows[(uint64_t)a.tokens * a.heads + packed * a.heads + q_head] = delta;
+        a.rows[(uint64_t)a.tokens * a.heads * 2 + packed * a.heads + q_head] = less;
     }
 
     f32x16 acc[kParts];
@@ -169,7 +216,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     for (int d = 0; d < kParts; ++d) acc[d] = f32x16{};
     Range range;
     bool out_of_sight = false;  // something was taken out
-    const auto tile = [&](int32_t i0, const uint8_t* k, const uint8_t* v, bool masked) SLLM_INLINE {
+    const auto tile = [&](int32_t i0, const uint8_t* k, const uint8_t* v, bool masked, auto any_less) SLLM_INLINE {
         RowFragments<T, D> kf, vf;
         ColumnFragments<T, D, 32> cf;
         const bool bad = masked && any_not_finite<T, D, kKeys>(k);
@@ -184,7 +231,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             cf.read(k, columns_at, 32 * n, 0);
             const f32x16 dp = vf.times(dout);
             phase();
-            weigh(s, dp, i0 + 32 * n, masked);
+            weigh(s, dp, i0 + 32 * n, masked, any_less);
             if constexpr (kHalf) {
                 range.fit(acc, s);
                 s *= range.up;
@@ -209,7 +256,11 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             }
         }
     };
-    each_tile(tile);
+    // (two loops: to take `less` from all scores costs 3 % where it is zero)
+    if (any_far)
+        each_tile([&](int32_t i0, const uint8_t* k, const uint8_t* v, bool masked) SLLM_INLINE { tile(i0, k, v, masked, std::true_type()); });
+    else
+        each_tile([&](int32_t i0, const uint8_t* k, const uint8_t* v, bool masked) SLLM_INLINE { tile(i0, k, v, masked, std::false_type()); });
     if (out_of_sight)
         for (int32_t i = 0; i < keys.total; ++i)
             put_back<T, D>(acc, static_cast<const T*>(a.k) + head * a.k_head + (uint64_t)(piece.first + (uint32_t)(i < keys.sinks ? i : lo + i - keys.sinks)) * a.k_token,
@@ -256,7 +307,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     constexpr bool kHalf = __is_same(T, _Float16), kTwice = sizeof(T) == 2;
     constexpr uint32_t kBytes = kTile * RowTile<T, D>::kPitch;
     __shared__ __align__(16) uint8_t q0[kBytes], o0[kBytes], q1[kBytes], o1[kBytes];
-    __shared__ __align__(16) uint8_t l0[256], d0[256], l1[256], d1[256];  // rows' lse and delta
+    __shared__ __align__(16) uint8_t l0[256], d0[256], e0[256], l1[256], d1[256], e1[256];  // rows' lse, delta and less
     __shared__ __align__(16) uint8_t values[kRows * RowTile<T, D>::kPitch];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t c = lane & 31, h = lane >> 5;
@@ -315,11 +366,11 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         o_at.set(tokens * a.dout_token, [&](uint32_t r) SLLM_INLINE { return place(a.dout_token, a.dout_head, r); });
     }
     const uint32_t heads0 = head * a.group;
-    const auto stage = [&](uint32_t r0, uint8_t* q, uint8_t* dout, uint8_t* lse, uint8_t* delta) SLLM_INLINE {
-        if (wave < 2) {
+    const auto stage = [&](uint32_t r0, uint8_t* q, uint8_t* dout, uint8_t* lse, uint8_t* delta, uint8_t* less) SLLM_INLINE {
+        if (wave < 3) {
             const uint32_t row = min(r0 + lane % kTile, row_end - 1), token = row / a.group;
-            const float* p = a.rows + (wave ? (uint64_t)a.tokens * a.heads : 0);
-            load_word_to_lds(p + (uint64_t)(piece.first + token) * a.heads + heads0 + row - token * a.group, wave ? delta : lse, 0);
+            const float* p = a.rows + wave * (uint64_t)a.tokens * a.heads;
+            load_word_to_lds(p + (uint64_t)(piece.first + token) * a.heads + heads0 + row - token * a.group, wave == 0 ? lse : wave == 1 ? delta : less, 0);
         }
         if (repeats && r0 + kTile <= row_end) {
             const uint64_t token = piece.first + r0 / a.group;
@@ -343,7 +394,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
     for (int d = 0; d < kParts; ++d) acc_k[d] = acc_v[d] = f32x16{};
     Range range;
     bool out_of_sight = false;  // something was taken out
-    const auto tile = [&](uint32_t r0, const uint8_t* q, const uint8_t* dout, const uint8_t* lse, const uint8_t* delta, bool masked) SLLM_INLINE {
+    const auto tile = [&](uint32_t r0, const uint8_t* q, const uint8_t* dout, const uint8_t* lse, const uint8_t* delta, const uint8_t* less,
+                          bool masked) SLLM_INLINE {
         // places of fragments are made anew each time: kept, they would take what sums need
         uint32_t here = threadIdx.x;
         asm volatile("" : "+v"(here));
@@ -365,7 +417,9 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         f32x16 s = {}, dp = {};
         Run run;
         ColumnFragments<T, D, 32> oc, qc;
+        const float one_less = lds_read<float>(less, (here & 31) * 4);
         read(run, 0);
+        const bool some_far = __any(one_less != 0);
         __builtin_amdgcn_s_setprio(1);
         phase();
 #pragma unroll
@@ -386,6 +440,13 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
             if (i + 2 < kSteps) run = next;
         }
         __builtin_amdgcn_s_setprio(0);
+        if (some_far)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 e = lds_read<f32x4>(less, h * 16 + 8 * g * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[4 * g + i] -= e[i];
+            }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const f32x4 l = lds_read<f32x4>(lse, h * 16 + 8 * g * 4), de = lds_read<f32x4>(delta, h * 16 + 8 * g * 4);
@@ -445,27 +506,27 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         }
         __builtin_amdgcn_s_setprio(0);
     };
-    const auto step = [&](uint32_t r0, const uint8_t* q, const uint8_t* o, const uint8_t* l, const uint8_t* d, uint8_t* next_q, uint8_t* next_o,
-                          uint8_t* next_l, uint8_t* next_d) SLLM_INLINE {
+    const auto step = [&](uint32_t r0, const uint8_t* q, const uint8_t* o, const uint8_t* l, const uint8_t* d, const uint8_t* e, uint8_t* next_q,
+                          uint8_t* next_o, uint8_t* next_l, uint8_t* next_d, uint8_t* next_e) SLLM_INLINE {
         wait_but_loads<0>();
         barrier();
-        if (r0 + kTile < row_end) stage(r0 + kTile, next_q, next_o, next_l, next_d);
+        if (r0 + kTile < row_end) stage(r0 + kTile, next_q, next_o, next_l, next_d, next_e);
         if constexpr (Far) {
             // every sink is seen, and other keys' sums are not kept
-            if (wave_key0 < sinks) tile(r0, q, o, l, d, r0 + kTile > row_end);
+            if (wave_key0 < sinks) tile(r0, q, o, l, d, e, r0 + kTile > row_end);
             return;
         }
         const uint32_t ta = r0 / a.group, tb = (min(r0 + kTile, row_end) - 1) / a.group;
         const bool all = ta >= wave_key1 && r0 + kTile <= row_end && (tb - wave_key0 < window || wave_key1 < sinks);
-        if (!(tb < wave_key0 || (wave_key0 >= sinks && ta >= wave_key1 + window))) tile(r0, q, o, l, d, !all);
+        if (!(tb < wave_key0 || (wave_key0 >= sinks && ta >= wave_key1 + window))) tile(r0, q, o, l, d, e, !all);
     };
     if (row_first < row_end)
-        stage(row_first, q0, o0, l0, d0);
+        stage(row_first, q0, o0, l0, d0, e0);
     else
         wait_but_loads<0>();  // those of the values
     for (uint32_t r0 = row_first; r0 < row_end; r0 += 2 * kTile) {
-        step(r0, q0, o0, l0, d0, q1, o1, l1, d1);
-        if (r0 + kTile < row_end) step(r0 + kTile, q1, o1, l1, d1, q0, o0, l0, d0);
+        step(r0, q0, o0, l0, d0, e0, q1, o1, l1, d1, e1);
+        if (r0 + kTile < row_end) step(r0 + kTile, q1, o1, l1, d1, e1, q0, o0, l0, d0, e0);
     }
     if (out_of_sight) {
         uint32_t seen_from, n_seen;
@@ -575,7 +636,7 @@ struct Room {
 };
 Room room_of(const AttentionGradArgs& a) {
     Room r;
-    r.parts = ((uint64_t)a.tokens * a.heads * 8 + 15) / 16 * 16;
+    r.parts = ((uint64_t)a.tokens * a.heads * 12 + 15) / 16 * 16;
     r.far = r.parts + (a.splits > 1 ? ((uint64_t)a.splits * a.tokens * a.kv_heads * a.dim * 8 + 15) / 16 * 16 : 0);
     r.bytes = r.far + (a.far ? a.far + 1ull : 0) * a.far_rows * a.kv_heads * a.dim * 8;
     return r;

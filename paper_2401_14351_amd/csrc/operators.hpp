@@ -134,7 +134,7 @@ struct AttentionGradArgs : AttentionArgs {  // out is read
     uint64_t dout_token = 0, dout_head = 0;
     void *dq = nullptr, *dk = nullptr, *dv = nullptr;
     uint64_t dq_token = 0, dq_head = 0, dk_token = 0, dk_head = 0, dv_token = 0, dv_head = 0;
-    float* rows = nullptr;  // tokens x heads, twice
+    float* rows = nullptr;  // tokens x heads, three times
     uint32_t splits = 1;    // of the rows that see a key
     float* parts = nullptr;
     // what rows behind the window give to sinks: in so many parts, rows of sinks in each, by

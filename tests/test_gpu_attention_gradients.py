@@ -6,7 +6,8 @@ import math
 import numpy as np
 import pytest
 
-from tests.test_gpu_attention import TYPES, check, host, normal
+from oracle import layer_oracle as O
+from tests.test_gpu_attention import FLUSH, TYPES, UNIT, assert_within, check, host, normal
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -53,3 +54,57 @@ def test_a_sink_of_minus_infinity(dtype):
     _, dk, dv = torch.autograd.grad(op.attention(*leaves, window=40, sinks=3), leaves, dout)
     assert not dk[1].any() and not dv[1].any()
     assert torch.isfinite(dk).all() and torch.isfinite(dv).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("power", [8, 10, 17, 20, 24, 29])
+@pytest.mark.parametrize("order", ["up", "down", "only", "below"])
+@pytest.mark.parametrize("window,sinks", [(None, 0), (100, 3)])
+def test_gradients_of_scores_far_from_zero(dtype, power, order, window, sinks):
+    """Scores of a large power of two, either sign, and something small, which 32 bits hold exactly.
+
+    A row's weights against its largest score then have exponents below 127 that are exact but for the product with
+    log2 e (2^-24 of it, twice), and a sum that divides them whose logarithm is off by 2^-23 of at most 9: less than
+    2^-15 of a weight.  Logarithms of rows' sums up to 2^9 go through 32 bits, with four roundings: less than 2^-13.  Beyond
+    that the output, of which delta is made, is off by half a step of its weights and of itself, and weights are rounded
+    to the type."""
+    n, heads, kv, dim = 301, 3, 1, 64
+    u, e = UNIT[dtype], 2.0 ** -24
+    step = max(2.0 ** (power - 23), 2.0 ** -4)
+    x = normal((n,), torch.float32, 5)
+    x = (x / step).round() * step if power < 24 else torch.zeros_like(x)
+    third = torch.arange(n, device="cuda") * 3 // n - 1.0  # -1, 0, 1
+    sign = {"up": third, "down": -third, "only": torch.ones_like(third), "below": -torch.ones_like(third)}[order]
+    q, k = torch.zeros(n, heads, dim, device="cuda"), torch.zeros(n, kv, dim, device="cuda")
+    q[..., 0], q[..., 1] = 2.0 ** (power // 2), 1
+    k[..., 0], k[..., 1] = (sign * 2.0 ** (power - power // 2))[:, None], x[:, None]
+    q, k, v, dout = q.to(dtype), k.to(dtype), normal((n, kv, dim), dtype, 7), normal((n, heads, dim), dtype, 8, 0.01)
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    got = torch.autograd.grad(op.attention(*leaves, window=window, sinks=sinks, scale=1.0), leaves, dout)
+
+    Q, K, V, D = (host(t) for t in (q, k, v, dout))
+    seen = O.visible(range(n), range(n), window, sinks)
+    want = [[np.zeros(t.shape), np.zeros(t.shape)] for t in (Q, K, V)]
+    w = 2.0 ** -13
+    sums = 4 * (heads * n + 16) * e
+    for h in range(heads):
+        g = h * kv // heads
+        out, p, _ = O.attend(Q[:, h], K[:, g], V[:, g], seen, 1.0)
+        e_out = (u + w + sums) * (p @ np.abs(V[:, g])) + u * np.abs(out) + FLUSH
+        dp, delta = D[:, h] @ V[:, g].T, (D[:, h] * out).sum(1, keepdims=True)
+        ds = np.where(seen, p * (dp - delta), 0.0)
+        e_dp = 2 * (dim + 8) * e * (np.abs(D[:, h]) @ np.abs(V[:, g]).T + (np.abs(D[:, h]) * np.abs(out)).sum(1, keepdims=True)) + \
+            (np.abs(D[:, h]) * e_out).sum(1, keepdims=True)
+        # (float16's ds are times a power of two that a row or key keeps: 2^-36 of the largest for the small)
+        small = 2.0 ** -36 * (dtype == torch.float16)
+        e_ds = np.where(seen, p * e_dp + np.abs(ds) * (u + w + 8 * e) + FLUSH, 0.0)
+        e_q, e_k = e_ds + small * np.abs(ds).max(1, keepdims=True), e_ds + small * np.abs(ds).max(0, keepdims=True)
+        for i, (value, bound) in enumerate(((ds @ K[:, g], e_q @ np.abs(K[:, g]) + sums * (np.abs(ds) @ np.abs(K[:, g]))),
+                                            (ds.T @ Q[:, h], e_k.T @ np.abs(Q[:, h]) + sums * (np.abs(ds).T @ np.abs(Q[:, h]))),
+                                            (p.T @ D[:, h], ((u + w + sums) * p).T @ np.abs(D[:, h]) +
+                                             (FLUSH + 2.0 ** -40) * (seen.T @ np.abs(D[:, h]))))):
+            to = h if i == 0 else g
+            want[i][0][:, to] += value
+            want[i][1][:, to] += bound
+    for name, t, (value, bound) in zip(("dq", "dk", "dv"), got, want):
+        assert_within(t, value, bound, dtype, name)
