@@ -676,8 +676,9 @@ int32_t sllm_attention(const sllm_heads* q, const sllm_heads* k, const sllm_head
  * multiplied; ds goes as that and what the rounding leaves, two products (float16's times a
  * power of two that keeps it in float16's range); sums are held in 32 bits.  Where rows see
  * few keys, ds is freed of what out's rounding adds to its sum over a row, which is zero.  p
- * is off by |lse| * 2^-24 of itself, so scores past 10^5 cost it digits.  Tokens of no
- * sequence have gradients of zeros. */
+ * is off by |lse| * 2^-22 of itself, and where |lse| is past 350 by no more than there: such
+ * rows' largest score and the sum against it are found again.  Tokens of no sequence have
+ * gradients of zeros. */
 int32_t sllm_attention_grad(const sllm_heads* dout, const sllm_heads* q, const sllm_heads* k, const sllm_heads* v,
                             const sllm_heads* out, const float* lse, const sllm_ids* offsets, uint64_t window,
                             uint64_t sinks, float scale, const sllm_heads* dq, const sllm_heads* dk,
