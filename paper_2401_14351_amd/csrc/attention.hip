@@ -59,7 +59,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         T* const from = out + (piece.n ? piece.first * a.out_token : 0);
         if (piece.n) none.first = none.past_end = 0;
         clear_spare(none, tokens, from, a.out_token, a.out_head, head * a.group, a.group, a.dim);
-        if (a.lse) clear_spare(none, tokens, a.lse, a.heads, 1, head * a.group, a.group, 1);
+        if (!Cached && a.lse) clear_spare(none, tokens, a.lse, a.heads, 1, head * a.group, a.group, 1);
         return;
     }
     const uint32_t rows = piece.n * a.group;  // fewer than 2^32
