@@ -67,19 +67,19 @@ def stacked(*parts: torch.Tensor) -> operators.Mx4:
 
 
 def rotate(x, first: int):
-    """Rotary positions from ``first`` on: x is (tokens, heads, HEAD)."""
+    """Rotary positions from ``first`` on: x is (tokens, heads, HEAD), the result in 32 bits."""
     angle = torch.arange(first, first + x.shape[0], device=x.device, dtype=torch.float32)[:, None, None] \
         * torch.pow(10000.0, -torch.arange(0, HEAD, 2, device=x.device, dtype=torch.float32) / HEAD)
     a, b = x[..., :HEAD // 2].float(), x[..., HEAD // 2:].float()
-    return torch.cat([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], -1).to(x.dtype)
+    return torch.cat([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], -1)
 
 
 class Cache:
-    """The keys and values of one sequence, layer by layer, and how many tokens it has had."""
+    """The keys and values of one sequence, layer by layer, in 32 bits, and how many tokens it has had."""
 
     def __init__(self, model: "Decoder"):
         window = model.window or 4096
-        self.layers = [operators.KvCache.empty(1, model.kv_heads, HEAD, window, model.sinks, dtype=model.dtype, device=model.table.device)
+        self.layers = [operators.KvCache.empty(1, model.kv_heads, HEAD, window, model.sinks, dtype=torch.float32, device=model.table.device)
                        for _ in model.layers]
         self.past, self.room = 0, None if model.window else window
 
@@ -111,11 +111,11 @@ class Decoder:
         return operators.mx4_linear(x, w, out_dtype=self.dtype)
 
     def attention(self, qkv, cache, layer: int):
-        """Causal attention of the new tokens over the cache's and themselves."""
+        """Causal attention of the new tokens over the cache's and themselves, in 32 bits."""
         kv = self.kv_heads * HEAD
         q, k, v = (y.unflatten(-1, (-1, HEAD)) for y in qkv.split([self.dim, kv, kv], -1))
         past = cache.past if cache else 0
-        q, k = rotate(q, past), rotate(k, past)
+        q, k, v = rotate(q, past), rotate(k, past), v.float()
         if cache is None:
             out = operators.attention(q, k, v, window=self.window, sinks=self.sinks)
         else:
@@ -123,7 +123,7 @@ class Decoder:
             offsets = None if n == 1 else torch.tensor([0, n], dtype=torch.int32, device=qkv.device)
             lengths = torch.tensor([past], dtype=torch.int64, device=qkv.device)
             out = operators.attention_cached(q, k, v, cache.layers[layer], lengths, offsets=offsets)
-        return out.flatten(1)
+        return out.flatten(1).to(self.dtype)
 
     def logits(self, tokens, cache=None, mx4: bool = False, table=None, bits=None):
         """(tokens, vocab); ``cache`` is a :class:`Cache`; ``bits`` (4 or 8, or ``mx4``) is what

@@ -1,0 +1,47 @@
+"""The decoder example's attention in 32 bits, over a cache."""
+
+import pytest
+
+from tests.test_gpu_decoder_window import example, text, views  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.mark.parametrize("window,sinks", [(None, 0), (9, 2)])
+def test_attention_in_32_bits(example, views, window, sinks):  # noqa: F811
+    """Of activations in 16 bits: rotated queries and keys and weights are not rounded to them, the result once.
+
+    Sums of 64 and of 40 terms in 32 bits, their exponents below 16, angles below 40 radians: 2^-14 of the largest."""
+    model = example.Decoder(views, torch.bfloat16, window, sinks)
+    n, head = 40, example.HEAD
+    qkv = torch.randn(n, model.dim + 2 * head, device="cuda", generator=torch.Generator("cuda").manual_seed(3)).to(torch.bfloat16)
+    with torch.no_grad():
+        got = model.attention(qkv, None, 0).double().cpu()
+    q, k, v = (t.unflatten(-1, (-1, head)).transpose(0, 1) for t in qkv.double().cpu().split([model.dim, head, head], -1))
+    angle = torch.arange(n, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, head, 2, dtype=torch.float64) / head)
+
+    def rotate(x):
+        a, b = x[..., :head // 2], x[..., head // 2:]
+        return torch.cat([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], -1)
+
+    i, j = torch.arange(n)[:, None], torch.arange(n)
+    seen = (j <= i) & ((i - j < (window or n)) | (j < sinks))
+    s = (rotate(q) @ rotate(k).transpose(1, 2) * head ** -0.5).masked_fill(~seen, -float("inf"))
+    want = (torch.softmax(s, -1) @ v).transpose(0, 1).flatten(1)
+    assert ((got - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -14 * want.abs().max()).all()
+
+
+def test_a_cache_in_32_bits(example, views, monkeypatch):  # noqa: F811
+    """And so is what is kept of a text whose activations have 16 bits."""
+    seen = []
+
+    def attention_cached(q, k, v, cache, *args, **kwargs):
+        seen.extend(t.dtype for t in (q, k, v, cache.k, cache.v))
+        return attend(q, k, v, cache, *args, **kwargs)
+
+    attend = example.operators.attention_cached
+    monkeypatch.setattr(example.operators, "attention_cached", attention_cached)
+    model = example.Decoder(views, torch.bfloat16)
+    assert len(model.answer(text(30), 3)) == 3
+    assert len(seen) == 3 * 3 * 5 and set(seen) == {torch.float32}
