@@ -78,10 +78,21 @@ class Cache:
     """The keys and values of one sequence, layer by layer, in 32 bits, and how many tokens it has had."""
 
     def __init__(self, model: "Decoder"):
-        window = model.window or 4096
-        self.layers = [operators.KvCache.empty(1, model.kv_heads, HEAD, window, model.sinks, dtype=torch.float32, device=model.table.device)
-                       for _ in model.layers]
-        self.past, self.room = 0, None if model.window else window
+        self.past, self.room, self.grows = 0, model.window or 1, not model.window
+        self.layers = [self._empty(model) for _ in model.layers]
+
+    def _empty(self, model: "Decoder"):
+        return operators.KvCache.empty(1, model.kv_heads, HEAD, self.room, model.sinks, dtype=torch.float32, device=model.table.device)
+
+    def reserve(self, model: "Decoder", n: int):
+        """Room for n tokens more: a window's is all there ever is, and without one the layers grow."""
+        if not self.grows or self.past + n <= self.room:
+            return
+        self.room = max(self.past + n, 2 * self.room)
+        for i, old in enumerate(self.layers):
+            new = self.layers[i] = self._empty(model)
+            for to, held in ((new.k, old.k), (new.v, old.v)):
+                to[:, :, :self.past] = held[:, :, :self.past]  # none has gone round: position p is in slot p
 
 
 class Decoder:
@@ -114,7 +125,7 @@ class Decoder:
         """Causal attention of the new tokens over the cache's and themselves, in 32 bits."""
         kv = self.kv_heads * HEAD
         q, k, v = (y.unflatten(-1, (-1, HEAD)) for y in qkv.split([self.dim, kv, kv], -1))
-        past = cache.past if cache else 0
+        past = 0 if cache is None else cache.past
         q, k, v = rotate(q, past), rotate(k, past), v.float()
         if cache is None:
             out = operators.attention(q, k, v, window=self.window, sinks=self.sinks)
@@ -129,8 +140,8 @@ class Decoder:
         """(tokens, vocab); ``cache`` is a :class:`Cache`; ``bits`` (4 or 8, or ``mx4``) is what
         activations have in products."""
         bits = 4 if mx4 else bits
-        if cache and cache.room is not None and cache.past + len(tokens) > cache.room:
-            raise ValueError(f"without a window a sequence has at most {cache.room} tokens")
+        if cache is not None:
+            cache.reserve(self, len(tokens))
         x = operators.embedding(self.table if table is None else table, tokens)
         new = None  # what the layer before has added
 
@@ -146,7 +157,7 @@ class Decoder:
             new = self.product(a, l["out"], bits)
             gate, up = self.product(norm(l["norm2"]), l["gate_up"], bits).chunk(2, -1)
             new = self.product(torch.nn.functional.silu(gate) * up, l["down"], bits)
-        if cache:
+        if cache is not None:
             cache.past += len(tokens)
         return self.product(norm(self.norm), self.head, bits)
 

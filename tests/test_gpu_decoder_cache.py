@@ -45,3 +45,25 @@ def test_a_cache_in_32_bits(example, views, monkeypatch):  # noqa: F811
     model = example.Decoder(views, torch.bfloat16)
     assert len(model.answer(text(30), 3)) == 3
     assert len(seen) == 3 * 3 * 5 and set(seen) == {torch.float32}
+
+
+@pytest.mark.parametrize("sinks", [0, 3])
+def test_a_cache_grows(example, views, sinks):  # noqa: F811
+    """Without a window a text has as many tokens as its caller likes: 4200 in pieces, as at once.
+
+    In 32 bits: sums of up to 2000 terms by matrices and of 4200 by attention, twice in three layers, are off by less than
+    2 (2000 + 3 * 2 * 4200) 2^-24 < 2^-8 of the largest logit."""
+    tokens = text(4200)
+    model = example.Decoder(views, torch.float32, None, sinks)
+    with torch.no_grad():
+        want = model.logits(tokens)
+        cache, got, at = example.Cache(model), [], 0
+        for n in (1, 1, 700, 1, 3390, 1, 1, 1, 1, 103):
+            got.append(model.logits(tokens[at:at + n], cache))
+            at += n
+    assert at == 4200 and (torch.cat(got) - want).abs().max() <= 2.0 ** -8 * want.abs().max()
+
+
+def test_an_answer_past_4096_tokens(example, views):  # noqa: F811
+    model = example.Decoder(views)
+    assert model.answer(text(4094), 6).shape == (6,)
