@@ -79,6 +79,7 @@ class Cache:
 
     def __init__(self, model: "Decoder"):
         self.past, self.room, self.grows = 0, model.window or 1, not model.window
+        self.lengths = torch.zeros(1, dtype=torch.int64, device=model.table.device)
         self.layers = [self._empty(model) for _ in model.layers]
 
     def _empty(self, model: "Decoder"):
@@ -93,6 +94,10 @@ class Cache:
             new = self.layers[i] = self._empty(model)
             for to, held in ((new.k, old.k), (new.v, old.v)):
                 to[:, :, :self.past] = held[:, :, :self.past]  # none has gone round: position p is in slot p
+
+    def advance(self, n: int):
+        self.past += n
+        self.lengths += n
 
 
 class Decoder:
@@ -121,7 +126,7 @@ class Decoder:
             x = (operators.mx4_quantize if bits == 4 else operators.mx8_quantize)(x)
         return operators.mx4_linear(x, w, out_dtype=self.dtype)
 
-    def attention(self, qkv, cache, layer: int):
+    def attention(self, qkv, cache, layer: int, offsets=None):
         """Causal attention of the new tokens over the cache's and themselves, in 32 bits."""
         kv = self.kv_heads * HEAD
         q, k, v = (y.unflatten(-1, (-1, HEAD)) for y in qkv.split([self.dim, kv, kv], -1))
@@ -130,18 +135,18 @@ class Decoder:
         if cache is None:
             out = operators.attention(q, k, v, window=self.window, sinks=self.sinks)
         else:
-            n = len(qkv)
-            offsets = None if n == 1 else torch.tensor([0, n], dtype=torch.int32, device=qkv.device)
-            lengths = torch.tensor([past], dtype=torch.int64, device=qkv.device)
-            out = operators.attention_cached(q, k, v, cache.layers[layer], lengths, offsets=offsets)
+            out = operators.attention_cached(q, k, v, cache.layers[layer], cache.lengths, offsets=offsets)
         return out.flatten(1).to(self.dtype)
 
     def logits(self, tokens, cache=None, mx4: bool = False, table=None, bits=None):
         """(tokens, vocab); ``cache`` is a :class:`Cache`; ``bits`` (4 or 8, or ``mx4``) is what
         activations have in products."""
         bits = 4 if mx4 else bits
+        n, offsets = len(tokens), None
         if cache is not None:
-            cache.reserve(self, len(tokens))
+            cache.reserve(self, n)
+            if n != 1:  # where the new tokens start and end, made on the GPU
+                offsets = torch.arange(2, dtype=torch.int32, device=tokens.device) * n
         x = operators.embedding(self.table if table is None else table, tokens)
         new = None  # what the layer before has added
 
@@ -153,12 +158,12 @@ class Decoder:
             return y
 
         for i, l in enumerate(self.layers):
-            a = self.attention(self.product(norm(l["norm1"]), l["qkv"], bits), cache, i)
+            a = self.attention(self.product(norm(l["norm1"]), l["qkv"], bits), cache, i, offsets)
             new = self.product(a, l["out"], bits)
             gate, up = self.product(norm(l["norm2"]), l["gate_up"], bits).chunk(2, -1)
             new = self.product(torch.nn.functional.silu(gate) * up, l["down"], bits)
         if cache is not None:
-            cache.past += len(tokens)
+            cache.advance(n)
         return self.product(norm(self.norm), self.head, bits)
 
     def answer(self, prompt, n: int, mx4_prompt: bool = False, bits=None):

@@ -67,3 +67,17 @@ def test_a_cache_grows(example, views, sinks):  # noqa: F811
 def test_an_answer_past_4096_tokens(example, views):  # noqa: F811
     model = example.Decoder(views)
     assert model.answer(text(4094), 6).shape == (6,)
+
+
+def test_steps_wait_for_nothing(example, views):  # noqa: F811
+    """A prompt's pieces and single tokens copy nothing from the host and read nothing back."""
+    model = example.Decoder(views, window=20, sinks=2)
+    tokens = text(64)
+    with torch.no_grad():
+        torch.cuda.set_sync_debug_mode("error")
+        try:
+            cache = example.Cache(model)
+            for n in (30, 1, 1, 5):
+                model.logits(tokens[:n], cache)
+        finally:
+            torch.cuda.set_sync_debug_mode("default")
