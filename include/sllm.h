@@ -661,7 +661,7 @@ typedef struct sllm_heads {
  * Scores, their running maximum and sum, and the output's sums are held in 32 bits;
  * weights are rounded to the dtype before they are multiplied with values, as the largest
  * weight of a row so far, or up to 2^8 times that, is one.  What a query does not see does
- * not count, infinities and NaN included.  scale is a positive number.
+ * not count, infinities and NaN included.  scale is a positive number up to 2.3e38.
  *
  * lse, if not NULL: tokens x heads floats, the logarithm of the sum of exp(scale * q . key)
  * over the keys seen (zero for tokens of no sequence), for the gradient. */

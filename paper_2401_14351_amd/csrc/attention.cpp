@@ -71,7 +71,9 @@ int32_t common_args(const sllm_heads* q, const sllm_heads* k, const sllm_heads* 
     if (q->heads && (!k->heads || q->heads % k->heads))
         return fail(SLLM_E_INVAL, "%llu heads do not share %llu heads of keys", (unsigned long long)q->heads, (unsigned long long)k->heads);
     if (!q->heads && k->heads) return fail(SLLM_E_INVAL, "no heads for %llu heads of keys", (unsigned long long)k->heads);
-    if (!(scale > 0) || !std::isfinite(scale)) return fail(SLLM_E_INVAL, "scale %g is not a positive number", scale);
+    // (weights are powers of two: the kernels take it times log2 e, in 32 bits)
+    if (!(scale > 0) || !std::isfinite(scale * 1.4426950408889634f))
+        return fail(SLLM_E_INVAL, "scale %g is not a positive number up to 2.3e38", scale);
     a->q = q->data, a->q_token = q->token_stride, a->q_head = q->head_stride;
     a->k = k->data, a->k_token = k->token_stride, a->k_head = k->head_stride;
     a->v = v->data, a->v_token = v->token_stride, a->v_head = v->head_stride;
