@@ -100,12 +100,12 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         delta = both[0] + both[1];
     }
     const bool far = __builtin_fabsf(lse) > kFar && __builtin_fabsf(lse) < __builtin_inff();
-    __shared__ bool wave_far[kWaves];
-    const bool some_far = __any(far);
+    __shared__ uint32_t wave_far[kWaves];
+    const uint32_t some_far = __any(far);
     if (lane == 0) wave_far[wave] = some_far;
     __syncthreads();
-    const bool any_far = wave_far[0] | wave_far[1] | wave_far[2] | wave_far[3];
     static_assert(kWaves == 4, "");
+    const bool any_far = __builtin_amdgcn_readfirstlane(wave_far[0] | wave_far[1] | wave_far[2] | wave_far[3]);
 
     const bool repeats = Vec && a.dim == D && max(a.k_token, a.v_token) < (1u << 24);
     LaneOffsets<T, D, kKeys, kWaves> k_at, v_at;
@@ -168,6 +168,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         });
         const f32x2 sums = both_halves(sum);
         if (far) less = ref.most, lse = __builtin_amdgcn_logf(sums[0] + sums[1]);
+        wait_but_loads<0>();
         barrier();  // the tiles have been read
     }
     const auto weigh = [&](f32x16& s, const f32x16& dp, int32_t i0, bool masked, auto any_less) SLLM_INLINE {
@@ -203,6 +204,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void atte
         });
         const f32x2 sums = both_halves(sum);
         delta += sums[0] + sums[1];
+        wait_but_loads<0>();
         barrier();  // the tiles have been read
     }
     if (h == 0 && wave_row + c < rows) {
