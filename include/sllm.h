@@ -488,7 +488,8 @@ int32_t sllm_close(sllm_ckpt* h);
  * the other uses, workspaces included.  The same inputs give the same bytes.
  *
  * Buffers are memory of HIP device `device`, each inside one allocation.  An
- * output overlaps no other buffer of its call.  A buffer of no bytes may be
+ * output overlaps no other buffer of its call, a buffer being all from its first
+ * byte to its last, with what lies between its rows.  A buffer of no bytes may be
  * NULL.  Sums are held in 32-bit floats and rounded once, to nearest even, to
  * the output's type.
  *
@@ -618,7 +619,8 @@ int32_t sllm_mx_octet_dequantize(const sllm_mx* src, const sllm_matrix* dst, int
 /* h = x + residual, rounded to their dtype, and y = h / sqrt(mean h^2 + eps) * gain, the mean
  * over a row's columns.  x, residual, h and y are of one shape and dtype, gain is one row of
  * any dtype; residual and h are both NULL or both not: h is x where there is none.  eps is
- * not negative.  inverse, if not NULL: each row's 1 / sqrt(mean h^2 + eps), for the gradient. */
+ * not negative, and where it is 0 a row's root mean square is 2^-127 at least: its inverse has
+ * to fit 32 bits.  inverse, if not NULL: each row's 1 / sqrt(mean h^2 + eps), for the gradient. */
 int32_t sllm_rms_norm(const sllm_matrix* x, const sllm_matrix* residual, const sllm_matrix* gain, float eps,
                       const sllm_matrix* h, const sllm_matrix* y, float* inverse, int32_t device, void* stream);
 

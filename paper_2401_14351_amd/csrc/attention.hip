@@ -29,14 +29,16 @@ constexpr int key_tile() {
 // the first.
 //
 // Bound by the matrix cores and the vector units in turn: of long texts (64 heads of 128
-// elements that share 8, 16384 tokens, a window of 4096, bf16) 1.92 to 1.98 ms, 0.97 to 1.0
-// PF/s where the library's large products reach 1.4; the matrix cores are busy 47 % of the
-// cycles, the vector units 42 %, LDS 24 % without conflicts.  Two workgroups a CU, since a
+// elements that share 8, 16384 tokens, a window of 4096, bf16) 1.91 to 1.99 ms in a row, 0.97 to
+// 1.0 PF/s (each from an idle GPU 2.04 to 2.17), where the library's large products reach 1.4;
+// the matrix cores are busy 47 % of the cycles, the vector units 42 %, LDS 24 % without
+// conflicts.  In 32 bits 85 TF/s of 154 (packed texts, as below).  Two workgroups a CU, since a
 // wave takes 240 registers, hide each other's loads; tiles of 64 keys keep the registers so
 // (32 in 32 bits).  Making the scores of the next 32 keys beside the weights of these was
 // slower (2253 us to 2012, and 8191 tokens in 32 heads, a window of 1024, 234 to 187): the
 // compiler needs the registers.  8191 tokens in five sequences take 162 us, 0.59 PF/s: 69
-// pieces of 32 heads, of which each starts and ends alone.
+// pieces of 32 heads for 512 places, 4.3 rounds, the last a third full, of which each piece
+// starts and ends alone.
 template <typename T, int D, bool Vec, bool Cached>
 __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void attention_rows(AttentionArgs a) {
     constexpr int kKeys = key_tile<T>(), kSteps = D / 16, kParts = D / 32;

@@ -51,9 +51,10 @@ struct Range {
 // a row, and dq = scale ds k.  As the forward pass: a row's statistics are its lane's.
 //
 // Three products of a tile, one of them twice, since ds is rounded: 32 heads of 128 elements,
-// 8192 tokens in four sequences, a window of 1024, bf16: 312 to 339 us, the matrix cores busy 34 %
-// of the cycles, the vector units 30 %.  17 rounds of workgroups at two a CU, of which each
-// waits for its first tiles, leave 1.5 waves a SIMD.
+// 8192 tokens in four sequences, a window of 1024, bf16: 314 to 344 us, the matrix cores busy 34 %
+// of the cycles, the vector units 31 %.  2176 workgroups at two a CU are 4.25 rounds, of which each
+// workgroup starts with a wait for its first tiles and the last has three places in four
+// empty: 1.6 waves a SIMD.
 template <typename T, int D, bool Vec>
 __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void attention_grad_q(AttentionGradArgs a) {
     constexpr int kKeys = tile_rows<T>(), kSteps = D / 16, kParts = D / 32;

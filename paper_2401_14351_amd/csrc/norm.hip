@@ -255,7 +255,7 @@ struct NormGradArgs {
 // With f = 1 / sqrt(mean h^2 + eps) and s = dy gain: dx = dh + f (s - h f^2 mean(s h)), and
 // the gain's gradient is the sum over rows of dy h f.  h only comes with its f, as the norm,
 // whose elements are of ordinary size whatever the row's are.  Bound by memory (8191 x 5120 in
-// bf16, 252 MB with no dh: 63 to 69 us; 16384 x 8192 161, 5.0 TB/s).  `Lanes` threads
+// bf16, 336 MB: 63 to 74 us; 16384 x 8192 161, 5.0 TB/s).  `Lanes` threads
 // take a row at a time, of every `slots`-th row, and keep their columns' sums; where a row
 // is too long for that the sums are kept in memory.  Short rows are taken by a workgroup side
 // by side, which adds up their sums.
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(Lanes < 256 ? 256 : Lanes) void rms_norm_grad(NormG
     }
 }
 
-// The slots' sums, in their order: 32 runs of slots side by side, then those (768 x 5120: 4.3 us).
+// The slots' sums, in their order: 32 runs of slots side by side, then those (512 x 5120: 4.0 us).
 template <typename G>
 __global__ __launch_bounds__(1024) void join_gain(const float* parts, uint32_t slots, uint64_t cols, G* out) {
     constexpr uint32_t kRuns = 32, kCols = 32;

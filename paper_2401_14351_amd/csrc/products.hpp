@@ -354,7 +354,7 @@ int32_t launch_narrow(const NarrowArgs& a, uint32_t tile, uint32_t splits, void*
 int32_t launch_mx8(const NarrowArgs& a, uint32_t tile, uint32_t splits, void* out, uint32_t out_dtype, hipStream_t stream);
 constexpr uint32_t kNarrowStep = 512;  // depth whose scales are loaded together
 
-// At most 32 rows of x in MX FP4 (x_scales set), 16 in MX FP8 (x_fp8 too) and other types.
+// At most 32 rows of x in MX FP4 (x_scales set) and MX FP8 (x_fp8 too), 16 in other types.
 struct SkinnyArgs {
     const void* x;
     const uint8_t* x_scales;
