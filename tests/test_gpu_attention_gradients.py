@@ -11,7 +11,7 @@ from tests.test_gpu_attention import FLUSH, TYPES, UNIT, assert_within, check, h
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
-from paper_2401_14351_amd import operators as op  # noqa: E402
+from paper_2401_14351_amd import binding, operators as op  # noqa: E402
 
 
 @pytest.fixture(autouse=True)
@@ -108,3 +108,53 @@ def test_gradients_of_scores_far_from_zero(dtype, power, order, window, sinks):
             want[i][1][:, to] += bound
     for name, t, (value, bound) in zip(("dq", "dk", "dv"), got, want):
         assert_within(t, value, bound, dtype, name)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths,heads,kv,dim,window,sinks", [([150, 0, 70, 301], 6, 2, 33, None, 0), ([500], 8, 1, 128, 60, 2),
+                                                               ([700, 3], 2, 2, 80, 20, 1), ([40] * 9, 40, 1, 16, 7, 3)])
+def test_layouts_of_scores_far_from_zero(lengths, heads, kv, dim, window, sinks, dtype):
+    """Scores of about 1500 that differ by tens, as those of ordinary size: within the bounds that these have by size."""
+    q, k, v, dout = shifted(lengths, heads, kv, dim, dtype, 1500.0)
+    check(q, k, v, lengths, window, sinks, dtype, dout=dout)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("window,sinks", [(None, 0), (50, 2), (2, 0)])
+def test_rows_beside_one_far_from_zero(dtype, window, sinks):
+    """A row of large scores changes its own gradient and its keys', no other row's, by not one bit.
+
+    By the gradients' entry point, the other rows' outputs and sums being the same: the output's own rows are rounded
+    against a largest weight that may be up to 2^8, and when it is taken anew depends on their neighbours."""
+    n, heads, kv, dim = 300, 4, 2, 64
+    q, k, v, dout = (normal((n, h, dim), dtype, i) for i, h in enumerate((heads, kv, kv, heads)))
+    L, scale, at = binding.lib(), dim ** -0.5, 133
+    rows = lambda *tensors: [op._heads(t, "t") for t in tensors]  # noqa: E731
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def forward(q):
+        out, lse = torch.empty_like(q), torch.empty(n, heads, device="cuda")
+        binding.check(L.sllm_attention(*rows(q, k, v), None, window or 0, sinks, scale, *rows(out), lse.data_ptr(), 0, stream))
+        return out, lse
+
+    def gradients(q, out, lse):
+        grads = [torch.empty_like(t) for t in (q, k, v)]
+        size = op._workspace(L.sllm_attention_grad_workspace, *rows(q, k), None, window or 0, sinks)
+        ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+        binding.check(L.sllm_attention_grad(*rows(dout, q, k, v, out), lse.data_ptr(), None, window or 0, sinks, scale, *rows(*grads),
+                                            ws.data_ptr(), size, 0, stream))
+        return grads
+
+    out, lse = forward(q)
+    clean = gradients(q, out, lse)
+    far = q.clone()
+    far[at] *= 3000
+    far_out, far_lse = forward(far)
+    assert (far_lse[at].abs() > 1000).any()
+    out[at], lse[at] = far_out[at], far_lse[at]
+    got = gradients(far, out, lse)
+    rest = [i for i in range(n) if i != at]
+    assert torch.equal(got[0][rest], clean[0][rest]) and all(torch.isfinite(t).all() for t in got)
+    hidden = [j for j in range(n) if j > at or (window is not None and at - j >= window and j >= sinks)]
+    for i in (1, 2):
+        assert torch.equal(got[i][hidden], clean[i][hidden])
